@@ -1,7 +1,8 @@
 """n-softsync parameter-server update (arXiv 1511.05950) as sm_100a CUDA kernels behind a C ABI.
 
-`binding` loads libsoftsync_ps.so and mirrors its entry points; everything it exports is reachable
-from this package (`paper_1511_05950_b200.ParameterServer`, `.ps_create`, ...).  The binding is
+`binding` loads libsoftsync_ps.so and mirrors its entry points; `learn` holds the operators for language-model learners and
+their server (losses from logits, gradient norm, AdamW).  Everything the two export is reachable
+from this package (`paper_1511_05950_b200.ParameterServer`, `.AdamW`, `.ps_create`, ...).  The binding is
 loaded on first use, so that `paper_1511_05950_b200.build` can be imported to build the library
 first; using anything else without the built library raises (there is no CPU fallback).
 """
@@ -16,7 +17,10 @@ def __getattr__(name):
     binding = importlib.import_module(".binding", __name__)
     if name == "binding":
         return binding
-    try:
-        return getattr(binding, name)
-    except AttributeError:
-        raise AttributeError("module %r has no attribute %r" % (__name__, name)) from None
+    learn = importlib.import_module(".learn", __name__)
+    if name == "learn":
+        return learn
+    for module in (learn, binding):
+        if hasattr(module, name):
+            return getattr(module, name)
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

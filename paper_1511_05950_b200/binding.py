@@ -52,7 +52,33 @@ EXPORTS = (
     "ps_push_gradient", "ps_push_gradient_host", "ps_acquire_slot", "ps_push_slot", "ps_release_slot", "ps_apply_update", "ps_flush", "ps_synchronize",
     "ps_get_update_log", "ps_peek_state", "ps_export_state", "ps_import_state", "ps_kernel_time", "ps_last_cuda_error", "ps_status_string",
     "ps_fused_update_static", "ps_bind_weight_replicas",
+    "ps_tensors_sizes", "ps_tensors_create", "ps_tensors_destroy", "ps_tensors_bind_adamw", "ps_grad_norm", "ps_adamw_step",
+    "ps_adamw_moments", "ps_loss_workspace", "ps_token_logprob", "ps_policy_loss", "ps_preference_loss",
 )
+
+
+# ---- structures of include/softsync_learn.h -----------------------------------
+PS_STATE_BLOCK, PS_LIST_MAX_GRADS = 256, 256
+
+
+class AdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64)]
+
+
+class Logits(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("dtype", C.c_int), ("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64),
+                ("tokens_dev", C.c_void_p), ("weights_dev", C.c_void_p), ("temperature", C.c_float)]
+
+
+class PolicyInputs(C.Structure):
+    _fields_ = [("old_logp_dev", C.c_void_p), ("advantages_dev", C.c_void_p), ("ref_logp_dev", C.c_void_p),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float), ("entropy_coef", C.c_float)]
+
+
+class PreferenceInputs(C.Structure):
+    _fields_ = [("offsets_dev", C.c_void_p), ("ref_logp_dev", C.c_void_p), ("pairs", C.c_int64),
+                ("beta", C.c_float), ("label_smoothing", C.c_float)]
 
 
 class SoftsyncError(RuntimeError):
@@ -105,6 +131,17 @@ def _load() -> C.CDLL:
         "ps_last_cuda_error": [vp],
         "ps_status_string": [i32],
         "ps_fused_update_static": [vp, vp, i64, C.POINTER(vp), C.POINTER(f32), i32, f32, f32, i32, i32, vp, C.POINTER(i32)],
+        "ps_tensors_sizes": [i32, vp, C.POINTER(i64), C.POINTER(i64)],
+        "ps_tensors_create": [C.POINTER(vp), i32, vp, vp, i64, vp],
+        "ps_tensors_destroy": [vp],
+        "ps_tensors_bind_adamw": [vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp],
+        "ps_grad_norm": [vp, vp, i32, vp, i32, f32, vp, vp],
+        "ps_adamw_step": [vp, vp, i32, vp, i32, C.POINTER(AdamwConfig), vp, vp],
+        "ps_adamw_moments": [vp, vp, vp, vp],
+        "ps_loss_workspace": [i64, i64, C.POINTER(i64)],
+        "ps_token_logprob": [C.POINTER(Logits), vp, vp, vp, vp],
+        "ps_policy_loss": [C.POINTER(Logits), C.POINTER(PolicyInputs), vp, vp, vp, vp, i64, vp, i64, vp],
+        "ps_preference_loss": [C.POINTER(Logits), C.POINTER(PreferenceInputs), vp, vp, vp, i64, vp, i64, vp],
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -151,6 +188,17 @@ ps_export_state = lib.ps_export_state
 ps_import_state = lib.ps_import_state
 ps_last_cuda_error = lib.ps_last_cuda_error
 ps_fused_update_static = lib.ps_fused_update_static
+ps_tensors_sizes = lib.ps_tensors_sizes
+ps_tensors_create = lib.ps_tensors_create
+ps_tensors_destroy = lib.ps_tensors_destroy
+ps_tensors_bind_adamw = lib.ps_tensors_bind_adamw
+ps_grad_norm = lib.ps_grad_norm
+ps_adamw_step = lib.ps_adamw_step
+ps_adamw_moments = lib.ps_adamw_moments
+ps_loss_workspace = lib.ps_loss_workspace
+ps_token_logprob = lib.ps_token_logprob
+ps_policy_loss = lib.ps_policy_loss
+ps_preference_loss = lib.ps_preference_loss
 
 
 def status_string(status: int) -> str:

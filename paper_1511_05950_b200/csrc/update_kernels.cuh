@@ -167,7 +167,7 @@ __device__ __forceinline__ void store_mirror(unsigned short *p, const float (&x)
 }
 
 // theta -> bf16 mirror on its own (after ps_init_weights or when a mirror is bound).
-__global__ void mirror_kernel(const float *w, unsigned short *mirror, long long n)
+static __global__ void mirror_kernel(const float *w, unsigned short *mirror, long long n)
 {
     const long long stride = static_cast<long long>(gridDim.x) * blockDim.x;
     for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += stride)
