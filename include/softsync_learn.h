@@ -99,8 +99,9 @@ typedef struct ps_logits {
     float temperature;                    /* > 0 */
 } ps_logits;
 
-/* Bytes of the device workspace that the two losses need for `rows` rows and `sequences` sequences (0 for the policy loss).  It has no
- * contents between calls; calls that share one must not overlap in time. */
+/* Bytes of the device workspace that the two losses need for `rows` rows and `sequences` sequences (0 for the policy loss).  Its first
+ * four bytes must be zero before its first use; every call leaves them so, whatever its sizes, and keeps nothing else there.
+ * Calls that share a workspace must not overlap in time. */
 int ps_loss_workspace(int64_t rows, int64_t sequences, int64_t *bytes);
 
 /* logp, lse, entropy (fp32, rows each; lse and entropy may be NULL): one pass over the logits. */

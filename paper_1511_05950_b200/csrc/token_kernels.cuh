@@ -8,9 +8,7 @@
 // elements are handled one by one, so nothing outside the row is read or written.
 //
 // What bounds these kernels: HBM (bf16: 2 bytes an element for the statistics, 4 for statistics and gradient), with the
-// exponential unit close behind: it gives 16 results a clock and SM, and at 7 TB/s 12 of them are wanted in either case.  So a
-// row is read ONCE and stays in registers between its statistics and its gradient, split over a cluster of up to eight
-// blocks where one block's registers do not hold it; the blocks exchange three numbers each through distributed shared memory.
+// exponential unit close behind: it gives 16 results a clock and SM, and at 7 TB/s 12 of them are wanted in either case.
 #pragma once
 
 #include "update_kernels.cuh"
@@ -22,6 +20,8 @@ namespace softsync {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kFloor = -1e30f;          // logits below this have p = 0 beside an ordinary maximum
+constexpr unsigned kFloorBits = 0xf149f149u;
+constexpr float kFloorBf16 = -0x1.92p99f; // the same in bf16, twice in kFloorBits
 
 // Whether no product of a logit above the floor with c overflows and every logit below the floor has p = 0 beside the maximum m.
 __device__ __forceinline__ bool ordinary(float m, float c) { return fabsf(m) < 1e29f && c < 1e7f && c > 1e-20f; }
@@ -102,18 +102,22 @@ __device__ __forceinline__ float logit_at(const GradFp32 *, const unsigned char 
 __device__ __forceinline__ float logit_at(const GradBf16 *, const unsigned char *row, long long j)
 { return __uint_as_float(static_cast<unsigned>(reinterpret_cast<const unsigned short *>(row)[j]) << 16); }
 
-// A row as vectors: vector q holds the elements [q * per_vector - phase, ...) of the row.
+// A row as vectors: vector q holds the elements [q * per_vector - phase, ...) of the row; those in [inner, full) lie inside it.
 template <typename GT>
 struct RowVectors {
     const unsigned char *row;
-    int phase, vocab, count;
+    int phase, vocab, inner, full, count;
     __device__ __forceinline__ RowVectors(const unsigned char *r, int v) : row(r), vocab(v)
     {
         phase = static_cast<int>(reinterpret_cast<uintptr_t>(r) & 15) / logit_bytes<GT>();
+        inner = phase ? 1 : 0;
+        full = (phase + v) / per_vector<GT>();
         count = (phase + v + per_vector<GT>() - 1) / per_vector<GT>();
     }
     __device__ __forceinline__ int first(int q) const { return q * per_vector<GT>() - phase; }
-    __device__ __forceinline__ bool whole(int q) const { return first(q) >= 0 && first(q) + per_vector<GT>() <= vocab; }
+    __device__ __forceinline__ bool whole(int q) const { return q >= inner && q < full; }
+    __device__ __forceinline__ bool ragged() const { return phase != 0 || count != full; }
+    __device__ __forceinline__ const unsigned char *at(int q) const { return row - phase * logit_bytes<GT>() + static_cast<long long>(q) * 16; }
 };
 
 __device__ __forceinline__ uint4 load_vector16(const void *p)
@@ -123,56 +127,90 @@ __device__ __forceinline__ uint4 load_vector16(const void *p)
     return r;
 }
 
-// Vector q, minus infinity where it reaches beyond the row.
 template <typename GT>
-__device__ __forceinline__ uint4 load_row_vector(const RowVectors<GT> &v, int q)
+__device__ __forceinline__ uint4 no_vector()               // minus infinity throughout
 {
-    const int j = v.first(q);
-    if (v.whole(q)) return load_vector16(v.row + static_cast<long long>(j) * logit_bytes<GT>());
+    constexpr unsigned w = logit_bytes<GT>() == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
+
+
+// A vector that reaches beyond the row, element by element; minus infinity out there.
+template <typename GT>
+__device__ __forceinline__ uint4 load_ragged_vector(const unsigned char *row, int j, int vocab)
+{
     uint4 r;
     unsigned *w = &r.x;
     if constexpr (logit_bytes<GT>() == 4) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = j + k >= 0 && j + k < v.vocab ? reinterpret_cast<const unsigned *>(v.row)[j + k] : 0xff800000u;
+        for (int k = 0; k < 4; ++k) w[k] = j + k >= 0 && j + k < vocab ? reinterpret_cast<const unsigned *>(row)[j + k] : 0xff800000u;
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const unsigned short *h = reinterpret_cast<const unsigned short *>(v.row);
-            const unsigned lo = j + 2 * k >= 0 && j + 2 * k < v.vocab ? h[j + 2 * k] : 0xff80u;
-            const unsigned hi = j + 2 * k + 1 >= 0 && j + 2 * k + 1 < v.vocab ? h[j + 2 * k + 1] : 0xff80u;
+            const unsigned short *h = reinterpret_cast<const unsigned short *>(row);
+            const unsigned lo = j + 2 * k >= 0 && j + 2 * k < vocab ? h[j + 2 * k] : 0xff80u;
+            const unsigned hi = j + 2 * k + 1 >= 0 && j + 2 * k + 1 < vocab ? h[j + 2 * k + 1] : 0xff80u;
             w[k] = lo | hi << 16;
         }
     }
     return r;
 }
 
-// Writes vector q's values g to the row at dst; `same` says that dst has the source row's place within 16 bytes.
-template <typename GT>
-__device__ __forceinline__ void store_row_vector(const RowVectors<GT> &v, int q, unsigned char *dst, bool same, const float (&g)[per_vector<GT>()])
+// The vectors q0, q0 + T, ... of a row; minus infinity beyond its end.
+template <typename GT, int T, int NV>
+__device__ __forceinline__ void load_vectors(uint4 (&x)[NV], const RowVectors<GT> &v, int q0)
 {
-    const int j = v.first(q);
-    if (same && v.whole(q)) {
-        uint4 r;
-        if constexpr (logit_bytes<GT>() == 4) r = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-        else r = make_uint4(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7]));
-        __stcs(reinterpret_cast<uint4 *>(dst + static_cast<long long>(j) * logit_bytes<GT>()), r);
-        return;
-    }
+    const unsigned char *p = v.at(q0);
 #pragma unroll
-    for (int k = 0; k < per_vector<GT>(); ++k)
-        if (j + k >= 0 && j + k < v.vocab) {
-            if constexpr (logit_bytes<GT>() == 4) reinterpret_cast<float *>(dst)[j + k] = g[k];
-            else reinterpret_cast<unsigned short *>(dst)[j + k] = __bfloat16_as_ushort(__float2bfloat16_rn(g[k]));
-        }
+    for (int k = 0; k < NV; ++k)
+        if (v.whole(q0 + k * T)) x[k] = load_vector16(p + k * T * 16);
+        else x[k] = no_vector<GT>();
+    if (!v.ragged()) return;
+    const int d = v.full - q0;
+    if (v.count != v.full && d >= 0 && d < NV * T && d % T == 0) {
+        const uint4 end = load_ragged_vector<GT>(v.row, v.first(v.full), v.vocab);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (d == k * T) x[k] = end;
+    }
+    if (v.phase && q0 == 0) x[0] = load_ragged_vector<GT>(v.row, -v.phase, v.vocab);
 }
 
-// Zeros over a whole row (its part of `parts`), by the row's own alignment.
 template <typename GT>
-__device__ __forceinline__ void zero_row(unsigned char *dst, int vocab, int part, int parts)
+__device__ __forceinline__ uint4 pack_vector(const float (&g)[per_vector<GT>()])
+{
+    if constexpr (logit_bytes<GT>() == 4) return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+    else return make_uint4(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7]));
+}
+// A vector's elements one by one, at the row's ends.
+template <typename GT>
+__device__ __forceinline__ void store_single(unsigned char *dst, int j, int vocab, uint4 packed)
+{
+    const unsigned *w = &packed.x;
+#pragma unroll
+    for (int k = 0; k < per_vector<GT>(); ++k)
+        if (j + k >= 0 && j + k < vocab) {
+            if constexpr (logit_bytes<GT>() == 4) reinterpret_cast<unsigned *>(dst)[j + k] = w[k];
+            else reinterpret_cast<unsigned short *>(dst)[j + k] = static_cast<unsigned short>(w[k / 2] >> (16 * (k & 1)));
+        }
+}
+template <typename GT>
+__device__ __forceinline__ void store_logit(unsigned char *dst, long long j, float x)
+{
+    if constexpr (logit_bytes<GT>() == 4) reinterpret_cast<float *>(dst)[j] = x;
+    else reinterpret_cast<unsigned short *>(dst)[j] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+}
+
+// Zeros over a whole row by `threads` threads, this one number `me`, by the row's own alignment.
+template <typename GT>
+__device__ __forceinline__ void zero_row(unsigned char *dst, int vocab, int me, int threads)
 {
     const RowVectors<GT> v(dst, vocab);
-    const float zero[per_vector<GT>()] = {};
-    for (int q = part * static_cast<int>(blockDim.x) + threadIdx.x; q < v.count; q += parts * blockDim.x) store_row_vector(v, q, dst, true, zero);
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int q = me; q < v.count; q += threads) {
+        if (v.whole(q)) __stcs(reinterpret_cast<uint4 *>(dst + static_cast<long long>(v.first(q)) * logit_bytes<GT>()), zero);
+        else store_single<GT>(dst, v.first(q), vocab, zero);
+    }
 }
 
 // The elements of word k of a vector, as fp32.
@@ -205,7 +243,7 @@ __device__ __forceinline__ float2 floored_pair(const uint4 &x, int k)
     if constexpr (logit_bytes<GT>() == 4)
         return make_float2(max_nan(__uint_as_float(w[2 * k]), kFloor), max_nan(__uint_as_float(w[2 * k + 1]), kFloor));
     else
-        return unpack_bf16(max_nan_bf16x2(w[k], 0xf149f149u));          // -9.95e29 in bf16
+        return unpack_bf16(max_nan_bf16x2(w[k], kFloorBits));
 }
 template <typename GT>
 __device__ __forceinline__ float2 plain_pair(const uint4 &x, int k)
@@ -215,39 +253,67 @@ __device__ __forceinline__ float2 plain_pair(const uint4 &x, int k)
     else return unpack_bf16(w[k]);
 }
 
-// Adds the vectors' exponentials relative to the maximum m to s, and (ENTROPY) times their exponents to t.  The difference to the
-// maximum is taken before it is scaled: the maximum's own exponent is exactly zero, and a row that a mask of the type's lowest value
-// leaves nothing of stays finite (its softmax is uniform).  Beside an ordinary maximum pairs go through packed instructions and the floor
-// stands in for minus infinity; else every exponent is held above -1000.
+// The vectors' sum of exponentials relative to m and (ENTROPY) of exponentials times exponents, added to s and t.  The difference to m
+// is taken before it is scaled: m's own exponent is exactly zero, and a row that a mask of the type's lowest value leaves nothing
+// of stays finite (its softmax is uniform).  FLOOR: minus infinity, whose p = 0 times its exponent would be NaN, is held at kFloor.
+template <typename GT, int NV, bool ENTROPY, bool FLOOR>
+__device__ __forceinline__ void packed_exponentials(const uint4 (&x)[NV], float m, float c, float &s, float &t)
+{
+    const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m);
+    float2 s2 = make_float2(0.f, 0.f), t2 = s2;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int k = 0; k < per_vector<GT>() / 2; ++k) {
+            const float2 d = mul2(add2(FLOOR ? floored_pair<GT>(x[v], k) : plain_pair<GT>(x[v], k), m2), c2);
+            const float2 e = make_float2(ex2(d.x), ex2(d.y));
+            s2 = add2(s2, e);
+            if constexpr (ENTROPY) t2 = fma2(e, d, t2);
+        }
+    s += s2.x + s2.y;
+    if constexpr (ENTROPY) t += t2.x + t2.y;
+}
+// Any m, NaN and infinities included: every exponent is held above -1000.
 template <typename GT, int NV, bool ENTROPY>
-__device__ __forceinline__ void row_exponentials(const uint4 (&x)[NV], float m, float c, float &s, float &t)
+__device__ __forceinline__ void single_exponentials(const uint4 (&x)[NV], float m, float c, float &s, float &t)
+{
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int k = 0; k < per_vector<GT>() / 2; ++k) {
+            const float2 y = plain_pair<GT>(x[v], k);
+            const float a = max_nan((y.x - m) * c, -1000.f), b = max_nan((y.y - m) * c, -1000.f);
+            const float e = ex2(a), f = ex2(b);
+            s += e + f;
+            if constexpr (ENTROPY) t += e * a + f * b;
+        }
+}
+
+// Takes the vectors into a warp's running sums s, t relative to its m (kLowest to begin with).  Any value of the row serves as m as
+// long as nothing overflows, so the maximum is looked for in the first vectors alone; those that follow are added without looking,
+// and only where that meets an infinity or a NaN, or sums become large, is the maximum looked for again and the sums moved to it.
+// (Looking everywhere costs half an instruction an element, the floor another half.)
+template <typename GT, int NV, bool ENTROPY>
+__device__ __forceinline__ void add_vectors(const uint4 (&x)[NV], float c, float &m, float &s, float &t)
 {
     if (ordinary(m, c)) {
-        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m);
-        float2 s2 = make_float2(0.f, 0.f), t2 = s2;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int k = 0; k < per_vector<GT>() / 2; ++k) {
-                const float2 d = mul2(add2(ENTROPY ? floored_pair<GT>(x[v], k) : plain_pair<GT>(x[v], k), m2), c2);
-                const float2 e = make_float2(ex2(d.x), ex2(d.y));
-                s2 = add2(s2, e);
-                if constexpr (ENTROPY) t2 = fma2(e, d, t2);
-            }
-        s += s2.x + s2.y;
-        if constexpr (ENTROPY) t += t2.x + t2.y;
-    } else {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int k = 0; k < per_vector<GT>() / 2; ++k) {
-                const float2 y = plain_pair<GT>(x[v], k);
-                const float a = max_nan((y.x - m) * c, -1000.f), b = max_nan((y.y - m) * c, -1000.f);
-                const float e = ex2(a), f = ex2(b);
-                s += e + f;
-                if constexpr (ENTROPY) t += e * a + f * b;
-            }
+        float s2 = 0.f, t2 = 0.f;
+        packed_exponentials<GT, NV, ENTROPY, false>(x, m, c, s2, t2);
+        if (__all_sync(0xffffffffu, s2 < 1e30f && (!ENTROPY || fabsf(t2) < 1e30f))) {
+            s += s2;
+            if constexpr (ENTROPY) t += t2;
+            return;
+        }
     }
+    const float top = fmaxf(warp_max(vectors_max<GT, NV>(x)), m);
+    if (top > m) {
+        const float d = fmaxf((m - top) * c, -1000.f), f = ex2(d);
+        t = f * fmaf(s, d, t);
+        s *= f;
+        m = top;
+    }
+    if (ordinary(m, c)) packed_exponentials<GT, NV, ENTROPY, true>(x, m, c, s, t);
+    else single_exponentials<GT, NV, ENTROPY>(x, m, c, s, t);
 }
 
 // What multiplies the exponentials of a part with maximum m in a whole with maximum `top`.
@@ -260,27 +326,79 @@ __device__ __forceinline__ float part_factor(float m, float top, float c, float 
 // Per-row factors of the gradient: dz_j = a (1[j = token] - p_j) + b p_j (log p_j + H).
 struct RowCoef { float a, b; };
 
-// Gradient of one vector.  With d = (x - m) c - log2 s:  p = 2^d,  g = p (b ln 2 d + (b H - a)).
-template <typename GT, bool ENTROPY>
-__device__ __forceinline__ void vector_gradient(const uint4 &x, float m, float log2_sum, float c, RowCoef k, float entropy, float (&g)[per_vector<GT>()])
-{
-    const float add = ENTROPY ? fmaf(k.b, entropy, -k.a) : -k.a, mult = k.b * kLn2;
-    if (ordinary(m, c)) {
-        const float2 c2 = make_float2(c, c), mm = make_float2(-m, -m), l2 = make_float2(-log2_sum, -log2_sum), a2 = make_float2(add, add), m2 = make_float2(mult, mult);
+// What the gradient of a row's elements needs.  With d = (x - m) c - log2 s:  p = 2^d,  g = p (b ln 2 d + (b H - a)).  For bf16 the
+// exponent is x c + shift, one instruction less: the rounding of the shift is a relative error of about 1e-6 in p, lost in
+// the 2e-3 of the result's own.
+struct RowGradient {
+    float m, log2_sum, c, add, mult, one, shift;
+    __device__ __forceinline__ RowGradient(float m_, float l2, float c_, RowCoef k, float entropy)
+        : m(m_), log2_sum(l2), c(c_), add(fmaf(k.b, entropy, -k.a)), mult(k.b * kLn2), one(k.a), shift(-fmaf(m_, c_, l2)) {}
+
+    // any maximum, beside an ordinary one with the bits of the vector form; the token's own entry has `one` to be added
+    template <typename GT, bool ENTROPY>
+    __device__ __forceinline__ float single(float x) const
+    {
+        constexpr float floor = logit_bytes<GT>() == 4 ? kFloor : kFloorBf16;
+        const float y = ENTROPY ? max_nan(x, floor) : x;
+        const float d = !ordinary(m, c) ? max_nan((x - m) * c, -1000.f) - log2_sum : logit_bytes<GT>() == 2 ? fmaf(y, c, shift) : fmaf(y - m, c, -log2_sum);
+        return __fmul_rn(ex2(d), ENTROPY ? fmaf(mult, d, add) : add);
+    }
+    // beside an ordinary maximum
+    template <typename GT, bool ENTROPY>
+    __device__ __forceinline__ uint4 vector(const uint4 &x) const
+    {
+        constexpr bool kShift = logit_bytes<GT>() == 2;
+        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m), l2 = kShift ? make_float2(shift, shift) : make_float2(-log2_sum, -log2_sum);
+        const float2 a2 = make_float2(add, add), b2 = make_float2(mult, mult);
+        float g[per_vector<GT>()];
 #pragma unroll
         for (int j = 0; j < per_vector<GT>() / 2; ++j) {
-            const float2 d = fma2(add2(ENTROPY ? floored_pair<GT>(x, j) : plain_pair<GT>(x, j), mm), c2, l2);
-            const float2 p = make_float2(ex2(d.x), ex2(d.y));
-            const float2 r = mul2(p, ENTROPY ? fma2(m2, d, a2) : a2);
+            const float2 y = ENTROPY ? floored_pair<GT>(x, j) : plain_pair<GT>(x, j);
+            const float2 d = fma2(kShift ? y : add2(y, m2), c2, l2);
+            const float2 r = mul2(make_float2(ex2(d.x), ex2(d.y)), ENTROPY ? fma2(b2, d, a2) : a2);
             g[2 * j] = r.x;
             g[2 * j + 1] = r.y;
         }
-    } else {
+        return pack_vector<GT>(g);
+    }
+};
+
+// Gradient of the vectors [lo, hi) of a row, written to the row at dst by the block's T threads; `vector(q)` gives vector q, `logit(j)`
+// the row's element j.  The token's entry is written once more, with its one, by the thread that has just written it, so the order
+// of the two is certain.  Where dst lies otherwise within 16 bytes than the row, or the row's maximum is out of the
+// ordinary, the elements go one by one.
+template <typename GT, int T, int UNROLL, bool ENTROPY, typename Vector, typename Logit>
+__device__ __forceinline__ void write_gradient(const RowVectors<GT> &v, int lo, int hi, unsigned char *dst, const RowGradient &f,
+                                               long long tok, float x_tok, Vector vector, Logit logit)
+{
+    if (((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c)) {
+        unsigned char *p = dst - v.phase * logit_bytes<GT>();
+        int q = lo + threadIdx.x;
+        if (!v.ragged()) {
+            for (; q + (UNROLL - 1) * T < hi; q += UNROLL * T) {
+                uint4 x[UNROLL];
 #pragma unroll
-        for (int j = 0; j < per_vector<GT>(); ++j) {
-            const float2 y = plain_pair<GT>(x, j / 2);
-            const float d = max_nan(((j & 1 ? y.y : y.x) - m) * c, -1000.f) - log2_sum;
-            g[j] = ex2(d) * (ENTROPY ? fmaf(mult, d, add) : add);
+                for (int k = 0; k < UNROLL; ++k) x[k] = vector(q + k * T);
+#pragma unroll
+                for (int k = 0; k < UNROLL; ++k)
+                    __stcs(reinterpret_cast<uint4 *>(p + static_cast<long long>(q) * 16 + k * T * 16), f.template vector<GT, ENTROPY>(x[k]));
+            }
+        }
+        for (; q < hi; q += T) {
+            const uint4 g = f.template vector<GT, ENTROPY>(vector(q));
+            if (v.whole(q)) __stcs(reinterpret_cast<uint4 *>(p + static_cast<long long>(q) * 16), g);
+            else store_single<GT>(dst, v.first(q), v.vocab, g);
+        }
+        if (static_cast<unsigned long long>(tok) < static_cast<unsigned long long>(v.vocab)) {
+            const int at = (static_cast<int>(tok) + v.phase) / per_vector<GT>();
+            if (at >= lo && at < hi && (at - lo) % T == static_cast<int>(threadIdx.x))
+                store_logit<GT>(dst, tok, __fadd_rn(f.template single<GT, ENTROPY>(x_tok), f.one));
+        }
+    } else {
+        const int end = min(v.first(hi), v.vocab);
+        for (int j = max(v.first(lo), 0) + threadIdx.x; j < end; j += T) {
+            const float g = f.template single<GT, ENTROPY>(logit(j));
+            store_logit<GT>(dst, j, j == tok ? __fadd_rn(g, f.one) : g);
         }
     }
 }
@@ -302,17 +420,25 @@ constexpr int kMaxCluster = 8;
 struct RowShared {
     float warp[3][32];                    // each warp's m, s, t
     float part[3][kMaxCluster];           // each block's m, s, t, written by the blocks
-    float row[5];                         // m, log2 s, entropy, a, b: what every thread needs for the gradient
-    float terms[5];                       // the row's share of the policy loss's sums
+    float row[6];                         // m, log2 s, entropy, a, b, token's logit: what every thread needs for the gradient
 };
 
-// The row's m, s, t from the warps' of all its blocks, in every lane of warp 0 (the other warps get nothing).  All threads of
-// all blocks call it; between its two halves of the cluster barrier the blocks write into one another's shared memory.
-// cluster_arrive() has been called once before, so that no block writes before its peer has started.
-__device__ __forceinline__ void join_row(RowShared &sh, float c, float &m, float &s, float &t)
+// m, s, t of 32 parts, one a lane, become those of the whole in every lane.
+__device__ __forceinline__ void join_lanes(float c, float &m, float &s, float &t)
+{
+    const float top = warp_max(m);
+    float d;
+    const float f = part_factor(m, top, c, d);
+    t = warp_sum(f * fmaf(s, d, t));
+    s = warp_sum(f * s);
+    m = top;
+}
+
+// The block's m, s, t from its warps' (each warp: the same m, and s and t to be summed over its lanes), in every lane of warp 0;
+// the other warps get nothing.
+__device__ __forceinline__ void join_warps(RowShared &sh, float c, float &m, float &s, float &t)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const unsigned blocks = cluster_size();
     s = warp_sum(s);
     t = warp_sum(t);
     if (lane == 0) { sh.warp[0][warp] = m; sh.warp[1][warp] = s; sh.warp[2][warp] = t; }
@@ -321,15 +447,18 @@ __device__ __forceinline__ void join_row(RowShared &sh, float c, float &m, float
         m = lane < warps ? sh.warp[0][lane] : kLowest;
         s = lane < warps ? sh.warp[1][lane] : 0.f;
         t = lane < warps ? sh.warp[2][lane] : 0.f;
-        const float top = warp_max(m);
-        float d;
-        const float f = part_factor(m, top, c, d);
-        t = warp_sum(f * fmaf(s, d, t));
-        s = warp_sum(f * s);
-        m = top;
+        join_lanes(c, m, s, t);
     }
+}
+
+// The same over all blocks of a cluster, which write into one another's shared memory and meet at the cluster's barrier.  The blocks have
+// met once before, so that none writes before its peer has started.
+__device__ __forceinline__ void join_cluster(RowShared &sh, float c, float &m, float &s, float &t)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned blocks = cluster_size();
+    join_warps(sh, c, m, s, t);
     if (blocks == 1) return;
-    cluster_wait();                                       // every block of the row has started
     if (warp == 0 && lane < static_cast<int>(blocks)) {
         const unsigned me = cluster_rank();
         store_to_rank(&sh.part[0][me], lane, m);
@@ -342,12 +471,7 @@ __device__ __forceinline__ void join_row(RowShared &sh, float c, float &m, float
         m = lane < static_cast<int>(blocks) ? sh.part[0][lane] : kLowest;
         s = lane < static_cast<int>(blocks) ? sh.part[1][lane] : 0.f;
         t = lane < static_cast<int>(blocks) ? sh.part[2][lane] : 0.f;
-        const float top = warp_max(m);
-        float d;
-        const float f = part_factor(m, top, c, d);
-        t = warp_sum(f * fmaf(s, d, t));
-        s = warp_sum(f * s);
-        m = top;
+        join_lanes(c, m, s, t);
     }
 }
 
@@ -355,22 +479,19 @@ __device__ __forceinline__ void join_row(RowShared &sh, float c, float &m, float
 struct StatsOut {
     float *logp, *lse, *entropy;          // lse, entropy may be null
     RowStat *stat;                        // may be null
-    RowCoef *coef;                        // set to zero for the kernel that follows (may be null), and so is
-    unsigned *counter;
+    RowCoef *coef;                        // set to zero for the kernel that follows (may be null)
 };
 
 // One cluster per row; each thread holds NV vectors of a batch at a time.  A batch's maximum is taken over the whole warp before
 // any exponential, so that the running sums are rescaled once a batch and by the same factor in every lane.
-template <typename GT, int NV, bool ENTROPY>
-__global__ void __launch_bounds__(512) row_stats_kernel(const __grid_constant__ RowsIn in, const __grid_constant__ StatsOut out)
+template <typename GT, int T, int NV, bool ENTROPY>
+__global__ void __launch_bounds__(T, 1536 / T) row_stats_kernel(const __grid_constant__ RowsIn in, const __grid_constant__ StatsOut out)
 {
     __shared__ RowShared sh;
     const int blocks = cluster_size(), rank = cluster_rank();
     const long long r = blockIdx.x / static_cast<unsigned>(blocks);
-    if (rank == 0 && threadIdx.x == 0) {
-        if (out.coef) out.coef[r] = RowCoef{0.f, 0.f};
-        if (out.counter && r == 0) *out.counter = 0;
-    }
+    griddep_launch_dependents();
+    if (rank == 0 && threadIdx.x == 0 && out.coef) out.coef[r] = RowCoef{0.f, 0.f};
     if (in.weights && in.weights[r] == 0.f) {              // the whole cluster leaves
         if (rank == 0 && threadIdx.x == 0) {
             out.logp[r] = 0.f;
@@ -379,7 +500,7 @@ __global__ void __launch_bounds__(512) row_stats_kernel(const __grid_constant__ 
         }
         return;
     }
-    if (blocks > 1) cluster_arrive();
+    if (blocks > 1) { cluster_arrive(); cluster_wait(); }
     const unsigned char *row = in.data + r * in.stride * logit_bytes<GT>();
     const RowVectors<GT> v(row, static_cast<int>(in.vocab));
     long long tok = -1;
@@ -388,27 +509,13 @@ __global__ void __launch_bounds__(512) row_stats_kernel(const __grid_constant__ 
         tok = in.tokens[r];
         if (tok >= 0 && tok < in.vocab) x_tok = logit_at(static_cast<const GT *>(nullptr), row, tok);
     }
-    const int threads = blockDim.x;
     float m = kLowest, s = 0.f, t = 0.f;
-    for (int base = rank * NV * threads; base < v.count; base += blocks * NV * threads) {
+    for (int base = rank * NV * T; base < v.count; base += blocks * NV * T) {
         uint4 x[NV];
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int q = base + k * threads + threadIdx.x;
-            x[k] = q < v.count ? load_row_vector(v, q) : (logit_bytes<GT>() == 4 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u)
-                                                                                 : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u));
-        }
-        const float top = fmaxf(warp_max(vectors_max<GT, NV>(x)), m);
-        if (top > m) {
-            float d;
-            const float f = part_factor(m, top, in.scale, d);
-            t = f * fmaf(s, d, t);
-            s *= f;
-            m = top;
-        }
-        row_exponentials<GT, NV, ENTROPY>(x, m, in.scale, s, t);
+        load_vectors<GT, T, NV>(x, v, base + threadIdx.x);
+        add_vectors<GT, NV, ENTROPY>(x, in.scale, m, s, t);
     }
-    join_row(sh, in.scale, m, s, t);
+    join_cluster(sh, in.scale, m, s, t);
     if (rank || threadIdx.x) return;
     const float l2 = log2f(s);
     out.logp[r] = (x_tok - m) * in.inv_temperature - kLn2 * l2;
@@ -430,34 +537,23 @@ __global__ void __launch_bounds__(kGradThreads) row_grad_kernel(const __grid_con
     const int segment = blockIdx.x % static_cast<unsigned>(segments);
     const unsigned char *row = in.data + r * in.stride * logit_bytes<GT>();
     unsigned char *dst = out + r * out_stride * logit_bytes<GT>();
+    griddep_wait();                                        // the factors
     const RowCoef k = coef[r];
     if ((in.weights && in.weights[r] == 0.f) || (k.a == 0.f && k.b == 0.f)) {        // nothing to read: the gradient is zero
-        zero_row<GT>(dst, static_cast<int>(in.vocab), segment, segments);
+        zero_row<GT>(dst, static_cast<int>(in.vocab), segment * kGradThreads + threadIdx.x, segments * kGradThreads);
         return;
     }
     const RowVectors<GT> v(row, static_cast<int>(in.vocab));
-    uint4 x[kGradVectors];
-    const int base = segment * kGradVectors * kGradThreads + threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < kGradVectors; ++i)
-        if (base + i * kGradThreads < v.count) x[i] = load_row_vector(v, base + i * kGradThreads);
+    const int lo = segment * kGradVectors * kGradThreads, hi = min(lo + kGradVectors * kGradThreads, v.count);
     const RowStat st = stat[r];
     const float h = ENTROPY ? entropy[r] : 0.f;
     const long long tok = in.tokens[r];
-    const bool same = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0;
-#pragma unroll
-    for (int i = 0; i < kGradVectors; ++i) {
-        const int q = base + i * kGradThreads;
-        if (q >= v.count) break;
-        float g[per_vector<GT>()];
-        vector_gradient<GT, ENTROPY>(x[i], st.max, st.log2_sum, in.scale, k, h, g);
-        const long long at = tok - v.first(q);
-        if (at >= 0 && at < per_vector<GT>())
-#pragma unroll
-            for (int j = 0; j < per_vector<GT>(); ++j)
-                if (j == at) g[j] += k.a;
-        store_row_vector(v, q, dst, same, g);
-    }
+    const float x_tok = tok >= 0 && tok < in.vocab ? logit_at(static_cast<const GT *>(nullptr), row, tok) : 0.f;
+    if (out == in.data) __syncthreads();                   // in place: the token's logit is read before it is replaced
+    write_gradient<GT, kGradThreads, kGradVectors, ENTROPY>(
+        v, lo, hi, dst, RowGradient(st.max, st.log2_sum, in.scale, k, h), tok, x_tok,
+        [&](int q) { return v.whole(q) ? load_vector16(v.at(q)) : load_ragged_vector<GT>(row, v.first(q), v.vocab); },
+        [&](int j) { return logit_at(static_cast<const GT *>(nullptr), row, j); });
 }
 
 // ---- the policy loss -----------------------------------------------------------------------------------------------------
@@ -489,199 +585,367 @@ __device__ __forceinline__ PolicyTerms policy_terms(const PolicyIn &in, float ad
 }
 
 constexpr int kTermThreads = 1024;
-constexpr int kRowGroup = 64;             // rows whose terms one warp adds up
 
-struct Totals {                           // written by policy_totals_kernel, or reset by it
-    double inv_weight;                    // 1 / sum of the weights, 0 where that is 0
-    unsigned groups_done;
-};
-
-// Sum over the block, the same bits in every thread.
-__device__ __forceinline__ double block_total(double x, double *scratch)
+// Sum over the first `threads` threads of a block (all of them call it and meet at `sync`), the same bits in every thread.
+template <typename Sync>
+__device__ __forceinline__ double block_total(double x, double *scratch, int threads, Sync sync)
 {
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    __syncthreads();
+    sync();
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
-    __syncthreads();
+    sync();
     double y = 0;
-    for (int k = 0; k < static_cast<int>(blockDim.x >> 5); ++k) y += scratch[k];
+    for (int k = 0; k < threads / 32; ++k) y += scratch[k];
     return y;
 }
 
-// The sum of the weights, and zeros in the counters.  The row kernel is launched as a dependent that may start at once: it
-// needs neither before it has read its row.
-static __global__ void __launch_bounds__(kTermThreads) policy_totals_kernel(const float *weights, long long rows, Totals *totals, unsigned *group_count, int groups)
-{
-    __shared__ double scratch[kTermThreads / 32];
-    griddep_launch_dependents();
-    for (int k = threadIdx.x; k < groups; k += blockDim.x) group_count[k] = 0;
-    double sum = 0;
-    if (weights)
-        for (long long r = threadIdx.x; r < rows; r += blockDim.x) sum += weights[r];
-    sum = weights ? block_total(sum, scratch) : static_cast<double>(rows);
-    if (threadIdx.x == 0) {
-        totals->inv_weight = sum != 0.0 ? 1.0 / sum : 0.0;
-        totals->groups_done = 0;
-    }
-}
-
-struct TermsOut {
-    Totals *totals;
-    unsigned *group_count;                // rows of each group that are done
-    float (*terms)[5];                    // each row's share of the five sums
-    double (*group_sum)[5];
+struct PolicyState {
+    double *inv_weight;                   // 1 / sum of the weights, 0 where that is 0
+    unsigned *done;                       // parts whose sums are there: zero before and after a call
+    double (*part_sum)[5];                // of the rows of each cluster (or block, policy_terms_kernel)
     float *stats;
 };
 
-// Called by one whole warp once per row, with the row's terms already times its share (zeros for a row of weight zero).  The warp that
-// completes a group of kRowGroup rows adds the group up, the one that completes the last group adds the groups up: always the same
-// additions, whichever warp does them.
-__device__ __forceinline__ void count_row(const TermsOut &out, long long rows, long long r, const float (&v)[5])
+__device__ __forceinline__ double inverse_or_zero(double sum) { return sum != 0.0 ? 1.0 / sum : 0.0; }
+
+static __global__ void __launch_bounds__(kTermThreads) policy_totals_kernel(const float *weights, long long rows, double *inv_weight)
+{
+    __shared__ double scratch[kTermThreads / 32];
+    griddep_launch_dependents();
+    double sum = 0;
+    if (weights)
+        for (long long r = threadIdx.x; r < rows; r += blockDim.x) sum += weights[r];
+    sum = weights ? block_total(sum, scratch, kTermThreads, [] { __syncthreads(); }) : static_cast<double>(rows);
+    if (threadIdx.x == 0) *inv_weight = inverse_or_zero(sum);
+}
+
+// Called by one warp of each of `parts` parts of the rows, with the part's sums: the one that comes last adds the parts up in their
+// order, so the result does not depend on which one that is.
+__device__ __forceinline__ void finish_sums(const PolicyState &st, int me, int parts, const double (&sum)[5])
 {
     const int lane = threadIdx.x & 31;
-    const long long group = r / kRowGroup, groups = (rows + kRowGroup - 1) / kRowGroup;
-    const long long first = group * kRowGroup;
-    const unsigned size = static_cast<unsigned>(min(static_cast<long long>(kRowGroup), rows - first));
     unsigned before = 0;
     if (lane == 0) {
 #pragma unroll
-        for (int q = 0; q < 5; ++q) __stcg(&out.terms[r][q], v[q]);
+        for (int q = 0; q < 5; ++q) __stcg(&st.part_sum[me][q], sum[q]);
         __threadfence();
-        before = atomicAdd(out.group_count + group, 1u);
+        before = atomicInc(st.done, parts - 1);           // back to zero by the last one
     }
-    if (__shfl_sync(0xffffffffu, before, 0) + 1 != size) return;
+    if (__shfl_sync(0xffffffffu, before, 0) + 1 != static_cast<unsigned>(parts)) return;
     __threadfence();
-    double sum[5] = {};
-    for (unsigned k = lane; k < size; k += 32)
-#pragma unroll
-        for (int q = 0; q < 5; ++q) sum[q] += __ldcg(&out.terms[first + k][q]);
-#pragma unroll
-    for (int q = 0; q < 5; ++q)
-        for (int o = 16; o; o >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], o);
-    if (lane == 0) {
-#pragma unroll
-        for (int q = 0; q < 5; ++q) __stcg(&out.group_sum[group][q], sum[q]);
-        __threadfence();
-        before = atomicAdd(&out.totals->groups_done, 1u);
+#pragma unroll 1
+    for (int q = 0; q < 5; ++q) {
+        double all = 0;
+        for (int k = lane; k < parts; k += 32) all += __ldcg(&st.part_sum[k][q]);
+        for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        if (lane == 0) st.stats[q] = static_cast<float>(all);
     }
-    if (__shfl_sync(0xffffffffu, before, 0) + 1 != groups) return;
-    __threadfence();
-    double all[5] = {};
-    for (long long k = lane; k < groups; k += 32)
-#pragma unroll
-        for (int q = 0; q < 5; ++q) all[q] += __ldcg(&out.group_sum[k][q]);
-#pragma unroll
-    for (int q = 0; q < 5; ++q)
-        for (int o = 16; o; o >>= 1) all[q] += __shfl_xor_sync(0xffffffffu, all[q], o);
-    if (lane == 0)
-#pragma unroll
-        for (int q = 0; q < 5; ++q) out.stats[q] = static_cast<float>(all[q]);
 }
 
-// Statistics, loss terms and gradient (out: null for none) of a row from one read: the row's vectors stay in the registers of its
-// cluster, at most NV a thread.
-template <typename GT, int NV, bool ENTROPY_GRAD>
-__global__ void __launch_bounds__(1024) policy_row_kernel(const __grid_constant__ RowsIn in, const __grid_constant__ PolicyIn pin,
-                                                          const __grid_constant__ TermsOut terms, float *logp, float *entropy,
-                                                          unsigned char *out, long long out_stride)
+// The terms alone, from statistics already there (rows too long to stay on chip): one warp for every gridDim-th row.
+static __global__ void __launch_bounds__(32) policy_terms_kernel(const __grid_constant__ RowsIn rows, const __grid_constant__ PolicyIn in,
+                                                                 const __grid_constant__ PolicyState st, const float *logp, const float *entropy, RowCoef *coef)
 {
-    __shared__ RowShared sh;
-    const int blocks = cluster_size(), rank = cluster_rank();
-    const long long r = blockIdx.x / static_cast<unsigned>(blocks);
-    unsigned char *dst = out + r * out_stride * logit_bytes<GT>();
-    const float w = in.weights ? in.weights[r] : 1.f;
-    if (w == 0.f) {                                        // the whole cluster takes this way
-        if (rank == 0 && threadIdx.x < 32) {
-            if (threadIdx.x == 0) { logp[r] = 0.f; entropy[r] = 0.f; }
-            griddep_wait();
-            const float none[5] = {};
-            count_row(terms, in.rows, r, none);
+    const float inv_weight = static_cast<float>(*st.inv_weight);
+    double sum[5] = {};
+    for (long long r = blockIdx.x; r < rows.rows; r += gridDim.x) {
+        const float w = rows.weights ? rows.weights[r] : 1.f;
+        RowCoef k{0.f, 0.f};
+        if (w != 0.f) {
+            const PolicyTerms o = policy_terms(in, in.advantages[r], in.old_logp[r], in.ref_logp ? in.ref_logp[r] : 0.f, logp[r], entropy[r]);
+            const float share = w * inv_weight;
+            k.a = o.slope * share * rows.inv_temperature;
+            k.b = in.entropy_coef * share * rows.inv_temperature;
+            for (int q = 0; q < 5; ++q) sum[q] += static_cast<double>(share) * o.v[q];
         }
-        if (out) zero_row<GT>(dst, static_cast<int>(in.vocab), rank, blocks);
-        return;
+        if (coef && threadIdx.x == 0) coef[r] = k;
     }
-    if (blocks > 1) cluster_arrive();
-    const unsigned char *row = in.data + r * in.stride * logit_bytes<GT>();
-    const RowVectors<GT> v(row, static_cast<int>(in.vocab));
-    const int threads = blockDim.x, base = rank * NV * threads + threadIdx.x;
-    uint4 x[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int q = base + k * threads;
-        x[k] = q < v.count ? load_row_vector(v, q) : (logit_bytes<GT>() == 4 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u)
-                                                                             : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u));
+    finish_sums(st, blockIdx.x, gridDim.x, sum);
+}
+
+// ---- the policy loss, rows kept on chip -------------------------------------------------------------------------------------
+constexpr int kRingThreads = 256, kRingVectors = 4, kRingChunk = kRingThreads * kRingVectors;      // vectors of a chunk: 16 KB
+constexpr int kRingSlots = 7;             // 112 KB of shared memory: two blocks an SM
+constexpr int kRingBytes = kRingSlots * kRingChunk * 16;
+
+constexpr int kOwnTotalRows = 4096;       // up to here every block adds the weights up for itself: no kernel before this one
+
+struct RingPlan {
+    int vectors, chunks;                  // of a row, in each block of its cluster
+    int own_total;
+    int wait_limit;
+};
+
+struct RingShared {
+    float warp[3][kRingThreads / 32];
+    float part[2][3][kMaxCluster];        // each block's m, s, t by the parity of the row, written by the blocks
+    float row[6];                         // m, log2 s, entropy, a, b, token's logit
+    int tok;                              // -1 where it is out of range
+    double sums[5];                       // of the cluster's rows, kept by its first block
+    double scratch[kRingThreads / 32];
+    unsigned long long full[kRingSlots], empty[kRingSlots], exchange[2];
+};
+
+__device__ __forceinline__ void mbar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void mbar_arrive_remote(const void *mine, unsigned rank)
+{
+    unsigned addr;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_addr(mine)), "r"(rank));
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(addr) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster_bounded(unsigned bar, unsigned parity, int limit)
+{
+    for (int tries = 0; tries < limit; ++tries) {
+        unsigned ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+        if (ok) return true;
     }
-    const long long tok = in.tokens[r];
-    float x_tok = CUDART_NAN_F, adv = 0.f, old_logp = 0.f, ref_logp = 0.f;
-    if (threadIdx.x < 32) {
-        if (tok >= 0 && tok < in.vocab) x_tok = logit_at(static_cast<const GT *>(nullptr), row, tok);
-        adv = pin.advantages[r];
-        old_logp = pin.old_logp[r];
-        if (pin.ref_logp) ref_logp = pin.ref_logp[r];
-    }
-    float m = fmaxf(warp_max(vectors_max<GT, NV>(x)), kLowest), s = 0.f, t = 0.f;
-    row_exponentials<GT, NV, true>(x, m, in.scale, s, t);
-    join_row(sh, in.scale, m, s, t);
-    if (threadIdx.x < 32) {
-        const float l2 = log2f(s), h = kLn2 * (l2 - t / s);
-        const float lp = (x_tok - m) * in.inv_temperature - kLn2 * l2;
-        const PolicyTerms o = policy_terms(pin, adv, old_logp, ref_logp, lp, h);
-        griddep_wait();
-        const float share = static_cast<float>(w * __ldcg(&terms.totals->inv_weight));
-        if (threadIdx.x == 0) {
-            sh.row[0] = m; sh.row[1] = l2; sh.row[2] = h;
-            sh.row[3] = o.slope * share * in.inv_temperature;
-            sh.row[4] = pin.entropy_coef * share * in.inv_temperature;
-        }
-        if (rank == 0 && threadIdx.x == 0) {
-            logp[r] = lp;
-            entropy[r] = h;
-#pragma unroll
-            for (int q = 0; q < 5; ++q) sh.terms[q] = o.v[q] * share;
-        }
+    return false;
+}
+__device__ __forceinline__ void ring_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kRingThreads) : "memory"); }
+
+// Statistics, loss terms and gradient (out: null for none) of all rows from one read of the logits: a row is spread over the shared memory of a cluster of
+// blocks and stays there between its statistics and its gradient.  Each block has a ring of 16 KB slots that one thread of an
+// extra warp keeps filling with bulk copies, chunk after chunk and row after row; the eight other warps take a row's statistics
+// chunk by chunk as it arrives, exchange them with the cluster's other blocks, and release each slot once the chunk's
+// gradient is written, so the next row's chunks are under way long before this one is done.  Two blocks an SM: one's exchange runs
+// under the other's arithmetic.  The clusters are as many as fit the GPU, each takes every parts-th row.
+//
+// A vector at a row's ragged end comes with ordinary loads, through a register of the thread that handles it (the last thread the
+// front's, the first thread the end's: never the same one).
+//
+// Every wait is bounded.  One that runs out makes the block's later rows NaN; it waits for nothing after that, but the copying thread
+// still sees, with a limit, its last copies arrive.
+template <typename GT, bool ENTROPY_GRAD>
+__global__ void __launch_bounds__(kRingThreads + 32, 2) policy_ring_kernel(const __grid_constant__ RowsIn in, const __grid_constant__ PolicyIn pin,
+                                                                           const __grid_constant__ PolicyState st, float *logp, float *entropy,
+                                                                           unsigned char *out, long long out_stride, const __grid_constant__ RingPlan plan)
+{
+    constexpr int T = kRingThreads, NV = kRingVectors, PV = per_vector<GT>();
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ RingShared sh;
+    const int blocks = cluster_size(), rank = cluster_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int parts = gridDim.x / static_cast<unsigned>(blocks), vocab = static_cast<int>(in.vocab);
+    const long long r0 = blockIdx.x / static_cast<unsigned>(blocks);
+    const int lo = rank * plan.vectors;
+    if (tid == 0) {
+        for (int k = 0; k < kRingSlots; ++k) { mbar_init(smem_addr(&sh.full[k]), 1); mbar_init(smem_addr(&sh.empty[k]), T / 32); }
+        for (int k = 0; k < 2; ++k) mbar_init(smem_addr(&sh.exchange[k]), blocks);
+        for (int k = 0; k < 5; ++k) sh.sums[k] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    const RowCoef coef{sh.row[3], sh.row[4]};
-    m = sh.row[0];
-    const float l2 = sh.row[1], h = sh.row[2];
-    const bool same = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int q = base + k * threads;
-        if (q >= v.count || !out) break;
-        float g[per_vector<GT>()];
-        vector_gradient<GT, ENTROPY_GRAD>(x[k], m, l2, in.scale, coef, h, g);
-        const long long at = tok - v.first(q);
-        if (at >= 0 && at < per_vector<GT>())
-#pragma unroll
-            for (int j = 0; j < per_vector<GT>(); ++j)
-                if (j == at) g[j] += coef.a;
-        store_row_vector(v, q, dst, same, g);
-    }
-    if (rank == 0 && threadIdx.x < 32) {
-        const float each[5] = {sh.terms[0], sh.terms[1], sh.terms[2], sh.terms[3], sh.terms[4]};
-        count_row(terms, in.rows, r, each);
-    }
-}
+    cluster_arrive();
+    cluster_wait();                                        // every block's barriers are there
 
-// The terms alone, from statistics already there: no gradient wanted, or rows too long to stay on chip.
-static __global__ void __launch_bounds__(256) policy_terms_kernel(const __grid_constant__ RowsIn rows, const __grid_constant__ PolicyIn in,
-                                                                  const __grid_constant__ TermsOut terms, const float *logp, const float *entropy, RowCoef *coef)
-{
-    const long long r = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;      // one warp a row
-    if (r >= rows.rows) return;
-    const float w = rows.weights ? rows.weights[r] : 1.f;
-    float each[5] = {};
-    RowCoef k{0.f, 0.f};
-    if (w != 0.f) {
-        const PolicyTerms o = policy_terms(in, in.advantages[r], in.old_logp[r], in.ref_logp ? in.ref_logp[r] : 0.f, logp[r], entropy[r]);
-        const float share = static_cast<float>(w * terms.totals->inv_weight);
-        k.a = o.slope * share * rows.inv_temperature;
-        k.b = in.entropy_coef * share * rows.inv_temperature;
-        for (int q = 0; q < 5; ++q) each[q] = o.v[q] * share;
+    if (warp == T / 32) {                                  // the copying warp
+        if (lane == 0) {
+            unsigned g = 0;                                // chunks issued
+            bool late = false;
+            for (long long r = r0; r < in.rows && !late; r += parts) {
+                if (in.weights && in.weights[r] == 0.f) continue;
+                const RowVectors<GT> v(in.data + r * in.stride * logit_bytes<GT>(), vocab);
+                const int hi = min(lo + plan.vectors, v.full);
+                for (int c = 0; c < plan.chunks; ++c, ++g) {
+                    const unsigned slot = g % kRingSlots, round = g / kRingSlots;
+                    if (round && !mbar_wait_bounded(smem_addr(&sh.empty[slot]), (round - 1) & 1, plan.wait_limit)) { late = true; break; }
+                    const int from = max(lo + c * kRingChunk, v.inner), to = min(lo + (c + 1) * kRingChunk, hi), n = max(to - from, 0);
+                    mbar_expect_tx(smem_addr(&sh.full[slot]), n * 16);
+                    if (n) bulk_load(smem_addr(ring + (static_cast<size_t>(slot) * kRingChunk + (from - lo - c * kRingChunk)) * 16), v.at(from), n * 16, smem_addr(&sh.full[slot]));
+                }
+            }
+            for (unsigned k = g > kRingSlots ? g - kRingSlots : 0; k < g; ++k)      // nothing may arrive after the block has gone
+                mbar_wait_bounded(smem_addr(&sh.full[k % kRingSlots]), (k / kRingSlots) & 1, plan.wait_limit);
+        }
+        __syncwarp();
+    } else {
+        const bool head = warp == 0;
+        // what warp 0 needs beside the logits is read a row ahead: the token first, then what hangs on it
+        struct Scalars { float x_tok, adv, old_logp, ref_logp; long long tok; };
+        auto weight = [&](long long i) { return i < in.rows ? (in.weights ? in.weights[i] : 1.f) : 0.f; };
+        auto first_scalars = [&](long long i, Scalars &o) {
+            if (!head || i >= in.rows) return;
+            o.tok = in.tokens[i];
+            o.adv = pin.advantages[i];
+            o.old_logp = pin.old_logp[i];
+            o.ref_logp = pin.ref_logp ? pin.ref_logp[i] : 0.f;
+        };
+        auto token_logit = [&](long long i, float wi, Scalars &o) {
+            if (head && wi != 0.f)
+                o.x_tok = o.tok >= 0 && o.tok < in.vocab ? logit_at(static_cast<const GT *>(nullptr), in.data + i * in.stride * logit_bytes<GT>(), o.tok) : CUDART_NAN_F;
+        };
+        Scalars now = {}, then = {};
+        float w = weight(r0);
+        first_scalars(r0, now);
+        token_logit(r0, w, now);
+        float inv_weight = 0.f;
+        if (plan.own_total) {
+            double sum = in.weights ? 0.0 : static_cast<double>(in.rows);
+            if (in.weights) {
+                for (int i = tid; i < static_cast<int>(in.rows); i += T) sum += in.weights[i];
+                sum = block_total(sum, sh.scratch, T, ring_sync);
+            }
+            inv_weight = static_cast<float>(inverse_or_zero(sum));
+        } else if (head) {
+            griddep_wait();
+            inv_weight = static_cast<float>(__ldcg(st.inv_weight));
+        }
+        int slot = 0;                                      // of the row's first chunk, and the phase it is in
+        unsigned phase = 0, turn = 0;                      // turn: rows exchanged so far
+        bool late = false;
+        auto advance = [](int &k, unsigned &ph) { if (++k == kRingSlots) { k = 0; ph ^= 1; } };
+        for (long long r = r0; r < in.rows; r += parts) {
+            const float w_next = weight(r + parts);
+            first_scalars(r + parts, then);
+            unsigned char *dst = out + r * out_stride * logit_bytes<GT>();
+            if (w == 0.f) {                                // the whole cluster takes this way
+                token_logit(r + parts, w_next, then);
+                if (out) zero_row<GT>(dst, vocab, rank * T + tid, blocks * T);
+                if (rank == 0 && tid == 0) { logp[r] = 0.f; entropy[r] = 0.f; }
+                w = w_next;
+                now = then;
+                continue;
+            }
+            const RowVectors<GT> v(in.data + r * in.stride * logit_bytes<GT>(), vocab);
+            const int hi = min(lo + plan.vectors, v.full);              // vectors of the block that are in the ring: [max(lo, inner), hi)
+            uint4 edge[1];
+            int edge_q = -1;
+            if (v.ragged()) {
+                if (v.phase && v.full && lo == 0 && tid == T - 1) edge_q = 0;
+                if (v.count != v.full && v.full >= lo && v.full < lo + plan.vectors && tid == 0) edge_q = v.full;
+                edge[0] = edge_q >= 0 ? load_ragged_vector<GT>(v.row, v.first(edge_q), vocab) : no_vector<GT>();
+            }
+
+            float m = kLowest, s = 0.f, t = 0.f;
+            const bool clean = lo >= v.inner;              // no ragged front in the block's first chunk
+            int here = slot;
+            unsigned ph = phase;
+            for (int left = hi - lo, c = 0; c < plan.chunks; ++c, left -= kRingChunk) {
+                late = late || !mbar_wait_bounded(smem_addr(&sh.full[here]), ph, plan.wait_limit);
+                const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + here * kRingChunk + tid;
+                if (left > T * NV / 2) {
+                    uint4 x[NV];
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) x[k] = mine[k * T];
+                    if (left < kRingChunk)
+#pragma unroll
+                        for (int k = 0; k < NV; ++k)
+                            if (k * T + tid >= left) x[k] = no_vector<GT>();
+                    if (c == 0 && !clean && tid == 0) x[0] = no_vector<GT>();
+                    add_vectors<GT, NV, true>(x, in.scale, m, s, t);
+                } else {
+                    for (int k = 0; k * T < left; ++k) {
+                        uint4 x[1] = {no_vector<GT>()};
+                        if (k * T + tid < left && (c > 0 || k * T + tid > 0 || clean)) x[0] = mine[k * T];
+                        add_vectors<GT, 1, true>(x, in.scale, m, s, t);
+                    }
+                }
+                advance(here, ph);
+            }
+            if (v.ragged() && __any_sync(0xffffffffu, edge_q >= 0)) add_vectors<GT, 1, true>(edge, in.scale, m, s, t);
+            if (late) s = CUDART_NAN_F;
+
+            s = warp_sum(s);
+            t = warp_sum(t);
+            if (lane == 0) { sh.warp[0][warp] = m; sh.warp[1][warp] = s; sh.warp[2][warp] = t; }
+            ring_sync();
+            if (head) {
+                m = lane < T / 32 ? sh.warp[0][lane] : kLowest;
+                s = lane < T / 32 ? sh.warp[1][lane] : 0.f;
+                t = lane < T / 32 ? sh.warp[2][lane] : 0.f;
+                join_lanes(in.scale, m, s, t);
+                if (blocks > 1) {
+                    const unsigned parity = turn & 1;
+                    if (lane < blocks) {
+                        store_to_rank(&sh.part[parity][0][rank], lane, m);
+                        store_to_rank(&sh.part[parity][1][rank], lane, s);
+                        store_to_rank(&sh.part[parity][2][rank], lane, t);
+                        mbar_arrive_remote(&sh.exchange[parity], lane);
+                    }
+                    late = late || !mbar_wait_cluster_bounded(smem_addr(&sh.exchange[parity]), (turn >> 1) & 1, plan.wait_limit);
+                    m = lane < blocks ? sh.part[parity][0][lane] : kLowest;
+                    s = lane < blocks ? sh.part[parity][1][lane] : 0.f;
+                    t = lane < blocks ? sh.part[parity][2][lane] : 0.f;
+                    join_lanes(in.scale, m, s, t);
+                    if (late) s = CUDART_NAN_F;
+                }
+                const float l2 = log2f(s), h = kLn2 * (l2 - t / s);
+                const float lp = (now.x_tok - m) * in.inv_temperature - kLn2 * l2;
+                const PolicyTerms o = policy_terms(pin, now.adv, now.old_logp, now.ref_logp, lp, h);
+                const float share = w * inv_weight;
+                if (lane == 0) {
+                    sh.row[0] = m; sh.row[1] = l2; sh.row[2] = h; sh.row[5] = now.x_tok;
+                    sh.row[3] = o.slope * share * in.inv_temperature;
+                    sh.row[4] = pin.entropy_coef * share * in.inv_temperature;
+                    sh.tok = now.tok >= 0 && now.tok < in.vocab ? static_cast<int>(now.tok) : -1;
+                }
+                if (rank == 0 && lane == 0) {
+                    logp[r] = lp;
+                    entropy[r] = h;
+#pragma unroll
+                    for (int k = 0; k < 5; ++k) sh.sums[k] += static_cast<double>(share) * o.v[k];
+                }
+            }
+            ++turn;
+            ring_sync();
+            token_logit(r + parts, w_next, then);
+            const RowGradient f(sh.row[0], sh.row[1], in.scale, RowCoef{sh.row[3], sh.row[4]}, sh.row[2]);
+            const int tok = sh.tok;
+            const bool plain = ((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c);
+            unsigned char *p = dst - v.phase * logit_bytes<GT>() + static_cast<long long>(lo + tid) * 16;
+            for (int left = hi - lo, c = 0; c < plan.chunks; ++c, left -= kRingChunk) {
+                const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + slot * kRingChunk + tid;
+                if (out && plain) {
+                    if (left >= kRingChunk && (c > 0 || clean)) {
+#pragma unroll
+                        for (int k = 0; k < NV; ++k) __stcs(reinterpret_cast<uint4 *>(p + k * T * 16), f.template vector<GT, ENTROPY_GRAD>(mine[k * T]));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < NV; ++k)
+                            if (k * T + tid < left && (c > 0 || k * T + tid > 0 || clean))
+                                __stcs(reinterpret_cast<uint4 *>(p + k * T * 16), f.template vector<GT, ENTROPY_GRAD>(mine[k * T]));
+                    }
+                    p += kRingChunk * 16;
+                } else if (out) {
+                    const unsigned char *bytes = ring + slot * kRingChunk * 16;
+                    const int base = lo + c * kRingChunk, first = v.first(base), begin = v.first(max(base, v.inner)), end = v.first(min(base + kRingChunk, hi));
+                    for (int j = begin + tid; j < end; j += T) {
+                        const float x = f.template single<GT, ENTROPY_GRAD>(logit_at(static_cast<const GT *>(nullptr), bytes, j - first));
+                        store_logit<GT>(dst, j, j == tok ? __fadd_rn(x, f.one) : x);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.empty[slot]));
+                advance(slot, phase);
+            }
+            if (out && plain && tok >= 0) {                // the token's entry once more, with its one, by the thread that has just written it
+                const int q = (tok + v.phase) / PV;
+                if (q >= max(lo, v.inner) && q < hi && (q - lo) % T == tid)
+                    store_logit<GT>(dst, tok, __fadd_rn(f.template single<GT, ENTROPY_GRAD>(sh.row[5]), f.one));
+            }
+            if (out && edge_q >= 0) {                      // the row's own elements of a ragged vector
+                const int j0 = v.first(edge_q);
+                const unsigned char *bytes = reinterpret_cast<const unsigned char *>(&edge[0]);
+#pragma unroll
+                for (int k = 0; k < PV; ++k) {
+                    const int j = j0 + k;
+                    if (j < 0 || j >= vocab) continue;
+                    const float y = logit_at(static_cast<const GT *>(nullptr), bytes, k);
+                    const float x = f.template single<GT, ENTROPY_GRAD>(y);
+                    store_logit<GT>(dst, j, j == tok ? __fadd_rn(x, f.one) : x);
+                }
+            }
+            w = w_next;
+            now = then;
+        }
+        if (head && rank == 0) {
+            __syncwarp();
+            finish_sums(st, static_cast<int>(r0), parts, sh.sums);
+        }
     }
-    if (coef && (threadIdx.x & 31) == 0) coef[r] = k;
-    count_row(terms, rows.rows, r, each);
+    cluster_arrive();
+    cluster_wait();                                        // no block goes while another may write to it
 }
 
 // ---- the preference loss -----------------------------------------------------------------------------------------------------
@@ -708,6 +972,8 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
 {
     __shared__ double scratch[kPairThreads / 32];
     __shared__ bool finish;
+    griddep_launch_dependents();
+    griddep_wait();                                        // the statistics
     const long long i = blockIdx.x;
     double pi[2];
     for (int side = 0; side < 2; ++side) {
@@ -718,7 +984,7 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
             const float w = rows.weights ? rows.weights[r] : 1.f;
             if (w != 0.f) s += static_cast<double>(w) * logp[r];
         }
-        s = block_total(s, scratch);
+        s = block_total(s, scratch, kPairThreads, [] { __syncthreads(); });
         if (threadIdx.x == 0) seq_logp[2 * i + side] = static_cast<float>(s);
         pi[side] = s - in.ref_logp[2 * i + side];
     }
@@ -750,7 +1016,7 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
 #pragma unroll
         for (int q = 0; q < 3; ++q) sum[q] += __ldcg(&each[k][q]);
     for (int q = 0; q < 3; ++q) {
-        const double s = block_total(sum[q], scratch);
+        const double s = block_total(sum[q], scratch, kPairThreads, [] { __syncthreads(); });
         if (threadIdx.x == 0) stats[q] = static_cast<float>(s / static_cast<double>(in.pairs));
     }
 }

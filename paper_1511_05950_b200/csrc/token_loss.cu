@@ -11,48 +11,58 @@ using softsync::aligned_to;
 using softsync::GradBf16;
 using softsync::GradFp32;
 using softsync::PolicyIn;
+using softsync::PolicyState;
 using softsync::PreferenceIn;
 using softsync::RowCoef;
 using softsync::RowsIn;
 using softsync::RowStat;
 using softsync::StatsOut;
-using softsync::TermsOut;
-using softsync::Totals;
 
 namespace {
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 int64_t div_up(int64_t x, int64_t by) { return (x + by - 1) / by; }
 
-// Places in the losses' workspace.
+constexpr int64_t kMaxParts = 1024;       // that the rows of a policy loss are summed in, at most
+
+// Places in the losses' workspace.  Its first word counts finished blocks and is zero between calls.
 struct Workspace {
-    Totals *totals = nullptr;
-    unsigned *counters = nullptr;
-    double (*sums)[5] = nullptr;           // policy loss: of each group of rows
-    double (*pairs)[3] = nullptr;          // preference loss: of each pair
-    RowStat *stat = nullptr;
-    RowCoef *coef = nullptr;
-    float (*terms)[5] = nullptr;
-    float *entropy = nullptr, *logp = nullptr;
     int64_t bytes = 0;
-    Workspace(void *p, int64_t rows, int64_t sequences)
-    {
-        const int64_t groups = div_up(rows, softsync::kRowGroup);
-        take(p, totals, 1);
-        take(p, counters, groups + 1);
-        take(p, sums, groups);
-        take(p, pairs, sequences / 2);
-        take(p, stat, rows);
-        take(p, coef, rows);
-        take(p, terms, rows);
-        take(p, entropy, rows);
-        take(p, logp, rows);
-    }
-private:
+    unsigned *done = nullptr;
+    explicit Workspace(void *p) { take(p, done, 1); }
+protected:
     template <typename T> void take(void *p, T *&out, int64_t count)
     {
         out = reinterpret_cast<T *>(static_cast<char *>(p) + bytes);
         bytes += round_up(count * static_cast<int64_t>(sizeof(T)), 256);
+    }
+};
+struct PolicyWorkspace : Workspace {
+    PolicyState st{};
+    RowStat *stat = nullptr;
+    RowCoef *coef = nullptr;
+    float *entropy = nullptr;
+    PolicyWorkspace(void *p, int64_t rows) : Workspace(p)
+    {
+        st.done = done;
+        take(p, st.inv_weight, 1);
+        take(p, st.part_sum, std::min(rows, kMaxParts));
+        take(p, stat, rows);
+        take(p, coef, rows);
+        take(p, entropy, rows);
+    }
+};
+struct PreferenceWorkspace : Workspace {
+    double (*pairs)[3] = nullptr;          // terms of each pair
+    RowStat *stat = nullptr;
+    RowCoef *coef = nullptr;
+    float *logp = nullptr;
+    PreferenceWorkspace(void *p, int64_t rows, int64_t sequences) : Workspace(p)
+    {
+        take(p, pairs, sequences / 2);
+        take(p, stat, rows);
+        take(p, coef, rows);
+        take(p, logp, rows);
     }
 };
 
@@ -107,14 +117,16 @@ int sm_count()
     return n;
 }
 
-// One cluster of `cluster` blocks per row.  dependent: the kernel may start while the one before it on the stream still runs.
+// `rows` clusters of `cluster` blocks.  dependent: the kernel may start while the one before it on the stream, one of this call's own,
+// still runs, and waits for it itself before it touches what that one writes.
 template <typename... P, typename... A>
-int launch_rows(void (*kernel)(P...), int64_t rows, int cluster, int threads, bool dependent, cudaStream_t st, A... args)
+int launch_rows(void (*kernel)(P...), int64_t rows, int cluster, int threads, int smem, bool dependent, cudaStream_t st, A... args)
 {
     if (rows * cluster > 0x7fffffff) return PS_ERR_INVALID_ARG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rows * cluster));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -135,18 +147,20 @@ int64_t row_vectors(const ps_logits *lg)
     return div_up(phase + lg->vocab, per);
 }
 
-int64_t warps(int64_t threads) { return std::min<int64_t>(512, std::max<int64_t>(64, round_up(threads, 32))); }
-
-constexpr int kStatsVectors = 4;
 constexpr int kMaxCluster = softsync::kMaxCluster;
+constexpr int kWaitLimit = 1 << 20;                    // polls of up to a microsecond each
 
 template <typename GT, bool ENTROPY>
 int launch_stats_as(const RowsIn &in, int64_t vectors, const StatsOut &out, cudaStream_t st)
 {
-    const int threads = static_cast<int>(warps(div_up(vectors, kStatsVectors)));
-    int cluster = 1;                                      // few rows: several blocks each, as long as every one has work
-    while (cluster < kMaxCluster && in.rows * cluster * 2 <= 2 * sm_count() && vectors > static_cast<int64_t>(cluster) * threads * kStatsVectors) cluster *= 2;
-    return launch_rows(softsync::row_stats_kernel<GT, kStatsVectors, ENTROPY>, in.rows, cluster, threads, false, st, in, out);
+    auto go = [&](auto kernel, int threads, int batch) {
+        int cluster = 1;                                  // few rows: several blocks each, as long as every one has work
+        while (cluster < kMaxCluster && in.rows * cluster * 2 <= 2 * sm_count() && vectors > static_cast<int64_t>(cluster) * threads * batch) cluster *= 2;
+        return launch_rows(kernel, in.rows, cluster, threads, 0, false, st, in, out);
+    };
+    if (vectors <= 128) return go(softsync::row_stats_kernel<GT, 64, 2, ENTROPY>, 64, 2);
+    if (vectors <= 1024) return go(softsync::row_stats_kernel<GT, 256, 4, ENTROPY>, 256, 4);
+    return go(softsync::row_stats_kernel<GT, 512, 4, ENTROPY>, 512, 4);
 }
 int launch_stats(const ps_logits *lg, const RowsIn &in, const StatsOut &out, bool entropy, cudaStream_t st)
 {
@@ -160,61 +174,80 @@ int launch_grad(const ps_logits *lg, const RowsIn &in, const RowStat *stat, cons
 {
     const int64_t segments = div_up(row_vectors(lg), softsync::kGradThreads * softsync::kGradVectors);
     if (lg->rows * segments > 0x7fffffff) return PS_ERR_INVALID_ARG;
-    const unsigned grid = static_cast<unsigned>(lg->rows * segments);
-    const int seg = static_cast<int>(segments), threads = softsync::kGradThreads;
-    unsigned char *dst = static_cast<unsigned char *>(out);
-    if (lg->dtype == PS_GRAD_BF16) {
-        if (entropy) softsync::row_grad_kernel<GradBf16, true><<<grid, threads, 0, st>>>(in, stat, coef, entropy, dst, stride, seg);
-        else softsync::row_grad_kernel<GradBf16, false><<<grid, threads, 0, st>>>(in, stat, coef, entropy, dst, stride, seg);
-    } else {
-        if (entropy) softsync::row_grad_kernel<GradFp32, true><<<grid, threads, 0, st>>>(in, stat, coef, entropy, dst, stride, seg);
-        else softsync::row_grad_kernel<GradFp32, false><<<grid, threads, 0, st>>>(in, stat, coef, entropy, dst, stride, seg);
-    }
-    return launched();
-}
-
-// How a row is spread for the kernel that keeps it in registers; vectors == 0: it does not fit.
-struct RowShape { int cluster, threads, vectors; };
-RowShape row_shape(int64_t n, int64_t rows)
-{
-    int cluster = 1, most = 512;
-    while (cluster < kMaxCluster && n > static_cast<int64_t>(cluster) * 512 * 8) cluster *= 2;
-    if (n > static_cast<int64_t>(cluster) * 512 * 8) most = 1024;
-    if (n > static_cast<int64_t>(cluster) * most * 8) return {0, 0, 0};
-    while (cluster < kMaxCluster && rows * cluster * 2 <= 2 * sm_count() && n > cluster * 512) cluster *= 2;      // few rows
-    const int64_t mine = div_up(n, cluster);
-    const int64_t threads = most == 1024 ? 1024 : warps(div_up(mine, 4));
-    return {cluster, static_cast<int>(threads), static_cast<int>(div_up(mine, threads))};
+    const int seg = static_cast<int>(segments);
+    auto go = [&](auto kernel) {
+        return launch_rows(kernel, lg->rows * segments, 1, softsync::kGradThreads, 0, true, st, in, stat, coef, entropy, static_cast<unsigned char *>(out),
+                           static_cast<long long>(stride), seg);
+    };
+    if (lg->dtype == PS_GRAD_BF16) return entropy ? go(softsync::row_grad_kernel<GradBf16, true>) : go(softsync::row_grad_kernel<GradBf16, false>);
+    return entropy ? go(softsync::row_grad_kernel<GradFp32, true>) : go(softsync::row_grad_kernel<GradFp32, false>);
 }
 
 struct PolicyCall {
     RowsIn rows;
     PolicyIn in;
-    TermsOut terms;
+    PolicyState st;
     float *logp, *entropy;
     unsigned char *out;
-    int64_t stride;
+    int64_t stride, vectors;
 };
+
+// Clusters of the ring kernel that run at once on the current GPU (asked once for each kernel, cluster size and GPU).
 template <typename GT, bool ENTROPY_GRAD>
-int launch_policy_as(const RowShape &sh, const PolicyCall &k, cudaStream_t st)
+int resident_clusters(int cluster)
 {
-    auto go = [&](auto kernel) {
-        return launch_rows(kernel, k.rows.rows, sh.cluster, sh.threads, true, st, k.rows, k.in, k.terms, k.logp, k.entropy, k.out, static_cast<long long>(k.stride));
-    };
-    switch (sh.vectors) {
-    case 1: case 2: return go(softsync::policy_row_kernel<GT, 2, ENTROPY_GRAD>);
-    case 3: case 4: return go(softsync::policy_row_kernel<GT, 4, ENTROPY_GRAD>);
-    case 5: return go(softsync::policy_row_kernel<GT, 5, ENTROPY_GRAD>);
-    case 6: return go(softsync::policy_row_kernel<GT, 6, ENTROPY_GRAD>);
-    case 7: return go(softsync::policy_row_kernel<GT, 7, ENTROPY_GRAD>);
-    default: return go(softsync::policy_row_kernel<GT, 8, ENTROPY_GRAD>);
-    }
+    const auto kernel = softsync::policy_ring_kernel<GT, ENTROPY_GRAD>;
+    static std::atomic<int> known[64][kMaxCluster + 1] = {};
+    int device = 0, n = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return 0;
+    if ((n = known[device][cluster].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, softsync::kRingBytes) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(cluster));
+    cfg.blockDim = dim3(softsync::kRingThreads + 32);
+    cfg.dynamicSmemBytes = softsync::kRingBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return 0;
+    known[device][cluster].store(n, std::memory_order_relaxed);
+    return n;
 }
-int launch_policy(int dtype, const RowShape &sh, const PolicyCall &k, cudaStream_t st)
+
+template <typename GT, bool ENTROPY_GRAD>
+int launch_ring_as(const PolicyCall &k, int cluster, cudaStream_t st)
+{
+    auto kernel = softsync::policy_ring_kernel<GT, ENTROPY_GRAD>;
+    softsync::RingPlan plan;
+    plan.vectors = static_cast<int>(div_up(k.vectors, cluster));
+    plan.chunks = static_cast<int>(div_up(plan.vectors, softsync::kRingChunk));
+    plan.own_total = k.rows.rows <= softsync::kOwnTotalRows;
+    plan.wait_limit = kWaitLimit;
+    const int64_t parts = std::min({static_cast<int64_t>(k.rows.rows), static_cast<int64_t>(resident_clusters<GT, ENTROPY_GRAD>(cluster)), kMaxParts});
+    if (parts < 1) return PS_ERR_CUDA;
+    return launch_rows(kernel, parts, cluster, softsync::kRingThreads + 32, softsync::kRingBytes, !plan.own_total, st, k.rows, k.in, k.st, k.logp, k.entropy,
+                       k.out, static_cast<long long>(k.stride), plan);
+}
+
+int launch_ring(int dtype, const PolicyCall &k, int cluster, cudaStream_t st)
 {
     const bool ent = k.in.entropy_coef != 0.f;
-    if (dtype == PS_GRAD_BF16) return ent ? launch_policy_as<GradBf16, true>(sh, k, st) : launch_policy_as<GradBf16, false>(sh, k, st);
-    return ent ? launch_policy_as<GradFp32, true>(sh, k, st) : launch_policy_as<GradFp32, false>(sh, k, st);
+    if (dtype == PS_GRAD_BF16) return ent ? launch_ring_as<GradBf16, true>(k, cluster, st) : launch_ring_as<GradBf16, false>(k, cluster, st);
+    return ent ? launch_ring_as<GradFp32, true>(k, cluster, st) : launch_ring_as<GradFp32, false>(k, cluster, st);
+}
+
+// Blocks that a row is spread over for the ring kernel; 0: it does not fit the largest cluster.  As few as hold a row (more blocks
+// means more exchange for less work each: 16384 x 32000 bf16 takes 417 us with one, 584 with two), except where rows are so few that
+// the GPU would stay half empty (48 x 32000 bf16: 12.6 us with four, 14.2 with one).
+int ring_cluster(int64_t vectors, int64_t rows)
+{
+    int64_t cluster = div_up(vectors, softsync::kRingSlots * softsync::kRingChunk);
+    if (cluster > kMaxCluster) return 0;
+    while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= 2 * sm_count() && vectors > cluster * softsync::kRingThreads) cluster *= 2;
+    return static_cast<int>(cluster);
 }
 
 }  // namespace
@@ -224,7 +257,7 @@ extern "C" {
 int ps_loss_workspace(int64_t rows, int64_t sequences, int64_t *bytes)
 {
     if (!bytes || rows < 0 || rows > kMaxRows || sequences < 0 || sequences > (int64_t{1} << 31)) return PS_ERR_INVALID_ARG;
-    *bytes = Workspace(nullptr, rows, sequences).bytes;
+    *bytes = std::max(PolicyWorkspace(nullptr, rows).bytes, PreferenceWorkspace(nullptr, rows, sequences).bytes);
     return PS_OK;
 }
 
@@ -234,7 +267,7 @@ int ps_token_logprob(const ps_logits *logits, float *logp_dev, float *lse_dev, f
     if (bad != PS_OK) return bad;
     if (logits->rows == 0) return PS_OK;
     if (!logp_dev || !aligned_to(logp_dev, 4) || !aligned_to(lse_dev, 4) || !aligned_to(entropy_dev, 4)) return PS_ERR_INVALID_ARG;
-    return launch_stats(logits, rows_in(logits), StatsOut{logp_dev, lse_dev, entropy_dev, nullptr, nullptr, nullptr}, entropy_dev != nullptr,
+    return launch_stats(logits, rows_in(logits), StatsOut{logp_dev, lse_dev, entropy_dev, nullptr, nullptr}, entropy_dev != nullptr,
                         static_cast<cudaStream_t>(stream));
 }
 
@@ -250,7 +283,7 @@ int ps_policy_loss(const ps_logits *logits, const ps_policy_inputs *in, float *s
         return PS_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (logits->rows == 0) return cudaMemsetAsync(stats_dev, 0, 5 * sizeof(float), st) == cudaSuccess ? PS_OK : PS_ERR_CUDA;
-    const Workspace ws(workspace_dev, logits->rows, 0);
+    const PolicyWorkspace ws(workspace_dev, logits->rows);
     if (!logp_dev || !in->old_logp_dev || !in->advantages_dev || !workspace_dev || workspace_bytes < ws.bytes ||
         !aligned_to(workspace_dev, 16) || !aligned_to(logp_dev, 4) || !aligned_to(entropy_dev, 4) || !aligned_to(in->old_logp_dev, 4) ||
         !aligned_to(in->advantages_dev, 4) || !aligned_to(in->ref_logp_dev, 4))
@@ -259,22 +292,22 @@ int ps_policy_loss(const ps_logits *logits, const ps_policy_inputs *in, float *s
     k.rows = rows_in(logits);
     k.in = PolicyIn{in->old_logp_dev, in->advantages_dev, in->ref_logp_dev, 1.f - in->clip_low, 1.f + in->clip_high,
                     in->ref_logp_dev ? in->kl_coef : 0.f, in->entropy_coef};
-    k.terms = TermsOut{ws.totals, ws.counters, ws.terms, ws.sums, stats_dev};
+    k.st = ws.st;
+    k.st.stats = stats_dev;
     k.logp = logp_dev;
     k.entropy = entropy_dev ? entropy_dev : ws.entropy;
     k.out = static_cast<unsigned char *>(dlogits_dev);
     k.stride = dlogits_stride;
-    const int64_t groups = div_up(logits->rows, softsync::kRowGroup);
-    const RowShape shape = row_shape(row_vectors(logits), logits->rows);
-    const bool one_read = shape.vectors != 0;
-    if (!one_read &&
-        (status = launch_stats(logits, k.rows, StatsOut{logp_dev, nullptr, k.entropy, ws.stat, nullptr, nullptr}, true, st)) != PS_OK)
-        return status;
-    softsync::policy_totals_kernel<<<1, softsync::kTermThreads, 0, st>>>(logits->weights_dev, logits->rows, ws.totals, ws.counters, static_cast<int>(groups));
-    if ((status = launched()) != PS_OK) return status;
-    if (one_read) return launch_policy(logits->dtype, shape, k, st);
-    softsync::policy_terms_kernel<<<static_cast<unsigned>(div_up(logits->rows, 8)), 256, 0, st>>>(k.rows, k.in, k.terms, logp_dev, k.entropy,
-                                                                                                dlogits_dev ? ws.coef : nullptr);
+    k.vectors = row_vectors(logits);
+    const int cluster = ring_cluster(k.vectors, logits->rows);
+    if (!cluster || logits->rows > softsync::kOwnTotalRows) {
+        softsync::policy_totals_kernel<<<1, softsync::kTermThreads, 0, st>>>(logits->weights_dev, logits->rows, k.st.inv_weight);
+        if ((status = launched()) != PS_OK) return status;
+    }
+    if (cluster) return launch_ring(logits->dtype, k, cluster, st);
+    if ((status = launch_stats(logits, k.rows, StatsOut{logp_dev, nullptr, k.entropy, ws.stat, nullptr}, true, st)) != PS_OK) return status;
+    softsync::policy_terms_kernel<<<static_cast<unsigned>(std::min(logits->rows, kMaxParts)), 32, 0, st>>>(k.rows, k.in, k.st, logp_dev, k.entropy,
+                                                                                                        dlogits_dev ? ws.coef : nullptr);
     if ((status = launched()) != PS_OK || !dlogits_dev) return status;
     return launch_grad(logits, k.rows, ws.stat, ws.coef, in->entropy_coef != 0.f ? k.entropy : nullptr, dlogits_dev, dlogits_stride, st);
 }
@@ -290,21 +323,17 @@ int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, 
     if (in->pairs && (!in->offsets_dev || !in->ref_logp_dev || !seq_logp_dev || !aligned_to(in->offsets_dev, 8) ||
                       !aligned_to(in->ref_logp_dev, 4) || !aligned_to(seq_logp_dev, 4)))
         return PS_ERR_INVALID_ARG;
-    const Workspace ws(workspace_dev, logits->rows, 2 * in->pairs);
+    const PreferenceWorkspace ws(workspace_dev, logits->rows, 2 * in->pairs);
     if (!workspace_dev || workspace_bytes < ws.bytes || !aligned_to(workspace_dev, 16)) return PS_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const RowsIn rows = rows_in(logits);
     const PreferenceIn p{reinterpret_cast<const long long *>(in->offsets_dev), in->ref_logp_dev, in->pairs, in->beta, in->label_smoothing};
-    if (logits->rows) status = launch_stats(logits, rows, StatsOut{ws.logp, nullptr, nullptr, ws.stat, ws.coef, ws.counters}, false, st);
-    else if (cudaMemsetAsync(ws.counters, 0, sizeof *ws.counters, st) != cudaSuccess) status = PS_ERR_CUDA;
-    if (status != PS_OK) return status;
-    if (in->pairs) {
-        softsync::preference_terms_kernel<<<static_cast<unsigned>(in->pairs), softsync::kPairThreads, 0, st>>>(
-            rows, p, ws.logp, seq_logp_dev, dlogits_dev ? ws.coef : nullptr, ws.pairs, ws.counters, stats_dev);
-        status = launched();
-    } else if (cudaMemsetAsync(stats_dev, 0, 3 * sizeof(float), st) != cudaSuccess) {
+    if (logits->rows && (status = launch_stats(logits, rows, StatsOut{ws.logp, nullptr, nullptr, ws.stat, ws.coef}, false, st)) != PS_OK) return status;
+    if (in->pairs)
+        status = launch_rows(softsync::preference_terms_kernel, in->pairs, 1, softsync::kPairThreads, 0, true, st, rows, p, ws.logp, seq_logp_dev,
+                             dlogits_dev ? ws.coef : nullptr, ws.pairs, ws.done, stats_dev);
+    else if (cudaMemsetAsync(stats_dev, 0, 3 * sizeof(float), st) != cudaSuccess)
         status = PS_ERR_CUDA;
-    }
     if (status != PS_OK || !dlogits_dev || !logits->rows) return status;
     return launch_grad(logits, rows, ws.stat, ws.coef, nullptr, dlogits_dev, dlogits_stride, st);
 }

@@ -8,6 +8,7 @@ current stream of the tensors' device.
 from __future__ import annotations
 
 import ctypes as C
+import threading
 from typing import List, NamedTuple, Optional, Sequence, Union
 
 import torch
@@ -16,6 +17,7 @@ from . import binding as B
 
 _DTYPES = {torch.float32: B.PS_GRAD_FP32, torch.bfloat16: B.PS_GRAD_BF16}
 INPLACE = "inplace"
+_numel, _is_contiguous, _get_device, _data_ptr = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr)
 
 
 def _stream(device: torch.device) -> int:
@@ -24,7 +26,10 @@ def _stream(device: torch.device) -> int:
 
 def _on(device: torch.device):
     """Makes `device` current for a call that has no handle to remember it."""
-    return torch.cuda.device(device) if torch.cuda.current_device() != device.index else B._NullCtx()
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+_HERE = B._NullCtx()
 
 
 def _cuda_device(device) -> torch.device:
@@ -84,23 +89,21 @@ class TensorList:
         if c not in self._pointers:
             self._pointers[c] = ((C.c_void_p * (c * n))(), (C.c_float * c)())
         ptrs, factors = self._pointers[c]
-        dtype, device, at = None, self.device, 0
+        dtypes, at = set(), 0
         for gradient in grads:
-            if len(gradient) != n:
-                raise ValueError("a gradient has %d tensors, the list %d" % (len(gradient), n))
-            for g, size in zip(gradient, self.sizes):
-                if g.dtype is not dtype:
-                    if dtype is not None or g.dtype not in _DTYPES:
-                        raise TypeError("gradients must all be fp32 or all bf16")
-                    dtype = g.dtype
-                if g.numel() != size or not g.is_contiguous():
-                    raise ValueError("gradient tensor %d must be contiguous with %d elements" % (at % n, size))
-                if g.device != device:
-                    raise ValueError("gradient tensor %d is on %s, the list on %s" % (at % n, g.device, device))
-                ptrs[at] = g.data_ptr()
-                at += 1
-        for l in range(c):
-            factors[l] = 1.0 if scales is None else scales[l]
+            if list(map(_numel, gradient)) != self.sizes:
+                raise ValueError("a gradient must have the list's %d tensors with %s elements" % (n, self.sizes if n < 20 else "its"))
+            if not all(map(_is_contiguous, gradient)):
+                raise ValueError("gradient tensors must be contiguous")
+            if set(map(_get_device, gradient)) != {self.device.index}:
+                raise ValueError("gradient tensors must live on the list's GPU, %s" % self.device)
+            dtypes.update([g.dtype for g in gradient])
+            ptrs[at:at + n] = list(map(_data_ptr, gradient))
+            at += n
+        dtype = dtypes.pop()
+        if dtypes or dtype not in _DTYPES:
+            raise TypeError("gradients must all be fp32 or all bf16")
+        factors[:] = [1.0] * c if scales is None else scales
         return ptrs, c, factors, _DTYPES[dtype]
 
     def grad_norm(self, grads, scales: Optional[Sequence[float]] = None, max_norm: float = float("inf"),
@@ -205,28 +208,29 @@ class PreferenceLoss(NamedTuple):
 
 
 def _logits(logits: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor], temperature: float) -> B.Logits:
-    if logits.dtype not in _DTYPES:
+    dtype = _DTYPES.get(logits.dtype)
+    if dtype is None:
         raise TypeError("logits must be fp32 or bf16, got %s" % logits.dtype)
     if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise ValueError("logits must be rows x vocabulary with the vocabulary contiguous")
     if not logits.is_cuda:
         raise ValueError("logits must live on the GPU")
     rows, vocab = logits.shape
-    if tokens.shape != (rows,):
-        raise ValueError("one token for each of the %d rows, got shape %s" % (rows, tuple(tokens.shape)))
-    B.require_tensor(tokens, torch.int64, rows, "tokens", on_gpu=True, device=logits.device)
-    _per_row(weights, rows, "weights", logits.device)
+    _per_row(tokens, rows, "tokens", logits, torch.int64)
+    _per_row(weights, rows, "weights", logits)
     stride = logits.stride(0) if rows > 1 else max(vocab, 1)
-    return B.Logits(logits.data_ptr(), _DTYPES[logits.dtype], rows, vocab, stride, tokens.data_ptr(),
-                    None if weights is None else weights.data_ptr(), temperature)
+    return B.Logits(logits.data_ptr(), dtype, rows, vocab, stride, tokens.data_ptr(), None if weights is None else weights.data_ptr(), temperature)
 
 
-def _per_row(t: Optional[torch.Tensor], rows: int, what: str, device: torch.device) -> None:
+def _per_row(t: Optional[torch.Tensor], rows: int, what: str, logits: torch.Tensor, dtype: torch.dtype = torch.float32) -> None:
     if t is None:
         return
-    if t.shape != (rows,):
-        raise ValueError("%s: one value for each of the %d rows, got shape %s" % (what, rows, tuple(t.shape)))
-    B.require_tensor(t, torch.float32, rows, what, on_gpu=True, device=device)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if t.dim() != 1 or t.numel() != rows or not t.is_contiguous():
+        raise ValueError("%s: %d values one behind the other, got shape %s with strides %s" % (what, rows, tuple(t.shape), t.stride()))
+    if t.get_device() != logits.get_device():
+        raise ValueError("%s is on %s, the logits on %s" % (what, t.device, logits.device))
 
 
 def _gradient_buffer(logits: torch.Tensor, grad: Union[bool, str, torch.Tensor]):
@@ -245,20 +249,30 @@ def _gradient_buffer(logits: torch.Tensor, grad: Union[bool, str, torch.Tensor])
     return grad, grad.stride(0) if rows > 1 else max(vocab, 1)
 
 
-def _workspace(rows: int, sequences: int, device: torch.device) -> torch.Tensor:
+_workspaces = {}                          # (device, stream, thread): a workspace that such calls use one after the other
+
+
+def _workspace(rows: int, sequences: int, device: torch.device, stream: int) -> torch.Tensor:
     need = C.c_int64()
     B._check(B.ps_loss_workspace(rows, sequences, C.byref(need)), "ps_loss_workspace")
-    return torch.empty(need.value, dtype=torch.uint8, device=device)
+    capturing = torch.cuda.is_current_stream_capturing()               # a graph keeps its own
+    key = (device.index, stream, threading.get_ident())
+    ws = None if capturing else _workspaces.get(key)
+    if ws is None or ws.numel() < need.value:
+        ws = torch.zeros(max(need.value, 1 << 16), dtype=torch.uint8, device=device)
+        if not capturing:
+            _workspaces[key] = ws
+    return ws
 
 
 def token_logprob(logits: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor] = None, temperature: float = 1.0) -> TokenLogprob:
     """Log probability of each row's token, log normaliser and entropy, from one pass over the logits (rows x vocabulary, fp32 or bf16).
     Rows of weight zero are not read and give zeros."""
     lg = _logits(logits, tokens, weights, temperature)
-    out = torch.empty((3, lg.rows), dtype=torch.float32, device=logits.device)
+    logp, lse, entropy = (torch.empty(lg.rows, dtype=torch.float32, device=logits.device) for _ in range(3))
     with _on(logits.device):
-        B._check(B.ps_token_logprob(C.byref(lg), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), _stream(logits.device)), "ps_token_logprob")
-    return TokenLogprob(out[0], out[1], out[2])
+        B._check(B.ps_token_logprob(C.byref(lg), logp.data_ptr(), lse.data_ptr(), entropy.data_ptr(), _stream(logits.device)), "ps_token_logprob")
+    return TokenLogprob(logp, lse, entropy)
 
 
 def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
@@ -269,18 +283,19 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     gradient replaces the logits), or False."""
     lg = _logits(logits, tokens, weights, temperature)
     for what, t in (("old_logp", old_logp), ("advantages", advantages), ("ref_logp", ref_logp)):
-        _per_row(t, lg.rows, what, logits.device)
+        _per_row(t, lg.rows, what, logits)
+    device = logits.device
     dlogits, stride = _gradient_buffer(logits, grad)
-    stats = torch.empty(5, dtype=torch.float32, device=logits.device)
-    out = torch.empty((2, lg.rows), dtype=torch.float32, device=logits.device)
-    ws = _workspace(lg.rows, 0, logits.device)
+    stats = torch.empty(5, dtype=torch.float32, device=device)
+    logp, entropy = (torch.empty(lg.rows, dtype=torch.float32, device=device) for _ in range(2))
     k = B.PolicyInputs(old_logp.data_ptr(), advantages.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(),
                        clip_low, clip_high, kl_coef, entropy_coef)
-    with _on(logits.device):
-        B._check(B.ps_policy_loss(C.byref(lg), C.byref(k), stats.data_ptr(), out[0].data_ptr(), out[1].data_ptr(),
-                                  None if dlogits is None else dlogits.data_ptr(), stride, ws.data_ptr(), ws.numel(), _stream(logits.device)),
-                 "ps_policy_loss")
-    return PolicyLoss(stats, out[0], out[1], dlogits)
+    with _on(device):
+        stream = _stream(device)
+        ws = _workspace(lg.rows, 0, device, stream)
+        B._check(B.ps_policy_loss(C.byref(lg), C.byref(k), stats.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
+                                  None if dlogits is None else dlogits.data_ptr(), stride, ws.data_ptr(), ws.numel(), stream), "ps_policy_loss")
+    return PolicyLoss(stats, logp, entropy, dlogits)
 
 
 def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.Tensor, ref_logp: torch.Tensor,
@@ -293,15 +308,16 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.T
     if offsets.dim() != 1 or offsets.numel() % 2 != 1:
         raise ValueError("offsets holds 2 * pairs + 1 row numbers")
     seqs = offsets.numel() - 1
-    B.require_tensor(offsets, torch.int64, seqs + 1, "offsets", on_gpu=True, device=logits.device)
-    _per_row(ref_logp, seqs, "ref_logp", logits.device)
+    _per_row(offsets, seqs + 1, "offsets", logits, torch.int64)
+    _per_row(ref_logp, seqs, "ref_logp", logits)
+    device = logits.device
     dlogits, stride = _gradient_buffer(logits, grad)
-    stats = torch.empty(3, dtype=torch.float32, device=logits.device)
-    seq_logp = torch.empty(seqs, dtype=torch.float32, device=logits.device)
-    ws = _workspace(lg.rows, seqs, logits.device)
+    stats = torch.empty(3, dtype=torch.float32, device=device)
+    seq_logp = torch.empty(seqs, dtype=torch.float32, device=device)
     k = B.PreferenceInputs(offsets.data_ptr(), ref_logp.data_ptr(), seqs // 2, beta, label_smoothing)
-    with _on(logits.device):
+    with _on(device):
+        stream = _stream(device)
+        ws = _workspace(lg.rows, seqs, device, stream)
         B._check(B.ps_preference_loss(C.byref(lg), C.byref(k), stats.data_ptr(), seq_logp.data_ptr(),
-                                      None if dlogits is None else dlogits.data_ptr(), stride, ws.data_ptr(), ws.numel(), _stream(logits.device)),
-                 "ps_preference_loss")
+                                      None if dlogits is None else dlogits.data_ptr(), stride, ws.data_ptr(), ws.numel(), stream), "ps_preference_loss")
     return PreferenceLoss(stats, seq_logp, dlogits)
