@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsoftsync_ps.so")
 SOURCES = ["softsync_ps.cu", "tensor_list.cu", "token_loss.cu"]
-HEADERS = [os.path.join(CSRC, h) for h in ("update_kernels.cuh", "tensor_kernels.cuh", "token_kernels.cuh", "host_util.h")] + \
+HEADERS = [os.path.join(CSRC, h) for h in ("update_kernels.cuh", "tensor_kernels.cuh", "token_kernels.cuh", "packed.cuh", "host_util.h")] + \
           [os.path.join(os.path.dirname(HERE), "include", h) for h in ("softsync_ps.h", "softsync_learn.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -11,7 +11,10 @@
 // documented order, whatever the launch shape, so results can be compared bit by bit.
 #pragma once
 
+#include "packed.cuh"
 #include "update_kernels.cuh"
+
+#include <math_constants.h>
 
 namespace softsync {
 
@@ -193,14 +196,18 @@ constexpr unsigned kMaxCodeM = 127, kMaxCodeV = 255;
 #define SOFTSYNC_M_UNIT 0x1p120f                                         // first moment: exponent bias 7 = 127 - 120
 #define SOFTSYNC_V_UNIT 0x1p112f                                         // second moment: bias 15 = 127 - 112
 
-__device__ __forceinline__ float decode_m(unsigned code, float scale)
+// Code k (0..3) of four in a word, as the fp32 number whose top it is.
+template <bool SIGNED>
+__device__ __forceinline__ float code_top(unsigned four, int k)
 {
-    const float x = __fmul_rn(__fmul_rn(__uint_as_float((code & 127u) << kDropBits), SOFTSYNC_M_UNIT), scale);
-    return code & 128u ? -x : x;
+    const unsigned top = four << (24 - 8 * k);
+    return __uint_as_float(SIGNED ? static_cast<unsigned>(static_cast<int>(top) >> 5) & 0x83f80000u : (top >> 5) & 0x07f80000u);
 }
-__device__ __forceinline__ float decode_v(unsigned code, float scale)
+template <bool SIGNED>
+__device__ __forceinline__ float2 decode_pair(unsigned four, int k, float scale)
 {
-    return __fmul_rn(__fmul_rn(__uint_as_float(code << kDropBits), SOFTSYNC_V_UNIT), scale);
+    const float unit = SIGNED ? SOFTSYNC_M_UNIT : SOFTSYNC_V_UNIT;
+    return mul2(mul2(make_float2(code_top<SIGNED>(four, k), code_top<SIGNED>(four, k + 1)), make_float2(unit, unit)), make_float2(scale, scale));
 }
 __device__ __forceinline__ float block_scale(unsigned e) { return __uint_as_float(e << 23); }
 
@@ -211,19 +218,44 @@ __device__ __forceinline__ unsigned block_exponent(unsigned top)
     if (top >= 0x7f800000u) return 255u;
     return min(max((top + (1u << kDropBits)) >> 23, 27u), 253u);
 }
-__device__ __forceinline__ unsigned encode(float mag, float inv_scale, float unit, unsigned rnd, unsigned top)
-{
-    const unsigned bits = __float_as_uint(__fmul_rn(__fmul_rn(mag, inv_scale), unit));
-    return min((bits + rnd) >> kDropBits, top);
-}
+// The code of a magnitude whose scaled fp32 bits are given.
+__device__ __forceinline__ unsigned code_of(float scaled, unsigned rnd, unsigned top) { return min((__float_as_uint(scaled) + rnd) >> kDropBits, top); }
 
-// 32 random bits for element i: an integer hash (two rounds of xor-shift and multiply) of its place and the step's key.
-__device__ __forceinline__ unsigned element_hash(unsigned long long i, unsigned key)
+// 32 random bits for the element whose place has the low word lo; hi_term: its high word times 0x9E3779B9.  An integer hash (two rounds
+// of xor-shift and multiply) of the place and the step's key.
+__device__ __forceinline__ unsigned element_hash(unsigned lo, unsigned hi_term, unsigned key)
 {
-    unsigned x = (static_cast<unsigned>(i) ^ key) + static_cast<unsigned>(i >> 32) * 0x9E3779B9u;
+    unsigned x = (lo ^ key) + hi_term;
     x ^= x >> 16; x *= 0x7FEB352Du;
     x ^= x >> 15; x *= 0x846CA68Bu;
     return x ^ (x >> 16);
+}
+
+// Square root and quotient, correctly rounded, without the branches of the compiler's: from the approximate reciprocal (root) by
+// Newton steps in fused multiply-adds whose last correction uses the exact remainder (Markstein, IBM J. Res. Dev. 34, 1990).  Both
+// pairs have to be ordinary numbers whose remainders do not underflow.
+__device__ __forceinline__ float2 rounded_sqrt(float2 v)
+{
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(v.x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(v.y));
+    const float2 half = make_float2(0.5f, 0.5f);
+    float2 g = mul2(v, y), h = mul2(y, half);
+    const float2 r = fma2(make_float2(-g.x, -g.y), h, half);
+    g = fma2(g, r, g);
+    h = fma2(h, r, h);
+    return fma2(fma2(make_float2(-g.x, -g.y), g, v), h, g);
+}
+__device__ __forceinline__ float2 rounded_quotient(float2 a, float2 b)
+{
+    float2 y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(b.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(b.y));
+    const float2 nb = make_float2(-b.x, -b.y);
+    y = fma2(fma2(nb, y, make_float2(1.f, 1.f)), y, y);
+    float2 q = mul2(a, y);
+    q = fma2(fma2(nb, q, a), y, q);
+    return fma2(fma2(nb, q, a), y, q);
 }
 
 // ---- AdamW -------------------------------------------------------------------------------------------------------------
@@ -235,24 +267,35 @@ struct AdamwParams {
     double lr_decay, step_size;           // lr * weight_decay; lr / (1 - beta1^t)
     float beta1, one_minus_beta1, beta2, one_minus_beta2, root_scale, eps;
     unsigned key;
+    int short_forms;                      // eps allows the short root and quotient
 };
+
+// Scaling that keeps the short root and quotient away from underflow: powers of two that the roundings do not see.  They serve while
+// m < 2^20 and v < 2^30, with an eps of at least 2^-40 (so no quotient overflows, and a root of zero may be taken for 2^-78) and a step
+// size of at least 2^-40.
+constexpr float kMScale = 0x1p64f, kVScale = 0x1p96f, kVLeast = 0x1p-60f;
+constexpr unsigned kMLimit = 0x49800000u, kVLimit = 0x4e800000u;         // bits of 2^20, 2^30
 
 template <typename GT, int BITS, bool VECTOR, int MAXP>
 __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTable<MAXP> &tab, const TensorRec &rec, int t,
                                             long long first, int lane, int count, float clip)
 {
-    float g[8], w[8], m[8], v[8];
+    float g[8];
+    float2 w[4], m[4], v[4];
     const long long at = rec.state_off + first;          // a multiple of kStateBlock
     float *wp = rec.w + first;
+    unsigned mcodes[2], vcodes[2];
+    float ms = 0.f, vs = 0.f;
     if constexpr (VECTOR) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float4 q = __ldcs(reinterpret_cast<const float4 *>(wp) + h * 32 + lane);
-            w[4 * h] = q.x; w[4 * h + 1] = q.y; w[4 * h + 2] = q.z; w[4 * h + 3] = q.w;
+            w[2 * h] = make_float2(q.x, q.y); w[2 * h + 1] = make_float2(q.z, q.w);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = j * 32 + lane < count ? wp[j * 32 + lane] : 0.f;
+        for (int j = 0; j < 8; j += 2)
+            w[j / 2] = make_float2(j * 32 + lane < count ? wp[j * 32 + lane] : 0.f, j * 32 + 32 + lane < count ? wp[j * 32 + 32 + lane] : 0.f);
     }
     if constexpr (BITS == 32) {
         const float *mp = static_cast<const float *>(p.m) + at, *vp = static_cast<const float *>(p.v) + at;
@@ -261,68 +304,109 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
             for (int h = 0; h < 2; ++h) {
                 const float4 a = __ldcs(reinterpret_cast<const float4 *>(mp) + h * 32 + lane);
                 const float4 b = __ldcs(reinterpret_cast<const float4 *>(vp) + h * 32 + lane);
-                m[4 * h] = a.x; m[4 * h + 1] = a.y; m[4 * h + 2] = a.z; m[4 * h + 3] = a.w;
-                v[4 * h] = b.x; v[4 * h + 1] = b.y; v[4 * h + 2] = b.z; v[4 * h + 3] = b.w;
+                m[2 * h] = make_float2(a.x, a.y); m[2 * h + 1] = make_float2(a.z, a.w);
+                v[2 * h] = make_float2(b.x, b.y); v[2 * h + 1] = make_float2(b.z, b.w);
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                m[j] = j * 32 + lane < count ? mp[j * 32 + lane] : 0.f;
-                v[j] = j * 32 + lane < count ? vp[j * 32 + lane] : 0.f;
+            for (int j = 0; j < 8; j += 2) {
+                const int e = j * 32 + lane;
+                m[j / 2] = make_float2(e < count ? mp[e] : 0.f, e + 32 < count ? mp[e + 32] : 0.f);
+                v[j / 2] = make_float2(e < count ? vp[e] : 0.f, e + 32 < count ? vp[e + 32] : 0.f);
             }
         }
     } else {
         const unsigned char *mp = static_cast<const unsigned char *>(p.m) + at, *vp = static_cast<const unsigned char *>(p.v) + at;
-        const float ms = block_scale(p.m_scale[at / kStateBlock]), vs = block_scale(p.v_scale[at / kStateBlock]);
-        if constexpr (VECTOR) {
+        ms = block_scale(p.m_scale[at / kStateBlock]);
+        vs = block_scale(p.v_scale[at / kStateBlock]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const unsigned a = __ldcs(reinterpret_cast<const unsigned *>(mp) + h * 32 + lane);
-                const unsigned b = __ldcs(reinterpret_cast<const unsigned *>(vp) + h * 32 + lane);
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (VECTOR) {
+                mcodes[h] = __ldcs(reinterpret_cast<const unsigned *>(mp) + h * 32 + lane);
+                vcodes[h] = __ldcs(reinterpret_cast<const unsigned *>(vp) + h * 32 + lane);
+            } else {
+                mcodes[h] = vcodes[h] = 0;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    m[4 * h + k] = decode_m((a >> (8 * k)) & 255u, ms);
-                    v[4 * h + k] = decode_v((b >> (8 * k)) & 255u, vs);
+                    const int e = (4 * h + k) * 32 + lane;
+                    if (e < count) {
+                        mcodes[h] |= static_cast<unsigned>(mp[e]) << (8 * k);
+                        vcodes[h] |= static_cast<unsigned>(vp[e]) << (8 * k);
+                    }
                 }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = j * 32 + lane < count;
-                m[j] = in ? decode_m(mp[j * 32 + lane], ms) : 0.f;
-                v[j] = in ? decode_v(vp[j * 32 + lane], vs) : 0.f;
             }
         }
     }
     weighted_gradient<GT, VECTOR>(g, tab, t, first, lane, count);
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            m[k] = decode_pair<true>(mcodes[k / 2], 2 * (k & 1), ms);
+            v[k] = decode_pair<false>(vcodes[k / 2], 2 * (k & 1), vs);
+        }
+        if (count < kStateBlock && (!(ms < CUDART_INF_F) || !(vs < CUDART_INF_F))) {       // a marked block: zero codes are NaN there, but not past the end
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (lane_elem<VECTOR>(lane, j) >= count) {
+                    if (j & 1) m[j / 2].y = v[j / 2].y = 0.f;
+                    else m[j / 2].x = v[j / 2].x = 0.f;
+                }
+        }
+    }
 
     const float decay = static_cast<float>(1.0 - p.lr_decay * (static_cast<double>(rec.lr_mult) * rec.decay_mult));
     const float step = static_cast<float>(p.step_size * rec.lr_mult);
+    const auto two = [](float x) { return make_float2(x, x); };
+    unsigned mt = 0, vt = 0;                             // the largest magnitudes, as bits
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float x = p.clip ? __fmul_rn(g[j], clip) : g[j];
-        m[j] = __fadd_rn(__fmul_rn(m[j], p.beta1), __fmul_rn(x, p.one_minus_beta1));
-        v[j] = __fadd_rn(__fmul_rn(v[j], p.beta2), __fmul_rn(__fmul_rn(x, x), p.one_minus_beta2));
-        const float den = __fadd_rn(__fmul_rn(__fsqrt_rn(v[j]), p.root_scale), p.eps);
-        w[j] = __fsub_rn(__fmul_rn(w[j], decay), __fmul_rn(__fdiv_rn(m[j], den), step));
+    for (int k = 0; k < 4; ++k) {
+        float2 x = make_float2(g[2 * k], g[2 * k + 1]);
+        if (p.clip) x = mul2(x, two(clip));
+        const float2 a = mul2(m[k], two(p.beta1)), b = mul2(x, two(p.one_minus_beta1));
+        const float2 c = mul2(v[k], two(p.beta2)), d = mul2(mul2(x, x), two(p.one_minus_beta2));
+        m[k] = make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
+        v[k] = make_float2(__fadd_rn(c.x, d.x), __fadd_rn(c.y, d.y));
+        mt = max(mt, max(__float_as_uint(m[k].x) & 0x7fffffffu, __float_as_uint(m[k].y) & 0x7fffffffu));
+        vt = max(vt, max(__float_as_uint(v[k].x) & 0x7fffffffu, __float_as_uint(v[k].y) & 0x7fffffffu));
+    }
+    if constexpr (BITS == 8) { mt = __reduce_max_sync(0xffffffffu, mt); vt = __reduce_max_sync(0xffffffffu, vt); }
+    if (__all_sync(0xffffffffu, p.short_forms && fabsf(step) >= 0x1p-40f && mt < kMLimit && vt < kVLimit)) {
+        const float2 rs = two(p.root_scale * 0x1p-48f), st = two(step * 0x1p-64f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float2 x = mul2(v[k], two(kVScale));
+            x = make_float2(fmaxf(x.x, kVLeast), fmaxf(x.y, kVLeast));
+            x = mul2(rounded_sqrt(x), rs);
+            const float2 den = make_float2(__fadd_rn(x.x, p.eps), __fadd_rn(x.y, p.eps));
+            const float2 u = mul2(rounded_quotient(mul2(m[k], two(kMScale)), den), st), y = mul2(w[k], two(decay));
+            w[k] = make_float2(__fsub_rn(y.x, u.x), __fsub_rn(y.y, u.y));
+        }
+    } else {
+        const auto one = [&](float wi, float mi, float vi) {
+            const float den = __fadd_rn(__fmul_rn(__fsqrt_rn(vi), p.root_scale), p.eps);
+            return __fsub_rn(__fmul_rn(wi, decay), __fmul_rn(__fdiv_rn(mi, den), step));
+        };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = make_float2(one(w[k].x, m[k].x, v[k].x), one(w[k].y, m[k].y, v[k].y));
     }
 
     if constexpr (VECTOR) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            __stcs(reinterpret_cast<float4 *>(wp) + h * 32 + lane, make_float4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
+            __stcs(reinterpret_cast<float4 *>(wp) + h * 32 + lane, make_float4(w[2 * h].x, w[2 * h].y, w[2 * h + 1].x, w[2 * h + 1].y));
         if (rec.mirror) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 __stcs(reinterpret_cast<uint2 *>(rec.mirror + first) + h * 32 + lane,
-                       make_uint2(pack_bf16x2(w[4 * h], w[4 * h + 1]), pack_bf16x2(w[4 * h + 2], w[4 * h + 3])));
+                       make_uint2(pack_bf16x2(w[2 * h].x, w[2 * h].y), pack_bf16x2(w[2 * h + 1].x, w[2 * h + 1].y)));
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j * 32 + lane < count) {
-                wp[j * 32 + lane] = w[j];
-                if (rec.mirror) rec.mirror[first + j * 32 + lane] = __bfloat16_as_ushort(__float2bfloat16_rn(w[j]));
+                const float x = j & 1 ? w[j / 2].y : w[j / 2].x;
+                wp[j * 32 + lane] = x;
+                if (rec.mirror) rec.mirror[first + j * 32 + lane] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
             }
     }
     if constexpr (BITS == 32) {
@@ -330,32 +414,35 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
         if constexpr (VECTOR) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                __stcs(reinterpret_cast<float4 *>(mp) + h * 32 + lane, make_float4(m[4 * h], m[4 * h + 1], m[4 * h + 2], m[4 * h + 3]));
-                __stcs(reinterpret_cast<float4 *>(vp) + h * 32 + lane, make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]));
+                __stcs(reinterpret_cast<float4 *>(mp) + h * 32 + lane, make_float4(m[2 * h].x, m[2 * h].y, m[2 * h + 1].x, m[2 * h + 1].y));
+                __stcs(reinterpret_cast<float4 *>(vp) + h * 32 + lane, make_float4(v[2 * h].x, v[2 * h].y, v[2 * h + 1].x, v[2 * h + 1].y));
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j * 32 + lane < count) { mp[j * 32 + lane] = m[j]; vp[j * 32 + lane] = v[j]; }
+                if (j * 32 + lane < count) {
+                    mp[j * 32 + lane] = j & 1 ? m[j / 2].y : m[j / 2].x;
+                    vp[j * 32 + lane] = j & 1 ? v[j / 2].y : v[j / 2].x;
+                }
         }
     } else {
-        // elements past the tensor's end hold zeros (their gradient and moments were never read) and leave the maxima alone
-        unsigned mt = 0, vt = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            mt = max(mt, __float_as_uint(m[j]) & 0x7fffffffu);
-            vt = max(vt, __float_as_uint(v[j]) & 0x7fffffffu);
-        }
-        const unsigned me = block_exponent(__reduce_max_sync(0xffffffffu, mt));
-        const unsigned ve = block_exponent(__reduce_max_sync(0xffffffffu, vt));
+        // elements past the tensor's end hold zeros (their gradient and codes were never read) and leave the maxima alone
+        const unsigned me = block_exponent(mt), ve = block_exponent(vt);
         const float mi = __uint_as_float((254u - min(me, 253u)) << 23), vi = __uint_as_float((254u - min(ve, 253u)) << 23);
+        const unsigned lo = static_cast<unsigned>(at), hi_term = static_cast<unsigned>(at >> 32) * 0x9E3779B9u;
         unsigned mc[8], vc[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned r = element_hash(static_cast<unsigned long long>(at) + lane_elem<VECTOR>(lane, j), p.key);
-            mc[j] = encode(fabsf(m[j]), mi, 1.f / SOFTSYNC_M_UNIT, (r & 0xffffu) << 3, kMaxCodeM) | (m[j] < 0.f ? 128u : 0u);
-            vc[j] = encode(v[j], vi, 1.f / SOFTSYNC_V_UNIT, (r >> 16) << 3, kMaxCodeV);
-            if (v[j] > 0.f) vc[j] = max(vc[j], 1u);
+        for (int k = 0; k < 4; ++k) {
+            const float2 a = mul2(mul2(make_float2(fabsf(m[k].x), fabsf(m[k].y)), two(mi)), two(1.f / SOFTSYNC_M_UNIT));
+            const float2 b = mul2(mul2(v[k], two(vi)), two(1.f / SOFTSYNC_V_UNIT));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int j = 2 * k + i;
+                const unsigned r = element_hash(lo + lane_elem<VECTOR>(lane, j), hi_term, p.key);
+                const float mj = i ? m[k].y : m[k].x, vj = i ? v[k].y : v[k].x;
+                mc[j] = code_of(i ? a.y : a.x, (r & 0xffffu) << 3, kMaxCodeM) | (mj < 0.f ? 128u : 0u);
+                vc[j] = max(code_of(i ? b.y : b.x, (r >> 16) << 3, kMaxCodeV), vj > 0.f ? 1u : 0u);
+            }
         }
         unsigned char *mp = static_cast<unsigned char *>(p.m) + at, *vp = static_cast<unsigned char *>(p.v) + at;
         if constexpr (VECTOR) {
@@ -380,7 +467,7 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
 }
 
 template <typename GT, int BITS, int MAXP>
-__global__ void __launch_bounds__(kListThreads) adamw_kernel(const __grid_constant__ ListTables lt,
+__global__ void __launch_bounds__(kListThreads, 4) adamw_kernel(const __grid_constant__ ListTables lt,
                                                              const __grid_constant__ GradTable<MAXP> tab,
                                                              const __grid_constant__ AdamwParams p)
 {
@@ -411,11 +498,9 @@ static __global__ void moments_kernel(const unsigned *m, const unsigned *v, cons
     if (i >= quads) return;
     const float a = block_scale(ms[i / (kStateBlock / 4)]), b = block_scale(vs[i / (kStateBlock / 4)]);
     const unsigned x = m[i], y = v[i];
-    float p[4], q[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) { p[k] = decode_m((x >> (8 * k)) & 255u, a); q[k] = decode_v((y >> (8 * k)) & 255u, b); }
-    __stcs(m_out + i, make_uint2(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])));
-    __stcs(v_out + i, make_uint2(pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3])));
+    const auto pack = [](float2 p, float2 q) { return make_uint2(pack_bf16x2(p.x, p.y), pack_bf16x2(q.x, q.y)); };
+    __stcs(m_out + i, pack(decode_pair<true>(x, 0, a), decode_pair<true>(x, 2, a)));
+    __stcs(v_out + i, pack(decode_pair<false>(y, 0, b), decode_pair<false>(y, 2, b)));
 }
 
 }  // namespace softsync

@@ -312,6 +312,7 @@ int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, cons
     p.one_minus_beta2 = static_cast<float>(1.0 - k.beta2);
     p.root_scale = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(k.beta2, t)));
     p.eps = static_cast<float>(k.eps);
+    p.short_forms = p.eps >= 0x1p-40f && p.root_scale <= 0x1p10f;
     p.key = step_key(k.seed, static_cast<uint64_t>(k.step));
     DeviceSwitch guard(list->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -11,6 +11,7 @@
 // exponential unit close behind: it gives 16 results a clock and SM, and at 7 TB/s 12 of them are wanted in either case.
 #pragma once
 
+#include "packed.cuh"
 #include "update_kernels.cuh"
 
 #include <math_constants.h>
@@ -74,26 +75,6 @@ __device__ __forceinline__ float warp_sum(float x)
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long *>(&a)),
-        "l"(*reinterpret_cast<unsigned long long *>(&b)), "l"(*reinterpret_cast<unsigned long long *>(&c)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    unsigned long long r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-
 // ---- 16-byte vectors of a row ------------------------------------------------------------------------------------------
 template <typename GT> __host__ __device__ constexpr int logit_bytes() { return sizeof(Raw<GT, 1>); }
 template <typename GT> __host__ __device__ constexpr int per_vector() { return 16 / logit_bytes<GT>(); }
