@@ -137,33 +137,95 @@ __device__ __forceinline__ double block_sum(double x, double *scratch)
     return y;
 }
 
-// Sum of squares of the weighted sum.  Each block walks every gridDim.x-th chunk; a block's sum goes to its own place, and the
-// block that finishes last adds the places up in their order, so no result depends on which block came first.
+// Eight consecutive elements of a gradient.
+template <typename GT> struct Raw8;
+template <> struct Raw8<GradFp32> { float4 a, b; };
+template <> struct Raw8<GradBf16> { float4 a; };
+__device__ __forceinline__ void load8(Raw8<GradFp32> &r, const unsigned char *p) { r.a = ld_stream_f4(reinterpret_cast<const float4 *>(p)); r.b = ld_stream_f4(reinterpret_cast<const float4 *>(p) + 1); }
+__device__ __forceinline__ void load8(Raw8<GradBf16> &r, const unsigned char *p) { r.a = ld_stream_f4(reinterpret_cast<const float4 *>(p)); }
+__device__ __forceinline__ float2 pair_of(const Raw8<GradFp32> &r, int k)
+{ return k == 0 ? make_float2(r.a.x, r.a.y) : k == 1 ? make_float2(r.a.z, r.a.w) : k == 2 ? make_float2(r.b.x, r.b.y) : make_float2(r.b.z, r.b.w); }
+__device__ __forceinline__ float2 pair_of(const Raw8<GradBf16> &r, int k)
+{
+    const unsigned w = __float_as_uint(k == 0 ? r.a.x : k == 1 ? r.a.y : k == 2 ? r.a.z : r.a.w);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+constexpr int kNormUnroll = 4;
+
+// Adds the squares of the weighted sum of the c gradients over elements [first, end) of tensor t to sq.  Where the gradients lie on the
+// 16-byte grid a thread has four loads of eight elements under way at a time, else (and at the end) single elements.
 template <typename GT, int MAXP>
-__global__ void __launch_bounds__(kListThreads) grad_norm_kernel(const __grid_constant__ ListTables lt,
-                                                                 const __grid_constant__ GradTable<MAXP> tab,
-                                                                 const __grid_constant__ NormTail tail)
+__device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAXP> &tab, int t, long long first, long long end)
+{
+    constexpr int GB = GradBytes<GT>::value, U = kNormUnroll;
+    const void *const *row = tab.g + (t - tab.t0) * tab.c;
+    bool on_grid = true;
+    for (int l = 0; l < tab.c; ++l) on_grid = on_grid && (reinterpret_cast<uintptr_t>(row[l]) & 15) == 0;        // first is a multiple of kChunk
+    long long at = first;
+    if (on_grid) {
+        for (; at + U * kChunk <= end; at += U * kChunk) {
+            float2 acc[U][4];
+            for (int l = 0; l < tab.c; ++l) {
+                const unsigned char *p = static_cast<const unsigned char *>(row[l]) + (at + threadIdx.x * 8) * GB;
+                const float2 s = make_float2(tab.s[l], tab.s[l]);
+                Raw8<GT> r[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) load8(r[u], p + u * kChunk * GB);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 x = mul2(s, pair_of(r[u], k));
+                        acc[u][k] = l == 0 ? x : make_float2(__fadd_rn(acc[u][k].x, x.x), __fadd_rn(acc[u][k].y, x.y));
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sq[k] = fma2(acc[u][k], acc[u][k], sq[k]);
+        }
+    }
+    for (; at < end; at += kListThreads * 8) {
+        float g[8] = {};
+        for (int l = 0; l < tab.c; ++l)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const long long e = at + j * kListThreads + threadIdx.x;
+                if (e >= end) continue;
+                Raw<GT, 1> r;
+                float x[1];
+                load_raw(r, row[l], e);
+                widen(r, x);
+                g[j] = l == 0 ? __fmul_rn(tab.s[l], x[0]) : __fadd_rn(g[j], __fmul_rn(tab.s[l], x[0]));
+            }
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) sq[j / 2] = fma2(make_float2(g[j], g[j + 1]), make_float2(g[j], g[j + 1]), sq[j / 2]);
+    }
+}
+
+// Sum of squares of the weighted sum.  The chunks are dealt out in runs of equal length, one a block, so a block looks a tensor up
+// once and then streams.  A block's sum goes to its own place, and the block that finishes last adds the places up in their order, so
+// no result depends on which block came first.
+template <typename GT, int MAXP>
+__global__ void __launch_bounds__(kListThreads, 3) grad_norm_kernel(const __grid_constant__ ListTables lt,
+                                                                    const __grid_constant__ GradTable<MAXP> tab,
+                                                                    const __grid_constant__ NormTail tail)
 {
     __shared__ double scratch[kListThreads / 32];
     __shared__ bool finish;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float sq[8] = {};
-    for (long long k = blockIdx.x; k < lt.nchunks; k += gridDim.x) {
+    const long long from = lt.nchunks * blockIdx.x / gridDim.x, to = lt.nchunks * (blockIdx.x + 1) / gridDim.x;
+    double mine = 0;
+    for (long long k = from; k < to;) {
         const int t = lt.chunk_tensor[lt.chunk0 + k];
         const TensorRec &rec = lt.recs[t];
-        const long long first = (lt.chunk0 + k - rec.first_chunk) * kChunk + warp * kStateBlock;
-        const long long left = rec.n - first;
-        if (left <= 0) continue;
-        const int count = left < kStateBlock ? static_cast<int>(left) : kStateBlock;
-        float g[8];
-        if (count == kStateBlock && grads_on_grid<GT>(tab, t)) weighted_gradient<GT, true>(g, tab, t, first, lane, count);
-        else weighted_gradient<GT, false>(g, tab, t, first, lane, count);
+        const long long n = rec.n, chunk = lt.chunk0 + k - rec.first_chunk, chunks = min((n + kChunk - 1) / kChunk - chunk, to - k);
+        float2 sq[4] = {};
+        add_squares<GT>(sq, tab, t, chunk * kChunk, min(n, (chunk + chunks) * kChunk));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sq[j] = fmaf(g[j], g[j], sq[j]);
+        for (int j = 0; j < 4; ++j) mine += static_cast<double>(sq[j].x) + static_cast<double>(sq[j].y);
+        k += chunks;
     }
-    double mine = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) mine += sq[j];
     const double sum = block_sum(mine, scratch);
     if (threadIdx.x == 0) {
         tail.partial[blockIdx.x] = tail.add ? tail.partial[blockIdx.x] + sum : sum;
@@ -192,7 +254,6 @@ __global__ void __launch_bounds__(kListThreads) grad_norm_kernel(const __grid_co
 // multiplication scales exactly, so the formats' own subnormals need no case of their own; the way back is the same
 // multiplication, and what lies below the kept bits is where the random number is added.
 constexpr int kDropBits = 19;                                            // 23 fraction bits of fp32 less the 4 kept
-constexpr unsigned kMaxCodeM = 127, kMaxCodeV = 255;
 #define SOFTSYNC_M_UNIT 0x1p120f                                         // first moment: exponent bias 7 = 127 - 120
 #define SOFTSYNC_V_UNIT 0x1p112f                                         // second moment: bias 15 = 127 - 112
 
@@ -200,26 +261,27 @@ constexpr unsigned kMaxCodeM = 127, kMaxCodeV = 255;
 template <bool SIGNED>
 __device__ __forceinline__ float code_top(unsigned four, int k)
 {
-    const unsigned top = four << (24 - 8 * k);
-    return __uint_as_float(SIGNED ? static_cast<unsigned>(static_cast<int>(top) >> 5) & 0x83f80000u : (top >> 5) & 0x07f80000u);
+    const unsigned top = __byte_perm(four, 0, k << 12 | 0x0444);          // the code in the highest byte
+    return __uint_as_float(SIGNED ? static_cast<unsigned>(static_cast<int>(top) >> (24 - kDropBits)) & 0x83f80000u : top >> (24 - kDropBits));
 }
+template <bool SIGNED>
+__device__ __forceinline__ float2 code_pair(unsigned four, int k) { return make_float2(code_top<SIGNED>(four, k), code_top<SIGNED>(four, k + 1)); }
 template <bool SIGNED>
 __device__ __forceinline__ float2 decode_pair(unsigned four, int k, float scale)
 {
     const float unit = SIGNED ? SOFTSYNC_M_UNIT : SOFTSYNC_V_UNIT;
-    return mul2(mul2(make_float2(code_top<SIGNED>(four, k), code_top<SIGNED>(four, k + 1)), make_float2(unit, unit)), make_float2(scale, scale));
+    return mul2(mul2(code_pair<SIGNED>(four, k), make_float2(unit, unit)), make_float2(scale, scale));
 }
 __device__ __forceinline__ float block_scale(unsigned e) { return __uint_as_float(e << 23); }
 
 // Exponent byte of a block whose largest magnitude has the bits `top`: the largest code is 31/16 of the power of two, so from
-// there on the next one is taken; 255 marks a block that met an infinity or a NaN.
+// there on the next one is taken (and no code ever exceeds the largest).  255 marks a block that met an infinity, a NaN or, like them
+// beyond the format, 31/16 * 2^126.
 __device__ __forceinline__ unsigned block_exponent(unsigned top)
 {
-    if (top >= 0x7f800000u) return 255u;
-    return min(max((top + (1u << kDropBits)) >> 23, 27u), 253u);
+    const unsigned e = (top + (1u << kDropBits)) >> 23;
+    return e > 253u ? 255u : max(e, 27u);
 }
-// The code of a magnitude whose scaled fp32 bits are given.
-__device__ __forceinline__ unsigned code_of(float scaled, unsigned rnd, unsigned top) { return min((__float_as_uint(scaled) + rnd) >> kDropBits, top); }
 
 // 32 random bits for the element whose place has the low word lo; hi_term: its high word times 0x9E3779B9.  An integer hash (two rounds
 // of xor-shift and multiply) of the place and the step's key.
@@ -265,7 +327,8 @@ struct AdamwParams {
     unsigned char *m_scale, *v_scale;
     const float *clip;                    // nullptr: none
     double lr_decay, step_size;           // lr * weight_decay; lr / (1 - beta1^t)
-    float beta1, one_minus_beta1, beta2, one_minus_beta2, root_scale, eps;
+    float2 beta1, one_minus_beta1, beta2, one_minus_beta2;               // each twice: one 64-bit operand of a packed multiply
+    float root_scale, eps;
     unsigned key;
     int short_forms;                      // eps allows the short root and quotient
 };
@@ -278,7 +341,7 @@ constexpr unsigned kMLimit = 0x49800000u, kVLimit = 0x4e800000u;         // bits
 
 template <typename GT, int BITS, bool VECTOR, int MAXP>
 __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTable<MAXP> &tab, const TensorRec &rec, int t,
-                                            long long first, int lane, int count, float clip)
+                                            long long first, int lane, int count, float clip, float decay, float step)
 {
     float g[8];
     float2 w[4], m[4], v[4];
@@ -354,20 +417,18 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
         }
     }
 
-    const float decay = static_cast<float>(1.0 - p.lr_decay * (static_cast<double>(rec.lr_mult) * rec.decay_mult));
-    const float step = static_cast<float>(p.step_size * rec.lr_mult);
     const auto two = [](float x) { return make_float2(x, x); };
     unsigned mt = 0, vt = 0;                             // the largest magnitudes, as bits
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         float2 x = make_float2(g[2 * k], g[2 * k + 1]);
         if (p.clip) x = mul2(x, two(clip));
-        const float2 a = mul2(m[k], two(p.beta1)), b = mul2(x, two(p.one_minus_beta1));
-        const float2 c = mul2(v[k], two(p.beta2)), d = mul2(mul2(x, x), two(p.one_minus_beta2));
+        const float2 a = mul2(m[k], p.beta1), b = mul2(x, p.one_minus_beta1);
+        const float2 c = mul2(v[k], p.beta2), d = mul2(mul2(x, x), p.one_minus_beta2);
         m[k] = make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
         v[k] = make_float2(__fadd_rn(c.x, d.x), __fadd_rn(c.y, d.y));
         mt = max(mt, max(__float_as_uint(m[k].x) & 0x7fffffffu, __float_as_uint(m[k].y) & 0x7fffffffu));
-        vt = max(vt, max(__float_as_uint(v[k].x) & 0x7fffffffu, __float_as_uint(v[k].y) & 0x7fffffffu));
+        vt = max(vt, max(__float_as_uint(v[k].x), __float_as_uint(v[k].y)));           // never below zero
     }
     if constexpr (BITS == 8) { mt = __reduce_max_sync(0xffffffffu, mt); vt = __reduce_max_sync(0xffffffffu, vt); }
     if (__all_sync(0xffffffffu, p.short_forms && fabsf(step) >= 0x1p-40f && mt < kMLimit && vt < kVLimit)) {
@@ -430,33 +491,44 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
         const unsigned me = block_exponent(mt), ve = block_exponent(vt);
         const float mi = __uint_as_float((254u - min(me, 253u)) << 23), vi = __uint_as_float((254u - min(ve, 253u)) << 23);
         const unsigned lo = static_cast<unsigned>(at), hi_term = static_cast<unsigned>(at >> 32) * 0x9E3779B9u;
-        unsigned mc[8], vc[8];
+        unsigned mc[2], vc[2];                           // four codes a word
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 a = mul2(mul2(make_float2(fabsf(m[k].x), fabsf(m[k].y)), two(mi)), two(1.f / SOFTSYNC_M_UNIT));
-            const float2 b = mul2(mul2(v[k], two(vi)), two(1.f / SOFTSYNC_V_UNIT));
+        for (int h = 0; h < 2; ++h) {
+            unsigned mtop[4], vtop[4];                   // each code in its number's highest byte
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int j = 2 * k + i;
+            for (int i = 0; i < 4; ++i) {
+                const int j = 4 * h + i;
+                const float mj = j & 1 ? m[j / 2].y : m[j / 2].x, vj = j & 1 ? v[j / 2].y : v[j / 2].x;
                 const unsigned r = element_hash(lo + lane_elem<VECTOR>(lane, j), hi_term, p.key);
-                const float mj = i ? m[k].y : m[k].x, vj = i ? v[k].y : v[k].x;
-                mc[j] = code_of(i ? a.y : a.x, (r & 0xffffu) << 3, kMaxCodeM) | (mj < 0.f ? 128u : 0u);
-                vc[j] = max(code_of(i ? b.y : b.x, (r >> 16) << 3, kMaxCodeV), vj > 0.f ? 1u : 0u);
+                // 16 random bits right below the kept ones, and 3 zeros: the sum's carry does the rounding
+                const unsigned low = __byte_perm(r, 0, 0x4104), high = __byte_perm(r, 0, 0x4324);
+                mtop[i] = (__float_as_uint(__fmul_rn(__fmul_rn(fabsf(mj), mi), 1.f / SOFTSYNC_M_UNIT)) << (24 - kDropBits)) + low;
+                if (mj < 0.f) mtop[i] |= 0x80000000u;
+                vtop[i] = (__float_as_uint(__fmul_rn(__fmul_rn(vj, vi), 1.f / SOFTSYNC_V_UNIT)) << (24 - kDropBits)) + high;
+            }
+            mc[h] = __byte_perm(__byte_perm(mtop[0], mtop[1], 0x0073), __byte_perm(mtop[2], mtop[3], 0x0073), 0x5410);
+            vc[h] = __byte_perm(__byte_perm(vtop[0], vtop[1], 0x0073), __byte_perm(vtop[2], vtop[3], 0x0073), 0x5410);
+            if ((vc[h] - 0x01010101u) & ~vc[h] & 0x80808080u) {          // a zero code among them: it stays one only for a v of zero
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = 4 * h + i;
+                    if (!(vc[h] & 255u << (8 * i)) && (j & 1 ? v[j / 2].y : v[j / 2].x) > 0.f) vc[h] |= 1u << (8 * i);
+                }
             }
         }
         unsigned char *mp = static_cast<unsigned char *>(p.m) + at, *vp = static_cast<unsigned char *>(p.v) + at;
         if constexpr (VECTOR) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                __stcs(reinterpret_cast<unsigned *>(mp) + h * 32 + lane, mc[4 * h] | mc[4 * h + 1] << 8 | mc[4 * h + 2] << 16 | mc[4 * h + 3] << 24);
-                __stcs(reinterpret_cast<unsigned *>(vp) + h * 32 + lane, vc[4 * h] | vc[4 * h + 1] << 8 | vc[4 * h + 2] << 16 | vc[4 * h + 3] << 24);
+                __stcs(reinterpret_cast<unsigned *>(mp) + h * 32 + lane, mc[h]);
+                __stcs(reinterpret_cast<unsigned *>(vp) + h * 32 + lane, vc[h]);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j * 32 + lane < count) {
-                    mp[j * 32 + lane] = static_cast<unsigned char>(mc[j]);
-                    vp[j * 32 + lane] = static_cast<unsigned char>(vc[j]);
+                    mp[j * 32 + lane] = static_cast<unsigned char>(mc[j / 4] >> (8 * (j & 3)));
+                    vp[j * 32 + lane] = static_cast<unsigned char>(vc[j / 4] >> (8 * (j & 3)));
                 }
         }
         if (lane == 0) {
@@ -483,10 +555,12 @@ __global__ void __launch_bounds__(kListThreads, 4) adamw_kernel(const __grid_con
         if (!(fabsf(p.clip[0]) <= 3.402823466e38f)) return;          // the norm is not finite: the step changes nothing
         clip = p.clip[1];
     }
+    const bool on_grid = (reinterpret_cast<uintptr_t>(rec.w) & 15) == 0 && (reinterpret_cast<uintptr_t>(rec.mirror) & 7) == 0 && grads_on_grid<GT>(tab, t);
+    const float decay = static_cast<float>(1.0 - p.lr_decay * (static_cast<double>(rec.lr_mult) * rec.decay_mult));
+    const float step = static_cast<float>(p.step_size * rec.lr_mult);
     const int count = left < kStateBlock ? static_cast<int>(left) : kStateBlock;
-    const bool grid = (reinterpret_cast<uintptr_t>(rec.w) & 15) == 0 && (reinterpret_cast<uintptr_t>(rec.mirror) & 7) == 0;
-    if (count == kStateBlock && grid && grads_on_grid<GT>(tab, t)) adamw_block<GT, BITS, true>(p, tab, rec, t, first, lane, count, clip);
-    else adamw_block<GT, BITS, false>(p, tab, rec, t, first, lane, count, clip);
+    if (count == kStateBlock && on_grid) adamw_block<GT, BITS, true>(p, tab, rec, t, first, lane, count, clip, decay, step);
+    else adamw_block<GT, BITS, false>(p, tab, rec, t, first, lane, count, clip, decay, step);
 }
 
 // Codes to the values they stand for.  One thread per four elements of the state arrays, the gaps between the tensors included

@@ -29,7 +29,7 @@ static_assert(kStateBlock == PS_STATE_BLOCK, "the header's block is the kernels'
 
 namespace {
 
-constexpr int kNormBlocksPerSm = 8;
+constexpr int kNormBlocksPerSm = 6;
 constexpr int kNormMaxBlocks = 4096;
 constexpr int kSmallTable = 32, kMediumTable = 512, kLargeTable = 3840;   // gradient pointers one launch carries
 
@@ -306,10 +306,11 @@ int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, cons
     p.clip = clip_dev;
     p.lr_decay = k.lr * k.weight_decay;
     p.step_size = k.lr / (1.0 - std::pow(k.beta1, t));
-    p.beta1 = static_cast<float>(k.beta1);
-    p.one_minus_beta1 = static_cast<float>(1.0 - k.beta1);
-    p.beta2 = static_cast<float>(k.beta2);
-    p.one_minus_beta2 = static_cast<float>(1.0 - k.beta2);
+    const auto twice = [](double x) { return make_float2(static_cast<float>(x), static_cast<float>(x)); };
+    p.beta1 = twice(k.beta1);
+    p.one_minus_beta1 = twice(1.0 - k.beta1);
+    p.beta2 = twice(k.beta2);
+    p.one_minus_beta2 = twice(1.0 - k.beta2);
     p.root_scale = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(k.beta2, t)));
     p.eps = static_cast<float>(k.eps);
     p.short_forms = p.eps >= 0x1p-40f && p.root_scale <= 0x1p10f;
