@@ -75,11 +75,12 @@ typedef struct ps_adamw_config {
  * fraction bits with bias 7, v 4 exponent bits and 4 fraction bits with bias 15, both with subnormals.  The step computes with the
  * fp32 values and rounds what it keeps at random to one of the two neighbours, so that the expectation stays: an average
  * that moves by less than half a code step would otherwise never move.  A v above zero keeps at least the smallest code, so that no
- * quotient loses its denominator.  A block that meets an infinity or a NaN decodes as such from then on. */
+ * quotient loses its denominator.  A block that meets an infinity, a NaN or
+ * a magnitude of 31/16 * 2^126 decodes to infinities and NaN from then on. */
 int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, const float *scales_host, int grad_dtype,
                   const ps_adamw_config *config, const float *clip_dev, void *stream);
 
-/* The bound 8-bit moments as the values they stand for, exactly, in bf16 state arrays (8-byte aligned).  state_bits 8 only. */
+/* The bound 8-bit moments as the values they stand for, exactly, in bf16 state arrays (16-byte aligned).  state_bits 8 only. */
 int ps_adamw_moments(ps_tensors_t *list, void *m_bf16_dev, void *v_bf16_dev, void *stream);
 
 /* ------------------------------------------------------------------------------------------------------------------

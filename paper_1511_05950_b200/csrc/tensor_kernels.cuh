@@ -254,8 +254,7 @@ __global__ void __launch_bounds__(kListThreads, 3) grad_norm_kernel(const __grid
 // multiplication scales exactly, so the formats' own subnormals need no case of their own; the way back is the same
 // multiplication, and what lies below the kept bits is where the random number is added.
 constexpr int kDropBits = 19;                                            // 23 fraction bits of fp32 less the 4 kept
-#define SOFTSYNC_M_UNIT 0x1p120f                                         // first moment: exponent bias 7 = 127 - 120
-#define SOFTSYNC_V_UNIT 0x1p112f                                         // second moment: bias 15 = 127 - 112
+// The units: 2^120 for the first moment (exponent bias 7 = 127 - 120), 2^112 for the second (15 = 127 - 112).
 
 // Code k (0..3) of four in a word, as the fp32 number whose top it is.
 template <bool SIGNED>
@@ -266,13 +265,30 @@ __device__ __forceinline__ float code_top(unsigned four, int k)
 }
 template <bool SIGNED>
 __device__ __forceinline__ float2 code_pair(unsigned four, int k) { return make_float2(code_top<SIGNED>(four, k), code_top<SIGNED>(four, k + 1)); }
+// What a block's codes are multiplied with: unit and scale in one as far as that is a number, the rest in `more` (1 for all but blocks
+// whose values pass 2^7 or 2^15; infinity for a marked one).
 template <bool SIGNED>
-__device__ __forceinline__ float2 decode_pair(unsigned four, int k, float scale)
-{
-    const float unit = SIGNED ? SOFTSYNC_M_UNIT : SOFTSYNC_V_UNIT;
-    return mul2(mul2(code_pair<SIGNED>(four, k), make_float2(unit, unit)), make_float2(scale, scale));
-}
-__device__ __forceinline__ float block_scale(unsigned e) { return __uint_as_float(e << 23); }
+struct BlockScale {
+    float scale, more;
+    __device__ __forceinline__ explicit BlockScale(unsigned e)
+    {
+        constexpr unsigned unit = SIGNED ? 120 : 112;
+        scale = __uint_as_float(min(e + unit, 254u) << 23);
+        more = e == 255u ? CUDART_INF_F : __uint_as_float(max(e + unit, 254u) - 127u << 23);
+    }
+    // four pairs of codes in two words
+    __device__ __forceinline__ void decode(float2 (&x)[4], unsigned a, unsigned b) const
+    {
+        const float2 s = make_float2(scale, scale);
+        x[0] = mul2(code_pair<SIGNED>(a, 0), s);
+        x[1] = mul2(code_pair<SIGNED>(a, 2), s);
+        x[2] = mul2(code_pair<SIGNED>(b, 0), s);
+        x[3] = mul2(code_pair<SIGNED>(b, 2), s);
+        if (more != 1.f)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], make_float2(more, more));
+    }
+};
 
 // Exponent byte of a block whose largest magnitude has the bits `top`: the largest code is 31/16 of the power of two, so from
 // there on the next one is taken (and no code ever exceeds the largest).  255 marks a block that met an infinity, a NaN or, like them
@@ -302,7 +318,7 @@ __device__ __forceinline__ float2 rounded_sqrt(float2 v)
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(v.x));
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(v.y));
     const float2 half = make_float2(0.5f, 0.5f);
-    float2 g = mul2(v, y), h = mul2(y, half);
+    float2 g = mul2(v, y), h = mul2(y, half);            // root, and half its reciprocal
     const float2 r = fma2(make_float2(-g.x, -g.y), h, half);
     g = fma2(g, r, g);
     h = fma2(h, r, h);
@@ -313,11 +329,11 @@ __device__ __forceinline__ float2 rounded_quotient(float2 a, float2 b)
     float2 y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(b.x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(b.y));
-    const float2 nb = make_float2(-b.x, -b.y);
-    y = fma2(fma2(nb, y, make_float2(1.f, 1.f)), y, y);
+    const float2 minus_b = make_float2(-b.x, -b.y);
+    y = fma2(fma2(minus_b, y, make_float2(1.f, 1.f)), y, y);
     float2 q = mul2(a, y);
-    q = fma2(fma2(nb, q, a), y, q);
-    return fma2(fma2(nb, q, a), y, q);
+    q = fma2(fma2(minus_b, q, a), y, q);
+    return fma2(fma2(minus_b, q, a), y, q);
 }
 
 // ---- AdamW -------------------------------------------------------------------------------------------------------------
@@ -348,7 +364,7 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
     const long long at = rec.state_off + first;          // a multiple of kStateBlock
     float *wp = rec.w + first;
     unsigned mcodes[2], vcodes[2];
-    float ms = 0.f, vs = 0.f;
+    unsigned me = 0, ve = 0;
     if constexpr (VECTOR) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -380,8 +396,8 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
         }
     } else {
         const unsigned char *mp = static_cast<const unsigned char *>(p.m) + at, *vp = static_cast<const unsigned char *>(p.v) + at;
-        ms = block_scale(p.m_scale[at / kStateBlock]);
-        vs = block_scale(p.v_scale[at / kStateBlock]);
+        me = p.m_scale[at / kStateBlock];
+        ve = p.v_scale[at / kStateBlock];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if constexpr (VECTOR) {
@@ -402,12 +418,9 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
     }
     weighted_gradient<GT, VECTOR>(g, tab, t, first, lane, count);
     if constexpr (BITS == 8) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            m[k] = decode_pair<true>(mcodes[k / 2], 2 * (k & 1), ms);
-            v[k] = decode_pair<false>(vcodes[k / 2], 2 * (k & 1), vs);
-        }
-        if (count < kStateBlock && (!(ms < CUDART_INF_F) || !(vs < CUDART_INF_F))) {       // a marked block: zero codes are NaN there, but not past the end
+        BlockScale<true>(me).decode(m, mcodes[0], mcodes[1]);
+        BlockScale<false>(ve).decode(v, vcodes[0], vcodes[1]);
+        if (count < kStateBlock && (me == 255u || ve == 255u)) {       // a marked block: zero codes are NaN there, but not past the end
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (lane_elem<VECTOR>(lane, j) >= count) {
@@ -488,8 +501,17 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
         }
     } else {
         // elements past the tensor's end hold zeros (their gradient and codes were never read) and leave the maxima alone
-        const unsigned me = block_exponent(mt), ve = block_exponent(vt);
-        const float mi = __uint_as_float((254u - min(me, 253u)) << 23), vi = __uint_as_float((254u - min(ve, 253u)) << 23);
+        me = block_exponent(mt);
+        ve = block_exponent(vt);
+        // to the codes' units: one factor unless the block's values pass 2^6 or 2^14 (the first product is then exact, or below every code)
+        if (me > 133u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) m[k] = mul2(m[k], two(0x1p-120f));
+        if (ve > 141u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], two(0x1p-112f));
+        const float mi = __uint_as_float((me > 133u ? 254u - min(me, 253u) : 134u - me) << 23);
+        const float vi = __uint_as_float((ve > 141u ? 254u - min(ve, 253u) : 142u - ve) << 23);
         const unsigned lo = static_cast<unsigned>(at), hi_term = static_cast<unsigned>(at >> 32) * 0x9E3779B9u;
         unsigned mc[2], vc[2];                           // four codes a word
 #pragma unroll
@@ -502,9 +524,9 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
                 const unsigned r = element_hash(lo + lane_elem<VECTOR>(lane, j), hi_term, p.key);
                 // 16 random bits right below the kept ones, and 3 zeros: the sum's carry does the rounding
                 const unsigned low = __byte_perm(r, 0, 0x4104), high = __byte_perm(r, 0, 0x4324);
-                mtop[i] = (__float_as_uint(__fmul_rn(__fmul_rn(fabsf(mj), mi), 1.f / SOFTSYNC_M_UNIT)) << (24 - kDropBits)) + low;
-                if (mj < 0.f) mtop[i] |= 0x80000000u;
-                vtop[i] = (__float_as_uint(__fmul_rn(__fmul_rn(vj, vi), 1.f / SOFTSYNC_V_UNIT)) << (24 - kDropBits)) + high;
+                mtop[i] = (__float_as_uint(__fmul_rn(fabsf(mj), mi)) << (24 - kDropBits)) + low;
+                mtop[i] |= __float_as_uint(mj) & 0x80000000u;
+                vtop[i] = (__float_as_uint(__fmul_rn(vj, vi)) << (24 - kDropBits)) + high;
             }
             mc[h] = __byte_perm(__byte_perm(mtop[0], mtop[1], 0x0073), __byte_perm(mtop[2], mtop[3], 0x0073), 0x5410);
             vc[h] = __byte_perm(__byte_perm(vtop[0], vtop[1], 0x0073), __byte_perm(vtop[2], vtop[3], 0x0073), 0x5410);
@@ -563,18 +585,20 @@ __global__ void __launch_bounds__(kListThreads, 4) adamw_kernel(const __grid_con
     else adamw_block<GT, BITS, false>(p, tab, rec, t, first, lane, count, clip, decay, step);
 }
 
-// Codes to the values they stand for.  One thread per four elements of the state arrays, the gaps between the tensors included
+// Codes to the values they stand for.  One thread per eight elements of the state arrays, the gaps between the tensors included
 // (they hold zeros there, or what the caller put there: the output's gaps are the caller's too).
-static __global__ void moments_kernel(const unsigned *m, const unsigned *v, const unsigned char *ms, const unsigned char *vs,
-                               uint2 *m_out, uint2 *v_out, long long quads)
+static __global__ void moments_kernel(const uint2 *m, const uint2 *v, const unsigned char *m_scale, const unsigned char *v_scale,
+                                      uint4 *m_out, uint4 *v_out, long long eights)
 {
     const long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
-    if (i >= quads) return;
-    const float a = block_scale(ms[i / (kStateBlock / 4)]), b = block_scale(vs[i / (kStateBlock / 4)]);
-    const unsigned x = m[i], y = v[i];
-    const auto pack = [](float2 p, float2 q) { return make_uint2(pack_bf16x2(p.x, p.y), pack_bf16x2(q.x, q.y)); };
-    __stcs(m_out + i, pack(decode_pair<true>(x, 0, a), decode_pair<true>(x, 2, a)));
-    __stcs(v_out + i, pack(decode_pair<false>(y, 0, b), decode_pair<false>(y, 2, b)));
+    if (i >= eights) return;
+    const uint2 x = __ldcs(m + i), y = __ldcs(v + i);
+    float2 a[4], b[4];
+    BlockScale<true>(m_scale[i / (kStateBlock / 8)]).decode(a, x.x, x.y);
+    BlockScale<false>(v_scale[i / (kStateBlock / 8)]).decode(b, y.x, y.y);
+    const auto pack = [](const float2 &q) { return pack_bf16x2(q.x, q.y); };
+    __stcs(m_out + i, make_uint4(pack(a[0]), pack(a[1]), pack(a[2]), pack(a[3])));
+    __stcs(v_out + i, make_uint4(pack(b[0]), pack(b[1]), pack(b[2]), pack(b[3])));
 }
 
 }  // namespace softsync

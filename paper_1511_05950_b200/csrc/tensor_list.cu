@@ -338,14 +338,14 @@ int ps_adamw_moments(ps_tensors_t *list, void *m_bf16_dev, void *v_bf16_dev, voi
   try {
     if (!is_live(list)) return PS_ERR_INVALID_ARG;
     if (list->state_bits != 8) return PS_ERR_NO_STATE;
-    if (!m_bf16_dev || !v_bf16_dev || m_bf16_dev == v_bf16_dev || !aligned_to(m_bf16_dev, 8) || !aligned_to(v_bf16_dev, 8)) return PS_ERR_INVALID_ARG;
-    const int64_t quads = list->state_elems / 4;
-    if (!quads) return PS_OK;
-    if ((quads + 255) / 256 > 0x7fffffff) return PS_ERR_INVALID_ARG;
+    if (!m_bf16_dev || !v_bf16_dev || m_bf16_dev == v_bf16_dev || !aligned_to(m_bf16_dev, 16) || !aligned_to(v_bf16_dev, 16)) return PS_ERR_INVALID_ARG;
+    const int64_t eights = list->state_elems / 8;
+    if (!eights) return PS_OK;
+    if ((eights + 255) / 256 > 0x7fffffff) return PS_ERR_INVALID_ARG;
     DeviceSwitch guard(list->device);
-    softsync::moments_kernel<<<static_cast<unsigned>((quads + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(
-        static_cast<const unsigned *>(list->m), static_cast<const unsigned *>(list->v), list->m_scale, list->v_scale,
-        static_cast<uint2 *>(m_bf16_dev), static_cast<uint2 *>(v_bf16_dev), quads);
+    softsync::moments_kernel<<<static_cast<unsigned>((eights + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(
+        static_cast<const uint2 *>(list->m), static_cast<const uint2 *>(list->v), list->m_scale, list->v_scale,
+        static_cast<uint4 *>(m_bf16_dev), static_cast<uint4 *>(v_bf16_dev), eights);
     return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA;
   } PS_CATCH_ALL
 }
