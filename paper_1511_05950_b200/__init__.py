@@ -22,5 +22,6 @@ def __getattr__(name):
         return learn
     for module in (learn, binding):
         if hasattr(module, name):
-            return getattr(module, name)
+            globals()[name] = getattr(module, name)          # found once: later uses do not come here
+            return globals()[name]
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

@@ -151,22 +151,22 @@ __device__ __forceinline__ float2 pair_of(const Raw8<GradBf16> &r, int k)
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 
-constexpr int kNormUnroll = 4;
-
 // Adds the squares of the weighted sum of the c gradients over elements [first, end) of tensor t to sq.  Where the gradients lie on the
-// 16-byte grid a thread has four loads of eight elements under way at a time, else (and at the end) single elements.
-template <typename GT, int MAXP>
+// 16-byte grid a thread has several loads of eight elements under way at a time, else (and at the end) single elements, those
+// of four gradients together.  ONE: c = 1.
+template <typename GT, bool ONE, int MAXP>
 __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAXP> &tab, int t, long long first, long long end)
 {
-    constexpr int GB = GradBytes<GT>::value, U = kNormUnroll;
-    const void *const *row = tab.g + (t - tab.t0) * tab.c;
+    constexpr int GB = GradBytes<GT>::value, U = ONE && GB == 2 ? 8 : 4;
+    const int c = ONE ? 1 : tab.c;
+    const void *const *row = tab.g + (t - tab.t0) * c;
     bool on_grid = true;
-    for (int l = 0; l < tab.c; ++l) on_grid = on_grid && (reinterpret_cast<uintptr_t>(row[l]) & 15) == 0;        // first is a multiple of kChunk
+    for (int l = 0; l < c; ++l) on_grid = on_grid && (reinterpret_cast<uintptr_t>(row[l]) & 15) == 0;            // first is a multiple of kChunk
     long long at = first;
     if (on_grid) {
         for (; at + U * kChunk <= end; at += U * kChunk) {
-            float2 acc[U][4];
-            for (int l = 0; l < tab.c; ++l) {
+            float2 acc[ONE ? 1 : U][4];
+            for (int l = 0; l < c; ++l) {
                 const unsigned char *p = static_cast<const unsigned char *>(row[l]) + (at + threadIdx.x * 8) * GB;
                 const float2 s = make_float2(tab.s[l], tab.s[l]);
                 Raw8<GT> r[U];
@@ -177,28 +177,48 @@ __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAX
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float2 x = mul2(s, pair_of(r[u], k));
-                        acc[u][k] = l == 0 ? x : make_float2(__fadd_rn(acc[u][k].x, x.x), __fadd_rn(acc[u][k].y, x.y));
+                        if constexpr (ONE) sq[k] = fma2(x, x, sq[k]);
+                        else acc[u][k] = l == 0 ? x : make_float2(__fadd_rn(acc[u][k].x, x.x), __fadd_rn(acc[u][k].y, x.y));
                     }
             }
+            if constexpr (!ONE) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sq[k] = fma2(acc[u][k], acc[u][k], sq[k]);
+                    for (int k = 0; k < 4; ++k) sq[k] = fma2(acc[u][k], acc[u][k], sq[k]);
+            }
         }
     }
-    for (; at < end; at += kListThreads * 8) {
+    constexpr int G = ONE ? 1 : 4;
+#pragma unroll 1
+    for (; at < end; at += kChunk) {
         float g[8] = {};
-        for (int l = 0; l < tab.c; ++l)
+#pragma unroll 1
+        for (int l0 = 0; l0 < c; l0 += G) {
+            float x[G][8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const long long e = at + j * kListThreads + threadIdx.x;
-                if (e >= end) continue;
-                Raw<GT, 1> r;
-                float x[1];
-                load_raw(r, row[l], e);
-                widen(r, x);
-                g[j] = l == 0 ? __fmul_rn(tab.s[l], x[0]) : __fadd_rn(g[j], __fmul_rn(tab.s[l], x[0]));
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const long long e = at + j * kListThreads + threadIdx.x;
+                    float y[1] = {0.f};
+                    if (l0 + i < c && e < end) {
+                        Raw<GT, 1> r;
+                        load_raw(r, row[l0 + i], e);
+                        widen(r, y);
+                    }
+                    x[i][j] = y[0];
+                }
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                if (l0 + i >= c) break;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float y = __fmul_rn(tab.s[l0 + i], x[i][j]);
+                    g[j] = l0 + i == 0 ? y : __fadd_rn(g[j], y);
+                }
             }
+        }
 #pragma unroll
         for (int j = 0; j < 8; j += 2) sq[j / 2] = fma2(make_float2(g[j], g[j + 1]), make_float2(g[j], g[j + 1]), sq[j / 2]);
     }
@@ -207,7 +227,7 @@ __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAX
 // Sum of squares of the weighted sum.  The chunks are dealt out in runs of equal length, one a block, so a block looks a tensor up
 // once and then streams.  A block's sum goes to its own place, and the block that finishes last adds the places up in their order, so
 // no result depends on which block came first.
-template <typename GT, int MAXP>
+template <typename GT, bool ONE, int MAXP>
 __global__ void __launch_bounds__(kListThreads, 3) grad_norm_kernel(const __grid_constant__ ListTables lt,
                                                                     const __grid_constant__ GradTable<MAXP> tab,
                                                                     const __grid_constant__ NormTail tail)
@@ -221,7 +241,7 @@ __global__ void __launch_bounds__(kListThreads, 3) grad_norm_kernel(const __grid
         const TensorRec &rec = lt.recs[t];
         const long long n = rec.n, chunk = lt.chunk0 + k - rec.first_chunk, chunks = min((n + kChunk - 1) / kChunk - chunk, to - k);
         float2 sq[4] = {};
-        add_squares<GT>(sq, tab, t, chunk * kChunk, min(n, (chunk + chunks) * kChunk));
+        add_squares<GT, ONE>(sq, tab, t, chunk * kChunk, min(n, (chunk + chunks) * kChunk));
 #pragma unroll
         for (int j = 0; j < 4; ++j) mine += static_cast<double>(sq[j].x) + static_cast<double>(sq[j].y);
         k += chunks;

@@ -8,6 +8,8 @@ current stream of the tensors' device.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import itertools
 import threading
 from typing import List, NamedTuple, Optional, Sequence, Union
 
@@ -21,12 +23,12 @@ _numel, _is_contiguous, _get_device, _data_ptr = (torch.Tensor.numel, torch.Tens
 
 
 def _stream(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _on(device: torch.device):
     """Makes `device` current for a call that has no handle to remember it."""
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    return _HERE if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
 
 
 _HERE = B._NullCtx()
@@ -89,20 +91,18 @@ class TensorList:
         if c not in self._pointers:
             self._pointers[c] = ((C.c_void_p * (c * n))(), (C.c_float * c)())
         ptrs, factors = self._pointers[c]
-        dtypes, at = set(), 0
-        for gradient in grads:
-            if list(map(_numel, gradient)) != self.sizes:
-                raise ValueError("a gradient must have the list's %d tensors with %s elements" % (n, self.sizes if n < 20 else "its"))
-            if not all(map(_is_contiguous, gradient)):
-                raise ValueError("gradient tensors must be contiguous")
-            if set(map(_get_device, gradient)) != {self.device.index}:
-                raise ValueError("gradient tensors must live on the list's GPU, %s" % self.device)
-            dtypes.update([g.dtype for g in gradient])
-            ptrs[at:at + n] = list(map(_data_ptr, gradient))
-            at += n
+        flat = list(itertools.chain.from_iterable(grads))
+        if [len(gradient) for gradient in grads] != [n] * c or list(map(_numel, flat)) != self.sizes * c:
+            raise ValueError("each gradient must have the list's %d tensors with the same numbers of elements" % n)
+        if not all(map(_is_contiguous, flat)):
+            raise ValueError("gradient tensors must be contiguous")
+        if set(map(_get_device, flat)) != {self.device.index}:
+            raise ValueError("gradient tensors must live on the list's GPU, %s" % self.device)
+        dtypes = {g.dtype for g in flat}
         dtype = dtypes.pop()
         if dtypes or dtype not in _DTYPES:
             raise TypeError("gradients must all be fp32 or all bf16")
+        ptrs[:] = list(map(_data_ptr, flat))
         factors[:] = [1.0] * c if scales is None else scales
         return ptrs, c, factors, _DTYPES[dtype]
 
@@ -239,8 +239,8 @@ def _gradient_buffer(logits: torch.Tensor, grad: Union[bool, str, torch.Tensor])
     if grad is False or grad is None:
         return None, vocab
     if grad is True:
-        grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-    elif isinstance(grad, str):
+        return torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), max(vocab, 1)
+    if isinstance(grad, str):
         if grad != INPLACE:
             raise ValueError("grad is True, False, %r or a tensor" % INPLACE)
         grad = logits.detach()
@@ -252,14 +252,20 @@ def _gradient_buffer(logits: torch.Tensor, grad: Union[bool, str, torch.Tensor])
 _workspaces = {}                          # (device, stream, thread): a workspace that such calls use one after the other
 
 
-def _workspace(rows: int, sequences: int, device: torch.device, stream: int) -> torch.Tensor:
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(rows: int, sequences: int) -> int:
     need = C.c_int64()
     B._check(B.ps_loss_workspace(rows, sequences, C.byref(need)), "ps_loss_workspace")
-    capturing = torch.cuda.is_current_stream_capturing()               # a graph keeps its own
+    return need.value
+
+
+def _workspace(rows: int, sequences: int, device: torch.device, stream: int) -> torch.Tensor:
+    need = _workspace_bytes(rows, sequences)
+    capturing = torch._C._cuda_isCurrentStreamCapturing()               # a graph keeps its own
     key = (device.index, stream, threading.get_ident())
     ws = None if capturing else _workspaces.get(key)
-    if ws is None or ws.numel() < need.value:
-        ws = torch.zeros(max(need.value, 1 << 16), dtype=torch.uint8, device=device)
+    if ws is None or ws.numel() < need:
+        ws = torch.zeros(max(need, 1 << 16), dtype=torch.uint8, device=device)
         if not capturing:
             _workspaces[key] = ws
     return ws
