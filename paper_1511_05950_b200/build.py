@@ -1,10 +1,12 @@
-"""Build libsoftsync_ps.so (the C-ABI library with its sm_100a kernels) in-tree with nvcc."""
+"""Build libsoftsync_ps.so (the C-ABI library with its sm_100a kernels) in-tree with nvcc, and the _marshal extension (argument checks and
+output tensors of learn.py over torch's C++ tensors) with the host compiler."""
 from __future__ import annotations
 
 import hashlib
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -38,13 +40,54 @@ def source_digest() -> str:
 def is_stale() -> bool:
     """True unless the library exists and was built from exactly the present sources (file times are not
     trusted: a copied tree does not keep them)."""
-    if not os.path.exists(LIB) or not os.path.exists(STAMP):
+    return _stale(LIB, STAMP, source_digest)
+
+
+def _stale(target: str, stamp: str, digest) -> bool:
+    if not os.path.exists(target) or not os.path.exists(stamp):
         return True
-    with open(STAMP) as f:
-        return f.read().strip() != source_digest()
+    with open(stamp) as f:
+        return f.read().strip() != digest()
+
+
+# ---- the _marshal extension ----------------------------------------------------
+MARSHAL = os.path.join(HERE, "_marshal.so")
+MARSHAL_STAMP = MARSHAL + ".hash"
+MARSHAL_SOURCES = [os.path.join(CSRC, "marshal.cpp")] + [os.path.join(os.path.dirname(HERE), "include", h) for h in ("softsync_ps.h", "softsync_learn.h")]
+MARSHAL_FLAGS = ["-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden"]
+
+
+def marshal_digest() -> str:
+    import torch
+    h = hashlib.sha256(" ".join(MARSHAL_FLAGS + [torch.__version__, sysconfig.get_python_version()]).encode())
+    for path in MARSHAL_SOURCES:
+        with open(path, "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()
+
+
+def build_marshal(force: bool = False) -> str:
+    if not force and not _stale(MARSHAL, MARSHAL_STAMP, marshal_digest):
+        return MARSHAL
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    include = [sysconfig.get_paths()["include"], os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include")]
+    libs = os.path.join(root, "lib")
+    cmd = [shutil.which("g++") or "g++"] + MARSHAL_FLAGS + ["-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    cmd += ["-isystem" + i for i in include] + ["-o", MARSHAL, MARSHAL_SOURCES[0], "-L" + libs, "-Wl,-rpath," + libs,
+                                                "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    if os.path.exists(MARSHAL_STAMP):
+        os.remove(MARSHAL_STAMP)
+    subprocess.run(cmd, check=True)
+    with open(MARSHAL_STAMP, "w") as f:
+        f.write(marshal_digest() + "\n")
+    return MARSHAL
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_marshal(force)
     if not force and not is_stale():
         return LIB
     cmd = [nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
@@ -58,11 +101,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 
 def ensure_built() -> str:
-    """Build the library if it is missing or was built from other sources.  A failed rebuild raises: a
+    """Build the library and the extension if they are missing or were built from other sources.  A failed rebuild raises: a
     library that does not match the header and the binding must not be loaded."""
-    if is_stale():
-        return build(force=True)
-    return LIB
+    return build(force=False)
 
 
 if __name__ == "__main__":

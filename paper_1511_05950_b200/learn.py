@@ -2,24 +2,25 @@
 probabilities, the clipped policy loss and the preference loss with their gradients with respect to the logits; on the server
 the global norm of weighted gradients and AdamW over many tensors with moments in 32 or 8 bits.
 
-As in `binding`, Python checks and marshals arguments and allocates outputs; the work is done by the library on torch's
-current stream of the tensors' device.
+As in `binding`, this side checks and marshals arguments and allocates outputs (the losses and gradient lists in the `_marshal`
+extension, csrc/marshal.cpp); the work is done by the library on torch's current stream of the tensors' device.
 """
 from __future__ import annotations
 
 import ctypes as C
-import functools
-import itertools
-import threading
+import os
 from typing import List, NamedTuple, Optional, Sequence, Union
 
 import torch
 
-from . import binding as B
+from . import binding as B, build as _build
 
-_DTYPES = {torch.float32: B.PS_GRAD_FP32, torch.bfloat16: B.PS_GRAD_BF16}
+if not os.path.exists(_build.MARSHAL):
+    raise RuntimeError("_marshal.so is not built (%s). Run `python -m paper_1511_05950_b200.build`." % _build.MARSHAL)
+from . import _marshal  # noqa: E402
+
+_marshal.bind(*[C.cast(f, C.c_void_p).value for f in (B.ps_loss_workspace, B.ps_token_logprob, B.ps_policy_loss, B.ps_preference_loss)])
 INPLACE = "inplace"
-_numel, _is_contiguous, _get_device, _data_ptr = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr)
 
 
 def _stream(device: torch.device) -> int:
@@ -89,22 +90,11 @@ class TensorList:
         if scales is not None and len(scales) != c:
             raise ValueError("one scale for each of the %d gradients, got %d" % (c, len(scales)))
         if c not in self._pointers:
-            self._pointers[c] = ((C.c_void_p * (c * n))(), (C.c_float * c)())
+            self._pointers[c] = ((C.c_void_p * (c * n))(), (C.c_float * c)())      # sized for what the extension writes
         ptrs, factors = self._pointers[c]
-        flat = list(itertools.chain.from_iterable(grads))
-        if [len(gradient) for gradient in grads] != [n] * c or list(map(_numel, flat)) != self.sizes * c:
-            raise ValueError("each gradient must have the list's %d tensors with the same numbers of elements" % n)
-        if not all(map(_is_contiguous, flat)):
-            raise ValueError("gradient tensors must be contiguous")
-        if set(map(_get_device, flat)) != {self.device.index}:
-            raise ValueError("gradient tensors must live on the list's GPU, %s" % self.device)
-        dtypes = {g.dtype for g in flat}
-        dtype = dtypes.pop()
-        if dtypes or dtype not in _DTYPES:
-            raise TypeError("gradients must all be fp32 or all bf16")
-        ptrs[:] = list(map(_data_ptr, flat))
+        dtype = _marshal.gradients(grads, C.addressof(self._sizes), n, self.device.index, C.addressof(ptrs), c)
         factors[:] = [1.0] * c if scales is None else scales
-        return ptrs, c, factors, _DTYPES[dtype]
+        return ptrs, c, factors, dtype
 
     def grad_norm(self, grads, scales: Optional[Sequence[float]] = None, max_norm: float = float("inf"),
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -207,78 +197,12 @@ class PreferenceLoss(NamedTuple):
     dlogits: Optional[torch.Tensor]
 
 
-def _logits(logits: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor], temperature: float) -> B.Logits:
-    dtype = _DTYPES.get(logits.dtype)
-    if dtype is None:
-        raise TypeError("logits must be fp32 or bf16, got %s" % logits.dtype)
-    if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
-        raise ValueError("logits must be rows x vocabulary with the vocabulary contiguous")
-    if not logits.is_cuda:
-        raise ValueError("logits must live on the GPU")
-    rows, vocab = logits.shape
-    _per_row(tokens, rows, "tokens", logits, torch.int64)
-    _per_row(weights, rows, "weights", logits)
-    stride = logits.stride(0) if rows > 1 else max(vocab, 1)
-    return B.Logits(logits.data_ptr(), dtype, rows, vocab, stride, tokens.data_ptr(), None if weights is None else weights.data_ptr(), temperature)
-
-
-def _per_row(t: Optional[torch.Tensor], rows: int, what: str, logits: torch.Tensor, dtype: torch.dtype = torch.float32) -> None:
-    if t is None:
-        return
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    if t.dim() != 1 or t.numel() != rows or not t.is_contiguous():
-        raise ValueError("%s: %d values one behind the other, got shape %s with strides %s" % (what, rows, tuple(t.shape), t.stride()))
-    if t.get_device() != logits.get_device():
-        raise ValueError("%s is on %s, the logits on %s" % (what, t.device, logits.device))
-
-
-def _gradient_buffer(logits: torch.Tensor, grad: Union[bool, str, torch.Tensor]):
-    """(tensor or None, row stride) the gradient goes to."""
-    rows, vocab = logits.shape
-    if grad is False or grad is None:
-        return None, vocab
-    if grad is True:
-        return torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), max(vocab, 1)
-    if isinstance(grad, str):
-        if grad != INPLACE:
-            raise ValueError("grad is True, False, %r or a tensor" % INPLACE)
-        grad = logits.detach()
-    if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.device != logits.device or (grad.stride(1) != 1 and vocab > 1):
-        raise ValueError("the gradient's buffer must have the logits' shape, type and device, with the vocabulary contiguous")
-    return grad, grad.stride(0) if rows > 1 else max(vocab, 1)
-
-
-_workspaces = {}                          # (device, stream, thread): a workspace that such calls use one after the other
-
-
-@functools.lru_cache(maxsize=1024)
-def _workspace_bytes(rows: int, sequences: int) -> int:
-    need = C.c_int64()
-    B._check(B.ps_loss_workspace(rows, sequences, C.byref(need)), "ps_loss_workspace")
-    return need.value
-
-
-def _workspace(rows: int, sequences: int, device: torch.device, stream: int) -> torch.Tensor:
-    need = _workspace_bytes(rows, sequences)
-    capturing = torch._C._cuda_isCurrentStreamCapturing()               # a graph keeps its own
-    key = (device.index, stream, threading.get_ident())
-    ws = None if capturing else _workspaces.get(key)
-    if ws is None or ws.numel() < need:
-        ws = torch.zeros(max(need, 1 << 16), dtype=torch.uint8, device=device)
-        if not capturing:
-            _workspaces[key] = ws
-    return ws
-
-
 def token_logprob(logits: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor] = None, temperature: float = 1.0) -> TokenLogprob:
     """Log probability of each row's token, log normaliser and entropy, from one pass over the logits (rows x vocabulary, fp32 or bf16).
     Rows of weight zero are not read and give zeros."""
-    lg = _logits(logits, tokens, weights, temperature)
-    logp, lse, entropy = (torch.empty(lg.rows, dtype=torch.float32, device=logits.device) for _ in range(3))
-    with _on(logits.device):
-        B._check(B.ps_token_logprob(C.byref(lg), logp.data_ptr(), lse.data_ptr(), entropy.data_ptr(), _stream(logits.device)), "ps_token_logprob")
-    return TokenLogprob(logp, lse, entropy)
+    status, *out = _marshal.token_logprob(logits, tokens, weights, temperature)
+    B._check(status, "ps_token_logprob")
+    return TokenLogprob(*out)
 
 
 def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
@@ -287,21 +211,10 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     """The clipped policy loss with a KL and an entropy term (formulas: include/softsync_learn.h) and its gradient with respect to the
     logits: `logits.backward(result.dlogits)` continues into the model.  grad: True (a new tensor), a tensor to write to, "inplace" (the
     gradient replaces the logits), or False."""
-    lg = _logits(logits, tokens, weights, temperature)
-    for what, t in (("old_logp", old_logp), ("advantages", advantages), ("ref_logp", ref_logp)):
-        _per_row(t, lg.rows, what, logits)
-    device = logits.device
-    dlogits, stride = _gradient_buffer(logits, grad)
-    stats = torch.empty(5, dtype=torch.float32, device=device)
-    logp, entropy = (torch.empty(lg.rows, dtype=torch.float32, device=device) for _ in range(2))
-    k = B.PolicyInputs(old_logp.data_ptr(), advantages.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(),
-                       clip_low, clip_high, kl_coef, entropy_coef)
-    with _on(device):
-        stream = _stream(device)
-        ws = _workspace(lg.rows, 0, device, stream)
-        B._check(B.ps_policy_loss(C.byref(lg), C.byref(k), stats.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
-                                  None if dlogits is None else dlogits.data_ptr(), stride, ws.data_ptr(), ws.numel(), stream), "ps_policy_loss")
-    return PolicyLoss(stats, logp, entropy, dlogits)
+    status, *out = _marshal.policy_loss(logits, tokens, weights, temperature, old_logp, advantages, ref_logp, clip_low, clip_high, kl_coef,
+                                        entropy_coef, grad)
+    B._check(status, "ps_policy_loss")
+    return PolicyLoss(*out)
 
 
 def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.Tensor, ref_logp: torch.Tensor,
@@ -310,20 +223,6 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.T
     """The preference loss over pairs of sequences (formulas: include/softsync_learn.h) and its gradient with respect to the logits.
     offsets: 2 * pairs + 1 ascending row numbers (int64, on the GPU); sequences 2i and 2i + 1 are pair i's preferred and other answer.  ref_logp: 2 *
     pairs.  grad: as in policy_loss."""
-    lg = _logits(logits, tokens, weights, temperature)
-    if offsets.dim() != 1 or offsets.numel() % 2 != 1:
-        raise ValueError("offsets holds 2 * pairs + 1 row numbers")
-    seqs = offsets.numel() - 1
-    _per_row(offsets, seqs + 1, "offsets", logits, torch.int64)
-    _per_row(ref_logp, seqs, "ref_logp", logits)
-    device = logits.device
-    dlogits, stride = _gradient_buffer(logits, grad)
-    stats = torch.empty(3, dtype=torch.float32, device=device)
-    seq_logp = torch.empty(seqs, dtype=torch.float32, device=device)
-    k = B.PreferenceInputs(offsets.data_ptr(), ref_logp.data_ptr(), seqs // 2, beta, label_smoothing)
-    with _on(device):
-        stream = _stream(device)
-        ws = _workspace(lg.rows, seqs, device, stream)
-        B._check(B.ps_preference_loss(C.byref(lg), C.byref(k), stats.data_ptr(), seq_logp.data_ptr(),
-                                      None if dlogits is None else dlogits.data_ptr(), stride, ws.data_ptr(), ws.numel(), stream), "ps_preference_loss")
-    return PreferenceLoss(stats, seq_logp, dlogits)
+    status, *out = _marshal.preference_loss(logits, tokens, weights, temperature, offsets, ref_logp, beta, label_smoothing, grad)
+    B._check(status, "ps_preference_loss")
+    return PreferenceLoss(*out)
