@@ -944,9 +944,10 @@ __device__ __forceinline__ void sequence_rows(const PreferenceIn &in, long long 
     hi = min(max(in.offsets[k + 1], lo), rows);
 }
 
-constexpr int kPairThreads = 256;
+constexpr int kPairThreads = 256, kSideThreads = kPairThreads / 2;
 
-// One block per pair; the block that ends last adds the pairs' terms up in their order.  `done` is zero before and after.
+// One block per pair, half of it for each sequence; the block that ends last adds the pairs' terms up in their order.  `done` is zero
+// before and after.
 static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(const __grid_constant__ RowsIn rows, const __grid_constant__ PreferenceIn in,
                                                                                const float *logp, float *seq_logp, RowCoef *coef, double (*each)[3],
                                                                                unsigned *done, float *stats)
@@ -954,38 +955,37 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
     __shared__ double scratch[kPairThreads / 32];
     __shared__ bool finish;
     griddep_launch_dependents();
-    griddep_wait();                                        // the statistics
     const long long i = blockIdx.x;
-    double pi[2];
-    for (int side = 0; side < 2; ++side) {
-        long long lo, hi;
-        sequence_rows(in, 2 * i + side, rows.rows, lo, hi);
-        double s = 0;
-        for (long long r = lo + threadIdx.x; r < hi; r += blockDim.x) {
-            const float w = rows.weights ? rows.weights[r] : 1.f;
-            if (w != 0.f) s += static_cast<double>(w) * logp[r];
-        }
-        s = block_total(s, scratch, kPairThreads, [] { __syncthreads(); });
-        if (threadIdx.x == 0) seq_logp[2 * i + side] = static_cast<float>(s);
-        pi[side] = s - in.ref_logp[2 * i + side];
+    const int side = threadIdx.x / kSideThreads, me = threadIdx.x % kSideThreads;
+    long long lo, hi;
+    sequence_rows(in, 2 * i + side, rows.rows, lo, hi);
+    const double ref = static_cast<double>(in.ref_logp[2 * i]) - static_cast<double>(in.ref_logp[2 * i + 1]);
+    griddep_wait();                                        // the statistics
+    double s = 0;
+    for (long long r = lo + me; r < hi; r += kSideThreads) {
+        const float w = rows.weights ? rows.weights[r] : 1.f;
+        if (w != 0.f) s += static_cast<double>(w) * logp[r];
     }
-    const double margin = in.beta * (pi[0] - pi[1]);
-    const double slope = (1.0 / (1.0 + exp(-margin)) - (1.0 - in.smoothing)) * in.beta / static_cast<double>(in.pairs);
-    if (coef)
-        for (int side = 0; side < 2; ++side) {
-            long long lo, hi;
-            sequence_rows(in, 2 * i + side, rows.rows, lo, hi);
-            for (long long r = lo + threadIdx.x; r < hi; r += blockDim.x) {
-                const float w = rows.weights ? rows.weights[r] : 1.f;
-                coef[r] = RowCoef{w != 0.f ? static_cast<float>((side ? -slope : slope) * w) * rows.inv_temperature : 0.f, 0.f};
-            }
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = s;
+    __syncthreads();
+    double pi[2] = {0, 0};
+    for (int k = 0; k < kPairThreads / 32; ++k) pi[k / (kSideThreads / 32)] += scratch[k];
+    if (me == 0) seq_logp[2 * i + side] = static_cast<float>(pi[side]);
+    const float margin = static_cast<float>(static_cast<double>(in.beta) * ((pi[0] - pi[1]) - ref));
+    if (coef) {
+        const float slope = (1.f / (1.f + expf(-margin)) - (1.f - in.smoothing)) * in.beta / static_cast<float>(in.pairs);
+        for (long long r = lo + me; r < hi; r += kSideThreads) {
+            const float w = rows.weights ? rows.weights[r] : 1.f;
+            coef[r] = RowCoef{w != 0.f ? (side ? -slope : slope) * w * rows.inv_temperature : 0.f, 0.f};
         }
+    }
     if (threadIdx.x == 0) {
-        const double up = log1p(exp(-fabs(margin)));                       // log(1 + e^-|x|)
-        const double loss = (1.0 - in.smoothing) * (up + fmax(-margin, 0.0)) + in.smoothing * (up + fmax(margin, 0.0));
-        __stcg(&each[i][0], isnan(margin) ? margin : loss);
-        __stcg(&each[i][1], margin > 0.0 ? 1.0 : 0.0);
-        __stcg(&each[i][2], margin);
+        const float up = log1pf(expf(-fabsf(margin)));                     // log(1 + e^-|x|)
+        const float loss = (1.f - in.smoothing) * (up + fmaxf(-margin, 0.f)) + in.smoothing * (up + fmaxf(margin, 0.f));
+        __stcg(&each[i][0], static_cast<double>(isnan(margin) ? margin : loss));
+        __stcg(&each[i][1], margin > 0.f ? 1.0 : 0.0);
+        __stcg(&each[i][2], static_cast<double>(margin));
         __threadfence();
         finish = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;
     }
@@ -997,8 +997,8 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
 #pragma unroll
         for (int q = 0; q < 3; ++q) sum[q] += __ldcg(&each[k][q]);
     for (int q = 0; q < 3; ++q) {
-        const double s = block_total(sum[q], scratch, kPairThreads, [] { __syncthreads(); });
-        if (threadIdx.x == 0) stats[q] = static_cast<float>(s / static_cast<double>(in.pairs));
+        const double total = block_total(sum[q], scratch, kPairThreads, [] { __syncthreads(); });
+        if (threadIdx.x == 0) stats[q] = static_cast<float>(total / static_cast<double>(in.pairs));
     }
 }
 

@@ -226,3 +226,61 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.T
     status, *out = _marshal.preference_loss(logits, tokens, weights, temperature, offsets, ref_logp, beta, label_smoothing, grad)
     B._check(status, "ps_preference_loss")
     return PreferenceLoss(*out)
+
+
+# ---- an n-softsync server whose update is an AdamW step -------------------------------------------------------------------
+
+class AdamWServer:
+    """The n-softsync protocol (Sections 2.1-2.4) with an AdamW step in the place of momentum SGD.
+
+    A `ParameterServer` without parameters keeps the clock: learners `pull` a timestamp, `push` a gradient (a list of one tensor for each
+    parameter) with it, and every c = floor(num_learners / n) pushes make a group.  `apply_update` takes the oldest group: g = sum_l s_l g_l
+    with s_l = 1 / (c sigma_l) (or the modulation's own penalty over c) in the server's summation order, clipped to max_norm if given, then
+    one AdamW step.  The learning rate is AdamW's: a group of equally stale gradients is scaled as a whole, which the step's normalisation
+    takes back, so staleness weighs gradients against one another, inside a group and through the moments from group to group.
+    Gradients are borrowed until the update that consumes them; all work goes to torch's current stream."""
+
+    def __init__(self, params: Sequence[torch.Tensor], num_learners: int, n: int, modulation: str = "inv_staleness",
+                 max_norm: Optional[float] = None, **adamw):
+        self.optimizer = AdamW(params, **adamw)
+        self.max_norm = max_norm
+        self._clock = B.ParameterServer(0, num_learners, n, 1.0, modulation=modulation)
+        self._token = torch.zeros(1, device=self.optimizer.device)          # stands for a gradient where the clock asks for one
+        self._pushed = {}                                                   # (learner, push index): gradient
+        self._pushes = [0] * num_learners
+        self.c = self._clock.c
+        self.last_norm = None                                               # (norm, factor) of the last update, on the device
+
+    def timestamps(self):
+        """(applied, logical)."""
+        return self._clock.timestamps()
+
+    def pull(self) -> int:
+        """The timestamp that a gradient computed on the present parameters must carry.  Complete groups are applied first, so that the
+        parameters are those of the timestamp."""
+        while self._clock.timestamps()[1] > self._clock.timestamps()[0]:
+            self.apply_update()
+        return self._clock.pull_weights()
+
+    def push(self, learner: int, grads: Sequence[torch.Tensor], ts: int) -> bool:
+        """True if this push completed a group."""
+        grads = list(grads)
+        self.optimizer._gradients(grads, None)                              # what the update would refuse is refused here
+        ready = self._clock.push_gradient(learner, self._token, ts)
+        self._pushed[learner, self._pushes[learner]] = grads
+        self._pushes[learner] += 1
+        return ready
+
+    def apply_update(self) -> None:
+        """Applies the oldest complete group."""
+        self._clock.apply_update()
+        entries = self._clock.update_log(self._clock.timestamps()[0] - 1, 1)
+        grads = [self._pushed.pop((int(e["learner"]), int(e["push_index"]))) for e in entries]
+        scales = [float(e["scale"]) for e in entries]
+        clip = None
+        if self.max_norm is not None:
+            clip = self.last_norm = self.optimizer.grad_norm(grads, scales, self.max_norm)
+        self.optimizer.step(grads, scales, clip=clip)
+
+    def staleness_histogram(self):
+        return self._clock.staleness_histogram()
