@@ -344,46 +344,6 @@ struct RowGradient {
     }
 };
 
-// Gradient of the vectors [lo, hi) of a row, written to the row at dst by the block's T threads; `vector(q)` gives vector q, `logit(j)`
-// the row's element j.  The token's entry is written once more, with its one, by the thread that has just written it, so the order
-// of the two is certain.  Where dst lies otherwise within 16 bytes than the row, or the row's maximum is out of the
-// ordinary, the elements go one by one.
-template <typename GT, int T, int UNROLL, bool ENTROPY, typename Vector, typename Logit>
-__device__ __forceinline__ void write_gradient(const RowVectors<GT> &v, int lo, int hi, unsigned char *dst, const RowGradient &f,
-                                               long long tok, float x_tok, Vector vector, Logit logit)
-{
-    if (((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c)) {
-        unsigned char *p = dst - v.phase * logit_bytes<GT>();
-        int q = lo + threadIdx.x;
-        if (!v.ragged()) {
-            for (; q + (UNROLL - 1) * T < hi; q += UNROLL * T) {
-                uint4 x[UNROLL];
-#pragma unroll
-                for (int k = 0; k < UNROLL; ++k) x[k] = vector(q + k * T);
-#pragma unroll
-                for (int k = 0; k < UNROLL; ++k)
-                    __stcs(reinterpret_cast<uint4 *>(p + static_cast<long long>(q) * 16 + k * T * 16), f.template vector<GT, ENTROPY>(x[k]));
-            }
-        }
-        for (; q < hi; q += T) {
-            const uint4 g = f.template vector<GT, ENTROPY>(vector(q));
-            if (v.whole(q)) __stcs(reinterpret_cast<uint4 *>(p + static_cast<long long>(q) * 16), g);
-            else store_single<GT>(dst, v.first(q), v.vocab, g);
-        }
-        if (static_cast<unsigned long long>(tok) < static_cast<unsigned long long>(v.vocab)) {
-            const int at = (static_cast<int>(tok) + v.phase) / per_vector<GT>();
-            if (at >= lo && at < hi && (at - lo) % T == static_cast<int>(threadIdx.x))
-                store_logit<GT>(dst, tok, __fadd_rn(f.template single<GT, ENTROPY>(x_tok), f.one));
-        }
-    } else {
-        const int end = min(v.first(hi), v.vocab);
-        for (int j = max(v.first(lo), 0) + threadIdx.x; j < end; j += T) {
-            const float g = f.template single<GT, ENTROPY>(logit(j));
-            store_logit<GT>(dst, j, j == tok ? __fadd_rn(g, f.one) : g);
-        }
-    }
-}
-
 // ---- clusters ------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ unsigned cluster_rank() { unsigned r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ unsigned cluster_size() { unsigned r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
@@ -509,32 +469,55 @@ __global__ void __launch_bounds__(T, 1536 / T) row_stats_kernel(const __grid_con
 constexpr int kGradThreads = 256, kGradVectors = 4;
 
 // One block per segment of a row, rows from the last to the first: the statistics pass went the other way, so the rows it read
-// last, which the L2 still holds, come first.
+// last, which the L2 still holds, come first.  The logits are on their way before the factors are there.
 template <typename GT, bool ENTROPY>
-__global__ void __launch_bounds__(kGradThreads) row_grad_kernel(const __grid_constant__ RowsIn in, const RowStat *stat, const RowCoef *coef,
+__global__ void __launch_bounds__(kGradThreads, 6) row_grad_kernel(const __grid_constant__ RowsIn in, const RowStat *stat, const RowCoef *coef,
                                                                 const float *entropy, unsigned char *out, long long out_stride, int segments)
 {
+    constexpr int T = kGradThreads, NV = kGradVectors, PV = per_vector<GT>();
     const long long r = in.rows - 1 - blockIdx.x / static_cast<unsigned>(segments);
-    const int segment = blockIdx.x % static_cast<unsigned>(segments);
+    const int segment = blockIdx.x % static_cast<unsigned>(segments), vocab = static_cast<int>(in.vocab);
     const unsigned char *row = in.data + r * in.stride * logit_bytes<GT>();
     unsigned char *dst = out + r * out_stride * logit_bytes<GT>();
+    const RowVectors<GT> v(row, vocab);
+    const bool masked = in.weights && in.weights[r] == 0.f;
+    const int lo = segment * NV * T, q0 = lo + threadIdx.x;
+    uint4 x[NV];
+    if (!masked) load_vectors<GT, T, NV>(x, v, q0);
     griddep_wait();                                        // the factors
     const RowCoef k = coef[r];
-    if ((in.weights && in.weights[r] == 0.f) || (k.a == 0.f && k.b == 0.f)) {        // nothing to read: the gradient is zero
-        zero_row<GT>(dst, static_cast<int>(in.vocab), segment * kGradThreads + threadIdx.x, segments * kGradThreads);
+    if (masked || (k.a == 0.f && k.b == 0.f)) {            // the gradient is zero, whatever the row holds
+        zero_row<GT>(dst, vocab, segment * T + threadIdx.x, segments * T);
         return;
     }
-    const RowVectors<GT> v(row, static_cast<int>(in.vocab));
-    const int lo = segment * kGradVectors * kGradThreads, hi = min(lo + kGradVectors * kGradThreads, v.count);
     const RowStat st = stat[r];
-    const float h = ENTROPY ? entropy[r] : 0.f;
     const long long tok = in.tokens[r];
-    const float x_tok = tok >= 0 && tok < in.vocab ? logit_at(static_cast<const GT *>(nullptr), row, tok) : 0.f;
-    if (out == in.data) __syncthreads();                   // in place: the token's logit is read before it is replaced
-    write_gradient<GT, kGradThreads, kGradVectors, ENTROPY>(
-        v, lo, hi, dst, RowGradient(st.max, st.log2_sum, in.scale, k, h), tok, x_tok,
-        [&](int q) { return v.whole(q) ? load_vector16(v.at(q)) : load_ragged_vector<GT>(row, v.first(q), v.vocab); },
-        [&](int j) { return logit_at(static_cast<const GT *>(nullptr), row, j); });
+    const RowGradient f(st.max, st.log2_sum, in.scale, k, ENTROPY ? entropy[r] : 0.f);
+    if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c)) {
+        const int tok_q = tok >= 0 && tok < vocab ? (static_cast<int>(tok) + v.phase) / PV : -1, tok_j = (static_cast<int>(tok) + v.phase) % PV;
+        unsigned char *p = dst - v.phase * logit_bytes<GT>() + static_cast<long long>(q0) * 16;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int q = q0 + i * T;
+            if (q >= v.count) break;
+            const uint4 g = f.template vector<GT, ENTROPY>(x[i]);
+            if (v.whole(q)) __stcs(reinterpret_cast<uint4 *>(p + i * T * 16), g);
+            else store_single<GT>(dst, v.first(q), vocab, g);
+            if (q == tok_q) {                              // the token's entry once more, with its one
+#pragma unroll
+                for (int j = 0; j < PV; ++j) {
+                    const float2 y = plain_pair<GT>(x[i], j / 2);
+                    if (j == tok_j) store_logit<GT>(dst, tok, __fadd_rn(f.template single<GT, ENTROPY>(j & 1 ? y.y : y.x), f.one));
+                }
+            }
+        }
+    } else {                                               // single elements, one a thread
+        const int end = min(v.first(lo + NV * T), vocab);
+        for (int j = max(v.first(lo), 0) + threadIdx.x; j < end; j += T) {
+            const float g = f.template single<GT, ENTROPY>(logit_at(static_cast<const GT *>(nullptr), row, j));
+            store_logit<GT>(dst, j, j == tok ? __fadd_rn(g, f.one) : g);
+        }
+    }
 }
 
 // ---- the policy loss -----------------------------------------------------------------------------------------------------
@@ -973,13 +956,6 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
     for (int k = 0; k < kPairThreads / 32; ++k) pi[k / (kSideThreads / 32)] += scratch[k];
     if (me == 0) seq_logp[2 * i + side] = static_cast<float>(pi[side]);
     const float margin = static_cast<float>(static_cast<double>(in.beta) * ((pi[0] - pi[1]) - ref));
-    if (coef) {
-        const float slope = (1.f / (1.f + expf(-margin)) - (1.f - in.smoothing)) * in.beta / static_cast<float>(in.pairs);
-        for (long long r = lo + me; r < hi; r += kSideThreads) {
-            const float w = rows.weights ? rows.weights[r] : 1.f;
-            coef[r] = RowCoef{w != 0.f ? (side ? -slope : slope) * w * rows.inv_temperature : 0.f, 0.f};
-        }
-    }
     if (threadIdx.x == 0) {
         const float up = log1pf(expf(-fabsf(margin)));                     // log(1 + e^-|x|)
         const float loss = (1.f - in.smoothing) * (up + fmaxf(-margin, 0.f)) + in.smoothing * (up + fmaxf(margin, 0.f));
@@ -989,17 +965,25 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
         __threadfence();
         finish = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;
     }
+    if (coef) {
+        const float slope = (1.f / (1.f + expf(-margin)) - (1.f - in.smoothing)) * in.beta / static_cast<float>(in.pairs);
+        for (long long r = lo + me; r < hi; r += kSideThreads) {
+            const float w = rows.weights ? rows.weights[r] : 1.f;
+            coef[r] = RowCoef{w != 0.f ? (side ? -slope : slope) * w * rows.inv_temperature : 0.f, 0.f};
+        }
+    }
     __syncthreads();
-    if (!finish) return;
+    if (!finish || threadIdx.x >= 32) return;
     __threadfence();
     double sum[3] = {};
-    for (long long k = threadIdx.x; k < in.pairs; k += blockDim.x)
+    for (long long k = threadIdx.x; k < in.pairs; k += 32)
 #pragma unroll
         for (int q = 0; q < 3; ++q) sum[q] += __ldcg(&each[k][q]);
-    for (int q = 0; q < 3; ++q) {
-        const double total = block_total(sum[q], scratch, kPairThreads, [] { __syncthreads(); });
-        if (threadIdx.x == 0) stats[q] = static_cast<float>(total / static_cast<double>(in.pairs));
-    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+        for (int o = 16; o; o >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], o);
+    if (threadIdx.x == 0)
+        for (int q = 0; q < 3; ++q) stats[q] = static_cast<float>(sum[q] / static_cast<double>(in.pairs));
 }
 
 }  // namespace softsync
