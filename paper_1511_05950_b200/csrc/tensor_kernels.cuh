@@ -19,8 +19,9 @@
 namespace softsync {
 
 constexpr int kStateBlock = 256;
-constexpr int kChunk = 2048;              // elements of a chunk: one block of 8 warps
+constexpr int kChunk = 512;               // elements of a chunk: one block of the AdamW kernel, two warps
 constexpr int kListThreads = kChunk / 8;
+constexpr int kNormThreads = 256, kNormStep = kNormThreads * 8;          // the norm takes so many elements at a time
 
 struct TensorRec {
     float *w;
@@ -164,14 +165,14 @@ __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAX
     for (int l = 0; l < c; ++l) on_grid = on_grid && (reinterpret_cast<uintptr_t>(row[l]) & 15) == 0;            // first is a multiple of kChunk
     long long at = first;
     if (on_grid) {
-        for (; at + U * kChunk <= end; at += U * kChunk) {
+        for (; at + U * kNormStep <= end; at += U * kNormStep) {
             float2 acc[ONE ? 1 : U][4];
             for (int l = 0; l < c; ++l) {
                 const unsigned char *p = static_cast<const unsigned char *>(row[l]) + (at + threadIdx.x * 8) * GB;
                 const float2 s = make_float2(tab.s[l], tab.s[l]);
                 Raw8<GT> r[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) load8(r[u], p + u * kChunk * GB);
+                for (int u = 0; u < U; ++u) load8(r[u], p + u * kNormStep * GB);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -191,7 +192,7 @@ __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAX
     }
     constexpr int G = ONE ? 1 : 4;
 #pragma unroll 1
-    for (; at < end; at += kChunk) {
+    for (; at < end; at += kNormStep) {
         float g[8] = {};
 #pragma unroll 1
         for (int l0 = 0; l0 < c; l0 += G) {
@@ -200,7 +201,7 @@ __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAX
             for (int i = 0; i < G; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const long long e = at + j * kListThreads + threadIdx.x;
+                    const long long e = at + j * kNormThreads + threadIdx.x;
                     float y[1] = {0.f};
                     if (l0 + i < c && e < end) {
                         Raw<GT, 1> r;
@@ -228,11 +229,11 @@ __device__ __forceinline__ void add_squares(float2 (&sq)[4], const GradTable<MAX
 // once and then streams.  A block's sum goes to its own place, and the block that finishes last adds the places up in their order, so
 // no result depends on which block came first.
 template <typename GT, bool ONE, int MAXP>
-__global__ void __launch_bounds__(kListThreads, 3) grad_norm_kernel(const __grid_constant__ ListTables lt,
+__global__ void __launch_bounds__(kNormThreads, 3) grad_norm_kernel(const __grid_constant__ ListTables lt,
                                                                     const __grid_constant__ GradTable<MAXP> tab,
                                                                     const __grid_constant__ NormTail tail)
 {
-    __shared__ double scratch[kListThreads / 32];
+    __shared__ double scratch[kNormThreads / 32];
     __shared__ bool finish;
     const long long from = lt.nchunks * blockIdx.x / gridDim.x, to = lt.nchunks * (blockIdx.x + 1) / gridDim.x;
     double mine = 0;
@@ -369,6 +370,13 @@ struct AdamwParams {
     int short_forms;                      // eps allows the short root and quotient
 };
 
+__device__ __forceinline__ float max3_nan(float a, float b, float c)    // NaN if one of them is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // Scaling that keeps the short root and quotient away from underflow: powers of two that the roundings do not see.  They serve while
 // m < 2^20 and v < 2^30, with an eps of at least 2^-40 (so no quotient overflows, and a root of zero may be taken for 2^-78) and a step
 // size of at least 2^-40.
@@ -451,7 +459,7 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
     }
 
     const auto two = [](float x) { return make_float2(x, x); };
-    unsigned mt = 0, vt = 0;                             // the largest magnitudes, as bits
+    float m_top = 0.f, v_top = 0.f;                      // the largest magnitudes; NaN if there is one
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         float2 x = make_float2(g[2 * k], g[2 * k + 1]);
@@ -460,9 +468,10 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
         const float2 c = mul2(v[k], p.beta2), d = mul2(mul2(x, x), p.one_minus_beta2);
         m[k] = make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
         v[k] = make_float2(__fadd_rn(c.x, d.x), __fadd_rn(c.y, d.y));
-        mt = max(mt, max(__float_as_uint(m[k].x) & 0x7fffffffu, __float_as_uint(m[k].y) & 0x7fffffffu));
-        vt = max(vt, max(__float_as_uint(v[k].x), __float_as_uint(v[k].y)));           // never below zero
+        m_top = max3_nan(m_top, fabsf(m[k].x), fabsf(m[k].y));
+        v_top = max3_nan(v_top, v[k].x, v[k].y);
     }
+    unsigned mt = __float_as_uint(m_top), vt = __float_as_uint(v_top);
     if constexpr (BITS == 8) { mt = __reduce_max_sync(0xffffffffu, mt); vt = __reduce_max_sync(0xffffffffu, vt); }
     if (__all_sync(0xffffffffu, p.short_forms && fabsf(step) >= 0x1p-40f && mt < kMLimit && vt < kVLimit)) {
         const float2 rs = two(p.root_scale * 0x1p-48f), st = two(step * 0x1p-64f);
@@ -580,8 +589,14 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
     }
 }
 
+// Blocks of two warps, so that an SM's registers are refilled in small pieces (61M elements, four fp32 gradients: 363 us, with eight warps
+// 370), and for 8-bit moments and a bf16 gradient, the form with the most instructions a byte, 18 of them an SM instead
+// of 16 (4.7e8 elements: 1455 us, with 16 1526).
+template <typename GT, int BITS>
+constexpr int adamw_blocks_per_sm() { return BITS == 8 && GradBytes<GT>::value == 2 ? 18 : 16; }
+
 template <typename GT, int BITS, int MAXP>
-__global__ void __launch_bounds__(kListThreads, 4) adamw_kernel(const __grid_constant__ ListTables lt,
+__global__ void __launch_bounds__(kListThreads, adamw_blocks_per_sm<GT, BITS>()) adamw_kernel(const __grid_constant__ ListTables lt,
                                                              const __grid_constant__ GradTable<MAXP> tab,
                                                              const __grid_constant__ AdamwParams p)
 {

@@ -281,7 +281,7 @@ int ps_grad_norm(ps_tensors_t *list, const void *const *grads_host, int c, const
     return launch_ranges(list, grads_host, c, scales_host, [&](const ListTables &lt, const auto &tab, bool first, bool last) {
         constexpr int MAXP = static_cast<int>(sizeof(tab.g) / sizeof(void *));
         const NormTail tail{list->partial_dev, list->done_dev, out_dev, max_norm, first ? 0 : 1, last ? 1 : 0};
-        const auto go = [&](auto kernel) { kernel<<<grid, kListThreads, 0, st>>>(lt, tab, tail); };
+        const auto go = [&](auto kernel) { kernel<<<grid, softsync::kNormThreads, 0, st>>>(lt, tab, tail); };
         if (grad_dtype == PS_GRAD_BF16) c == 1 ? go(softsync::grad_norm_kernel<GradBf16, true, MAXP>) : go(softsync::grad_norm_kernel<GradBf16, false, MAXP>);
         else c == 1 ? go(softsync::grad_norm_kernel<GradFp32, true, MAXP>) : go(softsync::grad_norm_kernel<GradFp32, false, MAXP>);
         return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA;
