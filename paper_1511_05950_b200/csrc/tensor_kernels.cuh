@@ -23,12 +23,13 @@ constexpr int kChunk = 512;               // elements of a chunk: one block of t
 constexpr int kListThreads = kChunk / 8;
 constexpr int kNormThreads = 256, kNormStep = kNormThreads * 8;          // the norm takes so many elements at a time
 
-struct TensorRec {
+struct __align__(16) TensorRec {          // three 16-byte loads
     float *w;
     unsigned short *mirror;
     long long n;                          // elements
-    long long state_off;                  // first element in the state arrays
-    long long first_chunk;
+    unsigned long long state_off;         // first element in the state arrays
+    unsigned first_chunk;
+    int on_grid;                          // w and mirror allow the vector form
     float lr_mult, decay_mult;
 };
 
@@ -36,16 +37,21 @@ struct TensorRec {
 // every call (a learner pushes another buffer each time), and passing them by value needs no copy to the device.
 template <int MAXP>
 struct GradTable {
-    static constexpr int kMaxC = MAXP < 256 ? MAXP : 256;
+    static constexpr int kPointers = MAXP, kMaxC = MAXP < 256 ? MAXP : 256;
     int t0, c;
     float s[kMaxC];
     const void *g[MAXP];
+};
+// With what a step multiplies each tensor's weights (x) and update (y) with.
+template <int MAXP>
+struct StepTable : GradTable<MAXP> {
+    float2 coef[MAXP];
 };
 
 struct ListTables {
     const TensorRec *recs;
     const int *chunk_tensor;
-    long long chunk0, nchunks;            // this launch's chunks
+    unsigned chunk0, nchunks;             // this launch's chunks
 };
 
 // Where a lane's element j (0..7) of a warp's 256 lies.  Vector form: two runs of four consecutive elements, so that
@@ -87,32 +93,30 @@ __device__ __forceinline__ void load_grad8(float (&g)[8], const unsigned char *p
     }
 }
 
-// The weighted sum of the c gradients of tensor `t` for the warp's elements from `first` on.
-template <typename GT, bool VECTOR, int MAXP>
-__device__ __forceinline__ void weighted_gradient(float (&acc)[8], const GradTable<MAXP> &tab, int t, long long first, int lane, int count)
+// The weighted sum of the c gradients of tensor `t` for the warp's elements from `first` on.  ONE: c = 1.
+template <typename GT, bool VECTOR, bool ONE, int MAXP>
+__device__ __forceinline__ void weighted_gradient(float2 (&acc)[4], const GradTable<MAXP> &tab, int t, long long first, int lane, int count)
 {
-    const void *const *row = tab.g + (t - tab.t0) * tab.c;
-    for (int l = 0; l < tab.c; ++l) {
+    const void *const *row = tab.g + (ONE ? t - tab.t0 : (t - tab.t0) * tab.c);
+    for (int l = 0; l < (ONE ? 1 : tab.c); ++l) {
         float g[8];
         load_grad8<GT, VECTOR>(g, static_cast<const unsigned char *>(row[l]) + first * GradBytes<GT>::value, lane, count);
-        const float s = tab.s[l];
-        if (l == 0) {
+        const float2 s = make_float2(tab.s[l], tab.s[l]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = __fmul_rn(s, g[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = __fadd_rn(acc[j], __fmul_rn(s, g[j]));
+        for (int k = 0; k < 4; ++k) {
+            const float2 x = mul2(s, make_float2(g[2 * k], g[2 * k + 1]));
+            acc[k] = ONE || l == 0 ? x : make_float2(__fadd_rn(acc[k].x, x.x), __fadd_rn(acc[k].y, x.y));
         }
     }
 }
 
 // Whether every gradient of the tensor lies on the grid of the vector form.
-template <typename GT, int MAXP>
+template <typename GT, bool ONE, int MAXP>
 __device__ __forceinline__ bool grads_on_grid(const GradTable<MAXP> &tab, int t)
 {
-    const void *const *row = tab.g + (t - tab.t0) * tab.c;
+    const void *const *row = tab.g + (ONE ? t - tab.t0 : (t - tab.t0) * tab.c);
     bool ok = true;
-    for (int l = 0; l < tab.c; ++l) ok = ok && (reinterpret_cast<uintptr_t>(row[l]) & (4 * GradBytes<GT>::value - 1)) == 0;
+    for (int l = 0; l < (ONE ? 1 : tab.c); ++l) ok = ok && (reinterpret_cast<uintptr_t>(row[l]) & (4 * GradBytes<GT>::value - 1)) == 0;
     return ok;
 }
 
@@ -235,7 +239,7 @@ __global__ void __launch_bounds__(kNormThreads, 3) grad_norm_kernel(const __grid
 {
     __shared__ double scratch[kNormThreads / 32];
     __shared__ bool finish;
-    const long long from = lt.nchunks * blockIdx.x / gridDim.x, to = lt.nchunks * (blockIdx.x + 1) / gridDim.x;
+    const long long from = static_cast<long long>(lt.nchunks) * blockIdx.x / gridDim.x, to = static_cast<long long>(lt.nchunks) * (blockIdx.x + 1) / gridDim.x;
     double mine = 0;
     for (long long k = from; k < to;) {
         const int t = lt.chunk_tensor[lt.chunk0 + k];
@@ -363,7 +367,6 @@ struct AdamwParams {
     void *m, *v;                          // state arrays: fp32 or bytes
     unsigned char *m_scale, *v_scale;
     const float *clip;                    // nullptr: none
-    double lr_decay, step_size;           // lr * weight_decay; lr / (1 - beta1^t)
     float2 beta1, one_minus_beta1, beta2, one_minus_beta2;               // each twice: one 64-bit operand of a packed multiply
     float root_scale, eps;
     unsigned key;
@@ -383,13 +386,13 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)    // NaN i
 constexpr float kMScale = 0x1p64f, kVScale = 0x1p96f, kVLeast = 0x1p-60f;
 constexpr unsigned kMLimit = 0x49800000u, kVLimit = 0x4e800000u;         // bits of 2^20, 2^30
 
-template <typename GT, int BITS, bool VECTOR, int MAXP>
-__device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTable<MAXP> &tab, const TensorRec &rec, int t,
-                                            long long first, int lane, int count, float clip, float decay, float step)
+template <typename GT, int BITS, bool VECTOR, bool ONE, int MAXP>
+__device__ __forceinline__ void adamw_block(const AdamwParams &p, const StepTable<MAXP> &tab, const TensorRec &rec, int t,
+                                            long long first, int lane, int count, float clip)
 {
-    float g[8];
-    float2 w[4], m[4], v[4];
-    const long long at = rec.state_off + first;          // a multiple of kStateBlock
+    float2 w[4], m[4], v[4], g[4];
+    const float decay = tab.coef[t - tab.t0].x, step = tab.coef[t - tab.t0].y;
+    const unsigned long long at = rec.state_off + static_cast<unsigned long long>(first);    // a multiple of kStateBlock
     float *wp = rec.w + first;
     unsigned mcodes[2], vcodes[2];
     unsigned me = 0, ve = 0;
@@ -444,7 +447,7 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
             }
         }
     }
-    weighted_gradient<GT, VECTOR>(g, tab, t, first, lane, count);
+    weighted_gradient<GT, VECTOR, ONE>(g, tab, t, first, lane, count);
     if constexpr (BITS == 8) {
         BlockScale<true>(me).decode(m, mcodes[0], mcodes[1]);
         BlockScale<false>(ve).decode(v, vcodes[0], vcodes[1]);
@@ -462,7 +465,7 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
     float m_top = 0.f, v_top = 0.f;                      // the largest magnitudes; NaN if there is one
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        float2 x = make_float2(g[2 * k], g[2 * k + 1]);
+        float2 x = g[k];
         if (p.clip) x = mul2(x, two(clip));
         const float2 a = mul2(m[k], p.beta1), b = mul2(x, p.one_minus_beta1);
         const float2 c = mul2(v[k], p.beta2), d = mul2(mul2(x, x), p.one_minus_beta2);
@@ -589,22 +592,26 @@ __device__ __forceinline__ void adamw_block(const AdamwParams &p, const GradTabl
     }
 }
 
-// Blocks of two warps, so that an SM's registers are refilled in small pieces (61M elements, four fp32 gradients: 363 us, with eight warps
-// 370), and for 8-bit moments and a bf16 gradient, the form with the most instructions a byte, 18 of them an SM instead
-// of 16 (4.7e8 elements: 1455 us, with 16 1526).
-template <typename GT, int BITS>
-constexpr int adamw_blocks_per_sm() { return BITS == 8 && GradBytes<GT>::value == 2 ? 18 : 16; }
+// Blocks of two warps, so that an SM's registers are refilled in small pieces (61M elements, four fp32 gradients: 363 us, with
+// eight warps 370).  For 8-bit moments, the form with the most instructions a byte, 18 of them an SM instead of 16 where the
+// registers carry it, with one gradient (4.7e8 elements, fp32 gradient and a mirror: 1366 us, with 16 1402).
+//
+// A thread has only eight elements, so what it does once counts: with one gradient there is no loop over them, a tensor's two
+// factors are computed on the host, in fp64, and a record comes in three loads (4.7e8 elements, bf16 gradient, 8-bit moments, mirror:
+// 1295 us, 5.80 TB/s; with the loop, the factors in every thread and 64-bit chunk numbers 1451).
+template <int BITS, bool ONE>
+constexpr int adamw_blocks_per_sm() { return BITS == 8 && ONE ? 18 : 16; }
 
-template <typename GT, int BITS, int MAXP>
-__global__ void __launch_bounds__(kListThreads, adamw_blocks_per_sm<GT, BITS>()) adamw_kernel(const __grid_constant__ ListTables lt,
-                                                             const __grid_constant__ GradTable<MAXP> tab,
-                                                             const __grid_constant__ AdamwParams p)
+template <typename GT, int BITS, bool ONE, int MAXP>
+__global__ void __launch_bounds__(kListThreads, adamw_blocks_per_sm<BITS, ONE>()) adamw_kernel(const __grid_constant__ ListTables lt,
+                                                                                             const __grid_constant__ StepTable<MAXP> tab,
+                                                                                             const __grid_constant__ AdamwParams p)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long chunk = lt.chunk0 + blockIdx.x;
+    const unsigned chunk = lt.chunk0 + blockIdx.x;
     const int t = lt.chunk_tensor[chunk];
     const TensorRec rec = lt.recs[t];
-    const long long first = (chunk - rec.first_chunk) * kChunk + warp * kStateBlock;
+    const long long first = static_cast<long long>(chunk - rec.first_chunk) * kChunk + warp * kStateBlock;
     const long long left = rec.n - first;
     if (left <= 0) return;
     float clip = 1.f;
@@ -612,12 +619,9 @@ __global__ void __launch_bounds__(kListThreads, adamw_blocks_per_sm<GT, BITS>())
         if (!(fabsf(p.clip[0]) <= 3.402823466e38f)) return;          // the norm is not finite: the step changes nothing
         clip = p.clip[1];
     }
-    const bool on_grid = (reinterpret_cast<uintptr_t>(rec.w) & 15) == 0 && (reinterpret_cast<uintptr_t>(rec.mirror) & 7) == 0 && grads_on_grid<GT>(tab, t);
-    const float decay = static_cast<float>(1.0 - p.lr_decay * (static_cast<double>(rec.lr_mult) * rec.decay_mult));
-    const float step = static_cast<float>(p.step_size * rec.lr_mult);
     const int count = left < kStateBlock ? static_cast<int>(left) : kStateBlock;
-    if (count == kStateBlock && on_grid) adamw_block<GT, BITS, true>(p, tab, rec, t, first, lane, count, clip, decay, step);
-    else adamw_block<GT, BITS, false>(p, tab, rec, t, first, lane, count, clip, decay, step);
+    if (count == kStateBlock && rec.on_grid && grads_on_grid<GT, ONE>(tab, t)) adamw_block<GT, BITS, true, ONE>(p, tab, rec, t, first, lane, count, clip);
+    else adamw_block<GT, BITS, false, ONE>(p, tab, rec, t, first, lane, count, clip);
 }
 
 // Codes to the values they stand for.  One thread per eight elements of the state arrays, the gaps between the tensors included

@@ -8,6 +8,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <type_traits>
 #include <unordered_set>
 #include <utility>
 #include <vector>
@@ -23,6 +24,7 @@ using softsync::kListThreads;
 using softsync::kStateBlock;
 using softsync::ListTables;
 using softsync::NormTail;
+using softsync::StepTable;
 using softsync::TensorRec;
 
 static_assert(kStateBlock == PS_STATE_BLOCK, "the header's block is the kernels'");
@@ -31,7 +33,8 @@ namespace {
 
 constexpr int kNormBlocksPerSm = 3;         // one wave: as many as the registers let run at once
 constexpr int kNormMaxBlocks = 4096;
-constexpr int kSmallTable = 32, kMediumTable = 512, kLargeTable = 3840;   // gradient pointers one launch carries
+// Gradient pointers one launch carries: what fits the 32,764 bytes of its parameters, with a step's coefficients or without, and less.
+constexpr int kSmallTable = 32, kMediumTable = 512, kLargeTable = 3840, kLargeStepTable = 1920;
 
 }  // namespace
 
@@ -112,41 +115,44 @@ int check_gradients(const ps_tensors *list, const void *const *grads, int c, con
     return PS_OK;
 }
 
-// Calls launch(tables, gradient table) for consecutive ranges of tensors whose gradient pointers fit one launch.
-template <int MAXP, typename Launch>
-int for_each_range(const ps_tensors *list, const void *const *grads, int c, const float *scales, Launch launch)
+// Calls launch(tables, gradient table) for consecutive ranges of tensors whose gradient pointers fit one launch; coef(tensor) gives a
+// step's coefficients.
+template <typename Table, typename Coef, typename Launch>
+int for_each_range(const ps_tensors *list, const void *const *grads, int c, const float *scales, Coef coef, Launch launch)
 {
     const int n = static_cast<int>(list->recs.size());
-    const int most = MAXP / c;
-    GradTable<MAXP> tab;
+    const int most = Table::kPointers / c;
+    Table tab;
     std::memset(tab.s, 0, sizeof tab.s);
     for (int l = 0; l < c; ++l) tab.s[l] = scales ? scales[l] : 1.f;
     tab.c = c;
     for (int t0 = 0; t0 < n; t0 += most) {
         const int t1 = std::min(n, t0 + most);
-        for (int t = t0; t < t1; ++t)
+        for (int t = t0; t < t1; ++t) {
             for (int l = 0; l < c; ++l) tab.g[(t - t0) * c + l] = grads[static_cast<size_t>(l) * n + t];
+            coef(tab, t - t0, list->recs[t]);
+        }
         tab.t0 = t0;
         ListTables lt;
         lt.recs = list->recs_dev;
         lt.chunk_tensor = list->chunk_tensor_dev;
         lt.chunk0 = list->recs[t0].first_chunk;
-        lt.nchunks = (t1 < n ? list->recs[t1].first_chunk : list->chunks) - lt.chunk0;
+        lt.nchunks = (t1 < n ? list->recs[t1].first_chunk : static_cast<unsigned>(list->chunks)) - lt.chunk0;
         const int status = launch(lt, tab, t0 == 0, t1 == n);
         if (status != PS_OK) return status;
     }
     return PS_OK;
 }
 
-// The smallest of the three parameter blocks that carries the whole call, else the largest, several times: a launch's cost grows
+// The smallest of three parameter blocks that carries the whole call, else the largest, several times: a launch's cost grows
 // with its parameters, which the small lists feel and the large ones do not.
-template <typename Launch>
-int launch_ranges(const ps_tensors *list, const void *const *grads, int c, const float *scales, Launch launch)
+template <template <int> class Table, int LARGE, typename Coef, typename Launch>
+int launch_ranges(const ps_tensors *list, const void *const *grads, int c, const float *scales, Coef coef, Launch launch)
 {
     const int64_t pointers = static_cast<int64_t>(list->recs.size()) * c;
-    if (pointers <= kSmallTable) return for_each_range<kSmallTable>(list, grads, c, scales, launch);
-    if (pointers <= kMediumTable) return for_each_range<kMediumTable>(list, grads, c, scales, launch);
-    return for_each_range<kLargeTable>(list, grads, c, scales, launch);
+    if (pointers <= kSmallTable) return for_each_range<Table<kSmallTable>>(list, grads, c, scales, coef, launch);
+    if (pointers <= kMediumTable) return for_each_range<Table<kMediumTable>>(list, grads, c, scales, coef, launch);
+    return for_each_range<Table<LARGE>>(list, grads, c, scales, coef, launch);
 }
 
 uint32_t step_key(uint64_t seed, uint64_t step)          // SplitMix64's finaliser over the seed's step-th place
@@ -188,7 +194,7 @@ int ps_tensors_create(ps_tensors_t **out, int num_tensors, const int64_t *sizes_
     int64_t chunk = 0, state = 0;
     for (int k = 0; k < num_tensors; ++k) {
         TensorRec &r = list->recs[k];
-        r = TensorRec{nullptr, nullptr, sizes_host[k], state, chunk, 1.f, 1.f};
+        r = TensorRec{nullptr, nullptr, sizes_host[k], static_cast<unsigned long long>(state), static_cast<unsigned>(chunk), 0, 1.f, 1.f};
         const int64_t n = (sizes_host[k] + kChunk - 1) / kChunk;
         std::fill(map.begin() + chunk, map.begin() + chunk + n, k);
         chunk += n;
@@ -249,6 +255,7 @@ int ps_tensors_bind_adamw(ps_tensors_t *list, float *const *weights_host, void *
         r.mirror = mirrors_host ? static_cast<unsigned short *>(mirrors_host[k]) : nullptr;
         r.lr_mult = lr_mult_host ? lr_mult_host[k] : 1.f;
         r.decay_mult = decay_mult_host ? decay_mult_host[k] : 1.f;
+        r.on_grid = aligned_to(r.w, 16) && aligned_to(r.mirror, 8);
         if (!std::isfinite(r.lr_mult) || !std::isfinite(r.decay_mult)) return PS_ERR_INVALID_ARG;
         if (!r.n) continue;
         if (!r.w || !aligned_to(r.w, 4) || !aligned_to(r.mirror, 2)) return PS_ERR_INVALID_ARG;
@@ -278,8 +285,9 @@ int ps_grad_norm(ps_tensors_t *list, const void *const *grads_host, int c, const
     DeviceSwitch guard(list->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int grid = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({list->chunks, static_cast<int64_t>(kNormBlocksPerSm) * list->sm_count, kNormMaxBlocks})));
-    return launch_ranges(list, grads_host, c, scales_host, [&](const ListTables &lt, const auto &tab, bool first, bool last) {
-        constexpr int MAXP = static_cast<int>(sizeof(tab.g) / sizeof(void *));
+    const auto none = [](auto &, int, const TensorRec &) {};
+    return launch_ranges<GradTable, kLargeTable>(list, grads_host, c, scales_host, none, [&](const ListTables &lt, const auto &tab, bool first, bool last) {
+        constexpr int MAXP = std::decay_t<decltype(tab)>::kPointers;
         const NormTail tail{list->partial_dev, list->done_dev, out_dev, max_norm, first ? 0 : 1, last ? 1 : 0};
         const auto go = [&](auto kernel) { kernel<<<grid, softsync::kNormThreads, 0, st>>>(lt, tab, tail); };
         if (grad_dtype == PS_GRAD_BF16) c == 1 ? go(softsync::grad_norm_kernel<GradBf16, true, MAXP>) : go(softsync::grad_norm_kernel<GradBf16, false, MAXP>);
@@ -305,8 +313,7 @@ int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, cons
     AdamwParams p;
     p.m = list->m; p.v = list->v; p.m_scale = list->m_scale; p.v_scale = list->v_scale;
     p.clip = clip_dev;
-    p.lr_decay = k.lr * k.weight_decay;
-    p.step_size = k.lr / (1.0 - std::pow(k.beta1, t));
+    const double lr_decay = k.lr * k.weight_decay, step_size = k.lr / (1.0 - std::pow(k.beta1, t));
     const auto twice = [](double x) { return make_float2(static_cast<float>(x), static_cast<float>(x)); };
     p.beta1 = twice(k.beta1);
     p.one_minus_beta1 = twice(1.0 - k.beta1);
@@ -318,17 +325,22 @@ int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, cons
     p.key = step_key(k.seed, static_cast<uint64_t>(k.step));
     DeviceSwitch guard(list->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return launch_ranges(list, grads_host, c, scales_host, [&](const ListTables &lt, const auto &tab, bool, bool) {
-        constexpr int MAXP = static_cast<int>(sizeof(tab.g) / sizeof(void *));
+    const auto coef = [&](auto &tab, int i, const TensorRec &r) {
+        tab.coef[i] = make_float2(static_cast<float>(1.0 - lr_decay * (static_cast<double>(r.lr_mult) * r.decay_mult)), static_cast<float>(step_size * r.lr_mult));
+    };
+    return launch_ranges<StepTable, kLargeStepTable>(list, grads_host, c, scales_host, coef, [&](const ListTables &lt, const auto &tab, bool, bool) {
+        constexpr int MAXP = std::decay_t<decltype(tab)>::kPointers;
         if (lt.nchunks == 0) return static_cast<int>(PS_OK);
-        const unsigned grid = static_cast<unsigned>(lt.nchunks);
-        if (list->state_bits == 32) {
-            if (grad_dtype == PS_GRAD_BF16) softsync::adamw_kernel<GradBf16, 32, MAXP><<<grid, kListThreads, 0, st>>>(lt, tab, p);
-            else softsync::adamw_kernel<GradFp32, 32, MAXP><<<grid, kListThreads, 0, st>>>(lt, tab, p);
-        } else {
-            if (grad_dtype == PS_GRAD_BF16) softsync::adamw_kernel<GradBf16, 8, MAXP><<<grid, kListThreads, 0, st>>>(lt, tab, p);
-            else softsync::adamw_kernel<GradFp32, 8, MAXP><<<grid, kListThreads, 0, st>>>(lt, tab, p);
-        }
+        const auto go = [&](auto kernel) { kernel<<<lt.nchunks, kListThreads, 0, st>>>(lt, tab, p); };
+        const auto with = [&](auto grad, auto bits) {
+            using GT = decltype(grad);
+            if (c == 1) go(softsync::adamw_kernel<GT, decltype(bits)::value, true, MAXP>);
+            else go(softsync::adamw_kernel<GT, decltype(bits)::value, false, MAXP>);
+        };
+        using Bits8 = std::integral_constant<int, 8>;
+        using Bits32 = std::integral_constant<int, 32>;
+        if (list->state_bits == 32) grad_dtype == PS_GRAD_BF16 ? with(GradBf16{}, Bits32{}) : with(GradFp32{}, Bits32{});
+        else grad_dtype == PS_GRAD_BF16 ? with(GradBf16{}, Bits8{}) : with(GradFp32{}, Bits8{});
         return cudaGetLastError() == cudaSuccess ? static_cast<int>(PS_OK) : static_cast<int>(PS_ERR_CUDA);
     });
   } PS_CATCH_ALL
