@@ -634,26 +634,36 @@ static __global__ void __launch_bounds__(32) policy_terms_kernel(const __grid_co
 }
 
 // ---- the policy loss, rows kept on chip -------------------------------------------------------------------------------------
-constexpr int kRingThreads = 256, kRingVectors = 4, kRingChunk = kRingThreads * kRingVectors;      // vectors of a chunk: 16 KB
-constexpr int kRingSlots = 7;             // 112 KB of shared memory: two blocks an SM
-constexpr int kRingBytes = kRingSlots * kRingChunk * 16;
+constexpr int kRingVectors = 4, kRingSlots = 7;
+constexpr int kNarrow = 256, kWide = 512;           // threads that do the arithmetic
+template <int T>
+struct RingShape {
+    static constexpr int chunk = T * kRingVectors;  // vectors: 16 or 32 KB
+    static constexpr int row = kRingSlots * chunk;  // the most of a row that one block holds
+    static constexpr int bytes = row * 16;          // 112 or 224 KB of shared memory
+    static constexpr int block = T + 64;            // and two warps more
+    static constexpr int per_sm = kWide / T;
+};
 
 constexpr int kOwnTotalRows = 4096;       // up to here every block adds the weights up for itself: no kernel before this one
 
 struct RingPlan {
     int vectors, chunks;                  // of a row, in each block of its cluster
+    int ahead;                            // chunks of the next row that fit the ring beside a whole row
     int own_total;
     int wait_limit;
 };
 
+template <int T>
 struct RingShared {
-    float warp[3][kRingThreads / 32];
+    float warp[3][T / 32];     // each warp's m, s, t
     float part[2][3][kMaxCluster];        // each block's m, s, t by the parity of the row, written by the blocks
     float row[6];                         // m, log2 s, entropy, a, b, token's logit
     int tok;                              // -1 where it is out of range
+    float inv_weight;
     double sums[5];                       // of the cluster's rows, kept by its first block
-    double scratch[kRingThreads / 32];
-    unsigned long long full[kRingSlots], empty[kRingSlots], exchange[2];
+    double scratch[T / 32];
+    unsigned long long full[kRingSlots], empty[kRingSlots], exchange[2], ready, go;
 };
 
 __device__ __forceinline__ void mbar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
@@ -673,28 +683,30 @@ __device__ __forceinline__ bool mbar_wait_cluster_bounded(unsigned bar, unsigned
     }
     return false;
 }
-__device__ __forceinline__ void ring_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kRingThreads) : "memory"); }
+template <int T>
+__device__ __forceinline__ void ring_sync() { asm volatile("bar.sync 1, %0;" :: "n"(T) : "memory"); }
 
 // Statistics, loss terms and gradient (out: null for none) of all rows from one read of the logits: a row is spread over the shared
-// memory of a cluster of blocks and stays there between its statistics and its gradient.  Each block has a ring of 16 KB slots that one thread of an
-// extra warp keeps filling with bulk copies, chunk after chunk and row after row; the eight other warps take a row's statistics
-// chunk by chunk as it arrives, exchange them with the cluster's other blocks, and release each slot once the chunk's
-// gradient is written, so the next row's chunks are under way long before this one is done.  Two blocks an SM: one's exchange runs
-// under the other's arithmetic.  The clusters are as many as fit the GPU, each takes every parts-th row.
+// memory of a cluster of blocks and stays there between its statistics and its gradient.  Each block has a ring of slots that one thread
+// of the copying warp keeps filling with bulk copies, chunk after chunk and row after row.  T threads take a row's statistics chunk by
+// chunk as it arrives, and write its gradient, releasing each slot as they go.  In between the joining warp adds up what the
+// warps and the cluster's other blocks found, computes the loss terms and the factors, while the T threads already take the statistics
+// of the next row's first chunks, as many as the ring has room for beside the whole row.  The clusters are as many as fit the GPU, each
+// takes every parts-th row.
 //
 // A vector at a row's ragged end comes with ordinary loads, through a register of the thread that handles it (the last thread the
 // front's, the first thread the end's: never the same one).
 //
 // Every wait is bounded.  One that runs out makes the block's later rows NaN; it waits for nothing after that, but the copying thread
 // still sees, with a limit, its last copies arrive.
-template <typename GT, bool ENTROPY_GRAD>
-__global__ void __launch_bounds__(kRingThreads + 32, 2) policy_ring_kernel(const __grid_constant__ RowsIn in, const __grid_constant__ PolicyIn pin,
-                                                                           const __grid_constant__ PolicyState st, float *logp, float *entropy,
-                                                                           unsigned char *out, long long out_stride, const __grid_constant__ RingPlan plan)
+template <typename GT, bool ENTROPY_GRAD, int T>
+__global__ void __launch_bounds__(RingShape<T>::block, RingShape<T>::per_sm) policy_ring_kernel(const __grid_constant__ RowsIn in, const __grid_constant__ PolicyIn pin,
+                                                                    const __grid_constant__ PolicyState st, float *logp, float *entropy,
+                                                                    unsigned char *out, long long out_stride, const __grid_constant__ RingPlan plan)
 {
-    constexpr int T = kRingThreads, NV = kRingVectors, PV = per_vector<GT>();
+    constexpr int NV = kRingVectors, PV = per_vector<GT>(), kRingChunk = RingShape<T>::chunk;
     extern __shared__ __align__(128) unsigned char ring[];
-    __shared__ RingShared sh;
+    __shared__ RingShared<T> sh;
     const int blocks = cluster_size(), rank = cluster_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int parts = gridDim.x / static_cast<unsigned>(blocks), vocab = static_cast<int>(in.vocab);
     const long long r0 = blockIdx.x / static_cast<unsigned>(blocks);
@@ -702,20 +714,27 @@ __global__ void __launch_bounds__(kRingThreads + 32, 2) policy_ring_kernel(const
     if (tid == 0) {
         for (int k = 0; k < kRingSlots; ++k) { mbar_init(smem_addr(&sh.full[k]), 1); mbar_init(smem_addr(&sh.empty[k]), T / 32); }
         for (int k = 0; k < 2; ++k) mbar_init(smem_addr(&sh.exchange[k]), blocks);
+        mbar_init(smem_addr(&sh.ready), T / 32);
+        mbar_init(smem_addr(&sh.go), 1);
         for (int k = 0; k < 5; ++k) sh.sums[k] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
     cluster_arrive();
     cluster_wait();                                        // every block's barriers are there
+    const auto row_at = [&](long long r) { return in.data + r * in.stride * logit_bytes<GT>(); };
 
     if (warp == T / 32) {                                  // the copying warp
         if (lane == 0) {
             unsigned g = 0;                                // chunks issued
             bool late = false;
+            const auto weight = [&](long long r) { return in.weights && r < in.rows ? in.weights[r] : 1.f; };
+            float w = weight(r0);
             for (long long r = r0; r < in.rows && !late; r += parts) {
-                if (in.weights && in.weights[r] == 0.f) continue;
-                const RowVectors<GT> v(in.data + r * in.stride * logit_bytes<GT>(), vocab);
+                const bool dead = w == 0.f;
+                w = weight(r + parts);
+                if (dead) continue;
+                const RowVectors<GT> v(row_at(r), vocab);
                 const int hi = min(lo + plan.vectors, v.full);
                 for (int c = 0; c < plan.chunks; ++c, ++g) {
                     const unsigned slot = g % kRingSlots, round = g / kRingSlots;
@@ -729,157 +748,171 @@ __global__ void __launch_bounds__(kRingThreads + 32, 2) policy_ring_kernel(const
                 mbar_wait_bounded(smem_addr(&sh.full[k % kRingSlots]), (k / kRingSlots) & 1, plan.wait_limit);
         }
         __syncwarp();
-    } else {
-        const bool head = warp == 0;
-        // what warp 0 needs beside the logits is read a row ahead: the token first, then what hangs on it
-        struct Scalars { float x_tok, adv, old_logp, ref_logp; long long tok; };
-        auto weight = [&](long long i) { return i < in.rows ? (in.weights ? in.weights[i] : 1.f) : 0.f; };
-        auto first_scalars = [&](long long i, Scalars &o) {
-            if (!head || i >= in.rows) return;
-            o.tok = in.tokens[i];
-            o.adv = pin.advantages[i];
-            o.old_logp = pin.old_logp[i];
-            o.ref_logp = pin.ref_logp ? pin.ref_logp[i] : 0.f;
-        };
-        auto token_logit = [&](long long i, float wi, Scalars &o) {
-            if (head && wi != 0.f)
-                o.x_tok = o.tok >= 0 && o.tok < in.vocab ? logit_at(static_cast<const GT *>(nullptr), in.data + i * in.stride * logit_bytes<GT>(), o.tok) : CUDART_NAN_F;
-        };
-        Scalars now = {}, then = {};
-        float w = weight(r0);
-        first_scalars(r0, now);
-        token_logit(r0, w, now);
-        float inv_weight = 0.f;
-        if (plan.own_total) {
-            double sum = in.weights ? 0.0 : static_cast<double>(in.rows);
-            if (in.weights) {
-                for (int i = tid; i < static_cast<int>(in.rows); i += T) sum += in.weights[i];
-                sum = block_total(sum, sh.scratch, T, ring_sync);
+    } else if (warp > T / 32) {                            // the joining warp
+        long long r = r0, tok = 0;
+        float w = 0.f, x_tok = 0.f, adv = 0.f, old_logp = 0.f, ref_logp = 0.f;
+        const auto find = [&] {                            // the next row with a weight, and what belongs to it beside its logits
+            for (; r < in.rows; r += parts) {
+                w = in.weights ? in.weights[r] : 1.f;
+                if (w != 0.f) break;
+                if (rank == 0 && lane == 0) { logp[r] = 0.f; entropy[r] = 0.f; }
             }
-            inv_weight = static_cast<float>(inverse_or_zero(sum));
-        } else if (head) {
+            if (r >= in.rows) return;
+            tok = in.tokens[r];
+            adv = pin.advantages[r];
+            old_logp = pin.old_logp[r];
+            ref_logp = pin.ref_logp ? pin.ref_logp[r] : 0.f;
+            x_tok = tok >= 0 && tok < in.vocab ? logit_at(static_cast<const GT *>(nullptr), row_at(r), tok) : CUDART_NAN_F;
+        };
+        find();
+        float inv_weight = 0.f;
+        if (!plan.own_total) {
             griddep_wait();
             inv_weight = static_cast<float>(__ldcg(st.inv_weight));
         }
-        int slot = 0;                                      // of the row's first chunk, and the phase it is in
-        unsigned phase = 0, turn = 0;                      // turn: rows exchanged so far
         bool late = false;
-        auto advance = [](int &k, unsigned &ph) { if (++k == kRingSlots) { k = 0; ph ^= 1; } };
-        for (long long r = r0; r < in.rows; r += parts) {
-            const float w_next = weight(r + parts);
-            first_scalars(r + parts, then);
-            unsigned char *dst = out + r * out_stride * logit_bytes<GT>();
-            if (w == 0.f) {                                // the whole cluster takes this way
-                token_logit(r + parts, w_next, then);
-                if (out) zero_row<GT>(dst, vocab, rank * T + tid, blocks * T);
-                if (rank == 0 && tid == 0) { logp[r] = 0.f; entropy[r] = 0.f; }
-                w = w_next;
-                now = then;
-                continue;
-            }
-            const RowVectors<GT> v(in.data + r * in.stride * logit_bytes<GT>(), vocab);
-            const int hi = min(lo + plan.vectors, v.full);              // vectors of the block that are in the ring: [max(lo, inner), hi)
-            uint4 edge[1];
-            int edge_q = -1;
-            if (v.ragged()) {
-                if (v.phase && v.full && lo == 0 && tid == T - 1) edge_q = 0;
-                if (v.count != v.full && v.full >= lo && v.full < lo + plan.vectors && tid == 0) edge_q = v.full;
-                edge[0] = edge_q >= 0 ? load_ragged_vector<GT>(v.row, v.first(edge_q), vocab) : no_vector<GT>();
-            }
-
-            float m = kLowest, s = 0.f, t = 0.f;
-            const bool clean = lo >= v.inner;              // no ragged front in the block's first chunk
-            int here = slot;
-            unsigned ph = phase;
-            for (int left = hi - lo, c = 0; c < plan.chunks; ++c, left -= kRingChunk) {
-                late = late || !mbar_wait_bounded(smem_addr(&sh.full[here]), ph, plan.wait_limit);
-                const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + here * kRingChunk + tid;
-                if (left > T * NV / 2) {
-                    uint4 x[NV];
-#pragma unroll
-                    for (int k = 0; k < NV; ++k) x[k] = mine[k * T];
-                    if (left < kRingChunk)
-#pragma unroll
-                        for (int k = 0; k < NV; ++k)
-                            if (k * T + tid >= left) x[k] = no_vector<GT>();
-                    if (c == 0 && !clean && tid == 0) x[0] = no_vector<GT>();
-                    add_vectors<GT, NV, true>(x, in.scale, m, s, t);
-                } else {
-                    for (int k = 0; k * T < left; ++k) {
-                        uint4 x[1] = {no_vector<GT>()};
-                        if (k * T + tid < left && (c > 0 || k * T + tid > 0 || clean)) x[0] = mine[k * T];
-                        add_vectors<GT, 1, true>(x, in.scale, m, s, t);
-                    }
+        for (unsigned turn = 0; r < in.rows; ++turn) {
+            late = late || !mbar_wait_bounded(smem_addr(&sh.ready), turn & 1, plan.wait_limit);
+            if (plan.own_total) inv_weight = sh.inv_weight;
+            float m = lane < T / 32 ? sh.warp[0][lane] : kLowest, s = lane < T / 32 ? sh.warp[1][lane] : 0.f, t = lane < T / 32 ? sh.warp[2][lane] : 0.f;
+            join_lanes(in.scale, m, s, t);
+            if (blocks > 1) {
+                const unsigned parity = turn & 1;
+                if (lane < blocks) {
+                    store_to_rank(&sh.part[parity][0][rank], lane, m);
+                    store_to_rank(&sh.part[parity][1][rank], lane, s);
+                    store_to_rank(&sh.part[parity][2][rank], lane, t);
+                    mbar_arrive_remote(&sh.exchange[parity], lane);
                 }
-                advance(here, ph);
-            }
-            if (v.ragged() && __any_sync(0xffffffffu, edge_q >= 0)) add_vectors<GT, 1, true>(edge, in.scale, m, s, t);
-            if (late) s = CUDART_NAN_F;
-
-            s = warp_sum(s);
-            t = warp_sum(t);
-            if (lane == 0) { sh.warp[0][warp] = m; sh.warp[1][warp] = s; sh.warp[2][warp] = t; }
-            ring_sync();
-            if (head) {
-                m = lane < T / 32 ? sh.warp[0][lane] : kLowest;
-                s = lane < T / 32 ? sh.warp[1][lane] : 0.f;
-                t = lane < T / 32 ? sh.warp[2][lane] : 0.f;
+                late = late || !mbar_wait_cluster_bounded(smem_addr(&sh.exchange[parity]), (turn >> 1) & 1, plan.wait_limit);
+                m = lane < blocks ? sh.part[parity][0][lane] : kLowest;
+                s = lane < blocks ? sh.part[parity][1][lane] : 0.f;
+                t = lane < blocks ? sh.part[parity][2][lane] : 0.f;
                 join_lanes(in.scale, m, s, t);
-                if (blocks > 1) {
-                    const unsigned parity = turn & 1;
-                    if (lane < blocks) {
-                        store_to_rank(&sh.part[parity][0][rank], lane, m);
-                        store_to_rank(&sh.part[parity][1][rank], lane, s);
-                        store_to_rank(&sh.part[parity][2][rank], lane, t);
-                        mbar_arrive_remote(&sh.exchange[parity], lane);
-                    }
-                    late = late || !mbar_wait_cluster_bounded(smem_addr(&sh.exchange[parity]), (turn >> 1) & 1, plan.wait_limit);
-                    m = lane < blocks ? sh.part[parity][0][lane] : kLowest;
-                    s = lane < blocks ? sh.part[parity][1][lane] : 0.f;
-                    t = lane < blocks ? sh.part[parity][2][lane] : 0.f;
-                    join_lanes(in.scale, m, s, t);
-                    if (late) s = CUDART_NAN_F;
-                }
-                const float l2 = log2f(s), h = kLn2 * (l2 - t / s);
-                const float lp = (now.x_tok - m) * in.inv_temperature - kLn2 * l2;
-                const PolicyTerms o = policy_terms(pin, now.adv, now.old_logp, now.ref_logp, lp, h);
-                const float share = w * inv_weight;
-                if (lane == 0) {
-                    sh.row[0] = m; sh.row[1] = l2; sh.row[2] = h; sh.row[5] = now.x_tok;
-                    sh.row[3] = o.slope * share * in.inv_temperature;
-                    sh.row[4] = pin.entropy_coef * share * in.inv_temperature;
-                    sh.tok = now.tok >= 0 && now.tok < in.vocab ? static_cast<int>(now.tok) : -1;
-                }
-                if (rank == 0 && lane == 0) {
+            }
+            if (late) s = CUDART_NAN_F;
+            const float l2 = log2f(s), h = kLn2 * (l2 - t / s);
+            const float lp = (x_tok - m) * in.inv_temperature - kLn2 * l2;
+            const PolicyTerms o = policy_terms(pin, adv, old_logp, ref_logp, lp, h);
+            const float share = w * inv_weight;
+            if (lane == 0) {
+                sh.row[0] = m; sh.row[1] = l2; sh.row[2] = h; sh.row[5] = x_tok;
+                sh.row[3] = o.slope * share * in.inv_temperature;
+                sh.row[4] = pin.entropy_coef * share * in.inv_temperature;
+                sh.tok = tok >= 0 && tok < in.vocab ? static_cast<int>(tok) : -1;
+                mbar_arrive(smem_addr(&sh.go));
+                if (rank == 0) {
                     logp[r] = lp;
                     entropy[r] = h;
 #pragma unroll
                     for (int k = 0; k < 5; ++k) sh.sums[k] += static_cast<double>(share) * o.v[k];
                 }
             }
+            __syncwarp();
+            r += parts;
+            find();
+        }
+        if (rank == 0) finish_sums(st, static_cast<int>(r0), parts, sh.sums);
+    } else {
+        if (plan.own_total) {
+            double sum = in.weights ? 0.0 : static_cast<double>(in.rows);
+            if (in.weights) {
+                for (int i = tid; i < static_cast<int>(in.rows); i += T) sum += in.weights[i];
+                sum = block_total(sum, sh.scratch, T, ring_sync<T>);
+            }
+            if (tid == 0) sh.inv_weight = static_cast<float>(inverse_or_zero(sum));
+        }
+        // The first row from r on that has a weight; those before it become zero.  w: the weight of r itself.
+        const auto weight = [&](long long r) { return in.weights && r < in.rows ? in.weights[r] : 1.f; };
+        const auto find = [&](long long r, float w) {
+            for (; r < in.rows && w == 0.f; r += parts, w = weight(r))
+                if (out) zero_row<GT>(out + r * out_stride * logit_bytes<GT>(), vocab, rank * T + tid, blocks * T);
+            return r;
+        };
+        const auto advance = [](int &k) { if (++k == kRingSlots) { k = 0; return 1u; } return 0u; };
+        long long due = find(r0, weight(r0)), r = due;     // due: the row whose gradient comes next; r: it or the next, whose statistics are taken
+        float m = kLowest, s = 0.f, t = 0.f, w_next = weight(due + parts);
+        int c = 0, here = 0, slot = 0;                     // r's next chunk and its slot; the slot of the gradient's next chunk
+        unsigned ph = 0, turn = 0;
+        bool late = false;
+        uint4 edge[1];
+        int edge_q = -1;
+        while (due < in.rows) {
+            {
+                const RowVectors<GT> v(row_at(r), vocab);
+                const int hi = min(lo + plan.vectors, v.full);          // vectors of the block that are in the ring: [max(lo, inner), hi)
+                const bool clean = lo >= v.inner;          // no ragged front in the block's first chunk
+                const int until = r == due ? plan.chunks : plan.ahead;
+                for (int left = hi - lo - c * kRingChunk; c < until; ++c, left -= kRingChunk) {
+                    late = late || !mbar_wait_bounded(smem_addr(&sh.full[here]), ph, plan.wait_limit);
+                    const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + here * kRingChunk + tid;
+                    if (left > T * NV / 2) {
+                        uint4 x[NV];
+#pragma unroll
+                        for (int k = 0; k < NV; ++k) x[k] = mine[k * T];
+                        if (left < kRingChunk)
+#pragma unroll
+                            for (int k = 0; k < NV; ++k)
+                                if (k * T + tid >= left) x[k] = no_vector<GT>();
+                        if (c == 0 && !clean && tid == 0) x[0] = no_vector<GT>();
+                        add_vectors<GT, NV, true>(x, in.scale, m, s, t);
+                    } else {
+                        for (int k = 0; k * T < left; ++k) {
+                            uint4 x[1] = {no_vector<GT>()};
+                            if (k * T + tid < left && (c > 0 || k * T + tid > 0 || clean)) x[0] = mine[k * T];
+                            add_vectors<GT, 1, true>(x, in.scale, m, s, t);
+                        }
+                    }
+                    ph ^= advance(here);
+                }
+                if (r == due) {
+                    edge_q = -1;
+                    if (v.ragged()) {
+                        if (v.phase && v.full && lo == 0 && tid == T - 1) edge_q = 0;
+                        if (v.count != v.full && v.full >= lo && v.full < lo + plan.vectors && tid == 0) edge_q = v.full;
+                        edge[0] = edge_q >= 0 ? load_ragged_vector<GT>(v.row, v.first(edge_q), vocab) : no_vector<GT>();
+                        if (__any_sync(0xffffffffu, edge_q >= 0)) add_vectors<GT, 1, true>(edge, in.scale, m, s, t);
+                    }
+                    if (late) s = CUDART_NAN_F;
+                    s = warp_sum(s);
+                    t = warp_sum(t);
+                    if (lane == 0) {
+                        sh.warp[0][warp] = m; sh.warp[1][warp] = s; sh.warp[2][warp] = t;
+                        mbar_arrive(smem_addr(&sh.ready));
+                    }
+                    r = find(r + parts, w_next);
+                    w_next = weight(r + parts);
+                    c = 0;
+                    m = kLowest; s = 0.f; t = 0.f;
+                    if (r < in.rows && plan.ahead > 0) continue;
+                }
+            }
+            late = late || !mbar_wait_bounded(smem_addr(&sh.go), turn & 1, plan.wait_limit);
             ++turn;
-            ring_sync();
-            token_logit(r + parts, w_next, then);
-            const RowGradient f(sh.row[0], sh.row[1], in.scale, RowCoef{sh.row[3], sh.row[4]}, sh.row[2]);
+            const RowGradient f(sh.row[0], late ? CUDART_NAN_F : sh.row[1], in.scale, RowCoef{sh.row[3], sh.row[4]}, sh.row[2]);
             const int tok = sh.tok;
+            const RowVectors<GT> v(row_at(due), vocab);
+            const int hi = min(lo + plan.vectors, v.full);
+            const bool clean = lo >= v.inner;
+            unsigned char *dst = out + due * out_stride * logit_bytes<GT>();
             const bool plain = ((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c);
             unsigned char *p = dst - v.phase * logit_bytes<GT>() + static_cast<long long>(lo + tid) * 16;
-            for (int left = hi - lo, c = 0; c < plan.chunks; ++c, left -= kRingChunk) {
+            for (int left = hi - lo, i = 0; i < plan.chunks; ++i, left -= kRingChunk) {
                 const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + slot * kRingChunk + tid;
                 if (out && plain) {
-                    if (left >= kRingChunk && (c > 0 || clean)) {
+                    if (left >= kRingChunk && (i > 0 || clean)) {
 #pragma unroll
                         for (int k = 0; k < NV; ++k) __stcs(reinterpret_cast<uint4 *>(p + k * T * 16), f.template vector<GT, ENTROPY_GRAD>(mine[k * T]));
                     } else {
 #pragma unroll
                         for (int k = 0; k < NV; ++k)
-                            if (k * T + tid < left && (c > 0 || k * T + tid > 0 || clean))
+                            if (k * T + tid < left && (i > 0 || k * T + tid > 0 || clean))
                                 __stcs(reinterpret_cast<uint4 *>(p + k * T * 16), f.template vector<GT, ENTROPY_GRAD>(mine[k * T]));
                     }
                     p += kRingChunk * 16;
                 } else if (out) {
                     const unsigned char *bytes = ring + slot * kRingChunk * 16;
-                    const int base = lo + c * kRingChunk, first = v.first(base), begin = v.first(max(base, v.inner)), end = v.first(min(base + kRingChunk, hi));
+                    const int base = lo + i * kRingChunk, first = v.first(base), begin = v.first(max(base, v.inner)), end = v.first(min(base + kRingChunk, hi));
                     for (int j = begin + tid; j < end; j += T) {
                         const float x = f.template single<GT, ENTROPY_GRAD>(logit_at(static_cast<const GT *>(nullptr), bytes, j - first));
                         store_logit<GT>(dst, j, j == tok ? __fadd_rn(x, f.one) : x);
@@ -887,7 +920,7 @@ __global__ void __launch_bounds__(kRingThreads + 32, 2) policy_ring_kernel(const
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.empty[slot]));
-                advance(slot, phase);
+                advance(slot);
             }
             if (out && plain && tok >= 0) {                // the token's entry once more, with its one, by the thread that has just written it
                 const int q = (tok + v.phase) / PV;
@@ -906,12 +939,8 @@ __global__ void __launch_bounds__(kRingThreads + 32, 2) policy_ring_kernel(const
                     store_logit<GT>(dst, j, j == tok ? __fadd_rn(x, f.one) : x);
                 }
             }
-            w = w_next;
-            now = then;
-        }
-        if (head && rank == 0) {
-            __syncwarp();
-            finish_sums(st, static_cast<int>(r0), parts, sh.sums);
+            __syncwarp();                                  // the row's shared values are read: lane 0 may tell of the next row
+            due = r;
         }
     }
     cluster_arrive();

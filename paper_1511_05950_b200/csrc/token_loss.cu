@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 using softsync::aligned_to;
 using softsync::GradBf16;
@@ -193,19 +194,20 @@ struct PolicyCall {
 };
 
 // Clusters of the ring kernel that run at once on the current GPU (asked once for each kernel, cluster size and GPU).
-template <typename GT, bool ENTROPY_GRAD>
+template <typename GT, bool ENTROPY_GRAD, int T>
 int resident_clusters(int cluster)
 {
-    const auto kernel = softsync::policy_ring_kernel<GT, ENTROPY_GRAD>;
+    using Shape = softsync::RingShape<T>;
+    const auto kernel = softsync::policy_ring_kernel<GT, ENTROPY_GRAD, T>;
     static std::atomic<int> known[64][kMaxCluster + 1] = {};
     int device = 0, n = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return 0;
     if ((n = known[device][cluster].load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, softsync::kRingBytes) != cudaSuccess) return 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::bytes) != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(cluster));
-    cfg.blockDim = dim3(softsync::kRingThreads + 32);
-    cfg.dynamicSmemBytes = softsync::kRingBytes;
+    cfg.blockDim = dim3(Shape::block);
+    cfg.dynamicSmemBytes = Shape::bytes;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
@@ -217,37 +219,51 @@ int resident_clusters(int cluster)
     return n;
 }
 
-template <typename GT, bool ENTROPY_GRAD>
+template <typename GT, bool ENTROPY_GRAD, int T>
 int launch_ring_as(const PolicyCall &k, int cluster, cudaStream_t st)
 {
-    auto kernel = softsync::policy_ring_kernel<GT, ENTROPY_GRAD>;
+    using Shape = softsync::RingShape<T>;
+    auto kernel = softsync::policy_ring_kernel<GT, ENTROPY_GRAD, T>;
     softsync::RingPlan plan;
     plan.vectors = static_cast<int>(div_up(k.vectors, cluster));
-    plan.chunks = static_cast<int>(div_up(plan.vectors, softsync::kRingChunk));
+    plan.chunks = static_cast<int>(div_up(plan.vectors, Shape::chunk));
+    plan.ahead = std::min(plan.chunks, softsync::kRingSlots - plan.chunks);
     plan.own_total = k.rows.rows <= softsync::kOwnTotalRows;
     plan.wait_limit = kWaitLimit;
-    const int64_t parts = std::min({static_cast<int64_t>(k.rows.rows), static_cast<int64_t>(resident_clusters<GT, ENTROPY_GRAD>(cluster)), kMaxParts});
+    const int64_t parts = std::min({static_cast<int64_t>(k.rows.rows), static_cast<int64_t>(resident_clusters<GT, ENTROPY_GRAD, T>(cluster)), kMaxParts});
     if (parts < 1) return PS_ERR_CUDA;
-    return launch_rows(kernel, parts, cluster, softsync::kRingThreads + 32, softsync::kRingBytes, !plan.own_total, st, k.rows, k.in, k.st, k.logp, k.entropy,
+    return launch_rows(kernel, parts, cluster, Shape::block, Shape::bytes, !plan.own_total, st, k.rows, k.in, k.st, k.logp, k.entropy,
                        k.out, static_cast<long long>(k.stride), plan);
 }
 
-int launch_ring(int dtype, const PolicyCall &k, int cluster, cudaStream_t st)
+// Which ring kernel, and the blocks that a row is spread over; no blocks: the row does not fit.
+//
+// As few blocks as hold a row: more means more exchange, and a cluster's blocks wait for one another at every row.  A row that fits one
+// narrow block has two of them on an SM, in different phases (16384 x 50257 bf16: 629 us, one wide block 715); one that needs more takes one
+// or two wide blocks (8192 x 152000 bf16: 937 us with two, 1011 with three narrow ones; 8192 x 65536: 380 with one, 406 with two).  Three
+// wide blocks leave more SMs out than five narrow ones (4096 x 128000 fp32: 777 us, 698), so beyond two the narrow ones take over as far
+// as they go.  Where rows are so few that the GPU would stay half empty, more narrow blocks share each (48 x 32000 bf16: 11.7 us with four).
+struct RingChoice { int threads, cluster; };
+RingChoice ring_choice(int64_t vectors, int64_t rows)
 {
-    const bool ent = k.in.entropy_coef != 0.f;
-    if (dtype == PS_GRAD_BF16) return ent ? launch_ring_as<GradBf16, true>(k, cluster, st) : launch_ring_as<GradBf16, false>(k, cluster, st);
-    return ent ? launch_ring_as<GradFp32, true>(k, cluster, st) : launch_ring_as<GradFp32, false>(k, cluster, st);
+    const int64_t narrow = div_up(vectors, softsync::RingShape<softsync::kNarrow>::row), wide = div_up(vectors, softsync::RingShape<softsync::kWide>::row);
+    if (narrow > 1 && (wide <= 2 || narrow > kMaxCluster) && (narrow > kMaxCluster || rows * narrow > sm_count()))
+        return RingChoice{softsync::kWide, wide <= kMaxCluster ? static_cast<int>(wide) : 0};
+    int64_t cluster = narrow;
+    while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= 2 * sm_count() && vectors > cluster * softsync::kNarrow) cluster *= 2;
+    return RingChoice{softsync::kNarrow, static_cast<int>(cluster)};
 }
 
-// Blocks that a row is spread over for the ring kernel; 0: it does not fit the largest cluster.  As few as hold a row (more blocks
-// means more exchange for less work each: 16384 x 32000 bf16 takes 417 us with one, 584 with two), except where rows are so few that
-// the GPU would stay half empty (48 x 32000 bf16: 12.6 us with four, 14.2 with one).
-int ring_cluster(int64_t vectors, int64_t rows)
+int launch_ring(int dtype, const PolicyCall &k, const RingChoice &choice, cudaStream_t st)
 {
-    int64_t cluster = div_up(vectors, softsync::kRingSlots * softsync::kRingChunk);
-    if (cluster > kMaxCluster) return 0;
-    while (cluster * 2 <= kMaxCluster && rows * cluster * 2 <= 2 * sm_count() && vectors > cluster * softsync::kRingThreads) cluster *= 2;
-    return static_cast<int>(cluster);
+    const auto go = [&](auto grad, auto ent) {
+        using GT = decltype(grad);
+        if (choice.threads == softsync::kNarrow) return launch_ring_as<GT, decltype(ent)::value, softsync::kNarrow>(k, choice.cluster, st);
+        return launch_ring_as<GT, decltype(ent)::value, softsync::kWide>(k, choice.cluster, st);
+    };
+    const bool ent = k.in.entropy_coef != 0.f;
+    if (dtype == PS_GRAD_BF16) return ent ? go(GradBf16{}, std::true_type{}) : go(GradBf16{}, std::false_type{});
+    return ent ? go(GradFp32{}, std::true_type{}) : go(GradFp32{}, std::false_type{});
 }
 
 }  // namespace
@@ -299,12 +315,12 @@ int ps_policy_loss(const ps_logits *logits, const ps_policy_inputs *in, float *s
     k.out = static_cast<unsigned char *>(dlogits_dev);
     k.stride = dlogits_stride;
     k.vectors = row_vectors(logits);
-    const int cluster = ring_cluster(k.vectors, logits->rows);
-    if (!cluster || logits->rows > softsync::kOwnTotalRows) {
+    const RingChoice ring = ring_choice(k.vectors, logits->rows);
+    if (!ring.cluster || logits->rows > softsync::kOwnTotalRows) {
         softsync::policy_totals_kernel<<<1, softsync::kTermThreads, 0, st>>>(logits->weights_dev, logits->rows, k.st.inv_weight);
         if ((status = launched()) != PS_OK) return status;
     }
-    if (cluster) return launch_ring(logits->dtype, k, cluster, st);
+    if (ring.cluster) return launch_ring(logits->dtype, k, ring, st);
     if ((status = launch_stats(logits, k.rows, StatsOut{logp_dev, nullptr, k.entropy, ws.stat, nullptr}, true, st)) != PS_OK) return status;
     softsync::policy_terms_kernel<<<static_cast<unsigned>(std::min(logits->rows, kMaxParts)), 32, 0, st>>>(k.rows, k.in, k.st, logp_dev, k.entropy,
                                                                                                         dlogits_dev ? ws.coef : nullptr);

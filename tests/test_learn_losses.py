@@ -441,3 +441,27 @@ def test_refusals_of_the_python_calls():
         with pytest.raises(error):
             call()
             pytest.fail("case %d was not refused" % k)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,pad,shift", [(1200, 3001, 0, 1), (640, 12001, 7, 0), (310, 50001, 0, 3), (170, 70001, 0, 0), (240, 65536, 8, 0), (160, 150001, 3, 2), (37, 600003, 0, 0)])
+def test_policy_loss_of_many_rows(dtype, rows, vocab, pad, shift):
+    """Several rows after one another in every block, with runs of rows without a weight between them."""
+    x, tokens, weights = make(rows, vocab, dtype, seed=rows + vocab, pad=pad, shift=shift, masked=0.3)
+    weights[rows // 3:rows // 2] = 0.0
+    weights[-1] = 0.0
+    old, adv, ref = policy_inputs(x, tokens, weights, 0.9, 6)
+    for kl, ent in ((0.05, 0.0), (0.05, 0.02)):
+        stats, logp, entropy, grad, p, share = policy_reference(x, tokens, weights, old, adv, ref, 0.2, 0.2, kl, ent, 0.9)
+        r = P.policy_loss(x, tokens, old, adv, weights, ref, 0.2, 0.2, kl, ent, 0.9)
+        tol = stat_tolerance(x, 0.9)
+        assert (r.logp.cpu().double() - logp).abs().max() <= tol and (r.entropy.cpu().double() - entropy).abs().max() <= tol
+        assert (r.stats.cpu().double() - stats).abs().max() <= 20 * tol + 16 * EPS * float(stats.abs().max())
+        scale = share / 0.9 * (4 * adv.double().cpu().abs() + kl * 20 + ent * (tol / EPS + 1))
+        gradient_close(r.dlogits, grad, scale, tol / EPS, dtype)
+        assert bool((r.dlogits[weights == 0] == 0).all())
+        del grad, p
+    first = r.dlogits.clone()
+    again = P.policy_loss(x, tokens, old, adv, weights, ref, 0.2, 0.2, kl, ent, 0.9, grad="inplace")
+    assert torch.equal(x, first) and torch.equal(again.stats, r.stats)
