@@ -51,6 +51,8 @@ struct PolicyWorkspace : Workspace {
         take(p, stat, rows);
         take(p, coef, rows);
         take(p, entropy, rows);
+        take(p, st.order, rows);
+        take(p, st.live, 1);
     }
 };
 struct PreferenceWorkspace : Workspace {
@@ -193,6 +195,12 @@ struct PolicyCall {
     int64_t stride, vectors;
 };
 
+int launch_totals(const RowsIn &rows, int from, const PolicyState &state, float *logp, float *entropy, cudaStream_t st)
+{
+    softsync::policy_totals_kernel<<<1, softsync::kTermThreads, 0, st>>>(rows.weights, rows.rows, from, state, logp, entropy);
+    return launched();
+}
+
 // Clusters of the ring kernel that run at once on the current GPU (asked once for each kernel, cluster size and GPU).
 template <typename GT, bool ENTROPY_GRAD, int T>
 int resident_clusters(int cluster)
@@ -228,11 +236,20 @@ int launch_ring_as(const PolicyCall &k, int cluster, cudaStream_t st)
     plan.vectors = static_cast<int>(div_up(k.vectors, cluster));
     plan.chunks = static_cast<int>(div_up(plan.vectors, Shape::chunk));
     plan.ahead = std::min(plan.chunks, softsync::kRingSlots - plan.chunks);
-    plan.own_total = k.rows.rows <= softsync::kOwnTotalRows;
     plan.wait_limit = kWaitLimit;
-    const int64_t parts = std::min({static_cast<int64_t>(k.rows.rows), static_cast<int64_t>(resident_clusters<GT, ENTROPY_GRAD, T>(cluster)), kMaxParts});
-    if (parts < 1) return PS_ERR_CUDA;
-    return launch_rows(kernel, parts, cluster, Shape::block, Shape::bytes, !plan.own_total, st, k.rows, k.in, k.st, k.logp, k.entropy,
+    const int64_t resident = resident_clusters<GT, ENTROPY_GRAD, T>(cluster);
+    if (resident < 1) return PS_ERR_CUDA;
+    const int64_t parts = std::min({static_cast<int64_t>(k.rows.rows), resident, kMaxParts});
+    // Weights: a kernel before this one adds them up and lists the rows, unless no cluster gets a second row, and every block adds for itself.
+    PolicyState state = k.st;
+    const bool listed = k.rows.weights && k.rows.rows > parts;
+    if (listed) {
+        const int status = launch_totals(k.rows, static_cast<int>(parts), state, k.logp, k.entropy, st);
+        if (status != PS_OK) return status;
+    } else {
+        state.order = nullptr;
+    }
+    return launch_rows(kernel, parts, cluster, Shape::block, Shape::bytes, listed, st, k.rows, k.in, state, k.logp, k.entropy,
                        k.out, static_cast<long long>(k.stride), plan);
 }
 
@@ -246,6 +263,7 @@ int launch_ring_as(const PolicyCall &k, int cluster, cudaStream_t st)
 struct RingChoice { int threads, cluster; };
 RingChoice ring_choice(int64_t vectors, int64_t rows)
 {
+    if (rows > (int64_t{1} << 30)) return RingChoice{softsync::kNarrow, 0};
     const int64_t narrow = div_up(vectors, softsync::RingShape<softsync::kNarrow>::row), wide = div_up(vectors, softsync::RingShape<softsync::kWide>::row);
     if (narrow > 1 && (wide <= 2 || narrow > kMaxCluster) && (narrow > kMaxCluster || rows * narrow > sm_count()))
         return RingChoice{softsync::kWide, wide <= kMaxCluster ? static_cast<int>(wide) : 0};
@@ -316,11 +334,9 @@ int ps_policy_loss(const ps_logits *logits, const ps_policy_inputs *in, float *s
     k.stride = dlogits_stride;
     k.vectors = row_vectors(logits);
     const RingChoice ring = ring_choice(k.vectors, logits->rows);
-    if (!ring.cluster || logits->rows > softsync::kOwnTotalRows) {
-        softsync::policy_totals_kernel<<<1, softsync::kTermThreads, 0, st>>>(logits->weights_dev, logits->rows, k.st.inv_weight);
-        if ((status = launched()) != PS_OK) return status;
-    }
     if (ring.cluster) return launch_ring(logits->dtype, k, ring, st);
+    k.st.order = k.st.live = nullptr;
+    if ((status = launch_totals(k.rows, 0, k.st, logp_dev, k.entropy, st)) != PS_OK) return status;
     if ((status = launch_stats(logits, k.rows, StatsOut{logp_dev, nullptr, k.entropy, ws.stat, nullptr}, true, st)) != PS_OK) return status;
     softsync::policy_terms_kernel<<<static_cast<unsigned>(std::min(logits->rows, kMaxParts)), 32, 0, st>>>(k.rows, k.in, k.st, logp_dev, k.entropy,
                                                                                                         dlogits_dev ? ws.coef : nullptr);
