@@ -751,6 +751,12 @@ __device__ __forceinline__ void ring_sync() { asm volatile("bar.sync 1, %0;" :: 
 // A vector at a row's ragged end comes with ordinary loads, through a register of the thread that handles it (the last thread the
 // front's, the first thread the end's: never the same one).
 //
+// What bounds it: one read and one write of two bytes an element go at 5.1 to 5.8 TB/s of algorithmic bytes in bf16 (16384 x 32000: 387 us;
+// 8192 x 131072: 740; 8192 x 152000: 930) and 6.0 in fp32 (4096 x 128000: 697), with 57 % of the issue slots, 58 % of the DRAM's
+// cycles and two thirds of the exponential unit's busy at 152000: 16 warps an SM are too few to fill one of them, and the rows'
+// bytes leave no room for more.  Of the forms tried (256 threads x 4 vectors x 7 slots x 2 blocks an SM, 128 x 8, 192 x 4 x 9, 384 x 2 x 9, 512 x
+// 2; one block of 256, 384 and 512) these two were the fastest.
+//
 // Every wait is bounded.  One that runs out makes the block's later rows NaN; it waits for nothing after that, but the copying thread
 // still sees, with a limit, its last copies arrive.
 template <typename GT, bool ENTROPY_GRAD, int T>
@@ -1042,7 +1048,7 @@ __device__ __forceinline__ void sequence_rows(const PreferenceIn &in, long long 
 constexpr int kPairThreads = 256, kSideThreads = kPairThreads / 2;
 
 // One block per pair, half of it for each sequence; the block that ends last adds the pairs' terms up in their order.  `done` is zero
-// before and after.
+// before and after.  A few microseconds of latency between the two large passes, whatever the sizes.
 static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(const __grid_constant__ RowsIn rows, const __grid_constant__ PreferenceIn in,
                                                                                const float *logp, float *seq_logp, RowCoef *coef, double (*each)[3],
                                                                                unsigned *done, float *stats)
@@ -1055,11 +1061,27 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
     long long lo, hi;
     sequence_rows(in, 2 * i + side, rows.rows, lo, hi);
     const double ref = static_cast<double>(in.ref_logp[2 * i]) - static_cast<double>(in.ref_logp[2 * i + 1]);
+    // Weights come eight at a time, the first ones before the statistics are there (two pairs of
+    // 1024 rows: 7.8 us, one at a time 14.3).
+    constexpr int N = 8;
+    float w[N];
+    const auto weights = [&](long long r0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const long long r = r0 + k * kSideThreads;
+            w[k] = r >= hi ? 0.f : rows.weights ? rows.weights[r] : 1.f;
+        }
+    };
+    weights(lo + me);
     griddep_wait();                                        // the statistics
     double s = 0;
-    for (long long r = lo + me; r < hi; r += kSideThreads) {
-        const float w = rows.weights ? rows.weights[r] : 1.f;
-        if (w != 0.f) s += static_cast<double>(w) * logp[r];
+    for (long long r0 = lo + me; r0 < hi; r0 += N * kSideThreads) {
+        if (r0 != lo + me) weights(r0);
+        float x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = r0 + k * kSideThreads < hi ? logp[r0 + k * kSideThreads] : 0.f;       // zero for a row without a weight
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += static_cast<double>(w[k]) * x[k];
     }
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = s;
@@ -1079,9 +1101,12 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
     }
     if (coef) {
         const float slope = (1.f / (1.f + expf(-margin)) - (1.f - in.smoothing)) * in.beta / static_cast<float>(in.pairs);
-        for (long long r = lo + me; r < hi; r += kSideThreads) {
-            const float w = rows.weights ? rows.weights[r] : 1.f;
-            coef[r] = RowCoef{w != 0.f ? (side ? -slope : slope) * w * rows.inv_temperature : 0.f, 0.f};
+        for (long long r0 = lo + me; r0 < hi; r0 += N * kSideThreads) {
+            if (hi - lo > N * kSideThreads) weights(r0);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (r0 + k * kSideThreads < hi)
+                    coef[r0 + k * kSideThreads] = RowCoef{w[k] != 0.f ? (side ? -slope : slope) * w[k] * rows.inv_temperature : 0.f, 0.f};
         }
     }
     __syncthreads();
