@@ -465,3 +465,34 @@ def test_policy_loss_of_many_rows(dtype, rows, vocab, pad, shift):
     first = r.dlogits.clone()
     again = P.policy_loss(x, tokens, old, adv, weights, ref, 0.2, 0.2, kl, ent, 0.9, grad="inplace")
     assert torch.equal(x, first) and torch.equal(again.stats, r.stats)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(700, 40), (330, 33000), (310, 70000)])
+def test_policy_loss_of_mostly_masked_rows(dtype, rows, vocab):
+    """More rows than are worked on at a time, of which none, the first, the last or all have a weight.  Masked rows hold NaN: they are not read.
+    Weights of one are the same as none given, bit by bit, and what a row contributes does not depend on where it stands."""
+    x, tokens, _ = make(rows, vocab, dtype, seed=rows, masked=0.0)
+    old = torch.full((rows,), -math.log(vocab), device="cuda")
+    adv = torch.linspace(-1, 1, rows, device="cuda")
+    every = P.policy_loss(x, tokens, old, adv, torch.ones(rows, device="cuda"), entropy_coef=0.01)
+    plain = P.policy_loss(x, tokens, old, adv, entropy_coef=0.01)
+    for a, b in zip(every, plain):
+        assert torch.equal(a, b)
+    for live in ([], [0], [rows - 1], [0, rows // 2, rows - 1]):
+        weights = torch.zeros(rows, device="cuda")
+        weights[live] = 1.0
+        y = torch.full_like(x, math.nan)
+        y[live] = x[live]
+        r = P.policy_loss(y, tokens, old, adv, weights, entropy_coef=0.01)
+        dead = weights == 0
+        assert bool((r.dlogits[dead] == 0).all()) and bool((r.logp[dead] == 0).all()) and bool((r.entropy[dead] == 0).all())
+        if not live:
+            assert r.stats.tolist() == [0.0] * 5
+            continue
+        few = P.policy_loss(x[live].contiguous(), tokens[live], old[live], adv[live], torch.ones(len(live), device="cuda"), entropy_coef=0.01)
+        assert torch.equal(r.logp[live], every.logp[live]) and torch.equal(r.entropy[live], every.entropy[live])
+        # the same rows alone may be cut into other parts: sums of fp32 in another order, at most vocab / 32 terms one by one
+        tol = EPS * (vocab / 32 + 64) * 16
+        assert (r.stats - few.stats).abs().max() <= tol * (1 + few.stats.abs().max())
