@@ -469,6 +469,27 @@ __global__ void __launch_bounds__(T, 1536 / T) row_stats_kernel(const __grid_con
     if (out.stat) out.stat[r] = RowStat{m, l2};
 }
 
+// Terms of the pairs of a preference loss, to be added up (stats may be null: nothing to do).
+struct PairTail {
+    const double (*each)[3];
+    long long pairs;
+    float *stats;
+};
+
+// By one warp, in the pairs' order.
+__device__ __forceinline__ void finish_pairs(const PairTail &tail)
+{
+    double sum[3] = {};
+    for (long long k = threadIdx.x; k < tail.pairs; k += 32)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) sum[q] += __ldcg(&tail.each[k][q]);
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+        for (int o = 16; o; o >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], o);
+    if (threadIdx.x == 0)
+        for (int q = 0; q < 3; ++q) tail.stats[q] = static_cast<float>(sum[q] / static_cast<double>(tail.pairs));
+}
+
 // ---- gradient from statistics -----------------------------------------------------------------------------------------------
 constexpr int kGradThreads = 256, kGradVectors = 4;
 
@@ -478,11 +499,17 @@ constexpr int kGradThreads = 256, kGradVectors = 4;
 // weight and so only written, in 200 us (6.7 TB/s).
 template <typename GT, bool ENTROPY>
 __global__ void __launch_bounds__(kGradThreads, 6) row_grad_kernel(const __grid_constant__ RowsIn in, const RowStat *stat, const RowCoef *coef,
-                                                                const float *entropy, unsigned char *out, long long out_stride, int segments)
+                                                                const float *entropy, unsigned char *out, long long out_stride, int segments, const __grid_constant__ PairTail tail)
 {
     constexpr int T = kGradThreads, NV = kGradVectors, PV = per_vector<GT>();
-    const long long r = in.rows - 1 - blockIdx.x / static_cast<unsigned>(segments);
-    const int segment = blockIdx.x % static_cast<unsigned>(segments), vocab = static_cast<int>(in.vocab);
+    if (tail.stats && blockIdx.x == 0) {                   // a block of its own
+        griddep_wait();
+        if (threadIdx.x < 32) finish_pairs(tail);
+        return;
+    }
+    const unsigned block = blockIdx.x - (tail.stats ? 1 : 0);
+    const long long r = in.rows - 1 - block / static_cast<unsigned>(segments);
+    const int segment = block % static_cast<unsigned>(segments), vocab = static_cast<int>(in.vocab);
     const unsigned char *row = in.data + r * in.stride * logit_bytes<GT>();
     unsigned char *dst = out + r * out_stride * logit_bytes<GT>();
     const RowVectors<GT> v(row, vocab);
@@ -1047,8 +1074,8 @@ __device__ __forceinline__ void sequence_rows(const PreferenceIn &in, long long 
 
 constexpr int kPairThreads = 256, kSideThreads = kPairThreads / 2;
 
-// One block per pair, half of it for each sequence; the block that ends last adds the pairs' terms up in their order.  `done` is zero
-// before and after.  A few microseconds of latency between the two large passes, whatever the sizes.
+// One block per pair, half of it for each sequence.  The pairs' terms are added up in their order by the gradient's kernel, which runs
+// next, or (stats not null) by the block that ends last here; `done` is zero before and after.  A few microseconds of latency between the two large passes, whatever the sizes.
 static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(const __grid_constant__ RowsIn rows, const __grid_constant__ PreferenceIn in,
                                                                                const float *logp, float *seq_logp, RowCoef *coef, double (*each)[3],
                                                                                unsigned *done, float *stats)
@@ -1096,8 +1123,10 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
         __stcg(&each[i][0], static_cast<double>(isnan(margin) ? margin : loss));
         __stcg(&each[i][1], margin > 0.f ? 1.0 : 0.0);
         __stcg(&each[i][2], static_cast<double>(margin));
-        __threadfence();
-        finish = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;
+        if (stats) {
+            __threadfence();
+            finish = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;
+        }
     }
     if (coef) {
         const float slope = (1.f / (1.f + expf(-margin)) - (1.f - in.smoothing)) * in.beta / static_cast<float>(in.pairs);
@@ -1109,18 +1138,11 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
                     coef[r0 + k * kSideThreads] = RowCoef{w[k] != 0.f ? (side ? -slope : slope) * w[k] * rows.inv_temperature : 0.f, 0.f};
         }
     }
+    if (!stats) return;
     __syncthreads();
     if (!finish || threadIdx.x >= 32) return;
     __threadfence();
-    double sum[3] = {};
-    for (long long k = threadIdx.x; k < in.pairs; k += 32)
-#pragma unroll
-        for (int q = 0; q < 3; ++q) sum[q] += __ldcg(&each[k][q]);
-#pragma unroll
-    for (int q = 0; q < 3; ++q)
-        for (int o = 16; o; o >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], o);
-    if (threadIdx.x == 0)
-        for (int q = 0; q < 3; ++q) stats[q] = static_cast<float>(sum[q] / static_cast<double>(in.pairs));
+    finish_pairs(PairTail{each, in.pairs, stats});
 }
 
 }  // namespace softsync

@@ -11,6 +11,7 @@
 using softsync::aligned_to;
 using softsync::GradBf16;
 using softsync::GradFp32;
+using softsync::PairTail;
 using softsync::PolicyIn;
 using softsync::PolicyState;
 using softsync::PreferenceIn;
@@ -173,14 +174,15 @@ int launch_stats(const ps_logits *lg, const RowsIn &in, const StatsOut &out, boo
 }
 
 int launch_grad(const ps_logits *lg, const RowsIn &in, const RowStat *stat, const RowCoef *coef, const float *entropy, void *out,
-                int64_t stride, cudaStream_t st)
+                int64_t stride, const PairTail &tail, cudaStream_t st)
 {
     const int64_t segments = div_up(row_vectors(lg), softsync::kGradThreads * softsync::kGradVectors);
-    if (lg->rows * segments > 0x7fffffff) return PS_ERR_INVALID_ARG;
+    const int64_t blocks = lg->rows * segments + (tail.stats ? 1 : 0);
+    if (blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
     const int seg = static_cast<int>(segments);
     auto go = [&](auto kernel) {
-        return launch_rows(kernel, lg->rows * segments, 1, softsync::kGradThreads, 0, true, st, in, stat, coef, entropy, static_cast<unsigned char *>(out),
-                           static_cast<long long>(stride), seg);
+        return launch_rows(kernel, blocks, 1, softsync::kGradThreads, 0, true, st, in, stat, coef, entropy, static_cast<unsigned char *>(out),
+                           static_cast<long long>(stride), seg, tail);
     };
     if (lg->dtype == PS_GRAD_BF16) return entropy ? go(softsync::row_grad_kernel<GradBf16, true>) : go(softsync::row_grad_kernel<GradBf16, false>);
     return entropy ? go(softsync::row_grad_kernel<GradFp32, true>) : go(softsync::row_grad_kernel<GradFp32, false>);
@@ -341,7 +343,7 @@ int ps_policy_loss(const ps_logits *logits, const ps_policy_inputs *in, float *s
     softsync::policy_terms_kernel<<<static_cast<unsigned>(std::min(logits->rows, kMaxParts)), 32, 0, st>>>(k.rows, k.in, k.st, logp_dev, k.entropy,
                                                                                                         dlogits_dev ? ws.coef : nullptr);
     if ((status = launched()) != PS_OK || !dlogits_dev) return status;
-    return launch_grad(logits, k.rows, ws.stat, ws.coef, in->entropy_coef != 0.f ? k.entropy : nullptr, dlogits_dev, dlogits_stride, st);
+    return launch_grad(logits, k.rows, ws.stat, ws.coef, in->entropy_coef != 0.f ? k.entropy : nullptr, dlogits_dev, dlogits_stride, PairTail{}, st);
 }
 
 int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, float *stats_dev, float *seq_logp_dev,
@@ -361,13 +363,14 @@ int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, 
     const RowsIn rows = rows_in(logits);
     const PreferenceIn p{reinterpret_cast<const long long *>(in->offsets_dev), in->ref_logp_dev, in->pairs, in->beta, in->label_smoothing};
     if (logits->rows && (status = launch_stats(logits, rows, StatsOut{ws.logp, nullptr, nullptr, ws.stat, ws.coef}, false, st)) != PS_OK) return status;
+    const bool grad = dlogits_dev && logits->rows;
     if (in->pairs)
-        status = launch_rows(softsync::preference_terms_kernel, in->pairs, 1, softsync::kPairThreads, 0, true, st, rows, p, ws.logp, seq_logp_dev,
-                             dlogits_dev ? ws.coef : nullptr, ws.pairs, ws.done, stats_dev);
+        status = launch_rows(softsync::preference_terms_kernel, in->pairs, 1, softsync::kPairThreads, 0, logits->rows > 0, st, rows, p, ws.logp, seq_logp_dev,
+                             grad ? ws.coef : nullptr, ws.pairs, ws.done, grad ? nullptr : stats_dev);
     else if (cudaMemsetAsync(stats_dev, 0, 3 * sizeof(float), st) != cudaSuccess)
         status = PS_ERR_CUDA;
-    if (status != PS_OK || !dlogits_dev || !logits->rows) return status;
-    return launch_grad(logits, rows, ws.stat, ws.coef, nullptr, dlogits_dev, dlogits_stride, st);
+    if (status != PS_OK || !grad) return status;
+    return launch_grad(logits, rows, ws.stat, ws.coef, nullptr, dlogits_dev, dlogits_stride, PairTail{ws.pairs, in->pairs, in->pairs ? stats_dev : nullptr}, st);
 }
 
 }  // extern "C"
