@@ -308,12 +308,19 @@ __device__ __forceinline__ float part_factor(float m, float top, float c, float 
 struct RowCoef { float a, b; };
 
 // What the gradient of a row's elements needs.  With d = (x - m) c - log2 s:  p = 2^d,  g = p (b ln 2 d + (b H - a)).  For bf16 the
-// exponent is x c + shift, one instruction less: the rounding of the shift is a relative error of about 1e-6 in p, lost in
-// the 2e-3 of the result's own.
+// exponent is x c + shift, one instruction less, where the shift is small: its rounding is an error of the exponent that a whole row
+// shares, below 1024 at most 2^-15, 1 % of the rounding of a bf16 result (2^-9).  Beyond (large logits, a finite mask over everything, a small
+// temperature) the difference to m is taken first, as for fp32: a row of -1e9 had its p 2^34 times too large from the shift.  The rows of
+// a well-behaved model never come there: logits of 32 at a temperature of 1 make a shift of 50.
+constexpr float kShiftLimit = 1024.f;
 struct RowGradient {
     float m, log2_sum, c, add, mult, one, shift;
     __device__ __forceinline__ RowGradient(float m_, float l2, float c_, RowCoef k, float entropy)
         : m(m_), log2_sum(l2), c(c_), add(fmaf(k.b, entropy, -k.a)), mult(k.b * kLn2), one(k.a), shift(-fmaf(m_, c_, l2)) {}
+
+    // whether the exponent is x c + shift: the same for the whole row
+    template <typename GT>
+    __device__ __forceinline__ bool shifted() const { return logit_bytes<GT>() == 2 && fabsf(shift) < kShiftLimit; }
 
     // any maximum, beside an ordinary one with the bits of the vector form; the token's own entry has `one` to be added
     template <typename GT, bool ENTROPY>
@@ -321,26 +328,32 @@ struct RowGradient {
     {
         constexpr float floor = logit_bytes<GT>() == 4 ? kFloor : kFloorBf16;
         const float y = ENTROPY ? max_nan(x, floor) : x;
-        const float d = !ordinary(m, c) ? max_nan((x - m) * c, -1000.f) - log2_sum : logit_bytes<GT>() == 2 ? fmaf(y, c, shift) : fmaf(y - m, c, -log2_sum);
+        const float d = !ordinary(m, c) ? max_nan((x - m) * c, -1000.f) - log2_sum : shifted<GT>() ? fmaf(y, c, shift) : fmaf(y - m, c, -log2_sum);
         return __fmul_rn(ex2(d), ENTROPY ? fmaf(mult, d, add) : add);
     }
-    // beside an ordinary maximum
-    template <typename GT, bool ENTROPY>
+    // beside an ordinary maximum; SHIFT: shifted()
+    template <typename GT, bool ENTROPY, bool SHIFT>
     __device__ __forceinline__ uint4 vector(const uint4 &x) const
     {
-        constexpr bool kShift = logit_bytes<GT>() == 2;
-        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m), l2 = kShift ? make_float2(shift, shift) : make_float2(-log2_sum, -log2_sum);
+        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m), l2 = SHIFT ? make_float2(shift, shift) : make_float2(-log2_sum, -log2_sum);
         const float2 a2 = make_float2(add, add), b2 = make_float2(mult, mult);
         float g[per_vector<GT>()];
 #pragma unroll
         for (int j = 0; j < per_vector<GT>() / 2; ++j) {
             const float2 y = ENTROPY ? floored_pair<GT>(x, j) : plain_pair<GT>(x, j);
-            const float2 d = fma2(kShift ? y : add2(y, m2), c2, l2);
+            const float2 d = fma2(SHIFT ? y : add2(y, m2), c2, l2);
             const float2 r = mul2(make_float2(ex2(d.x), ex2(d.y)), ENTROPY ? fma2(b2, d, a2) : a2);
             g[2 * j] = r.x;
             g[2 * j + 1] = r.y;
         }
         return pack_vector<GT>(g);
+    }
+    template <typename GT, bool ENTROPY>
+    __device__ __forceinline__ uint4 vector_of(const uint4 &x) const
+    {
+        if constexpr (logit_bytes<GT>() == 2)
+            if (shifted<GT>()) return vector<GT, ENTROPY, true>(x);
+        return vector<GT, ENTROPY, false>(x);
     }
 };
 
@@ -533,7 +546,7 @@ __global__ void __launch_bounds__(kGradThreads, 6) row_grad_kernel(const __grid_
         for (int i = 0; i < NV; ++i) {
             const int q = q0 + i * T;
             if (q >= v.count) break;
-            const uint4 g = f.template vector<GT, ENTROPY>(x[i]);
+            const uint4 g = f.template vector_of<GT, ENTROPY>(x[i]);
             if (v.whole(q)) __stcs(reinterpret_cast<uint4 *>(p + i * T * 16), g);
             else store_single<GT>(dst, v.first(q), vocab, g);
             if (q == tok_q) {                              // the token's entry once more, with its one
@@ -1005,18 +1018,20 @@ __global__ void __launch_bounds__(RingShape<T>::block, RingShape<T>::per_sm) pol
             const bool clean = lo >= v.inner;
             unsigned char *dst = out + static_cast<long long>(due) * out_stride * logit_bytes<GT>();
             const bool plain = ((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c);
+            constexpr bool kShift = logit_bytes<GT>() == 2;
+            const bool usual = !kShift || f.template shifted<GT>();
             unsigned char *p = dst - v.phase * logit_bytes<GT>() + static_cast<long long>(lo + tid) * 16;
             for (int left = hi - lo, k = 0; k < plan.chunks; ++k, left -= kRingChunk) {
                 const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + slot * kRingChunk + tid;
                 if (out && plain) {
-                    if (left >= kRingChunk && (k > 0 || clean)) {
+                    if (left >= kRingChunk && (k > 0 || clean) && usual) {
 #pragma unroll
-                        for (int q = 0; q < NV; ++q) __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD>(mine[q * T]));
+                        for (int q = 0; q < NV; ++q) __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, kShift>(mine[q * T]));
                     } else {
 #pragma unroll
                         for (int q = 0; q < NV; ++q)
                             if (q * T + tid < left && (k > 0 || q * T + tid > 0 || clean))
-                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD>(mine[q * T]));
+                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector_of<GT, ENTROPY_GRAD>(mine[q * T]));
                     }
                     p += kRingChunk * 16;
                 } else if (out) {

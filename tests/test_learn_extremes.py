@@ -1,0 +1,85 @@
+"""Losses where their inputs are far from a well-behaved model's, compared with float64."""
+import pytest
+import torch
+
+import paper_1511_05950_b200 as P
+
+gpu = pytest.mark.gpu
+EPS = 2.0 ** -24
+
+
+def large_rows(vocab, dtype):
+    """(logits on the GPU, tokens): rows whose softmax is ordinary although their logits are large."""
+    g = torch.Generator().manual_seed(vocab)
+    r = lambda: torch.randn(vocab, generator=g)
+    half = r()
+    half[vocab // 2:] = -1e9
+    ties = torch.full((vocab,), -1e6)
+    ties[::3] = -1e6 - 8192
+    rows = [torch.full((vocab,), -1e9), torch.full((vocab,), -1e4), torch.full((vocab,), -65504.0), torch.full((vocab,), 1e7), torch.full((vocab,), -1e15),
+            half, ties, r() + 3e4, r() * 1e4, r() * 3, r() + 700.0, torch.full((vocab,), -1e9)]
+    x = torch.stack(rows).to(dtype).cuda()
+    return x, x.float().argmax(1)                                     # a likely token: its log probability is a number of ordinary size
+
+
+def softmax64(x, temperature):
+    return torch.softmax(x.double() / temperature, 1)
+
+
+def relative_error_of_p(vocab, dtype):
+    """Where p counts (above 2^-40) the exponent is below 40 and comes from a difference, a scaling and a subtraction, rounded once each; a
+    thread adds up at most vocab / 32 terms one by one; for bf16 the exponent may be off by 2^-15 as a whole."""
+    return EPS * (4 * 40 + 64 + vocab / 32) + (2.0 ** -15 if dtype == torch.bfloat16 else 0.0)
+
+
+def assert_gradient(got, p, tokens, a, b, dtype, vocab):
+    """got against a (1[token] - p) + b p (log p + H), a and b per row."""
+    hot = torch.zeros_like(p).scatter_(1, tokens[:, None], 1.0)
+    logp = torch.where(p > 0, p, 1.0).log()
+    entropy = -(p * logp).sum(1, keepdim=True)
+    want = a[:, None] * (hot - p) + b[:, None] * p * (logp + entropy)
+    rel = relative_error_of_p(vocab, dtype)
+    size = a.abs()[:, None] * (p + 16 * EPS) + b.abs()[:, None] * p * (logp.abs() + entropy + 2)
+    bound = rel * size + EPS * (a.abs() + b.abs())[:, None] * 2.0 ** -16 + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 16 * EPS)
+    err = (got.double() - want).abs()
+    worst = (err / bound).amax(1)
+    assert (err <= bound).all(), worst.tolist()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [40, 5003, 60000, 152000, 1000003])
+@pytest.mark.parametrize("temperature,ent", [(1.0, 0.0), (1.0, 0.02), (0.004, 0.0)])
+def test_policy_gradient_of_large_logits(dtype, vocab, temperature, ent):
+    x, tokens = large_rows(vocab, dtype)
+    rows = x.shape[0]
+    p = softmax64(x, temperature)
+    old = p.gather(1, tokens[:, None]).squeeze(1).log().float()       # ratio one
+    adv = torch.linspace(0.5, 2.0, rows, device="cuda")
+    r = P.policy_loss(x, tokens, old, adv, temperature=temperature, entropy_coef=ent)
+    a = -adv.double() * (r.logp.double() - old.double()).exp() / rows / temperature      # the ratio that the call's own log probabilities give
+    b = torch.full_like(a, ent / rows / temperature)
+    assert_gradient(r.dlogits, p, tokens, a, b, dtype, vocab)
+    # a buffer whose rows lie elsewhere in a 16-byte vector takes single elements: the same bits
+    wide = torch.zeros(rows, vocab + 5, dtype=dtype, device="cuda")
+    P.policy_loss(x, tokens, old, adv, temperature=temperature, entropy_coef=ent, grad=wide[:, 1:1 + vocab])
+    assert torch.equal(wide[:, 1:1 + vocab], r.dlogits)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [40, 5003, 152000])
+def test_preference_gradient_of_large_logits(dtype, vocab):
+    x, tokens = large_rows(vocab, dtype)
+    rows = x.shape[0]
+    p = softmax64(x, 1.0)
+    logp = p.gather(1, tokens[:, None]).squeeze(1).log()
+    offsets = torch.arange(rows + 1, device="cuda")
+    r = P.preference_loss(x, tokens, offsets, logp.float(), beta=0.1)  # margins of zero
+    slope = -0.5 * 0.1 / (rows // 2)
+    a = torch.where(torch.arange(rows, device="cuda") % 2 == 0, slope, -slope).double()
+    # the margin's own error, beta (4 log probabilities of at most ~14 rounded to fp32), moves the slope by a quarter of it
+    wide = torch.zeros(rows, vocab + 5, dtype=dtype, device="cuda")
+    P.preference_loss(x, tokens, offsets, logp.float(), beta=0.1, grad=wide[:, 1:1 + vocab])
+    assert torch.equal(wide[:, 1:1 + vocab], r.dlogits)
+    assert_gradient(r.dlogits, p, tokens, a, torch.zeros_like(a), dtype, vocab)
