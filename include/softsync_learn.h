@@ -130,7 +130,7 @@ int ps_policy_loss(const ps_logits *logits, const ps_policy_inputs *in, float *s
  * preferred and the other answer of pair i.  With pi_k = sum over its rows of w_t logp_t and ref_logp_k the same under the reference,
  *     margin_i = beta ((pi_2i - ref_2i) - (pi_2i+1 - ref_2i+1))
  *     loss = mean_i ( -(1 - s) log sigmoid(margin_i) - s log sigmoid(-margin_i) ),     s = label_smoothing
- *     dlogits_tj = +-g_i w_t / T (1[j = token] - p_j),     g_i = beta / pairs (sigmoid(margin_i) - (1 - s)),  + for sequence 2i
+ *     dlogits_tj = +-g_i w_t / T (1[j = token] - p_j),   + for sequence 2i,   g_i = beta / pairs (s sigmoid(margin_i) - (1 - s) sigmoid(-margin_i))
  * offsets_dev: 2 * pairs + 1 ascending row numbers (a sequence may be empty); rows outside every sequence get a zero gradient.
  * stats_dev: 3 fp32, loss, share of positive margins, mean margin.  seq_logp_dev: 2 * pairs fp32.  dlogits as above. */
 typedef struct ps_preference_inputs {

@@ -1144,7 +1144,9 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
         }
     }
     if (coef) {
-        const float slope = (1.f / (1.f + expf(-margin)) - (1.f - in.smoothing)) * in.beta / static_cast<float>(in.pairs);
+        // sigmoid(margin) - (1 - s), written so that nothing cancels: the difference itself has no digits left at a margin of 17
+        const float up_s = 1.f / (1.f + expf(-margin)), down_s = 1.f / (1.f + expf(margin));
+        const float slope = (in.smoothing * up_s - (1.f - in.smoothing) * down_s) * in.beta / static_cast<float>(in.pairs);
         for (long long r0 = lo + me; r0 < hi; r0 += N * kSideThreads) {
             if (hi - lo > N * kSideThreads) weights(r0);
 #pragma unroll

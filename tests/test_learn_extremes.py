@@ -83,3 +83,32 @@ def test_preference_gradient_of_large_logits(dtype, vocab):
     P.preference_loss(x, tokens, offsets, logp.float(), beta=0.1, grad=wide[:, 1:1 + vocab])
     assert torch.equal(wide[:, 1:1 + vocab], r.dlogits)
     assert_gradient(r.dlogits, p, tokens, a, torch.zeros_like(a), dtype, vocab)
+
+
+@gpu
+@pytest.mark.parametrize("smooth", [0.0, 0.1])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_preference_gradient_of_confident_pairs(dtype, smooth):
+    """The factor of pair i is beta / pairs (s sigmoid(margin) - (1 - s) sigmoid(-margin)): small for a pair that the model ranks right, and as
+    exact as the margin is.  That is rounded to fp32 once, after log probabilities whose errors are below 1e-5 each: relative to a
+    sigmoid that falls as e^-margin, at most beta * 4e-5 + 60 * 2^-24 < 5e-5; the products add a dozen roundings."""
+    margins = torch.tensor([0.0, 3.0, 9.0, 12.0, 15.0, 17.5, 25.0, 60.0, -3.0, -12.0, -17.5, -60.0], dtype=torch.float64)
+    pairs, vocab, beta = len(margins), 97, 0.5
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(2 * pairs, vocab, generator=g).to(dtype).cuda()
+    tokens = torch.randint(0, vocab, (2 * pairs,), generator=g).cuda()
+    p = softmax64(x, 1.0)
+    logp = p.gather(1, tokens[:, None]).squeeze(1).log().cpu()
+    ref = torch.zeros(2 * pairs, dtype=torch.float64)
+    ref[1::2] = margins / beta - (logp[0::2] - logp[1::2])             # margin = beta (logp_0 - logp_1 + ref_1)
+    ref = ref.float()
+    r = P.preference_loss(x, tokens, torch.arange(2 * pairs + 1, device="cuda"), ref.cuda(), beta=beta, label_smoothing=smooth)
+    margin = beta * (logp[0::2] - logp[1::2] + ref[1::2].double())
+    slope = (smooth * torch.sigmoid(margin) - (1 - smooth) * torch.sigmoid(-margin)) * beta / pairs
+    a = torch.stack([slope, -slope], 1).view(-1).cuda()[:, None]
+    want = a * (torch.zeros_like(p).scatter_(1, tokens[:, None], 1.0) - p)
+    err = (r.dlogits.double() - want).abs()
+    part = (smooth * torch.sigmoid(margin) + (1 - smooth) * torch.sigmoid(-margin)) * beta / pairs      # what rounds before the two are subtracted
+    size = torch.stack([part, part], 1).view(-1).cuda()[:, None] * want.abs() / a.abs()
+    bound = size * 1e-4 + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)
+    assert (err <= bound).all(), (err / bound).amax(1).tolist()
