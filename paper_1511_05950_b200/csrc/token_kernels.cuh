@@ -297,6 +297,10 @@ __device__ __forceinline__ void add_vectors(const uint4 (&x)[NV], float c, float
     else single_exponentials<GT, NV, ENTROPY>(x, m, c, s, t);
 }
 
+// log2 of a row's sum; NaN, and with it all the row's results, where nothing has a probability (a row of minus infinities) and where
+// the token has no logit (NaN in its place).
+__device__ __forceinline__ float log2_or_nan(float s, float x_tok) { return s > 0.f && x_tok == x_tok ? log2f(s) : CUDART_NAN_F; }
+
 // What multiplies the exponentials of a part with maximum m in a whole with maximum `top`.
 __device__ __forceinline__ float part_factor(float m, float top, float c, float &d)
 {
@@ -475,7 +479,7 @@ __global__ void __launch_bounds__(T, 1536 / T) row_stats_kernel(const __grid_con
     }
     join_cluster(sh, in.scale, m, s, t);
     if (rank || threadIdx.x) return;
-    const float l2 = log2f(s);
+    const float l2 = log2_or_nan(s, x_tok);
     out.logp[r] = (x_tok - m) * in.inv_temperature - kLn2 * l2;
     if (out.lse) out.lse[r] = m * in.inv_temperature + kLn2 * l2;
     if (ENTROPY && out.entropy) out.entropy[r] = kLn2 * (l2 - t / s);
@@ -903,7 +907,7 @@ __global__ void __launch_bounds__(RingShape<T>::block, RingShape<T>::per_sm) pol
                 join_lanes(in.scale, m, s, t);
             }
             if (late) s = CUDART_NAN_F;
-            const float l2 = log2f(s), h = kLn2 * (l2 - t / s);
+            const float l2 = log2_or_nan(s, x_tok), h = kLn2 * (l2 - t / s);
             const float lp = (x_tok - m) * in.inv_temperature - kLn2 * l2;
             const PolicyTerms o = policy_terms(pin, adv, old_logp, ref_logp, lp, h);
             const float share = w * inv_weight;

@@ -1,4 +1,6 @@
 """Losses where their inputs are far from a well-behaved model's, compared with float64."""
+import math
+
 import pytest
 import torch
 
@@ -112,3 +114,21 @@ def test_preference_gradient_of_confident_pairs(dtype, smooth):
     size = torch.stack([part, part], 1).view(-1).cuda()[:, None] * want.abs() / a.abs()
     bound = size * 1e-4 + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)
     assert (err <= bound).all(), (err / bound).amax(1).tolist()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [1, 40, 5003, 152000])
+def test_rows_without_a_result_are_nan_in_every_output(dtype, vocab):
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(8, vocab, generator=g).to(dtype).cuda()
+    tokens = torch.zeros(8, dtype=torch.int64, device="cuda")
+    want = P.token_logprob(x, tokens)
+    x[1], x[2, vocab // 2], x[3, vocab - 1] = -math.inf, math.nan, math.inf
+    tokens[4], tokens[5], tokens[6] = -1, vocab, 1 << 40
+    r = P.token_logprob(x, tokens)
+    q = P.policy_loss(x, tokens, torch.zeros(8, device="cuda"), torch.ones(8, device="cuda"), entropy_coef=0.1)
+    for got, good in ((r.logp, want.logp), (r.lse, want.lse), (r.entropy, want.entropy), (q.logp, None), (q.entropy, None)):
+        assert bool(torch.isnan(got[1:7]).all()) and bool(torch.isfinite(got[[0, 7]]).all())
+        assert good is None or torch.equal(got[[0, 7]], good[[0, 7]])
+    assert bool(torch.isnan(q.dlogits[1:7].float()).any(1).all()) and bool(torch.isfinite(q.dlogits[[0, 7]].float()).all())
