@@ -1028,14 +1028,19 @@ __global__ void __launch_bounds__(RingShape<T>::block, RingShape<T>::per_sm) pol
             for (int left = hi - lo, k = 0; k < plan.chunks; ++k, left -= kRingChunk) {
                 const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + slot * kRingChunk + tid;
                 if (out && plain) {
-                    if (left >= kRingChunk && (k > 0 || clean) && usual) {
+                    if (!usual) {
+#pragma unroll 1
+                        for (int q = 0; q < NV; ++q)
+                            if (q * T + tid < left && (k > 0 || q * T + tid > 0 || clean))
+                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, false>(mine[q * T]));
+                    } else if (left >= kRingChunk && (k > 0 || clean)) {
 #pragma unroll
                         for (int q = 0; q < NV; ++q) __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, kShift>(mine[q * T]));
                     } else {
 #pragma unroll
                         for (int q = 0; q < NV; ++q)
                             if (q * T + tid < left && (k > 0 || q * T + tid > 0 || clean))
-                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector_of<GT, ENTROPY_GRAD>(mine[q * T]));
+                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, kShift>(mine[q * T]));
                     }
                     p += kRingChunk * 16;
                 } else if (out) {
