@@ -52,7 +52,8 @@ int ps_tensors_bind_adamw(ps_tensors_t *list, float *const *weights_host, void *
  *     out_dev[1] = max_norm / |g| where |g| > max_norm, else 1 (NaN where the norm is NaN)
  * grads_host: c * num_tensors device pointers, gradient after gradient, of grad_dtype (ps_grad_dtype) values.  scales_host: c fp32
  * factors (Eq. 3 and the 1/c of Eq. 2 are the caller's), or NULL for 1.  Products and sums of g are rounded one by one in fp32, in the
- * order given; squares are summed in fp32 within a thread and in fp64 beyond it, in a fixed order: the same call gives the same bits. */
+ * order given; squares are added in fp32 up to a few dozen at a time (so one above 3.4e38 makes the norm infinite) and in fp64 beyond
+ * that, in a fixed order: the same call gives the same bits. */
 int ps_grad_norm(ps_tensors_t *list, const void *const *grads_host, int c, const float *scales_host, int grad_dtype,
                  float max_norm, float *out_dev, void *stream);
 

@@ -1,6 +1,7 @@
-"""Losses where their inputs are far from a well-behaved model's, compared with float64."""
+"""Losses and the gradient norm where their inputs are far from a well-behaved model's, compared with float64."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -132,3 +133,17 @@ def test_rows_without_a_result_are_nan_in_every_output(dtype, vocab):
         assert bool(torch.isnan(got[1:7]).all()) and bool(torch.isfinite(got[[0, 7]]).all())
         assert good is None or torch.equal(got[[0, 7]], good[[0, 7]])
     assert bool(torch.isnan(q.dlogits[1:7].float()).any(1).all()) and bool(torch.isfinite(q.dlogits[[0, 7]].float()).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype,c,shift", [(torch.bfloat16, 1, 0), (torch.float32, 1, 0), (torch.bfloat16, 2, 0), (torch.float32, 1, 1)])
+def test_norm_of_long_gradients(dtype, c, shift):
+    """A constant gradient is the worst case of a long sum: every addition rounds the same way.  Sums in fp32 end after at most 8 additions and
+    3 joins, so the squares' sum is exact to 12 EPS, the norm to half of that; weighting rounds c products and c - 1 sums, the result once."""
+    n = 3 << 27 if dtype == torch.bfloat16 else 3 << 26
+    scale = 0.7371
+    grads = [[torch.full((n + shift,), 1.171875, dtype=dtype, device="cuda")[shift:]]] * c
+    scales = [scale] * c
+    got = float(P.TensorList([n]).grad_norm(grads, scales)[0])
+    exact = c * float(np.float32(scale)) * 1.171875 * math.sqrt(n)
+    assert abs(got - exact) <= (6 + 2 * c + 1) * EPS * exact
