@@ -271,16 +271,18 @@ __device__ __forceinline__ void single_exponentials(const uint4 (&x)[NV], float 
 }
 
 // Takes the vectors into a warp's running sums s, t relative to its m (kLowest to begin with).  Any value of the row serves as m as
-// long as nothing overflows, so the maximum is looked for in the first vectors alone; those that follow are added without looking,
-// and only where that meets an infinity or a NaN, or sums become large, is the maximum looked for again and the sums moved to it.
-// (Looking everywhere costs half an instruction an element, the floor another half.)
+// long as nothing above it is far above it, so the maximum is looked for in the first vectors alone; those that follow are added without
+// looking, and only where that meets an infinity or a NaN, or a sum past kNearSum, is the maximum looked for again and the sums moved to
+// it.  (Looking everywhere costs half an instruction an element, the floor another half.)  An exponent of up to 10 is rounded to 2^-22 at
+// most; without the bound a confident token 60 above the first vectors took its row's log probability 4e-6 off, from there 1e-6.
+constexpr float kNearSum = 1024.f;
 template <typename GT, int NV, bool ENTROPY>
 __device__ __forceinline__ void add_vectors(const uint4 (&x)[NV], float c, float &m, float &s, float &t)
 {
     if (ordinary(m, c)) {
         float s2 = 0.f, t2 = 0.f;
         packed_exponentials<GT, NV, ENTROPY, false>(x, m, c, s2, t2);
-        if (__all_sync(0xffffffffu, s2 < 1e30f && (!ENTROPY || fabsf(t2) < 1e30f))) {
+        if (__all_sync(0xffffffffu, s2 < kNearSum && (!ENTROPY || fabsf(t2) < 1e30f))) {
             s += s2;
             if constexpr (ENTROPY) t += t2;
             return;

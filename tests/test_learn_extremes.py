@@ -147,3 +147,28 @@ def test_norm_of_long_gradients(dtype, c, shift):
     got = float(P.TensorList([n]).grad_norm(grads, scales)[0])
     exact = c * float(np.float32(scale)) * 1.171875 * math.sqrt(n)
     assert abs(got - exact) <= (6 + 2 * c + 1) * EPS * exact
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,rows", [(5003, 41), (50257, 41), (152000, 41), (1000003, 5)])
+def test_confident_rows(dtype, vocab, rows):
+    """Normalised logits (log probabilities) whose token has nearly all the probability and stands late in its row.  The sums are relative to a
+    value at most 10 log2(e)-units, 7 natural ones, below the row's maximum.  In units of EPS: the difference to it is rounded to 4, the
+    exponent to 6 + 8, 10 of them after the factor ln 2, the exponential to 4, its sum to 4, the logarithm (below 16) to 6 and its product to
+    4, the difference of the token's logit to 4: 40 for log probability and normaliser.  The entropy's quotient carries the exponent's error and
+    that of a product and a quotient once more: 64."""
+    g = torch.Generator("cuda").manual_seed(vocab)
+    x = torch.randn(rows, vocab, device="cuda", generator=g)
+    tokens = torch.randint(vocab // 2, vocab, (rows,), device="cuda", generator=g)
+    x.scatter_(1, tokens[:, None], torch.linspace(20 + math.log(vocab / 5e4), 60, rows, device="cuda")[:, None])
+    x = torch.log_softmax(x, 1).to(dtype)
+    exact = torch.log_softmax(x.double(), 1)
+    logp, lse = exact.gather(1, tokens[:, None]).squeeze(1), torch.logsumexp(x.double(), 1)
+    entropy = -(exact.exp() * exact).sum(1)
+    r = P.token_logprob(x, tokens)
+    q = P.policy_loss(x, tokens, torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda"), grad=False)
+    for name, got, want, tol in (("logp", r.logp, logp, 40), ("lse", r.lse, lse, 40), ("entropy", r.entropy, entropy, 64), ("policy logp", q.logp, logp, 40),
+                                 ("policy entropy", q.entropy, entropy, 64)):
+        err = float((got.double() - want).abs().max())
+        assert err <= tol * EPS, (name, err / EPS)
