@@ -238,8 +238,8 @@ int ps_tensors_bind_adamw(ps_tensors_t *list, float *const *weights_host, void *
 {
   try {
     if (!is_live(list) || !weights_host || (state_bits != 32 && state_bits != 8)) return PS_ERR_INVALID_ARG;
-    if (!m_dev || !v_dev || !aligned_to(m_dev, 16) || !aligned_to(v_dev, 16)) return PS_ERR_INVALID_ARG;
-    if (state_bits == 8 && (!m_scale_dev || !v_scale_dev)) return PS_ERR_INVALID_ARG;
+    if (!aligned_to(m_dev, 16) || !aligned_to(v_dev, 16)) return PS_ERR_INVALID_ARG;
+    if (list->state_elems && (!m_dev || !v_dev || (state_bits == 8 && (!m_scale_dev || !v_scale_dev)))) return PS_ERR_INVALID_ARG;
     std::vector<Range> ranges;
     const int64_t state_bytes = list->state_elems * (state_bits / 8);
     ranges.push_back(range_of(m_dev, state_bytes));
@@ -351,9 +351,9 @@ int ps_adamw_moments(ps_tensors_t *list, void *m_bf16_dev, void *v_bf16_dev, voi
   try {
     if (!is_live(list)) return PS_ERR_INVALID_ARG;
     if (list->state_bits != 8) return PS_ERR_NO_STATE;
-    if (!m_bf16_dev || !v_bf16_dev || m_bf16_dev == v_bf16_dev || !aligned_to(m_bf16_dev, 16) || !aligned_to(v_bf16_dev, 16)) return PS_ERR_INVALID_ARG;
     const int64_t eights = list->state_elems / 8;
     if (!eights) return PS_OK;
+    if (!m_bf16_dev || !v_bf16_dev || m_bf16_dev == v_bf16_dev || !aligned_to(m_bf16_dev, 16) || !aligned_to(v_bf16_dev, 16)) return PS_ERR_INVALID_ARG;
     if ((eights + 255) / 256 > 0x7fffffff) return PS_ERR_INVALID_ARG;
     DeviceSwitch guard(list->device);
     softsync::moments_kernel<<<static_cast<unsigned>((eights + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(
