@@ -70,7 +70,8 @@ typedef struct ps_adamw_config {
  *     m = beta1 m + (1 - beta1) g;     v = beta2 v + (1 - beta2) g^2
  *     w = w (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * with lr times the tensor's lr_mult and wd = weight_decay times its decay_mult.  Every product, sum, quotient and root is rounded once
- * to fp32, in the order ((m*, (1-beta1)*g), (v*, (1-beta2)*(g*g)), root * (1/sqrt(1-beta2^t)) + eps, quotient, * step size).
+ * to fp32, in the order ((m*, (1-beta1)*g), (v*, (1-beta2)*(g*g)), root * (1/sqrt(1-beta2^t)) + eps, quotient, * step size).  Of a quotient
+ * below 2^-126 it is left open whether it is rounded to a subnormal before the product or only with it.
  *
  * Moments in 8 bits: the PS_STATE_BLOCK elements of a block share a power of two 2^(scale - 127); m is a sign, 3 exponent bits and 4
  * fraction bits with bias 7, v 4 exponent bits and 4 fraction bits with bias 15, both with subnormals.  The step computes with the

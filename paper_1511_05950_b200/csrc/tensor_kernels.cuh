@@ -11,7 +11,7 @@
 // 32-bit step uses 27 %.
 //
 // Arithmetic contract, as in the momentum kernels: every product, sum, quotient and root is rounded to fp32 by itself, in the
-// documented order, whatever the launch shape, so results can be compared bit by bit.
+// documented order, whatever the launch shape, so results can be compared bit by bit (one exception: quotients below 2^-126, at kMScale).
 #pragma once
 
 #include "packed.cuh"
@@ -394,9 +394,10 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)    // NaN i
     return r;
 }
 
-// Scaling that keeps the short root and quotient away from underflow: powers of two that the roundings do not see.  They serve while
-// m < 2^20 and v < 2^30, with an eps of at least 2^-40 (so no quotient overflows, and a root of zero may be taken for 2^-78) and a step
-// size of at least 2^-40.
+// Scaling that keeps the short root and quotient away from underflow: powers of two that the roundings do not see, but for a quotient
+// below 2^-126, which keeps all its bits here and is a subnormal in the other form (a step of the weight below 2^-126 times the step size, so
+// only a weight of about zero shows it).  They serve while m < 2^20 and v < 2^30, with an eps of at least 2^-40 (so no quotient overflows, and
+// a root of zero may be taken for 2^-78) and a step size of at least 2^-40.
 constexpr float kMScale = 0x1p64f, kVScale = 0x1p96f, kVLeast = 0x1p-60f;
 constexpr unsigned kMLimit = 0x49800000u, kVLimit = 0x4e800000u;         // bits of 2^20, 2^30
 

@@ -103,6 +103,20 @@ def test_coefficients_of_every_tensor_over_several_launches():
 
 
 @gpu
+def test_quotients_below_the_smallest_normal_number():
+    """m / (root + eps) below 2^-126 is rounded to a subnormal or kept with all its bits, and only then multiplied with the step size: two results,
+    at most one subnormal step (2^-149) apart for a step size of up to one, so only a weight of about zero shows which."""
+    n = 1024
+    r = np.random.default_rng(3)
+    g = (r.standard_normal(n) * 1e-38).astype(np.float32)
+    w = torch.zeros(n, device="cuda")
+    opt = P.AdamW([w], lr=0.5, betas=(0.0, 0.999), eps=1.0, weight_decay=0.0)
+    opt.step([torch.from_numpy(g).cuda()])
+    exact = -0.5 * g.astype(np.float64)
+    assert np.abs(w.cpu().numpy().astype(np.float64) - exact).max() <= 2.0 ** -149
+
+
+@gpu
 @pytest.mark.parametrize("bits", [32, 8])
 def test_lists_without_elements(bits):
     w = [torch.empty(0, device="cuda"), torch.empty(0, device="cuda")]
