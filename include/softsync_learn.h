@@ -82,6 +82,9 @@ typedef struct ps_adamw_config {
 int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, const float *scales_host, int grad_dtype,
                   const ps_adamw_config *config, const float *clip_dev, void *stream);
 
+/* PS_OK if ps_adamw_step takes this configuration, else what it would return for it.  Needs no GPU. */
+int ps_adamw_check(const ps_adamw_config *config);
+
 /* The bound 8-bit moments as the values they stand for, exactly, in bf16 state arrays (16-byte aligned).  state_bits 8 only. */
 int ps_adamw_moments(ps_tensors_t *list, void *m_bf16_dev, void *v_bf16_dev, void *stream);
 

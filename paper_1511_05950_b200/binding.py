@@ -53,7 +53,7 @@ EXPORTS = (
     "ps_get_update_log", "ps_peek_state", "ps_export_state", "ps_import_state", "ps_kernel_time", "ps_last_cuda_error", "ps_status_string",
     "ps_fused_update_static", "ps_bind_weight_replicas",
     "ps_tensors_sizes", "ps_tensors_create", "ps_tensors_destroy", "ps_tensors_bind_adamw", "ps_grad_norm", "ps_adamw_step",
-    "ps_adamw_moments", "ps_loss_workspace", "ps_token_logprob", "ps_policy_loss", "ps_preference_loss",
+    "ps_adamw_check", "ps_adamw_moments", "ps_loss_workspace", "ps_token_logprob", "ps_policy_loss", "ps_preference_loss",
 )
 
 
@@ -137,6 +137,7 @@ def _load() -> C.CDLL:
         "ps_tensors_bind_adamw": [vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp],
         "ps_grad_norm": [vp, vp, i32, vp, i32, f32, vp, vp],
         "ps_adamw_step": [vp, vp, i32, vp, i32, C.POINTER(AdamwConfig), vp, vp],
+        "ps_adamw_check": [C.POINTER(AdamwConfig)],
         "ps_adamw_moments": [vp, vp, vp, vp],
         "ps_loss_workspace": [i64, i64, C.POINTER(i64)],
         "ps_token_logprob": [C.POINTER(Logits), vp, vp, vp, vp],
@@ -194,6 +195,7 @@ ps_tensors_destroy = lib.ps_tensors_destroy
 ps_tensors_bind_adamw = lib.ps_tensors_bind_adamw
 ps_grad_norm = lib.ps_grad_norm
 ps_adamw_step = lib.ps_adamw_step
+ps_adamw_check = lib.ps_adamw_check
 ps_adamw_moments = lib.ps_adamw_moments
 ps_loss_workspace = lib.ps_loss_workspace
 ps_token_logprob = lib.ps_token_logprob

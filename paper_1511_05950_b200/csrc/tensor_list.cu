@@ -297,6 +297,15 @@ int ps_grad_norm(ps_tensors_t *list, const void *const *grads_host, int c, const
   } PS_CATCH_ALL
 }
 
+int ps_adamw_check(const ps_adamw_config *config)
+{
+    if (!config) return PS_ERR_INVALID_ARG;
+    const ps_adamw_config &k = *config;
+    if (!std::isfinite(k.lr) || k.lr < 0 || !(k.beta1 >= 0 && k.beta1 < 1) || !(k.beta2 >= 0 && k.beta2 < 1)) return PS_ERR_INVALID_ARG;
+    if (!std::isfinite(k.eps) || k.eps < 0 || !std::isfinite(k.weight_decay) || k.step < 1) return PS_ERR_INVALID_ARG;
+    return PS_OK;
+}
+
 int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, const float *scales_host, int grad_dtype,
                   const ps_adamw_config *config, const float *clip_dev, void *stream)
 {
@@ -304,10 +313,9 @@ int ps_adamw_step(ps_tensors_t *list, const void *const *grads_host, int c, cons
     if (!is_live(list) || !config) return PS_ERR_INVALID_ARG;
     if (!list->state_bits) return PS_ERR_NO_STATE;
     const ps_adamw_config &k = *config;
-    if (!std::isfinite(k.lr) || k.lr < 0 || !(k.beta1 >= 0 && k.beta1 < 1) || !(k.beta2 >= 0 && k.beta2 < 1)) return PS_ERR_INVALID_ARG;
-    if (!std::isfinite(k.eps) || k.eps < 0 || !std::isfinite(k.weight_decay) || k.step < 1) return PS_ERR_INVALID_ARG;
-    if (!aligned_to(clip_dev, 4)) return PS_ERR_INVALID_ARG;
-    const int bad = check_gradients(list, grads_host, c, scales_host, grad_dtype);
+    int bad = ps_adamw_check(config);
+    if (bad == PS_OK && !aligned_to(clip_dev, 4)) bad = PS_ERR_INVALID_ARG;
+    if (bad == PS_OK) bad = check_gradients(list, grads_host, c, scales_host, grad_dtype);
     if (bad != PS_OK) return bad;
     const double t = static_cast<double>(k.step);
     AdamwParams p;

@@ -8,6 +8,7 @@ extension, csrc/marshal.cpp); the work is done by the library on torch's current
 from __future__ import annotations
 
 import ctypes as C
+import itertools
 import os
 from typing import List, NamedTuple, Optional, Sequence, Union
 
@@ -154,15 +155,23 @@ class AdamW(TensorList):
                  "ps_tensors_bind_adamw")
         self._config = B.AdamwConfig()
 
+    def _configure(self):
+        k = self._config
+        k.lr, (k.beta1, k.beta2), k.eps, k.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
+        k.step, k.seed = self.steps + 1, self.seed
+        return k
+
+    def check(self) -> None:
+        """Raises if the next step would refuse lr, betas, eps, weight_decay or steps as they are."""
+        B._check(B.ps_adamw_check(C.byref(self._configure())), "ps_adamw_check")
+
     def step(self, grads, scales: Optional[Sequence[float]] = None, clip: Optional[torch.Tensor] = None) -> None:
         """One step with g = sum_l scales[l] * grads[l] (times clip[1] if `clip`, the result of grad_norm, is given: where its norm is not
         finite nothing changes).  The step is counted in `steps` either way."""
         ptrs, c, factors, dtype = self._gradients(grads, scales)
         if clip is not None:
             B.require_tensor(clip, torch.float32, 2, "clip", on_gpu=True, device=self.device)
-        k = self._config
-        k.lr, (k.beta1, k.beta2), k.eps, k.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
-        k.step, k.seed = self.steps + 1, self.seed
+        k = self._configure()
         B._check(B.ps_adamw_step(self._h, ptrs, c, factors, dtype, C.byref(k), None if clip is None else clip.data_ptr(),
                                  _stream(self.device)), "ps_adamw_step")
         self.steps += 1
@@ -244,9 +253,11 @@ class AdamWServer:
                  max_norm: Optional[float] = None, **adamw):
         self.optimizer = AdamW(params, **adamw)
         self.max_norm = max_norm
+        self._check()
         self._clock = B.ParameterServer(0, num_learners, n, 1.0, modulation=modulation)
         self._token = torch.zeros(1, device=self.optimizer.device)          # stands for a gradient where the clock asks for one
-        self._pushed = {}                                                   # (learner, push index): gradient
+        self._pushed = {}                                                   # (learner, push index): gradient, in the order of the pushes
+        self._dtype = None                                                  # of the gradients: the first push's
         self._pushes = [0] * num_learners
         self.c = self._clock.c
         self.last_norm = None                                               # (norm, factor) of the last update, on the device
@@ -263,16 +274,28 @@ class AdamWServer:
         return self._clock.pull_weights()
 
     def push(self, learner: int, grads: Sequence[torch.Tensor], ts: int) -> bool:
-        """True if this push completed a group."""
+        """True if this push completed a group.  All gradients have the first one's type."""
         grads = list(grads)
-        self.optimizer._gradients(grads, None)                              # what the update would refuse is refused here
+        dtype = self.optimizer._gradients(grads, None)[3]                   # what the update would refuse is refused here
+        if self._dtype not in (None, dtype):
+            raise TypeError("gradients must all be fp32 or all bf16; this server's are %s" % ("bf16" if self._dtype == B.PS_GRAD_BF16 else "fp32"))
         ready = self._clock.push_gradient(learner, self._token, ts)
+        self._dtype = dtype
         self._pushed[learner, self._pushes[learner]] = grads
         self._pushes[learner] += 1
         return ready
 
+    def _check(self) -> None:
+        if self.max_norm is not None and not self.max_norm > 0:
+            raise ValueError("max_norm must be above zero, got %r" % (self.max_norm,))
+        self.optimizer.check()
+
     def apply_update(self) -> None:
-        """Applies the oldest complete group."""
+        """Applies the oldest complete group.  Where the step would refuse it, nothing has changed when this raises."""
+        group = list(itertools.islice(self._pushed.values(), self.c))
+        if len(group) == self.c:                                            # else the clock refuses
+            self._check()
+            self.optimizer._gradients(group, None)
         self._clock.apply_update()
         entries = self._clock.update_log(self._clock.timestamps()[0] - 1, 1)
         grads = [self._pushed.pop((int(e["learner"]), int(e["push_index"]))) for e in entries]
