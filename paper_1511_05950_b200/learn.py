@@ -46,7 +46,8 @@ def _cuda_device(device) -> torch.device:
 # ---- a list of tensors ------------------------------------------------------------------------------------------------
 
 class TensorList:
-    """A list of tensors by their sizes, for the global norm of their gradients.  One list's calls go to one stream at a time."""
+    """A list of tensors by their sizes, for the global norm of their gradients.  One list's calls go to one stream at a time; which one
+    may change from call to call, and a list may be dropped while its work is under way."""
 
     def __init__(self, sizes: Sequence[int], device=None):
         self._h = C.c_void_p()
@@ -57,6 +58,7 @@ class TensorList:
         B._check(B.ps_tensors_sizes(len(self.sizes), self._sizes, C.byref(elems), C.byref(need)), "ps_tensors_sizes")
         self.state_elems = elems.value
         self._workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        self._own, self._streams = [self._workspace], {_stream(self.device)}   # memory nobody else knows of; the streams it was used on
         with _on(self.device):
             B._check(B.ps_tensors_create(C.byref(self._h), len(self.sizes), self._sizes, self._workspace.data_ptr(), need.value,
                                          _stream(self.device)), "ps_tensors_create")
@@ -72,6 +74,16 @@ class TensorList:
             self.destroy()
         except Exception:
             pass
+
+    def _stream(self) -> int:
+        """The current stream.  torch's allocator is told of each, so that it gives the list's own memory, which is that of the stream the list
+        was made on, to nobody before the work there is done."""
+        stream = _stream(self.device)
+        if stream not in self._streams:
+            for t in self._own:
+                t.record_stream(torch.cuda.current_stream(self.device))
+            self._streams.add(stream)
+        return stream
 
     def state_offsets(self) -> List[int]:
         """First element of each tensor in a state array."""
@@ -106,7 +118,7 @@ class TensorList:
             out = torch.empty(2, dtype=torch.float32, device=self.device)
         else:
             B.require_tensor(out, torch.float32, 2, "norm output", on_gpu=True, device=self.device)
-        B._check(B.ps_grad_norm(self._h, ptrs, c, factors, dtype, max_norm, out.data_ptr(), _stream(self.device)), "ps_grad_norm")
+        B._check(B.ps_grad_norm(self._h, ptrs, c, factors, dtype, max_norm, out.data_ptr(), self._stream()), "ps_grad_norm")
         return out
 
 
@@ -141,6 +153,7 @@ class AdamW(TensorList):
         shapes = [(torch.float32, self.state_elems)] * 2 if state_bits == 32 else [(torch.uint8, self.state_elems)] * 2 + [(torch.uint8, blocks)] * 2
         if state is None:
             state = [torch.zeros(max(1, k), dtype=d, device=self.device) for d, k in shapes]
+            self._own += state
         if len(state) != len(shapes):
             raise ValueError("state of %d-bit moments has %d arrays, got %d" % (state_bits, len(shapes), len(state)))
         for t, (d, k) in zip(state, shapes):
@@ -173,7 +186,7 @@ class AdamW(TensorList):
             B.require_tensor(clip, torch.float32, 2, "clip", on_gpu=True, device=self.device)
         k = self._configure()
         B._check(B.ps_adamw_step(self._h, ptrs, c, factors, dtype, C.byref(k), None if clip is None else clip.data_ptr(),
-                                 _stream(self.device)), "ps_adamw_step")
+                                 self._stream()), "ps_adamw_step")
         self.steps += 1
 
     def moments(self):
@@ -181,7 +194,7 @@ class AdamW(TensorList):
         if self.state_bits == 32:
             return self.state
         m, v = (torch.empty(self.state_elems, dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        B._check(B.ps_adamw_moments(self._h, m.data_ptr(), v.data_ptr(), _stream(self.device)), "ps_adamw_moments")
+        B._check(B.ps_adamw_moments(self._h, m.data_ptr(), v.data_ptr(), self._stream()), "ps_adamw_moments")
         return m, v
 
 
@@ -247,7 +260,8 @@ class AdamWServer:
     with s_l = 1 / (c sigma_l) (or the modulation's own penalty over c) in the server's summation order, clipped to max_norm if given, then
     one AdamW step.  The learning rate is AdamW's: a group of equally stale gradients is scaled as a whole, which the step's normalisation
     takes back, so staleness weighs gradients against one another, inside a group and through the moments from group to group.
-    Gradients are borrowed until the update that consumes them; all work goes to torch's current stream."""
+    Gradients are borrowed until the update that consumes them; all work goes to torch's current stream, which has to come after whatever
+    wrote the group's gradients."""
 
     def __init__(self, params: Sequence[torch.Tensor], num_learners: int, n: int, modulation: str = "inv_staleness",
                  max_norm: Optional[float] = None, **adamw):
@@ -304,6 +318,9 @@ class AdamWServer:
         if self.max_norm is not None:
             clip = self.last_norm = self.optimizer.grad_norm(grads, scales, self.max_norm)
         self.optimizer.step(grads, scales, clip=clip)
+        stream = torch.cuda.current_stream(self.optimizer.device)
+        for g in itertools.chain.from_iterable(grads):                      # they may be dropped now: not before the step has read them
+            g.record_stream(stream)
 
     def staleness_histogram(self):
         return self._clock.staleness_histogram()
