@@ -72,17 +72,25 @@ struct Logits {
     at::Tensor floats(int64_t n) const { return at::empty({n}, t.options().dtype(at::kFloat)); }
 };
 
+// Tells autograd that a tensor's values have changed: a backward pass that saved it then raises instead of using the new ones.
+void changed(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Where the gradient goes: True (a new tensor), False or None (nowhere), "inplace" (over the logits) or a tensor.
 struct Gradient {
     at::Tensor t;
     void *data = nullptr;
     int64_t stride = 0;
+    bool given = false;                   // written over values that somebody may have saved
     Gradient(PyObject *grad, const Logits &lg)
     {
         if (grad == Py_False || grad == Py_None) return;
         if (grad == Py_True) {
             t = at::empty(lg.t.sizes(), lg.t.options());
         } else {
+            given = true;
             if (PyUnicode_Check(grad)) {
                 TORCH_CHECK_VALUE(PyUnicode_CompareWithASCIIString(grad, "inplace") == 0, "grad is True, False, 'inplace' or a tensor");
                 t = lg.t.detach();
@@ -95,6 +103,7 @@ struct Gradient {
         data = t.data_ptr();
         stride = t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.size(1), 1);
     }
+    void written(int status) const { if (given && status == PS_OK) changed(t); }
 };
 
 // A workspace for one call on this stream.  Calls of one thread on one stream follow one another and share theirs, which keeps what
@@ -179,6 +188,7 @@ PyObject *policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor ws = workspace(lg.c.rows, 0, lg.t, stream);
     const int status = call_policy_loss(&lg.c, &in, static_cast<float *>(stats.data_ptr()), static_cast<float *>(logp.data_ptr()),
                                         static_cast<float *>(entropy.data_ptr()), grad.data, grad.stride, ws.data_ptr(), ws.numel(), stream);
+    grad.written(status);
     return result(status, {stats, logp, entropy, grad.t});
     END_HANDLE_TH_ERRORS
 }
@@ -205,6 +215,7 @@ PyObject *preference_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor ws = workspace(lg.c.rows, sequences, lg.t, stream);
     const int status = call_preference_loss(&lg.c, &in, static_cast<float *>(stats.data_ptr()), static_cast<float *>(seq_logp.data_ptr()), grad.data, grad.stride,
                                             ws.data_ptr(), ws.numel(), stream);
+    grad.written(status);
     return result(status, {stats, seq_logp, grad.t});
     END_HANDLE_TH_ERRORS
 }
@@ -250,9 +261,21 @@ PyObject *gradients(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// (sequence of tensors): all of them have been written to
+PyObject *written(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 1);
+    const Fast tensors(a[0], "a sequence of tensors");
+    for (Py_ssize_t k = 0; k < tensors.size(); ++k) changed(tensor_of(tensors[k], "a written tensor"));
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 #define SOFTSYNC_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     SOFTSYNC_FAST(bind), SOFTSYNC_FAST(token_logprob), SOFTSYNC_FAST(policy_loss), SOFTSYNC_FAST(preference_loss), SOFTSYNC_FAST(gradients),
+    SOFTSYNC_FAST(written),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

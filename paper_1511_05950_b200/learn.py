@@ -158,6 +158,7 @@ class AdamW(TensorList):
             raise ValueError("state of %d-bit moments has %d arrays, got %d" % (state_bits, len(shapes), len(state)))
         for t, (d, k) in zip(state, shapes):
             B.require_tensor(t, d, k, "state array", on_gpu=True, device=self.device)
+        self._written = params + [t for t in mirrors if t is not None]
         self.params, self.mirrors, self.state, self.state_bits = params, mirrors, tuple(state), state_bits
         self.lr, self.betas, self.eps, self.weight_decay, self.steps, self.seed = lr, betas, eps, weight_decay, step, seed
         p_arr = (C.c_void_p * n)(*[p.data_ptr() for p in params])
@@ -187,6 +188,7 @@ class AdamW(TensorList):
         k = self._configure()
         B._check(B.ps_adamw_step(self._h, ptrs, c, factors, dtype, C.byref(k), None if clip is None else clip.data_ptr(),
                                  self._stream()), "ps_adamw_step")
+        _marshal.written(self._written)
         self.steps += 1
 
     def moments(self):
@@ -232,7 +234,8 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
                 kl_coef: float = 0.0, entropy_coef: float = 0.0, temperature: float = 1.0, grad: Union[bool, str, torch.Tensor] = True) -> PolicyLoss:
     """The clipped policy loss with a KL and an entropy term (formulas: include/softsync_learn.h) and its gradient with respect to the
     logits: `logits.backward(result.dlogits)` continues into the model.  grad: True (a new tensor), a tensor to write to, "inplace" (the
-    gradient replaces the logits), or False."""
+    gradient replaces the logits, which autograd takes as it takes any change in place: not for logits that their producer saved for its
+    backward pass, as a soft cap's tanh does), or False."""
     status, *out = _marshal.policy_loss(logits, tokens, weights, temperature, old_logp, advantages, ref_logp, clip_low, clip_high, kl_coef,
                                         entropy_coef, grad)
     B._check(status, "ps_policy_loss")

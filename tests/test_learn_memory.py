@@ -90,3 +90,67 @@ def test_pushed_gradients_stay_until_the_update_has_read_them():
     assert not b.taken(where)
     b.away.synchronize()
     assert all(bool((p < 1).all()) for p in params)
+
+
+# ---- what autograd sees ---------------------------------------------------------------------------------------------------
+
+def loss_calls(logits):
+    """The two losses with their gradient in place of the logits."""
+    rows = logits.shape[0]
+    tokens = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    old, adv = torch.full((rows,), -2.0, device="cuda"), torch.ones(rows, device="cuda")
+    return {"policy": lambda grad: P.policy_loss(logits, tokens, old, adv, grad=grad),
+            "preference": lambda grad: P.preference_loss(logits, tokens, torch.arange(rows + 1, device="cuda"), old, grad=grad)}
+
+
+@gpu
+@pytest.mark.parametrize("which", ["policy", "preference"])
+def test_a_gradient_in_place_of_saved_logits_is_noticed(which):
+    x = torch.randn(4, 50, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).requires_grad_(True)
+    logits = torch.tanh(x)                                             # saves its output
+    before = logits._version
+    r = loss_calls(logits)[which]("inplace")
+    assert logits._version == before + 1 and r.dlogits.data_ptr() == logits.data_ptr()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        logits.backward(r.dlogits)
+    w = torch.eye(50, device="cuda").requires_grad_(True)
+    logits = torch.tanh(x.detach()) @ w                                # does not
+    apart = loss_calls(logits)[which](True).dlogits
+    assert logits._version == 0
+    logits.backward(loss_calls(logits)[which]("inplace").dlogits)
+    assert torch.allclose(w.grad, torch.tanh(x.detach()).t() @ apart, rtol=1e-5, atol=1e-7)
+
+
+@gpu
+@pytest.mark.parametrize("which", ["policy", "preference"])
+def test_a_given_buffer_counts_as_written_and_a_refused_call_does_not(which):
+    logits = torch.randn(4, 50, device="cuda")
+    buffer = torch.zeros(4, 50, device="cuda")
+    loss_calls(logits)[which](buffer)
+    assert buffer._version == 1 and logits._version == 0
+    wide = torch.zeros(5, 50, device="cuda")
+    with pytest.raises(P.SoftsyncError):                               # overlaps the logits
+        loss_calls(wide[:4])[which](wide[1:])
+    assert wide._version == 0
+    with torch.inference_mode():
+        unwatched = torch.randn(4, 50, device="cuda")
+        loss_calls(unwatched)[which]("inplace")
+
+
+@gpu
+def test_a_step_on_saved_parameters_is_noticed():
+    w = torch.eye(40, device="cuda")
+    mirror = w.bfloat16()
+    x = torch.randn(3, 40, device="cuda").requires_grad_(True)
+    y, z = x @ w, x.bfloat16() @ mirror                                # both save their second factor
+    optimizer = P.AdamW([w], mirrors=[mirror])
+    versions = w._version, mirror._version
+    optimizer.step([torch.ones_like(w)])
+    assert w._version > versions[0] and mirror._version > versions[1]
+    for out in (y, z):
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
+    with pytest.raises(P.SoftsyncError):
+        optimizer.lr = -1.0
+        optimizer.step([torch.ones_like(w)])
+    assert w._version == versions[0] + 1
