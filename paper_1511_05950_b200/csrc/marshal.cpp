@@ -11,7 +11,6 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <map>
-#include <thread>
 #include <tuple>
 
 namespace {
@@ -106,18 +105,23 @@ struct Gradient {
     void written(int status) const { if (given && status == PS_OK) changed(t); }
 };
 
-// A workspace for one call on this stream.  Calls of one thread on one stream follow one another and share theirs, which keeps what
-// the library asks of it (a zero at its front) from call to call; a captured graph gets its own.
+// A workspace for one call on this stream.  Calls on one stream follow one another, whichever thread makes them (each holds the interpreter's
+// lock from here to its last launch), and share theirs, which keeps what the library asks of it (a zero at its front) from call to call; a
+// captured graph gets its own.  A program that keeps making streams gets new ones now and then: what is given up goes back to
+// its stream's part of the allocator, behind the work that uses it.
 at::Tensor workspace(int64_t rows, int64_t sequences, const at::Tensor &like, cudaStream_t stream)
 {
-    static auto *kept = new std::map<std::tuple<int, cudaStream_t, std::thread::id>, at::Tensor>;      // never destroyed: CUDA goes first at exit
+    constexpr size_t most = 128;          // torch's own pools have 64 streams a GPU
+    static auto *kept = new std::map<std::tuple<int, cudaStream_t>, at::Tensor>;      // never destroyed: CUDA goes first at exit
     int64_t need = 0;
     TORCH_CHECK_VALUE(loss_workspace(rows, sequences, &need) == PS_OK, "too many rows or sequences");
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     C10_CUDA_CHECK(cudaStreamIsCapturing(stream, &capture));
     const auto fresh = [&] { return at::zeros({std::max<int64_t>(need, 1 << 16)}, like.options().dtype(at::kByte)); };
     if (capture != cudaStreamCaptureStatusNone) return fresh();
-    at::Tensor &ws = (*kept)[{like.get_device(), stream, std::this_thread::get_id()}];
+    const std::tuple<int, cudaStream_t> key{like.get_device(), stream};
+    if (kept->size() >= most && !kept->count(key)) kept->clear();
+    at::Tensor &ws = (*kept)[key];
     if (!ws.defined() || ws.numel() < need) ws = fresh();
     return ws;
 }

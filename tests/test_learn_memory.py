@@ -1,4 +1,6 @@
 """Whose memory the operators use and for how long: streams, versions that autograd watches, workspaces, captured graphs."""
+import threading
+
 import pytest
 import torch
 
@@ -154,3 +156,101 @@ def test_a_step_on_saved_parameters_is_noticed():
         optimizer.lr = -1.0
         optimizer.step([torch.ones_like(w)])
     assert w._version == versions[0] + 1
+
+
+# ---- workspaces -------------------------------------------------------------------------------------------------------------
+
+def inputs(rows, vocab, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    x = torch.randn(rows, vocab, device="cuda", generator=g, dtype=torch.bfloat16).mul_(2)
+    tokens = torch.randint(0, vocab, (rows,), device="cuda", generator=g)
+    weights = (torch.rand(rows, device="cuda", generator=g) > 0.3).float()
+    old = torch.randn(rows, device="cuda", generator=g) * 0.1 - 9
+    adv = torch.randn(rows, device="cuda", generator=g)
+    offsets = torch.linspace(0, rows, 5, device="cuda").long()
+    return x, tokens, weights, old, adv, offsets
+
+
+def both_losses(x, tokens, weights, old, adv, offsets):
+    policy = P.policy_loss(x, tokens, old, adv, weights, entropy_coef=0.01)
+    preference = P.preference_loss(x, tokens, offsets, old[:4], weights)
+    return [policy.stats, policy.logp, policy.entropy, policy.dlogits, preference.stats, preference.seq_logp, preference.dlogits]
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+CASES = [(9, 500), (700, 3001), (5, 152000), (2100, 40), (400, 33000)]
+
+
+@gpu
+def test_calls_of_many_threads_share_what_is_kept():
+    x = inputs(9, 500, 1)
+    want = both_losses(*x)
+    results = []
+
+    def work():
+        results.append(same(both_losses(*x), want))
+
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for _ in range(40):
+        t = threading.Thread(target=work)
+        t.start()
+        t.join()
+    torch.cuda.synchronize()
+    assert results == [True] * 40 and torch.cuda.memory_allocated() == before
+
+
+@gpu
+def test_losses_of_different_sizes_one_after_the_other():
+    """They share a workspace that grows, and the larger ones leave their traces in it."""
+    data = [inputs(r, v, k) for k, (r, v) in enumerate(CASES)]
+    want = [both_losses(*d) for d in data]
+    for order in ([4, 0, 3, 1, 2], [0, 0, 1, 0, 3, 0, 2, 4, 0]):
+        for k in order:
+            assert same(both_losses(*data[k]), want[k])
+
+
+@gpu
+def test_threads_on_streams_of_their_own_at_the_same_time():
+    data = [inputs(r, v, k) for k, (r, v) in enumerate(CASES)]
+    want = [both_losses(*d) for d in data]
+    torch.cuda.synchronize()
+    results = {}
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = [both_losses(*data[k]) for _ in range(10)]
+            torch.cuda.current_stream().synchronize()
+            results[k] = all(same(g, want[k]) for g in got)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(data))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert results == {k: True for k in range(len(data))}
+
+
+@gpu
+@pytest.mark.parametrize("rows,vocab", CASES + [(4, 1000003)])
+def test_a_captured_graph_has_a_workspace_of_its_own(rows, vocab):
+    """Recorded once, replayed on other inputs, with calls of the same stream in between."""
+    x = inputs(rows, vocab, 1)
+    both_losses(*x)                                                    # what a kernel asks once of the GPU is asked before
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both_losses(*x)
+    for seed in (2, 3):
+        y = inputs(rows, vocab, seed)
+        for a, b in zip(x, y):
+            a.copy_(b)
+        graph.replay()
+        want = both_losses(*y)
+        assert same(out, want)
+        graph.replay()
+        assert same(out, want)
