@@ -4,9 +4,13 @@
 their server (losses from logits, gradient norm, AdamW).  Everything the two export is reachable
 from this package (`paper_1511_05950_b200.ParameterServer`, `.AdamW`, `.ps_create`, ...).  The binding is
 loaded on first use, so that `paper_1511_05950_b200.build` can be imported to build the library
-first; using anything else without the built library raises (there is no CPU fallback).
+first; using anything else without the built library raises (there is no CPU fallback).  The server needs the library
+alone; what `learn` exports needs the _marshal extension too.
 """
 import importlib
+
+_LEARN = frozenset(("AdamW", "AdamWServer", "INPLACE", "PolicyLoss", "PreferenceLoss", "TensorList", "TokenLogprob", "policy_loss", "preference_loss",
+                    "token_logprob"))
 
 
 def __getattr__(name):
@@ -14,14 +18,16 @@ def __getattr__(name):
         raise AttributeError(name)
     if name == "build":                      # importable before the library exists
         return importlib.import_module(".build", __name__)
+    if name == "learn" or name in _LEARN:
+        learn = importlib.import_module(".learn", __name__)
+        if name == "learn":
+            return learn
+        globals()[name] = getattr(learn, name)               # found once: later uses do not come here
+        return globals()[name]
     binding = importlib.import_module(".binding", __name__)
     if name == "binding":
         return binding
-    learn = importlib.import_module(".learn", __name__)
-    if name == "learn":
-        return learn
-    for module in (learn, binding):
-        if hasattr(module, name):
-            globals()[name] = getattr(module, name)          # found once: later uses do not come here
-            return globals()[name]
-    raise AttributeError("module %r has no attribute %r" % (__name__, name))
+    try:
+        return getattr(binding, name)
+    except AttributeError:
+        raise AttributeError("module %r has no attribute %r" % (__name__, name)) from None

@@ -7,6 +7,7 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -78,16 +79,16 @@ def build_marshal(force: bool = False) -> str:
     cmd = [shutil.which("g++") or "g++"] + MARSHAL_FLAGS + ["-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
     cmd += ["-isystem" + i for i in include] + ["-o", MARSHAL, MARSHAL_SOURCES[0], "-L" + libs, "-Wl,-rpath," + libs,
                                                 "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
-    if os.path.exists(MARSHAL_STAMP):
-        os.remove(MARSHAL_STAMP)
+    for old in (MARSHAL_STAMP, MARSHAL):         # an extension of other sources must not be loaded if this fails
+        if os.path.exists(old):
+            os.remove(old)
     subprocess.run(cmd, check=True)
     with open(MARSHAL_STAMP, "w") as f:
         f.write(marshal_digest() + "\n")
     return MARSHAL
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    build_marshal(force)
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     cmd = [nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
@@ -100,10 +101,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build(force: bool = False, verbose: bool = False) -> str:
+    """Builds the library, then the extension; raises if either fails."""
+    lib = build_library(force, verbose)
+    build_marshal(force)
+    return lib
+
+
 def ensure_built() -> str:
-    """Build the library and the extension if they are missing or were built from other sources.  A failed rebuild raises: a
-    library that does not match the header and the binding must not be loaded."""
-    return build(force=False)
+    """Build the library and the extension if they are missing or were built from other sources.  A failed rebuild of the library raises: a
+    library that does not match the header and the binding must not be loaded.  One of the extension warns: the server needs
+    nothing of it, and what does raises when it is used."""
+    lib = build_library()
+    try:
+        build_marshal()
+    except (OSError, RuntimeError, subprocess.CalledProcessError) as e:
+        warnings.warn("the _marshal extension could not be built (%s): the operators of learn.py are not available" % e)
+    return lib
 
 
 if __name__ == "__main__":
