@@ -154,6 +154,10 @@ int64_t row_vectors(const ps_logits *lg)
 constexpr int kMaxCluster = softsync::kMaxCluster;
 constexpr int kWaitLimit = 1 << 20;                    // polls of up to a microsecond each
 
+// Threads of a row's blocks: as few as keep the row's loads under way, since warps without a vector of their own and a wider join cost time.
+// Two vectors a thread and batch with 64 threads, four beyond.  Measured on 2.5e8 elements, all with the entropy, 64 | 256 | 512 threads:
+// 256 vectors a row (2048 bf16) 344 | 438 | 905 us, 276 (1100 fp32) 716 | 676 | 1348; 6283 vectors (50257 bf16) 197 | 102 | 129, 8192 (65536 bf16)
+// 188 | 90 | 88, 25000 (200000 bf16) 284 | 104 | 98; with few rows (256 of 100000 bf16) 76 | 23 | 20.
 template <typename GT, bool ENTROPY>
 int launch_stats_as(const RowsIn &in, int64_t vectors, const StatsOut &out, cudaStream_t st)
 {
@@ -162,8 +166,8 @@ int launch_stats_as(const RowsIn &in, int64_t vectors, const StatsOut &out, cuda
         while (cluster < kMaxCluster && in.rows * cluster * 2 <= 2 * sm_count() && vectors > static_cast<int64_t>(cluster) * threads * batch) cluster *= 2;
         return launch_rows(kernel, in.rows, cluster, threads, 0, false, st, in, out);
     };
-    if (vectors <= 128) return go(softsync::row_stats_kernel<GT, 64, 2, ENTROPY>, 64, 2);
-    if (vectors <= 1024) return go(softsync::row_stats_kernel<GT, 256, 4, ENTROPY>, 256, 4);
+    if (vectors <= 256) return go(softsync::row_stats_kernel<GT, 64, 2, ENTROPY>, 64, 2);
+    if (vectors < 8192) return go(softsync::row_stats_kernel<GT, 256, 4, ENTROPY>, 256, 4);
     return go(softsync::row_stats_kernel<GT, 512, 4, ENTROPY>, 512, 4);
 }
 int launch_stats(const ps_logits *lg, const RowsIn &in, const StatsOut &out, bool entropy, cudaStream_t st)
