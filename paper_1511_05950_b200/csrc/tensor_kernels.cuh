@@ -7,8 +7,8 @@
 //
 // Every pass touches every byte once and is bound by HBM: AdamW reads and writes 28 bytes an element with one fp32 gradient and
 // 32-bit moments, 16 with a bf16 gradient, 8-bit moments and a bf16 mirror.  The codes and their random rounding cost some 70
-// instructions an element, which makes the instruction issue the second bound there (72 % of its slots used at 5.8 TB/s); the
-// 32-bit step uses 27 %.
+// instructions an element, which makes the instruction issue the second bound there (72 % of its slots used at 4.7e8 elements and 5.8 TB/s);
+// the 32-bit step uses 27 %.
 //
 // Arithmetic contract, as in the momentum kernels: every product, sum, quotient and root is rounded to fp32 by itself, in the
 // documented order, whatever the launch shape, so results can be compared bit by bit (one exception: quotients below 2^-126, at kMScale).
@@ -339,7 +339,8 @@ __device__ __forceinline__ unsigned block_exponent(unsigned top)
 }
 
 // 32 random bits for the element whose place has the low word lo; hi_term: its high word times 0x9E3779B9.  An integer hash (two rounds
-// of xor-shift and multiply) of the place and the step's key.
+// of xor-shift and multiply) of the place and the step's key; multipliers and shifts are those that C. Wellons published in 2018 from a search for
+// 32-bit hashes of low bias (0x7FEB352D, 0x846CA68B; 16, 15, 16).
 __device__ __forceinline__ unsigned element_hash(unsigned lo, unsigned hi_term, unsigned key)
 {
     unsigned x = (lo ^ key) + hi_term;
