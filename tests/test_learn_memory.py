@@ -1,4 +1,5 @@
 """Whose memory the operators use and for how long: streams, versions that autograd watches, workspaces, captured graphs."""
+import gc
 import threading
 
 import pytest
@@ -10,15 +11,16 @@ gpu = pytest.mark.gpu
 
 
 class Busy:
-    """Two streams, the second with some tens of milliseconds of work ahead of what it is given."""
+    """Two streams, the second with a fifth of a second of work ahead of what it is given."""
 
     def __init__(self):
         self.home, self.away = torch.cuda.Stream(), torch.cuda.Stream()
 
     def start(self):
+        gc.collect()                                                   # not while the other stream is at work: it takes a while after many tests
         self.away.wait_stream(self.home)
         with torch.cuda.stream(self.away):
-            torch.cuda._sleep(100_000_000)
+            torch.cuda._sleep(400_000_000)
 
     def taken(self, places):
         """Whether an allocation of any size of `places` on the first stream gets one of those places now, while the second is still at work."""
@@ -27,7 +29,8 @@ class Busy:
             for place, size in places:
                 held += [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(3)]
         hit = {t.data_ptr() for t in held} & {place for place, _ in places}
-        assert not self.away.query(), "the work ended too early to show anything"
+        if self.away.query():
+            pytest.skip("the host took too long: the other stream's work has ended, which shows nothing")
         return bool(hit)
 
 
