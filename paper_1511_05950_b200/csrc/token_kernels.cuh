@@ -320,13 +320,17 @@ struct RowCoef { float a, b; };
 // a well-behaved model never come there: logits of 32 at a temperature of 1 make a shift of 50.
 constexpr float kShiftLimit = 1024.f;
 struct RowGradient {
-    float m, log2_sum, c, add, mult, one, shift;
-    __device__ __forceinline__ RowGradient(float m_, float l2, float c_, RowCoef k, float entropy)
-        : m(m_), log2_sum(l2), c(c_), add(fmaf(k.b, entropy, -k.a)), mult(k.b * kLn2), one(k.a), shift(-fmaf(m_, c_, l2)) {}
-
-    // whether the exponent is x c + shift: the same for the whole row
+    float c, add, mult, one, off, base;                    // the exponent is (x - off) c + base
+    bool regular, shifted;                                 // the maximum is ordinary; off is zero: the same for the whole row
     template <typename GT>
-    __device__ __forceinline__ bool shifted() const { return logit_bytes<GT>() == 2 && fabsf(shift) < kShiftLimit; }
+    __device__ __forceinline__ RowGradient(const GT *, float m, float l2, float c_, RowCoef k, float entropy)
+        : c(c_), add(fmaf(k.b, entropy, -k.a)), mult(k.b * kLn2), one(k.a), regular(ordinary(m, c_))
+    {
+        const float shift = -fmaf(m, c, l2);
+        shifted = logit_bytes<GT>() == 2 && regular && fabsf(shift) < kShiftLimit;
+        off = shifted ? 0.f : m;
+        base = shifted ? shift : -l2;
+    }
 
     // any maximum, beside an ordinary one with the bits of the vector form; the token's own entry has `one` to be added
     template <typename GT, bool ENTROPY>
@@ -334,14 +338,14 @@ struct RowGradient {
     {
         constexpr float floor = logit_bytes<GT>() == 4 ? kFloor : kFloorBf16;
         const float y = ENTROPY ? max_nan(x, floor) : x;
-        const float d = !ordinary(m, c) ? max_nan((x - m) * c, -1000.f) - log2_sum : shifted<GT>() ? fmaf(y, c, shift) : fmaf(y - m, c, -log2_sum);
+        const float d = regular ? fmaf(y - off, c, base) : max_nan((x - off) * c, -1000.f) + base;
         return __fmul_rn(ex2(d), ENTROPY ? fmaf(mult, d, add) : add);
     }
-    // beside an ordinary maximum; SHIFT: shifted()
+    // beside an ordinary maximum; SHIFT: shifted
     template <typename GT, bool ENTROPY, bool SHIFT>
     __device__ __forceinline__ uint4 vector(const uint4 &x) const
     {
-        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m), l2 = SHIFT ? make_float2(shift, shift) : make_float2(-log2_sum, -log2_sum);
+        const float2 c2 = make_float2(c, c), m2 = make_float2(-off, -off), l2 = make_float2(base, base);
         const float2 a2 = make_float2(add, add), b2 = make_float2(mult, mult);
         float g[per_vector<GT>()];
 #pragma unroll
@@ -358,7 +362,7 @@ struct RowGradient {
     __device__ __forceinline__ uint4 vector_of(const uint4 &x) const
     {
         if constexpr (logit_bytes<GT>() == 2)
-            if (shifted<GT>()) return vector<GT, ENTROPY, true>(x);
+            if (shifted) return vector<GT, ENTROPY, true>(x);
         return vector<GT, ENTROPY, false>(x);
     }
 };
@@ -544,8 +548,8 @@ __global__ void __launch_bounds__(kGradThreads, 6) row_grad_kernel(const __grid_
     }
     const RowStat st = stat[r];
     const long long tok = in.tokens[r];
-    const RowGradient f(st.max, st.log2_sum, in.scale, k, ENTROPY ? entropy[r] : 0.f);
-    if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c)) {
+    const RowGradient f(static_cast<const GT *>(nullptr), st.max, st.log2_sum, in.scale, k, ENTROPY ? entropy[r] : 0.f);
+    if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && f.regular) {
         const int tok_q = tok >= 0 && tok < vocab ? (static_cast<int>(tok) + v.phase) / PV : -1, tok_j = (static_cast<int>(tok) + v.phase) % PV;
         unsigned char *p = dst - v.phase * logit_bytes<GT>() + static_cast<long long>(q0) * 16;
 #pragma unroll
@@ -1017,32 +1021,27 @@ __global__ void __launch_bounds__(RingShape<T>::block, RingShape<T>::per_sm) pol
             }
             late = late || !mbar_wait_bounded(smem_addr(&sh.go), turn & 1, plan.wait_limit);
             ++turn;
-            const RowGradient f(sh.row[0], late ? CUDART_NAN_F : sh.row[1], in.scale, RowCoef{sh.row[3], sh.row[4]}, sh.row[2]);
+            const RowGradient f(static_cast<const GT *>(nullptr), sh.row[0], late ? CUDART_NAN_F : sh.row[1], in.scale, RowCoef{sh.row[3], sh.row[4]}, sh.row[2]);
             const int tok = sh.tok;
             const RowVectors<GT> v(row_at(due), vocab);
             const int hi = min(lo + plan.vectors, v.full);
             const bool clean = lo >= v.inner;
             unsigned char *dst = out + static_cast<long long>(due) * out_stride * logit_bytes<GT>();
-            const bool plain = ((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && ordinary(f.m, f.c);
+            const bool plain = ((reinterpret_cast<uintptr_t>(v.row) ^ reinterpret_cast<uintptr_t>(dst)) & 15) == 0 && f.regular;
             constexpr bool kShift = logit_bytes<GT>() == 2;
-            const bool usual = !kShift || f.template shifted<GT>();
+            const bool shifted = !kShift || f.shifted;     // a whole chunk of such a row saves the subtraction
             unsigned char *p = dst - v.phase * logit_bytes<GT>() + static_cast<long long>(lo + tid) * 16;
             for (int left = hi - lo, k = 0; k < plan.chunks; ++k, left -= kRingChunk) {
                 const uint4 *mine = reinterpret_cast<const uint4 *>(ring) + slot * kRingChunk + tid;
                 if (out && plain) {
-                    if (!usual) {
-#pragma unroll 1
-                        for (int q = 0; q < NV; ++q)
-                            if (q * T + tid < left && (k > 0 || q * T + tid > 0 || clean))
-                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, false>(mine[q * T]));
-                    } else if (left >= kRingChunk && (k > 0 || clean)) {
+                    if (shifted && left >= kRingChunk && (k > 0 || clean)) {
 #pragma unroll
                         for (int q = 0; q < NV; ++q) __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, kShift>(mine[q * T]));
                     } else {
 #pragma unroll
                         for (int q = 0; q < NV; ++q)
                             if (q * T + tid < left && (k > 0 || q * T + tid > 0 || clean))
-                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, kShift>(mine[q * T]));
+                                __stcs(reinterpret_cast<uint4 *>(p + q * T * 16), f.template vector<GT, ENTROPY_GRAD, false>(mine[q * T]));
                     }
                     p += kRingChunk * 16;
                 } else if (out) {
