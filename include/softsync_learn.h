@@ -122,6 +122,7 @@ int ps_token_logprob(const ps_logits *logits, float *logp_dev, float *lse_dev, f
  *     a = (-rho A where rho A <= clamp(rho) A, else 0) + kl_coef (1 - exp(d)).
  * ref_logp_dev may be NULL: no KL term (kl_coef is ignored).  dlogits_dev: logits' dtype, rows of vocab values dlogits_stride elements
  * apart; it may be the logits' own memory (same stride): the gradient then replaces them; else it must not overlap them.  NULL: no gradient.
+ * A row that lies at the same place within 16 bytes in both is written in vectors, others (a dense gradient of padded rows) element by element.
  * stats_dev: 5 fp32, weighted means of loss, clipped term, KL term, entropy, and the share of clipped tokens.
  * logp_dev, entropy_dev: rows fp32 each (zero where the weight is zero); entropy_dev may be NULL. */
 typedef struct ps_policy_inputs {

@@ -801,8 +801,8 @@ __device__ __forceinline__ void ring_sync() { asm volatile("bar.sync 1, %0;" :: 
 // A vector at a row's ragged end comes with ordinary loads, through a register of the thread that handles it (the last thread the
 // front's, the first thread the end's: never the same one).
 //
-// What bounds it: one read and one write of two bytes an element go at 5.1 to 5.8 TB/s of algorithmic bytes in bf16 (16384 x 32000: 387 us;
-// 8192 x 131072: 740; 8192 x 152000: 930) and 6.0 in fp32 (4096 x 128000: 697), with 57 % of the issue slots, 58 % of the DRAM's
+// What bounds it: one read and one write of two bytes an element go at 5.1 to 5.6 TB/s of algorithmic bytes in bf16 (16384 x 32000: 400 us;
+// 8192 x 131072: 770; 8192 x 152000: 929) and 6.0 in fp32 (4096 x 128000: 704), with 57 % of the issue slots, 58 % of the DRAM's
 // cycles and two thirds of the exponential unit's busy at 152000: 16 warps an SM are too few to fill one of them, and the rows'
 // bytes leave no room for more.  Of the forms tried (256 threads x 4 vectors x 7 slots x 2 blocks an SM, 128 x 8, 192 x 4 x 9, 384 x 2 x 9, 512 x
 // 2; one block of 256, 384 and 512) these two were the fastest.
@@ -1114,7 +1114,7 @@ static __global__ void __launch_bounds__(kPairThreads) preference_terms_kernel(c
     sequence_rows(in, 2 * i + side, rows.rows, lo, hi);
     const double ref = static_cast<double>(in.ref_logp[2 * i]) - static_cast<double>(in.ref_logp[2 * i + 1]);
     // Weights come eight at a time, the first ones before the statistics are there (two pairs of
-    // 1024 rows: 7.8 us, one at a time 14.3).
+    // 1024 rows: 7.0 us, one at a time 14.3).
     constexpr int N = 8;
     float w[N];
     const auto weights = [&](long long r0) {
