@@ -148,6 +148,105 @@ typedef struct ps_preference_inputs {
 int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, float *stats_dev, float *seq_logp_dev,
                        void *dlogits_dev, int64_t dlogits_stride, void *workspace_dev, int64_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Losses without logits.  The logits of a position are the products of its hidden state with the rows of the output matrix (the head),
+ *     z_tj = hidden_t . head_j / T,     lse_t = log sum_j exp(z_tj),     logp_t = z_t,token - lse_t
+ * They are computed a tile at a time (tensor cores, fp32 sums) and never leave the chip; the gradients compute them again, a piece of the
+ * vocabulary after the other, and of a piece only the rounded bf16 values
+ *     G_tj = a_t (p_tj - 1[j = token])
+ * are held in the workspace, for the two products  dhidden = scale G head  and  dhead = scale G^T hidden  (sums in fp32, in a fixed order).
+ * Rows with a weight (or a dlogp) of exactly zero take no part, whatever they or their token hold: they are not read, their outputs and their
+ * dhidden are zero.  A token outside [0, vocab) makes its row's results NaN; a row with a NaN or an infinity has NaN results (minus infinity as the
+ * product of a finite row with an entry of the head is a barred entry, p = 0).  NaN results of a row with a weight reach the loss and dhead.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef struct ps_head {
+    const void *hidden_dev;               /* bf16, rows of `width` values, hidden_stride elements apart */
+    const void *head_dev;                 /* bf16, vocab rows of `width` values, head_stride elements apart */
+    int64_t rows, width, vocab, hidden_stride, head_stride;
+    const int64_t *tokens_dev;            /* rows token ids */
+    float temperature;                    /* > 0 */
+} ps_head;
+
+/* Bytes of the device workspace (256-byte aligned) of the calls below; grad: of those with gradients.  It need not be initialised and holds nothing
+ * between calls; calls that share one must not overlap in time.  Where the width is no multiple of 8, or a matrix is not aligned to 16 bytes
+ * (address and stride), the workspace has room for an aligned copy of it. */
+int ps_head_workspace(const ps_head *head, int grad, int64_t *bytes);
+
+/* logp, lse (fp32, rows each) of the rows with a weight; zeros elsewhere.  weights_dev: rows fp32, or NULL (all). */
+int ps_head_logprob(const ps_head *head, const float *weights_dev, float *logp_dev, float *lse_dev, void *workspace_dev, int64_t workspace_bytes,
+                    void *stream);
+
+/* The gradients of any loss of the log probabilities, from dlogp_t = dloss/dlogp_t and lse (of ps_head_logprob): a_t = -dlogp_t, scale = 1 / T.
+ * dhidden_dev: rows x width, dhead_dev: vocab x width, dense, 16-byte aligned, bf16; either may be NULL. */
+int ps_head_logprob_grad(const ps_head *head, const float *lse_dev, const float *dlogp_dev, void *dhidden_dev, void *dhead_dev, void *workspace_dev,
+                         int64_t workspace_bytes, void *stream);
+
+/* loss = -sum w_t logp_t / sum w (0 where sum w is 0) and its gradients: a_t = w_t, scale = 1 / (T sum w).  stats_dev: 2 fp32, loss and sum of the
+ * weights.  logp_dev, lse_dev: rows fp32.  dhidden_dev, dhead_dev: as above. */
+int ps_head_cross_entropy(const ps_head *head, const float *weights_dev, float *stats_dev, float *logp_dev, float *lse_dev, void *dhidden_dev, void *dhead_dev,
+                          void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Activations in 8 bits.  PS_PACK_BLOCK columns of a row share a power of two u = 2^(s - 127), s a byte:
+ *     u = 2^(floor(log2 max|x|) - 6), at least 2^-126;     code = x / u rounded to the nearest integer (ties to even), cut to +-127;     value = code u
+ * A block with an infinity or a NaN has s = 255 and reads back as NaN.  Rows of codes are padded with zeros to a multiple of PS_PACK_BLOCK:
+ * codes_dev: rows * round_up(cols, PS_PACK_BLOCK) bytes, 16-byte aligned; scales_dev: rows * ceil(cols / PS_PACK_BLOCK) bytes.  Values are exact in bf16
+ * and fp32.  dtype: ps_grad_dtype of the activations (fp32 or bf16).
+ * ------------------------------------------------------------------------------------------------------------------ */
+#define PS_PACK_BLOCK 32
+
+int ps_pack8(const void *x_dev, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int8_t *codes_dev, uint8_t *scales_dev, void *stream);
+int ps_unpack8(const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows, int64_t cols, void *out_dev, int dtype, int64_t row_stride, void *stream);
+
+/* Root-mean-square norm of the residual stream, row by row:
+ *     total = x + residual, rounded to dtype (x where residual_dev is NULL);     r = 1 / sqrt(mean(total^2) + eps);     n = total r
+ *     out = n gain, rounded to dtype (n where gain_dev is NULL);     codes, scales = 8 bits of n (before the gain, which the backward pass and
+ *     ps_packed_weight_grad apply)
+ * total_dev (total_stride elements a row) may be NULL, or the memory of x or of residual (with the same stride); out_dev (dense) may be NULL, or x's memory where
+ * its rows are dense too; codes_dev and scales_dev may both be NULL.  rstd_dev: r, rows fp32.  Other overlaps are refused or undefined. */
+typedef struct ps_norm {
+    const void *x_dev, *residual_dev, *gain_dev;
+    int dtype, gain_dtype;                /* ps_grad_dtype each */
+    int64_t rows, cols, x_stride, residual_stride, total_stride;
+    float eps;                            /* >= 0 */
+    void *total_dev, *out_dev;
+    int8_t *codes_dev;
+    uint8_t *scales_dev;
+    float *rstd_dev;
+} ps_norm;
+int ps_rms_norm(const ps_norm *norm, void *stream);
+
+/* Its backward pass, from the 8 bits (codes_dev, scales_dev) or, where those are NULL, from total:
+ *     g = dout gain;     dx = r (g - n mean(g n)) + dtotal, rounded to dtype: the gradient of x and of residual;     dgain = sum over rows of dout n
+ * dtotal_dev (what comes back along the residual stream) and gain_dev may be NULL; dgain_dev: cols values of gain_dtype, or NULL.  dx_dev: dense; it may be
+ * dout's or dtotal's memory where that is dense.  Sums have a fixed order. */
+typedef struct ps_norm_grad {
+    const void *dout_dev, *total_dev, *gain_dev, *dtotal_dev;
+    const int8_t *codes_dev;
+    const uint8_t *scales_dev;
+    const float *rstd_dev;
+    int dtype, gain_dtype;
+    int64_t rows, cols, dout_stride, total_stride, dtotal_stride;
+    void *dx_dev, *dgain_dev;
+} ps_norm_grad;
+int ps_norm_grad_workspace(int64_t rows, int64_t cols, int64_t *bytes);
+int ps_rms_norm_grad(const ps_norm_grad *grad, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* The gradient of a weight matrix (outs x cols) whose product took the kept activations n, times a gain, as input:
+ *     dweight_jk = gain_k sum_t dout_tj n_tk
+ * dout_dev: bf16, rows of `outs` values; n: the 8 bits, which enter the tensor cores exactly; sums in fp32, in a fixed order.  gain_dev: cols values of
+ * gain_dtype, or NULL.  dweight_dev: outs x cols, dense, 16-byte aligned, of out_dtype. */
+typedef struct ps_packed_grad {
+    const void *dout_dev, *gain_dev;
+    const int8_t *codes_dev;
+    const uint8_t *scales_dev;
+    int gain_dtype, out_dtype;
+    int64_t rows, outs, cols, dout_stride;
+    void *dweight_dev;
+} ps_packed_grad;
+int ps_packed_grad_workspace(const ps_packed_grad *grad, int64_t *bytes);
+int ps_packed_weight_grad(const ps_packed_grad *grad, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -54,11 +54,13 @@ EXPORTS = (
     "ps_fused_update_static", "ps_bind_weight_replicas",
     "ps_tensors_sizes", "ps_tensors_create", "ps_tensors_destroy", "ps_tensors_bind_adamw", "ps_grad_norm", "ps_adamw_step",
     "ps_adamw_check", "ps_adamw_moments", "ps_loss_workspace", "ps_token_logprob", "ps_policy_loss", "ps_preference_loss",
+    "ps_head_workspace", "ps_head_logprob", "ps_head_logprob_grad", "ps_head_cross_entropy", "ps_pack8", "ps_unpack8", "ps_rms_norm",
+    "ps_norm_grad_workspace", "ps_rms_norm_grad", "ps_packed_grad_workspace", "ps_packed_weight_grad",
 )
 
 
 # ---- structures of include/softsync_learn.h -----------------------------------
-PS_STATE_BLOCK, PS_LIST_MAX_GRADS = 256, 256
+PS_STATE_BLOCK, PS_LIST_MAX_GRADS, PS_PACK_BLOCK = 256, 256, 32
 
 
 class AdamwConfig(C.Structure):
@@ -79,6 +81,29 @@ class PolicyInputs(C.Structure):
 class PreferenceInputs(C.Structure):
     _fields_ = [("offsets_dev", C.c_void_p), ("ref_logp_dev", C.c_void_p), ("pairs", C.c_int64),
                 ("beta", C.c_float), ("label_smoothing", C.c_float)]
+
+
+class Head(C.Structure):
+    _fields_ = [("hidden_dev", C.c_void_p), ("head_dev", C.c_void_p), ("rows", C.c_int64), ("width", C.c_int64), ("vocab", C.c_int64),
+                ("hidden_stride", C.c_int64), ("head_stride", C.c_int64), ("tokens_dev", C.c_void_p), ("temperature", C.c_float)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("x_dev", C.c_void_p), ("residual_dev", C.c_void_p), ("gain_dev", C.c_void_p), ("dtype", C.c_int), ("gain_dtype", C.c_int),
+                ("rows", C.c_int64), ("cols", C.c_int64), ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("total_stride", C.c_int64),
+                ("eps", C.c_float), ("total_dev", C.c_void_p), ("out_dev", C.c_void_p), ("codes_dev", C.c_void_p), ("scales_dev", C.c_void_p),
+                ("rstd_dev", C.c_void_p)]
+
+
+class NormGrad(C.Structure):
+    _fields_ = [("dout_dev", C.c_void_p), ("total_dev", C.c_void_p), ("gain_dev", C.c_void_p), ("dtotal_dev", C.c_void_p), ("codes_dev", C.c_void_p),
+                ("scales_dev", C.c_void_p), ("rstd_dev", C.c_void_p), ("dtype", C.c_int), ("gain_dtype", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("dout_stride", C.c_int64), ("total_stride", C.c_int64), ("dtotal_stride", C.c_int64), ("dx_dev", C.c_void_p), ("dgain_dev", C.c_void_p)]
+
+
+class PackedGrad(C.Structure):
+    _fields_ = [("dout_dev", C.c_void_p), ("gain_dev", C.c_void_p), ("codes_dev", C.c_void_p), ("scales_dev", C.c_void_p), ("gain_dtype", C.c_int),
+                ("out_dtype", C.c_int), ("rows", C.c_int64), ("outs", C.c_int64), ("cols", C.c_int64), ("dout_stride", C.c_int64), ("dweight_dev", C.c_void_p)]
 
 
 class SoftsyncError(RuntimeError):
@@ -143,6 +168,17 @@ def _load() -> C.CDLL:
         "ps_token_logprob": [C.POINTER(Logits), vp, vp, vp, vp],
         "ps_policy_loss": [C.POINTER(Logits), C.POINTER(PolicyInputs), vp, vp, vp, vp, i64, vp, i64, vp],
         "ps_preference_loss": [C.POINTER(Logits), C.POINTER(PreferenceInputs), vp, vp, vp, i64, vp, i64, vp],
+        "ps_head_workspace": [C.POINTER(Head), i32, C.POINTER(i64)],
+        "ps_head_logprob": [C.POINTER(Head), vp, vp, vp, vp, i64, vp],
+        "ps_head_logprob_grad": [C.POINTER(Head), vp, vp, vp, vp, vp, i64, vp],
+        "ps_head_cross_entropy": [C.POINTER(Head), vp, vp, vp, vp, vp, vp, vp, i64, vp],
+        "ps_pack8": [vp, i32, i64, i64, i64, vp, vp, vp],
+        "ps_unpack8": [vp, vp, i64, i64, vp, i32, i64, vp],
+        "ps_rms_norm": [C.POINTER(Norm), vp],
+        "ps_norm_grad_workspace": [i64, i64, C.POINTER(i64)],
+        "ps_rms_norm_grad": [C.POINTER(NormGrad), vp, i64, vp],
+        "ps_packed_grad_workspace": [C.POINTER(PackedGrad), C.POINTER(i64)],
+        "ps_packed_weight_grad": [C.POINTER(PackedGrad), vp, i64, vp],
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -201,6 +237,17 @@ ps_loss_workspace = lib.ps_loss_workspace
 ps_token_logprob = lib.ps_token_logprob
 ps_policy_loss = lib.ps_policy_loss
 ps_preference_loss = lib.ps_preference_loss
+ps_head_workspace = lib.ps_head_workspace
+ps_head_logprob = lib.ps_head_logprob
+ps_head_logprob_grad = lib.ps_head_logprob_grad
+ps_head_cross_entropy = lib.ps_head_cross_entropy
+ps_pack8 = lib.ps_pack8
+ps_unpack8 = lib.ps_unpack8
+ps_rms_norm = lib.ps_rms_norm
+ps_norm_grad_workspace = lib.ps_norm_grad_workspace
+ps_rms_norm_grad = lib.ps_rms_norm_grad
+ps_packed_grad_workspace = lib.ps_packed_grad_workspace
+ps_packed_weight_grad = lib.ps_packed_weight_grad
 
 
 def status_string(status: int) -> str:

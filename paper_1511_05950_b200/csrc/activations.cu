@@ -1,0 +1,206 @@
+// Entry points of softsync_learn.h that work on rows of activations: the norm with its backward pass, packing and unpacking.
+#include "../../include/softsync_learn.h"
+#include "host_util.h"
+#include "norm_kernels.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+using softsync::aligned_to;
+using softsync::NormGradIn;
+using softsync::NormIn;
+using bf16 = __nv_bfloat16;
+
+namespace {
+
+constexpr int64_t kMaxRows = 0x7fffffff, kMaxCols = int64_t{1} << 28;
+
+int64_t div_up(int64_t x, int64_t by) { return (x + by - 1) / by; }
+int launched() { return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA; }
+bool is_dtype(int t) { return t == PS_GRAD_FP32 || t == PS_GRAD_BF16; }
+int64_t size_of(int dtype) { return dtype == PS_GRAD_BF16 ? 2 : 4; }
+
+// Rows `stride` elements apart, at a place that the type allows.
+bool rows_ok(const void *p, int dtype, int64_t rows, int64_t cols, int64_t stride)
+{
+    return p && aligned_to(p, size_of(dtype)) && (rows <= 1 || (stride >= cols && stride <= (int64_t{1} << 60) / rows));
+}
+bool vectors_ok(const void *p, int dtype, int64_t rows, int64_t stride) { return aligned_to(p, 16) && (rows <= 1 || stride * size_of(dtype) % 16 == 0); }
+bool shape_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxCols; }
+bool packed_ok(const int8_t *codes, const uint8_t *scales) { return codes && scales && aligned_to(codes, 16); }
+
+template <typename T>
+int launch_norm(const NormIn &in, cudaStream_t st)
+{
+    const int64_t units = div_up(in.cols, softsync::kUnit);
+    const auto go = [&](auto kernel, int warps) {
+        const int64_t blocks = warps == 1 ? div_up(in.rows, softsync::kNormRows) : in.rows;
+        kernel<<<static_cast<unsigned>(blocks), warps == 1 ? 32 * softsync::kNormRows : 32 * warps, 0, st>>>(in);
+        return launched();
+    };
+    if (units <= 32) return go(softsync::rms_norm_kernel<T, 1, 1>, 1);
+    if (units <= 64) return go(softsync::rms_norm_kernel<T, 1, 2>, 1);
+    if (units <= 128) return go(softsync::rms_norm_kernel<T, 1, 4>, 1);
+    if (units <= 256) return go(softsync::rms_norm_kernel<T, 4, 2>, 4);
+    if (units <= 512) return go(softsync::rms_norm_kernel<T, 4, 4>, 4);
+    if (units <= 1024) return go(softsync::rms_norm_kernel<T, 8, 4>, 8);
+    if (units <= 2048) return go(softsync::rms_norm_kernel<T, 16, 4>, 16);
+    softsync::rms_norm_long_kernel<T><<<static_cast<unsigned>(in.rows), softsync::kLongThreads, 0, st>>>(in);
+    return launched();
+}
+
+// Blocks of the backward pass, and with them the parts that the gain's gradient is summed in.
+constexpr int64_t kGradBlocks = 592, kLongParts = 64;
+struct GradShape { int warps, units; int64_t blocks, parts; };
+GradShape grad_shape(int64_t rows, int64_t cols)
+{
+    const int64_t units = div_up(cols, softsync::kUnit);
+    const auto of = [&](int warps, int per) {
+        const int64_t groups = warps == 1 ? softsync::kNormRows : 1, blocks = std::min(div_up(rows, groups), kGradBlocks);
+        return GradShape{warps, per, blocks, blocks * groups};
+    };
+    if (units <= 32) return of(1, 1);
+    if (units <= 64) return of(1, 2);
+    if (units <= 128) return of(1, 4);
+    if (units <= 256) return of(4, 2);
+    if (units <= 512) return of(8, 2);
+    if (units <= 1024) return of(16, 2);
+    if (units <= 2048) return of(16, 4);
+    return GradShape{0, 0, rows, std::min(rows, kLongParts)};
+}
+
+template <typename T>
+int launch_norm_grad(const NormGradIn &in, const GradShape &shape, cudaStream_t st)
+{
+    const auto go = [&](auto kernel) {
+        kernel<<<static_cast<unsigned>(shape.blocks), shape.warps == 1 ? 32 * softsync::kNormRows : 32 * shape.warps, 0, st>>>(in);
+        return launched();
+    };
+    switch (shape.warps * 8 + shape.units) {
+    case 1 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 1, 1>);
+    case 1 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 1, 2>);
+    case 1 * 8 + 4: return go(softsync::rms_norm_grad_kernel<T, 1, 4>);
+    case 4 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 4, 2>);
+    case 8 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 8, 2>);
+    case 16 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 16, 2>);
+    case 16 * 8 + 4: return go(softsync::rms_norm_grad_kernel<T, 16, 4>);
+    }
+    softsync::rms_norm_grad_long_kernel<T><<<static_cast<unsigned>(in.rows), softsync::kLongThreads, 0, st>>>(in);
+    int status = launched();
+    if (status != PS_OK || !in.parts) return status;
+    const dim3 grid(static_cast<unsigned>(div_up(div_up(in.cols, softsync::kUnit), 128)), static_cast<unsigned>(shape.parts));
+    softsync::gain_grad_long_kernel<T><<<grid, 128, 0, st>>>(in);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int ps_pack8(const void *x_dev, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int8_t *codes_dev, uint8_t *scales_dev, void *stream)
+{
+    if (!is_dtype(dtype) || !shape_ok(rows, cols)) return PS_ERR_INVALID_ARG;
+    if (rows == 0) return PS_OK;
+    if (!rows_ok(x_dev, dtype, rows, cols, row_stride) || !packed_ok(codes_dev, scales_dev)) return PS_ERR_INVALID_ARG;
+    const int64_t blocks = div_up(rows * (div_up(cols, PS_PACK_BLOCK) * (PS_PACK_BLOCK / softsync::kUnit)), softsync::kPackThreads * softsync::kPackTurns);
+    if (blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
+    const auto go = [&](auto *x) {
+        softsync::pack_kernel<<<static_cast<unsigned>(blocks), softsync::kPackThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+            x, rows, static_cast<int>(cols), row_stride, reinterpret_cast<uint2 *>(codes_dev), scales_dev, vectors_ok(x_dev, dtype, rows, row_stride));
+        return launched();
+    };
+    return dtype == PS_GRAD_BF16 ? go(static_cast<const bf16 *>(x_dev)) : go(static_cast<const float *>(x_dev));
+}
+
+int ps_unpack8(const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows, int64_t cols, void *out_dev, int dtype, int64_t row_stride, void *stream)
+{
+    if (!is_dtype(dtype) || !shape_ok(rows, cols)) return PS_ERR_INVALID_ARG;
+    if (rows == 0) return PS_OK;
+    if (!rows_ok(out_dev, dtype, rows, cols, row_stride) || !packed_ok(codes_dev, scales_dev)) return PS_ERR_INVALID_ARG;
+    const int64_t blocks = div_up(rows * (div_up(cols, PS_PACK_BLOCK) * (PS_PACK_BLOCK / softsync::kUnit)), softsync::kPackThreads * softsync::kPackTurns);
+    if (blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
+    const auto go = [&](auto *out) {
+        softsync::unpack_kernel<<<static_cast<unsigned>(blocks), softsync::kPackThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+            reinterpret_cast<const uint2 *>(codes_dev), scales_dev, rows, static_cast<int>(cols), out, row_stride, vectors_ok(out_dev, dtype, rows, row_stride));
+        return launched();
+    };
+    return dtype == PS_GRAD_BF16 ? go(static_cast<bf16 *>(out_dev)) : go(static_cast<float *>(out_dev));
+}
+
+int ps_rms_norm(const ps_norm *a, void *stream)
+{
+    if (!a || !is_dtype(a->dtype) || !shape_ok(a->rows, a->cols) || !(a->eps >= 0.f) || !std::isfinite(a->eps)) return PS_ERR_INVALID_ARG;
+    if (a->gain_dev && (!is_dtype(a->gain_dtype) || !aligned_to(a->gain_dev, size_of(a->gain_dtype)))) return PS_ERR_INVALID_ARG;
+    if (a->rows == 0) return PS_OK;
+    if (!rows_ok(a->x_dev, a->dtype, a->rows, a->cols, a->x_stride) || !a->rstd_dev || !aligned_to(a->rstd_dev, 4)) return PS_ERR_INVALID_ARG;
+    if (a->residual_dev && !rows_ok(a->residual_dev, a->dtype, a->rows, a->cols, a->residual_stride)) return PS_ERR_INVALID_ARG;
+    if (a->total_dev && !rows_ok(a->total_dev, a->dtype, a->rows, a->cols, a->total_stride)) return PS_ERR_INVALID_ARG;
+    if (a->total_dev && a->rows > 1 && ((a->total_dev == a->x_dev && a->total_stride != a->x_stride) ||
+                                        (a->total_dev == a->residual_dev && a->total_stride != a->residual_stride)))
+        return PS_ERR_INVALID_ARG;
+    if (a->out_dev && (!rows_ok(a->out_dev, a->dtype, a->rows, a->cols, a->cols) || a->out_dev == a->total_dev || a->out_dev == a->residual_dev ||
+                       (a->out_dev == a->x_dev && a->rows > 1 && a->x_stride != a->cols)))
+        return PS_ERR_INVALID_ARG;
+    if ((a->codes_dev || a->scales_dev) && !packed_ok(a->codes_dev, a->scales_dev)) return PS_ERR_INVALID_ARG;
+    NormIn in;
+    in.x = a->x_dev; in.residual = a->residual_dev; in.gain = a->gain_dev;
+    in.gain_bf16 = a->gain_dtype == PS_GRAD_BF16;
+    in.rows = a->rows; in.x_stride = a->x_stride; in.residual_stride = a->residual_stride; in.total_stride = a->total_stride;
+    in.cols = static_cast<int>(a->cols);
+    in.eps = a->eps;
+    in.total = a->total_dev; in.out = a->out_dev;
+    in.codes = reinterpret_cast<uint2 *>(a->codes_dev);
+    in.scales = a->scales_dev;
+    in.rstd = a->rstd_dev;
+    in.aligned = vectors_ok(a->x_dev, a->dtype, a->rows, a->x_stride) && vectors_ok(a->residual_dev, a->dtype, a->rows, a->residual_dev ? a->residual_stride : 0) &&
+                 vectors_ok(a->total_dev, a->dtype, a->rows, a->total_dev ? a->total_stride : 0) && vectors_ok(a->out_dev, a->dtype, a->rows, a->out_dev ? a->cols : 0) &&
+                 aligned_to(a->gain_dev, 16);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return a->dtype == PS_GRAD_BF16 ? launch_norm<bf16>(in, st) : launch_norm<float>(in, st);
+}
+
+int ps_norm_grad_workspace(int64_t rows, int64_t cols, int64_t *bytes)
+{
+    if (!bytes || !shape_ok(rows, cols)) return PS_ERR_INVALID_ARG;
+    *bytes = grad_shape(rows, cols).parts * cols * 4;
+    return PS_OK;
+}
+
+int ps_rms_norm_grad(const ps_norm_grad *a, void *workspace_dev, int64_t workspace_bytes, void *stream)
+{
+    if (!a || !is_dtype(a->dtype) || !shape_ok(a->rows, a->cols)) return PS_ERR_INVALID_ARG;
+    if ((a->gain_dev || a->dgain_dev) && (!is_dtype(a->gain_dtype) || !aligned_to(a->gain_dev, size_of(a->gain_dtype)) || !aligned_to(a->dgain_dev, size_of(a->gain_dtype))))
+        return PS_ERR_INVALID_ARG;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a->rows == 0)
+        return a->dgain_dev && cudaMemsetAsync(a->dgain_dev, 0, static_cast<size_t>(a->cols * size_of(a->gain_dtype)), st) != cudaSuccess ? PS_ERR_CUDA : PS_OK;
+    if (!rows_ok(a->dout_dev, a->dtype, a->rows, a->cols, a->dout_stride) || !rows_ok(a->dx_dev, a->dtype, a->rows, a->cols, a->cols)) return PS_ERR_INVALID_ARG;
+    if (!a->rstd_dev || !aligned_to(a->rstd_dev, 4)) return PS_ERR_INVALID_ARG;
+    if (a->dtotal_dev && !rows_ok(a->dtotal_dev, a->dtype, a->rows, a->cols, a->dtotal_stride)) return PS_ERR_INVALID_ARG;
+    if (a->codes_dev || a->scales_dev ? !packed_ok(a->codes_dev, a->scales_dev) || a->total_dev : !rows_ok(a->total_dev, a->dtype, a->rows, a->cols, a->total_stride))
+        return PS_ERR_INVALID_ARG;
+    if (a->rows > 1 && ((a->dx_dev == a->dout_dev && a->dout_stride != a->cols) || (a->dx_dev == a->dtotal_dev && a->dtotal_stride != a->cols))) return PS_ERR_INVALID_ARG;
+    const GradShape shape = grad_shape(a->rows, a->cols);
+    // rows beyond a block's registers: the gain's gradient reads dout again after dx is there
+    if (a->dx_dev == a->total_dev || (!shape.warps && a->dgain_dev && a->dx_dev == a->dout_dev)) return PS_ERR_INVALID_ARG;
+    if (a->dgain_dev && (!workspace_dev || !aligned_to(workspace_dev, 16) || workspace_bytes < shape.parts * a->cols * 4)) return PS_ERR_INVALID_ARG;
+    NormGradIn in;
+    in.dout = a->dout_dev; in.gain = a->gain_dev; in.dtotal = a->dtotal_dev; in.total = a->total_dev;
+    in.codes = reinterpret_cast<const uint2 *>(a->codes_dev);
+    in.scales = a->scales_dev;
+    in.rstd = a->rstd_dev;
+    in.dx = a->dx_dev;
+    in.parts = a->dgain_dev ? static_cast<float *>(workspace_dev) : nullptr;
+    in.gain_bf16 = a->gain_dtype == PS_GRAD_BF16;
+    in.rows = a->rows; in.dout_stride = a->dout_stride; in.dtotal_stride = a->dtotal_stride; in.total_stride = a->total_stride;
+    in.cols = static_cast<int>(a->cols);
+    in.aligned = vectors_ok(a->dout_dev, a->dtype, a->rows, a->dout_stride) && vectors_ok(a->dx_dev, a->dtype, a->rows, a->cols) &&
+                 vectors_ok(a->dtotal_dev, a->dtype, a->rows, a->dtotal_dev ? a->dtotal_stride : 0) && vectors_ok(a->total_dev, a->dtype, a->rows, a->total_dev ? a->total_stride : 0) &&
+                 aligned_to(a->gain_dev, 16);
+    const int status = a->dtype == PS_GRAD_BF16 ? launch_norm_grad<bf16>(in, shape, st) : launch_norm_grad<float>(in, shape, st);
+    if (status != PS_OK || !a->dgain_dev) return status;
+    softsync::gain_grad_kernel<<<static_cast<unsigned>(div_up(a->cols, 32)), 32 * softsync::kGainWarps, 0, st>>>(in.parts, static_cast<int>(shape.parts), in.cols, a->dgain_dev, in.gain_bf16);
+    return launched();
+}
+
+}  // extern "C"

@@ -19,6 +19,17 @@ decltype(&ps_loss_workspace) loss_workspace;
 decltype(&ps_token_logprob) call_token_logprob;
 decltype(&ps_policy_loss) call_policy_loss;
 decltype(&ps_preference_loss) call_preference_loss;
+decltype(&ps_head_workspace) head_workspace;
+decltype(&ps_head_logprob) call_head_logprob;
+decltype(&ps_head_logprob_grad) call_head_logprob_grad;
+decltype(&ps_head_cross_entropy) call_head_cross_entropy;
+decltype(&ps_pack8) call_pack8;
+decltype(&ps_unpack8) call_unpack8;
+decltype(&ps_rms_norm) call_rms_norm;
+decltype(&ps_norm_grad_workspace) norm_grad_workspace;
+decltype(&ps_rms_norm_grad) call_rms_norm_grad;
+decltype(&ps_packed_grad_workspace) packed_grad_workspace;
+decltype(&ps_packed_weight_grad) call_packed_weight_grad;
 
 const at::Tensor &tensor_of(PyObject *o, const char *what)
 {
@@ -138,20 +149,21 @@ PyObject *result(int status, std::initializer_list<at::Tensor> tensors)
 
 void expect(Py_ssize_t got, Py_ssize_t want) { TORCH_CHECK_TYPE(got == want, "expected ", want, " arguments, got ", got); }
 
-// (addresses of ps_loss_workspace, ps_token_logprob, ps_policy_loss, ps_preference_loss)
+// (addresses of the entry points, in the order of this list)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    expect(n, 4);
-    void *p[4];
-    for (int k = 0; k < 4; ++k) {
-        p[k] = PyLong_AsVoidPtr(a[k]);
-        if (!p[k]) throw python_error();
-    }
-    loss_workspace = reinterpret_cast<decltype(loss_workspace)>(p[0]);
-    call_token_logprob = reinterpret_cast<decltype(call_token_logprob)>(p[1]);
-    call_policy_loss = reinterpret_cast<decltype(call_policy_loss)>(p[2]);
-    call_preference_loss = reinterpret_cast<decltype(call_preference_loss)>(p[3]);
+    expect(n, 15);
+    Py_ssize_t k = 0;
+    const auto take = [&](auto &f) {
+        void *p = PyLong_AsVoidPtr(a[k++]);
+        if (!p) throw python_error();
+        f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(p);
+    };
+    take(loss_workspace); take(call_token_logprob); take(call_policy_loss); take(call_preference_loss);
+    take(head_workspace); take(call_head_logprob); take(call_head_logprob_grad); take(call_head_cross_entropy);
+    take(call_pack8); take(call_unpack8); take(call_rms_norm); take(norm_grad_workspace); take(call_rms_norm_grad);
+    take(packed_grad_workspace); take(call_packed_weight_grad);
     Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS
 }
@@ -276,10 +288,295 @@ PyObject *written(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- losses without logits, norm, activations in 8 bits ----------------------------------------------------------------------
+bool rows_fine(const at::Tensor &t) { return t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1); }
+int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.size(1), 1); }
+template <typename T> T *data(const at::Tensor &t) { return t.defined() ? static_cast<T *>(t.data_ptr()) : nullptr; }
+template <typename T> const T *const_data(const at::Tensor &t) { return t.defined() ? static_cast<const T *>(t.const_data_ptr()) : nullptr; }
+at::Tensor scratch(int64_t bytes, const at::Tensor &like) { return at::empty({std::max<int64_t>(bytes, 16)}, like.options().dtype(at::kByte)); }
+
+// Rows of activations on the GPU, fp32 or bf16.
+const at::Tensor &rows_of(PyObject *o, const char *what)
+{
+    const at::Tensor &t = tensor_of(o, what);
+    TORCH_CHECK_TYPE(grad_dtype(t.scalar_type()) >= 0, what, " must be fp32 or bf16, got ", t.scalar_type());
+    TORCH_CHECK_VALUE(rows_fine(t), what, " must be rows x columns with the columns contiguous");
+    TORCH_CHECK_VALUE(t.is_cuda(), what, " must live on the GPU");
+    return t;
+}
+// Rows of the same shape, type and GPU; undefined for None.
+at::Tensor rows_like(PyObject *o, const char *what, const at::Tensor &like)
+{
+    if (o == Py_None) return at::Tensor();
+    const at::Tensor &t = tensor_of(o, what);
+    TORCH_CHECK_TYPE(t.scalar_type() == like.scalar_type(), what, " must be ", like.scalar_type(), ", got ", t.scalar_type());
+    TORCH_CHECK_VALUE(rows_fine(t) && t.sizes() == like.sizes(), what, " must be ", like.size(0), " x ", like.size(1), " with the columns contiguous, got shape ", t.sizes(),
+                      " with strides ", t.strides());
+    TORCH_CHECK_VALUE(t.device() == like.device(), what, " is on ", t.device(), ", expected ", like.device());
+    return t;
+}
+// A factor for each column; undefined for None.
+at::Tensor gain_of(PyObject *o, int64_t cols, const at::Tensor &like)
+{
+    if (o == Py_None) return at::Tensor();
+    const at::Tensor &t = tensor_of(o, "gain");
+    TORCH_CHECK_TYPE(grad_dtype(t.scalar_type()) >= 0, "gain must be fp32 or bf16, got ", t.scalar_type());
+    TORCH_CHECK_VALUE(t.dim() == 1 && t.numel() == cols && t.is_contiguous(), "gain: ", cols, " values one behind the other, got shape ", t.sizes(), " with strides ", t.strides());
+    TORCH_CHECK_VALUE(t.device() == like.device(), "gain is on ", t.device(), ", expected ", like.device());
+    return t;
+}
+
+int64_t padded(int64_t cols) { return (cols + PS_PACK_BLOCK - 1) / PS_PACK_BLOCK * PS_PACK_BLOCK; }
+
+struct Packed {
+    at::Tensor codes, scales;
+    int64_t rows = 0, cols = 0;
+    Packed() = default;
+    Packed(int64_t r, int64_t c, const at::Tensor &like) : rows(r), cols(c)
+    {
+        codes = at::empty({r, padded(c)}, like.options().dtype(at::kChar));
+        scales = at::empty({r, padded(c) / PS_PACK_BLOCK}, like.options().dtype(at::kByte));
+    }
+    Packed(PyObject *codes_, PyObject *scales_, PyObject *cols_) : codes(tensor_of(codes_, "codes")), scales(tensor_of(scales_, "scales"))
+    {
+        cols = PyLong_AsLongLong(cols_);
+        if (cols == -1 && PyErr_Occurred()) throw python_error();
+        TORCH_CHECK_TYPE(codes.scalar_type() == at::kChar && scales.scalar_type() == at::kByte, "codes must be int8 and scales uint8, got ", codes.scalar_type(), " and ",
+                         scales.scalar_type());
+        TORCH_CHECK_VALUE(cols >= 1 && codes.dim() == 2 && codes.is_contiguous() && codes.size(1) == padded(cols), "codes of ", cols, " columns must be rows x ", padded(cols),
+                          ", contiguous, got shape ", codes.sizes(), " with strides ", codes.strides());
+        rows = codes.size(0);
+        TORCH_CHECK_VALUE(scales.dim() == 2 && scales.is_contiguous() && scales.size(0) == rows && scales.size(1) == padded(cols) / PS_PACK_BLOCK, "scales must be ", rows, " x ",
+                          padded(cols) / PS_PACK_BLOCK, ", contiguous, got shape ", scales.sizes(), " with strides ", scales.strides());
+        TORCH_CHECK_VALUE(codes.is_cuda() && codes.device() == scales.device(), "codes and scales must live on one GPU, got ", codes.device(), " and ", scales.device());
+    }
+};
+
+struct Head {
+    const at::Tensor &hidden, &head;
+    ps_head c;
+    Head(PyObject *hidden_, PyObject *head_, PyObject *tokens, PyObject *temperature) : hidden(tensor_of(hidden_, "hidden")), head(tensor_of(head_, "head"))
+    {
+        TORCH_CHECK_TYPE(hidden.scalar_type() == at::kBFloat16 && head.scalar_type() == at::kBFloat16, "hidden and head must be bf16, got ", hidden.scalar_type(), " and ",
+                         head.scalar_type());
+        TORCH_CHECK_VALUE(rows_fine(hidden) && rows_fine(head), "hidden must be rows x width and head vocabulary x width, with the width contiguous");
+        TORCH_CHECK_VALUE(hidden.size(1) == head.size(1), "hidden has width ", hidden.size(1), ", head ", head.size(1));
+        TORCH_CHECK_VALUE(hidden.is_cuda() && hidden.device() == head.device(), "hidden and head must live on one GPU, got ", hidden.device(), " and ", head.device());
+        c.hidden_dev = hidden.const_data_ptr();
+        c.head_dev = head.const_data_ptr();
+        c.rows = hidden.size(0);
+        c.width = hidden.size(1);
+        c.vocab = head.size(0);
+        c.hidden_stride = row_stride(hidden);
+        c.head_stride = row_stride(head);
+        c.tokens_dev = per_row<int64_t>(tokens, c.rows, "tokens", hidden);
+        c.temperature = static_cast<float>(number(temperature));
+    }
+    at::Tensor floats(int64_t n) const { return at::empty({n}, hidden.options().dtype(at::kFloat)); }
+    at::Tensor workspace(bool grad) const
+    {
+        int64_t need = 0;
+        TORCH_CHECK_VALUE(head_workspace(&c, grad, &need) == PS_OK, "no such call: ", c.rows, " rows of width ", c.width, " (strides ", c.hidden_stride, ", ", c.head_stride, "), ", c.vocab,
+                          " entries, temperature ", c.temperature);
+        return scratch(need, hidden);
+    }
+};
+
+// Which gradients: True, False or None, "hidden", "head".
+struct Wanted {
+    bool hidden = false, head = false;
+    explicit Wanted(PyObject *o)
+    {
+        if (o == Py_False || o == Py_None) return;
+        if (o == Py_True) { hidden = head = true; return; }
+        TORCH_CHECK_VALUE(PyUnicode_Check(o), "grad is True, False, 'hidden' or 'head'");
+        hidden = PyUnicode_CompareWithASCIIString(o, "hidden") == 0;
+        head = PyUnicode_CompareWithASCIIString(o, "head") == 0;
+        TORCH_CHECK_VALUE(hidden || head, "grad is True, False, 'hidden' or 'head'");
+    }
+    at::Tensor of_hidden(const Head &h) const { return hidden ? at::empty({h.c.rows, h.c.width}, h.hidden.options()) : at::Tensor(); }
+    at::Tensor of_head(const Head &h) const { return head ? at::empty({h.c.vocab, h.c.width}, h.head.options()) : at::Tensor(); }
+};
+
+// (hidden, head, tokens, weights, temperature) -> (status, logp, lse)
+PyObject *head_logprob(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 5);
+    const Head h(a[0], a[1], a[2], a[4]);
+    const float *weights = per_row<float>(a[3], h.c.rows, "weights", h.hidden, true);
+    const c10::cuda::CUDAGuard guard(h.hidden.device());
+    const at::Tensor logp = h.floats(h.c.rows), lse = h.floats(h.c.rows), ws = h.workspace(false);
+    const int status = call_head_logprob(&h.c, weights, data<float>(logp), data<float>(lse), ws.data_ptr(), ws.numel(), c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {logp, lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// (hidden, head, tokens, lse, dlogp, temperature, grad) -> (status, dhidden, dhead)
+PyObject *head_logprob_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 7);
+    const Head h(a[0], a[1], a[2], a[5]);
+    const float *lse = per_row<float>(a[3], h.c.rows, "lse", h.hidden), *dlogp = per_row<float>(a[4], h.c.rows, "dlogp", h.hidden);
+    const Wanted want(a[6]);
+    const c10::cuda::CUDAGuard guard(h.hidden.device());
+    const at::Tensor dhidden = want.of_hidden(h), dhead = want.of_head(h), ws = h.workspace(true);
+    const int status = call_head_logprob_grad(&h.c, lse, dlogp, data<void>(dhidden), data<void>(dhead), ws.data_ptr(), ws.numel(), c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {dhidden, dhead});
+    END_HANDLE_TH_ERRORS
+}
+
+// (hidden, head, tokens, weights, temperature, grad) -> (status, stats, logp, lse, dhidden, dhead)
+PyObject *head_cross_entropy(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 6);
+    const Head h(a[0], a[1], a[2], a[4]);
+    const float *weights = per_row<float>(a[3], h.c.rows, "weights", h.hidden, true);
+    const Wanted want(a[5]);
+    const c10::cuda::CUDAGuard guard(h.hidden.device());
+    const at::Tensor stats = h.floats(2), logp = h.floats(h.c.rows), lse = h.floats(h.c.rows), dhidden = want.of_hidden(h), dhead = want.of_head(h),
+                     ws = h.workspace(want.hidden || want.head);
+    const int status = call_head_cross_entropy(&h.c, weights, data<float>(stats), data<float>(logp), data<float>(lse), data<void>(dhidden), data<void>(dhead), ws.data_ptr(), ws.numel(),
+                                               c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {stats, logp, lse, dhidden, dhead});
+    END_HANDLE_TH_ERRORS
+}
+
+// (x) -> (status, codes, scales)
+PyObject *pack8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 1);
+    const at::Tensor &x = rows_of(a[0], "x");
+    const c10::cuda::CUDAGuard guard(x.device());
+    const Packed p(x.size(0), x.size(1), x);
+    const int status = call_pack8(x.const_data_ptr(), grad_dtype(x.scalar_type()), p.rows, p.cols, row_stride(x), data<int8_t>(p.codes), data<uint8_t>(p.scales),
+                                  c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {p.codes, p.scales});
+    END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, cols, whether bf16) -> (status, values)
+PyObject *unpack8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 4);
+    const Packed p(a[0], a[1], a[2]);
+    const c10::cuda::CUDAGuard guard(p.codes.device());
+    const bool half = a[3] == Py_True;
+    const at::Tensor out = at::empty({p.rows, p.cols}, p.codes.options().dtype(half ? at::kBFloat16 : at::kFloat));
+    const int status = call_unpack8(const_data<int8_t>(p.codes), const_data<uint8_t>(p.scales), p.rows, p.cols, out.data_ptr(), half ? PS_GRAD_BF16 : PS_GRAD_FP32, p.cols,
+                                    c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {out});
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, gain, residual, eps, whether out, whether codes, whether the total replaces the residual) -> (status, out, total, codes, scales, rstd)
+PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 7);
+    const at::Tensor &x = rows_of(a[0], "x");
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const at::Tensor gain = gain_of(a[1], cols, x), residual = rows_like(a[2], "residual", x);
+    const bool want_out = a[4] == Py_True, want_codes = a[5] == Py_True, inplace = a[6] == Py_True;
+    TORCH_CHECK_VALUE(!inplace || residual.defined(), "inplace needs a residual to replace");
+    const c10::cuda::CUDAGuard guard(x.device());
+    ps_norm c{};
+    c.eps = static_cast<float>(number(a[3]));
+    at::Tensor total = residual.defined() ? inplace ? residual : at::empty({rows, cols}, x.options()) : at::Tensor(), out;
+    if (want_out) out = at::empty({rows, cols}, x.options());
+    const Packed p = want_codes ? Packed(rows, cols, x) : Packed();
+    const at::Tensor rstd = at::empty({rows}, x.options().dtype(at::kFloat));
+    c.x_dev = x.const_data_ptr(); c.residual_dev = const_data<void>(residual); c.gain_dev = const_data<void>(gain);
+    c.dtype = grad_dtype(x.scalar_type());
+    c.gain_dtype = gain.defined() ? grad_dtype(gain.scalar_type()) : c.dtype;
+    c.rows = rows; c.cols = cols; c.x_stride = row_stride(x);
+    c.residual_stride = residual.defined() ? row_stride(residual) : cols;
+    c.total_stride = total.defined() ? row_stride(total) : cols;
+    c.total_dev = data<void>(total); c.out_dev = data<void>(out);
+    c.codes_dev = data<int8_t>(p.codes); c.scales_dev = data<uint8_t>(p.scales); c.rstd_dev = data<float>(rstd);
+    const int status = call_rms_norm(&c, c10::cuda::getCurrentCUDAStream().stream());
+    if (inplace && status == PS_OK) changed(residual);
+    return result(status, {out, total, p.codes, p.scales, rstd});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dout, codes or total, scales or None, rstd, gain, dtotal, whether the gain's gradient) -> (status, dx, dgain)
+PyObject *rms_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 7);
+    const at::Tensor &dout = rows_of(a[0], "dout");
+    const int64_t rows = dout.size(0), cols = dout.size(1);
+    Packed p;
+    at::Tensor total;
+    if (a[2] != Py_None) {
+        PyObject *wanted = PyLong_FromLongLong(cols);
+        if (!wanted) throw python_error();
+        const struct Drop { PyObject *o; ~Drop() { Py_DECREF(o); } } drop{wanted};
+        p = Packed(a[1], a[2], wanted);
+        TORCH_CHECK_VALUE(p.rows == rows && p.codes.device() == dout.device(), "codes of ", p.rows, " rows on ", p.codes.device(), ", dout has ", rows, " on ", dout.device());
+    } else {
+        total = rows_like(a[1], "total", dout);
+        TORCH_CHECK_TYPE(total.defined(), "what the norm kept: a Packed8 or the total");
+    }
+    const float *rstd = per_row<float>(a[3], rows, "rstd", dout);
+    const at::Tensor gain = gain_of(a[4], cols, dout), dtotal = rows_like(a[5], "dtotal", dout);
+    const bool want_gain = a[6] == Py_True && gain.defined();
+    const c10::cuda::CUDAGuard guard(dout.device());
+    const at::Tensor dx = at::empty({rows, cols}, dout.options()), dgain = want_gain ? at::empty({cols}, gain.options()) : at::Tensor();
+    int64_t need = 0;
+    TORCH_CHECK_VALUE(norm_grad_workspace(rows, cols, &need) == PS_OK, "too many rows or columns, or none: ", rows, " x ", cols);
+    const at::Tensor ws = scratch(want_gain ? need : 0, dout);
+    ps_norm_grad c{};
+    c.dout_dev = dout.const_data_ptr(); c.total_dev = const_data<void>(total); c.gain_dev = const_data<void>(gain); c.dtotal_dev = const_data<void>(dtotal);
+    c.codes_dev = const_data<int8_t>(p.codes); c.scales_dev = const_data<uint8_t>(p.scales); c.rstd_dev = rstd;
+    c.dtype = grad_dtype(dout.scalar_type());
+    c.gain_dtype = gain.defined() ? grad_dtype(gain.scalar_type()) : c.dtype;
+    c.rows = rows; c.cols = cols; c.dout_stride = row_stride(dout);
+    c.total_stride = total.defined() ? row_stride(total) : cols;
+    c.dtotal_stride = dtotal.defined() ? row_stride(dtotal) : cols;
+    c.dx_dev = dx.data_ptr(); c.dgain_dev = data<void>(dgain);
+    const int status = call_rms_norm_grad(&c, ws.data_ptr(), ws.numel(), c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {dx, dgain});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dout, codes, scales, cols, gain, whether fp32) -> (status, dweight)
+PyObject *packed_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    expect(n, 6);
+    const at::Tensor &dout = rows_of(a[0], "dout");
+    TORCH_CHECK_TYPE(dout.scalar_type() == at::kBFloat16, "dout must be bf16, got ", dout.scalar_type());
+    const Packed p(a[1], a[2], a[3]);
+    TORCH_CHECK_VALUE(p.rows == dout.size(0) && p.codes.device() == dout.device(), "codes of ", p.rows, " rows on ", p.codes.device(), ", dout has ", dout.size(0), " on ", dout.device());
+    const at::Tensor gain = gain_of(a[4], p.cols, dout);
+    const bool wide = a[5] == Py_True;
+    const c10::cuda::CUDAGuard guard(dout.device());
+    const at::Tensor dweight = at::empty({dout.size(1), p.cols}, dout.options().dtype(wide ? at::kFloat : at::kBFloat16));
+    ps_packed_grad c{};
+    c.dout_dev = dout.const_data_ptr(); c.gain_dev = const_data<void>(gain); c.codes_dev = const_data<int8_t>(p.codes); c.scales_dev = const_data<uint8_t>(p.scales);
+    c.gain_dtype = gain.defined() ? grad_dtype(gain.scalar_type()) : PS_GRAD_FP32;
+    c.out_dtype = wide ? PS_GRAD_FP32 : PS_GRAD_BF16;
+    c.rows = p.rows; c.outs = dout.size(1); c.cols = p.cols; c.dout_stride = row_stride(dout);
+    c.dweight_dev = dweight.data_ptr();
+    int64_t need = 0;
+    TORCH_CHECK_VALUE(packed_grad_workspace(&c, &need) == PS_OK, "no such product: ", c.rows, " rows of ", c.outs, " (stride ", c.dout_stride, ") and ", c.cols);
+    const at::Tensor ws = scratch(need, dout);
+    const int status = call_packed_weight_grad(&c, ws.data_ptr(), ws.numel(), c10::cuda::getCurrentCUDAStream().stream());
+    return result(status, {dweight});
+    END_HANDLE_TH_ERRORS
+}
+
 #define SOFTSYNC_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     SOFTSYNC_FAST(bind), SOFTSYNC_FAST(token_logprob), SOFTSYNC_FAST(policy_loss), SOFTSYNC_FAST(preference_loss), SOFTSYNC_FAST(gradients),
-    SOFTSYNC_FAST(written),
+    SOFTSYNC_FAST(written), SOFTSYNC_FAST(head_logprob), SOFTSYNC_FAST(head_logprob_grad), SOFTSYNC_FAST(head_cross_entropy), SOFTSYNC_FAST(pack8),
+    SOFTSYNC_FAST(unpack8), SOFTSYNC_FAST(rms_norm), SOFTSYNC_FAST(rms_norm_grad), SOFTSYNC_FAST(packed_weight_grad),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

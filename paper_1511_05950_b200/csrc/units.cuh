@@ -1,0 +1,174 @@
+// Units of eight elements of a row: one or two 16-byte vectors of activations (bf16 or fp32), one 8-byte vector of codes; four neighbouring
+// lanes hold the 32 columns that share a scale.  A unit whose address or length does not allow vectors is taken element by element.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace softsync {
+
+constexpr int kUnit = 8;                  // elements
+constexpr int kPackBlock = 32;            // columns that share a scale
+constexpr unsigned kAllLanes = 0xffffffffu;
+
+// ---- eight elements ----------------------------------------------------------------------------------------------------
+struct Unit { float v[kUnit]; };
+
+__device__ __forceinline__ float unit_value(const float *p) { return *p; }
+__device__ __forceinline__ float unit_value(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+
+__device__ __forceinline__ uint4 load_stream16(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+    return r;
+}
+
+// A unit as it lies in memory, so that loads are under way before anything is computed.
+template <typename T> struct RawUnit;
+template <> struct RawUnit<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const void *p) { a = load_stream16(p); }
+    __device__ __forceinline__ Unit values() const
+    {
+        Unit u;
+        const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { u.v[2 * k] = __uint_as_float(w[k] << 16); u.v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+        return u;
+    }
+};
+template <> struct RawUnit<float> {
+    uint4 a, b;
+    __device__ __forceinline__ void load(const void *p) { a = load_stream16(p); b = load_stream16(static_cast<const char *>(p) + 16); }
+    __device__ __forceinline__ Unit values() const
+    {
+        return Unit{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                     __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)}};
+    }
+};
+
+__device__ __forceinline__ unsigned bf16_pair(float lo, float hi)
+{
+    unsigned r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Elements [0, n) of a unit (n <= 8; zeros beyond); whole: all eight, from an address that allows vectors.
+template <typename T>
+__device__ __forceinline__ void load_unit(RawUnit<T> &raw, const T *p, int n, bool whole)
+{
+    if (whole) {
+        raw.load(p);
+        return;
+    }
+    T part[kUnit];
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) part[k] = k < n ? p[k] : T(0.f);
+    unsigned *w = reinterpret_cast<unsigned *>(&raw);
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __bfloat16_as_ushort(part[2 * k]) | static_cast<unsigned>(__bfloat16_as_ushort(part[2 * k + 1])) << 16;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(part[k]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_unit(T *p, const Unit &u, int n, bool whole)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (whole) {
+            *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(u.v[0], u.v[1]), bf16_pair(u.v[2], u.v[3]), bf16_pair(u.v[4], u.v[5]), bf16_pair(u.v[6], u.v[7]));
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) if (k < n) p[k] = __float2bfloat16_rn(u.v[k]);
+    } else {
+        if (whole) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(u.v[0], u.v[1], u.v[2], u.v[3]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(u.v[4], u.v[5], u.v[6], u.v[7]);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) if (k < n) p[k] = u.v[k];
+    }
+}
+
+template <typename T> __device__ __forceinline__ float rounded(float x);
+template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
+template <> __device__ __forceinline__ float rounded<__nv_bfloat16>(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
+
+// ---- 8 bits with a scale -----------------------------------------------------------------------------------------------
+// The byte s of a block stands for the unit 2^(s - 127) = 2^(floor(log2 max|x|) - 6), at least 2^-126; 255 for a block with an infinity or a
+// NaN, whose codes are zero and whose values are NaN (zero times infinity).  Taken from the bits, so there is no rounding but the code's own.
+__device__ __forceinline__ unsigned block_scale(unsigned max_bits)
+{
+    const unsigned e = max_bits >> 23;
+    return e == 255u ? 255u : e > 7u ? e - 6u : 1u;
+}
+__device__ __forceinline__ float scale_unit(unsigned s) { return __uint_as_float(s << 23); }
+
+// Eight codes from the eight values of this lane; the four lanes of a block have to call it together.
+__device__ __forceinline__ uint2 pack_unit(const Unit &u, unsigned &scale)
+{
+    unsigned m = 0;
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) m = max(m, __float_as_uint(u.v[k]) & 0x7fffffffu);
+    m = max(m, __shfl_xor_sync(kAllLanes, m, 1));
+    m = max(m, __shfl_xor_sync(kAllLanes, m, 2));
+    scale = block_scale(m);
+    // x / unit + 1.5 * 2^23 rounds to nearest, ties to even: |x| / unit is below 128, so the code is in the sum's low byte
+    const float inv = scale == 255u ? 0.f : __uint_as_float((254u - scale) << 23);
+    unsigned b[kUnit];
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) {
+        const float x = scale == 255u ? 0.f : fminf(fmaxf(u.v[k] * inv, -127.f), 127.f);
+        b[k] = __float_as_uint(x + 12582912.f);
+    }
+    return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+}
+
+// The values of eight codes: exact (a code has 7 bits and the unit is a power of two).
+__device__ __forceinline__ Unit unpack_unit(uint2 codes, unsigned scale)
+{
+    const float unit = scale_unit(scale);
+    Unit u;
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) {
+        const unsigned w = k < 4 ? codes.x : codes.y;
+        u.v[k] = static_cast<float>(static_cast<int>(w << (24 - 8 * (k & 3))) >> 24) * unit;
+    }
+    return u;
+}
+
+__device__ __forceinline__ Unit load_gain(const void *gain, int is_bf16, int col, int n, bool whole)
+{
+    if (!gain) return Unit{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
+    Unit u;
+    if (is_bf16) {
+        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(gain) + col;
+        if (whole) {
+            RawUnit<__nv_bfloat16> raw;
+            raw.a = __ldg(reinterpret_cast<const uint4 *>(p));
+            return raw.values();
+        }
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) u.v[k] = k < n ? unit_value(p + k) : 0.f;
+    } else {
+        const float *p = static_cast<const float *>(gain) + col;
+        if (whole) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+            return Unit{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+        }
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) u.v[k] = k < n ? p[k] : 0.f;
+    }
+    return u;
+}
+
+}  // namespace softsync

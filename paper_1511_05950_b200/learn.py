@@ -20,7 +20,10 @@ if not os.path.exists(_build.MARSHAL):
     raise RuntimeError("_marshal.so is not built (%s). Run `python -m paper_1511_05950_b200.build`." % _build.MARSHAL)
 from . import _marshal  # noqa: E402
 
-_marshal.bind(*[C.cast(f, C.c_void_p).value for f in (B.ps_loss_workspace, B.ps_token_logprob, B.ps_policy_loss, B.ps_preference_loss)])
+_marshal.bind(*[C.cast(f, C.c_void_p).value for f in (
+    B.ps_loss_workspace, B.ps_token_logprob, B.ps_policy_loss, B.ps_preference_loss, B.ps_head_workspace, B.ps_head_logprob, B.ps_head_logprob_grad,
+    B.ps_head_cross_entropy, B.ps_pack8, B.ps_unpack8, B.ps_rms_norm, B.ps_norm_grad_workspace, B.ps_rms_norm_grad, B.ps_packed_grad_workspace,
+    B.ps_packed_weight_grad)])
 INPLACE = "inplace"
 
 
@@ -251,6 +254,168 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.T
     status, *out = _marshal.preference_loss(logits, tokens, weights, temperature, offsets, ref_logp, beta, label_smoothing, grad)
     B._check(status, "ps_preference_loss")
     return PreferenceLoss(*out)
+
+
+# ---- losses without logits ----------------------------------------------------------------------------------------------
+
+class HeadLogprob(NamedTuple):
+    logp: torch.Tensor
+    lse: torch.Tensor
+
+
+class HeadGrad(NamedTuple):
+    dhidden: Optional[torch.Tensor]
+    dhead: Optional[torch.Tensor]
+
+
+class HeadCrossEntropy(NamedTuple):
+    stats: torch.Tensor                  # loss, sum of the weights
+    logp: torch.Tensor
+    lse: torch.Tensor
+    dhidden: Optional[torch.Tensor]
+    dhead: Optional[torch.Tensor]
+
+
+def head_logprob(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                 temperature: float = 1.0) -> HeadLogprob:
+    """Log probability of each row's token and log normaliser, from hidden states (rows x width) and the output matrix (vocabulary x width), both
+    bf16, without the logits ever being in memory.  Rows of weight zero are not read and give zeros."""
+    status, *out = _marshal.head_logprob(hidden, head, tokens, weights, temperature)
+    B._check(status, "ps_head_logprob")
+    return HeadLogprob(*out)
+
+
+def head_logprob_grad(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor,
+                      temperature: float = 1.0, grad: Union[bool, str] = True) -> HeadGrad:
+    """The gradients of any loss of `head_logprob`'s log probabilities, from dlogp (the loss's gradient with respect to them, fp32) and lse.  Rows
+    with a dlogp of zero are not read.  grad: True (both), "hidden" or "head"."""
+    status, *out = _marshal.head_logprob_grad(hidden, head, tokens, lse, dlogp, temperature, grad)
+    B._check(status, "ps_head_logprob_grad")
+    return HeadGrad(*out)
+
+
+def head_cross_entropy(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                       temperature: float = 1.0, grad: Union[bool, str] = True) -> HeadCrossEntropy:
+    """The cross entropy -sum w logp / sum w of the tokens and its gradients with respect to the hidden states and the output matrix (formulas:
+    include/softsync_learn.h): `hidden.backward(result.dhidden)` continues into the model.  Rows of weight zero are not read.  grad: True, "hidden",
+    "head" or False."""
+    status, *out = _marshal.head_cross_entropy(hidden, head, tokens, weights, temperature, grad)
+    B._check(status, "ps_head_cross_entropy")
+    return HeadCrossEntropy(*out)
+
+
+# ---- activations in 8 bits, and the norm that makes them ------------------------------------------------------------------
+
+class Packed8(NamedTuple):
+    """Activations in 8 bits (form: include/softsync_learn.h): int8 codes (rows x columns rounded up to PS_PACK_BLOCK), one byte for each PS_PACK_BLOCK codes, and the
+    number of columns."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+
+
+class RmsNorm(NamedTuple):
+    out: Optional[torch.Tensor]
+    total: torch.Tensor
+    packed: Optional[Packed8]
+    rstd: torch.Tensor
+
+
+class RmsNormGrad(NamedTuple):
+    dx: torch.Tensor
+    dgain: Optional[torch.Tensor]
+
+
+def pack8(x: torch.Tensor) -> Packed8:
+    """Rows of activations (fp32 or bf16) in 8 bits: 32 columns share a power of two, each value is off by at most 1/128 of the largest's power of
+    two (1/64 where it would round past the last code)."""
+    status, codes, scales = _marshal.pack8(x)
+    B._check(status, "ps_pack8")
+    return Packed8(codes, scales, x.shape[1])
+
+
+def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The values that the codes stand for, exactly, in bf16 or fp32."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("values are bf16 or fp32, not %s" % dtype)
+    status, out = _marshal.unpack8(*packed, dtype == torch.bfloat16)
+    B._check(status, "ps_unpack8")
+    return out
+
+
+def rms_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, out: bool = True,
+             pack: bool = False, inplace: bool = False) -> RmsNorm:
+    """total = x + residual, n = total / sqrt(mean(total^2) + eps), out = n * gain, row by row in one pass.  pack: n (before the gain) in 8 bits too,
+    which is what `rms_norm_grad` and `packed_weight_grad` take: nothing else of the activations need be kept for the backward pass.  inplace: the total replaces
+    the residual."""
+    status, y, total, codes, scales, rstd = _marshal.rms_norm(x, gain, residual, eps, bool(out), bool(pack), bool(inplace))
+    B._check(status, "ps_rms_norm")
+    return RmsNorm(y, x if total is None else total, Packed8(codes, scales, x.shape[1]) if pack else None, rstd)
+
+
+def rms_norm_grad(dout: torch.Tensor, kept: Union[Packed8, torch.Tensor], rstd: torch.Tensor, gain: Optional[torch.Tensor] = None,
+                  dtotal: Optional[torch.Tensor] = None, grad_gain: bool = True) -> RmsNormGrad:
+    """The norm's backward pass from what it kept (`packed`, or `total`).  dx is the gradient of x and of the residual; dtotal: what comes back to
+    the total by other ways."""
+    if isinstance(kept, torch.Tensor):
+        a, b = kept, None
+    else:
+        a, b, cols = kept
+        if dout.dim() != 2 or dout.shape[1] != cols:
+            raise ValueError("dout has shape %s, what was kept %d columns" % (tuple(dout.shape), cols))
+    status, dx, dgain = _marshal.rms_norm_grad(dout, a, b, rstd, gain, dtotal, bool(grad_gain))
+    B._check(status, "ps_rms_norm_grad")
+    return RmsNormGrad(dx, dgain)
+
+
+def packed_weight_grad(dout: torch.Tensor, packed: Packed8, gain: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """dout^T (n * gain): the gradient of a weight matrix (outputs x columns) whose input was n * gain, with n kept in 8 bits.  dout: bf16, rows x
+    outputs.  dtype: of the result, bf16 or fp32."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("the gradient is bf16 or fp32, not %s" % dtype)
+    status, dweight = _marshal.packed_weight_grad(dout, *packed, gain, dtype == torch.float32)
+    B._check(status, "ps_packed_weight_grad")
+    return dweight
+
+
+class _NormLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gain, weight, residual, eps):
+        ctx.set_materialize_grads(False)
+        r = rms_norm(x, gain, residual, eps, pack=True)
+        ctx.save_for_backward(*r.packed[:2], r.rstd, gain, weight)
+        return r.out @ weight.T, r.total
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dz, dtotal):
+        codes, scales, rstd, gain, weight = ctx.saved_tensors
+        needs_x, needs_gain, needs_weight, needs_residual, _ = ctx.needs_input_grad
+        if dz is None:
+            return (dtotal if needs_x else None), None, None, (dtotal if needs_residual else None), None
+        dz, dtotal = dz.contiguous(), None if dtotal is None else dtotal.contiguous()
+        packed = Packed8(codes, scales, weight.shape[1])
+        dx = dgain = None
+        if needs_x or needs_gain or needs_residual:
+            dx, dgain = rms_norm_grad(dz @ weight, packed, rstd, gain, dtotal, needs_gain)
+        dweight = packed_weight_grad(dz, packed, gain) if needs_weight else None
+        return (dx if needs_x else None), dgain, dweight, (dx if needs_residual else None), None
+
+
+def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
+    """(z, total) with total = x + residual and z = (n * gain) @ weight.T (`rms_norm`, then a linear layer; all bf16, x and residual with
+    any leading dimensions), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
+    input would take 4.  The gradients are those of the kept values; z and total are not touched by the 8 bits."""
+    for t, what in ((x, "x"), (weight, "weight"), *(((residual, "residual"),) if residual is not None else ())):
+        if t.dtype != torch.bfloat16:
+            raise TypeError("%s must be bf16, got %s" % (what, t.dtype))
+    if weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
+        raise ValueError("x has width %d, weight shape %s" % (x.shape[-1], tuple(weight.shape)))
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError("residual has shape %s, x %s" % (tuple(residual.shape), tuple(x.shape)))
+    rows = x.reshape(-1, x.shape[-1])
+    z, total = _NormLinear.apply(rows, gain, weight, None if residual is None else residual.reshape(rows.shape), eps)
+    return z.view(*x.shape[:-1], weight.shape[0]), total.view(x.shape)
 
 
 # ---- an n-softsync server whose update is an AdamW step -------------------------------------------------------------------
