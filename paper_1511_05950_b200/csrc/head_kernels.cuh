@@ -17,6 +17,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
 {
     __shared__ int counts[32];
     __shared__ double sums[32];
+    let_next_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int base = 0;
     double sum = 0;
@@ -69,23 +70,38 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
 }
 
 // Rows of a matrix one behind the other in 16-byte vectors, padded with zeros: all of them, or the listed ones, and zero rows up to a whole stage of
-// a product's contraction.  A block a row.
-__global__ void __launch_bounds__(128) gather_kernel(const __nv_bfloat16 *x, int rows, int width, long long stride, const int *order, const int *live, int aligned,
-                                                     __nv_bfloat16 *out, int out_stride)
+// a product's contraction.  A block a row; `zeros`: where a row without a place is set to zero.
+struct GatherIn {
+    const __nv_bfloat16 *x;
+    int rows, width;
+    long long stride;
+    const int *order, *place, *live;       // may be null
+    int aligned;
+    __nv_bfloat16 *out;
+    int out_stride;
+    __nv_bfloat16 *zeros;                  // may be null; dense rows
+};
+__global__ void __launch_bounds__(128) gather_kernel(const __grid_constant__ GatherIn in)
 {
-    const int row = blockIdx.x, count = live ? *live : rows;
+    wait_for_earlier();
+    let_next_start();
+    const int row = blockIdx.x, count = in.live ? *in.live : in.rows;
+    if (in.zeros && row < in.rows && in.place[row] < 0)
+        for (int col = threadIdx.x * kUnit; col < in.width; col += 128 * kUnit)
+            store_unit(in.zeros + static_cast<long long>(row) * in.width + col, Unit{}, in.width - col, in.width % kUnit == 0);
     if (row >= (count + kStep - 1) / kStep * kStep) return;
-    const __nv_bfloat16 *from = x + (row < count ? (order ? order[row] : row) * stride : 0);
-    for (int col = threadIdx.x * kUnit; col < out_stride; col += 128 * kUnit) {
-        const int left = row < count ? width - col : 0;
+    const __nv_bfloat16 *from = in.x + (row < count ? (in.order ? in.order[row] : row) * in.stride : 0);
+    for (int col = threadIdx.x * kUnit; col < in.out_stride; col += 128 * kUnit) {
+        const int left = row < count ? in.width - col : 0;
         RawUnit<__nv_bfloat16> raw;
-        load_unit(raw, from + (left > 0 ? col : 0), left, aligned && left >= kUnit);
-        *reinterpret_cast<uint4 *>(out + static_cast<long long>(row) * out_stride + col) = raw.a;
+        load_unit(raw, from + (left > 0 ? col : 0), left, in.aligned && left >= kUnit);
+        *reinterpret_cast<uint4 *>(in.out + static_cast<long long>(row) * in.out_stride + col) = raw.a;
     }
 }
 
-// A row's parts joined: lse and log probability; and the block's share of sum w logp.  32 rows a block, the warps share the parts.
-constexpr int kJoinWarps = 16;
+// A row's parts joined: normaliser, lse, log probability; and, by the last block, the loss.  Eight rows a block, 64 threads share a row's parts (152000
+// entries: 1188 parts).  Bound by latency: two loads' worth of waiting and a short tree.
+constexpr int kJoinRows = 8, kJoinThreads = 512;
 struct JoinIn {
     const float2 *parts;
     long long part_stride;
@@ -97,101 +113,144 @@ struct JoinIn {
     int rows, vocab;
     float scale, inv_temperature;          // log2(e) / T, 1 / T
     float *logp, *lse;
-    double *sums;                          // one for each block, or null
+    float2 *norms;
+    double *sums;                          // sum w logp of each block
+    unsigned *done;
+    const float *total;                    // sum of the weights, or null: rows
+    float *stats;                          // loss and sum of the weights, or null
 };
-__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_constant__ JoinIn in)
+__device__ __forceinline__ float2 join_parts(float2 a, float2 b, float scale)
 {
-    __shared__ float2 found[kJoinWarps][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = static_cast<int>(blockIdx.x) * 32 + lane, count = in.live ? *in.live : in.rows;
-    const auto join = [&](float2 a, float2 b) {
-        const float m = fmaxf(a.x, b.x);
-        if (m == -CUDART_INF_F) return make_float2(m, a.y + b.y);           // both empty, or NaN
-        return make_float2(m, a.y * mma_ex2((a.x - m) * in.scale) + b.y * mma_ex2((b.x - m) * in.scale));
-    };
+    const float m = fmaxf(a.x, b.x);
+    if (m == -CUDART_INF_F) return make_float2(m, a.y + b.y);               // both empty, or NaN
+    return make_float2(m, a.y * mma_ex2((a.x - m) * scale) + b.y * mma_ex2((b.x - m) * scale));
+}
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinIn in)
+{
+    __shared__ float2 found[kJoinThreads / 32][kJoinRows];
+    __shared__ bool last;
+    wait_for_earlier();
+    let_next_start();
+    const int tid = threadIdx.x, of = tid % kJoinRows, slice = tid / kJoinRows;
+    const int row = static_cast<int>(blockIdx.x) * kJoinRows + of, count = in.live ? *in.live : in.rows;
     float2 s = make_float2(-CUDART_INF_F, 0.f);
     if (row < count)
 #pragma unroll 4
-        for (int k = warp; k < in.count; k += kJoinWarps) s = join(s, in.parts[k * in.part_stride + row]);
-    found[warp][lane] = s;
-    __syncthreads();
-    if (warp) return;
-    double share = 0;
-    if (row < count) {
-        for (int w = 1; w < kJoinWarps; ++w) s = join(s, found[w][lane]);
-        const int at = in.order ? in.order[row] : row;
-        const long long t = in.tokens[at];
-        const bool known = t >= 0 && t < in.vocab;
-        // products' difference first: the rounding is that of a small number where the token is likely
-        const float rest = s.y == 0.f ? CUDART_NAN_F : logf(s.y), lse = known ? fmaf(s.x, in.inv_temperature, rest) : CUDART_NAN_F;
-        const float logp = known ? fmaf(in.picked[row] - s.x, in.inv_temperature, -rest) : CUDART_NAN_F;
-        in.lse[at] = lse;
-        in.logp[at] = logp;
-        share = in.weights ? static_cast<double>(in.weights[at]) * logp : logp;
+        for (int k = slice; k < in.count; k += kJoinThreads / kJoinRows) s = join_parts(s, __ldcg(in.parts + k * in.part_stride + row), in.scale);
+#pragma unroll
+    for (int o = 16; o >= kJoinRows; o >>= 1) {
+        float2 b;
+        b.x = __shfl_xor_sync(kAllLanes, s.x, o);
+        b.y = __shfl_xor_sync(kAllLanes, s.y, o);
+        s = (tid & 31) & o ? join_parts(b, s, in.scale) : join_parts(s, b, in.scale);
     }
-    if (!in.sums) return;
-    for (int o = 16; o; o >>= 1) share += __shfl_xor_sync(kAllLanes, share, o);
-    if (lane == 0) in.sums[blockIdx.x] = share;
-}
-
-// loss and sum of the weights.
-__global__ void __launch_bounds__(256) loss_kernel(const double *sums, int blocks, const float *total, int rows, float *stats)
-{
-    __shared__ double part[8];
-    double s = 0;
-    for (int k = threadIdx.x; k < blocks; k += 256) s += sums[k];
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAllLanes, s, o);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    if ((tid & 31) < kJoinRows) found[tid >> 5][of] = s;
     __syncthreads();
-    if (threadIdx.x) return;
-    for (int w = 1; w < 8; ++w) s += part[w];
-    const float all = total ? *total : static_cast<float>(rows);
-    stats[0] = all == 0.f ? 0.f : static_cast<float>(-s / all);
-    stats[1] = all;
+    if (tid >= 32) {
+        if (!in.stats) return;
+    } else {
+        double share = 0;
+        if (tid < kJoinRows && row < count) {
+            s = found[0][of];
+            for (int w = 1; w < kJoinThreads / 32; ++w) s = join_parts(s, found[w][of], in.scale);
+            const int at = in.order ? in.order[row] : row;
+            const long long t = in.tokens[at];
+            const bool known = t >= 0 && t < in.vocab;
+            if (!known || s.y == 0.f) s.y = CUDART_NAN_F;
+            // products' difference first: the rounding is that of a small number where the token is likely
+            const float rest = logf(s.y), logp = known ? fmaf(in.picked[row] - s.x, in.inv_temperature, -rest) : CUDART_NAN_F;
+            in.norms[row] = make_float2(s.x, log2f(s.y));
+            in.lse[at] = fmaf(s.x, in.inv_temperature, rest);
+            in.logp[at] = logp;
+            share = in.weights ? static_cast<double>(in.weights[at]) * logp : logp;
+        }
+        if (!in.stats) return;
+        for (int o = kJoinRows / 2; o; o >>= 1) share += __shfl_xor_sync(kAllLanes, share, o);
+        if (tid == 0) {
+            in.sums[blockIdx.x] = share;
+            __threadfence();
+            last = atomicAdd(in.done, 1u) == gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    __shared__ double part[kJoinThreads / 32];
+    double sum = 0;
+    for (int k = tid; k < static_cast<int>(gridDim.x); k += kJoinThreads) sum += __ldcg(in.sums + k);
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
+    if ((tid & 31) == 0) part[tid >> 5] = sum;
+    __syncthreads();
+    if (tid) return;
+    for (int w = 1; w < kJoinThreads / 32; ++w) sum += part[w];
+    const float all = in.total ? *in.total : static_cast<float>(in.rows);
+    in.stats[0] = all == 0.f ? 0.f : static_cast<float>(-sum / all);
+    in.stats[1] = all;
 }
 
-// Sums of a product's splits added up, in order, times alpha (and a gain for each column); rows by their place, zeros where they have none.
-struct SplitSum {
-    const float *part;
-    long long part_stride, part_rows;
-    int splits;
-    const int *place;                      // may be null: row r at r
-    int rows, cols;
-    float alpha;
-    const float *alpha_dev;
-    const void *gain;
-    int gain_bf16;
-    void *out;
-    int out_bf16, vectors;
-    long long stride;
+// G of the kept piece, from its exponentials and in their place: p = e 2^(scale (part's maximum - row's) - log2 sum).  A token that is its part's
+// maximum has e = 1 exactly, any other has p <= 1/2: so p - 1 does not suffer from e's rounding.  Bound by HBM (one read, one write).
+constexpr int kKeptThreads = 256, kKeptTurns = 4, kKeptColumns = kKeptThreads * kKeptTurns * kUnit;
+struct KeptIn {
+    uint4 *g;                              // eight values each
+    long long stride;                      // vectors of a row
+    int first, width, segments;            // blocks a row
+    const float2 *parts, *norms;
+    long long part_stride;
+    const long long *tokens;
+    const int *order, *live;
+    const float *coef;
+    float sign, scale;
+    int rows;
 };
-__global__ void __launch_bounds__(128) split_sum_kernel(const __grid_constant__ SplitSum in)
+__global__ void __launch_bounds__(kKeptThreads) kept_grad_kernel(const __grid_constant__ KeptIn in)
 {
-    const int row = blockIdx.x;
-    const int from = in.place ? in.place[row] : row;
-    const float factor = in.alpha_dev ? in.alpha * *in.alpha_dev : in.alpha;
-    for (int col = threadIdx.x * kUnit; col < in.cols; col += 128 * kUnit) {
-        Unit u{};
-        const int left = in.cols - col;
-        const bool whole = in.vectors && left >= kUnit;
-        if (from >= 0) {
-            const float *p = in.part + from * in.part_stride + col;
-            for (int s = 0; s < in.splits; ++s, p += in.part_rows) {
-                const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-                const float v[kUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    wait_for_earlier();
+    let_next_start();
+    const int row = static_cast<int>(blockIdx.x / static_cast<unsigned>(in.segments)), segment = static_cast<int>(blockIdx.x % static_cast<unsigned>(in.segments));
+    const int count = in.live ? *in.live : in.rows;
+    if (row >= (count + kStep - 1) / kStep * kStep) return;
+    uint4 *g = in.g + row * in.stride;
+    const int col0 = segment * kKeptColumns + static_cast<int>(threadIdx.x) * kUnit;
+    uint4 e[kKeptTurns];
+    float top[kKeptTurns];
+    if (row < count) {
 #pragma unroll
-                for (int k = 0; k < kUnit; ++k) u.v[k] += v[k];
-            }
-#pragma unroll
-            for (int k = 0; k < kUnit; ++k) u.v[k] *= factor;
-            if (in.gain) {
-                const Unit w = load_gain(in.gain, in.gain_bf16, col, left, whole);
-#pragma unroll
-                for (int k = 0; k < kUnit; ++k) u.v[k] *= w.v[k];
+        for (int j = 0; j < kKeptTurns; ++j) {
+            const int col = col0 + j * kKeptThreads * kUnit;
+            if (col < in.width) {
+                e[j] = g[col / kUnit];
+                top[j] = __ldg(&in.parts[static_cast<long long>((in.first + col) / kHalf) * in.part_stride + row].x);
             }
         }
-        if (in.out_bf16) store_unit(static_cast<__nv_bfloat16 *>(in.out) + row * in.stride + col, u, left, whole);
-        else store_unit(static_cast<float *>(in.out) + row * in.stride + col, u, left, whole);
+    }
+    const int at = row < count ? in.order ? in.order[row] : row : 0;
+    const long long token = row < count ? in.tokens[at] - in.first : -1;
+    const float a = row < count ? in.coef ? in.sign * in.coef[at] : 1.f : 0.f;
+    const float2 norm = row < count ? in.norms[row] : make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kKeptTurns; ++j) {
+        const int col = col0 + j * kKeptThreads * kUnit;
+        if (col >= in.width) break;
+        uint4 out = make_uint4(0, 0, 0, 0);
+        if (row < count) {
+            const float f = a * mma_ex2(fmaf(top[j] - norm.x, in.scale, -norm.y)) * 18446744073709551616.f;
+            const unsigned w[4] = {e[j].x, e[j].y, e[j].z, e[j].w};
+            Unit u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 v = shares_below(w[k]);
+                u.v[2 * k] = v.x * f;
+                u.v[2 * k + 1] = v.y * f;
+            }
+            if (token >= col && token < col + kUnit) {
+                const int own = static_cast<int>(token) - col;
+#pragma unroll
+                for (int k = 0; k < kUnit; ++k) if (k == own) u.v[k] -= a;
+            }
+            out = make_uint4(bf16_pair(u.v[0], u.v[1]), bf16_pair(u.v[2], u.v[3]), bf16_pair(u.v[4], u.v[5]), bf16_pair(u.v[6], u.v[7]));
+        }
+        g[col / kUnit] = out;
     }
 }
 

@@ -3,7 +3,8 @@
 // A pair of CTAs takes a tile of 256 x 256 (tcgen05.mma, cta_group::2): each holds 128 rows of A and 128 of B for every 64 steps of the contraction,
 // in a ring of stages that one thread a CTA fills with TMA loads (128-byte swizzle), and 128 rows of the sums in its tensor memory,
 // twice, so that the epilogue of one tile runs under the products of the next.  Warps: 0 loads, 1 issues the products (of the pair's first CTA), 2 owns
-// the tensor memory, 4 to 11 are the epilogue (a warp reaches the 32 lanes of its number modulo 4; two warps share them, half the columns each).
+// the tensor memory, 4 to 11 are the epilogue (a warp reaches the 32 lanes of its number modulo 4; two warps share them, half the columns each), 12
+// to 19, where B comes as 8-bit codes, turn them into bf16, with the scales that warp 3 brings.
 //
 // Either operand may lie with its contraction dimension contiguous (rows of A, "K-major") or with its other one (A given as its transpose,
 // "MN-major"): the loads bring blocks of 64 x 64 as they lie, and the descriptors tell the tensor cores.
@@ -22,11 +23,22 @@
 namespace softsync {
 
 constexpr int kTile = 256, kHalf = 128, kStep = 64;          // tile, rows of an operand in a CTA, contraction steps of a stage
-constexpr int kStages = 6;
-constexpr int kStageBytes = 2 * kHalf * kStep * 2;
-constexpr int kMmaThreads = 384, kEpilogueWarp = 4, kEpilogueWarps = 8;
-constexpr int kMmaShared = kStages * kStageBytes + 1024;      // the ring, aligned to the swizzle's 1024 bytes
+constexpr int kOperandBytes = kHalf * kStep * 2, kStageBytes = 2 * kOperandBytes;
+constexpr int kCodeBytes = kHalf * kStep;                      // a stage's codes
+constexpr int kEpilogueWarp = 4, kEpilogueWarps = 8, kCodeWarp = 12, kCodeWarps = 4, kCodeGroups = 2;
+constexpr int kScaleWarp = 3, kScaleStages = 16, kScaleBatch = 8, kScaleBytes = 4 * kStep;
 constexpr int kMmaWaitLimit = 1 << 20;                         // polls of up to a microsecond
+
+constexpr int kDeskRow = 128;                                  // bytes of a row where an epilogue warp turns a row a lane into neighbouring lanes of a row
+
+// Threads, stages and shared memory of a kernel, with B as bf16 or as codes (with a ring of their own).
+template <bool CODES> struct MmaShape {
+    static constexpr int threads = 32 * (kCodeWarp + (CODES ? kCodeWarps * kCodeGroups : 0)), stages = CODES ? 5 : 6, code_stages = CODES ? 5 : 0;
+    static constexpr int desk_rows = CODES ? 16 : 32;
+    static constexpr int code_ring = stages * kStageBytes, desks = code_ring + code_stages * kCodeBytes;      // places in shared memory
+    static constexpr int scales = desks + kEpilogueWarps * desk_rows * kDeskRow;
+    static constexpr int shared = scales + (CODES ? kScaleStages * kScaleBytes : 0) + 1024;         // aligned to the swizzle's 1024 bytes
+};
 
 // ---- instructions ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ unsigned mma_smem(const void *p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
@@ -51,9 +63,17 @@ __device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+// At the pair's first CTA.  A release in the cluster's scope waits for everything that the SM has under way: 1600 cycles where a stage takes 512.  It
+// is not needed: what the barrier guards is each CTA's own shared or tensor memory, read by that SM's tensor core, so the writer's proxy fence and a
+// release in the CTA's scope put it in order, and reads of tensor memory have fences of their own.
 __device__ __forceinline__ void bar_arrive_leader(unsigned bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(leaders(bar)) : "memory");
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" :: "r"(leaders(bar)) : "memory");
+}
+__device__ __forceinline__ void bar_relaxed_leader(unsigned bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(leaders(bar)) : "memory");
 }
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity)
 {
@@ -70,6 +90,14 @@ __device__ __forceinline__ void tile_load(unsigned dst, const CUtensorMap *map, 
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(leader_bar) : "memory");
 }
+// Into this CTA alone, with its own barrier.
+__device__ __forceinline__ void code_load(unsigned dst, const CUtensorMap *map, int x, int y, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void mma_pair(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -83,12 +111,18 @@ __device__ __forceinline__ void commit_pair(unsigned bar)      // arrives at bot
 __device__ __forceinline__ void tmem_load32(unsigned addr, float (&v)[32])
 {
     unsigned *r = reinterpret_cast<unsigned *>(v);
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-                   "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
-                   "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                  : "r"(addr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_load16(unsigned addr, float (&v)[16])
+{
+    unsigned *r = reinterpret_cast<unsigned *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr) : "memory");
 }
 __device__ __forceinline__ float mma_ex2(float x)
 {
@@ -115,105 +149,185 @@ struct MmaPlan {
     int m, n, k;                          // extents; where `live` is given it replaces m (live_is_k 0) or k (1)
     const int *live;
     int live_is_k;
-    int splits;                           // parts that the contraction is split into, each with sums of its own
+    int slots;                            // pairs that work at once, where the last tiles may be split along the contraction; else 0
     int group;                            // row tiles whose turns come before the next column tile's
 };
 
-struct TileAt { int m, n, split, first, steps; };            // tile indices, split, and its stages of the contraction
+// Into how many parts the last `rest` tiles (fewer than slots) are split along their `steps`, so that they fill the GPU.  In steps of 0.4 us: a round
+// takes its steps and about 6 for filling and draining the pipeline; the parts are summed by a kernel of its own (8, and 0.2 for each part's 256 KB
+// written and read).
+constexpr int kMostParts = 3;             // times slots: room in the workspace
+__host__ __device__ inline int split_count(int rest, int steps, int slots)
+{
+    constexpr int tried[10] = {2, 3, 4, 6, 8, 12, 16, 24, 37, 74};
+    int best = 1, cost = 5 * (steps + 6);
+    if (steps < 16) return 1;
+#pragma unroll
+    for (int j = 0; j < 10; ++j) {
+        const int s = tried[j];
+        if (s * 4 > steps || rest * s > kMostParts * slots) continue;
+        const int c = 5 * ((rest * s + slots - 1) / slots * ((steps + s - 1) / s + 6) + 8) + rest * s;
+        if (c < cost) { cost = c; best = s; }
+    }
+    return best;
+}
+
+struct TileAt { int m, n, part, first, steps; };             // tile indices, number of the part (-1: the whole tile), and its stages of the contraction
 
 struct TileWalk {
-    int tiles_m, tiles_n, all_steps, splits, group;
-    long long count;
+    int tiles_m, tiles_n, all_steps, splits, group, whole, count;        // fewer than 2^31 items: the host sees to that
     __device__ __forceinline__ TileWalk(const MmaPlan &p)
     {
         const int live = p.live ? *p.live : 0, m = p.live && !p.live_is_k ? live : p.m, k = p.live && p.live_is_k ? live : p.k;
         tiles_m = (m + kTile - 1) / kTile;
         tiles_n = (p.n + kTile - 1) / kTile;
         all_steps = (k + kStep - 1) / kStep;
-        splits = p.splits;
         group = p.group;
-        count = static_cast<long long>(tiles_m) * tiles_n * splits;
+        whole = count = tiles_m * tiles_n;
+        splits = 1;
+        if (!p.slots) return;
+        const int rest = static_cast<int>(static_cast<unsigned>(count) % static_cast<unsigned>(p.slots));
+        if (!rest || (splits = split_count(rest, all_steps, p.slots)) == 1) return;
+        whole = count - rest;
+        count = whole + rest * splits;
     }
-    __device__ __forceinline__ TileAt at(long long t) const
+    __device__ __forceinline__ void place(unsigned tile, int &m, int &n) const
+    {
+        const unsigned band = static_cast<unsigned>(group) * static_cast<unsigned>(tiles_n), b = tile / band, at = tile - b * band;
+        const unsigned high = static_cast<unsigned>(min(group, tiles_m - static_cast<int>(b) * group));
+        n = static_cast<int>(at / high);
+        m = static_cast<int>(b) * group + static_cast<int>(at % high);
+    }
+    __device__ __forceinline__ TileAt at(int t) const
     {
         TileAt r;
-        const long long tiles = static_cast<long long>(tiles_m) * tiles_n;
-        r.split = static_cast<int>(t / tiles);
-        const long long in = t - r.split * tiles;
-        const long long band = static_cast<long long>(group) * tiles_n;
-        const int b = static_cast<int>(in / band), high = min(group, tiles_m - b * group);
-        const int at = static_cast<int>(in - b * band);
-        r.n = at / high;
-        r.m = b * group + at % high;
-        const int per = (all_steps + splits - 1) / splits;
-        r.first = min(all_steps, r.split * per);
-        r.steps = min(all_steps, r.first + per) - r.first;
+        r.part = -1; r.first = 0; r.steps = all_steps;
+        if (t >= whole) {
+            r.part = t - whole;
+            const int per = (all_steps + splits - 1) / splits, tile = r.part / splits, split = r.part - tile * splits;
+            r.first = min(all_steps, split * per);
+            r.steps = min(all_steps, r.first + per) - r.first;
+            t = whole + tile;
+        }
+        place(static_cast<unsigned>(t), r.m, r.n);
         return r;
     }
 };
 
-// ---- epilogues: each is called by the 32 lanes of a warp, a row a lane, 32 columns at a time -----------------------------------
-// Maximum and sum of exponentials of a row's 128 columns, and the token's product.
+// ---- an epilogue warp's desk ---------------------------------------------------------------------------------------------
+// Tensor memory gives a lane one row; stored like that, 16 bytes of 32 different rows at a time, a tile's 64 KB took 4096 trips of the load-store
+// unit (2.1 us).  So rows go through shared memory, and neighbouring lanes store neighbouring vectors.  Sixteenths of 128 (of a row of 64 bytes: quarters) change
+// places with the row's number, so that eight lanes never meet in a bank.
+__device__ __forceinline__ void desk_put(unsigned at, uint4 v)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 desk_get(unsigned at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned wide_place(int row, int vector) { return row * 128 + ((vector ^ (row & 7)) << 4); }
+__device__ __forceinline__ unsigned narrow_place(int row, int vector) { return row * 64 + ((vector ^ ((row >> 1) & 3)) << 4); }
+
+// ---- epilogues: each is called by the 32 lanes of a warp, a row a lane ------------------------------------------------------
+// 16 bits of an exponential between 0 and 1: 6 of exponent, 10 of fraction, and no sign.  Half a step is 2^-11 of the value, down to 2^-62: a rare
+// entry's share is as exact as a likely one's, which it would not be in fp16.  They are bits 13 to 28 of the float times 2^-64 (its exponent
+// less 64), rounded.
+__device__ __forceinline__ unsigned share_bits(float a, float b)
+{
+    const unsigned x = static_cast<unsigned>(max(__float_as_int(a) - (0x20000000 - 0x1000), 0)), y = static_cast<unsigned>(max(__float_as_int(b) - (0x20000000 - 0x1000), 0));
+    return __byte_perm(x >> 13, y << 3, 0x7610);
+}
+__device__ __forceinline__ float2 shares_below(unsigned w)       // times 2^-64
+{
+    return make_float2(__uint_as_float((w & 0xffffu) << 13), __uint_as_float(w >> 3 & 0x1fffe000u));
+}
+
+// Maximum and sum of exponentials of a row's 128 columns, and the token's product; of the piece of the vocabulary that is kept, the exponentials
+// themselves, relative to that maximum, in 16 bits.
+//
+// The tensor cores cut the running sum to 24 bits at every step, towards zero: over a width of 4096 that took 2e-6 of a product (256 steps of 16).  So its sums
+// are taken out of tensor memory every kChunk stages and added up here, rounded to nearest: 4e-7.
 struct StatsEpilogue {
+    static constexpr int kChunk = 16;
     const int *order;                     // the rows that take part, or null: all
     const long long *tokens;
     int rows, vocab;
     const int *live;
     float scale;                          // log2(e) / T
-    float2 *parts;                        // [column half][row]: maximum of the products, sum of 2^(scale (x - maximum))
+    float2 *parts;                        // [128 columns][row]: maximum of the products, sum of 2^(scale (x - maximum))
     long long part_stride;
     float *picked;                        // the token's product
+    uint16_t *kept;                       // of columns from `first` on; may be null
+    long long kept_stride;
+    int first;
+    unsigned *done;                       // counter of the next kernel, set to zero
 
-    int row, tok;
-    bool valid;
-    float top, sum;
-    __device__ __forceinline__ void begin(int r, int)
+    __device__ __forceinline__ void take(float (&x)[kHalf], int row, int col, bool late, unsigned desk) const
     {
-        row = r;
-        valid = r < (live ? *live : rows);
-        const long long t = valid ? tokens[order ? order[r] : r] : -1;
-        tok = t >= 0 && t < vocab ? static_cast<int>(t) : -1;
-        top = -CUDART_INF_F;
-        sum = 0.f;
-    }
-    __device__ __forceinline__ void take(float (&x)[32], int col)
-    {
-        if (col >= vocab) return;
-        if (col + 32 > vocab) {
+        if (col >= vocab) return;                              // the same for the whole warp
+        const bool valid = row < (live ? *live : rows);
+        const long long t = valid ? tokens[order ? order[row] : row] : -1;
+        if (col + kHalf > vocab) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) if (col + k >= vocab) x[k] = -CUDART_INF_F;
+            for (int k = 0; k < kHalf; ++k) if (col + k >= vocab) x[k] = -CUDART_INF_F;
         }
-        const unsigned at = static_cast<unsigned>(tok - col);
-        if (__any_sync(kAllLanes, at < 32u)) {
+        const bool mine = t >= col && t < col + kHalf && t < vocab;
+        if (__any_sync(kAllLanes, mine)) {
+            const int at = static_cast<int>(t - col);
             float z = 0.f;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) z = at == static_cast<unsigned>(k) ? x[k] : z;
-            if (at < 32u && valid) picked[row] = z;
+            for (int k = 0; k < kHalf; ++k) z = at == k ? x[k] : z;
+            if (mine) picked[row] = z;
         }
-        float m = top;
+        if (late) x[0] = CUDART_NAN_F;
+        float m[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-        for (int k = 0; k < 32; ++k) m = fmaxf(m, x[k]);
-        const float shift = m == -CUDART_INF_F ? 0.f : m * scale;
-        float s[4] = {sum * mma_ex2(top * scale - shift), 0.f, 0.f, 0.f};
-        if (top == -CUDART_INF_F) s[0] = 0.f;
+        for (int k = 4; k < kHalf; ++k) m[k & 3] = fmaxf(m[k & 3], x[k]);
+        const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), from = top == -CUDART_INF_F ? 0.f : top;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < 32; ++k) s[k & 3] += mma_ex2(fmaf(x[k], scale, -shift));
-        sum = (s[0] + s[1]) + (s[2] + s[3]);
-        top = m;
-    }
-    __device__ __forceinline__ void end(int col, int)
-    {
-        if (valid && col < vocab) parts[static_cast<long long>(col / kHalf) * part_stride + row] = make_float2(top, sum);
+        for (int k = 0; k < kHalf; ++k) { x[k] = mma_ex2((x[k] - from) * scale); s[k & 3] += x[k]; }
+        if (valid) parts[static_cast<long long>(col / kHalf) * part_stride + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+        if (!kept || col < first) return;
+        const int lane = threadIdx.x & 31, row0 = row - lane;
+        const unsigned there = __ballot_sync(kAllLanes, valid);
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 64) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float *v = x + c + 8 * k;
+                desk_put(desk + wide_place(lane, k), make_uint4(share_bits(v[0], v[1]), share_bits(v[2], v[3]), share_bits(v[4], v[5]), share_bits(v[6], v[7])));
+            }
+            __syncwarp();
+#pragma unroll
+            for (int r = lane >> 3; r < 32; r += 4) {
+                const uint4 v = desk_get(desk + wide_place(r, lane & 7));
+                if (there >> r & 1) *reinterpret_cast<uint4 *>(kept + (row0 + r) * kept_stride + (col - first) + c + 8 * (lane & 7)) = v;
+            }
+            __syncwarp();
+        }
     }
 };
 
+// A row's normaliser as the products' maximum and log2 of the sum relative to it: p = 2^(scale (x - maximum) - log2 sum), whose rounding is that of small
+// numbers where p is near one.
+__device__ __forceinline__ float2 row_normaliser(const float2 *norms, const float *lse, int row, int at)
+{
+    return norms ? norms[row] : make_float2(0.f, lse[at] * 1.4426950408889634f);
+}
+
 // G = a (p - 1[j = token]) of a piece of the vocabulary, rounded to bf16.
 struct GradEpilogue {
+    static constexpr int kChunk = 1 << 30;
     const int *order;
     const long long *tokens;
+    const float2 *norms;                  // of the rows that take part, or null: from lse
     const float *lse, *coef;              // of all rows; coef null: 1
     float sign;                           // of coef
-    int rows, vocab;
+    int rows;
     const int *live;
     float scale;
     int first, width;                     // the piece: columns [first, first + width)
@@ -221,118 +335,215 @@ struct GradEpilogue {
     long long g_stride;
 
     int row, tok, write;
-    float a, shift;
+    float a;
+    float2 norm;
     __device__ __forceinline__ void begin(int r, int)
     {
         const int n = live ? *live : rows;
         row = r;
         write = r < (n + kStep - 1) / kStep * kStep;        // rows up to a whole stage of the next product: zeros
-        a = 0.f; shift = 0.f; tok = -1;
+        a = 0.f; norm = make_float2(0.f, 0.f); tok = -1;
         if (r < n) {
             const int at = order ? order[r] : r;
             const long long t = tokens[at];
             tok = t >= first && t < first + width ? static_cast<int>(t - first) : -1;
             a = coef ? sign * coef[at] : 1.f;
-            shift = lse[at] * 1.4426950408889634f;
+            norm = row_normaliser(norms, lse, r, at);
         }
     }
-    __device__ __forceinline__ void take(float (&x)[32], int col)
+    template <int ROWS>
+    __device__ __forceinline__ void take(float (&x)[32], int col, unsigned desk)
     {
+        static_assert(ROWS == 32, "a desk of whole rows");
         if (col >= width) return;
         const unsigned at = static_cast<unsigned>(tok - col);
         const bool picked = __any_sync(kAllLanes, at < 32u);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = mma_ex2(fmaf(x[k], scale, -shift));
+        for (int k = 0; k < 32; ++k) x[k] = mma_ex2(fmaf(x[k] - norm.x, scale, -norm.y));
         if (picked) {
 #pragma unroll
             for (int k = 0; k < 32; ++k) x[k] -= at == static_cast<unsigned>(k) ? 1.f : 0.f;
         }
-        if (!write) return;
-        uint4 *to = reinterpret_cast<uint4 *>(g + row * g_stride + col);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float *v = x + 8 * k;
+        for (int k = 0; k < 32; ++k) x[k] = a == 0.f ? 0.f : a * x[k];
+        const int lane = threadIdx.x & 31, row0 = row - lane, k = lane & 3;
+        const unsigned there = __ballot_sync(kAllLanes, write);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = a == 0.f ? 0.f : a * v[j];
-            if (col + 8 * k < width)
-                to[k] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+        for (int j = 0; j < 4; ++j) {
+            const float *v = x + 8 * j;
+            desk_put(desk + narrow_place(lane, j), make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])));
         }
+        __syncwarp();
+#pragma unroll
+        for (int r = lane >> 2; r < 32; r += 8) {
+            const uint4 v = desk_get(desk + narrow_place(r, k));
+            if ((there >> r & 1) && col + 8 * k < width) *reinterpret_cast<uint4 *>(g + (row0 + r) * g_stride + col + 8 * k) = v;
+        }
+        __syncwarp();
     }
-    __device__ __forceinline__ void end(int, int) {}
 };
 
-// The product itself: alpha D (times a gain for each column), or fp32 sums of a split for a later kernel.
-struct StoreEpilogue {
+// Where a product goes: alpha (D + sum) times a gain for each column, rounded once; or D (+ sum) in fp32, for another product to be added.
+struct StoreTarget {
     int rows, cols;
+    const int *live;                      // rows that there are, or null
+    const int *order;                     // where they go, or null
     float alpha;
     const float *alpha_dev;               // may be null
     const void *gain;                     // may be null
     int gain_bf16;
-    void *out;                            // bf16 or fp32, or null: sums to `part`
+    void *out;                            // bf16 or fp32; null: to `sum`
     int out_bf16, vectors;
     long long stride;
-    float *part;
-    long long part_stride, part_rows;     // elements of a row, and of a split
-    int add;                              // to what is there
+    float *sum;
+    long long sum_stride;                 // whole vectors
+    int add;                              // what `sum` holds
+    float *parts;                         // 256 x 256 sums of each part of a split tile
 
-    int row;
-    float factor;
-    float *to;
-    __device__ __forceinline__ void begin(int r, int split)
+    __device__ __forceinline__ int count() const { return live ? *live : rows; }
+    __device__ __forceinline__ float factor() const { return alpha_dev ? alpha * *alpha_dev : alpha; }
+    __device__ __forceinline__ void store(int row, int place, int col, Unit &u, float factor) const
     {
-        row = r;
-        factor = alpha_dev ? alpha * *alpha_dev : alpha;
-        if (part) to = part + split * part_rows + r * part_stride;
-    }
-    __device__ __forceinline__ void take(float (&x)[32], int col)
-    {
-        if (row >= rows || col >= cols) return;
-        if (!out) {                                       // padded to whole vectors
-            float4 *p = reinterpret_cast<float4 *>(to + col);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (col + 4 * k >= part_stride) break;
-                float4 v = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
-                if (add) { const float4 o = p[k]; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
-                p[k] = v;
-            }
+        const int left = cols - col;
+        if (left <= 0) return;
+        float *s = sum + static_cast<long long>(row) * sum_stride + col;
+        if (add) {
+            const float4 a = reinterpret_cast<const float4 *>(s)[0], b = reinterpret_cast<const float4 *>(s)[1];
+            u.v[0] += a.x; u.v[1] += a.y; u.v[2] += a.z; u.v[3] += a.w; u.v[4] += b.x; u.v[5] += b.y; u.v[6] += b.z; u.v[7] += b.w;
+        }
+        if (!out) {
+            store_unit(s, u, kUnit, true);
             return;
         }
+        const bool whole = vectors && left >= kUnit;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int c = col + 8 * k, left = cols - c;
-            if (left <= 0) break;
-            const bool whole = vectors && left >= kUnit;
-            Unit u;
+        for (int j = 0; j < kUnit; ++j) u.v[j] *= factor;
+        if (gain) {
+            const Unit w = load_gain(gain, gain_bf16, col, left, whole);
 #pragma unroll
-            for (int j = 0; j < kUnit; ++j) u.v[j] = x[8 * k + j] * factor;
-            if (gain) {
-                const Unit w = load_gain(gain, gain_bf16, c, left, whole);
+            for (int j = 0; j < kUnit; ++j) u.v[j] *= w.v[j];
+        }
+        if (out_bf16) store_unit(static_cast<__nv_bfloat16 *>(out) + place * stride + col, u, left, whole);
+        else store_unit(static_cast<float *>(out) + place * stride + col, u, left, whole);
+    }
+};
+struct StoreEpilogue {
+    static constexpr int kChunk = 1 << 30;
+    StoreTarget target;
+
+    int row0, place;                      // the warp's first row; where this lane's row goes, -1: nowhere
+    float factor;
+    float *part;
+    __device__ __forceinline__ void begin(int r, int p)
+    {
+        row0 = r - static_cast<int>(threadIdx.x & 31);
+        place = r >= target.count() ? -1 : target.order ? target.order[r] : r;
+        factor = target.factor();
+        part = p >= 0 ? target.parts + (static_cast<long long>(p) * kTile + row0 % kTile) * kTile : nullptr;
+    }
+    template <int ROWS>
+    __device__ __forceinline__ void take(float (&x)[32], int col, unsigned desk)
+    {
+        if (col >= target.cols) return;
+        const int lane = threadIdx.x & 31, unit = lane & 3;
 #pragma unroll
-                for (int j = 0; j < kUnit; ++j) u.v[j] *= w.v[j];
+        for (int first = 0; first < 32; first += ROWS) {
+            if (ROWS == 32 || lane / ROWS == first / ROWS) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    desk_put(desk + wide_place(lane % ROWS, k), make_uint4(__float_as_uint(x[4 * k]), __float_as_uint(x[4 * k + 1]), __float_as_uint(x[4 * k + 2]), __float_as_uint(x[4 * k + 3])));
             }
-            if (out_bf16) store_unit(static_cast<__nv_bfloat16 *>(out) + row * stride + c, u, left, whole);
-            else store_unit(static_cast<float *>(out) + row * stride + c, u, left, whole);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < ROWS / 8; ++j) {
+                const int d = j * 8 + (lane >> 2), r = first + d, to = __shfl_sync(kAllLanes, place, r);
+                const uint4 a = desk_get(desk + wide_place(d, 2 * unit)), b = desk_get(desk + wide_place(d, 2 * unit + 1));
+                if (to < 0) continue;
+                if (part) {
+                    uint4 *p = reinterpret_cast<uint4 *>(part + r * kTile + col % kTile + 8 * unit);
+                    p[0] = a;
+                    p[1] = b;
+                    continue;
+                }
+                Unit u{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w), __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z),
+                        __uint_as_float(b.w)}};
+                target.store(row0 + r, to, col + 8 * unit, u, factor);
+            }
+            __syncwarp();
         }
     }
-    __device__ __forceinline__ void end(int, int) {}
 };
 
-// ---- the kernel --------------------------------------------------------------------------------------------------------
-template <typename Epilogue, bool MN_A, bool MN_B>
-__global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                              const __grid_constant__ MmaPlan plan, const __grid_constant__ Epilogue given)
+// The split tiles' parts added up, in order.  A block takes eight rows of a tile, a warp one, a lane a unit of eight columns.
+constexpr int kSumRows = 8;
+__global__ void __launch_bounds__(256) split_sum_kernel(const __grid_constant__ MmaPlan plan, const __grid_constant__ StoreTarget target)
 {
+    wait_for_earlier();
+    let_next_start();
+    const TileWalk walk(plan);
+    const int rest = static_cast<int>(blockIdx.x) / (kTile / kSumRows), first = static_cast<int>(blockIdx.x) % (kTile / kSumRows) * kSumRows;
+    if (rest >= (walk.count - walk.whole) / walk.splits) return;
+    int m, n;
+    walk.place(walk.whole + rest, m, n);
+    const int lane = threadIdx.x & 31, count = target.count();
+    const float factor = target.factor();
+    const int r = first + (threadIdx.x >> 5), row = m * kTile + r;
+    if (row >= count) return;
+    const float *p = target.parts + (static_cast<long long>(rest) * walk.splits * kTile + r) * kTile + lane * kUnit;
+    Unit u{};
+#pragma unroll 8
+    for (int s = 0; s < walk.splits; ++s) {
+        const float4 a = __ldcs(reinterpret_cast<const float4 *>(p + s * kTile * kTile)), b = __ldcs(reinterpret_cast<const float4 *>(p + s * kTile * kTile) + 1);
+        u.v[0] += a.x; u.v[1] += a.y; u.v[2] += a.z; u.v[3] += a.w; u.v[4] += b.x; u.v[5] += b.y; u.v[6] += b.z; u.v[7] += b.w;
+    }
+    target.store(row, target.order ? target.order[row] : row, n * kTile + lane * kUnit, u, factor);
+}
+
+// ---- B from 8-bit codes ------------------------------------------------------------------------------------------------
+struct CodesIn {
+    const uint8_t *scales;                // `blocks` for each row
+    int rows, blocks, words;              // words: four neighbours can be read as one
+};
+
+// Four codes as bf16, exactly: with b = code + 128 in the low byte of the float 2^23 + b, minus 2^23 + 128, times the unit.  (One multiply-add of both
+// would overflow for units above 2^104.)
+__device__ __forceinline__ uint2 codes_to_bf16(unsigned codes, float unit)
+{
+    const unsigned b = codes ^ 0x80808080u;
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = (__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440 + k)) - 8388736.f) * unit;
+    return make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+}
+
+// ---- the kernel --------------------------------------------------------------------------------------------------------
+template <typename Epilogue, bool MN_A, bool MN_B, bool CODES>
+__global__ void __cluster_dims__(2) __launch_bounds__(MmaShape<CODES>::threads, 1)
+mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmaPlan plan, const __grid_constant__ Epilogue given,
+           const __grid_constant__ CodesIn codes)
+{
+    static_assert(!CODES || MN_B, "codes lie with their columns contiguous");
+    using Shape = MmaShape<CODES>;
+    constexpr int kStages = Shape::stages, kCodeStages = Shape::code_stages;
+    constexpr bool WHOLE = Epilogue::kChunk < (1 << 30);      // the epilogue takes all 128 columns of a row at once
     extern __shared__ unsigned char raw_ring[];
-    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], ready[2], drained[2];
+    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], ready[2], drained[2], code_full[CODES ? 2 * kCodeStages : 1], code_empty[CODES ? 2 * kCodeStages : 1];
+    __shared__ __align__(8) unsigned long long scale_full[CODES ? kScaleStages : 1], scale_empty[CODES ? kScaleStages : 1];
     __shared__ unsigned tmem_base;
-    const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u;
+    const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u, code_ring = ring + Shape::code_ring;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = pair_rank();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { bar_init(mma_smem(&full[s]), 1); bar_init(mma_smem(&empty[s]), 1); }
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(mma_smem(&full[s]), CODES ? 1 + 2 * kCodeWarps : 1);   // with codes: the copies, and four warps in each CTA
+            bar_init(mma_smem(&empty[s]), 1);
+        }
+        if constexpr (CODES) for (int s = 0; s < 2 * kCodeStages; ++s) { bar_init(mma_smem(&code_full[s]), 1); bar_init(mma_smem(&code_empty[s]), kCodeWarps); }
+        if constexpr (CODES) for (int s = 0; s < kScaleStages; ++s) { bar_init(mma_smem(&scale_full[s]), 1); bar_init(mma_smem(&scale_empty[s]), kCodeWarps); }
         for (int b = 0; b < 2; ++b) { bar_init(mma_smem(&ready[b]), 1); bar_init(mma_smem(&drained[b]), 2 * kEpilogueWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_b) : "memory");
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(mma_smem(&tmem_base)) : "memory");
@@ -343,25 +554,34 @@ __global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel
     pair_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const unsigned tmem = tmem_base;
+    wait_for_earlier();
+    let_next_start();
     const TileWalk walk(plan);
-    const long long start = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-
+    const int start = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
     if (warp == 0) {
         if (lane == 0) {
             unsigned turn = 0;                             // stages filled so far
             bool late = false;
-            for (long long t = start; t < walk.count && !late; t += pairs) {
+            for (int t = start; t < walk.count && !late; t += pairs) {
                 const TileAt at = walk.at(t);
                 const int ya = at.m * kTile + static_cast<int>(rank) * kHalf, yb = at.n * kTile + static_cast<int>(rank) * kHalf;
                 for (int s = 0; s < at.steps; ++s, ++turn) {
                     const unsigned slot = turn % kStages, round = turn / kStages;
-                    if (round && !bar_wait(mma_smem(&empty[slot]), (round - 1) & 1)) { late = true; break; }
-                    const unsigned bar = leaders(mma_smem(&full[slot])), a = ring + slot * kStageBytes, b = a + kStageBytes / 2;
-                    if (rank == 0) bar_expect(mma_smem(&full[slot]), 2 * kStageBytes);
                     const int x = (at.first + s) * kStep;
+                    if constexpr (CODES) {
+                        // Twice as many barriers as slots: each serves one of the two groups that turn the codes, which so knows its last phase.
+                        const unsigned here = turn % (2 * kCodeStages), before = turn - kCodeStages, at_bar = before % (2 * kCodeStages);
+                        if (turn >= kCodeStages && !bar_wait(mma_smem(&code_empty[at_bar]), (before / (2 * kCodeStages)) & 1)) { late = true; break; }
+                        bar_expect(mma_smem(&code_full[here]), kCodeBytes);
+                        code_load(code_ring + turn % kCodeStages * kCodeBytes, &map_b, yb, x, mma_smem(&code_full[here]));
+                    }
+                    if (round && !bar_wait(mma_smem(&empty[slot]), (round - 1) & 1)) { late = true; break; }
+                    const unsigned bar = leaders(mma_smem(&full[slot])), a = ring + slot * kStageBytes, b = a + kOperandBytes;
+                    if (rank == 0) bar_expect(mma_smem(&full[slot]), CODES ? 2 * kOperandBytes : 2 * kStageBytes);
                     if constexpr (MN_A) { tile_load(a, &map_a, ya, x, bar); tile_load(a + 8192, &map_a, ya + 64, x, bar); }
                     else tile_load(a, &map_a, x, ya, bar);
-                    if constexpr (MN_B) { tile_load(b, &map_b, yb, x, bar); tile_load(b + 8192, &map_b, yb + 64, x, bar); }
+                    if constexpr (CODES) continue;
+                    else if constexpr (MN_B) { tile_load(b, &map_b, yb, x, bar); tile_load(b + 8192, &map_b, yb + 64, x, bar); }
                     else tile_load(b, &map_b, x, yb, bar);
                 }
             }
@@ -370,67 +590,172 @@ __global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel
                 late = late || !bar_wait(mma_smem(&empty[k % kStages]), (k / kStages) & 1);
                 if (late && rank == 0) bar_wait(mma_smem(&full[k % kStages]), (k / kStages) & 1);
             }
+            if constexpr (CODES)                           // the last may have been asked for before its stage was free
+                for (unsigned k = turn > kCodeStages ? turn - kCodeStages : 0; late && k <= turn; ++k) bar_wait(mma_smem(&code_full[k % (2 * kCodeStages)]), (k / (2 * kCodeStages)) & 1);
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            unsigned turn = 0, tile = 0;
+            unsigned turn = 0, sums = 0;
             bool late = false;
-            for (long long t = start; t < walk.count && !late; t += pairs) {
+            for (int t = start; t < walk.count && !late; t += pairs) {
                 const TileAt at = walk.at(t);
-                if (!at.steps) continue;
-                const unsigned buffer = tile & 1, use = tile >> 1;
-                ++tile;
-                if (use && !bar_wait(mma_smem(&drained[buffer]), (use - 1) & 1)) { late = true; break; }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                unsigned buffer = 0;
                 for (int s = 0; s < at.steps; ++s, ++turn) {
+                    const int in = s % Epilogue::kChunk;
+                    if (in == 0) {
+                        if (s) commit_pair(mma_smem(&ready[buffer]));
+                        buffer = sums & 1;
+                        const unsigned use = sums >> 1;
+                        ++sums;
+                        if (use && !bar_wait(mma_smem(&drained[buffer]), (use - 1) & 1)) { late = true; break; }
+                    }
                     const unsigned slot = turn % kStages;
                     if (!bar_wait(mma_smem(&full[slot]), (turn / kStages) & 1)) { late = true; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t a = operand_descriptor<MN_A>(ring + slot * kStageBytes), b = operand_descriptor<MN_B>(ring + slot * kStageBytes + kStageBytes / 2);
+                    const uint64_t a = operand_descriptor<MN_A>(ring + slot * kStageBytes), b = operand_descriptor<MN_B>(ring + slot * kStageBytes + kOperandBytes);
 #pragma unroll
                     for (int k = 0; k < kStep / 16; ++k)
-                        mma_pair(tmem + buffer * kTile, a + k * kDescriptorStep<MN_A>, b + k * kDescriptorStep<MN_B>, kInstruction<MN_A, MN_B>, s || k);
+                        mma_pair(tmem + buffer * kTile, a + k * kDescriptorStep<MN_A>, b + k * kDescriptorStep<MN_B>, kInstruction<MN_A, MN_B>, in || k);
                     commit_pair(mma_smem(&empty[slot]));
                 }
-                if (!late) commit_pair(mma_smem(&ready[buffer]));
+                if (!late && at.steps) commit_pair(mma_smem(&ready[buffer]));
             }
         }
-    } else if (warp >= kEpilogueWarp) {
+    } else if (CODES && warp == kScaleWarp) {
+        // A stage's scales: four bytes (this CTA's 128 columns) of each of 64 rows, a word each in shared memory.  Eight stages' loads are under way at once,
+        // since one takes as long as three stages' products.
+        unsigned turn = 0;
+        bool late = false;
+        for (int t = start; t < walk.count && !late; t += pairs) {
+            const TileAt at = walk.at(t);
+            const int first = (at.n * kTile + static_cast<int>(rank) * kHalf) / kPackBlock;
+            for (int s = 0; s < at.steps && !late; s += kScaleBatch) {
+                unsigned w[kScaleBatch][2];
+#pragma unroll
+                for (int j = 0; j < kScaleBatch; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = (at.first + s + j) * kStep + 32 * h + lane;
+                        const uint8_t *p = codes.scales + static_cast<long long>(row) * codes.blocks + first;
+                        w[j][h] = 0;
+                        if (s + j >= at.steps || row >= codes.rows) continue;
+                        if (codes.words && first + 4 <= codes.blocks) w[j][h] = __ldg(reinterpret_cast<const unsigned *>(p));
+                        else
+                            for (int b = 0; b < 4 && first + b < codes.blocks; ++b) w[j][h] |= static_cast<unsigned>(__ldg(p + b)) << (8 * b);
+                    }
+#pragma unroll
+                for (int j = 0; j < kScaleBatch; ++j) {
+                    if (s + j >= at.steps || late) break;
+                    const unsigned slot = turn % kScaleStages, round = turn / kScaleStages;
+                    late = round && !bar_wait(mma_smem(&scale_empty[slot]), (round - 1) & 1);
+                    const unsigned to = ring + Shape::scales + slot * kScaleBytes + 4 * lane;
+                    asm volatile("st.shared.u32 [%0], %1;\n\tst.shared.u32 [%0 + 128], %2;" :: "r"(to), "r"(w[j][0]), "r"(w[j][1]) : "memory");
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(mma_smem(&scale_full[slot]));
+                    ++turn;
+                }
+            }
+        }
+    } else if (warp >= kEpilogueWarp && warp < kEpilogueWarp + kEpilogueWarps) {
         Epilogue ep = given;
         const int quarter = warp & 3, half = (warp - kEpilogueWarp) >> 2;
-        unsigned tile = 0;
+        const unsigned lanes = tmem + (static_cast<unsigned>(quarter * 32) << 16) + half * kHalf, desk = ring + Shape::desks + (warp - kEpilogueWarp) * (Shape::desk_rows * kDeskRow);
+        unsigned sums = 0;
         bool late = false;
-        for (long long t = start; t < walk.count; t += pairs) {
+        if constexpr (WHOLE) if (blockIdx.x == 0 && threadIdx.x == 32 * kEpilogueWarp && given.done) *given.done = 0;
+        for (int t = start; t < walk.count; t += pairs) {
             const TileAt at = walk.at(t);
-            const unsigned buffer = tile & 1, use = tile >> 1;
-            if (at.steps) {
-                ++tile;
-                late = late || !bar_wait(mma_smem(&ready[buffer]), use & 1);
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            }
-            const int col = at.n * kTile + half * kHalf;
-            ep.begin(at.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane, at.split);
+            const int col = at.n * kTile + half * kHalf, row = at.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
+            if constexpr (WHOLE) {
+                float x[kHalf];
+#pragma unroll
+                for (int k = 0; k < kHalf; ++k) x[k] = 0.f;
 #pragma unroll 1
-            for (int c = 0; c < kHalf; c += 32) {
-                float x[32];
+                for (int s = 0; s < at.steps; s += Epilogue::kChunk) {
+                    const unsigned buffer = sums & 1;
+                    late = late || !bar_wait(mma_smem(&ready[buffer]), (sums >> 1) & 1);
+                    ++sums;
+                    __syncwarp();
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += 16) {
+                        float y[16];
+                        tmem_load16(lanes + buffer * kTile + c, y);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) x[c + k] += y[k];
+                    }
+                    __syncwarp();
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    if (lane == 0) bar_relaxed_leader(mma_smem(&drained[buffer]));
+                }
+                ep.take(x, row, col, late, desk);
+            } else {
+                const unsigned buffer = sums & 1;
+                if (at.steps) {
+                    late = late || !bar_wait(mma_smem(&ready[buffer]), (sums >> 1) & 1);
+                    ++sums;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                }
+                ep.begin(row, at.part);
+#pragma unroll 1
+                for (int c = 0; c < kHalf; c += 32) {
+                    float x[32];
+                    __syncwarp();
+                    if (at.steps) {
+                        tmem_load32(lanes + buffer * kTile + c, x);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = 0.f;
+                    }
+                    if (late) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = CUDART_NAN_F;
+                    }
+                    ep.template take<Shape::desk_rows>(x, col + c, desk);
+                }
                 __syncwarp();
                 if (at.steps) {
-                    tmem_load32(tmem + (static_cast<unsigned>(quarter * 32) << 16) + buffer * kTile + half * kHalf + c, x);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) x[k] = 0.f;
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    if (lane == 0) bar_relaxed_leader(mma_smem(&drained[buffer]));
                 }
-                if (late) {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) x[k] = CUDART_NAN_F;
-                }
-                ep.take(x, col + c);
             }
-            ep.end(col, at.split);
-            __syncwarp();
-            if (at.steps) {
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                if (lane == 0) bar_arrive_leader(mma_smem(&drained[buffer]));
+        }
+    } else if (CODES && warp >= kCodeWarp) {
+        if constexpr (CODES) {
+            // Two groups of four warps take the stages in turn, so that one's waiting hides behind the other's work.  A thread takes 64 columns of one row (a contraction
+            // step) of a stage: eight neighbouring lanes read and write eight different sixteenths of the swizzle's 1024 bytes.  About 250 instructions a stage
+            // and thread, in twice the 512 cycles that its products take.
+            const int k = threadIdx.x & 63, block = (threadIdx.x >> 6) & 1, group = (warp - kCodeWarp) / kCodeWarps;
+            unsigned turn = 0;
+            bool late = false;
+            for (int t = start; t < walk.count && !late; t += pairs) {
+                const TileAt at = walk.at(t);
+                for (int s = static_cast<int>((group + turn) & 1); s < at.steps; s += 2) {          // the group's stages of this tile
+                    const unsigned now = turn + s, slot = now % kStages, round = now / kStages, here = now % (2 * kCodeStages), of = now % kScaleStages;
+                    if (!bar_wait(mma_smem(&scale_full[of]), (now / kScaleStages) & 1) || !bar_wait(mma_smem(&code_full[here]), (now / (2 * kCodeStages)) & 1)) { late = true; break; }
+                    unsigned scales;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(scales) : "r"(ring + Shape::scales + of * kScaleBytes + 4 * k + 2 * block) : "memory");
+                    const unsigned from = code_ring + now % kCodeStages * kCodeBytes + k * 128, to = ring + slot * kStageBytes + kOperandBytes + block * 8192 + k * 128;
+                    uint4 c[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) c[j] = desk_get(from + (((block * 4 + j) ^ (k & 7)) << 4));
+                    if (round && !bar_wait(mma_smem(&empty[slot]), (round - 1) & 1)) { late = true; break; }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float u = scale_unit(j < 2 ? scales & 255u : scales >> 8);
+                        const uint2 p = codes_to_bf16(c[j].x, u), q = codes_to_bf16(c[j].y, u), r = codes_to_bf16(c[j].z, u), w = codes_to_bf16(c[j].w, u);
+                        desk_put(to + (((2 * j) ^ (k & 7)) << 4), make_uint4(p.x, p.y, q.x, q.y));
+                        desk_put(to + (((2 * j + 1) ^ (k & 7)) << 4), make_uint4(r.x, r.y, w.x, w.y));
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {                       // the codes' slots only now that their values have been used: the loads may be under way until then
+                        bar_arrive_leader(mma_smem(&full[slot]));
+                        bar_arrive(mma_smem(&code_empty[here]));
+                        bar_arrive(mma_smem(&scale_empty[of]));
+                    }
+                }
+                turn += at.steps;
             }
         }
     }

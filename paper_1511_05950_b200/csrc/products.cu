@@ -18,11 +18,10 @@ namespace {
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 int64_t div_up(int64_t x, int64_t by) { return (x + by - 1) / by; }
-int launched() { return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA; }
 
 constexpr int64_t kMaxRows = int64_t{1} << 26, kMaxWidth = int64_t{1} << 20, kMaxVocab = int64_t{1} << 28;
 constexpr int kPairs = 74;                                 // CTA pairs that the GPU holds: sizes of workspaces go by it, launches by the device
-constexpr int64_t kPieceBytes = int64_t{256} << 20;        // of G, or the hidden states' own size where that is more
+constexpr int64_t kPieceBytes = int64_t{1} << 30;          // of G, or the hidden states' own size where that is more
 
 // ---- a matrix for the loads ---------------------------------------------------------------------------------------------
 struct Matrix {
@@ -45,17 +44,18 @@ EncodeTiled encoder()
     return f;
 }
 
-// Blocks of 64 columns (128 bytes, swizzled) by box_rows rows; zeros outside the matrix.
-bool encode(CUtensorMap &map, const Matrix &m, int box_rows)
+// Boxes of 128 bytes (swizzled) by box_rows rows; zeros outside the matrix.
+bool encode(CUtensorMap &map, CUtensorMapDataType type, int size, const void *data, int64_t rows, int64_t cols, int64_t stride, int box_rows)
 {
     const EncodeTiled f = encoder();
     if (!f) return false;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(m.stride * 2)};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(kStep), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
-    return f(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16 *>(m.data), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride * size)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
+    return f(&map, type, 2, const_cast<void *>(data), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+bool encode(CUtensorMap &map, const Matrix &m, int box_rows) { return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.data, m.rows, m.cols, m.stride, box_rows); }
 
 int pairs_on_device()
 {
@@ -70,39 +70,62 @@ int pairs_on_device()
     return n;
 }
 
-// D = A B^T.  MN_A: A is given as k x m (else m x k), MN_B: B as k x n (else n x k).
-template <bool MN_A, bool MN_B, typename Epilogue>
-int launch_product(const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue, cudaStream_t st)
+int slots_on_device() { return std::min(pairs_on_device(), kPairs); }
+
+// dependent: the kernel may start while the one before it on the stream, one of this call's own, still runs, and waits for it itself.
+template <typename... K, typename... A>
+int launch(void (*kernel)(K...), int64_t blocks, int threads, int shared, bool dependent, cudaStream_t st, A... args)
 {
-    CUtensorMap map_a, map_b;
-    if (!encode(map_a, a, MN_A ? kStep : kHalf) || !encode(map_b, b, MN_B ? kStep : kHalf)) return PS_ERR_CUDA;
-    const auto kernel = softsync::mma_kernel<Epilogue, MN_A, MN_B>;
+    if (blocks < 1 || blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(shared);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? PS_OK : PS_ERR_CUDA;
+}
+
+// D = A B^T.  MN_A: A is given as k x m (else m x k), MN_B: B as k x n (else n x k).
+template <bool MN_A, bool MN_B, bool CODES = false, typename Epilogue>
+int launch_product(const CUtensorMap &map_a, const CUtensorMap &map_b, const MmaPlan &plan, const Epilogue &epilogue, bool dependent, cudaStream_t st, const softsync::CodesIn &codes = {})
+{
+    using Shape = softsync::MmaShape<CODES>;
+    const auto kernel = softsync::mma_kernel<Epilogue, MN_A, MN_B, CODES>;
     static std::atomic<bool> ready[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return PS_ERR_CUDA;
     if (!ready[device].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, softsync::kMmaShared) != cudaSuccess) return PS_ERR_CUDA;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::shared) != cudaSuccess) return PS_ERR_CUDA;
         ready[device].store(true, std::memory_order_relaxed);
     }
-    const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile) * plan.splits;
-    const int64_t pairs = std::min<int64_t>(tiles, pairs_on_device());
+    const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile);
+    if (tiles > 0x70000000) return PS_ERR_INVALID_ARG;
+    const int64_t pairs = plan.slots ? plan.slots : std::min<int64_t>(tiles, pairs_on_device());
     if (pairs < 1) return PS_ERR_CUDA;
-    kernel<<<static_cast<unsigned>(2 * pairs), softsync::kMmaThreads, softsync::kMmaShared, st>>>(map_a, map_b, plan, epilogue);
-    return launched();
+    return launch(kernel, 2 * pairs, Shape::threads, Shape::shared, dependent, st, map_a, map_b, plan, epilogue, codes);
+}
+template <bool MN_A, bool MN_B, typename Epilogue>
+int launch_product(const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue, bool dependent, cudaStream_t st)
+{
+    CUtensorMap map_a, map_b;
+    if (!encode(map_a, a, MN_A ? kStep : kHalf) || !encode(map_b, b, MN_B ? kStep : kHalf)) return PS_ERR_CUDA;
+    return launch_product<MN_A, MN_B>(map_a, map_b, plan, epilogue, dependent, st);
 }
 
-// Parts of the contraction, so that few tiles still fill the GPU: the number, at most 16 and a stage for each at least, with the least
-// of rounds x stages.
-int splits_of(int64_t tiles, int64_t steps)
+// The sums of a product whose last tiles are split, unless it is known that none are.
+int launch_split_sum(const MmaPlan &plan, const softsync::StoreTarget &target, cudaStream_t st)
 {
-    int best = 1;
-    int64_t cost = div_up(tiles, kPairs) * steps;
-    for (int s = 2; s <= 16 && s * 4 <= steps; ++s) {
-        const int64_t c = div_up(tiles * s, kPairs) * div_up(steps, s) + s;             // and the sums of each have to be read again
-        if (c < cost) { cost = c; best = s; }
-    }
-    return best;
+    const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile), rest = plan.live && !plan.live_is_k ? std::min<int64_t>(tiles, plan.slots - 1) : tiles % plan.slots;
+    if (!rest || (!plan.live && softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots) == 1)) return PS_OK;
+    return launch(softsync::split_sum_kernel, rest * (kTile / softsync::kSumRows), 256, 0, true, st, plan, target);
 }
+int64_t part_elements() { return int64_t{softsync::kMostParts} * kPairs * kTile * kTile; }
+
 int group_of(int64_t tiles_m) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(tiles_m, 16))); }
 
 // ---- workspaces --------------------------------------------------------------------------------------------------------
@@ -119,50 +142,46 @@ struct Places {
 
 bool matrix_aligned(const void *p, int64_t rows, int64_t stride) { return aligned_to(p, 16) && (rows <= 1 || stride % 8 == 0); }
 
+// The vocabulary in pieces: [first, vocab), the widest, whose exponentials the statistics' pass keeps, so that its logits are computed once; and those
+// before it, of `piece` columns each.
 struct HeadPlan : Places {
-    int64_t rows, width, vocab, rows_padded, width_padded, pieces, piece, tiles_n, parts;
+    int64_t rows, width, vocab, rows_padded, width_padded, first, piece, g_stride, parts, part_count;
     bool copy_head, copy_hidden;
-    int splits;                            // of dhidden's product
-    // statistics
-    float2 *stat = nullptr;
+    float2 *stat = nullptr, *norms = nullptr;
     float *picked = nullptr, *inverse = nullptr, *sum = nullptr;
     double *sums = nullptr;
+    unsigned *done = nullptr;
     int *order = nullptr, *place = nullptr, *live = nullptr;
     bf16 *hidden = nullptr, *head = nullptr;
-    // gradients
     bf16 *g = nullptr;
-    float *part = nullptr;
+    float *dhidden = nullptr, *split = nullptr;
     HeadPlan(const ps_head &h, bool grad, bool listed, void *p) : Places(p), rows(h.rows), width(h.width), vocab(h.vocab)
     {
         rows_padded = round_up(rows, kStep);
         width_padded = round_up(width, 8);
         copy_head = !matrix_aligned(h.head_dev, vocab, h.head_stride);
         copy_hidden = listed || !matrix_aligned(h.hidden_dev, rows, h.hidden_stride);
-        tiles_n = div_up(vocab, kTile);
-        parts = div_up(vocab, kHalf);
-        const int64_t budget = std::max(kPieceBytes, rows * width * 2);
-        const int64_t most = std::max<int64_t>(kTile, budget / (2 * rows_padded) / kTile * kTile);
-        pieces = div_up(vocab, most);
-        piece = std::min(most, round_up(div_up(vocab, pieces), kTile));
-        pieces = div_up(vocab, piece);
-        splits = splits_of(div_up(rows, kTile) * div_up(width, kTile), div_up(std::min(piece, vocab), kStep));
+        part_count = div_up(vocab, kHalf);
+        const int64_t most = std::max<int64_t>(kTile, std::max(kPieceBytes, rows * width * 2) / (2 * rows_padded) / kTile * kTile);
+        first = vocab > most ? round_up(vocab - most, kTile) : 0;
+        piece = first ? round_up(div_up(first, div_up(first, most)), kTile) : 0;
+        g_stride = round_up(std::max(piece, vocab - first), kTile);
         take(inverse, 1);
         take(sum, 1);
         take(live, 1);
+        take(done, 1);
         take(order, rows);
         take(place, rows);
         take(picked, rows);
-        take(sums, div_up(rows, 32));
+        take(norms, rows);
+        take(sums, div_up(rows, softsync::kJoinRows));
         if (copy_hidden) take(hidden, rows_padded * width_padded);
         if (copy_head) take(head, round_up(vocab, kStep) * width_padded);
-        const int64_t shared = bytes;                       // the statistics are done with before a piece of G is written
-        take(stat, parts * rows);
+        take(stat, part_count * rows);
         if (!grad) return;
-        const int64_t after_stat = bytes;
-        bytes = shared;
-        take(g, rows_padded * piece);
-        take(part, splits * rows * width_padded);
-        bytes = std::max(bytes, after_stat);
+        take(g, rows_padded * g_stride);
+        take(split, part_elements());
+        if (first) take(dhidden, rows * width_padded);
     }
 };
 
@@ -199,69 +218,91 @@ struct HeadCall {
     const int *order() const { return listed ? w.order : nullptr; }
     const int *live() const { return listed ? w.live : nullptr; }
 
-    int begin(const float *factors, float *zero_a, float *zero_b)
+    bool started = false;                  // a kernel of this call is under way
+    bool dependent() { const bool d = started; started = true; return d; }
+
+    int begin(const float *factors, float *zero_a, float *zero_b, void *dhidden)
     {
         int status = PS_OK;
-        if (listed) {
-            softsync::order_kernel<<<1, softsync::kOrderThreads, 0, st>>>(factors, static_cast<int>(h.rows), {w.order, w.place, w.live, w.inverse, w.sum, zero_a, zero_b});
-            status = launched();
+        if (listed)
+            status = launch(softsync::order_kernel, 1, softsync::kOrderThreads, 0, dependent(), st, factors, static_cast<int>(h.rows),
+                            softsync::OrderOut{w.order, w.place, w.live, w.inverse, w.sum, zero_a, zero_b});
+        softsync::GatherIn in{};
+        in.width = static_cast<int>(h.width); in.out_stride = static_cast<int>(w.width_padded);
+        if (status == PS_OK && w.copy_head) {
+            in.x = static_cast<const bf16 *>(h.head_dev); in.rows = static_cast<int>(h.vocab); in.stride = h.head_stride; in.out = w.head;
+            status = launch(softsync::gather_kernel, round_up(h.vocab, kStep), 128, 0, dependent(), st, in);
         }
-        const auto copy = [&](const void *from, int64_t rows, int64_t padded, int64_t stride, const int *ord, const int *n, bf16 *to) {
-            softsync::gather_kernel<<<static_cast<unsigned>(padded), 128, 0, st>>>(static_cast<const bf16 *>(from), static_cast<int>(rows), static_cast<int>(h.width), stride, ord, n,
-                                                                                  matrix_aligned(from, rows, stride), to, static_cast<int>(w.width_padded));
-            return launched();
-        };
-        if (status == PS_OK && w.copy_hidden) status = copy(h.hidden_dev, h.rows, w.rows_padded, h.hidden_stride, order(), live(), w.hidden);
-        if (status == PS_OK && w.copy_head) status = copy(h.head_dev, h.vocab, round_up(h.vocab, kStep), h.head_stride, nullptr, nullptr, w.head);
+        if (status == PS_OK && w.copy_hidden) {
+            in.x = static_cast<const bf16 *>(h.hidden_dev); in.rows = static_cast<int>(h.rows); in.stride = h.hidden_stride; in.out = w.hidden;
+            in.aligned = matrix_aligned(h.hidden_dev, h.rows, h.hidden_stride);
+            if (listed) { in.order = w.order; in.place = w.place; in.live = w.live; in.zeros = static_cast<bf16 *>(dhidden); }
+            status = launch(softsync::gather_kernel, w.rows_padded, 128, 0, dependent(), st, in);
+        }
         return status;
     }
-    int statistics(const float *weights, float *logp, float *lse, bool sums)
+    // stats: loss and sum of the weights, or null.  keep: the exponentials of the columns from w.first on.
+    int statistics(const float *weights, float *logp, float *lse, float *stats, bool keep)
     {
         softsync::StatsEpilogue ep{};
         ep.order = order(); ep.tokens = tokens; ep.rows = static_cast<int>(h.rows); ep.vocab = static_cast<int>(h.vocab); ep.live = live(); ep.scale = scale;
-        ep.parts = w.stat; ep.part_stride = h.rows; ep.picked = w.picked;
-        MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), live(), 0, 1, group_of(div_up(h.rows, kTile))};
-        const int status = launch_product<false, false>(hidden, head, plan, ep, st);
+        ep.parts = w.stat; ep.part_stride = h.rows; ep.picked = w.picked; ep.done = w.done;
+        if (keep) { ep.kept = reinterpret_cast<uint16_t *>(w.g); ep.kept_stride = w.g_stride; ep.first = static_cast<int>(w.first); }
+        const MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), live(), 0, 0, group_of(div_up(h.rows, kTile))};
+        const int status = launch_product<false, false>(hidden, head, plan, ep, dependent(), st);
         if (status != PS_OK) return status;
-        softsync::JoinIn in{w.stat, h.rows, static_cast<int>(w.parts), w.picked, tokens, order(), live(), weights, ep.rows, ep.vocab, scale, inv_temperature, logp, lse,
-                            sums ? w.sums : nullptr};
-        softsync::join_kernel<<<static_cast<unsigned>(div_up(h.rows, 32)), 32 * softsync::kJoinWarps, 0, st>>>(in);
-        return launched();
+        softsync::JoinIn in{};
+        in.parts = w.stat; in.part_stride = h.rows; in.count = static_cast<int>(w.part_count); in.picked = w.picked; in.tokens = tokens; in.order = order(); in.live = live();
+        in.weights = weights; in.rows = ep.rows; in.vocab = ep.vocab; in.scale = scale; in.inv_temperature = inv_temperature; in.logp = logp; in.lse = lse; in.norms = w.norms;
+        in.sums = w.sums; in.done = w.done; in.total = listed ? w.sum : nullptr; in.stats = stats;
+        return launch(softsync::join_kernel, div_up(h.rows, softsync::kJoinRows), softsync::kJoinThreads, 0, dependent(), st, in);
     }
-    // coef: of every row, or null for 1; alpha times *alpha_dev: of both gradients
+    // lse: of every row; null after statistics that kept.  coef: of every row, or null for 1; alpha times *alpha_dev: of both gradients.
     int gradients(const float *lse, const float *coef, float sign, float alpha, const float *alpha_dev, void *dhidden, void *dhead)
     {
-        int status = PS_OK;
-        const int rows = static_cast<int>(h.rows), width = static_cast<int>(h.width);
-        for (int64_t first = 0; first < h.vocab && status == PS_OK; first += w.piece) {
-            const int n = static_cast<int>(std::min(w.piece, h.vocab - first));
-            const Matrix entries{head.data + first * head.stride, n, h.width, head.stride};
-            softsync::GradEpilogue ge{};
-            ge.order = order(); ge.tokens = tokens; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live(); ge.scale = scale;
-            ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.piece;
-            MmaPlan plan{rows, n, width, live(), 0, 1, group_of(div_up(rows, kTile))};
-            if ((status = launch_product<false, false>(hidden, entries, plan, ge, st)) != PS_OK) break;
-            const Matrix g{w.g, w.rows_padded, n, w.piece};
-            if (dhidden) {
-                softsync::StoreEpilogue se{};
-                se.rows = rows; se.cols = width;
-                se.part = w.part; se.part_stride = w.width_padded; se.part_rows = h.rows * w.width_padded; se.add = first > 0;
-                MmaPlan p{rows, width, n, live(), 0, w.splits, group_of(div_up(rows, kTile))};
-                if ((status = launch_product<false, true>(g, entries, p, se, st)) != PS_OK) break;
+        const int rows = static_cast<int>(h.rows), width = static_cast<int>(h.width), slots = slots_on_device();
+        if (slots < 1) return PS_ERR_CUDA;
+        const int64_t pieces = 1 + (w.first ? div_up(w.first, w.piece) : 0);
+        for (int64_t k = 0; k < pieces; ++k) {                                  // the kept one first: the others take its place
+            const int64_t first = k ? (k - 1) * w.piece : w.first;
+            const int n = static_cast<int>(k ? std::min(w.piece, w.first - first) : h.vocab - first);
+            const Matrix entries{head.data + first * head.stride, n, h.width, head.stride}, g{w.g, w.rows_padded, n, w.g_stride};
+            int status;
+            if (k == 0 && !lse) {
+                softsync::KeptIn in{};
+                in.g = reinterpret_cast<uint4 *>(w.g); in.stride = w.g_stride / 8; in.first = static_cast<int>(first); in.width = n;
+                in.segments = static_cast<int>(div_up(n, softsync::kKeptColumns)); in.parts = w.stat; in.norms = w.norms; in.part_stride = h.rows; in.tokens = tokens;
+                in.order = order(); in.live = live(); in.coef = coef; in.sign = sign; in.scale = scale; in.rows = rows;
+                status = launch(softsync::kept_grad_kernel, w.rows_padded * in.segments, softsync::kKeptThreads, 0, dependent(), st, in);
+            } else {
+                softsync::GradEpilogue ge{};
+                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.live = live(); ge.scale = scale;
+                ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
+                const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(div_up(rows, kTile))};
+                status = launch_product<false, false>(hidden, entries, plan, ge, dependent(), st);
             }
-            if (dhead) {
+            if (status == PS_OK && dhidden) {
                 softsync::StoreEpilogue se{};
-                se.rows = n; se.cols = width; se.alpha = alpha; se.alpha_dev = alpha_dev;
-                se.out = static_cast<bf16 *>(dhead) + first * h.width; se.out_bf16 = 1; se.vectors = h.width % 8 == 0; se.stride = h.width;
-                MmaPlan p{n, width, rows, live(), 1, 1, group_of(div_up(n, kTile))};
-                status = launch_product<true, true>(g, hidden, p, se, st);
+                softsync::StoreTarget &t = se.target;
+                t.rows = rows; t.cols = width; t.live = live(); t.order = order(); t.alpha = alpha; t.alpha_dev = alpha_dev;
+                if (k == pieces - 1) { t.out = dhidden; t.out_bf16 = 1; t.vectors = width % 8 == 0; t.stride = width; }
+                t.sum = w.dhidden; t.sum_stride = w.width_padded; t.add = k > 0; t.parts = w.split;
+                const MmaPlan plan{rows, width, n, live(), 0, slots, group_of(div_up(rows, kTile))};
+                status = launch_product<false, true>(g, entries, plan, se, dependent(), st);
+                if (status == PS_OK) status = launch_split_sum(plan, t, st);
             }
+            if (status == PS_OK && dhead) {
+                softsync::StoreEpilogue se{};
+                softsync::StoreTarget &t = se.target;
+                t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = static_cast<bf16 *>(dhead) + first * h.width; t.out_bf16 = 1;
+                t.vectors = width % 8 == 0; t.stride = width; t.parts = w.split;
+                const MmaPlan plan{n, width, rows, live(), 1, slots, group_of(div_up(n, kTile))};
+                status = launch_product<true, true>(g, hidden, plan, se, dependent(), st);
+                if (status == PS_OK) status = launch_split_sum(plan, t, st);
+            }
+            if (status != PS_OK) return status;
         }
-        if (status != PS_OK || !dhidden) return status;
-        softsync::SplitSum in{w.part, w.width_padded, h.rows * w.width_padded, w.splits, listed ? w.place : nullptr, rows, width, alpha, alpha_dev, nullptr, 0, dhidden, 1,
-                              h.width % 8 == 0, h.width};
-        softsync::split_sum_kernel<<<static_cast<unsigned>(rows), 128, 0, st>>>(in);
-        return launched();
+        return PS_OK;
     }
 };
 
@@ -292,8 +333,8 @@ int ps_head_logprob(const ps_head *head, const float *weights_dev, float *logp_d
     if (!logp_dev || !lse_dev || !aligned_to(logp_dev, 4) || !aligned_to(lse_dev, 4) || !aligned_to(weights_dev, 4)) return PS_ERR_INVALID_ARG;
     HeadCall call(*head, false, weights_dev != nullptr, workspace_dev, static_cast<cudaStream_t>(stream));
     if (!workspace_dev || !aligned_to(workspace_dev, 256) || workspace_bytes < call.w.bytes) return PS_ERR_INVALID_ARG;
-    const int status = call.begin(weights_dev, logp_dev, lse_dev);
-    return status == PS_OK ? call.statistics(nullptr, logp_dev, lse_dev, false) : status;
+    const int status = call.begin(weights_dev, logp_dev, lse_dev, nullptr);
+    return status == PS_OK ? call.statistics(nullptr, logp_dev, lse_dev, nullptr, false) : status;
 }
 
 int ps_head_logprob_grad(const ps_head *head, const float *lse_dev, const float *dlogp_dev, void *dhidden_dev, void *dhead_dev, void *workspace_dev,
@@ -308,7 +349,7 @@ int ps_head_logprob_grad(const ps_head *head, const float *lse_dev, const float 
     if (!dhidden_dev && !dhead_dev) return PS_OK;
     HeadCall call(*head, true, true, workspace_dev, st);
     if (!workspace_dev || !aligned_to(workspace_dev, 256) || workspace_bytes < call.w.bytes) return PS_ERR_INVALID_ARG;
-    const int status = call.begin(dlogp_dev, nullptr, nullptr);
+    const int status = call.begin(dlogp_dev, nullptr, nullptr, dhidden_dev);
     return status == PS_OK ? call.gradients(lse_dev, dlogp_dev, -1.f, call.inv_temperature, nullptr, dhidden_dev, dhead_dev) : status;
 }
 
@@ -324,13 +365,11 @@ int ps_head_cross_entropy(const ps_head *head, const float *weights_dev, float *
     const bool grad = dhidden_dev || dhead_dev, listed = weights_dev != nullptr;
     HeadCall call(*head, grad, listed, workspace_dev, st);
     if (!workspace_dev || !aligned_to(workspace_dev, 256) || workspace_bytes < call.w.bytes) return PS_ERR_INVALID_ARG;
-    int status = call.begin(weights_dev, logp_dev, lse_dev);
-    if (status == PS_OK) status = call.statistics(weights_dev, logp_dev, lse_dev, true);
-    if (status != PS_OK) return status;
-    const int rows = static_cast<int>(head->rows);
-    softsync::loss_kernel<<<1, 256, 0, st>>>(call.w.sums, static_cast<int>(div_up(rows, 32)), listed ? call.w.sum : nullptr, rows, stats_dev);
-    if ((status = launched()) != PS_OK || !grad) return status;
-    return call.gradients(lse_dev, weights_dev, 1.f, listed ? call.inv_temperature : call.inv_temperature / static_cast<float>(rows), listed ? call.w.inverse : nullptr, dhidden_dev, dhead_dev);
+    int status = call.begin(weights_dev, logp_dev, lse_dev, dhidden_dev);
+    if (status == PS_OK) status = call.statistics(weights_dev, logp_dev, lse_dev, stats_dev, grad);
+    if (status != PS_OK || !grad) return status;
+    return call.gradients(nullptr, weights_dev, 1.f, listed ? call.inv_temperature : call.inv_temperature / static_cast<float>(head->rows), listed ? call.w.inverse : nullptr, dhidden_dev,
+                          dhead_dev);
 }
 
 }  // extern "C"
@@ -341,16 +380,13 @@ namespace {
 struct PackedPlan : Places {
     int64_t outs_padded, cols_padded;
     bool copy_dout;
-    int splits;
-    bf16 *dout = nullptr, *values = nullptr;
-    float *part = nullptr;
-    PackedPlan(const ps_packed_grad &a, void *p) : Places(p), outs_padded(round_up(a.outs, 8)), cols_padded(round_up(a.cols, 8))
+    bf16 *dout = nullptr;
+    float *split = nullptr;
+    PackedPlan(const ps_packed_grad &a, void *p) : Places(p), outs_padded(round_up(a.outs, 8)), cols_padded(round_up(a.cols, PS_PACK_BLOCK))
     {
         copy_dout = !matrix_aligned(a.dout_dev, a.rows, a.dout_stride);
-        splits = splits_of(div_up(a.outs, kTile) * div_up(a.cols, kTile), div_up(a.rows, kStep));
         if (copy_dout) take(dout, round_up(a.rows, kStep) * outs_padded);
-        take(values, a.rows * cols_padded);
-        if (splits > 1) take(part, splits * a.outs * cols_padded);
+        take(split, part_elements());
     }
 };
 
@@ -386,29 +422,28 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     const PackedPlan w(*a, workspace_dev);
     if (!workspace_dev || !aligned_to(workspace_dev, 256) || workspace_bytes < w.bytes) return PS_ERR_INVALID_ARG;
     const int rows = static_cast<int>(a->rows), outs = static_cast<int>(a->outs), cols = static_cast<int>(a->cols);
+    const int slots = slots_on_device();
+    if (slots < 1) return PS_ERR_CUDA;
     Matrix dout{static_cast<const bf16 *>(a->dout_dev), rows, outs, rows > 1 ? a->dout_stride : w.outs_padded};
     int status = PS_OK;
     if (w.copy_dout) {
-        softsync::gather_kernel<<<static_cast<unsigned>(round_up(rows, kStep)), 128, 0, st>>>(dout.data, rows, outs, a->dout_stride, nullptr, nullptr, 0, w.dout, static_cast<int>(w.outs_padded));
-        status = launched();
+        softsync::GatherIn in{};
+        in.x = dout.data; in.rows = rows; in.width = outs; in.stride = a->dout_stride; in.out = w.dout; in.out_stride = static_cast<int>(w.outs_padded);
+        status = launch(softsync::gather_kernel, round_up(rows, kStep), 128, 0, false, st, in);
         dout = Matrix{w.dout, rows, outs, w.outs_padded};
     }
-    if (status == PS_OK) status = ps_unpack8(a->codes_dev, a->scales_dev, rows, cols, w.values, PS_GRAD_BF16, w.cols_padded, stream);
     if (status != PS_OK) return status;
-    const Matrix values{w.values, rows, cols, w.cols_padded};
-    const int vectors = a->cols % 8 == 0 && aligned_to(a->gain_dev, 16), gain_bf16 = a->gain_dtype == PS_GRAD_BF16, out_bf16 = a->out_dtype == PS_GRAD_BF16;
+    CUtensorMap map_a, map_b;
+    if (!encode(map_a, dout, kStep) || !encode(map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a->codes_dev, rows, w.cols_padded, w.cols_padded, kStep)) return PS_ERR_CUDA;
     softsync::StoreEpilogue se{};
-    se.rows = outs; se.cols = cols; se.alpha = 1.f;
-    if (w.splits > 1) {
-        se.part = w.part; se.part_stride = w.cols_padded; se.part_rows = a->outs * w.cols_padded;
-    } else {
-        se.gain = a->gain_dev; se.gain_bf16 = gain_bf16; se.out = a->dweight_dev; se.out_bf16 = out_bf16; se.vectors = vectors; se.stride = cols;
-    }
-    const MmaPlan plan{outs, cols, rows, nullptr, 0, w.splits, group_of(div_up(outs, kTile))};
-    if ((status = launch_product<true, true>(dout, values, plan, se, st)) != PS_OK || w.splits == 1) return status;
-    softsync::SplitSum in{w.part, w.cols_padded, a->outs * w.cols_padded, w.splits, nullptr, outs, cols, 1.f, nullptr, a->gain_dev, gain_bf16, a->dweight_dev, out_bf16, vectors, cols};
-    softsync::split_sum_kernel<<<static_cast<unsigned>(outs), 128, 0, st>>>(in);
-    return launched();
+    softsync::StoreTarget &t = se.target;
+    t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = a->dweight_dev; t.out_bf16 = a->out_dtype == PS_GRAD_BF16;
+    t.vectors = a->cols % 8 == 0 && aligned_to(a->gain_dev, 16); t.stride = cols; t.parts = w.split;
+    const MmaPlan plan{outs, cols, rows, nullptr, 0, slots, group_of(div_up(outs, kTile))};
+    const int blocks = static_cast<int>(w.cols_padded / PS_PACK_BLOCK);
+    const softsync::CodesIn codes{a->scales_dev, rows, blocks, blocks % 4 == 0 && aligned_to(a->scales_dev, 4)};
+    status = launch_product<true, true, true>(map_a, map_b, plan, se, w.copy_dout, st, codes);
+    return status == PS_OK ? launch_split_sum(plan, t, st) : status;
 }
 
 }  // extern "C"

@@ -4,7 +4,7 @@ output matrix.
 Tolerances.  Products of bf16 values are exact in fp32.  A sum of K of them is off by at most (K / 16 + 16) 2^-23 of the sum of their magnitudes
 (16 at a time, each addition rounded or cut to 24 bits), which is at most |h| |w|: `products`.  The exponent's argument is rounded twice, the exponential
 has two units in the last place, the sums of a row are of 32 terms, then of 4 runs, then of its parts.  A gradient's G = a (p - 1[token]) is rounded to bf16 (half a step:
-2^-8) and has the error of p, which is zero below 2^-126; the sums over vocabulary or rows are products again; the result is rounded to bf16 once.
+2^-8) and has the error of p, which may come through 16 bits of its own (half a step 2^-11, zero below 2^-62); the sums over vocabulary or rows are products again; the result is rounded to bf16 once.
 """
 import ctypes as C
 import math
@@ -59,7 +59,7 @@ class Reference:
         g = p.clone()
         g[self.rows, self.t] -= 1
         a = a.double()[:, None] / self.temperature
-        off = a.abs() * (HALF * g.abs() + (2 * self.tol + 8 * EPS) * p + 2.0 ** -126)
+        off = a.abs() * (HALF * g.abs() + (2 * self.tol + 8 * EPS + 2.0 ** -11) * p + 2.0 ** -62)
         g, size = a * g, a.abs() * g.abs()
 
         def product(m, off, size, other, k):
