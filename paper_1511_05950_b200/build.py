@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsoftsync_ps.so")
 SOURCES = ["softsync_ps.cu", "tensor_list.cu", "token_loss.cu", "activations.cu", "products.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("update_kernels.cuh", "tensor_kernels.cuh", "token_kernels.cuh", "packed.cuh", "host_util.h", "units.cuh",
-                                             "norm_kernels.cuh", "mma_kernels.cuh", "head_kernels.cuh")] + \
+                                             "pack_kernels.cuh", "norm_kernels.cuh", "mma_kernels.cuh", "head_kernels.cuh")] + \
           [os.path.join(os.path.dirname(HERE), "include", h) for h in ("softsync_ps.h", "softsync_learn.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -2,13 +2,16 @@
 #include "../../include/softsync_learn.h"
 #include "host_util.h"
 #include "norm_kernels.cuh"
+#include "pack_kernels.cuh"
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 using softsync::aligned_to;
 using softsync::NormGradIn;
 using softsync::NormIn;
+using softsync::PackShape;
 using bf16 = __nv_bfloat16;
 
 namespace {
@@ -16,7 +19,6 @@ namespace {
 constexpr int64_t kMaxRows = 0x7fffffff, kMaxCols = int64_t{1} << 28;
 
 int64_t div_up(int64_t x, int64_t by) { return (x + by - 1) / by; }
-int launched() { return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA; }
 bool is_dtype(int t) { return t == PS_GRAD_FP32 || t == PS_GRAD_BF16; }
 int64_t size_of(int dtype) { return dtype == PS_GRAD_BF16 ? 2 : 4; }
 
@@ -29,14 +31,32 @@ bool vectors_ok(const void *p, int dtype, int64_t rows, int64_t stride) { return
 bool shape_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxCols; }
 bool packed_ok(const int8_t *codes, const uint8_t *scales) { return codes && scales && aligned_to(codes, 16); }
 
+// A launch for every so many rows as have fewer than 2^32 units (nearly always one).
+template <typename F>
+int over_rows(int64_t rows, int64_t cols, int64_t stride, bool aligned, F launch)
+{
+    PackShape shape;
+    shape.units = static_cast<int>(div_up(cols, PS_PACK_BLOCK) * (PS_PACK_BLOCK / softsync::kUnit));
+    shape.cols = static_cast<int>(cols);
+    shape.magic = ~uint64_t{0} / static_cast<uint64_t>(shape.units) + 1;
+    shape.stride = stride;
+    shape.aligned = aligned;
+    const int64_t block = softsync::kPackThreads * softsync::kPackTurns, most = ((int64_t{1} << 32) - block) / shape.units;
+    for (int64_t first = 0; first < rows; first += most) {
+        const int64_t count = std::min(most, rows - first) * shape.units;
+        shape.count = static_cast<unsigned>(count);
+        if (!launch(first, first * shape.units, shape, div_up(count, block))) return PS_ERR_CUDA;
+    }
+    return PS_OK;
+}
+
 template <typename T>
 int launch_norm(const NormIn &in, cudaStream_t st)
 {
     const int64_t units = div_up(in.cols, softsync::kUnit);
     const auto go = [&](auto kernel, int warps) {
         const int64_t blocks = warps == 1 ? div_up(in.rows, softsync::kNormRows) : in.rows;
-        kernel<<<static_cast<unsigned>(blocks), warps == 1 ? 32 * softsync::kNormRows : 32 * warps, 0, st>>>(in);
-        return launched();
+        return softsync::launch(kernel, blocks, warps == 1 ? 32 * softsync::kNormRows : 32 * warps, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
     };
     if (units <= 32) return go(softsync::rms_norm_kernel<T, 1, 1>, 1);
     if (units <= 64) return go(softsync::rms_norm_kernel<T, 1, 2>, 1);
@@ -45,52 +65,45 @@ int launch_norm(const NormIn &in, cudaStream_t st)
     if (units <= 512) return go(softsync::rms_norm_kernel<T, 4, 4>, 4);
     if (units <= 1024) return go(softsync::rms_norm_kernel<T, 8, 4>, 8);
     if (units <= 2048) return go(softsync::rms_norm_kernel<T, 16, 4>, 16);
-    softsync::rms_norm_long_kernel<T><<<static_cast<unsigned>(in.rows), softsync::kLongThreads, 0, st>>>(in);
-    return launched();
+    return softsync::launch(softsync::rms_norm_long_kernel<T>, in.rows, softsync::kLongThreads, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
 }
 
-// Blocks of the backward pass, and with them the parts that the gain's gradient is summed in.
-constexpr int64_t kGradBlocks = 592, kLongParts = 64;
+// Blocks of the backward pass, as many as are resident at once, and with them the parts that the gain's gradient is summed in.
+constexpr int64_t kSms = 148, kLongParts = 64;
 struct GradShape { int warps, units; int64_t blocks, parts; };
 GradShape grad_shape(int64_t rows, int64_t cols)
 {
     const int64_t units = div_up(cols, softsync::kUnit);
     const auto of = [&](int warps, int per) {
-        const int64_t groups = warps == 1 ? softsync::kNormRows : 1, blocks = std::min(div_up(rows, groups), kGradBlocks);
+        const int64_t groups = warps == 1 ? softsync::kNormRows : 1, blocks = std::min(div_up(rows, groups), kSms * (warps <= 4 ? 4 : warps == 8 ? 2 : 1));
         return GradShape{warps, per, blocks, blocks * groups};
     };
     if (units <= 32) return of(1, 1);
     if (units <= 64) return of(1, 2);
-    if (units <= 128) return of(1, 4);
     if (units <= 256) return of(4, 2);
     if (units <= 512) return of(8, 2);
     if (units <= 1024) return of(16, 2);
-    if (units <= 2048) return of(16, 4);
     return GradShape{0, 0, rows, std::min(rows, kLongParts)};
 }
 
-template <typename T>
+template <typename T, bool CODES>
 int launch_norm_grad(const NormGradIn &in, const GradShape &shape, cudaStream_t st)
 {
     const auto go = [&](auto kernel) {
-        kernel<<<static_cast<unsigned>(shape.blocks), shape.warps == 1 ? 32 * softsync::kNormRows : 32 * shape.warps, 0, st>>>(in);
-        return launched();
+        return softsync::launch(kernel, shape.blocks, shape.warps == 1 ? 32 * softsync::kNormRows : 32 * shape.warps, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
     };
     switch (shape.warps * 8 + shape.units) {
-    case 1 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 1, 1>);
-    case 1 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 1, 2>);
-    case 1 * 8 + 4: return go(softsync::rms_norm_grad_kernel<T, 1, 4>);
-    case 4 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 4, 2>);
-    case 8 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 8, 2>);
-    case 16 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 16, 2>);
-    case 16 * 8 + 4: return go(softsync::rms_norm_grad_kernel<T, 16, 4>);
+    case 1 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 1, 1, CODES>);
+    case 1 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 1, 2, CODES>);
+    case 4 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 4, 2, CODES>);
+    case 8 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 8, 2, CODES>);
+    case 16 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 16, 2, CODES>);
     }
-    softsync::rms_norm_grad_long_kernel<T><<<static_cast<unsigned>(in.rows), softsync::kLongThreads, 0, st>>>(in);
-    int status = launched();
-    if (status != PS_OK || !in.parts) return status;
+    if (!softsync::launch(softsync::rms_norm_grad_long_kernel<T, CODES>, in.rows, softsync::kLongThreads, 0, true, st, in)) return PS_ERR_CUDA;
+    if (!in.parts) return PS_OK;
     const dim3 grid(static_cast<unsigned>(div_up(div_up(in.cols, softsync::kUnit), 128)), static_cast<unsigned>(shape.parts));
-    softsync::gain_grad_long_kernel<T><<<grid, 128, 0, st>>>(in);
-    return launched();
+    softsync::gain_grad_long_kernel<T, CODES><<<grid, 128, 0, st>>>(in);
+    return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA;
 }
 
 }  // namespace
@@ -102,12 +115,11 @@ int ps_pack8(const void *x_dev, int dtype, int64_t rows, int64_t cols, int64_t r
     if (!is_dtype(dtype) || !shape_ok(rows, cols)) return PS_ERR_INVALID_ARG;
     if (rows == 0) return PS_OK;
     if (!rows_ok(x_dev, dtype, rows, cols, row_stride) || !packed_ok(codes_dev, scales_dev)) return PS_ERR_INVALID_ARG;
-    const int64_t blocks = div_up(rows * (div_up(cols, PS_PACK_BLOCK) * (PS_PACK_BLOCK / softsync::kUnit)), softsync::kPackThreads * softsync::kPackTurns);
-    if (blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
     const auto go = [&](auto *x) {
-        softsync::pack_kernel<<<static_cast<unsigned>(blocks), softsync::kPackThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-            x, rows, static_cast<int>(cols), row_stride, reinterpret_cast<uint2 *>(codes_dev), scales_dev, vectors_ok(x_dev, dtype, rows, row_stride));
-        return launched();
+        return over_rows(rows, cols, row_stride, vectors_ok(x_dev, dtype, rows, row_stride), [&](int64_t first, int64_t unit, const PackShape &shape, int64_t blocks) {
+            return softsync::launch(softsync::pack_kernel<std::remove_cv_t<std::remove_pointer_t<decltype(x)>>>, blocks, softsync::kPackThreads, 0, true, static_cast<cudaStream_t>(stream),
+                                    x + first * row_stride, shape, reinterpret_cast<uint2 *>(codes_dev) + unit, scales_dev + unit / 4);
+        });
     };
     return dtype == PS_GRAD_BF16 ? go(static_cast<const bf16 *>(x_dev)) : go(static_cast<const float *>(x_dev));
 }
@@ -117,12 +129,11 @@ int ps_unpack8(const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows,
     if (!is_dtype(dtype) || !shape_ok(rows, cols)) return PS_ERR_INVALID_ARG;
     if (rows == 0) return PS_OK;
     if (!rows_ok(out_dev, dtype, rows, cols, row_stride) || !packed_ok(codes_dev, scales_dev)) return PS_ERR_INVALID_ARG;
-    const int64_t blocks = div_up(rows * (div_up(cols, PS_PACK_BLOCK) * (PS_PACK_BLOCK / softsync::kUnit)), softsync::kPackThreads * softsync::kPackTurns);
-    if (blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
     const auto go = [&](auto *out) {
-        softsync::unpack_kernel<<<static_cast<unsigned>(blocks), softsync::kPackThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-            reinterpret_cast<const uint2 *>(codes_dev), scales_dev, rows, static_cast<int>(cols), out, row_stride, vectors_ok(out_dev, dtype, rows, row_stride));
-        return launched();
+        return over_rows(rows, cols, row_stride, vectors_ok(out_dev, dtype, rows, row_stride), [&](int64_t first, int64_t unit, const PackShape &shape, int64_t blocks) {
+            return softsync::launch(softsync::unpack_kernel<std::remove_pointer_t<decltype(out)>>, blocks, softsync::kPackThreads, 0, true, static_cast<cudaStream_t>(stream),
+                                    reinterpret_cast<const uint2 *>(codes_dev) + unit, scales_dev + unit / 4, shape, out + first * row_stride);
+        });
     };
     return dtype == PS_GRAD_BF16 ? go(static_cast<bf16 *>(out_dev)) : go(static_cast<float *>(out_dev));
 }
@@ -197,10 +208,11 @@ int ps_rms_norm_grad(const ps_norm_grad *a, void *workspace_dev, int64_t workspa
     in.aligned = vectors_ok(a->dout_dev, a->dtype, a->rows, a->dout_stride) && vectors_ok(a->dx_dev, a->dtype, a->rows, a->cols) &&
                  vectors_ok(a->dtotal_dev, a->dtype, a->rows, a->dtotal_dev ? a->dtotal_stride : 0) && vectors_ok(a->total_dev, a->dtype, a->rows, a->total_dev ? a->total_stride : 0) &&
                  aligned_to(a->gain_dev, 16);
-    const int status = a->dtype == PS_GRAD_BF16 ? launch_norm_grad<bf16>(in, shape, st) : launch_norm_grad<float>(in, shape, st);
+    const auto go = [&](auto codes) { return a->dtype == PS_GRAD_BF16 ? launch_norm_grad<bf16, codes>(in, shape, st) : launch_norm_grad<float, codes>(in, shape, st); };
+    const int status = in.codes ? go(std::true_type{}) : go(std::false_type{});
     if (status != PS_OK || !a->dgain_dev) return status;
-    softsync::gain_grad_kernel<<<static_cast<unsigned>(div_up(a->cols, 32)), 32 * softsync::kGainWarps, 0, st>>>(in.parts, static_cast<int>(shape.parts), in.cols, a->dgain_dev, in.gain_bf16);
-    return launched();
+    return softsync::launch(softsync::gain_grad_kernel, div_up(a->cols, 32), 32 * softsync::kGainWarps, 0, true, st, in.parts, static_cast<int>(shape.parts), in.cols, a->dgain_dev,
+                            in.gain_bf16) ? PS_OK : PS_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -3,8 +3,7 @@
 // A pair of CTAs takes a tile of 256 x 256 (tcgen05.mma, cta_group::2): each holds 128 rows of A and 128 of B for every 64 steps of the contraction,
 // in a ring of stages that one thread a CTA fills with TMA loads (128-byte swizzle), and 128 rows of the sums in its tensor memory,
 // twice, so that the epilogue of one tile runs under the products of the next.  Warps: 0 loads, 1 issues the products (of the pair's first CTA), 2 owns
-// the tensor memory, 4 to 11 are the epilogue (a warp reaches the 32 lanes of its number modulo 4; two warps share them, half the columns each), 12
-// to 19, where B comes as 8-bit codes, turn them into bf16, with the scales that warp 3 brings.
+// the tensor memory, 4 to 11 are the epilogue (a warp reaches the 32 lanes of its number modulo 4; two warps share them, half the columns each).
 //
 // Either operand may lie with its contraction dimension contiguous (rows of A, "K-major") or with its other one (A given as its transpose,
 // "MN-major"): the loads bring blocks of 64 x 64 as they lie, and the descriptors tell the tensor cores.
@@ -24,21 +23,11 @@ namespace softsync {
 
 constexpr int kTile = 256, kHalf = 128, kStep = 64;          // tile, rows of an operand in a CTA, contraction steps of a stage
 constexpr int kOperandBytes = kHalf * kStep * 2, kStageBytes = 2 * kOperandBytes;
-constexpr int kCodeBytes = kHalf * kStep;                      // a stage's codes
-constexpr int kEpilogueWarp = 4, kEpilogueWarps = 8, kCodeWarp = 12, kCodeWarps = 4, kCodeGroups = 2;
-constexpr int kScaleWarp = 3, kScaleStages = 16, kScaleBatch = 8, kScaleBytes = 4 * kStep;
+constexpr int kEpilogueWarp = 4, kEpilogueWarps = 8, kMmaThreads = 32 * (kEpilogueWarp + kEpilogueWarps);
+constexpr int kStages = 6;
+constexpr int kDeskBytes = 4096;                               // where an epilogue warp turns a row a lane into neighbouring lanes of a row
+constexpr int kDesks = kStages * kStageBytes, kMmaShared = kDesks + kEpilogueWarps * kDeskBytes + 1024;       // aligned to the swizzle's 1024 bytes
 constexpr int kMmaWaitLimit = 1 << 20;                         // polls of up to a microsecond
-
-constexpr int kDeskRow = 128;                                  // bytes of a row where an epilogue warp turns a row a lane into neighbouring lanes of a row
-
-// Threads, stages and shared memory of a kernel, with B as bf16 or as codes (with a ring of their own).
-template <bool CODES> struct MmaShape {
-    static constexpr int threads = 32 * (kCodeWarp + (CODES ? kCodeWarps * kCodeGroups : 0)), stages = CODES ? 5 : 6, code_stages = CODES ? 5 : 0;
-    static constexpr int desk_rows = CODES ? 16 : 32;
-    static constexpr int code_ring = stages * kStageBytes, desks = code_ring + code_stages * kCodeBytes;      // places in shared memory
-    static constexpr int scales = desks + kEpilogueWarps * desk_rows * kDeskRow;
-    static constexpr int shared = scales + (CODES ? kScaleStages * kScaleBytes : 0) + 1024;         // aligned to the swizzle's 1024 bytes
-};
 
 // ---- instructions ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ unsigned mma_smem(const void *p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
@@ -63,15 +52,9 @@ __device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
-// At the pair's first CTA.  A release in the cluster's scope waits for everything that the SM has under way: 1600 cycles where a stage takes 512.  It
-// is not needed: what the barrier guards is each CTA's own shared or tensor memory, read by that SM's tensor core, so the writer's proxy fence and a
-// release in the CTA's scope put it in order, and reads of tensor memory have fences of their own.
+// At the pair's first CTA.  Relaxed: a release in the cluster's scope waits for everything that the SM has under way (1600 cycles, where a stage takes 512), and what is
+// put in order here, reads of tensor memory, has fences of its own.
 __device__ __forceinline__ void bar_arrive_leader(unsigned bar)
-{
-    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" :: "r"(leaders(bar)) : "memory");
-}
-__device__ __forceinline__ void bar_relaxed_leader(unsigned bar)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(leaders(bar)) : "memory");
 }
@@ -90,14 +73,6 @@ __device__ __forceinline__ void tile_load(unsigned dst, const CUtensorMap *map, 
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(leader_bar) : "memory");
 }
-// Into this CTA alone, with its own barrier.
-__device__ __forceinline__ void code_load(unsigned dst, const CUtensorMap *map, int x, int y, unsigned bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void mma_pair(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -351,10 +326,8 @@ struct GradEpilogue {
             norm = row_normaliser(norms, lse, r, at);
         }
     }
-    template <int ROWS>
     __device__ __forceinline__ void take(float (&x)[32], int col, unsigned desk)
     {
-        static_assert(ROWS == 32, "a desk of whole rows");
         if (col >= width) return;
         const unsigned at = static_cast<unsigned>(tok - col);
         const bool picked = __any_sync(kAllLanes, at < 32u);
@@ -441,36 +414,30 @@ struct StoreEpilogue {
         factor = target.factor();
         part = p >= 0 ? target.parts + (static_cast<long long>(p) * kTile + row0 % kTile) * kTile : nullptr;
     }
-    template <int ROWS>
     __device__ __forceinline__ void take(float (&x)[32], int col, unsigned desk)
     {
         if (col >= target.cols) return;
         const int lane = threadIdx.x & 31, unit = lane & 3;
 #pragma unroll
-        for (int first = 0; first < 32; first += ROWS) {
-            if (ROWS == 32 || lane / ROWS == first / ROWS) {
+        for (int k = 0; k < 8; ++k)
+            desk_put(desk + wide_place(lane, k), make_uint4(__float_as_uint(x[4 * k]), __float_as_uint(x[4 * k + 1]), __float_as_uint(x[4 * k + 2]), __float_as_uint(x[4 * k + 3])));
+        __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    desk_put(desk + wide_place(lane % ROWS, k), make_uint4(__float_as_uint(x[4 * k]), __float_as_uint(x[4 * k + 1]), __float_as_uint(x[4 * k + 2]), __float_as_uint(x[4 * k + 3])));
+        for (int j = 0; j < 4; ++j) {
+            const int r = j * 8 + (lane >> 2), to = __shfl_sync(kAllLanes, place, r);
+            const uint4 a = desk_get(desk + wide_place(r, 2 * unit)), b = desk_get(desk + wide_place(r, 2 * unit + 1));
+            if (to < 0) continue;
+            if (part) {
+                uint4 *p = reinterpret_cast<uint4 *>(part + r * kTile + col % kTile + 8 * unit);
+                p[0] = a;
+                p[1] = b;
+                continue;
             }
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < ROWS / 8; ++j) {
-                const int d = j * 8 + (lane >> 2), r = first + d, to = __shfl_sync(kAllLanes, place, r);
-                const uint4 a = desk_get(desk + wide_place(d, 2 * unit)), b = desk_get(desk + wide_place(d, 2 * unit + 1));
-                if (to < 0) continue;
-                if (part) {
-                    uint4 *p = reinterpret_cast<uint4 *>(part + r * kTile + col % kTile + 8 * unit);
-                    p[0] = a;
-                    p[1] = b;
-                    continue;
-                }
-                Unit u{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w), __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z),
-                        __uint_as_float(b.w)}};
-                target.store(row0 + r, to, col + 8 * unit, u, factor);
-            }
-            __syncwarp();
+            Unit u{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w), __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z),
+                    __uint_as_float(b.w)}};
+            target.store(row0 + r, to, col + 8 * unit, u, factor);
         }
+        __syncwarp();
     }
 };
 
@@ -499,47 +466,20 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const __grid_constant__ 
     target.store(row, target.order ? target.order[row] : row, n * kTile + lane * kUnit, u, factor);
 }
 
-// ---- B from 8-bit codes ------------------------------------------------------------------------------------------------
-struct CodesIn {
-    const uint8_t *scales;                // `blocks` for each row
-    int rows, blocks, words;              // words: four neighbours can be read as one
-};
-
-// Four codes as bf16, exactly: with b = code + 128 in the low byte of the float 2^23 + b, minus 2^23 + 128, times the unit.  (One multiply-add of both
-// would overflow for units above 2^104.)
-__device__ __forceinline__ uint2 codes_to_bf16(unsigned codes, float unit)
-{
-    const unsigned b = codes ^ 0x80808080u;
-    float v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440 + k)) - 8388736.f) * unit;
-    return make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-}
-
 // ---- the kernel --------------------------------------------------------------------------------------------------------
-template <typename Epilogue, bool MN_A, bool MN_B, bool CODES>
-__global__ void __cluster_dims__(2) __launch_bounds__(MmaShape<CODES>::threads, 1)
-mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmaPlan plan, const __grid_constant__ Epilogue given,
-           const __grid_constant__ CodesIn codes)
+template <typename Epilogue, bool MN_A, bool MN_B>
+__global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1)
+mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmaPlan plan, const __grid_constant__ Epilogue given)
 {
-    static_assert(!CODES || MN_B, "codes lie with their columns contiguous");
-    using Shape = MmaShape<CODES>;
-    constexpr int kStages = Shape::stages, kCodeStages = Shape::code_stages;
     constexpr bool WHOLE = Epilogue::kChunk < (1 << 30);      // the epilogue takes all 128 columns of a row at once
     extern __shared__ unsigned char raw_ring[];
-    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], ready[2], drained[2], code_full[CODES ? 2 * kCodeStages : 1], code_empty[CODES ? 2 * kCodeStages : 1];
-    __shared__ __align__(8) unsigned long long scale_full[CODES ? kScaleStages : 1], scale_empty[CODES ? kScaleStages : 1];
+    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], ready[2], drained[2];
     __shared__ unsigned tmem_base;
-    const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u, code_ring = ring + Shape::code_ring;
+    const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = pair_rank();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            bar_init(mma_smem(&full[s]), CODES ? 1 + 2 * kCodeWarps : 1);   // with codes: the copies, and four warps in each CTA
-            bar_init(mma_smem(&empty[s]), 1);
-        }
-        if constexpr (CODES) for (int s = 0; s < 2 * kCodeStages; ++s) { bar_init(mma_smem(&code_full[s]), 1); bar_init(mma_smem(&code_empty[s]), kCodeWarps); }
-        if constexpr (CODES) for (int s = 0; s < kScaleStages; ++s) { bar_init(mma_smem(&scale_full[s]), 1); bar_init(mma_smem(&scale_empty[s]), kCodeWarps); }
+        for (int s = 0; s < kStages; ++s) { bar_init(mma_smem(&full[s]), 1); bar_init(mma_smem(&empty[s]), 1); }
         for (int b = 0; b < 2; ++b) { bar_init(mma_smem(&ready[b]), 1); bar_init(mma_smem(&drained[b]), 2 * kEpilogueWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_a) : "memory");
@@ -568,20 +508,12 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
                 for (int s = 0; s < at.steps; ++s, ++turn) {
                     const unsigned slot = turn % kStages, round = turn / kStages;
                     const int x = (at.first + s) * kStep;
-                    if constexpr (CODES) {
-                        // Twice as many barriers as slots: each serves one of the two groups that turn the codes, which so knows its last phase.
-                        const unsigned here = turn % (2 * kCodeStages), before = turn - kCodeStages, at_bar = before % (2 * kCodeStages);
-                        if (turn >= kCodeStages && !bar_wait(mma_smem(&code_empty[at_bar]), (before / (2 * kCodeStages)) & 1)) { late = true; break; }
-                        bar_expect(mma_smem(&code_full[here]), kCodeBytes);
-                        code_load(code_ring + turn % kCodeStages * kCodeBytes, &map_b, yb, x, mma_smem(&code_full[here]));
-                    }
                     if (round && !bar_wait(mma_smem(&empty[slot]), (round - 1) & 1)) { late = true; break; }
                     const unsigned bar = leaders(mma_smem(&full[slot])), a = ring + slot * kStageBytes, b = a + kOperandBytes;
-                    if (rank == 0) bar_expect(mma_smem(&full[slot]), CODES ? 2 * kOperandBytes : 2 * kStageBytes);
+                    if (rank == 0) bar_expect(mma_smem(&full[slot]), 2 * kStageBytes);
                     if constexpr (MN_A) { tile_load(a, &map_a, ya, x, bar); tile_load(a + 8192, &map_a, ya + 64, x, bar); }
                     else tile_load(a, &map_a, x, ya, bar);
-                    if constexpr (CODES) continue;
-                    else if constexpr (MN_B) { tile_load(b, &map_b, yb, x, bar); tile_load(b + 8192, &map_b, yb + 64, x, bar); }
+                    if constexpr (MN_B) { tile_load(b, &map_b, yb, x, bar); tile_load(b + 8192, &map_b, yb + 64, x, bar); }
                     else tile_load(b, &map_b, x, yb, bar);
                 }
             }
@@ -590,8 +522,6 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
                 late = late || !bar_wait(mma_smem(&empty[k % kStages]), (k / kStages) & 1);
                 if (late && rank == 0) bar_wait(mma_smem(&full[k % kStages]), (k / kStages) & 1);
             }
-            if constexpr (CODES)                           // the last may have been asked for before its stage was free
-                for (unsigned k = turn > kCodeStages ? turn - kCodeStages : 0; late && k <= turn; ++k) bar_wait(mma_smem(&code_full[k % (2 * kCodeStages)]), (k / (2 * kCodeStages)) & 1);
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -621,45 +551,10 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
                 if (!late && at.steps) commit_pair(mma_smem(&ready[buffer]));
             }
         }
-    } else if (CODES && warp == kScaleWarp) {
-        // A stage's scales: four bytes (this CTA's 128 columns) of each of 64 rows, a word each in shared memory.  Eight stages' loads are under way at once,
-        // since one takes as long as three stages' products.
-        unsigned turn = 0;
-        bool late = false;
-        for (int t = start; t < walk.count && !late; t += pairs) {
-            const TileAt at = walk.at(t);
-            const int first = (at.n * kTile + static_cast<int>(rank) * kHalf) / kPackBlock;
-            for (int s = 0; s < at.steps && !late; s += kScaleBatch) {
-                unsigned w[kScaleBatch][2];
-#pragma unroll
-                for (int j = 0; j < kScaleBatch; ++j)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int row = (at.first + s + j) * kStep + 32 * h + lane;
-                        const uint8_t *p = codes.scales + static_cast<long long>(row) * codes.blocks + first;
-                        w[j][h] = 0;
-                        if (s + j >= at.steps || row >= codes.rows) continue;
-                        if (codes.words && first + 4 <= codes.blocks) w[j][h] = __ldg(reinterpret_cast<const unsigned *>(p));
-                        else
-                            for (int b = 0; b < 4 && first + b < codes.blocks; ++b) w[j][h] |= static_cast<unsigned>(__ldg(p + b)) << (8 * b);
-                    }
-#pragma unroll
-                for (int j = 0; j < kScaleBatch; ++j) {
-                    if (s + j >= at.steps || late) break;
-                    const unsigned slot = turn % kScaleStages, round = turn / kScaleStages;
-                    late = round && !bar_wait(mma_smem(&scale_empty[slot]), (round - 1) & 1);
-                    const unsigned to = ring + Shape::scales + slot * kScaleBytes + 4 * lane;
-                    asm volatile("st.shared.u32 [%0], %1;\n\tst.shared.u32 [%0 + 128], %2;" :: "r"(to), "r"(w[j][0]), "r"(w[j][1]) : "memory");
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(mma_smem(&scale_full[slot]));
-                    ++turn;
-                }
-            }
-        }
-    } else if (warp >= kEpilogueWarp && warp < kEpilogueWarp + kEpilogueWarps) {
+    } else if (warp >= kEpilogueWarp) {
         Epilogue ep = given;
         const int quarter = warp & 3, half = (warp - kEpilogueWarp) >> 2;
-        const unsigned lanes = tmem + (static_cast<unsigned>(quarter * 32) << 16) + half * kHalf, desk = ring + Shape::desks + (warp - kEpilogueWarp) * (Shape::desk_rows * kDeskRow);
+        const unsigned lanes = tmem + (static_cast<unsigned>(quarter * 32) << 16) + half * kHalf, desk = ring + kDesks + (warp - kEpilogueWarp) * kDeskBytes;
         unsigned sums = 0;
         bool late = false;
         if constexpr (WHOLE) if (blockIdx.x == 0 && threadIdx.x == 32 * kEpilogueWarp && given.done) *given.done = 0;
@@ -686,7 +581,7 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
                     }
                     __syncwarp();
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    if (lane == 0) bar_relaxed_leader(mma_smem(&drained[buffer]));
+                    if (lane == 0) bar_arrive_leader(mma_smem(&drained[buffer]));
                 }
                 ep.take(x, row, col, late, desk);
             } else {
@@ -711,51 +606,13 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
 #pragma unroll
                         for (int k = 0; k < 32; ++k) x[k] = CUDART_NAN_F;
                     }
-                    ep.template take<Shape::desk_rows>(x, col + c, desk);
+                    ep.take(x, col + c, desk);
                 }
                 __syncwarp();
                 if (at.steps) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    if (lane == 0) bar_relaxed_leader(mma_smem(&drained[buffer]));
+                    if (lane == 0) bar_arrive_leader(mma_smem(&drained[buffer]));
                 }
-            }
-        }
-    } else if (CODES && warp >= kCodeWarp) {
-        if constexpr (CODES) {
-            // Two groups of four warps take the stages in turn, so that one's waiting hides behind the other's work.  A thread takes 64 columns of one row (a contraction
-            // step) of a stage: eight neighbouring lanes read and write eight different sixteenths of the swizzle's 1024 bytes.  About 250 instructions a stage
-            // and thread, in twice the 512 cycles that its products take.
-            const int k = threadIdx.x & 63, block = (threadIdx.x >> 6) & 1, group = (warp - kCodeWarp) / kCodeWarps;
-            unsigned turn = 0;
-            bool late = false;
-            for (int t = start; t < walk.count && !late; t += pairs) {
-                const TileAt at = walk.at(t);
-                for (int s = static_cast<int>((group + turn) & 1); s < at.steps; s += 2) {          // the group's stages of this tile
-                    const unsigned now = turn + s, slot = now % kStages, round = now / kStages, here = now % (2 * kCodeStages), of = now % kScaleStages;
-                    if (!bar_wait(mma_smem(&scale_full[of]), (now / kScaleStages) & 1) || !bar_wait(mma_smem(&code_full[here]), (now / (2 * kCodeStages)) & 1)) { late = true; break; }
-                    unsigned scales;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(scales) : "r"(ring + Shape::scales + of * kScaleBytes + 4 * k + 2 * block) : "memory");
-                    const unsigned from = code_ring + now % kCodeStages * kCodeBytes + k * 128, to = ring + slot * kStageBytes + kOperandBytes + block * 8192 + k * 128;
-                    uint4 c[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) c[j] = desk_get(from + (((block * 4 + j) ^ (k & 7)) << 4));
-                    if (round && !bar_wait(mma_smem(&empty[slot]), (round - 1) & 1)) { late = true; break; }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float u = scale_unit(j < 2 ? scales & 255u : scales >> 8);
-                        const uint2 p = codes_to_bf16(c[j].x, u), q = codes_to_bf16(c[j].y, u), r = codes_to_bf16(c[j].z, u), w = codes_to_bf16(c[j].w, u);
-                        desk_put(to + (((2 * j) ^ (k & 7)) << 4), make_uint4(p.x, p.y, q.x, q.y));
-                        desk_put(to + (((2 * j + 1) ^ (k & 7)) << 4), make_uint4(r.x, r.y, w.x, w.y));
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {                       // the codes' slots only now that their values have been used: the loads may be under way until then
-                        bar_arrive_leader(mma_smem(&full[slot]));
-                        bar_arrive(mma_smem(&code_empty[here]));
-                        bar_arrive(mma_smem(&scale_empty[of]));
-                    }
-                }
-                turn += at.steps;
             }
         }
     }

@@ -70,6 +70,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
 {
     __shared__ float part[2][32];
     constexpr int T_ROW = 32 * WARPS;
+    wait_for_earlier();
+    let_next_start();
     const int tid = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x;
     const long long row = WARPS == 1 ? static_cast<long long>(blockIdx.x) * kNormRows + (threadIdx.x >> 5) : blockIdx.x;
     if (row >= in.rows) return;                            // a whole warp, and no barrier in that form
@@ -126,6 +128,8 @@ template <typename T>
 __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(const __grid_constant__ NormIn in)
 {
     __shared__ double part[kLongThreads / 32];
+    wait_for_earlier();
+    let_next_start();
     const long long row = blockIdx.x;
     const T *x = static_cast<const T *>(in.x) + row * in.x_stride, *res = static_cast<const T *>(in.residual) + (in.residual ? row * in.residual_stride : 0);
     T *total = static_cast<T *>(in.total) + (in.total ? row * in.total_stride : 0);
@@ -187,24 +191,26 @@ struct NormGradIn {
 };
 
 // n of one unit, from the codes or from the total.
-template <typename T>
-struct KeptUnit {
-    RawUnit<T> raw;
+template <typename T, bool CODES> struct KeptUnit;
+template <typename T> struct KeptUnit<T, true> {
     uint2 codes;
     unsigned scale;
+    __device__ __forceinline__ void load(const NormGradIn &in, long long row, int unit, int)
+    {
+        const int units = (in.cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
+        codes = __ldcs(in.codes + row * units + unit);
+        scale = __ldcs(in.scales + row * (units / 4) + unit / 4);
+    }
+    __device__ __forceinline__ Unit values(float) const { return unpack_unit(codes, scale); }
+};
+template <typename T> struct KeptUnit<T, false> {
+    RawUnit<T> raw;
     __device__ __forceinline__ void load(const NormGradIn &in, long long row, int unit, int left)
     {
-        if (in.codes) {
-            const int units = (in.cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
-            codes = __ldcs(in.codes + row * units + unit);
-            scale = __ldcs(in.scales + row * (units / 4) + unit / 4);
-        } else {
-            load_unit(raw, static_cast<const T *>(in.total) + row * in.total_stride + unit * kUnit, left, in.aligned && left >= kUnit);
-        }
+        load_unit(raw, static_cast<const T *>(in.total) + row * in.total_stride + unit * kUnit, left, in.aligned && left >= kUnit);
     }
-    __device__ __forceinline__ Unit values(const NormGradIn &in, float rstd) const
+    __device__ __forceinline__ Unit values(float rstd) const
     {
-        if (in.codes) return unpack_unit(codes, scale);
         Unit u = raw.values();
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) u.v[k] *= rstd;
@@ -212,13 +218,36 @@ struct KeptUnit {
     }
 };
 
+// What a thread loads of one row.
+template <typename T, int WARPS, int UNITS, bool CODES>
+struct GradRow {
+    RawUnit<T> dout[UNITS], dtotal[UNITS];
+    KeptUnit<T, CODES> kept[UNITS];
+    float rstd;
+    __device__ __forceinline__ void load(const NormGradIn &in, long long row, int tid)
+    {
+        const T *d = static_cast<const T *>(in.dout) + row * in.dout_stride, *t = static_cast<const T *>(in.dtotal) + (in.dtotal ? row * in.dtotal_stride : 0);
+        rstd = in.rstd[row];
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int unit = j * 32 * WARPS + tid, left = in.cols - unit * kUnit;
+            if (left <= 0) continue;
+            load_unit(dout[j], d + unit * kUnit, left, in.aligned && left >= kUnit);
+            kept[j].load(in, row, unit, left);
+            if (in.dtotal) load_unit(dtotal[j], t + unit * kUnit, left, in.aligned && left >= kUnit);
+        }
+    }
+};
+
 // g = dout gain, dx = dtotal + r (g - n mean(g n)), and each block's part of dgain = sum of dout n over its rows: rows are dealt out in turn, so
-// the parts, and their sum in the next kernel, have a fixed order.
-template <typename T, int WARPS, int UNITS>
-__global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_norm_grad_kernel(const __grid_constant__ NormGradIn in)
+// the parts, and their sum in the next kernel, have a fixed order.  The next row's loads are under way while a row waits for its sum.
+template <typename T, int WARPS, int UNITS, bool CODES>
+__global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, WARPS <= 4 ? 4 : WARPS == 8 ? 2 : 1) rms_norm_grad_kernel(const __grid_constant__ NormGradIn in)
 {
     __shared__ float part[2][32];
     constexpr int T_ROW = 32 * WARPS, GROUPS = WARPS == 1 ? kNormRows : 1;
+    wait_for_earlier();
+    let_next_start();
     const int tid = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x, group = WARPS == 1 ? threadIdx.x >> 5 : 0;
     Unit acc[UNITS];
 #pragma unroll
@@ -226,29 +255,22 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) acc[j].v[k] = 0.f;
     int slot = 0;
-    for (long long row = static_cast<long long>(blockIdx.x) * GROUPS + group; row < in.rows; row += static_cast<long long>(gridDim.x) * GROUPS, slot ^= 1) {
-        const T *dout = static_cast<const T *>(in.dout) + row * in.dout_stride;
-        const T *dtotal = static_cast<const T *>(in.dtotal) + (in.dtotal ? row * in.dtotal_stride : 0);
-        RawUnit<T> d[UNITS], t[UNITS];
-        KeptUnit<T> kept[UNITS];
-        const float r = in.rstd[row];
-#pragma unroll
-        for (int j = 0; j < UNITS; ++j) {
-            const int unit = j * T_ROW + tid, left = in.cols - unit * kUnit;
-            if (left > 0) {
-                load_unit(d[j], dout + unit * kUnit, left, in.aligned && left >= kUnit);
-                kept[j].load(in, row, unit, left);
-                if (in.dtotal) load_unit(t[j], dtotal + unit * kUnit, left, in.aligned && left >= kUnit);
-            }
-        }
+    const long long step = static_cast<long long>(gridDim.x) * GROUPS;
+    long long row = static_cast<long long>(blockIdx.x) * GROUPS + group;
+    GradRow<T, WARPS, UNITS, CODES> next;
+    if (row < in.rows) next.load(in, row, tid);
+    for (; row < in.rows; row += step, slot ^= 1) {
+        const float r = next.rstd;
         Unit g[UNITS], n[UNITS];
+        RawUnit<T> more[UNITS];
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
             const int unit = j * T_ROW + tid, left = in.cols - unit * kUnit;
             if (left <= 0) continue;
-            g[j] = d[j].values();
-            n[j] = kept[j].values(in, r);
+            g[j] = next.dout[j].values();
+            n[j] = next.kept[j].values(r);
+            more[j] = next.dtotal[j];
             const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, in.aligned && left >= kUnit);
             float s = 0.f;
 #pragma unroll
@@ -259,6 +281,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
             }
             sum += s;
         }
+        if (row + step < in.rows) next.load(in, row + step, tid);
         const float mean = row_sum<WARPS>(sum, part, slot) / static_cast<float>(in.cols);
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
@@ -268,9 +291,9 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) dx.v[k] = r * fmaf(-n[j].v[k], mean, g[j].v[k]);
             if (in.dtotal) {
-                const Unit more = t[j].values();
+                const Unit m = more[j].values();
 #pragma unroll
-                for (int k = 0; k < kUnit; ++k) dx.v[k] += more.v[k];
+                for (int k = 0; k < kUnit; ++k) dx.v[k] += m.v[k];
             }
             store_unit(static_cast<T *>(in.dx) + row * in.cols + col, dx, left, in.aligned && left >= kUnit);
         }
@@ -286,19 +309,21 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
 }
 
 // Longer rows: dout and the kept values are read twice (the second time mostly from the L2); the gain's gradient is a kernel of its own.
-template <typename T>
+template <typename T, bool CODES>
 __global__ void __launch_bounds__(kLongThreads) rms_norm_grad_long_kernel(const __grid_constant__ NormGradIn in)
 {
     __shared__ double part[kLongThreads / 32];
+    wait_for_earlier();
+    let_next_start();
     const long long row = blockIdx.x;
     const float r = in.rstd[row];
     const auto values = [&](int unit, int left, Unit &g, Unit &n) {
         RawUnit<T> d;
-        KeptUnit<T> kept;
+        KeptUnit<T, CODES> kept;
         load_unit(d, static_cast<const T *>(in.dout) + row * in.dout_stride + unit * kUnit, left, in.aligned && left >= kUnit);
         kept.load(in, row, unit, left);
         g = d.values();
-        n = kept.values(in, r);
+        n = kept.values(r);
         const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, in.aligned && left >= kUnit);
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) g.v[k] *= gain.v[k];
@@ -334,18 +359,20 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_grad_long_kernel(const 
         store_unit(static_cast<T *>(in.dx) + row * in.cols + col, dx, left, in.aligned && left >= kUnit);
     }
 }
-template <typename T>
+template <typename T, bool CODES>
 __global__ void __launch_bounds__(128) gain_grad_long_kernel(const __grid_constant__ NormGradIn in)
 {
+    wait_for_earlier();
+    let_next_start();
     const int unit = static_cast<int>(blockIdx.x) * 128 + static_cast<int>(threadIdx.x), left = in.cols - unit * kUnit;
     if (left <= 0) return;
     Unit acc{};
     for (long long row = blockIdx.y; row < in.rows; row += gridDim.y) {
         RawUnit<T> d;
-        KeptUnit<T> kept;
+        KeptUnit<T, CODES> kept;
         load_unit(d, static_cast<const T *>(in.dout) + row * in.dout_stride + unit * kUnit, left, in.aligned && left >= kUnit);
         kept.load(in, row, unit, left);
-        const Unit g = d.values(), n = kept.values(in, in.rstd[row]);
+        const Unit g = d.values(), n = kept.values(in.rstd[row]);
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) acc.v[k] = fmaf(g.v[k], n.v[k], acc.v[k]);
     }
@@ -359,6 +386,8 @@ constexpr int kGainWarps = 16;
 __global__ void __launch_bounds__(32 * kGainWarps) gain_grad_kernel(const float *parts, int count, int cols, void *dgain, int is_bf16)
 {
     __shared__ float sums[kGainWarps][32];
+    wait_for_earlier();
+    let_next_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = static_cast<int>(blockIdx.x) * 32 + lane;
     float s = 0.f;
     if (col < cols)
@@ -369,55 +398,6 @@ __global__ void __launch_bounds__(32 * kGainWarps) gain_grad_kernel(const float 
     for (int k = 1; k < kGainWarps; ++k) s += sums[k][lane];
     if (is_bf16) static_cast<__nv_bfloat16 *>(dgain)[col] = __float2bfloat16_rn(s);
     else static_cast<float *>(dgain)[col] = s;
-}
-
-// ---- packing and unpacking ---------------------------------------------------------------------------------------------
-// One unit a thread and turn, kPackTurns of them under way; a row's units are padded to whole blocks.  Bound by HBM.
-constexpr int kPackThreads = 256, kPackTurns = 4;
-template <typename T>
-__global__ void __launch_bounds__(kPackThreads) pack_kernel(const T *x, long long rows, int cols, long long stride, uint2 *codes, uint8_t *scales, int aligned)
-{
-    const int units = (cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
-    const long long count = rows * units, base = static_cast<long long>(blockIdx.x) * (kPackThreads * kPackTurns) + threadIdx.x;
-    RawUnit<T> raw[kPackTurns];
-#pragma unroll
-    for (int j = 0; j < kPackTurns; ++j) {
-        const long long at = base + j * kPackThreads;
-        const long long row = at / units;
-        const int col = static_cast<int>(at - row * units) * kUnit, left = at < count ? cols - col : 0;
-        load_unit(raw[j], x + (left > 0 ? row * stride + col : 0), left, aligned && left >= kUnit);
-    }
-#pragma unroll
-    for (int j = 0; j < kPackTurns; ++j) {
-        const long long at = base + j * kPackThreads;
-        unsigned scale;
-        const uint2 c = pack_unit(raw[j].values(), scale);
-        if (at < count) {
-            codes[at] = c;
-            if ((at & 3) == 0) scales[at >> 2] = static_cast<uint8_t>(scale);
-        }
-    }
-}
-template <typename T>
-__global__ void __launch_bounds__(kPackThreads) unpack_kernel(const uint2 *codes, const uint8_t *scales, long long rows, int cols, T *out, long long stride, int aligned)
-{
-    const int units = (cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
-    const long long count = rows * units, base = static_cast<long long>(blockIdx.x) * (kPackThreads * kPackTurns) + threadIdx.x;
-    uint2 c[kPackTurns];
-    unsigned s[kPackTurns];
-#pragma unroll
-    for (int j = 0; j < kPackTurns; ++j) {
-        const long long at = base + j * kPackThreads;
-        if (at < count) { c[j] = __ldcs(codes + at); s[j] = __ldcs(scales + (at >> 2)); }
-    }
-#pragma unroll
-    for (int j = 0; j < kPackTurns; ++j) {
-        const long long at = base + j * kPackThreads;
-        if (at >= count) break;
-        const long long row = at / units;
-        const int col = static_cast<int>(at - row * units) * kUnit, left = cols - col;
-        if (left > 0) store_unit(out + row * stride + col, unpack_unit(c[j], s[j]), left, aligned && left >= kUnit);
-    }
 }
 
 }  // namespace softsync

@@ -44,18 +44,17 @@ EncodeTiled encoder()
     return f;
 }
 
-// Boxes of 128 bytes (swizzled) by box_rows rows; zeros outside the matrix.
-bool encode(CUtensorMap &map, CUtensorMapDataType type, int size, const void *data, int64_t rows, int64_t cols, int64_t stride, int box_rows)
+// Blocks of 64 columns (128 bytes, swizzled) by box_rows rows; zeros outside the matrix.
+bool encode(CUtensorMap &map, const Matrix &m, int box_rows)
 {
     const EncodeTiled f = encoder();
     if (!f) return false;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride * size)};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
-    return f(&map, type, 2, const_cast<void *>(data), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(m.stride * 2)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(kStep), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
+    return f(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16 *>(m.data), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-bool encode(CUtensorMap &map, const Matrix &m, int box_rows) { return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.data, m.rows, m.cols, m.stride, box_rows); }
 
 int pairs_on_device()
 {
@@ -72,49 +71,31 @@ int pairs_on_device()
 
 int slots_on_device() { return std::min(pairs_on_device(), kPairs); }
 
-// dependent: the kernel may start while the one before it on the stream, one of this call's own, still runs, and waits for it itself.
 template <typename... K, typename... A>
-int launch(void (*kernel)(K...), int64_t blocks, int threads, int shared, bool dependent, cudaStream_t st, A... args)
+int start(void (*kernel)(K...), int64_t blocks, int threads, int shared, bool dependent, cudaStream_t st, const A &...args)
 {
-    if (blocks < 1 || blocks > 0x7fffffff) return PS_ERR_INVALID_ARG;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = static_cast<size_t>(shared);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = dependent ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? PS_OK : PS_ERR_CUDA;
+    return softsync::launch(kernel, blocks, threads, shared, dependent, st, args...) ? PS_OK : PS_ERR_CUDA;
 }
 
 // D = A B^T.  MN_A: A is given as k x m (else m x k), MN_B: B as k x n (else n x k).
-template <bool MN_A, bool MN_B, bool CODES = false, typename Epilogue>
-int launch_product(const CUtensorMap &map_a, const CUtensorMap &map_b, const MmaPlan &plan, const Epilogue &epilogue, bool dependent, cudaStream_t st, const softsync::CodesIn &codes = {})
+template <bool MN_A, bool MN_B, typename Epilogue>
+int launch_product(const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue, bool dependent, cudaStream_t st)
 {
-    using Shape = softsync::MmaShape<CODES>;
-    const auto kernel = softsync::mma_kernel<Epilogue, MN_A, MN_B, CODES>;
+    CUtensorMap map_a, map_b;
+    if (!encode(map_a, a, MN_A ? kStep : kHalf) || !encode(map_b, b, MN_B ? kStep : kHalf)) return PS_ERR_CUDA;
+    const auto kernel = softsync::mma_kernel<Epilogue, MN_A, MN_B>;
     static std::atomic<bool> ready[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return PS_ERR_CUDA;
     if (!ready[device].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::shared) != cudaSuccess) return PS_ERR_CUDA;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, softsync::kMmaShared) != cudaSuccess) return PS_ERR_CUDA;
         ready[device].store(true, std::memory_order_relaxed);
     }
     const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile);
     if (tiles > 0x70000000) return PS_ERR_INVALID_ARG;
     const int64_t pairs = plan.slots ? plan.slots : std::min<int64_t>(tiles, pairs_on_device());
     if (pairs < 1) return PS_ERR_CUDA;
-    return launch(kernel, 2 * pairs, Shape::threads, Shape::shared, dependent, st, map_a, map_b, plan, epilogue, codes);
-}
-template <bool MN_A, bool MN_B, typename Epilogue>
-int launch_product(const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue, bool dependent, cudaStream_t st)
-{
-    CUtensorMap map_a, map_b;
-    if (!encode(map_a, a, MN_A ? kStep : kHalf) || !encode(map_b, b, MN_B ? kStep : kHalf)) return PS_ERR_CUDA;
-    return launch_product<MN_A, MN_B>(map_a, map_b, plan, epilogue, dependent, st);
+    return start(kernel, 2 * pairs, softsync::kMmaThreads, softsync::kMmaShared, dependent, st, map_a, map_b, plan, epilogue);
 }
 
 // The sums of a product whose last tiles are split, unless it is known that none are.
@@ -122,7 +103,7 @@ int launch_split_sum(const MmaPlan &plan, const softsync::StoreTarget &target, c
 {
     const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile), rest = plan.live && !plan.live_is_k ? std::min<int64_t>(tiles, plan.slots - 1) : tiles % plan.slots;
     if (!rest || (!plan.live && softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots) == 1)) return PS_OK;
-    return launch(softsync::split_sum_kernel, rest * (kTile / softsync::kSumRows), 256, 0, true, st, plan, target);
+    return start(softsync::split_sum_kernel, rest * (kTile / softsync::kSumRows), 256, 0, true, st, plan, target);
 }
 int64_t part_elements() { return int64_t{softsync::kMostParts} * kPairs * kTile * kTile; }
 
@@ -225,19 +206,19 @@ struct HeadCall {
     {
         int status = PS_OK;
         if (listed)
-            status = launch(softsync::order_kernel, 1, softsync::kOrderThreads, 0, dependent(), st, factors, static_cast<int>(h.rows),
+            status = start(softsync::order_kernel, 1, softsync::kOrderThreads, 0, dependent(), st, factors, static_cast<int>(h.rows),
                             softsync::OrderOut{w.order, w.place, w.live, w.inverse, w.sum, zero_a, zero_b});
         softsync::GatherIn in{};
         in.width = static_cast<int>(h.width); in.out_stride = static_cast<int>(w.width_padded);
         if (status == PS_OK && w.copy_head) {
             in.x = static_cast<const bf16 *>(h.head_dev); in.rows = static_cast<int>(h.vocab); in.stride = h.head_stride; in.out = w.head;
-            status = launch(softsync::gather_kernel, round_up(h.vocab, kStep), 128, 0, dependent(), st, in);
+            status = start(softsync::gather_kernel, round_up(h.vocab, kStep), 128, 0, dependent(), st, in);
         }
         if (status == PS_OK && w.copy_hidden) {
             in.x = static_cast<const bf16 *>(h.hidden_dev); in.rows = static_cast<int>(h.rows); in.stride = h.hidden_stride; in.out = w.hidden;
             in.aligned = matrix_aligned(h.hidden_dev, h.rows, h.hidden_stride);
             if (listed) { in.order = w.order; in.place = w.place; in.live = w.live; in.zeros = static_cast<bf16 *>(dhidden); }
-            status = launch(softsync::gather_kernel, w.rows_padded, 128, 0, dependent(), st, in);
+            status = start(softsync::gather_kernel, w.rows_padded, 128, 0, dependent(), st, in);
         }
         return status;
     }
@@ -255,7 +236,7 @@ struct HeadCall {
         in.parts = w.stat; in.part_stride = h.rows; in.count = static_cast<int>(w.part_count); in.picked = w.picked; in.tokens = tokens; in.order = order(); in.live = live();
         in.weights = weights; in.rows = ep.rows; in.vocab = ep.vocab; in.scale = scale; in.inv_temperature = inv_temperature; in.logp = logp; in.lse = lse; in.norms = w.norms;
         in.sums = w.sums; in.done = w.done; in.total = listed ? w.sum : nullptr; in.stats = stats;
-        return launch(softsync::join_kernel, div_up(h.rows, softsync::kJoinRows), softsync::kJoinThreads, 0, dependent(), st, in);
+        return start(softsync::join_kernel, div_up(h.rows, softsync::kJoinRows), softsync::kJoinThreads, 0, dependent(), st, in);
     }
     // lse: of every row; null after statistics that kept.  coef: of every row, or null for 1; alpha times *alpha_dev: of both gradients.
     int gradients(const float *lse, const float *coef, float sign, float alpha, const float *alpha_dev, void *dhidden, void *dhead)
@@ -273,7 +254,7 @@ struct HeadCall {
                 in.g = reinterpret_cast<uint4 *>(w.g); in.stride = w.g_stride / 8; in.first = static_cast<int>(first); in.width = n;
                 in.segments = static_cast<int>(div_up(n, softsync::kKeptColumns)); in.parts = w.stat; in.norms = w.norms; in.part_stride = h.rows; in.tokens = tokens;
                 in.order = order(); in.live = live(); in.coef = coef; in.sign = sign; in.scale = scale; in.rows = rows;
-                status = launch(softsync::kept_grad_kernel, w.rows_padded * in.segments, softsync::kKeptThreads, 0, dependent(), st, in);
+                status = start(softsync::kept_grad_kernel, w.rows_padded * in.segments, softsync::kKeptThreads, 0, dependent(), st, in);
             } else {
                 softsync::GradEpilogue ge{};
                 ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.live = live(); ge.scale = scale;
@@ -380,12 +361,13 @@ namespace {
 struct PackedPlan : Places {
     int64_t outs_padded, cols_padded;
     bool copy_dout;
-    bf16 *dout = nullptr;
+    bf16 *dout = nullptr, *values = nullptr;
     float *split = nullptr;
     PackedPlan(const ps_packed_grad &a, void *p) : Places(p), outs_padded(round_up(a.outs, 8)), cols_padded(round_up(a.cols, PS_PACK_BLOCK))
     {
         copy_dout = !matrix_aligned(a.dout_dev, a.rows, a.dout_stride);
         if (copy_dout) take(dout, round_up(a.rows, kStep) * outs_padded);
+        take(values, a.rows * cols_padded);
         take(split, part_elements());
     }
 };
@@ -429,20 +411,20 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     if (w.copy_dout) {
         softsync::GatherIn in{};
         in.x = dout.data; in.rows = rows; in.width = outs; in.stride = a->dout_stride; in.out = w.dout; in.out_stride = static_cast<int>(w.outs_padded);
-        status = launch(softsync::gather_kernel, round_up(rows, kStep), 128, 0, false, st, in);
+        status = start(softsync::gather_kernel, round_up(rows, kStep), 128, 0, false, st, in);
         dout = Matrix{w.dout, rows, outs, w.outs_padded};
     }
     if (status != PS_OK) return status;
-    CUtensorMap map_a, map_b;
-    if (!encode(map_a, dout, kStep) || !encode(map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a->codes_dev, rows, w.cols_padded, w.cols_padded, kStep)) return PS_ERR_CUDA;
+    // The codes' values go through memory: turned into bf16 under way (four to eight more warps, from a ring of codes to the tensor cores' one) they took the shared memory's
+    // bandwidth from the products (8192 x 8192 x 2048: 285 us in all, against 10 and 180).
+    if ((status = ps_unpack8(a->codes_dev, a->scales_dev, rows, cols, w.values, PS_GRAD_BF16, w.cols_padded, stream)) != PS_OK) return status;
+    const Matrix values{w.values, rows, cols, w.cols_padded};
     softsync::StoreEpilogue se{};
     softsync::StoreTarget &t = se.target;
     t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = a->dweight_dev; t.out_bf16 = a->out_dtype == PS_GRAD_BF16;
     t.vectors = a->cols % 8 == 0 && aligned_to(a->gain_dev, 16); t.stride = cols; t.parts = w.split;
     const MmaPlan plan{outs, cols, rows, nullptr, 0, slots, group_of(div_up(outs, kTile))};
-    const int blocks = static_cast<int>(w.cols_padded / PS_PACK_BLOCK);
-    const softsync::CodesIn codes{a->scales_dev, rows, blocks, blocks % 4 == 0 && aligned_to(a->scales_dev, 4)};
-    status = launch_product<true, true, true>(map_a, map_b, plan, se, w.copy_dout, st, codes);
+    status = launch_product<true, true>(dout, values, plan, se, true, st);
     return status == PS_OK ? launch_split_sum(plan, t, st) : status;
 }
 

@@ -12,6 +12,11 @@ constexpr int kUnit = 8;                  // elements
 constexpr int kPackBlock = 32;            // columns that share a scale
 constexpr unsigned kAllLanes = 0xffffffffu;
 
+// A kernel of these waits for the one before it on the stream before it touches memory, and lets the next one start: launched as dependent, kernels prepare themselves
+// under the end of their predecessor.
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---- eight elements ----------------------------------------------------------------------------------------------------
 struct Unit { float v[kUnit]; };
 
