@@ -18,6 +18,7 @@
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace softsync {
 
@@ -127,31 +128,47 @@ struct MmaPlan {
     int slots;                            // pairs that work at once, where the last tiles may be split along the contraction; else 0
     int group;                            // row tiles whose turns come before the next column tile's
 };
+// How the operands lie: MN-major or K-major.
+template <bool A, bool B> struct Lying { static constexpr bool mn_a = A, mn_b = B; };
 
 // Into how many parts the last `rest` tiles (fewer than slots) are split along their `steps`, so that they fill the GPU.  In steps of 0.4 us: a round
 // takes its steps and about 6 for filling and draining the pipeline; the parts are summed by a kernel of its own (8, and 0.2 for each part's 256 KB
 // written and read).
 constexpr int kMostParts = 3;             // times slots: room in the workspace
-__host__ __device__ inline int split_count(int rest, int steps, int slots)
+constexpr int kSplitChoices = 11;
+__host__ __device__ inline int split_choice(int j)
 {
-    constexpr int tried[10] = {2, 3, 4, 6, 8, 12, 16, 24, 37, 74};
-    int best = 1, cost = 5 * (steps + 6);
-    if (steps < 16) return 1;
-#pragma unroll
-    for (int j = 0; j < 10; ++j) {
-        const int s = tried[j];
-        if (s * 4 > steps || rest * s > kMostParts * slots) continue;
-        const int c = 5 * ((rest * s + slots - 1) / slots * ((steps + s - 1) / s + 6) + 8) + rest * s;
-        if (c < cost) { cost = c; best = s; }
-    }
-    return best;
+    constexpr int tried[kSplitChoices] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 37, 74};
+    return tried[j];
+}
+__host__ __device__ inline int split_cost(int s, int rest, int steps, int slots)
+{
+    if (s == 1) return 5 * (steps + 6);
+    if (steps < 16 || s * 4 > steps || rest * s > kMostParts * slots) return 0x7fffffff;
+    return 5 * ((rest * s + slots - 1) / slots * ((steps + s - 1) / s + 6) + 8) + rest * s;
+}
+inline int split_count(int rest, int steps, int slots)
+{
+    int best = 0;
+    for (int j = 1; j < kSplitChoices; ++j)
+        if (split_cost(split_choice(j), rest, steps, slots) < split_cost(split_choice(best), rest, steps, slots)) best = j;
+    return split_choice(best);
+}
+// The same by a warp, a choice a lane (one by one they took 0.4 us): the first of the cheapest.
+__device__ __forceinline__ int warp_split_count(int rest, int steps, int slots)
+{
+    const int lane = threadIdx.x & 31, j = lane < kSplitChoices ? lane : 0;
+    constexpr unsigned long long packed = 1ull | 2ull << 7 | 3ull << 14 | 4ull << 21 | 6ull << 28 | 8ull << 35 | 12ull << 42 | 16ull << 49 | 24ull << 56;
+    const int s = j < 9 ? static_cast<int>(packed >> (7 * j) & 127) : j == 9 ? 37 : 74;
+    const unsigned cost = static_cast<unsigned>(split_cost(s, rest, steps, slots)), least = __reduce_min_sync(kAllLanes, cost);
+    return __shfl_sync(kAllLanes, s, __ffs(static_cast<int>(__ballot_sync(kAllLanes, cost == least))) - 1);
 }
 
 struct TileAt { int m, n, part, first, steps; };             // tile indices, number of the part (-1: the whole tile), and its stages of the contraction
 
 struct TileWalk {
     int tiles_m, tiles_n, all_steps, splits, group, whole, count;        // fewer than 2^31 items: the host sees to that
-    __device__ __forceinline__ TileWalk(const MmaPlan &p)
+    __device__ __forceinline__ explicit TileWalk(const MmaPlan &p)          // by whole warps
     {
         const int live = p.live ? *p.live : 0, m = p.live && !p.live_is_k ? live : p.m, k = p.live && p.live_is_k ? live : p.k;
         tiles_m = (m + kTile - 1) / kTile;
@@ -162,7 +179,7 @@ struct TileWalk {
         splits = 1;
         if (!p.slots) return;
         const int rest = static_cast<int>(static_cast<unsigned>(count) % static_cast<unsigned>(p.slots));
-        if (!rest || (splits = split_count(rest, all_steps, p.slots)) == 1) return;
+        if (!rest || (splits = warp_split_count(rest, all_steps, p.slots)) == 1) return;
         whole = count - rest;
         count = whole + rest * splits;
     }
@@ -441,123 +458,127 @@ struct StoreEpilogue {
     }
 };
 
-// The split tiles' parts added up, in order.  A block takes eight rows of a tile, a warp one, a lane a unit of eight columns.
-constexpr int kSumRows = 8;
-__global__ void __launch_bounds__(256) split_sum_kernel(const __grid_constant__ MmaPlan plan, const __grid_constant__ StoreTarget target)
+// One product of a launch: operands, extents, and what becomes of it.
+template <typename Epilogue>
+struct alignas(64) MmaJob {
+    CUtensorMap a, b;
+    MmaPlan plan;
+    Epilogue epilogue;
+};
+
+// The split tiles' parts added up, of up to two products.  Up to eight warps share a row's parts (all of whose loads are under way at once), a lane takes eight
+// columns; the warps' sums are added in order.
+struct SplitSums {
+    MmaPlan plan[2];
+    StoreTarget target[2];
+    int blocks;                           // of the first product
+};
+__global__ void __launch_bounds__(256) split_sum_kernel(const __grid_constant__ SplitSums in)
 {
+    __shared__ float sums[8][32][kUnit + 1];
     wait_for_earlier();
     let_next_start();
-    const TileWalk walk(plan);
-    const int rest = static_cast<int>(blockIdx.x) / (kTile / kSumRows), first = static_cast<int>(blockIdx.x) % (kTile / kSumRows) * kSumRows;
-    if (rest >= (walk.count - walk.whole) / walk.splits) return;
-    int m, n;
-    walk.place(walk.whole + rest, m, n);
-    const int lane = threadIdx.x & 31, count = target.count();
+    const int job = static_cast<int>(blockIdx.x) >= in.blocks, block = static_cast<int>(blockIdx.x) - (job ? in.blocks : 0);
+    const int blocks = job ? static_cast<int>(gridDim.x) - in.blocks : in.blocks;
+    const StoreTarget &target = in.target[job];
+    const TileWalk walk(in.plan[job]);
+    if (walk.splits == 1) return;
+    int share = 1;                        // warps of a row
+    while (share < 8 && share < walk.splits) share *= 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, of = warp & (share - 1), rows = 8 / share, count = target.count();
     const float factor = target.factor();
-    const int r = first + (threadIdx.x >> 5), row = m * kTile + r;
-    if (row >= count) return;
-    const float *p = target.parts + (static_cast<long long>(rest) * walk.splits * kTile + r) * kTile + lane * kUnit;
-    Unit u{};
+    for (int first = block * rows; first < (walk.count - walk.whole) / walk.splits * kTile; first += blocks * rows) {          // rows of split tiles
+        const int rest = first / kTile, r = first % kTile + warp / share;
+        int m, n;
+        walk.place(static_cast<unsigned>(walk.whole + rest), m, n);
+        const int row = m * kTile + r, col = n * kTile + lane * kUnit;
+        Unit u{};
+        if (row < count) {
+            const float *p = target.parts + (static_cast<long long>(rest) * walk.splits * kTile + r) * kTile + lane * kUnit;
 #pragma unroll 8
-    for (int s = 0; s < walk.splits; ++s) {
-        const float4 a = __ldcs(reinterpret_cast<const float4 *>(p + s * kTile * kTile)), b = __ldcs(reinterpret_cast<const float4 *>(p + s * kTile * kTile) + 1);
-        u.v[0] += a.x; u.v[1] += a.y; u.v[2] += a.z; u.v[3] += a.w; u.v[4] += b.x; u.v[5] += b.y; u.v[6] += b.z; u.v[7] += b.w;
+            for (int s = of; s < walk.splits; s += share) {
+                const float4 *q = reinterpret_cast<const float4 *>(p + static_cast<long long>(s) * kTile * kTile);
+                const float4 a = __ldcs(q), b = __ldcs(q + 1);
+                u.v[0] += a.x; u.v[1] += a.y; u.v[2] += a.z; u.v[3] += a.w; u.v[4] += b.x; u.v[5] += b.y; u.v[6] += b.z; u.v[7] += b.w;
+            }
+        }
+        if (of) {
+#pragma unroll
+            for (int k = 0; k < kUnit; ++k) sums[warp][lane][k] = u.v[k];
+        }
+        __syncthreads();
+        if (!of && row < count) {
+            for (int w = 1; w < share; ++w) {
+#pragma unroll
+                for (int k = 0; k < kUnit; ++k) u.v[k] += sums[warp + w][lane][k];
+            }
+            target.store(row, target.order ? target.order[row] : row, col, u, factor);
+        }
+        __syncthreads();                  // sums are written again
     }
-    target.store(row, target.order ? target.order[row] : row, n * kTile + lane * kUnit, u, factor);
 }
 
 // ---- the kernel --------------------------------------------------------------------------------------------------------
-template <typename Epilogue, bool MN_A, bool MN_B>
-__global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1)
-mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmaPlan plan, const __grid_constant__ Epilogue given)
+// What the warps of a CTA know of its barriers, and how far they are.
+struct MmaState {
+    unsigned long long full[kStages], empty[kStages], ready[2], drained[2];
+};
+
+// One job's tiles, by every warp in its role.  turn, sums: stages and sums so far; late: a wait ran out; start: this pair's first tile.
+template <typename Epilogue, typename L>
+__device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &bars, unsigned ring, unsigned tmem, unsigned rank, int pairs, int &start, unsigned &turn, unsigned &sums, bool &late)
 {
     constexpr bool WHOLE = Epilogue::kChunk < (1 << 30);      // the epilogue takes all 128 columns of a row at once
-    extern __shared__ unsigned char raw_ring[];
-    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], ready[2], drained[2];
-    __shared__ unsigned tmem_base;
-    const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const unsigned rank = pair_rank();
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { bar_init(mma_smem(&full[s]), 1); bar_init(mma_smem(&empty[s]), 1); }
-        for (int b = 0; b < 2; ++b) { bar_init(mma_smem(&ready[b]), 1); bar_init(mma_smem(&drained[b]), 2 * kEpilogueWarps); }
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_a) : "memory");
-        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_b) : "memory");
-    }
-    if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(mma_smem(&tmem_base)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    pair_sync();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const unsigned tmem = tmem_base;
-    wait_for_earlier();
-    let_next_start();
-    const TileWalk walk(plan);
-    const int start = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
+    const TileWalk walk(job.plan);
     if (warp == 0) {
         if (lane == 0) {
-            unsigned turn = 0;                             // stages filled so far
-            bool late = false;
             for (int t = start; t < walk.count && !late; t += pairs) {
                 const TileAt at = walk.at(t);
                 const int ya = at.m * kTile + static_cast<int>(rank) * kHalf, yb = at.n * kTile + static_cast<int>(rank) * kHalf;
                 for (int s = 0; s < at.steps; ++s, ++turn) {
                     const unsigned slot = turn % kStages, round = turn / kStages;
                     const int x = (at.first + s) * kStep;
-                    if (round && !bar_wait(mma_smem(&empty[slot]), (round - 1) & 1)) { late = true; break; }
-                    const unsigned bar = leaders(mma_smem(&full[slot])), a = ring + slot * kStageBytes, b = a + kOperandBytes;
-                    if (rank == 0) bar_expect(mma_smem(&full[slot]), 2 * kStageBytes);
-                    if constexpr (MN_A) { tile_load(a, &map_a, ya, x, bar); tile_load(a + 8192, &map_a, ya + 64, x, bar); }
-                    else tile_load(a, &map_a, x, ya, bar);
-                    if constexpr (MN_B) { tile_load(b, &map_b, yb, x, bar); tile_load(b + 8192, &map_b, yb + 64, x, bar); }
-                    else tile_load(b, &map_b, x, yb, bar);
+                    if (round && !bar_wait(mma_smem(&bars.empty[slot]), (round - 1) & 1)) { late = true; break; }
+                    const unsigned bar = leaders(mma_smem(&bars.full[slot])), a = ring + slot * kStageBytes, b = a + kOperandBytes;
+                    if (rank == 0) bar_expect(mma_smem(&bars.full[slot]), 2 * kStageBytes);
+                    if constexpr (L::mn_a) { tile_load(a, &job.a, ya, x, bar); tile_load(a + 8192, &job.a, ya + 64, x, bar); }
+                    else tile_load(a, &job.a, x, ya, bar);
+                    if constexpr (L::mn_b) { tile_load(b, &job.b, yb, x, bar); tile_load(b + 8192, &job.b, yb + 64, x, bar); }
+                    else tile_load(b, &job.b, x, yb, bar);
                 }
-            }
-            // every copy has arrived, and every stage's release, before either CTA may leave
-            for (unsigned k = turn > kStages ? turn - kStages : 0; k < turn; ++k) {
-                late = late || !bar_wait(mma_smem(&empty[k % kStages]), (k / kStages) & 1);
-                if (late && rank == 0) bar_wait(mma_smem(&full[k % kStages]), (k / kStages) & 1);
             }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            unsigned turn = 0, sums = 0;
-            bool late = false;
             for (int t = start; t < walk.count && !late; t += pairs) {
                 const TileAt at = walk.at(t);
                 unsigned buffer = 0;
                 for (int s = 0; s < at.steps; ++s, ++turn) {
                     const int in = s % Epilogue::kChunk;
                     if (in == 0) {
-                        if (s) commit_pair(mma_smem(&ready[buffer]));
+                        if (s) commit_pair(mma_smem(&bars.ready[buffer]));
                         buffer = sums & 1;
                         const unsigned use = sums >> 1;
                         ++sums;
-                        if (use && !bar_wait(mma_smem(&drained[buffer]), (use - 1) & 1)) { late = true; break; }
+                        if (use && !bar_wait(mma_smem(&bars.drained[buffer]), (use - 1) & 1)) { late = true; break; }
                     }
                     const unsigned slot = turn % kStages;
-                    if (!bar_wait(mma_smem(&full[slot]), (turn / kStages) & 1)) { late = true; break; }
+                    if (!bar_wait(mma_smem(&bars.full[slot]), (turn / kStages) & 1)) { late = true; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t a = operand_descriptor<MN_A>(ring + slot * kStageBytes), b = operand_descriptor<MN_B>(ring + slot * kStageBytes + kOperandBytes);
+                    const uint64_t a = operand_descriptor<L::mn_a>(ring + slot * kStageBytes), b = operand_descriptor<L::mn_b>(ring + slot * kStageBytes + kOperandBytes);
 #pragma unroll
-                    for (int k = 0; k < kStep / 16; ++k)
-                        mma_pair(tmem + buffer * kTile, a + k * kDescriptorStep<MN_A>, b + k * kDescriptorStep<MN_B>, kInstruction<MN_A, MN_B>, in || k);
-                    commit_pair(mma_smem(&empty[slot]));
+                    for (int k = 0; k < kStep / 16; ++k) mma_pair(tmem + buffer * kTile, a + k * kDescriptorStep<L::mn_a>, b + k * kDescriptorStep<L::mn_b>, kInstruction<L::mn_a, L::mn_b>, in || k);
+                    commit_pair(mma_smem(&bars.empty[slot]));
                 }
-                if (!late && at.steps) commit_pair(mma_smem(&ready[buffer]));
+                if (!late && at.steps) commit_pair(mma_smem(&bars.ready[buffer]));
             }
         }
     } else if (warp >= kEpilogueWarp) {
-        Epilogue ep = given;
+        Epilogue ep = job.epilogue;
         const int quarter = warp & 3, half = (warp - kEpilogueWarp) >> 2;
         const unsigned lanes = tmem + (static_cast<unsigned>(quarter * 32) << 16) + half * kHalf, desk = ring + kDesks + (warp - kEpilogueWarp) * kDeskBytes;
-        unsigned sums = 0;
-        bool late = false;
-        if constexpr (WHOLE) if (blockIdx.x == 0 && threadIdx.x == 32 * kEpilogueWarp && given.done) *given.done = 0;
+        if constexpr (WHOLE) if (blockIdx.x == 0 && threadIdx.x == 32 * kEpilogueWarp && ep.done) *ep.done = 0;
         for (int t = start; t < walk.count; t += pairs) {
             const TileAt at = walk.at(t);
             const int col = at.n * kTile + half * kHalf, row = at.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
@@ -568,7 +589,7 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
 #pragma unroll 1
                 for (int s = 0; s < at.steps; s += Epilogue::kChunk) {
                     const unsigned buffer = sums & 1;
-                    late = late || !bar_wait(mma_smem(&ready[buffer]), (sums >> 1) & 1);
+                    late = late || !bar_wait(mma_smem(&bars.ready[buffer]), (sums >> 1) & 1);
                     ++sums;
                     __syncwarp();
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -581,13 +602,13 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
                     }
                     __syncwarp();
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    if (lane == 0) bar_arrive_leader(mma_smem(&drained[buffer]));
+                    if (lane == 0) bar_arrive_leader(mma_smem(&bars.drained[buffer]));
                 }
                 ep.take(x, row, col, late, desk);
             } else {
                 const unsigned buffer = sums & 1;
                 if (at.steps) {
-                    late = late || !bar_wait(mma_smem(&ready[buffer]), (sums >> 1) & 1);
+                    late = late || !bar_wait(mma_smem(&bars.ready[buffer]), (sums >> 1) & 1);
                     ++sums;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 }
@@ -611,11 +632,54 @@ mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CU
                 __syncwarp();
                 if (at.steps) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    if (lane == 0) bar_arrive_leader(mma_smem(&drained[buffer]));
+                    if (lane == 0) bar_arrive_leader(mma_smem(&bars.drained[buffer]));
                 }
             }
         }
     }
+    __syncwarp();                                      // the next walk is a whole warp's
+    start = (start + pairs - walk.count % pairs) % pairs;           // turns go on where they are
+}
+
+// Of two jobs (M not void) the second's tiles follow the first's.
+template <typename Epilogue, typename L, typename M>
+__global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaJob<Epilogue> first, const __grid_constant__ MmaJob<Epilogue> second)
+{
+    extern __shared__ unsigned char raw_ring[];
+    __shared__ __align__(8) MmaState bars;
+    __shared__ unsigned tmem_base;
+    const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned rank = pair_rank();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) { bar_init(mma_smem(&bars.full[s]), 1); bar_init(mma_smem(&bars.empty[s]), 1); }
+        for (int b = 0; b < 2; ++b) { bar_init(mma_smem(&bars.ready[b]), 1); bar_init(mma_smem(&bars.drained[b]), 2 * kEpilogueWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&first.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&first.b) : "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(mma_smem(&tmem_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    pair_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const unsigned tmem = tmem_base;
+    wait_for_earlier();
+    let_next_start();
+    const int pairs = static_cast<int>(gridDim.x >> 1);
+    int start = static_cast<int>(blockIdx.x >> 1);
+    unsigned turn = 0, sums = 0;                           // stages and sums so far, of both products
+    bool late = false;
+    run_job<Epilogue, L>(first, bars, ring, tmem, rank, pairs, start, turn, sums, late);
+    if constexpr (!std::is_void_v<M>) run_job<Epilogue, M>(second, bars, ring, tmem, rank, pairs, start, turn, sums, late);
+    if (warp == 0 && lane == 0)                            // every copy has arrived, and every stage's release, before either CTA may leave
+        for (unsigned k = turn > kStages ? turn - kStages : 0; k < turn; ++k) {
+            late = late || !bar_wait(mma_smem(&bars.empty[k % kStages]), (k / kStages) & 1);
+            if (late && rank == 0) bar_wait(mma_smem(&bars.full[k % kStages]), (k / kStages) & 1);
+        }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();

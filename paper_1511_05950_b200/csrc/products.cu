@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 using softsync::aligned_to;
 using softsync::kHalf;
@@ -77,13 +78,33 @@ int start(void (*kernel)(K...), int64_t blocks, int threads, int shared, bool de
     return softsync::launch(kernel, blocks, threads, shared, dependent, st, args...) ? PS_OK : PS_ERR_CUDA;
 }
 
-// D = A B^T.  MN_A: A is given as k x m (else m x k), MN_B: B as k x n (else n x k).
-template <bool MN_A, bool MN_B, typename Epilogue>
-int launch_product(const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue, bool dependent, cudaStream_t st)
+using softsync::Lying;
+
+// D = A B^T.  L::mn_a: A is given as k x m (else m x k), L::mn_b: B as k x n (else n x k).
+template <typename L, typename Epilogue>
+bool job_of(softsync::MmaJob<Epilogue> &job, const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue)
 {
-    CUtensorMap map_a, map_b;
-    if (!encode(map_a, a, MN_A ? kStep : kHalf) || !encode(map_b, b, MN_B ? kStep : kHalf)) return PS_ERR_CUDA;
-    const auto kernel = softsync::mma_kernel<Epilogue, MN_A, MN_B>;
+    job.plan = plan;
+    job.epilogue = epilogue;
+    return encode(job.a, a, L::mn_a ? kStep : kHalf) && encode(job.b, b, L::mn_b ? kStep : kHalf);
+}
+
+// Items of a product (parts of split tiles one by one): exactly, or at most where only the device knows the extents.
+int64_t items_of(const MmaPlan &plan)
+{
+    const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile);
+    if (!plan.slots) return tiles;
+    if (plan.live) return std::max<int64_t>(tiles, plan.slots);
+    const int rest = static_cast<int>(tiles % plan.slots);
+    return rest ? tiles + int64_t{rest} * (softsync::split_count(rest, static_cast<int>(div_up(plan.k, kStep)), plan.slots) - 1) : tiles;
+}
+
+// One product, or two whose operands are both there: one launch's fixed time (10 us) for both.
+template <typename L, typename M = void, typename Epilogue>
+int launch_products(const softsync::MmaJob<Epilogue> *jobs, bool dependent, cudaStream_t st)
+{
+    constexpr int count = std::is_void_v<M> ? 1 : 2;
+    const auto kernel = softsync::mma_kernel<Epilogue, L, M>;
     static std::atomic<bool> ready[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return PS_ERR_CUDA;
@@ -91,19 +112,31 @@ int launch_product(const Matrix &a, const Matrix &b, const MmaPlan &plan, const 
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, softsync::kMmaShared) != cudaSuccess) return PS_ERR_CUDA;
         ready[device].store(true, std::memory_order_relaxed);
     }
-    const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile);
-    if (tiles > 0x70000000) return PS_ERR_INVALID_ARG;
-    const int64_t pairs = plan.slots ? plan.slots : std::min<int64_t>(tiles, pairs_on_device());
+    int64_t items = 0;
+    for (int k = 0; k < count; ++k) {
+        const int64_t n = items_of(jobs[k].plan);
+        if (n > 0x70000000) return PS_ERR_INVALID_ARG;
+        items += n;
+    }
+    const int64_t pairs = std::min<int64_t>(items, pairs_on_device());
     if (pairs < 1) return PS_ERR_CUDA;
-    return start(kernel, 2 * pairs, softsync::kMmaThreads, softsync::kMmaShared, dependent, st, map_a, map_b, plan, epilogue);
+    return start(kernel, 2 * pairs, softsync::kMmaThreads, softsync::kMmaShared, dependent, st, jobs[0], jobs[count - 1]);
 }
 
-// The sums of a product whose last tiles are split, unless it is known that none are.
-int launch_split_sum(const MmaPlan &plan, const softsync::StoreTarget &target, cudaStream_t st)
+// The sums of up to two products whose last tiles may be split.
+int launch_split_sums(const softsync::MmaJob<softsync::StoreEpilogue> *jobs, int count, cudaStream_t st)
 {
-    const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile), rest = plan.live && !plan.live_is_k ? std::min<int64_t>(tiles, plan.slots - 1) : tiles % plan.slots;
-    if (!rest || (!plan.live && softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots) == 1)) return PS_OK;
-    return start(softsync::split_sum_kernel, rest * (kTile / softsync::kSumRows), 256, 0, true, st, plan, target);
+    softsync::SplitSums in;
+    int64_t blocks[2] = {0, 0};
+    for (int k = 0; k < count; ++k) {
+        const MmaPlan &plan = in.plan[k] = jobs[k].plan;
+        in.target[k] = jobs[k].epilogue.target;
+        const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile), rest = plan.live && !plan.live_is_k ? std::min<int64_t>(tiles, plan.slots - 1) : tiles % plan.slots;
+        const int splits = plan.live || !rest ? 2 : softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots);
+        if (splits > 1) blocks[k] = std::min<int64_t>(rest * kTile / 4, 8 * plan.slots);          // rows in turn: 2 to 8 warps each
+    }
+    in.blocks = static_cast<int>(blocks[0]);
+    return blocks[0] + blocks[1] ? start(softsync::split_sum_kernel, blocks[0] + blocks[1], 256, 0, true, st, in) : PS_OK;
 }
 int64_t part_elements() { return int64_t{softsync::kMostParts} * kPairs * kTile * kTile; }
 
@@ -161,7 +194,7 @@ struct HeadPlan : Places {
         take(stat, part_count * rows);
         if (!grad) return;
         take(g, rows_padded * g_stride);
-        take(split, part_elements());
+        take(split, 2 * part_elements());
         if (first) take(dhidden, rows * width_padded);
     }
 };
@@ -230,7 +263,9 @@ struct HeadCall {
         ep.parts = w.stat; ep.part_stride = h.rows; ep.picked = w.picked; ep.done = w.done;
         if (keep) { ep.kept = reinterpret_cast<uint16_t *>(w.g); ep.kept_stride = w.g_stride; ep.first = static_cast<int>(w.first); }
         const MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), live(), 0, 0, group_of(div_up(h.rows, kTile))};
-        const int status = launch_product<false, false>(hidden, head, plan, ep, dependent(), st);
+        softsync::MmaJob<softsync::StatsEpilogue> job;
+        if (!job_of<Lying<false, false>>(job, hidden, head, plan, ep)) return PS_ERR_CUDA;
+        const int status = launch_products<Lying<false, false>>(&job, dependent(), st);
         if (status != PS_OK) return status;
         softsync::JoinIn in{};
         in.parts = w.stat; in.part_stride = h.rows; in.count = static_cast<int>(w.part_count); in.picked = w.picked; in.tokens = tokens; in.order = order(); in.live = live();
@@ -243,6 +278,8 @@ struct HeadCall {
     {
         const int rows = static_cast<int>(h.rows), width = static_cast<int>(h.width), slots = slots_on_device();
         if (slots < 1) return PS_ERR_CUDA;
+        using OfHidden = Lying<false, true>;
+        using OfHead = Lying<true, true>;
         const int64_t pieces = 1 + (w.first ? div_up(w.first, w.piece) : 0);
         for (int64_t k = 0; k < pieces; ++k) {                                  // the kept one first: the others take its place
             const int64_t first = k ? (k - 1) * w.piece : w.first;
@@ -260,27 +297,29 @@ struct HeadCall {
                 ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.live = live(); ge.scale = scale;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
                 const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(div_up(rows, kTile))};
-                status = launch_product<false, false>(hidden, entries, plan, ge, dependent(), st);
+                softsync::MmaJob<softsync::GradEpilogue> job;
+                status = job_of<Lying<false, false>>(job, hidden, entries, plan, ge) ? launch_products<Lying<false, false>>(&job, dependent(), st) : PS_ERR_CUDA;
             }
+            softsync::MmaJob<softsync::StoreEpilogue> jobs[2];
+            int count = 0;
             if (status == PS_OK && dhidden) {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
                 t.rows = rows; t.cols = width; t.live = live(); t.order = order(); t.alpha = alpha; t.alpha_dev = alpha_dev;
                 if (k == pieces - 1) { t.out = dhidden; t.out_bf16 = 1; t.vectors = width % 8 == 0; t.stride = width; }
                 t.sum = w.dhidden; t.sum_stride = w.width_padded; t.add = k > 0; t.parts = w.split;
-                const MmaPlan plan{rows, width, n, live(), 0, slots, group_of(div_up(rows, kTile))};
-                status = launch_product<false, true>(g, entries, plan, se, dependent(), st);
-                if (status == PS_OK) status = launch_split_sum(plan, t, st);
+                if (!job_of<OfHidden>(jobs[count++], g, entries, MmaPlan{rows, width, n, live(), 0, slots, group_of(div_up(rows, kTile))}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && dhead) {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
                 t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = static_cast<bf16 *>(dhead) + first * h.width; t.out_bf16 = 1;
-                t.vectors = width % 8 == 0; t.stride = width; t.parts = w.split;
-                const MmaPlan plan{n, width, rows, live(), 1, slots, group_of(div_up(n, kTile))};
-                status = launch_product<true, true>(g, hidden, plan, se, dependent(), st);
-                if (status == PS_OK) status = launch_split_sum(plan, t, st);
+                t.vectors = width % 8 == 0; t.stride = width; t.parts = w.split + part_elements();
+                if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, live(), 1, slots, group_of(div_up(n, kTile))}, se)) return PS_ERR_CUDA;
             }
+            if (status == PS_OK && count) 
+                status = count == 2 ? launch_products<OfHidden, OfHead>(jobs, dependent(), st) : dhidden ? launch_products<OfHidden>(jobs, dependent(), st) : launch_products<OfHead>(jobs, dependent(), st);
+            if (status == PS_OK && count) status = launch_split_sums(jobs, count, st);
             if (status != PS_OK) return status;
         }
         return PS_OK;
@@ -423,9 +462,10 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     softsync::StoreTarget &t = se.target;
     t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = a->dweight_dev; t.out_bf16 = a->out_dtype == PS_GRAD_BF16;
     t.vectors = a->cols % 8 == 0 && aligned_to(a->gain_dev, 16); t.stride = cols; t.parts = w.split;
-    const MmaPlan plan{outs, cols, rows, nullptr, 0, slots, group_of(div_up(outs, kTile))};
-    status = launch_product<true, true>(dout, values, plan, se, true, st);
-    return status == PS_OK ? launch_split_sum(plan, t, st) : status;
+    softsync::MmaJob<softsync::StoreEpilogue> job;
+    if (!job_of<Lying<true, true>>(job, dout, values, MmaPlan{outs, cols, rows, nullptr, 0, slots, group_of(div_up(outs, kTile))}, se)) return PS_ERR_CUDA;
+    status = launch_products<Lying<true, true>>(&job, true, st);
+    return status == PS_OK ? launch_split_sums(&job, 1, st) : status;
 }
 
 }  // extern "C"
