@@ -44,6 +44,14 @@ __device__ __forceinline__ unsigned leaders(unsigned addr)    // the same place 
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
     return r;
 }
+// One lane of a warp that runs as a whole: what it alone does keeps its operands in the warp's own registers.  Under a branch on the lane's number they were moved there
+// one by one, and the products of a stage took longer to issue than to compute.
+__device__ __forceinline__ bool elected()
+{
+    unsigned r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void pair_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -529,17 +537,17 @@ template <typename Epilogue, typename L>
 __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &bars, unsigned ring, unsigned tmem, unsigned rank, int pairs, int &start, unsigned &turn, unsigned &sums, bool &late)
 {
     constexpr bool WHOLE = Epilogue::kChunk < (1 << 30);      // the epilogue takes all 128 columns of a row at once
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kAllLanes, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const TileWalk walk(job.plan);
     if (warp == 0) {
-        if (lane == 0) {
-            for (int t = start; t < walk.count && !late; t += pairs) {
-                const TileAt at = walk.at(t);
-                const int ya = at.m * kTile + static_cast<int>(rank) * kHalf, yb = at.n * kTile + static_cast<int>(rank) * kHalf;
-                for (int s = 0; s < at.steps; ++s, ++turn) {
-                    const unsigned slot = turn % kStages, round = turn / kStages;
-                    const int x = (at.first + s) * kStep;
-                    if (round && !bar_wait(mma_smem(&bars.empty[slot]), (round - 1) & 1)) { late = true; break; }
+        for (int t = start; t < walk.count && !late; t += pairs) {
+            const TileAt at = walk.at(t);
+            const int ya = at.m * kTile + static_cast<int>(rank) * kHalf, yb = at.n * kTile + static_cast<int>(rank) * kHalf;
+            for (int s = 0; s < at.steps; ++s, ++turn) {
+                const unsigned slot = turn % kStages, round = turn / kStages;
+                const int x = (at.first + s) * kStep;
+                if (round && !bar_wait(mma_smem(&bars.empty[slot]), (round - 1) & 1)) { late = true; break; }
+                if (elected()) {
                     const unsigned bar = leaders(mma_smem(&bars.full[slot])), a = ring + slot * kStageBytes, b = a + kOperandBytes;
                     if (rank == 0) bar_expect(mma_smem(&bars.full[slot]), 2 * kStageBytes);
                     if constexpr (L::mn_a) { tile_load(a, &job.a, ya, x, bar); tile_load(a + 8192, &job.a, ya + 64, x, bar); }
@@ -547,32 +555,36 @@ __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &b
                     if constexpr (L::mn_b) { tile_load(b, &job.b, yb, x, bar); tile_load(b + 8192, &job.b, yb + 64, x, bar); }
                     else tile_load(b, &job.b, x, yb, bar);
                 }
+                __syncwarp();
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            for (int t = start; t < walk.count && !late; t += pairs) {
-                const TileAt at = walk.at(t);
-                unsigned buffer = 0;
-                for (int s = 0; s < at.steps; ++s, ++turn) {
-                    const int in = s % Epilogue::kChunk;
-                    if (in == 0) {
-                        if (s) commit_pair(mma_smem(&bars.ready[buffer]));
-                        buffer = sums & 1;
-                        const unsigned use = sums >> 1;
-                        ++sums;
-                        if (use && !bar_wait(mma_smem(&bars.drained[buffer]), (use - 1) & 1)) { late = true; break; }
-                    }
-                    const unsigned slot = turn % kStages;
-                    if (!bar_wait(mma_smem(&bars.full[slot]), (turn / kStages) & 1)) { late = true; break; }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t a = operand_descriptor<L::mn_a>(ring + slot * kStageBytes), b = operand_descriptor<L::mn_b>(ring + slot * kStageBytes + kOperandBytes);
+        for (int t = start; rank == 0 && t < walk.count && !late; t += pairs) {
+            const TileAt at = walk.at(t);
+            unsigned buffer = 0;
+            for (int s = 0; s < at.steps; ++s, ++turn) {
+                const int in = s % Epilogue::kChunk;
+                if (in == 0) {
+                    if (s && elected()) commit_pair(mma_smem(&bars.ready[buffer]));
+                    buffer = sums & 1;
+                    const unsigned use = sums >> 1;
+                    ++sums;
+                    if (use && !bar_wait(mma_smem(&bars.drained[buffer]), (use - 1) & 1)) { late = true; break; }
+                }
+                const unsigned slot = turn % kStages;
+                if (!bar_wait(mma_smem(&bars.full[slot]), (turn / kStages) & 1)) { late = true; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t a = operand_descriptor<L::mn_a>(ring + slot * kStageBytes), b = operand_descriptor<L::mn_b>(ring + slot * kStageBytes + kOperandBytes);
+                if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < kStep / 16; ++k) mma_pair(tmem + buffer * kTile, a + k * kDescriptorStep<L::mn_a>, b + k * kDescriptorStep<L::mn_b>, kInstruction<L::mn_a, L::mn_b>, in || k);
+                    for (int k = 0; k < kStep / 16; ++k)
+                        mma_pair(tmem + buffer * kTile, a + k * kDescriptorStep<L::mn_a>, b + k * kDescriptorStep<L::mn_b>, kInstruction<L::mn_a, L::mn_b>, in || k);
                     commit_pair(mma_smem(&bars.empty[slot]));
                 }
-                if (!late && at.steps) commit_pair(mma_smem(&bars.ready[buffer]));
+                __syncwarp();
             }
+            if (!late && at.steps && elected()) commit_pair(mma_smem(&bars.ready[buffer]));
+            __syncwarp();
         }
     } else if (warp >= kEpilogueWarp) {
         Epilogue ep = job.epilogue;
@@ -649,7 +661,7 @@ __global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel
     __shared__ __align__(8) MmaState bars;
     __shared__ unsigned tmem_base;
     const unsigned ring = (mma_smem(raw_ring) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kAllLanes, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const unsigned rank = pair_rank();
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { bar_init(mma_smem(&bars.full[s]), 1); bar_init(mma_smem(&bars.empty[s]), 1); }

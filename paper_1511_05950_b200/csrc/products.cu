@@ -133,7 +133,7 @@ int launch_split_sums(const softsync::MmaJob<softsync::StoreEpilogue> *jobs, int
         in.target[k] = jobs[k].epilogue.target;
         const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile), rest = plan.live && !plan.live_is_k ? std::min<int64_t>(tiles, plan.slots - 1) : tiles % plan.slots;
         const int splits = plan.live || !rest ? 2 : softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots);
-        if (splits > 1) blocks[k] = std::min<int64_t>(rest * kTile / 4, 8 * plan.slots);          // rows in turn: 2 to 8 warps each
+        if (splits > 1) blocks[k] = std::min<int64_t>(rest * kTile / 2, 32 * plan.slots);         // rows in turn: 2 to 8 warps each
     }
     in.blocks = static_cast<int>(blocks[0]);
     return blocks[0] + blocks[1] ? start(softsync::split_sum_kernel, blocks[0] + blocks[1], 256, 0, true, st, in) : PS_OK;
