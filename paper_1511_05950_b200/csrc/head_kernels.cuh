@@ -38,12 +38,13 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
         }
         if (lane == 31) counts[warp] = before;
         __syncthreads();
-        int offset = base, all = 0;
-        for (int w = 0; w < 32; ++w) {
-            if (w < warp) offset += counts[w];
-            all += counts[w];
+        int upto = counts[lane];                           // every warp adds up the warps' counts for itself
+        for (int o = 1; o < 32; o <<= 1) {
+            const int other = __shfl_up_sync(kAllLanes, upto, o);
+            if (lane >= o) upto += other;
         }
-        offset += before - mine;
+        const int all = __shfl_sync(kAllLanes, upto, 31);
+        int offset = base + before - mine + (warp ? __shfl_sync(kAllLanes, upto, warp - 1) : 0);
 #pragma unroll
         for (int k = 0; k < kOrderRun; ++k) {
             if (at + k >= rows) break;
@@ -62,9 +63,11 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
     if (lane == 0) sums[warp] = sum;
     __syncthreads();
-    if (threadIdx.x) return;
+    if (warp) return;
+    sum = sums[lane];
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
+    if (lane) return;
     *out.live = base;
-    for (int w = 1; w < 32; ++w) sum += sums[w];
     if (out.sum) *out.sum = static_cast<float>(sum);
     if (out.inverse) *out.inverse = sum == 0 ? 0.f : static_cast<float>(1.0 / sum);
 }
@@ -150,9 +153,15 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         if (!in.stats) return;
     } else {
         double share = 0;
+        s = found[tid / kJoinRows][of];
+#pragma unroll
+        for (int w = 32 / kJoinRows; w < kJoinThreads / 32; w += 32 / kJoinRows) s = join_parts(s, found[w + tid / kJoinRows][of], in.scale);
+#pragma unroll
+        for (int o = 16; o >= kJoinRows; o >>= 1) {
+            const float2 b = make_float2(__shfl_xor_sync(kAllLanes, s.x, o), __shfl_xor_sync(kAllLanes, s.y, o));
+            s = tid & o ? join_parts(b, s, in.scale) : join_parts(s, b, in.scale);
+        }
         if (tid < kJoinRows && row < count) {
-            s = found[0][of];
-            for (int w = 1; w < kJoinThreads / 32; ++w) s = join_parts(s, found[w][of], in.scale);
             const int at = in.order ? in.order[row] : row;
             const long long t = in.tokens[at];
             const bool known = t >= 0 && t < in.vocab;

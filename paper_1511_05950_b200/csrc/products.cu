@@ -140,7 +140,11 @@ int launch_split_sums(const softsync::MmaJob<softsync::StoreEpilogue> *jobs, int
 }
 int64_t part_elements() { return int64_t{softsync::kMostParts} * kPairs * kTile * kTile; }
 
-int group_of(int64_t tiles_m) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(tiles_m, 16))); }
+// Row tiles that take turns before the next column tile's: as many as leave their operand in the L2 (32 MB of it), so that the other one is read once for all of them.
+int group_of(int64_t m, int64_t k)
+{
+    return static_cast<int>(std::max<int64_t>(1, std::min(div_up(m, kTile), (int64_t{32} << 20) / (2 * kTile * std::max<int64_t>(k, 1)))));
+}
 
 // ---- workspaces --------------------------------------------------------------------------------------------------------
 struct Places {
@@ -262,7 +266,7 @@ struct HeadCall {
         ep.order = order(); ep.tokens = tokens; ep.rows = static_cast<int>(h.rows); ep.vocab = static_cast<int>(h.vocab); ep.live = live(); ep.scale = scale;
         ep.parts = w.stat; ep.part_stride = h.rows; ep.picked = w.picked; ep.done = w.done;
         if (keep) { ep.kept = reinterpret_cast<uint16_t *>(w.g); ep.kept_stride = w.g_stride; ep.first = static_cast<int>(w.first); }
-        const MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), live(), 0, 0, group_of(div_up(h.rows, kTile))};
+        const MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), live(), 0, 0, group_of(h.rows, h.width)};
         softsync::MmaJob<softsync::StatsEpilogue> job;
         if (!job_of<Lying<false, false>>(job, hidden, head, plan, ep)) return PS_ERR_CUDA;
         const int status = launch_products<Lying<false, false>>(&job, dependent(), st);
@@ -296,7 +300,7 @@ struct HeadCall {
                 softsync::GradEpilogue ge{};
                 ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.live = live(); ge.scale = scale;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
-                const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(div_up(rows, kTile))};
+                const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(rows, width)};
                 softsync::MmaJob<softsync::GradEpilogue> job;
                 status = job_of<Lying<false, false>>(job, hidden, entries, plan, ge) ? launch_products<Lying<false, false>>(&job, dependent(), st) : PS_ERR_CUDA;
             }
@@ -308,14 +312,14 @@ struct HeadCall {
                 t.rows = rows; t.cols = width; t.live = live(); t.order = order(); t.alpha = alpha; t.alpha_dev = alpha_dev;
                 if (k == pieces - 1) { t.out = dhidden; t.out_bf16 = 1; t.vectors = width % 8 == 0; t.stride = width; }
                 t.sum = w.dhidden; t.sum_stride = w.width_padded; t.add = k > 0; t.parts = w.split;
-                if (!job_of<OfHidden>(jobs[count++], g, entries, MmaPlan{rows, width, n, live(), 0, slots, group_of(div_up(rows, kTile))}, se)) return PS_ERR_CUDA;
+                if (!job_of<OfHidden>(jobs[count++], g, entries, MmaPlan{rows, width, n, live(), 0, slots, group_of(rows, n)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && dhead) {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
                 t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = static_cast<bf16 *>(dhead) + first * h.width; t.out_bf16 = 1;
                 t.vectors = width % 8 == 0; t.stride = width; t.parts = w.split + part_elements();
-                if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, live(), 1, slots, group_of(div_up(n, kTile))}, se)) return PS_ERR_CUDA;
+                if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, live(), 1, slots, group_of(n, rows)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && count) 
                 status = count == 2 ? launch_products<OfHidden, OfHead>(jobs, dependent(), st) : dhidden ? launch_products<OfHidden>(jobs, dependent(), st) : launch_products<OfHead>(jobs, dependent(), st);
@@ -463,7 +467,7 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = a->dweight_dev; t.out_bf16 = a->out_dtype == PS_GRAD_BF16;
     t.vectors = a->cols % 8 == 0 && aligned_to(a->gain_dev, 16); t.stride = cols; t.parts = w.split;
     softsync::MmaJob<softsync::StoreEpilogue> job;
-    if (!job_of<Lying<true, true>>(job, dout, values, MmaPlan{outs, cols, rows, nullptr, 0, slots, group_of(div_up(outs, kTile))}, se)) return PS_ERR_CUDA;
+    if (!job_of<Lying<true, true>>(job, dout, values, MmaPlan{outs, cols, rows, nullptr, 0, slots, group_of(outs, rows)}, se)) return PS_ERR_CUDA;
     status = launch_products<Lying<true, true>>(&job, true, st);
     return status == PS_OK ? launch_split_sums(&job, 1, st) : status;
 }
