@@ -79,7 +79,7 @@ def build_marshal(force: bool = False) -> str:
     libs = os.path.join(root, "lib")
     cmd = [shutil.which("g++") or "g++"] + MARSHAL_FLAGS + ["-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
     cmd += ["-isystem" + i for i in include] + ["-o", MARSHAL, MARSHAL_SOURCES[0], "-L" + libs, "-Wl,-rpath," + libs,
-                                                "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+                                                "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
     for old in (MARSHAL_STAMP, MARSHAL):         # an extension of other sources must not be loaded if this fails
         if os.path.exists(old):
             os.remove(old)

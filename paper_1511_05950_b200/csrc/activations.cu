@@ -50,7 +50,7 @@ int over_rows(int64_t rows, int64_t cols, int64_t stride, bool aligned, F launch
     return PS_OK;
 }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 int launch_norm(const NormIn &in, cudaStream_t st)
 {
     const int64_t units = div_up(in.cols, softsync::kUnit);
@@ -58,51 +58,58 @@ int launch_norm(const NormIn &in, cudaStream_t st)
         const int64_t blocks = warps == 1 ? div_up(in.rows, softsync::kNormRows) : in.rows;
         return softsync::launch(kernel, blocks, warps == 1 ? 32 * softsync::kNormRows : 32 * warps, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
     };
-    if (units <= 32) return go(softsync::rms_norm_kernel<T, 1, 1>, 1);
-    if (units <= 64) return go(softsync::rms_norm_kernel<T, 1, 2>, 1);
-    if (units <= 128) return go(softsync::rms_norm_kernel<T, 1, 4>, 1);
-    if (units <= 256) return go(softsync::rms_norm_kernel<T, 4, 2>, 4);
-    if (units <= 512) return go(softsync::rms_norm_kernel<T, 4, 4>, 4);
-    if (units <= 1024) return go(softsync::rms_norm_kernel<T, 8, 4>, 8);
-    if (units <= 2048) return go(softsync::rms_norm_kernel<T, 16, 4>, 16);
-    return softsync::launch(softsync::rms_norm_long_kernel<T>, in.rows, softsync::kLongThreads, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
+    if (units <= 32) return go(softsync::rms_norm_kernel<T, 1, 1, ALIGNED>, 1);
+    if (units <= 64) return go(softsync::rms_norm_kernel<T, 1, 2, ALIGNED>, 1);
+    if (units <= 128) return go(softsync::rms_norm_kernel<T, 1, 4, ALIGNED>, 1);
+    if (units <= 256) return go(softsync::rms_norm_kernel<T, 4, 2, ALIGNED>, 4);
+    if (units <= 512) return go(softsync::rms_norm_kernel<T, 4, 4, ALIGNED>, 4);
+    if (units <= 1024) return go(softsync::rms_norm_kernel<T, 8, 4, ALIGNED>, 8);
+    if (units <= 2048) return go(softsync::rms_norm_kernel<T, 16, 4, ALIGNED>, 16);
+    return softsync::launch(softsync::rms_norm_long_kernel<T, ALIGNED>, in.rows, softsync::kLongThreads, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
 }
 
 // Blocks of the backward pass, as many as are resident at once, and with them the parts that the gain's gradient is summed in.
 constexpr int64_t kSms = 148, kLongParts = 64;
 struct GradShape { int warps, units; int64_t blocks, parts; };
+template <typename T>
 GradShape grad_shape(int64_t rows, int64_t cols)
 {
     const int64_t units = div_up(cols, softsync::kUnit);
-    const auto of = [&](int warps, int per) {
-        const int64_t groups = warps == 1 ? softsync::kNormRows : 1, blocks = std::min(div_up(rows, groups), kSms * (warps <= 4 ? 4 : warps == 8 ? 2 : 1));
+    const auto of = [&](int warps, auto per) {
+        const int64_t groups = warps == 1 ? softsync::kNormRows : 1, resident = softsync::kGradWarps<T, per> / (warps == 1 ? softsync::kNormRows : warps);
+        const int64_t blocks = std::min(div_up(rows, groups), kSms * resident);
         return GradShape{warps, per, blocks, blocks * groups};
     };
-    if (units <= 32) return of(1, 1);
-    if (units <= 64) return of(1, 2);
-    if (units <= 256) return of(4, 2);
-    if (units <= 512) return of(8, 2);
-    if (units <= 1024) return of(16, 2);
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    if (units <= 32) return of(1, one);
+    if (units <= 64) return of(1, two);
+    if (units <= 128) return of(4, one);
+    if (units <= 256) return of(8, one);
+    if (units <= 512) return of(16, one);
+    if (units <= 1024) return of(16, two);
     return GradShape{0, 0, rows, std::min(rows, kLongParts)};
 }
+GradShape grad_shape(int dtype, int64_t rows, int64_t cols) { return dtype == PS_GRAD_BF16 ? grad_shape<bf16>(rows, cols) : grad_shape<float>(rows, cols); }
 
-template <typename T, bool CODES>
+template <typename T, bool CODES, bool ALIGNED>
 int launch_norm_grad(const NormGradIn &in, const GradShape &shape, cudaStream_t st)
 {
     const auto go = [&](auto kernel) {
         return softsync::launch(kernel, shape.blocks, shape.warps == 1 ? 32 * softsync::kNormRows : 32 * shape.warps, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
     };
     switch (shape.warps * 8 + shape.units) {
-    case 1 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 1, 1, CODES>);
-    case 1 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 1, 2, CODES>);
-    case 4 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 4, 2, CODES>);
-    case 8 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 8, 2, CODES>);
-    case 16 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 16, 2, CODES>);
+    case 1 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 1, 1, CODES, ALIGNED>);
+    case 1 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 1, 2, CODES, ALIGNED>);
+    case 4 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 4, 1, CODES, ALIGNED>);
+    case 8 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 8, 1, CODES, ALIGNED>);
+    case 16 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 16, 1, CODES, ALIGNED>);
+    case 16 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 16, 2, CODES, ALIGNED>);
     }
-    if (!softsync::launch(softsync::rms_norm_grad_long_kernel<T, CODES>, in.rows, softsync::kLongThreads, 0, true, st, in)) return PS_ERR_CUDA;
+    if (!softsync::launch(softsync::rms_norm_grad_long_kernel<T, CODES, ALIGNED>, in.rows, softsync::kLongThreads, 0, true, st, in)) return PS_ERR_CUDA;
     if (!in.parts) return PS_OK;
     const dim3 grid(static_cast<unsigned>(div_up(div_up(in.cols, softsync::kUnit), 128)), static_cast<unsigned>(shape.parts));
-    softsync::gain_grad_long_kernel<T, CODES><<<grid, 128, 0, st>>>(in);
+    softsync::gain_grad_long_kernel<T, CODES, ALIGNED><<<grid, 128, 0, st>>>(in);
     return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA;
 }
 
@@ -131,7 +138,9 @@ int ps_unpack8(const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows,
     if (!rows_ok(out_dev, dtype, rows, cols, row_stride) || !packed_ok(codes_dev, scales_dev)) return PS_ERR_INVALID_ARG;
     const auto go = [&](auto *out) {
         return over_rows(rows, cols, row_stride, vectors_ok(out_dev, dtype, rows, row_stride), [&](int64_t first, int64_t unit, const PackShape &shape, int64_t blocks) {
-            return softsync::launch(softsync::unpack_kernel<std::remove_pointer_t<decltype(out)>>, blocks, softsync::kPackThreads, 0, true, static_cast<cudaStream_t>(stream),
+            using T = std::remove_pointer_t<decltype(out)>;
+            const int64_t warps = shape.count / static_cast<unsigned>(shape.units) * div_up(shape.units, 32);
+            return softsync::launch(shape.aligned ? softsync::unpack_kernel<T> : softsync::unpack_rows_kernel<T>, shape.aligned ? blocks : div_up(warps, softsync::kPackThreads / 32), softsync::kPackThreads, 0, true, static_cast<cudaStream_t>(stream),
                                     reinterpret_cast<const uint2 *>(codes_dev) + unit, scales_dev + unit / 4, shape, out + first * row_stride);
         });
     };
@@ -163,17 +172,18 @@ int ps_rms_norm(const ps_norm *a, void *stream)
     in.codes = reinterpret_cast<uint2 *>(a->codes_dev);
     in.scales = a->scales_dev;
     in.rstd = a->rstd_dev;
-    in.aligned = vectors_ok(a->x_dev, a->dtype, a->rows, a->x_stride) && vectors_ok(a->residual_dev, a->dtype, a->rows, a->residual_dev ? a->residual_stride : 0) &&
+    const bool aligned = vectors_ok(a->x_dev, a->dtype, a->rows, a->x_stride) && vectors_ok(a->residual_dev, a->dtype, a->rows, a->residual_dev ? a->residual_stride : 0) &&
                  vectors_ok(a->total_dev, a->dtype, a->rows, a->total_dev ? a->total_stride : 0) && vectors_ok(a->out_dev, a->dtype, a->rows, a->out_dev ? a->cols : 0) &&
                  aligned_to(a->gain_dev, 16);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return a->dtype == PS_GRAD_BF16 ? launch_norm<bf16>(in, st) : launch_norm<float>(in, st);
+    const auto go = [&](auto vectors) { return a->dtype == PS_GRAD_BF16 ? launch_norm<bf16, vectors>(in, st) : launch_norm<float, vectors>(in, st); };
+    return aligned ? go(std::true_type{}) : go(std::false_type{});
 }
 
 int ps_norm_grad_workspace(int64_t rows, int64_t cols, int64_t *bytes)
 {
     if (!bytes || !shape_ok(rows, cols)) return PS_ERR_INVALID_ARG;
-    *bytes = grad_shape(rows, cols).parts * cols * 4;
+    *bytes = std::max(grad_shape<bf16>(rows, cols).parts, grad_shape<float>(rows, cols).parts) * cols * 4;
     return PS_OK;
 }
 
@@ -191,7 +201,7 @@ int ps_rms_norm_grad(const ps_norm_grad *a, void *workspace_dev, int64_t workspa
     if (a->codes_dev || a->scales_dev ? !packed_ok(a->codes_dev, a->scales_dev) || a->total_dev : !rows_ok(a->total_dev, a->dtype, a->rows, a->cols, a->total_stride))
         return PS_ERR_INVALID_ARG;
     if (a->rows > 1 && ((a->dx_dev == a->dout_dev && a->dout_stride != a->cols) || (a->dx_dev == a->dtotal_dev && a->dtotal_stride != a->cols))) return PS_ERR_INVALID_ARG;
-    const GradShape shape = grad_shape(a->rows, a->cols);
+    const GradShape shape = grad_shape(a->dtype, a->rows, a->cols);
     // rows beyond a block's registers: the gain's gradient reads dout again after dx is there
     if (a->dx_dev == a->total_dev || (!shape.warps && a->dgain_dev && a->dx_dev == a->dout_dev)) return PS_ERR_INVALID_ARG;
     if (a->dgain_dev && (!workspace_dev || !aligned_to(workspace_dev, 16) || workspace_bytes < shape.parts * a->cols * 4)) return PS_ERR_INVALID_ARG;
@@ -205,11 +215,15 @@ int ps_rms_norm_grad(const ps_norm_grad *a, void *workspace_dev, int64_t workspa
     in.gain_bf16 = a->gain_dtype == PS_GRAD_BF16;
     in.rows = a->rows; in.dout_stride = a->dout_stride; in.dtotal_stride = a->dtotal_stride; in.total_stride = a->total_stride;
     in.cols = static_cast<int>(a->cols);
-    in.aligned = vectors_ok(a->dout_dev, a->dtype, a->rows, a->dout_stride) && vectors_ok(a->dx_dev, a->dtype, a->rows, a->cols) &&
+    const bool aligned = vectors_ok(a->dout_dev, a->dtype, a->rows, a->dout_stride) && vectors_ok(a->dx_dev, a->dtype, a->rows, a->cols) &&
                  vectors_ok(a->dtotal_dev, a->dtype, a->rows, a->dtotal_dev ? a->dtotal_stride : 0) && vectors_ok(a->total_dev, a->dtype, a->rows, a->total_dev ? a->total_stride : 0) &&
                  aligned_to(a->gain_dev, 16);
-    const auto go = [&](auto codes) { return a->dtype == PS_GRAD_BF16 ? launch_norm_grad<bf16, codes>(in, shape, st) : launch_norm_grad<float, codes>(in, shape, st); };
-    const int status = in.codes ? go(std::true_type{}) : go(std::false_type{});
+    const auto go = [&](auto codes, auto vectors) {
+        return a->dtype == PS_GRAD_BF16 ? launch_norm_grad<bf16, codes, vectors>(in, shape, st) : launch_norm_grad<float, codes, vectors>(in, shape, st);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    const int status = in.codes ? aligned ? go(yes, yes) : go(yes, no) : aligned ? go(no, yes) : go(no, no);
     if (status != PS_OK || !a->dgain_dev) return status;
     return softsync::launch(softsync::gain_grad_kernel, div_up(a->cols, 32), 32 * softsync::kGainWarps, 0, true, st, in.parts, static_cast<int>(shape.parts), in.cols, a->dgain_dev,
                             in.gain_bf16) ? PS_OK : PS_ERR_CUDA;

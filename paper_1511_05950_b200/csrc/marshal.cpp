@@ -5,6 +5,7 @@
 
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -289,11 +290,13 @@ PyObject *written(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 // ---- losses without logits, norm, activations in 8 bits ----------------------------------------------------------------------
+// A new tensor on the GPU of another one, past the dispatcher (a third of its time, and a call of the norm makes five).
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &like) { return at::detail::empty_cuda(sizes, type, like.device(), std::nullopt); }
 bool rows_fine(const at::Tensor &t) { return t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1); }
 int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.size(1), 1); }
 template <typename T> T *data(const at::Tensor &t) { return t.defined() ? static_cast<T *>(t.data_ptr()) : nullptr; }
 template <typename T> const T *const_data(const at::Tensor &t) { return t.defined() ? static_cast<const T *>(t.const_data_ptr()) : nullptr; }
-at::Tensor scratch(int64_t bytes, const at::Tensor &like) { return at::empty({std::max<int64_t>(bytes, 16)}, like.options().dtype(at::kByte)); }
+at::Tensor scratch(int64_t bytes, const at::Tensor &like) { return fresh({std::max<int64_t>(bytes, 16)}, at::kByte, like); }
 
 // Rows of activations on the GPU, fp32 or bf16.
 const at::Tensor &rows_of(PyObject *o, const char *what)
@@ -334,8 +337,8 @@ struct Packed {
     Packed() = default;
     Packed(int64_t r, int64_t c, const at::Tensor &like) : rows(r), cols(c)
     {
-        codes = at::empty({r, padded(c)}, like.options().dtype(at::kChar));
-        scales = at::empty({r, padded(c) / PS_PACK_BLOCK}, like.options().dtype(at::kByte));
+        codes = fresh({r, padded(c)}, at::kChar, like);
+        scales = fresh({r, padded(c) / PS_PACK_BLOCK}, at::kByte, like);
     }
     Packed(PyObject *codes_, PyObject *scales_, PyObject *cols_) : codes(tensor_of(codes_, "codes")), scales(tensor_of(scales_, "scales"))
     {
@@ -372,7 +375,7 @@ struct Head {
         c.tokens_dev = per_row<int64_t>(tokens, c.rows, "tokens", hidden);
         c.temperature = static_cast<float>(number(temperature));
     }
-    at::Tensor floats(int64_t n) const { return at::empty({n}, hidden.options().dtype(at::kFloat)); }
+    at::Tensor floats(int64_t n) const { return fresh({n}, at::kFloat, hidden); }
     at::Tensor workspace(bool grad) const
     {
         int64_t need = 0;
@@ -394,8 +397,8 @@ struct Wanted {
         head = PyUnicode_CompareWithASCIIString(o, "head") == 0;
         TORCH_CHECK_VALUE(hidden || head, "grad is True, False, 'hidden' or 'head'");
     }
-    at::Tensor of_hidden(const Head &h) const { return hidden ? at::empty({h.c.rows, h.c.width}, h.hidden.options()) : at::Tensor(); }
-    at::Tensor of_head(const Head &h) const { return head ? at::empty({h.c.vocab, h.c.width}, h.head.options()) : at::Tensor(); }
+    at::Tensor of_hidden(const Head &h) const { return hidden ? fresh({h.c.rows, h.c.width}, at::kBFloat16, h.hidden) : at::Tensor(); }
+    at::Tensor of_head(const Head &h) const { return head ? fresh({h.c.vocab, h.c.width}, at::kBFloat16, h.head) : at::Tensor(); }
 };
 
 // (hidden, head, tokens, weights, temperature) -> (status, logp, lse)
@@ -466,7 +469,7 @@ PyObject *unpack8(PyObject *, PyObject *const *a, Py_ssize_t n)
     const Packed p(a[0], a[1], a[2]);
     const c10::cuda::CUDAGuard guard(p.codes.device());
     const bool half = a[3] == Py_True;
-    const at::Tensor out = at::empty({p.rows, p.cols}, p.codes.options().dtype(half ? at::kBFloat16 : at::kFloat));
+    const at::Tensor out = fresh({p.rows, p.cols}, half ? at::kBFloat16 : at::kFloat, p.codes);
     const int status = call_unpack8(const_data<int8_t>(p.codes), const_data<uint8_t>(p.scales), p.rows, p.cols, out.data_ptr(), half ? PS_GRAD_BF16 : PS_GRAD_FP32, p.cols,
                                     c10::cuda::getCurrentCUDAStream().stream());
     return result(status, {out});
@@ -486,10 +489,10 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     const c10::cuda::CUDAGuard guard(x.device());
     ps_norm c{};
     c.eps = static_cast<float>(number(a[3]));
-    at::Tensor total = residual.defined() ? inplace ? residual : at::empty({rows, cols}, x.options()) : at::Tensor(), out;
-    if (want_out) out = at::empty({rows, cols}, x.options());
+    at::Tensor total = residual.defined() ? inplace ? residual : fresh({rows, cols}, x.scalar_type(), x) : at::Tensor(), out;
+    if (want_out) out = fresh({rows, cols}, x.scalar_type(), x);
     const Packed p = want_codes ? Packed(rows, cols, x) : Packed();
-    const at::Tensor rstd = at::empty({rows}, x.options().dtype(at::kFloat));
+    const at::Tensor rstd = fresh({rows}, at::kFloat, x);
     c.x_dev = x.const_data_ptr(); c.residual_dev = const_data<void>(residual); c.gain_dev = const_data<void>(gain);
     c.dtype = grad_dtype(x.scalar_type());
     c.gain_dtype = gain.defined() ? grad_dtype(gain.scalar_type()) : c.dtype;
@@ -527,7 +530,7 @@ PyObject *rms_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor gain = gain_of(a[4], cols, dout), dtotal = rows_like(a[5], "dtotal", dout);
     const bool want_gain = a[6] == Py_True && gain.defined();
     const c10::cuda::CUDAGuard guard(dout.device());
-    const at::Tensor dx = at::empty({rows, cols}, dout.options()), dgain = want_gain ? at::empty({cols}, gain.options()) : at::Tensor();
+    const at::Tensor dx = fresh({rows, cols}, dout.scalar_type(), dout), dgain = want_gain ? fresh({cols}, gain.scalar_type(), gain) : at::Tensor();
     int64_t need = 0;
     TORCH_CHECK_VALUE(norm_grad_workspace(rows, cols, &need) == PS_OK, "too many rows or columns, or none: ", rows, " x ", cols);
     const at::Tensor ws = scratch(want_gain ? need : 0, dout);
@@ -557,7 +560,7 @@ PyObject *packed_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor gain = gain_of(a[4], p.cols, dout);
     const bool wide = a[5] == Py_True;
     const c10::cuda::CUDAGuard guard(dout.device());
-    const at::Tensor dweight = at::empty({dout.size(1), p.cols}, dout.options().dtype(wide ? at::kFloat : at::kBFloat16));
+    const at::Tensor dweight = fresh({dout.size(1), p.cols}, wide ? at::kFloat : at::kBFloat16, dout);
     ps_packed_grad c{};
     c.dout_dev = dout.const_data_ptr(); c.gain_dev = const_data<void>(gain); c.codes_dev = const_data<int8_t>(p.codes); c.scales_dev = const_data<uint8_t>(p.scales);
     c.gain_dtype = gain.defined() ? grad_dtype(gain.scalar_type()) : PS_GRAD_FP32;

@@ -37,14 +37,13 @@ struct NormIn {
     uint2 *codes;                         // may be null; rows of round_up(cols, 32) codes
     uint8_t *scales;
     float *rstd;
-    int aligned;                          // every row and the gain allow vectors
 };
 
-// What is left of a row's unit once its normalised values n are known.
-template <typename T>
-__device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, int unit, const Unit &n, const Unit &gain, bool live)
+// What is left of a row's unit once its normalised values n are known; by whole warps.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, int unit, const Unit &n, const Unit &gain, WarpDesk<T> *desk)
 {
-    const int col = unit * kUnit, left = in.cols - col, units = (in.cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
+    const int units = (in.cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
     if (in.codes) {                                       // the whole warp: lanes of a block work together
         unsigned scale;
         const uint2 codes = pack_unit(n, scale);
@@ -53,11 +52,11 @@ __device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, in
             if ((unit & 3) == 0) in.scales[row * (units / 4) + unit / 4] = static_cast<uint8_t>(scale);
         }
     }
-    if (in.out && live) {
+    if (in.out) {
         Unit y;
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) y.v[k] = n.v[k] * gain.v[k];
-        store_unit(static_cast<T *>(in.out) + row * in.cols + col, y, left, in.aligned && left >= kUnit);
+        store_row<ALIGNED>(static_cast<T *>(in.out) + row * in.cols, unit, in.cols, y, desk);
     }
 }
 
@@ -65,10 +64,11 @@ __device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, in
 // WARPS warps a row (one warp: a block has kNormRows rows), UNITS units a thread: the row stays in registers between its sum and its outputs, so
 // each byte crosses HBM once.
 constexpr int kNormRows = 4;
-template <typename T, int WARPS, int UNITS>
+template <typename T, int WARPS, int UNITS, bool ALIGNED>
 __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_norm_kernel(const __grid_constant__ NormIn in)
 {
     __shared__ float part[2][32];
+    __shared__ WarpDesk<T> desk[ALIGNED ? 1 : WARPS == 1 ? kNormRows : WARPS];
     constexpr int T_ROW = 32 * WARPS;
     wait_for_earlier();
     let_next_start();
@@ -81,8 +81,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
     for (int j = 0; j < UNITS; ++j) {
         const int col = (j * T_ROW + tid) * kUnit, left = in.cols - col;
         if (left > 0) {
-            load_unit(a[j], x + col, left, in.aligned && left >= kUnit);
-            if (in.residual) load_unit(b[j], res + col, left, in.aligned && left >= kUnit);
+            load_unit(a[j], x + col, left, ALIGNED && left >= kUnit);
+            if (in.residual) load_unit(b[j], res + col, left, ALIGNED && left >= kUnit);
         }
     }
     Unit u[UNITS];
@@ -97,11 +97,11 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
 #pragma unroll
                 for (int k = 0; k < kUnit; ++k) u[j].v[k] = rounded<T>(u[j].v[k] + r.v[k]);
             }
-            if (in.total) store_unit(static_cast<T *>(in.total) + row * in.total_stride + col, u[j], left, in.aligned && left >= kUnit);
         } else {
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) u[j].v[k] = 0.f;
         }
+        if (in.total) store_row<ALIGNED>(static_cast<T *>(in.total) + row * in.total_stride, j * T_ROW + tid, in.cols, u[j], desk);
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) s = fmaf(u[j].v[k], u[j].v[k], s);
@@ -117,24 +117,25 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) u[j].v[k] *= r;
         Unit gain{};
-        if (in.out && left > 0) gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, in.aligned && left >= kUnit);
-        norm_outputs<T>(in, row, unit, u[j], gain, left > 0);
+        if (in.out && left > 0) gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, ALIGNED && left >= kUnit);
+        norm_outputs<T, ALIGNED>(in, row, unit, u[j], gain, desk);
     }
 }
 
 // Rows longer than the registers of a block: read twice (the second time mostly from the L2), squares added up in fp64 across a thread's units.
 constexpr int kLongThreads = 512;
-template <typename T>
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(const __grid_constant__ NormIn in)
 {
     __shared__ double part[kLongThreads / 32];
+    __shared__ WarpDesk<T> desk[ALIGNED ? 1 : kLongThreads / 32];
     wait_for_earlier();
     let_next_start();
     const long long row = blockIdx.x;
     const T *x = static_cast<const T *>(in.x) + row * in.x_stride, *res = static_cast<const T *>(in.residual) + (in.residual ? row * in.residual_stride : 0);
     T *total = static_cast<T *>(in.total) + (in.total ? row * in.total_stride : 0);
     const auto values = [&](int col, int left) {
-        const bool whole = in.aligned && left >= kUnit;
+        const bool whole = ALIGNED && left >= kUnit;
         RawUnit<T> a, b;
         load_unit(a, x + col, left, whole);
         Unit u = a.values();
@@ -167,12 +168,15 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(const __gri
         Unit u{}, gain{};
         if (left > 0) {
             u = values(col, left);
-            if (in.total) store_unit(total + col, u, left, in.aligned && left >= kUnit);
-            if (in.out) gain = load_gain(in.gain, in.gain_bf16, col, left, in.aligned && left >= kUnit);
+            if (in.out) gain = load_gain(in.gain, in.gain_bf16, col, left, ALIGNED && left >= kUnit);
+        }
+        if (in.total) {
+            __syncwarp();                                  // total may be the residual: no lane writes before all have read
+            store_row<ALIGNED>(total, unit, in.cols, u, desk);
         }
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) u.v[k] *= r;
-        norm_outputs<T>(in, row, unit, u, gain, left > 0);
+        norm_outputs<T, ALIGNED>(in, row, unit, u, gain, desk);
     }
 }
 
@@ -187,12 +191,11 @@ struct NormGradIn {
     int gain_bf16;
     long long rows, dout_stride, dtotal_stride, total_stride;
     int cols;
-    int aligned;
 };
 
 // n of one unit, from the codes or from the total.
-template <typename T, bool CODES> struct KeptUnit;
-template <typename T> struct KeptUnit<T, true> {
+template <typename T, bool CODES, bool ALIGNED> struct KeptUnit;
+template <typename T, bool ALIGNED> struct KeptUnit<T, true, ALIGNED> {
     uint2 codes;
     unsigned scale;
     __device__ __forceinline__ void load(const NormGradIn &in, long long row, int unit, int)
@@ -203,11 +206,11 @@ template <typename T> struct KeptUnit<T, true> {
     }
     __device__ __forceinline__ Unit values(float) const { return unpack_unit(codes, scale); }
 };
-template <typename T> struct KeptUnit<T, false> {
+template <typename T, bool ALIGNED> struct KeptUnit<T, false, ALIGNED> {
     RawUnit<T> raw;
     __device__ __forceinline__ void load(const NormGradIn &in, long long row, int unit, int left)
     {
-        load_unit(raw, static_cast<const T *>(in.total) + row * in.total_stride + unit * kUnit, left, in.aligned && left >= kUnit);
+        load_unit(raw, static_cast<const T *>(in.total) + row * in.total_stride + unit * kUnit, left, ALIGNED && left >= kUnit);
     }
     __device__ __forceinline__ Unit values(float rstd) const
     {
@@ -218,11 +221,14 @@ template <typename T> struct KeptUnit<T, false> {
     }
 };
 
+// Warps of an SM: as many as have registers for what a thread holds of two rows.
+template <typename T, int UNITS> constexpr int kGradWarps = UNITS == 1 && sizeof(T) == 2 ? 32 : 16;
+
 // What a thread loads of one row.
-template <typename T, int WARPS, int UNITS, bool CODES>
+template <typename T, int WARPS, int UNITS, bool CODES, bool ALIGNED>
 struct GradRow {
     RawUnit<T> dout[UNITS], dtotal[UNITS];
-    KeptUnit<T, CODES> kept[UNITS];
+    KeptUnit<T, CODES, ALIGNED> kept[UNITS];
     float rstd;
     __device__ __forceinline__ void load(const NormGradIn &in, long long row, int tid)
     {
@@ -232,19 +238,20 @@ struct GradRow {
         for (int j = 0; j < UNITS; ++j) {
             const int unit = j * 32 * WARPS + tid, left = in.cols - unit * kUnit;
             if (left <= 0) continue;
-            load_unit(dout[j], d + unit * kUnit, left, in.aligned && left >= kUnit);
+            load_unit(dout[j], d + unit * kUnit, left, ALIGNED && left >= kUnit);
             kept[j].load(in, row, unit, left);
-            if (in.dtotal) load_unit(dtotal[j], t + unit * kUnit, left, in.aligned && left >= kUnit);
+            if (in.dtotal) load_unit(dtotal[j], t + unit * kUnit, left, ALIGNED && left >= kUnit);
         }
     }
 };
 
 // g = dout gain, dx = dtotal + r (g - n mean(g n)), and each block's part of dgain = sum of dout n over its rows: rows are dealt out in turn, so
 // the parts, and their sum in the next kernel, have a fixed order.  The next row's loads are under way while a row waits for its sum.
-template <typename T, int WARPS, int UNITS, bool CODES>
-__global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, WARPS <= 4 ? 4 : WARPS == 8 ? 2 : 1) rms_norm_grad_kernel(const __grid_constant__ NormGradIn in)
+template <typename T, int WARPS, int UNITS, bool CODES, bool ALIGNED>
+__global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGradWarps<T, UNITS> / (WARPS == 1 ? kNormRows : WARPS)) rms_norm_grad_kernel(const __grid_constant__ NormGradIn in)
 {
     __shared__ float part[2][32];
+    __shared__ WarpDesk<T> desk[ALIGNED ? 1 : WARPS == 1 ? kNormRows : WARPS];
     constexpr int T_ROW = 32 * WARPS, GROUPS = WARPS == 1 ? kNormRows : 1;
     wait_for_earlier();
     let_next_start();
@@ -257,7 +264,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, WARP
     int slot = 0;
     const long long step = static_cast<long long>(gridDim.x) * GROUPS;
     long long row = static_cast<long long>(blockIdx.x) * GROUPS + group;
-    GradRow<T, WARPS, UNITS, CODES> next;
+    GradRow<T, WARPS, UNITS, CODES, ALIGNED> next;
     if (row < in.rows) next.load(in, row, tid);
     for (; row < in.rows; row += step, slot ^= 1) {
         const float r = next.rstd;
@@ -271,7 +278,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, WARP
             g[j] = next.dout[j].values();
             n[j] = next.kept[j].values(r);
             more[j] = next.dtotal[j];
-            const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, in.aligned && left >= kUnit);
+            const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, ALIGNED && left >= kUnit);
             float s = 0.f;
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) {
@@ -285,17 +292,19 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, WARP
         const float mean = row_sum<WARPS>(sum, part, slot) / static_cast<float>(in.cols);
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
-            const int col = (j * T_ROW + tid) * kUnit, left = in.cols - col;
-            if (left <= 0) continue;
-            Unit dx;
+            const int unit = j * T_ROW + tid;
+            if (ALIGNED && unit * kUnit >= in.cols) continue;
+            Unit dx{};
+            if (ALIGNED || unit * kUnit < in.cols) {
 #pragma unroll
-            for (int k = 0; k < kUnit; ++k) dx.v[k] = r * fmaf(-n[j].v[k], mean, g[j].v[k]);
-            if (in.dtotal) {
-                const Unit m = more[j].values();
+                for (int k = 0; k < kUnit; ++k) dx.v[k] = r * fmaf(-n[j].v[k], mean, g[j].v[k]);
+                if (in.dtotal) {
+                    const Unit m = more[j].values();
 #pragma unroll
-                for (int k = 0; k < kUnit; ++k) dx.v[k] += m.v[k];
+                    for (int k = 0; k < kUnit; ++k) dx.v[k] += m.v[k];
+                }
             }
-            store_unit(static_cast<T *>(in.dx) + row * in.cols + col, dx, left, in.aligned && left >= kUnit);
+            store_row<ALIGNED>(static_cast<T *>(in.dx) + row * in.cols, unit, in.cols, dx, desk);
         }
     }
     if (!in.parts) return;
@@ -309,7 +318,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, WARP
 }
 
 // Longer rows: dout and the kept values are read twice (the second time mostly from the L2); the gain's gradient is a kernel of its own.
-template <typename T, bool CODES>
+template <typename T, bool CODES, bool ALIGNED>
 __global__ void __launch_bounds__(kLongThreads) rms_norm_grad_long_kernel(const __grid_constant__ NormGradIn in)
 {
     __shared__ double part[kLongThreads / 32];
@@ -319,12 +328,12 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_grad_long_kernel(const 
     const float r = in.rstd[row];
     const auto values = [&](int unit, int left, Unit &g, Unit &n) {
         RawUnit<T> d;
-        KeptUnit<T, CODES> kept;
-        load_unit(d, static_cast<const T *>(in.dout) + row * in.dout_stride + unit * kUnit, left, in.aligned && left >= kUnit);
+        KeptUnit<T, CODES, ALIGNED> kept;
+        load_unit(d, static_cast<const T *>(in.dout) + row * in.dout_stride + unit * kUnit, left, ALIGNED && left >= kUnit);
         kept.load(in, row, unit, left);
         g = d.values();
         n = kept.values(r);
-        const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, in.aligned && left >= kUnit);
+        const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, ALIGNED && left >= kUnit);
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) g.v[k] *= gain.v[k];
     };
@@ -351,15 +360,15 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_grad_long_kernel(const 
         for (int k = 0; k < kUnit; ++k) dx.v[k] = r * fmaf(-n.v[k], mean, g.v[k]);
         if (in.dtotal) {
             RawUnit<T> t;
-            load_unit(t, static_cast<const T *>(in.dtotal) + row * in.dtotal_stride + col, left, in.aligned && left >= kUnit);
+            load_unit(t, static_cast<const T *>(in.dtotal) + row * in.dtotal_stride + col, left, ALIGNED && left >= kUnit);
             const Unit more = t.values();
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) dx.v[k] += more.v[k];
         }
-        store_unit(static_cast<T *>(in.dx) + row * in.cols + col, dx, left, in.aligned && left >= kUnit);
+        store_unit(static_cast<T *>(in.dx) + row * in.cols + col, dx, left, ALIGNED && left >= kUnit);
     }
 }
-template <typename T, bool CODES>
+template <typename T, bool CODES, bool ALIGNED>
 __global__ void __launch_bounds__(128) gain_grad_long_kernel(const __grid_constant__ NormGradIn in)
 {
     wait_for_earlier();
@@ -369,8 +378,8 @@ __global__ void __launch_bounds__(128) gain_grad_long_kernel(const __grid_consta
     Unit acc{};
     for (long long row = blockIdx.y; row < in.rows; row += gridDim.y) {
         RawUnit<T> d;
-        KeptUnit<T, CODES> kept;
-        load_unit(d, static_cast<const T *>(in.dout) + row * in.dout_stride + unit * kUnit, left, in.aligned && left >= kUnit);
+        KeptUnit<T, CODES, ALIGNED> kept;
+        load_unit(d, static_cast<const T *>(in.dout) + row * in.dout_stride + unit * kUnit, left, ALIGNED && left >= kUnit);
         kept.load(in, row, unit, left);
         const Unit g = d.values(), n = kept.values(in.rstd[row]);
 #pragma unroll
@@ -391,6 +400,7 @@ __global__ void __launch_bounds__(32 * kGainWarps) gain_grad_kernel(const float 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = static_cast<int>(blockIdx.x) * 32 + lane;
     float s = 0.f;
     if (col < cols)
+#pragma unroll 8
         for (int k = warp; k < count; k += kGainWarps) s += parts[static_cast<long long>(k) * cols + col];
     sums[warp][lane] = s;
     __syncthreads();

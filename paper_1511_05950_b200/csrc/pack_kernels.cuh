@@ -71,8 +71,26 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const uint2 *codes
         int col;
         shape.find(at, row, col);
         const int left = shape.cols - col;
-        if (left > 0) store_unit(out + row * shape.stride + col, unpack_unit(c[j], s[j]), left, shape.aligned && left >= kUnit);
+        if (left > 0) store_unit(out + row * shape.stride + col, unpack_unit(c[j], s[j]), left, left >= kUnit);
     }
+}
+
+// The same for rows that allow no vectors: a warp takes 32 units of one row.
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads) unpack_rows_kernel(const uint2 *codes, const uint8_t *scales, const __grid_constant__ PackShape shape, T *out)
+{
+    __shared__ WarpDesk<T> desk[kPackThreads / 32];
+    wait_for_earlier();
+    let_next_start();
+    const unsigned warps = static_cast<unsigned>(shape.units + 31) / 32, item = blockIdx.x * (kPackThreads / 32) + (threadIdx.x >> 5), row = item / warps;
+    if (row >= shape.count / static_cast<unsigned>(shape.units)) return;            // a whole warp
+    const int unit = static_cast<int>(item - row * warps) * 32 + static_cast<int>(threadIdx.x & 31);
+    Unit u{};
+    if (unit < shape.units) {
+        const unsigned at = row * static_cast<unsigned>(shape.units) + unit;
+        u = unpack_unit(__ldcs(codes + at), __ldcs(scales + (at >> 2)));
+    }
+    store_row<false>(out + row * shape.stride, unit, shape.cols, u, desk);
 }
 
 }  // namespace softsync

@@ -103,6 +103,27 @@ __device__ __forceinline__ void store_unit(T *p, const Unit &u, int n, bool whol
     }
 }
 
+// Stores of rows that allow no vectors: a warp's 32 units (256 neighbouring elements of a row) go through shared memory, so that neighbouring lanes write
+// neighbouring elements; unit by unit, a store of two bytes touched as many sectors as one of sixteen (5003 x 1100, bf16: 22 us).
+template <typename T> struct WarpDesk { alignas(16) T v[32 * kUnit]; };
+
+// This lane's unit of a row, by all lanes of a warp that has 32 neighbouring units.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void store_row(T *row, int unit, int cols, const Unit &u, WarpDesk<T> *desk)
+{
+    const int lane = threadIdx.x & 31, left = cols - unit * kUnit;
+    if constexpr (ALIGNED) {
+        if (left > 0) store_unit(row + unit * kUnit, u, left, left >= kUnit);
+    } else {
+        T *v = desk[threadIdx.x >> 5].v;
+        store_unit(v + lane * kUnit, u, kUnit, true);
+        __syncwarp();
+        const int first = (unit - lane) * kUnit + lane;
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) if (first + k * 32 < cols) row[first + k * 32] = v[lane + k * 32];
+        __syncwarp();
+    }
+}
 template <typename T> __device__ __forceinline__ float rounded(float x);
 template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
 template <> __device__ __forceinline__ float rounded<__nv_bfloat16>(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
@@ -117,23 +138,30 @@ __device__ __forceinline__ unsigned block_scale(unsigned max_bits)
 }
 __device__ __forceinline__ float scale_unit(unsigned s) { return __uint_as_float(s << 23); }
 
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // Eight codes from the eight values of this lane; the four lanes of a block have to call it together.
 __device__ __forceinline__ uint2 pack_unit(const Unit &u, unsigned &scale)
 {
-    unsigned m = 0;
+    float top = max_or_nan(fabsf(u.v[0]), fabsf(u.v[1]));
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) m = max(m, __float_as_uint(u.v[k]) & 0x7fffffffu);
+    for (int k = 2; k < kUnit; ++k) top = max_or_nan(top, fabsf(u.v[k]));
+    unsigned m = __float_as_uint(top);                      // a NaN is above every number, an infinity above every finite one
     m = max(m, __shfl_xor_sync(kAllLanes, m, 1));
     m = max(m, __shfl_xor_sync(kAllLanes, m, 2));
     scale = block_scale(m);
-    // x / unit + 1.5 * 2^23 rounds to nearest, ties to even: |x| / unit is below 128, so the code is in the sum's low byte
-    const float inv = scale == 255u ? 0.f : __uint_as_float((254u - scale) << 23);
+    // x / unit + 1.5 * 2^23 rounds to nearest, ties to even (the product is exact: the sum is rounded once): |x| / unit is below 128, so the code is in the low byte
+    constexpr float middle = 12582912.f;
+    const float inv = __uint_as_float((254u - scale) << 23);
     unsigned b[kUnit];
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) {
-        const float x = scale == 255u ? 0.f : fminf(fmaxf(u.v[k] * inv, -127.f), 127.f);
-        b[k] = __float_as_uint(x + 12582912.f);
-    }
+    for (int k = 0; k < kUnit; ++k) b[k] = __float_as_uint(fminf(fmaxf(fmaf(u.v[k], inv, middle), middle - 127.f), middle + 127.f));
+    if (scale == 255u) return make_uint2(0, 0);
     return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
                       __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
 }
