@@ -151,13 +151,16 @@ int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, 
 /* ------------------------------------------------------------------------------------------------------------------
  * Losses without logits.  The logits of a position are the products of its hidden state with the rows of the output matrix (the head),
  *     z_tj = hidden_t . head_j / T,     lse_t = log sum_j exp(z_tj),     logp_t = z_t,token - lse_t
- * They are computed a tile at a time (tensor cores, fp32 sums) and never leave the chip; the gradients compute them again, a piece of the
- * vocabulary after the other, and of a piece only the rounded bf16 values
+ * They are computed a tile at a time (tensor cores, fp32 sums) and never leave the chip.  The gradients go through the vocabulary piece by piece; of a piece
+ * the rounded bf16 values
  *     G_tj = a_t (p_tj - 1[j = token])
- * are held in the workspace, for the two products  dhidden = scale G head  and  dhead = scale G^T hidden  (sums in fp32, in a fixed order).
+ * are held in the workspace, for the two products  dhidden = scale G head  and  dhead = scale G^T hidden  (sums in fp32, in a fixed order).  A piece is as wide as
+ * 1 GiB of G allows (or as many bytes as the hidden states have, where that is more); ps_head_cross_entropy keeps the exponentials of the last piece from
+ * its statistics (16 bits each, 10 of fraction), the other pieces' logits are computed again.
  * Rows with a weight (or a dlogp) of exactly zero take no part, whatever they or their token hold: they are not read, their outputs and their
- * dhidden are zero.  A token outside [0, vocab) makes its row's results NaN; a row with a NaN or an infinity has NaN results (minus infinity as the
- * product of a finite row with an entry of the head is a barred entry, p = 0).  NaN results of a row with a weight reach the loss and dhead.
+ * dhidden are zero.  A token outside [0, vocab) makes its row's results NaN; so does a NaN or an infinity in a row, or a product that is plus infinity.  An entry of the head
+ * whose product with a row is minus infinity is barred (p = 0); a row of nothing else is NaN, and infinities of the head make dhidden NaN.  NaN
+ * results of a row that takes part reach the loss and dhead.  Outputs must not overlap inputs.
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef struct ps_head {
     const void *hidden_dev;               /* bf16, rows of `width` values, hidden_stride elements apart */

@@ -292,7 +292,7 @@ PyObject *written(PyObject *, PyObject *const *a, Py_ssize_t n)
 // ---- losses without logits, norm, activations in 8 bits ----------------------------------------------------------------------
 // A new tensor on the GPU of another one, past the dispatcher (a third of its time, and a call of the norm makes five).
 at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &like) { return at::detail::empty_cuda(sizes, type, like.device(), std::nullopt); }
-bool rows_fine(const at::Tensor &t) { return t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1); }
+bool rows_fine(const at::Tensor &t) { return t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1 || t.size(0) == 0); }       // without rows any strides will do
 int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.size(1), 1); }
 template <typename T> T *data(const at::Tensor &t) { return t.defined() ? static_cast<T *>(t.data_ptr()) : nullptr; }
 template <typename T> const T *const_data(const at::Tensor &t) { return t.defined() ? static_cast<const T *>(t.const_data_ptr()) : nullptr; }

@@ -135,6 +135,7 @@ struct MmaPlan {
     int live_is_k;
     int slots;                            // pairs that work at once, where the last tiles may be split along the contraction; else 0
     int group;                            // row tiles whose turns come before the next column tile's
+    int splits;                           // of the last tiles, where the host knows (no `live`)
 };
 // How the operands lie: MN-major or K-major.
 template <bool A, bool B> struct Lying { static constexpr bool mn_a = A, mn_b = B; };
@@ -187,16 +188,21 @@ struct TileWalk {
         splits = 1;
         if (!p.slots) return;
         const int rest = static_cast<int>(static_cast<unsigned>(count) % static_cast<unsigned>(p.slots));
-        if (!rest || (splits = warp_split_count(rest, all_steps, p.slots)) == 1) return;
+        if (!rest || (splits = p.live ? warp_split_count(rest, all_steps, p.slots) : p.splits) == 1) return;
         whole = count - rest;
         count = whole + rest * splits;
     }
     __device__ __forceinline__ void place(unsigned tile, int &m, int &n) const
     {
+        if (tiles_m <= group) {
+            n = static_cast<int>(tile / static_cast<unsigned>(tiles_m));
+            m = static_cast<int>(tile) - n * tiles_m;
+            return;
+        }
         const unsigned band = static_cast<unsigned>(group) * static_cast<unsigned>(tiles_n), b = tile / band, at = tile - b * band;
         const unsigned high = static_cast<unsigned>(min(group, tiles_m - static_cast<int>(b) * group));
         n = static_cast<int>(at / high);
-        m = static_cast<int>(b) * group + static_cast<int>(at % high);
+        m = static_cast<int>(b * static_cast<unsigned>(group) + (at - static_cast<unsigned>(n) * high));
     }
     __device__ __forceinline__ TileAt at(int t) const
     {
@@ -327,7 +333,7 @@ struct GradEpilogue {
     const float2 *norms;                  // of the rows that take part, or null: from lse
     const float *lse, *coef;              // of all rows; coef null: 1
     float sign;                           // of coef
-    int rows;
+    int rows, vocab;
     const int *live;
     float scale;
     int first, width;                     // the piece: columns [first, first + width)
@@ -349,6 +355,7 @@ struct GradEpilogue {
             tok = t >= first && t < first + width ? static_cast<int>(t - first) : -1;
             a = coef ? sign * coef[at] : 1.f;
             norm = row_normaliser(norms, lse, r, at);
+            if (t < 0 || t >= vocab) norm.y = CUDART_NAN_F;
         }
     }
     __device__ __forceinline__ void take(float (&x)[32], int col, unsigned desk)
@@ -400,69 +407,97 @@ struct StoreTarget {
 
     __device__ __forceinline__ int count() const { return live ? *live : rows; }
     __device__ __forceinline__ float factor() const { return alpha_dev ? alpha * *alpha_dev : alpha; }
-    __device__ __forceinline__ void store(int row, int place, int col, Unit &u, float factor) const
+    __device__ __forceinline__ void add_sum(int row, int col, Unit &u) const
     {
-        const int left = cols - col;
-        if (left <= 0) return;
-        float *s = sum + static_cast<long long>(row) * sum_stride + col;
-        if (add) {
-            const float4 a = reinterpret_cast<const float4 *>(s)[0], b = reinterpret_cast<const float4 *>(s)[1];
-            u.v[0] += a.x; u.v[1] += a.y; u.v[2] += a.z; u.v[3] += a.w; u.v[4] += b.x; u.v[5] += b.y; u.v[6] += b.z; u.v[7] += b.w;
-        }
-        if (!out) {
-            store_unit(s, u, kUnit, true);
-            return;
-        }
-        const bool whole = vectors && left >= kUnit;
+        const float4 *s = reinterpret_cast<const float4 *>(sum + static_cast<long long>(row) * sum_stride + col);
+        const float4 a = s[0], b = s[1];
+        u.v[0] += a.x; u.v[1] += a.y; u.v[2] += a.z; u.v[3] += a.w; u.v[4] += b.x; u.v[5] += b.y; u.v[6] += b.z; u.v[7] += b.w;
+    }
+    __device__ __forceinline__ void write(void *row, int col, int left, bool whole, Unit &u, const Unit &w, float factor) const
+    {
 #pragma unroll
         for (int j = 0; j < kUnit; ++j) u.v[j] *= factor;
         if (gain) {
-            const Unit w = load_gain(gain, gain_bf16, col, left, whole);
 #pragma unroll
             for (int j = 0; j < kUnit; ++j) u.v[j] *= w.v[j];
         }
-        if (out_bf16) store_unit(static_cast<__nv_bfloat16 *>(out) + place * stride + col, u, left, whole);
-        else store_unit(static_cast<float *>(out) + place * stride + col, u, left, whole);
+        if (out_bf16) store_unit(static_cast<__nv_bfloat16 *>(row) + col, u, left, whole);
+        else store_unit(static_cast<float *>(row) + col, u, left, whole);
+    }
+    // A row's unit of sums, to where it belongs.
+    __device__ __forceinline__ void store(int row, int col, Unit &u) const
+    {
+        const int left = cols - col;
+        if (left <= 0) return;
+        if (add) add_sum(row, col, u);
+        if (!out) {
+            store_unit(sum + static_cast<long long>(row) * sum_stride + col, u, kUnit, true);
+            return;
+        }
+        const bool whole = vectors && left >= kUnit;
+        Unit w;
+        if (gain) w = load_gain(gain, gain_bf16, col, left, whole);
+        write(static_cast<unsigned char *>(out) + static_cast<long long>(order ? order[row] : row) * stride * (out_bf16 ? 2 : 4), col, left, whole, u, w, factor());
     }
 };
 struct StoreEpilogue {
     static constexpr int kChunk = 1 << 30;
     StoreTarget target;
 
-    int row0, place;                      // the warp's first row; where this lane's row goes, -1: nowhere
+    // This lane stores eight columns of four rows (8 j + lane / 4) of every 32 x 32 sums: their places (null: none), found once a tile.
+    int row0;
     float factor;
     float *part;
+    unsigned char *to[4];
     __device__ __forceinline__ void begin(int r, int p)
     {
-        row0 = r - static_cast<int>(threadIdx.x & 31);
-        place = r >= target.count() ? -1 : target.order ? target.order[r] : r;
+        const int lane = threadIdx.x & 31, count = target.count();
+        row0 = r - lane;
         factor = target.factor();
         part = p >= 0 ? target.parts + (static_cast<long long>(p) * kTile + row0 % kTile) * kTile : nullptr;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = row0 + 8 * j + (lane >> 2);
+            to[j] = nullptr;
+            if (row >= count) continue;
+            if (target.out) to[j] = static_cast<unsigned char *>(target.out) + static_cast<long long>(target.order ? target.order[row] : row) * target.stride * (target.out_bf16 ? 2 : 4);
+            else to[j] = reinterpret_cast<unsigned char *>(target.sum + static_cast<long long>(row) * target.sum_stride);
+        }
     }
     __device__ __forceinline__ void take(float (&x)[32], int col, unsigned desk)
     {
         if (col >= target.cols) return;
-        const int lane = threadIdx.x & 31, unit = lane & 3;
+        const int lane = threadIdx.x & 31, unit = lane & 3, at = col + kUnit * unit, left = target.cols - at;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             desk_put(desk + wide_place(lane, k), make_uint4(__float_as_uint(x[4 * k]), __float_as_uint(x[4 * k + 1]), __float_as_uint(x[4 * k + 2]), __float_as_uint(x[4 * k + 3])));
+        const bool whole = target.vectors && left >= kUnit;
+        Unit gain;
+        if (target.gain && left > 0) gain = load_gain(target.gain, target.gain_bf16, at, left, whole);
         __syncwarp();
+        uint4 v[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int r = j * 8 + (lane >> 2), to = __shfl_sync(kAllLanes, place, r);
-            const uint4 a = desk_get(desk + wide_place(r, 2 * unit)), b = desk_get(desk + wide_place(r, 2 * unit + 1));
-            if (to < 0) continue;
-            if (part) {
-                uint4 *p = reinterpret_cast<uint4 *>(part + r * kTile + col % kTile + 8 * unit);
-                p[0] = a;
-                p[1] = b;
-                continue;
-            }
-            Unit u{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w), __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z),
-                    __uint_as_float(b.w)}};
-            target.store(row0 + r, to, col + 8 * unit, u, factor);
+            v[2 * j] = desk_get(desk + wide_place(j * 8 + (lane >> 2), 2 * unit));
+            v[2 * j + 1] = desk_get(desk + wide_place(j * 8 + (lane >> 2), 2 * unit + 1));
         }
         __syncwarp();
+        if (left <= 0) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (!to[j]) continue;
+            if (part) {
+                uint4 *p = reinterpret_cast<uint4 *>(part + (j * 8 + (lane >> 2)) * kTile + at % kTile);
+                p[0] = v[2 * j];
+                p[1] = v[2 * j + 1];
+                continue;
+            }
+            Unit u{{__uint_as_float(v[2 * j].x), __uint_as_float(v[2 * j].y), __uint_as_float(v[2 * j].z), __uint_as_float(v[2 * j].w), __uint_as_float(v[2 * j + 1].x),
+                    __uint_as_float(v[2 * j + 1].y), __uint_as_float(v[2 * j + 1].z), __uint_as_float(v[2 * j + 1].w)}};
+            if (target.add) target.add_sum(row0 + j * 8 + (lane >> 2), at, u);
+            if (target.out) target.write(to[j], at, left, whole, u, gain, factor);
+            else store_unit(reinterpret_cast<float *>(to[j]) + at, u, kUnit, true);
+        }
     }
 };
 
@@ -494,7 +529,6 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const __grid_constant__ 
     int share = 1;                        // warps of a row
     while (share < 8 && share < walk.splits) share *= 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, of = warp & (share - 1), rows = 8 / share, count = target.count();
-    const float factor = target.factor();
     for (int first = block * rows; first < (walk.count - walk.whole) / walk.splits * kTile; first += blocks * rows) {          // rows of split tiles
         const int rest = first / kTile, r = first % kTile + warp / share;
         int m, n;
@@ -520,7 +554,7 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const __grid_constant__ 
 #pragma unroll
                 for (int k = 0; k < kUnit; ++k) u.v[k] += sums[warp + w][lane][k];
             }
-            target.store(row, target.order ? target.order[row] : row, col, u, factor);
+            target.store(row, col, u);
         }
         __syncthreads();                  // sums are written again
     }

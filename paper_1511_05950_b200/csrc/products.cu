@@ -85,6 +85,10 @@ template <typename L, typename Epilogue>
 bool job_of(softsync::MmaJob<Epilogue> &job, const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue)
 {
     job.plan = plan;
+    if (plan.slots && !plan.live) {
+        const int64_t rest = div_up(plan.m, kTile) * div_up(plan.n, kTile) % plan.slots;
+        job.plan.splits = rest ? softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots) : 1;
+    }
     job.epilogue = epilogue;
     return encode(job.a, a, L::mn_a ? kStep : kHalf) && encode(job.b, b, L::mn_b ? kStep : kHalf);
 }
@@ -96,7 +100,7 @@ int64_t items_of(const MmaPlan &plan)
     if (!plan.slots) return tiles;
     if (plan.live) return std::max<int64_t>(tiles, plan.slots);
     const int rest = static_cast<int>(tiles % plan.slots);
-    return rest ? tiles + int64_t{rest} * (softsync::split_count(rest, static_cast<int>(div_up(plan.k, kStep)), plan.slots) - 1) : tiles;
+    return tiles + int64_t{rest} * (plan.splits - 1);
 }
 
 // One product, or two whose operands are both there: one launch's fixed time (10 us) for both.
@@ -132,8 +136,7 @@ int launch_split_sums(const softsync::MmaJob<softsync::StoreEpilogue> *jobs, int
         const MmaPlan &plan = in.plan[k] = jobs[k].plan;
         in.target[k] = jobs[k].epilogue.target;
         const int64_t tiles = div_up(plan.m, kTile) * div_up(plan.n, kTile), rest = plan.live && !plan.live_is_k ? std::min<int64_t>(tiles, plan.slots - 1) : tiles % plan.slots;
-        const int splits = plan.live || !rest ? 2 : softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots);
-        if (splits > 1) blocks[k] = std::min<int64_t>(rest * kTile / 2, 32 * plan.slots);         // rows in turn: 2 to 8 warps each
+        if (plan.live || plan.splits > 1) blocks[k] = std::min<int64_t>(rest * kTile / 2, 32 * plan.slots);         // rows in turn: 2 to 8 warps each
     }
     in.blocks = static_cast<int>(blocks[0]);
     return blocks[0] + blocks[1] ? start(softsync::split_sum_kernel, blocks[0] + blocks[1], 256, 0, true, st, in) : PS_OK;
@@ -298,7 +301,7 @@ struct HeadCall {
                 status = start(softsync::kept_grad_kernel, w.rows_padded * in.segments, softsync::kKeptThreads, 0, dependent(), st, in);
             } else {
                 softsync::GradEpilogue ge{};
-                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.live = live(); ge.scale = scale;
+                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live(); ge.scale = scale;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
                 const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(rows, width)};
                 softsync::MmaJob<softsync::GradEpilogue> job;

@@ -115,14 +115,46 @@ def test_cross_entropy_and_gradients(rows, width, vocab):
 
 @gpu
 def test_pieces_of_the_vocabulary():
-    """More rows and entries than one piece of G holds: three pieces, the last one short and of an odd width."""
-    hidden, head, tokens, weights = make(8192, 64, 33001, seed=5, masked=0.1)
-    ref = Reference(hidden, head, tokens)
+    """More rows and entries than one piece of G holds (1 GiB): the kept one and two that are computed again, of an odd width in all."""
+    rows, vocab = 20001, 60001
+    hidden, head, tokens, weights = make(rows, 64, vocab, seed=5, masked=0.1)
     r = P.head_cross_entropy(hidden, head, tokens, weights=weights)
-    keep = weights != 0
-    assert close(r.logp, ref.logp * keep, ref.tol)
-    dhidden, tol_h, dhead, tol_w = ref.gradients(weights.double() / weights.double().sum())
-    assert close(r.dhidden, dhidden, tol_h) and close(r.dhead, dhead, tol_w)
+    a = weights.double() / weights.double().sum()
+    dhead, tol_w = torch.zeros(vocab, 64, dtype=torch.float64, device="cuda"), torch.zeros(vocab, 64, dtype=torch.float64, device="cuda")
+    for first in range(0, rows, 5000):                                 # the reference by rows: their gradients of the head add up
+        part = slice(first, first + 5000)
+        ref = Reference(hidden[part], head, tokens[part])
+        keep = weights[part] != 0
+        assert close(r.logp[part], ref.logp * keep, ref.tol)
+        dhidden, tol_h, more, tol = ref.gradients(a[part])
+        assert close(r.dhidden[part], dhidden, tol_h)
+        dhead += more
+        tol_w += tol
+    assert close(r.dhead, dhead, tol_w + (rows / 16) * 2.0 ** -23 * (a[:, None] * hidden.double().abs()).sum(0))
+    again = P.head_logprob_grad(hidden, head, tokens, r.lse, -a.float())
+    assert float((again.dhidden.double() - r.dhidden.double()).norm()) <= 2 * HALF * float(r.dhidden.double().norm())
+    assert float((again.dhead.double() - r.dhead.double()).norm()) <= 2 * HALF * float(r.dhead.double().norm())
+
+
+@gpu
+def test_a_head_of_more_than_two_to_the_31_values():
+    rows, width, vocab = 5, 4096, 530001
+    hidden, _, _, _ = make(rows, width, 2, seed=6)
+    g = torch.Generator("cuda").manual_seed(7)
+    head = torch.empty(vocab, width, dtype=BF16, device="cuda").normal_(generator=g).mul_(2.0 / math.sqrt(width))
+    tokens = torch.tensor([0, vocab - 1, 5, 524290, vocab - 1], device="cuda")
+    r = P.head_cross_entropy(hidden, head, tokens)
+    z = torch.cat([hidden.double() @ part.double().T for part in head.split(65536)], 1)
+    lse = torch.logsumexp(z, 1)
+    logp = z[torch.arange(rows), tokens] - lse
+    tol = 2 * products(float(hidden.double().norm(dim=1).max()), float(head[:1000].float().norm(dim=1).max()) * 1.2, width) + EPS * (300 + vocab / 128)
+    assert close(r.logp, logp, tol)
+    for last in (slice(vocab - 300, vocab), slice(524200, 524400), slice(0, 10)):
+        p = torch.exp(z[:, last] - lse[:, None])
+        one = (tokens[:, None] == torch.arange(last.start, last.stop, device="cuda")).double()
+        want = (p - one).T @ hidden.double() / rows
+        size = ((p - one).abs() + p).T @ hidden.double().abs() / rows
+        assert close(r.dhead[last], want, (HALF + 2.0 ** -11 + 4 * tol) * size + HALF * want.abs() + 1e-30)
 
 
 @gpu
@@ -194,6 +226,18 @@ def test_a_bad_row_spoils_itself_and_the_sums(kind):
     assert torch.equal(r.logp[others], want.logp[others]) and torch.equal(r.dhidden[others], want.dhidden[others])
     assert bool(r.logp[77].isnan()) and bool(r.lse[77].isnan()) and bool(r.dhidden[77].isnan().all())
     assert bool(r.stats[0].isnan()) and bool(r.dhead.isnan().any())
+
+
+@gpu
+def test_a_bad_token_in_the_gradient():
+    hidden, head, tokens, weights = make(70, 64, 300, seed=14, masked=0.0)
+    lse = P.head_logprob(hidden, head, tokens).lse
+    tokens[3] = 300
+    g = P.head_logprob_grad(hidden, head, tokens, lse, -weights)
+    assert bool(g.dhidden[3].isnan().all()) and bool(g.dhead.isnan().any()) and int(g.dhidden.isnan().any(1).sum()) == 1
+    weights[3] = 0.0                                                   # and now it takes no part
+    g = P.head_logprob_grad(hidden, head, tokens, lse, -weights)
+    assert bool(g.dhidden.isfinite().all()) and bool(g.dhead.isfinite().all()) and bool((g.dhidden[3] == 0).all())
 
 
 @gpu

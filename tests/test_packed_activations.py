@@ -101,6 +101,23 @@ def test_nothing_is_written_beside_the_rows():
     assert P.pack8(x[:0]).codes.shape == (0, 64) and P.unpack8(P.pack8(x[:0])).shape == (0, 40)
 
 
+@gpu
+def test_more_than_two_to_the_32_values():
+    rows, cols = 70001, 65600
+    g = torch.Generator("cuda").manual_seed(2)
+    x = torch.empty(rows, cols, dtype=BF16, device="cuda").normal_(generator=g)
+    packed = P.pack8(x)
+    back = P.unpack8(packed)
+    for part in (slice(0, 2), slice(rows // 2, rows // 2 + 2), slice(rows - 2, rows)):
+        one = P.Packed8(packed.codes[part], packed.scales[part], cols)
+        assert same_codes(one, x[part]) and torch.equal(back[part], P.unpack8(P.pack8(x[part].clone())))
+    r = P.rms_norm(x, pack=True)
+    want = P.rms_norm(x[-2:].clone(), pack=True)
+    assert torch.equal(r.out[-2:], want.out) and torch.equal(r.packed.codes[-2:], want.packed.codes)
+    dx = P.rms_norm_grad(x, r.packed, r.rstd).dx
+    assert torch.equal(dx[-2:], P.rms_norm_grad(x[-2:].clone(), want.packed, want.rstd).dx)
+
+
 # ---- norm -----------------------------------------------------------------------------------------------------------------
 
 SHAPES = [  # rows, cols, pad, shift
@@ -316,6 +333,10 @@ def test_norm_linear_parts_of_the_gradient():
     assert torch.equal(w.grad, P.packed_weight_grad(torch.ones_like(z), kept, gain)) and bool(a.grad.isfinite().all())
     with torch.no_grad():
         assert not P.norm_linear(a, gain, weight)[0].requires_grad
+    none, w = x[:0].clone().requires_grad_(True), weight.clone().requires_grad_(True)
+    z, total = P.norm_linear(none, gain, w)
+    (z.sum() + total.sum()).backward()
+    assert z.shape == (0, 32) and none.grad.shape == (0, 64) and bool((w.grad == 0).all())
 
 
 @gpu
@@ -369,6 +390,29 @@ def test_a_step_of_all_of_them():
     server.push(0, [x.contiguous() for x in grads], server.pull())
     server.apply_update()
     assert all(bool(a.isfinite().all()) and not torch.equal(a, b) for a, b in zip(params, masters))
+
+
+@gpu
+def test_two_streams_at_once():
+    g = torch.Generator().manual_seed(22)
+    sets = [(rows_of(g, 500, 1000, BF16), rows_of(g, 500, 300, BF16)) for _ in range(2)]
+    gain = torch.ones(1000, device="cuda")
+
+    def run(x, dz):
+        fwd = P.rms_norm(x, gain, x, pack=True)
+        back = P.rms_norm_grad(x, fwd.packed, fwd.rstd, gain, x)
+        return (*fwd.packed[:2], fwd.out, fwd.total, *back, P.packed_weight_grad(dz, fwd.packed, gain))
+
+    want = [run(*s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(run(*sets[k]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for k in range(2) for r in got[k] for a, b in zip(r, want[k]))
 
 
 @gpu
