@@ -73,7 +73,9 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
 }
 
 // Rows of a matrix one behind the other in 16-byte vectors, padded with zeros: all of them, or the listed ones, and zero rows up to a whole stage of
-// a product's contraction.  A block a row; `zeros`: where a row without a place is set to zero.
+// a product's contraction.  `zeros`: where a row without a place is set to zero.  A warp takes 256 columns of a row; where rows allow no vectors, its lanes
+// read neighbouring values.
+constexpr int kGatherThreads = 256, kGatherColumns = 32 * kUnit;
 struct GatherIn {
     const __nv_bfloat16 *x;
     int rows, width;
@@ -84,22 +86,31 @@ struct GatherIn {
     int out_stride;
     __nv_bfloat16 *zeros;                  // may be null; dense rows
 };
-__global__ void __launch_bounds__(128) gather_kernel(const __grid_constant__ GatherIn in)
+__global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ GatherIn in)
 {
+    __shared__ WarpDesk<__nv_bfloat16> desks[kGatherThreads / 32];
     wait_for_earlier();
     let_next_start();
-    const int row = blockIdx.x, count = in.live ? *in.live : in.rows;
-    if (in.zeros && row < in.rows && in.place[row] < 0)
-        for (int col = threadIdx.x * kUnit; col < in.width; col += 128 * kUnit)
-            store_unit(in.zeros + static_cast<long long>(row) * in.width + col, Unit{}, in.width - col, in.width % kUnit == 0);
-    if (row >= (count + kStep - 1) / kStep * kStep) return;
+    const int chunks = (in.out_stride + kGatherColumns - 1) / kGatherColumns, lane = threadIdx.x & 31;
+    const long long item = static_cast<long long>(blockIdx.x) * (kGatherThreads / 32) + (threadIdx.x >> 5);
+    const int row = static_cast<int>(item / chunks), first = static_cast<int>(item - static_cast<long long>(row) * chunks) * kGatherColumns, col = first + lane * kUnit;
+    const int count = in.live ? *in.live : in.rows;
+    if (in.zeros && row < in.rows && in.place[row] < 0 && col < in.width)
+        store_unit(in.zeros + static_cast<long long>(row) * in.width + col, Unit{}, in.width - col, in.width % kUnit == 0);
+    if (row >= (count + kStep - 1) / kStep * kStep) return;          // a whole warp
+    const int width = row < count ? in.width : 0;
     const __nv_bfloat16 *from = in.x + (row < count ? (in.order ? in.order[row] : row) * in.stride : 0);
-    for (int col = threadIdx.x * kUnit; col < in.out_stride; col += 128 * kUnit) {
-        const int left = row < count ? in.width - col : 0;
-        RawUnit<__nv_bfloat16> raw;
-        load_unit(raw, from + (left > 0 ? col : 0), left, in.aligned && left >= kUnit);
-        *reinterpret_cast<uint4 *>(in.out + static_cast<long long>(row) * in.out_stride + col) = raw.a;
+    RawUnit<__nv_bfloat16> raw;
+    if (in.aligned) {
+        load_unit(raw, from + (col < width ? col : 0), width - col, width - col >= kUnit);
+    } else {
+        __nv_bfloat16 *v = desks[threadIdx.x >> 5].v;
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) v[k * 32 + lane] = first + k * 32 + lane < width ? from[first + k * 32 + lane] : __nv_bfloat16(0.f);
+        __syncwarp();
+        raw.a = *reinterpret_cast<const uint4 *>(v + lane * kUnit);
     }
+    if (col < in.out_stride) *reinterpret_cast<uint4 *>(in.out + static_cast<long long>(row) * in.out_stride + col) = raw.a;
 }
 
 // A row's parts joined: normaliser, lse, log probability; and, by the last block, the loss.  Eight rows a block, 64 threads share a row's parts (152000

@@ -444,8 +444,9 @@ struct StoreEpilogue {
     static constexpr int kChunk = 1 << 30;
     StoreTarget target;
 
-    // This lane stores eight columns of four rows (8 j + lane / 4) of every 32 x 32 sums: their places (null: none), found once a tile.
-    int row0;
+    // This lane stores eight columns of four rows (8 j + lane / 4) of every 32 x 32 sums: their places (null: none), found once a tile.  Where rows allow no vectors it
+    // stores one column of all rows, whose places the lanes hold (-1: none).
+    int row0, place;
     float factor;
     float *part;
     unsigned char *to[4];
@@ -455,6 +456,8 @@ struct StoreEpilogue {
         row0 = r - lane;
         factor = target.factor();
         part = p >= 0 ? target.parts + (static_cast<long long>(p) * kTile + row0 % kTile) * kTile : nullptr;
+        place = -1;
+        if (r < count) place = target.order ? target.order[r] : r;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int row = row0 + 8 * j + (lane >> 2);
@@ -471,6 +474,30 @@ struct StoreEpilogue {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             desk_put(desk + wide_place(lane, k), make_uint4(__float_as_uint(x[4 * k]), __float_as_uint(x[4 * k + 1]), __float_as_uint(x[4 * k + 2]), __float_as_uint(x[4 * k + 3])));
+        if (target.out && !target.vectors && !part) {
+            const int c = col + lane;
+            float w = factor;
+            if (target.gain && c < target.cols) w *= target.gain_bf16 ? unit_value(static_cast<const __nv_bfloat16 *>(target.gain) + c) : static_cast<const float *>(target.gain)[c];
+            __syncwarp();
+#pragma unroll 1
+            for (int row = 0; row < 32; row += 8) {        // eight rows' values under way at once
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[k]) : "r"(desk + wide_place(row + k, lane >> 2) + 4 * (lane & 3)) : "memory");
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int at_row = __shfl_sync(kAllLanes, place, row + k);
+                    if (at_row < 0 || c >= target.cols) continue;
+                    if (target.add) v[k] += target.sum[static_cast<long long>(row0 + row + k) * target.sum_stride + c];
+                    const long long to_value = at_row * target.stride + c;
+                    if (target.out_bf16) static_cast<__nv_bfloat16 *>(target.out)[to_value] = __float2bfloat16_rn(v[k] * w);
+                    else static_cast<float *>(target.out)[to_value] = v[k] * w;
+                }
+            }
+            __syncwarp();
+            return;
+        }
         const bool whole = target.vectors && left >= kUnit;
         Unit gain;
         if (target.gain && left > 0) gain = load_gain(target.gain, target.gain_bf16, at, left, whole);

@@ -149,6 +149,8 @@ int group_of(int64_t m, int64_t k)
     return static_cast<int>(std::max<int64_t>(1, std::min(div_up(m, kTile), (int64_t{32} << 20) / (2 * kTile * std::max<int64_t>(k, 1)))));
 }
 
+int64_t gather_blocks(int64_t rows, int64_t stride) { return div_up(rows * div_up(stride, softsync::kGatherColumns), softsync::kGatherThreads / 32); }
+
 // ---- workspaces --------------------------------------------------------------------------------------------------------
 struct Places {
     int64_t bytes = 0;
@@ -252,13 +254,13 @@ struct HeadCall {
         in.width = static_cast<int>(h.width); in.out_stride = static_cast<int>(w.width_padded);
         if (status == PS_OK && w.copy_head) {
             in.x = static_cast<const bf16 *>(h.head_dev); in.rows = static_cast<int>(h.vocab); in.stride = h.head_stride; in.out = w.head;
-            status = start(softsync::gather_kernel, round_up(h.vocab, kStep), 128, 0, dependent(), st, in);
+            status = start(softsync::gather_kernel, gather_blocks(round_up(h.vocab, kStep), w.width_padded), softsync::kGatherThreads, 0, dependent(), st, in);
         }
         if (status == PS_OK && w.copy_hidden) {
             in.x = static_cast<const bf16 *>(h.hidden_dev); in.rows = static_cast<int>(h.rows); in.stride = h.hidden_stride; in.out = w.hidden;
             in.aligned = matrix_aligned(h.hidden_dev, h.rows, h.hidden_stride);
             if (listed) { in.order = w.order; in.place = w.place; in.live = w.live; in.zeros = static_cast<bf16 *>(dhidden); }
-            status = start(softsync::gather_kernel, w.rows_padded, 128, 0, dependent(), st, in);
+            status = start(softsync::gather_kernel, gather_blocks(w.rows_padded, w.width_padded), softsync::kGatherThreads, 0, dependent(), st, in);
         }
         return status;
     }
@@ -457,7 +459,7 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     if (w.copy_dout) {
         softsync::GatherIn in{};
         in.x = dout.data; in.rows = rows; in.width = outs; in.stride = a->dout_stride; in.out = w.dout; in.out_stride = static_cast<int>(w.outs_padded);
-        status = start(softsync::gather_kernel, round_up(rows, kStep), 128, 0, false, st, in);
+        status = start(softsync::gather_kernel, gather_blocks(round_up(rows, kStep), w.outs_padded), softsync::kGatherThreads, 0, false, st, in);
         dout = Matrix{w.dout, rows, outs, w.outs_padded};
     }
     if (status != PS_OK) return status;

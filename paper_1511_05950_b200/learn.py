@@ -413,6 +413,8 @@ def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, resid
         raise ValueError("x has width %d, weight shape %s" % (x.shape[-1], tuple(weight.shape)))
     if residual is not None and residual.shape != x.shape:
         raise ValueError("residual has shape %s, x %s" % (tuple(residual.shape), tuple(x.shape)))
+    if x.dim() == 2:
+        return _NormLinear.apply(x, gain, weight, residual, eps)
     rows = x.reshape(-1, x.shape[-1])
     z, total = _NormLinear.apply(rows, gain, weight, None if residual is None else residual.reshape(rows.shape), eps)
     return z.view(*x.shape[:-1], weight.shape[0]), total.view(x.shape)
