@@ -55,7 +55,7 @@ __device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, in
     if (in.out) {
         Unit y;
 #pragma unroll
-        for (int k = 0; k < kUnit; ++k) y.v[k] = n.v[k] * gain.v[k];
+        for (int k = 0; k < kUnitPairs; ++k) y.set(k, mul2(n.pair(k), gain.pair(k)));
         store_row<ALIGNED>(static_cast<T *>(in.out) + row * in.cols, unit, in.cols, y, desk);
     }
 }
@@ -95,17 +95,17 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
             if (in.residual) {
                 const Unit r = b[j].values();
 #pragma unroll
-                for (int k = 0; k < kUnit; ++k) u[j].v[k] = rounded<T>(u[j].v[k] + r.v[k]);
+                for (int k = 0; k < kUnitPairs; ++k) u[j].set(k, rounded<T>(add2(u[j].pair(k), r.pair(k))));
             }
         } else {
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) u[j].v[k] = 0.f;
         }
         if (in.total) store_row<ALIGNED>(static_cast<T *>(in.total) + row * in.total_stride, j * T_ROW + tid, in.cols, u[j], desk);
-        float s = 0.f;
+        float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < kUnit; ++k) s = fmaf(u[j].v[k], u[j].v[k], s);
-        sum += s;
+        for (int k = 0; k < kUnitPairs; ++k) s = fma2(u[j].pair(k), u[j].pair(k), s);
+        sum += s.x + s.y;
     }
     sum = row_sum<WARPS>(sum, part, 0);
     const float r = __frsqrt_rn(sum / static_cast<float>(in.cols) + in.eps);
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
         const int unit = j * T_ROW + tid, left = in.cols - unit * kUnit;
         if (j * T_ROW * kUnit >= in.cols) break;           // the same for the whole row
 #pragma unroll
-        for (int k = 0; k < kUnit; ++k) u[j].v[k] *= r;
+        for (int k = 0; k < kUnitPairs; ++k) u[j].set(k, mul2(u[j].pair(k), make_float2(r, r)));
         Unit gain{};
         if (in.out && left > 0) gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, ALIGNED && left >= kUnit);
         norm_outputs<T, ALIGNED>(in, row, unit, u[j], gain, desk);
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(const __gri
             load_unit(b, res + col, left, whole);
             const Unit r = b.values();
 #pragma unroll
-            for (int k = 0; k < kUnit; ++k) u.v[k] = rounded<T>(u.v[k] + r.v[k]);
+            for (int k = 0; k < kUnitPairs; ++k) u.set(k, rounded<T>(add2(u.pair(k), r.pair(k))));
         }
         return u;
     };
@@ -279,14 +279,14 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
             n[j] = next.kept[j].values(r);
             more[j] = next.dtotal[j];
             const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, ALIGNED && left >= kUnit);
-            float s = 0.f;
+            float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < kUnit; ++k) {
-                acc[j].v[k] = fmaf(g[j].v[k], n[j].v[k], acc[j].v[k]);
-                g[j].v[k] *= gain.v[k];
-                s = fmaf(g[j].v[k], n[j].v[k], s);
+            for (int k = 0; k < kUnitPairs; ++k) {
+                acc[j].set(k, fma2(g[j].pair(k), n[j].pair(k), acc[j].pair(k)));
+                if (in.gain) g[j].set(k, mul2(g[j].pair(k), gain.pair(k)));
+                s = fma2(g[j].pair(k), n[j].pair(k), s);
             }
-            sum += s;
+            sum += s.x + s.y;
         }
         if (row + step < in.rows) next.load(in, row + step, tid);
         const float mean = row_sum<WARPS>(sum, part, slot) / static_cast<float>(in.cols);
@@ -297,11 +297,11 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
             Unit dx{};
             if (ALIGNED || unit * kUnit < in.cols) {
 #pragma unroll
-                for (int k = 0; k < kUnit; ++k) dx.v[k] = r * fmaf(-n[j].v[k], mean, g[j].v[k]);
+                for (int k = 0; k < kUnitPairs; ++k) dx.set(k, mul2(fma2(n[j].pair(k), make_float2(-mean, -mean), g[j].pair(k)), make_float2(r, r)));
                 if (in.dtotal) {
                     const Unit m = more[j].values();
 #pragma unroll
-                    for (int k = 0; k < kUnit; ++k) dx.v[k] += m.v[k];
+                    for (int k = 0; k < kUnitPairs; ++k) dx.set(k, add2(dx.pair(k), m.pair(k)));
                 }
             }
             store_row<ALIGNED>(static_cast<T *>(in.dx) + row * in.cols, unit, in.cols, dx, desk);

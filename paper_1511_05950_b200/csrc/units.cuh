@@ -2,6 +2,8 @@
 // lanes hold the 32 columns that share a scale.  A unit whose address or length does not allow vectors is taken element by element.
 #pragma once
 
+#include "packed.cuh"
+
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -18,7 +20,12 @@ __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontro
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- eight elements ----------------------------------------------------------------------------------------------------
-struct Unit { float v[kUnit]; };
+struct alignas(16) Unit {
+    float v[kUnit];
+    __device__ __forceinline__ float2 pair(int k) const { return make_float2(v[2 * k], v[2 * k + 1]); }
+    __device__ __forceinline__ void set(int k, float2 x) { v[2 * k] = x.x; v[2 * k + 1] = x.y; }
+};
+constexpr int kUnitPairs = kUnit / 2;
 
 __device__ __forceinline__ float unit_value(const float *p) { return *p; }
 __device__ __forceinline__ float unit_value(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
@@ -124,9 +131,13 @@ __device__ __forceinline__ void store_row(T *row, int unit, int cols, const Unit
         __syncwarp();
     }
 }
-template <typename T> __device__ __forceinline__ float rounded(float x);
-template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
-template <> __device__ __forceinline__ float rounded<__nv_bfloat16>(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
+template <typename T> __device__ __forceinline__ float2 rounded(float2 x);
+template <> __device__ __forceinline__ float2 rounded<float>(float2 x) { return x; }
+template <> __device__ __forceinline__ float2 rounded<__nv_bfloat16>(float2 x)
+{
+    const unsigned w = bf16_pair(x.x, x.y);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
 
 // ---- 8 bits with a scale -----------------------------------------------------------------------------------------------
 // The byte s of a block stands for the unit 2^(s - 127) = 2^(floor(log2 max|x|) - 6), at least 2^-126; 255 for a block with an infinity or a
@@ -155,26 +166,36 @@ __device__ __forceinline__ uint2 pack_unit(const Unit &u, unsigned &scale)
     m = max(m, __shfl_xor_sync(kAllLanes, m, 1));
     m = max(m, __shfl_xor_sync(kAllLanes, m, 2));
     scale = block_scale(m);
-    // x / unit + 1.5 * 2^23 rounds to nearest, ties to even (the product is exact: the sum is rounded once): |x| / unit is below 128, so the code is in the low byte
+    // x / unit + 1.5 * 2^23 rounds to nearest, ties to even (the product is exact: the sum is rounded once): |x| / unit is below 128, so the code is in the low byte.
+    // Only a block whose largest is 127.5 units or more has codes to cut: its mantissa tells.
     constexpr float middle = 12582912.f;
     const float inv = __uint_as_float((254u - scale) << 23);
-    unsigned b[kUnit];
+    Unit b;
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) b[k] = __float_as_uint(fminf(fmaxf(fmaf(u.v[k], inv, middle), middle - 127.f), middle + 127.f));
+    for (int k = 0; k < kUnitPairs; ++k) b.set(k, fma2(u.pair(k), make_float2(inv, inv), make_float2(middle, middle)));
+    if ((m & 0x7fffffu) >= 0x7f0000u) {
+        if (scale == 255u) return make_uint2(0, 0);
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) b.v[k] = fminf(fmaxf(b.v[k], middle - 127.f), middle + 127.f);
+    }
     if (scale == 255u) return make_uint2(0, 0);
-    return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
-                      __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+    const auto bytes = [&](int k) {
+        return __byte_perm(__byte_perm(__float_as_uint(b.v[k]), __float_as_uint(b.v[k + 1]), 0x0040), __byte_perm(__float_as_uint(b.v[k + 2]), __float_as_uint(b.v[k + 3]), 0x0040), 0x5410);
+    };
+    return make_uint2(bytes(0), bytes(4));
 }
 
-// The values of eight codes: exact (a code has 7 bits and the unit is a power of two).
+// The values of eight codes: exact (a code has 7 bits and the unit is a power of two).  With b = code + 128 in the low byte of the float 2^23 + b, minus 2^23 + 128,
+// times the unit: two codes an instruction, and none of the slow conversions.
 __device__ __forceinline__ Unit unpack_unit(uint2 codes, unsigned scale)
 {
     const float unit = scale_unit(scale);
+    const unsigned w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
     Unit u;
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) {
-        const unsigned w = k < 4 ? codes.x : codes.y;
-        u.v[k] = static_cast<float>(static_cast<int>(w << (24 - 8 * (k & 3))) >> 24) * unit;
+    for (int k = 0; k < kUnitPairs; ++k) {
+        const unsigned b = w[k / 2], lo = __byte_perm(b, 0x4b000000u, 0x7440 + 2 * (k & 1)), hi = __byte_perm(b, 0x4b000000u, 0x7441 + 2 * (k & 1));
+        u.set(k, mul2(add2(make_float2(__uint_as_float(lo), __uint_as_float(hi)), make_float2(-8388736.f, -8388736.f)), make_float2(unit, unit)));
     }
     return u;
 }
