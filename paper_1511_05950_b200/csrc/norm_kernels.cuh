@@ -279,14 +279,14 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
             n[j] = next.kept[j].values(r);
             more[j] = next.dtotal[j];
             const Unit gain = load_gain(in.gain, in.gain_bf16, unit * kUnit, left, ALIGNED && left >= kUnit);
-            float2 s = make_float2(0.f, 0.f);
+            float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < kUnitPairs; ++k) {
-                acc[j].set(k, fma2(g[j].pair(k), n[j].pair(k), acc[j].pair(k)));
-                if (in.gain) g[j].set(k, mul2(g[j].pair(k), gain.pair(k)));
-                s = fma2(g[j].pair(k), n[j].pair(k), s);
+            for (int k = 0; k < kUnit; ++k) {
+                acc[j].v[k] = fmaf(g[j].v[k], n[j].v[k], acc[j].v[k]);
+                g[j].v[k] *= gain.v[k];
+                s = fmaf(g[j].v[k], n[j].v[k], s);
             }
-            sum += s.x + s.y;
+            sum += s;
         }
         if (row + step < in.rows) next.load(in, row + step, tid);
         const float mean = row_sum<WARPS>(sum, part, slot) / static_cast<float>(in.cols);
@@ -297,11 +297,11 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
             Unit dx{};
             if (ALIGNED || unit * kUnit < in.cols) {
 #pragma unroll
-                for (int k = 0; k < kUnitPairs; ++k) dx.set(k, mul2(fma2(n[j].pair(k), make_float2(-mean, -mean), g[j].pair(k)), make_float2(r, r)));
+                for (int k = 0; k < kUnit; ++k) dx.v[k] = r * fmaf(-n[j].v[k], mean, g[j].v[k]);
                 if (in.dtotal) {
                     const Unit m = more[j].values();
 #pragma unroll
-                    for (int k = 0; k < kUnitPairs; ++k) dx.set(k, add2(dx.pair(k), m.pair(k)));
+                    for (int k = 0; k < kUnit; ++k) dx.v[k] += m.v[k];
                 }
             }
             store_row<ALIGNED>(static_cast<T *>(in.dx) + row * in.cols, unit, in.cols, dx, desk);
