@@ -5,6 +5,7 @@
 #include "pack_kernels.cuh"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -85,16 +86,49 @@ GradShape grad_shape(int64_t rows, int64_t cols)
     if (units <= 32) return of(1, one);
     if (units <= 64) return of(1, two);
     if (units <= 128) return of(4, one);
-    if (units <= 256) return of(8, one);
-    if (units <= 512) return of(16, one);
+    if (units <= 256) return of(4, two);
+    if (units <= 512) return of(8, two);
     if (units <= 1024) return of(16, two);
     return GradShape{0, 0, rows, std::min(rows, kLongParts)};
 }
 GradShape grad_shape(int dtype, int64_t rows, int64_t cols) { return dtype == PS_GRAD_BF16 ? grad_shape<bf16>(rows, cols) : grad_shape<float>(rows, cols); }
 
+constexpr int kNoRoom = 1;
+// The kernel with a ring, where the blocks of an SM have room for at least three rows each; else kNoRoom.
+template <typename T, int WARPS, int UNITS>
+int launch_ring(const NormGradIn &in, const GradShape &shape, cudaStream_t st)
+{
+    const auto kernel = softsync::rms_norm_grad_ring_kernel<T, WARPS, UNITS>;
+    constexpr int resident = softsync::kGradWarps<T, UNITS> / WARPS, room = (224 * 1024) / resident - 1536;          // an SM's shared memory, less what a block takes beside its ring
+    softsync::GradRing ring;
+    ring.row_bytes = in.cols * static_cast<int>(sizeof(T));
+    ring.code_bytes = static_cast<int>(div_up(in.cols, PS_PACK_BLOCK) * PS_PACK_BLOCK);
+    ring.slot_bytes = ring.row_bytes * (in.dtotal ? 2 : 1) + ring.code_bytes;
+    ring.slots = std::min(room / ring.slot_bytes, softsync::kMostSlots);
+    if (ring.slots < 3) return kNoRoom;
+    static std::atomic<bool> ready[64] = {};
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return PS_ERR_CUDA;
+    if (!ready[device].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room) != cudaSuccess) return PS_ERR_CUDA;
+        ready[device].store(true, std::memory_order_relaxed);
+    }
+    return softsync::launch(kernel, shape.blocks, 32 * WARPS, ring.slots * ring.slot_bytes, true, st, in, ring) ? PS_OK : PS_ERR_CUDA;
+}
+
 template <typename T, bool CODES, bool ALIGNED>
 int launch_norm_grad(const NormGradIn &in, const GradShape &shape, cudaStream_t st)
 {
+    if (CODES && ALIGNED && in.cols % softsync::kUnit == 0) {
+        int status = kNoRoom;
+        switch (shape.warps * 8 + shape.units) {
+        case 4 * 8 + 1: status = launch_ring<T, 4, 1>(in, shape, st); break;
+        case 4 * 8 + 2: status = launch_ring<T, 4, 2>(in, shape, st); break;
+        case 8 * 8 + 2: status = launch_ring<T, 8, 2>(in, shape, st); break;
+        case 16 * 8 + 2: status = launch_ring<T, 16, 2>(in, shape, st); break;
+        }
+        if (status != kNoRoom) return status;
+    }
     const auto go = [&](auto kernel) {
         return softsync::launch(kernel, shape.blocks, shape.warps == 1 ? 32 * softsync::kNormRows : 32 * shape.warps, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
     };
@@ -102,8 +136,8 @@ int launch_norm_grad(const NormGradIn &in, const GradShape &shape, cudaStream_t 
     case 1 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 1, 1, CODES, ALIGNED>);
     case 1 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 1, 2, CODES, ALIGNED>);
     case 4 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 4, 1, CODES, ALIGNED>);
-    case 8 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 8, 1, CODES, ALIGNED>);
-    case 16 * 8 + 1: return go(softsync::rms_norm_grad_kernel<T, 16, 1, CODES, ALIGNED>);
+    case 4 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 4, 2, CODES, ALIGNED>);
+    case 8 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 8, 2, CODES, ALIGNED>);
     case 16 * 8 + 2: return go(softsync::rms_norm_grad_kernel<T, 16, 2, CODES, ALIGNED>);
     }
     if (!softsync::launch(softsync::rms_norm_grad_long_kernel<T, CODES, ALIGNED>, in.rows, softsync::kLongThreads, 0, true, st, in)) return PS_ERR_CUDA;

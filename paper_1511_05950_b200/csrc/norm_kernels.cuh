@@ -20,8 +20,16 @@ __device__ __forceinline__ float row_sum(float x, float (*part)[32], int slot)
     if constexpr (WARPS > 1) {
         if ((threadIdx.x & 31) == 0) part[slot][threadIdx.x >> 5] = x;
         __syncthreads();
-        x = (threadIdx.x & 31) < WARPS ? part[slot][threadIdx.x & 31] : 0.f;
-        x = norm_warp_sum(x);
+        if constexpr (WARPS <= 8) {                        // a few broadcast loads, instead of another tree
+            const float4 *p = reinterpret_cast<const float4 *>(part[slot]);
+            float4 s = p[0];
+#pragma unroll
+            for (int k = 1; k < WARPS / 4; ++k) { const float4 t = p[k]; s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w; }
+            x = (s.x + s.y) + (s.z + s.w);
+        } else {
+            x = (threadIdx.x & 31) < WARPS ? part[slot][threadIdx.x & 31] : 0.f;
+            x = norm_warp_sum(x);
+        }
     }
     return x;
 }
@@ -67,7 +75,7 @@ constexpr int kNormRows = 4;
 template <typename T, int WARPS, int UNITS, bool ALIGNED>
 __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_norm_kernel(const __grid_constant__ NormIn in)
 {
-    __shared__ float part[2][32];
+    __shared__ __align__(16) float part[2][32];
     __shared__ WarpDesk<T> desk[ALIGNED ? 1 : WARPS == 1 ? kNormRows : WARPS];
     constexpr int T_ROW = 32 * WARPS;
     wait_for_earlier();
@@ -250,7 +258,7 @@ struct GradRow {
 template <typename T, int WARPS, int UNITS, bool CODES, bool ALIGNED>
 __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGradWarps<T, UNITS> / (WARPS == 1 ? kNormRows : WARPS)) rms_norm_grad_kernel(const __grid_constant__ NormGradIn in)
 {
-    __shared__ float part[2][32];
+    __shared__ __align__(16) float part[2][32];
     __shared__ WarpDesk<T> desk[ALIGNED ? 1 : WARPS == 1 ? kNormRows : WARPS];
     constexpr int T_ROW = 32 * WARPS, GROUPS = WARPS == 1 ? kNormRows : 1;
     wait_for_earlier();
@@ -314,6 +322,147 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
         float *to = in.parts + (static_cast<long long>(blockIdx.x) * GROUPS + group) * in.cols + col;
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) if (col + k < in.cols) to[k] = acc[j].v[k];
+    }
+}
+
+// The same for rows whose bytes are whole vectors, from the codes: rows come by bulk copies into a ring of shared memory, several ahead, and a thread's registers hold one row. (With the next row's
+// loads in registers, the loads under way covered the latency of HBM only while nothing waited: 88 us of 16384 x 4096 in bf16, where 72 are the bytes' at the copy rate.)
+//
+// A slot is free once every thread has taken its part, which the barrier of the row's sum shows.  Waits are bounded: one that runs out makes the block's later rows
+// and its part NaN; it waits for nothing after that but the copies under way, with the same limit.
+constexpr int kNormWaitLimit = 1 << 20, kMostSlots = 8;
+__device__ __forceinline__ unsigned norm_smem(const void *p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ bool norm_wait(unsigned bar, unsigned parity)
+{
+    for (int tries = 0; tries < kNormWaitLimit; ++tries) {
+        unsigned ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void norm_copy(unsigned to, const void *from, unsigned bytes, unsigned bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+
+struct GradRing { int slots, row_bytes, code_bytes, slot_bytes; };          // of a row of activations, of codes, of all that a slot holds
+template <typename T, int WARPS, int UNITS>
+__global__ void __launch_bounds__(32 * WARPS, kGradWarps<T, UNITS> / WARPS) rms_norm_grad_ring_kernel(const __grid_constant__ NormGradIn in, const __grid_constant__ GradRing ring)
+{
+    extern __shared__ __align__(128) unsigned char slots[];
+    __shared__ __align__(16) float part[2][32];
+    __shared__ __align__(8) unsigned long long full[kMostSlots];
+    constexpr int T_ROW = 32 * WARPS;
+    const int tid = threadIdx.x, units = in.cols / kUnit, blocks = (in.cols + kPackBlock - 1) / kPackBlock;
+    if (tid == 0) {
+        for (int k = 0; k < ring.slots; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(norm_smem(&full[k])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    wait_for_earlier();
+    let_next_start();
+    const long long step = gridDim.x;
+    const auto fetch = [&](long long row, int slot) {
+        const unsigned bar = norm_smem(&full[slot]), to = norm_smem(slots + slot * ring.slot_bytes);
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(ring.row_bytes * (in.dtotal ? 2 : 1) + ring.code_bytes) : "memory");
+        norm_copy(to, static_cast<const T *>(in.dout) + row * in.dout_stride, ring.row_bytes, bar);
+        norm_copy(to + ring.row_bytes, reinterpret_cast<const unsigned char *>(in.codes) + row * ring.code_bytes, ring.code_bytes, bar);
+        if (in.dtotal) norm_copy(to + ring.row_bytes + ring.code_bytes, static_cast<const T *>(in.dtotal) + row * in.dtotal_stride, ring.row_bytes, bar);
+    };
+    long long row = blockIdx.x;
+    if (tid == 0)
+        for (int k = 0; k < ring.slots; ++k) if (row + k * step < in.rows) fetch(row + k * step, k);
+    Unit acc[UNITS];
+    unsigned scale[UNITS], next_scale[UNITS];
+    float r = 0.f, next_r = 0.f;
+    const float *rstd = in.rstd + row;
+    const uint8_t *scales = in.scales + row * blocks + tid / 4;
+    const auto ahead = [&](long long at) {                 // what is too small to copy in bulk, a row ahead
+        if (at >= in.rows) return;
+        next_r = __ldg(rstd);
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) if (j * T_ROW + tid < units) next_scale[j] = __ldg(scales + j * (T_ROW / 4));
+        rstd += step;
+        scales += step * blocks;
+    };
+    T *dx_row = static_cast<T *>(in.dx) + row * in.cols + tid * kUnit;
+    const float share = 1.f / static_cast<float>(in.cols);
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) {
+        next_scale[j] = 0;
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) acc[j].v[k] = 0.f;
+    }
+    ahead(row);
+    Unit gains[UNITS];                                     // of this thread's columns, for all its rows
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) if (j * T_ROW + tid < units) gains[j] = load_gain(in.gain, in.gain_bf16, (j * T_ROW + tid) * kUnit, kUnit, true);
+    bool late = false;
+    int slot = 0, side = 0;
+    unsigned parity = 0;
+    for (; row < in.rows; row += step, side ^= 1) {
+        r = next_r;
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) scale[j] = next_scale[j];
+        ahead(row + step);
+        late = late || !norm_wait(norm_smem(&full[slot]), parity);
+        if (late) r = __int_as_float(0x7fc00000);
+        const unsigned char *here = slots + slot * ring.slot_bytes;
+        Unit g[UNITS], n[UNITS];
+        RawUnit<T> more[UNITS];
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int unit = j * T_ROW + tid;
+            if (unit >= units) continue;
+            RawUnit<T> d;
+            d.take(here + unit * (kUnit * sizeof(T)));
+            const uint2 codes = *reinterpret_cast<const uint2 *>(here + ring.row_bytes + unit * kUnit);
+            if (in.dtotal) more[j].take(here + ring.row_bytes + ring.code_bytes + unit * (kUnit * sizeof(T)));
+            g[j] = d.values();
+            n[j] = unpack_unit(codes, scale[j]);
+            float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kUnitPairs; ++k) {
+                acc[j].set(k, fma2(g[j].pair(k), n[j].pair(k), acc[j].pair(k)));
+                g[j].set(k, mul2(g[j].pair(k), gains[j].pair(k)));
+                s = fma2(g[j].pair(k), n[j].pair(k), s);
+            }
+            sum += s.x + s.y;
+        }
+        const float mean = row_sum<WARPS>(sum, part, side) * share;
+        if (tid == 0 && !late && row + ring.slots * step < in.rows) fetch(row + ring.slots * step, slot);
+        if (++slot == ring.slots) { slot = 0; parity ^= 1; }
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int unit = j * T_ROW + tid;
+            if (unit >= units) continue;
+            Unit dx;
+            if (in.dtotal) {
+                const Unit m = more[j].values();
+#pragma unroll
+                for (int k = 0; k < kUnitPairs; ++k)
+                    dx.set(k, fma2(fma2(n[j].pair(k), make_float2(-mean, -mean), g[j].pair(k)), make_float2(r, r), m.pair(k)));
+            } else {
+#pragma unroll
+                for (int k = 0; k < kUnitPairs; ++k) dx.set(k, mul2(fma2(n[j].pair(k), make_float2(-mean, -mean), g[j].pair(k)), make_float2(r, r)));
+            }
+            store_unit(dx_row + j * (T_ROW * kUnit), dx, kUnit, true);
+        }
+        dx_row += step * in.cols;
+    }
+    if (late && tid == 0)                                  // copies may still be under way
+        for (int k = 0; k < ring.slots; ++k) { norm_wait(norm_smem(&full[k]), 0); norm_wait(norm_smem(&full[k]), 1); }
+    if (!in.parts) return;
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) {
+        const int unit = j * T_ROW + tid;
+        if (unit >= units) continue;
+        if (late) acc[j].v[0] = __int_as_float(0x7fc00000);
+        float4 *to = reinterpret_cast<float4 *>(in.parts + static_cast<long long>(blockIdx.x) * in.cols + unit * kUnit);
+        to[0] = make_float4(acc[j].v[0], acc[j].v[1], acc[j].v[2], acc[j].v[3]);
+        to[1] = make_float4(acc[j].v[4], acc[j].v[5], acc[j].v[6], acc[j].v[7]);
     }
 }
 

@@ -42,6 +42,7 @@ template <typename T> struct RawUnit;
 template <> struct RawUnit<__nv_bfloat16> {
     uint4 a;
     __device__ __forceinline__ void load(const void *p) { a = load_stream16(p); }
+    __device__ __forceinline__ void take(const void *p) { a = *static_cast<const uint4 *>(p); }
     __device__ __forceinline__ Unit values() const
     {
         Unit u;
@@ -54,6 +55,7 @@ template <> struct RawUnit<__nv_bfloat16> {
 template <> struct RawUnit<float> {
     uint4 a, b;
     __device__ __forceinline__ void load(const void *p) { a = load_stream16(p); b = load_stream16(static_cast<const char *>(p) + 16); }
+    __device__ __forceinline__ void take(const void *p) { a = static_cast<const uint4 *>(p)[0]; b = static_cast<const uint4 *>(p)[1]; }
     __device__ __forceinline__ Unit values() const
     {
         return Unit{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),

@@ -212,18 +212,26 @@ def test_norm_backward(dtype, rows, cols, pad, shift):
 
 
 @gpu
-def test_many_rows_of_the_gains_gradient():
-    """More rows than blocks: every block adds up several."""
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("rows,cols", [(6001, 64), (6001, 1024), (3001, 1100), (5003, 2048), (3001, 4096), (1999, 8192), (1300, 8200)])
+def test_many_rows(dtype, rows, cols):
+    """More rows than blocks: every block goes round its slots of shared memory several times and adds up the gain's gradient."""
     g = torch.Generator().manual_seed(3)
-    for rows, cols in ((6001, 64), (3001, 1100), (1300, 8200)):
-        x, dout = rows_of(g, rows, cols, BF16), rows_of(g, rows, cols, BF16)
-        gain = torch.ones(cols, device="cuda")
-        fwd = P.rms_norm(x, gain, pack=True)
-        r = P.rms_norm_grad(dout, fwd.packed, fwd.rstd, gain)
-        terms = dout.double() * P.unpack8(fwd.packed, FP32).double()
+    x, dout, dtotal = rows_of(g, rows, cols, dtype), rows_of(g, rows, cols, dtype), rows_of(g, rows, cols, dtype, pad=8)
+    gain = (torch.randn(cols, generator=g) + 1).cuda()
+    fwd = P.rms_norm(x, gain, pack=True)
+    n, rstd = P.unpack8(fwd.packed, FP32).double(), fwd.rstd.double()[:, None]
+    for more in (None, dtotal):
+        r = P.rms_norm_grad(dout, fwd.packed, fwd.rstd, gain, more)
+        gd = dout.double() * gain.double()
+        dx = rstd * (gd - n * (gd * n).mean(1, keepdim=True)) + (0 if more is None else more.double())
+        off = (SUM + 8) * EPS * (rstd * (gd.abs() + n.abs() * (gd * n).abs().mean(1, keepdim=True)) + (0 if more is None else more.double().abs()))
+        assert bool(((r.dx.double() - dx).abs() <= off + HALF[dtype] * dx.abs() + 1e-40).all())
+        terms = dout.double() * n
         assert bool(((r.dgain.double() - terms.sum(0)).abs() <= (rows / 32 + SUM) * EPS * terms.abs().sum(0)).all())
-        one = P.rms_norm_grad(dout[-1:], P.Packed8(fwd.packed.codes[-1:], fwd.packed.scales[-1:], cols), fwd.rstd[-1:], gain)
-        assert torch.equal(one.dx[0], r.dx[-1])
+        assert torch.equal(r.dx, P.rms_norm_grad(dout, fwd.packed, fwd.rstd, gain, more).dx)
+    one = P.rms_norm_grad(dout[-1:], P.Packed8(fwd.packed.codes[-1:], fwd.packed.scales[-1:], cols), fwd.rstd[-1:], gain, dtotal[-1:])
+    assert torch.equal(one.dx[0], r.dx[-1])
 
 
 @gpu
