@@ -51,6 +51,12 @@ int over_rows(int64_t rows, int64_t cols, int64_t stride, bool aligned, F launch
     return PS_OK;
 }
 
+// Warps of a row and units (of eight elements) a thread.  As many units as a thread can hold where rows are many: a row costs each of its warps some hundred instructions. More warps where
+// rows are few and the row's latency counts.  us, bf16, residual, both outputs; 32 rows (in a graph) | 64 M elements:
+//     width 1024: 1 x 4 3.6 | 94.7, 4 x 1 1.9 | 100.9 (1 x 4 pulls ahead beyond 2368 rows)       2048: 4 x 2 2.5 | 92.5, 8 x 1 2.1 | 106.0 (592 rows: 3.1, 3.3)
+//     width 4096: 4 x 4 3.7 | 93.3, 8 x 2 2.7 | 94.9, 16 x 1 2.3 | 113.6 (296 rows: 4.1, 3.2, 3.4; 1184: 6.4, 6.9, 7.9)       8192: 8 x 4 4.1 | 94.7, 16 x 2 3.2 | 95.1 (296 rows: 4.9, 5.2)
+// fp32 at 8192: 16 x 2 at every number of rows (296: 6.7 against 10.1; 8192: 89.2, 91.3).  Rows of more than 16384 are read twice (16384: 201 us against 96).
+constexpr int64_t kSms = 148;
 template <typename T, bool ALIGNED>
 int launch_norm(const NormIn &in, cudaStream_t st)
 {
@@ -61,16 +67,21 @@ int launch_norm(const NormIn &in, cudaStream_t st)
     };
     if (units <= 32) return go(softsync::rms_norm_kernel<T, 1, 1, ALIGNED>, 1);
     if (units <= 64) return go(softsync::rms_norm_kernel<T, 1, 2, ALIGNED>, 1);
-    if (units <= 128) return go(softsync::rms_norm_kernel<T, 1, 4, ALIGNED>, 1);
-    if (units <= 256) return go(softsync::rms_norm_kernel<T, 4, 2, ALIGNED>, 4);
-    if (units <= 512) return go(softsync::rms_norm_kernel<T, 4, 4, ALIGNED>, 4);
-    if (units <= 1024) return go(softsync::rms_norm_kernel<T, 8, 4, ALIGNED>, 8);
+    if (units <= 128) return in.rows <= 16 * kSms ? go(softsync::rms_norm_kernel<T, 4, 1, ALIGNED>, 4) : go(softsync::rms_norm_kernel<T, 1, 4, ALIGNED>, 1);
+    if (units <= 256) return in.rows <= 2 * kSms ? go(softsync::rms_norm_kernel<T, 8, 1, ALIGNED>, 8) : go(softsync::rms_norm_kernel<T, 4, 2, ALIGNED>, 4);
+    if (units <= 512) {
+        if (in.rows <= kSms) return go(softsync::rms_norm_kernel<T, 16, 1, ALIGNED>, 16);
+        return in.rows <= 4 * kSms ? go(softsync::rms_norm_kernel<T, 8, 2, ALIGNED>, 8) : go(softsync::rms_norm_kernel<T, 4, 4, ALIGNED>, 4);
+    }
+    if (units <= 1024) return in.rows <= kSms || sizeof(T) == 4 ? go(softsync::rms_norm_kernel<T, 16, 2, ALIGNED>, 16) : go(softsync::rms_norm_kernel<T, 8, 4, ALIGNED>, 8);
     if (units <= 2048) return go(softsync::rms_norm_kernel<T, 16, 4, ALIGNED>, 16);
     return softsync::launch(softsync::rms_norm_long_kernel<T, ALIGNED>, in.rows, softsync::kLongThreads, 0, true, st, in) ? PS_OK : PS_ERR_CUDA;
 }
 
-// Blocks of the backward pass, as many as are resident at once, and with them the parts that the gain's gradient is summed in.
-constexpr int64_t kSms = 148, kLongParts = 64;
+// Blocks of the backward pass, as many as are resident at once, and with them the parts that the gain's gradient is summed in.  Two units a thread where a row has enough, with
+// its bytes through the ring where they are whole vectors (us, 64 M elements bf16, ring / loads to registers): width 1024 4 x 1 79.0 / 95.2, 4 x 2 91.6 / 121.0; 2048 4 x 2 77.3 /
+// 95.1, 8 x 1 78.5 / 93.4; 4096 8 x 2 77.2 / 96.3, 16 x 1 79.5 / 94.9; 8192 16 x 2 77.8 / 97.2, long 207.  Narrow rows have a warp each: 512 1 x 2 99.0, 4 x 1 113.7 / 124.7.
+constexpr int64_t kLongParts = 64;
 struct GradShape { int warps, units; int64_t blocks, parts; };
 template <typename T>
 GradShape grad_shape(int64_t rows, int64_t cols)

