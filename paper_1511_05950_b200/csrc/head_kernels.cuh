@@ -113,6 +113,45 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
     if (col < in.out_stride) *reinterpret_cast<uint4 *>(in.out + static_cast<long long>(row) * in.out_stride + col) = raw.a;
 }
 
+// Rows of whole vectors to dense rows of any width, seen as one run of values: a warp takes 256 of them, reads neighbouring values and writes aligned vectors.  (Written
+// by the product itself, two bytes a lane, 70723 x 3711 took 0.9 ms, and 0.25 by way of aligned rows.)  magic: 2^64 / cols, rounded up, as in PackShape; 0 for one column.
+constexpr int kDenseThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kDenseThreads) dense_rows_kernel(const T *from, long long stride, unsigned count, int cols, unsigned long long magic, T *to)
+{
+    __shared__ WarpDesk<T> desks[kDenseThreads / 32];
+    wait_for_earlier();
+    let_next_start();
+    const int lane = threadIdx.x & 31;
+    const unsigned first = (blockIdx.x * (kDenseThreads / 32) + (threadIdx.x >> 5)) * (32u * kUnit);
+    if (first >= count) return;                            // a whole warp
+    T *v = desks[threadIdx.x >> 5].v;
+    const unsigned width = static_cast<unsigned>(cols), row0 = magic ? static_cast<unsigned>(__umul64hi(first, magic)) : first, col0 = first - row0 * width;
+    T got[kUnit];                                          // all eight under way at once
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) {
+        const unsigned at = first + k * 32 + lane;
+        unsigned row = row0, col = col0 + k * 32 + lane;
+        if (cols >= 32 * kUnit) {                          // at most one row ends among them
+            if (col >= width) { col -= width; ++row; }
+        } else {
+            row = magic ? static_cast<unsigned>(__umul64hi(at, magic)) : at;
+            col = at - row * width;
+        }
+        got[k] = at < count ? from[row * stride + col] : T(0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) v[k * 32 + lane] = got[k];
+    __syncwarp();
+    const unsigned mine = first + lane * kUnit;
+    if (mine + kUnit <= count) {
+#pragma unroll
+        for (int k = 0; k < static_cast<int>(sizeof(T)) / 2; ++k) reinterpret_cast<uint4 *>(to + mine)[k] = reinterpret_cast<const uint4 *>(v + lane * kUnit)[k];
+    } else {
+        for (unsigned k = mine; k < count; ++k) to[k] = v[k - first];
+    }
+}
+
 // A row's parts joined: normaliser, lse, log probability; and, by the last block, the loss.  Eight rows a block, 64 threads share a row's parts (152000
 // entries: 1188 parts).  Bound by latency: two loads' worth of waiting and a short tree (512 rows of 1188 parts: 11.6 us; with 32 rows a block it took 25.8).
 constexpr int kJoinRows = 8, kJoinThreads = 512;

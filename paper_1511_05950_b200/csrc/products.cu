@@ -143,6 +143,20 @@ int launch_split_sums(const softsync::MmaJob<softsync::StoreEpilogue> *jobs, int
     in.blocks = static_cast<int>(blocks[0]);
     return blocks[0] + blocks[1] ? start(softsync::split_sum_kernel, blocks[0] + blocks[1], 256, 0, true, st, in) : PS_OK;
 }
+// A product's rows of `stride` values to where they belong, dense: a launch for every so many rows (of a multiple of eight) as have fewer than 2^32 values.
+template <typename T>
+int launch_dense_rows(const T *from, int64_t rows, int64_t cols, int64_t stride, T *to, cudaStream_t st)
+{
+    const int64_t most = ((int64_t{1} << 32) - 4096) / cols / 8 * 8;
+    const unsigned long long magic = cols == 1 ? 0 : ~0ull / static_cast<unsigned long long>(cols) + 1;
+    for (int64_t first = 0; first < rows; first += most) {
+        const int64_t count = std::min(most, rows - first) * cols;
+        const int status = start(softsync::dense_rows_kernel<T>, div_up(count, softsync::kDenseThreads * softsync::kUnit), softsync::kDenseThreads, 0, true, st, from + first * stride,
+                                 static_cast<long long>(stride), static_cast<unsigned>(count), static_cast<int>(cols), magic, to + first * cols);
+        if (status != PS_OK) return status;
+    }
+    return PS_OK;
+}
 int64_t part_elements() { return int64_t{softsync::kMostParts} * kPairs * kTile * kTile; }
 
 // Row tiles that take turns before the next column tile's: as many as leave their operand in the L2 (32 MB of it), so that the other one is read once for all of them
@@ -179,7 +193,7 @@ struct HeadPlan : Places {
     unsigned *done = nullptr;
     int *order = nullptr, *place = nullptr, *live = nullptr;
     bf16 *hidden = nullptr, *head = nullptr;
-    bf16 *g = nullptr;
+    bf16 *g = nullptr, *dhead = nullptr;   // dhead: a piece's rows, where dense ones allow no vectors
     float *dhidden = nullptr, *split = nullptr;
     HeadPlan(const ps_head &h, bool grad, bool listed, void *p) : Places(p), rows(h.rows), width(h.width), vocab(h.vocab)
     {
@@ -208,6 +222,7 @@ struct HeadPlan : Places {
         take(g, rows_padded * g_stride);
         take(split, 2 * part_elements());
         if (first) take(dhidden, rows * width_padded);
+        if (width_padded != width) take(dhead, std::max(piece, vocab - first) * width_padded);
     }
 };
 
@@ -325,13 +340,14 @@ struct HeadCall {
             if (status == PS_OK && dhead) {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
-                t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = static_cast<bf16 *>(dhead) + first * h.width; t.out_bf16 = 1;
-                t.vectors = width % 8 == 0; t.stride = width; t.parts = w.split + part_elements();
+                t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = w.dhead ? w.dhead : static_cast<bf16 *>(dhead) + first * h.width;
+                t.out_bf16 = 1; t.vectors = 1; t.stride = w.width_padded; t.parts = w.split + part_elements();
                 if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, live(), 1, slots, group_of(n, rows)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && count) 
                 status = count == 2 ? launch_products<OfHidden, OfHead>(jobs, dependent(), st) : dhidden ? launch_products<OfHidden>(jobs, dependent(), st) : launch_products<OfHead>(jobs, dependent(), st);
             if (status == PS_OK && count) status = launch_split_sums(jobs, count, st);
+            if (status == PS_OK && dhead && w.dhead) status = launch_dense_rows(w.dhead, n, h.width, w.width_padded, static_cast<bf16 *>(dhead) + first * h.width, st);
             if (status != PS_OK) return status;
         }
         return PS_OK;
@@ -413,6 +429,7 @@ struct PackedPlan : Places {
     int64_t outs_padded, cols_padded;
     bool copy_dout;
     bf16 *dout = nullptr, *values = nullptr;
+    void *dweight = nullptr;               // rows of cols_padded values, where dense ones allow no vectors
     float *split = nullptr;
     PackedPlan(const ps_packed_grad &a, void *p) : Places(p), outs_padded(round_up(a.outs, 8)), cols_padded(round_up(a.cols, PS_PACK_BLOCK))
     {
@@ -420,6 +437,11 @@ struct PackedPlan : Places {
         if (copy_dout) take(dout, round_up(a.rows, kStep) * outs_padded);
         take(values, a.rows * cols_padded);
         take(split, part_elements());
+        if (a.cols % 8) {
+            char *place;
+            take(place, a.outs * cols_padded * (a.out_dtype == PS_GRAD_BF16 ? 2 : 4));
+            dweight = place;
+        }
     }
 };
 
@@ -472,12 +494,15 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     const Matrix values{w.values, rows, cols, w.cols_padded};
     softsync::StoreEpilogue se{};
     softsync::StoreTarget &t = se.target;
-    t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = a->dweight_dev; t.out_bf16 = a->out_dtype == PS_GRAD_BF16;
-    t.vectors = a->cols % 8 == 0 && aligned_to(a->gain_dev, 16); t.stride = cols; t.parts = w.split;
+    t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = w.dweight ? w.dweight : a->dweight_dev;
+    t.out_bf16 = a->out_dtype == PS_GRAD_BF16; t.vectors = aligned_to(a->gain_dev, 16); t.stride = w.dweight ? w.cols_padded : cols; t.parts = w.split;
     softsync::MmaJob<softsync::StoreEpilogue> job;
     if (!job_of<Lying<true, true>>(job, dout, values, MmaPlan{outs, cols, rows, nullptr, 0, slots, group_of(outs, rows)}, se)) return PS_ERR_CUDA;
     status = launch_products<Lying<true, true>>(&job, true, st);
-    return status == PS_OK ? launch_split_sums(&job, 1, st) : status;
+    if (status == PS_OK) status = launch_split_sums(&job, 1, st);
+    if (status != PS_OK || !w.dweight) return status;
+    return t.out_bf16 ? launch_dense_rows(static_cast<const bf16 *>(w.dweight), outs, cols, w.cols_padded, static_cast<bf16 *>(a->dweight_dev), st)
+                      : launch_dense_rows(static_cast<const float *>(w.dweight), outs, cols, w.cols_padded, static_cast<float *>(a->dweight_dev), st);
 }
 
 }  // extern "C"
