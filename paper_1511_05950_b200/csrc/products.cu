@@ -198,9 +198,11 @@ struct HeadPlan : Places {
     HeadPlan(const ps_head &h, bool grad, bool listed, void *p) : Places(p), rows(h.rows), width(h.width), vocab(h.vocab)
     {
         rows_padded = round_up(rows, kStep);
-        width_padded = round_up(width, 8);
+        width_padded = round_up(width, kStep);              // of copies: rows of whole lines
         copy_head = !matrix_aligned(h.head_dev, vocab, h.head_stride);
-        copy_hidden = listed || !matrix_aligned(h.hidden_dev, rows, h.hidden_stride);
+        // Rows that straddle lines of 128 bytes are loaded slowly: 1024 x 2040 x 50257 733 us as they lie, 626 from a copy (log probabilities alone 232 and 176); 512 x 1000 196 and 199 (62
+        // and 52), 1024 x 200 151 and 163.  The head stays: its copy would cost as much memory as the call is to save.
+        copy_hidden = listed || !matrix_aligned(h.hidden_dev, rows, h.hidden_stride) || (h.hidden_stride % kStep && rows > 2 * kTile && width > 2 * kTile);
         part_count = div_up(vocab, kHalf);
         const int64_t most = std::max<int64_t>(kTile, std::max(kPieceBytes, rows * width * 2) / (2 * rows_padded) / kTile * kTile);
         first = vocab > most ? round_up(vocab - most, kTile) : 0;
@@ -222,7 +224,7 @@ struct HeadPlan : Places {
         take(g, rows_padded * g_stride);
         take(split, 2 * part_elements());
         if (first) take(dhidden, rows * width_padded);
-        if (width_padded != width) take(dhead, std::max(piece, vocab - first) * width_padded);
+        if (width % 8) take(dhead, std::max(piece, vocab - first) * width_padded);
     }
 };
 
@@ -341,7 +343,7 @@ struct HeadCall {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
                 t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = w.dhead ? w.dhead : static_cast<bf16 *>(dhead) + first * h.width;
-                t.out_bf16 = 1; t.vectors = 1; t.stride = w.width_padded; t.parts = w.split + part_elements();
+                t.out_bf16 = 1; t.vectors = 1; t.stride = w.dhead ? w.width_padded : h.width; t.parts = w.split + part_elements();
                 if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, live(), 1, slots, group_of(n, rows)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && count) 
@@ -431,7 +433,7 @@ struct PackedPlan : Places {
     bf16 *dout = nullptr, *values = nullptr;
     void *dweight = nullptr;               // rows of cols_padded values, where dense ones allow no vectors
     float *split = nullptr;
-    PackedPlan(const ps_packed_grad &a, void *p) : Places(p), outs_padded(round_up(a.outs, 8)), cols_padded(round_up(a.cols, PS_PACK_BLOCK))
+    PackedPlan(const ps_packed_grad &a, void *p) : Places(p), outs_padded(round_up(a.outs, kStep)), cols_padded(round_up(a.cols, kStep))
     {
         copy_dout = !matrix_aligned(a.dout_dev, a.rows, a.dout_stride);
         if (copy_dout) take(dout, round_up(a.rows, kStep) * outs_padded);

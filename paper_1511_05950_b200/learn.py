@@ -405,7 +405,8 @@ class _NormLinear(torch.autograd.Function):
 def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
     """(z, total) with total = x + residual and z = (n * gain) @ weight.T (`rms_norm`, then a linear layer; all bf16, x and residual with
     any leading dimensions), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
-    input would take 4.  The gradients are those of the kept values; z and total are not touched by the 8 bits."""
+    input would take 4.  The gradients are those of the kept values; z and total are not touched by the 8 bits.  A backward pass is
+    captured into a CUDA graph as any other of torch's: with no eager graph of the same leaves alive."""
     for t, what in ((x, "x"), (weight, "weight"), *(((residual, "residual"),) if residual is not None else ())):
         if t.dtype != torch.bfloat16:
             raise TypeError("%s must be bf16, got %s" % (what, t.dtype))

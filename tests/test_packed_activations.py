@@ -401,6 +401,39 @@ def test_a_step_of_all_of_them():
 
 
 @gpu
+def test_norm_linear_captured():
+    """A whole step, forward and backward, replayed with other inputs."""
+    g = torch.Generator().manual_seed(23)
+    x, residual, dz, dtotal = (rows_of(g, 200, k, BF16) for k in (128, 128, 96, 128))
+    gain, weight = (torch.randn(*s, generator=g).to(BF16).cuda() for s in ((128,), (96, 128)))
+    leaves = [t.requires_grad_(True) for t in (x, gain, weight)]
+
+    def step():
+        for t in leaves:
+            t.grad = None
+        z, total = P.norm_linear(x, gain, weight, residual=residual)
+        torch.autograd.backward([z, total], [dz, dtotal])
+        return [z, total] + [t.grad for t in leaves]
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for _ in range(2):
+            out = step()
+        del out                                                        # no eager graph of these leaves lives on
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = [t.detach() for t in step()]
+    with torch.no_grad():
+        for t in (x, residual, dz, dtotal):
+            t.copy_(rows_of(g, *t.shape, BF16))
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in got]
+    assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
+@gpu
 def test_two_streams_at_once():
     g = torch.Generator().manual_seed(22)
     sets = [(rows_of(g, 500, 1000, BF16), rows_of(g, 500, 300, BF16)) for _ in range(2)]
