@@ -222,7 +222,8 @@ int ps_rms_norm(const ps_norm *norm, void *stream);
 /* Its backward pass, from the 8 bits (codes_dev, scales_dev) or, where those are NULL, from total:
  *     g = dout gain;     dx = r (g - n mean(g n)) + dtotal, rounded to dtype: the gradient of x and of residual;     dgain = sum over rows of dout n
  * dtotal_dev (what comes back along the residual stream) and gain_dev may be NULL; dgain_dev: cols values of gain_dtype, or NULL.  dx_dev: dense; it may be
- * dout's or dtotal's memory where that is dense.  Sums have a fixed order. */
+ * dout's or dtotal's memory where that is dense (dout's not beyond 8192 columns with a dgain).  Sums have a fixed order.  The workspace (16-byte aligned) is for
+ * dgain: it need not be initialised and holds nothing between calls; calls that share one must not overlap in time. */
 typedef struct ps_norm_grad {
     const void *dout_dev, *total_dev, *gain_dev, *dtotal_dev;
     const int8_t *codes_dev;
@@ -238,7 +239,8 @@ int ps_rms_norm_grad(const ps_norm_grad *grad, void *workspace_dev, int64_t work
 /* The gradient of a weight matrix (outs x cols) whose product took the kept activations n, times a gain, as input:
  *     dweight_jk = gain_k sum_t dout_tj n_tk
  * dout_dev: bf16, rows of `outs` values; n: the 8 bits, which enter the tensor cores exactly; sums in fp32, in a fixed order.  gain_dev: cols values of
- * gain_dtype, or NULL.  dweight_dev: outs x cols, dense, 16-byte aligned, of out_dtype. */
+ * gain_dtype, or NULL.  dweight_dev: outs x cols, dense, 16-byte aligned, of out_dtype; no input's memory.  The workspace (256-byte aligned, as above) has room for the
+ * values of the codes in bf16. */
 typedef struct ps_packed_grad {
     const void *dout_dev, *gain_dev;
     const int8_t *codes_dev;
