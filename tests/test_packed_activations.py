@@ -169,6 +169,21 @@ def test_the_total_in_the_residuals_place(cols):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("cols", [64, 300, 1001, 4096, 20000])
+@pytest.mark.parametrize("eps", [1e-12, 1e-5])
+def test_codes_of_blocks_of_zeros(dtype, cols, eps):
+    """Rows, and blocks within rows, that hold nothing: the least unit, and codes that are 0 whatever the row's factor."""
+    g = torch.Generator().manual_seed(cols)
+    x = rows_of(g, 4, cols, dtype)
+    x[1], x[2, :32], x[3, 32:] = 0.0, 0.0, 0.0
+    r = P.rms_norm(x, eps=eps, pack=True)
+    assert same_codes(r.packed, x.float() * r.rstd[:, None])
+    assert bool((r.packed.codes[1] == 0).all()) and bool((r.packed.scales[1] == 1).all()) and bool((r.out[1] == 0).all())
+    assert bool((r.packed.codes[2, :32] == 0).all()) and bool((r.packed.codes[3, 32:] == 0).all())
+
+
+@gpu
 def test_rows_of_zeros_and_bad_rows():
     x = torch.randn(6, 300, device="cuda").to(BF16)
     x[1], x[2, 4], x[3, 5] = 0.0, float("nan"), float("inf")
