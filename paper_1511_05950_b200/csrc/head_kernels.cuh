@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kKeptThreads) kept_grad_kernel(const __grid_co
             const int col = col0 + j * kKeptThreads * kUnit;
             if (col < in.width) {
                 e[j] = g[col / kUnit];
-                top[j] = __ldg(&in.parts[static_cast<long long>((in.first + col) / kHalf) * in.part_stride + row].x);
+                top[j] = __ldcg(&in.parts[static_cast<long long>((in.first + col) / kHalf) * in.part_stride + row].x);
             }
         }
     }

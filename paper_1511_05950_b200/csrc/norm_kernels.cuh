@@ -380,9 +380,9 @@ __global__ void __launch_bounds__(32 * WARPS, kGradWarps<T, UNITS> / WARPS) rms_
     const uint8_t *scales = in.scales + row * blocks + tid / 4;
     const auto ahead = [&](long long at) {                 // what is too small to copy in bulk, a row ahead
         if (at >= in.rows) return;
-        next_r = __ldg(rstd);
+        next_r = *rstd;
 #pragma unroll
-        for (int j = 0; j < UNITS; ++j) if (j * T_ROW + tid < units) next_scale[j] = __ldg(scales + j * (T_ROW / 4));
+        for (int j = 0; j < UNITS; ++j) if (j * T_ROW + tid < units) next_scale[j] = scales[j * (T_ROW / 4)];
         rstd += step;
         scales += step * blocks;
     };

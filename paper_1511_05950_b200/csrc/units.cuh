@@ -15,7 +15,8 @@ constexpr int kPackBlock = 32;            // columns that share a scale
 constexpr unsigned kAllLanes = 0xffffffffu;
 
 // A kernel of these waits for the one before it on the stream before it touches memory, and lets the next one start: launched as dependent, kernels prepare themselves
-// under the end of their predecessor.
+// under the end of their predecessor.  So they are there while the predecessor still writes, and none of them may read by way of the non-coherent cache
+// (__ldg, ld.global.nc), whose values have to stand still from a kernel's start to its end.
 __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
@@ -210,7 +211,7 @@ __device__ __forceinline__ Unit load_gain(const void *gain, int is_bf16, int col
         const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(gain) + col;
         if (whole) {
             RawUnit<__nv_bfloat16> raw;
-            raw.a = __ldg(reinterpret_cast<const uint4 *>(p));
+            raw.a = *reinterpret_cast<const uint4 *>(p);
             return raw.values();
         }
 #pragma unroll
@@ -218,7 +219,7 @@ __device__ __forceinline__ Unit load_gain(const void *gain, int is_bf16, int col
     } else {
         const float *p = static_cast<const float *>(gain) + col;
         if (whole) {
-            const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
             return Unit{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
         }
 #pragma unroll
