@@ -328,8 +328,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kGra
 // The same for rows whose bytes are whole vectors, from the codes: rows come by bulk copies into a ring of shared memory, several ahead, and a thread's registers hold one row. (With the next row's
 // loads in registers instead the same arithmetic takes 96 us where this takes 77, 4096 wide, 64 M elements of bf16.)  Bound by HBM: 472 MB in 72 us, then 7 for the gain's.
 //
-// A slot is free once every thread has taken its part, which the barrier of the row's sum shows.  Waits are bounded: one that runs out makes the block's later rows
-// and its part NaN; it waits for nothing after that but the copies under way, with the same limit.
+// A slot is free once every thread has taken its part, which the barrier of the row's sum shows.  Waits are bounded: one that runs out makes the rest of the block's rows
+// NaN, and its thread's columns of the block's part; it waits for nothing after that but the copies under way, with the same limit.
 constexpr int kNormWaitLimit = 1 << 20, kMostSlots = 8;
 __device__ __forceinline__ unsigned norm_smem(const void *p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ bool norm_wait(unsigned bar, unsigned parity)
@@ -407,11 +407,10 @@ __global__ void __launch_bounds__(32 * WARPS, kGradWarps<T, UNITS> / WARPS) rms_
         for (int j = 0; j < UNITS; ++j) scale[j] = next_scale[j];
         ahead(row + step);
         late = late || !norm_wait(norm_smem(&full[slot]), parity);
-        if (late) r = __int_as_float(0x7fc00000);
         const unsigned char *here = slots + slot * ring.slot_bytes;
         Unit g[UNITS], n[UNITS];
         RawUnit<T> more[UNITS];
-        float sum = 0.f;
+        float sum = late ? __int_as_float(0x7fc00000) : 0.f;          // one late thread is enough: the row's mean, and with it the whole row
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
             const int unit = j * T_ROW + tid;
@@ -459,7 +458,10 @@ __global__ void __launch_bounds__(32 * WARPS, kGradWarps<T, UNITS> / WARPS) rms_
     for (int j = 0; j < UNITS; ++j) {
         const int unit = j * T_ROW + tid;
         if (unit >= units) continue;
-        if (late) acc[j].v[0] = __int_as_float(0x7fc00000);
+        if (late) {
+#pragma unroll
+            for (int k = 0; k < kUnit; ++k) acc[j].v[k] = __int_as_float(0x7fc00000);
+        }
         float4 *to = reinterpret_cast<float4 *>(in.parts + static_cast<long long>(blockIdx.x) * in.cols + unit * kUnit);
         to[0] = make_float4(acc[j].v[0], acc[j].v[1], acc[j].v[2], acc[j].v[3]);
         to[1] = make_float4(acc[j].v[4], acc[j].v[5], acc[j].v[6], acc[j].v[7]);
