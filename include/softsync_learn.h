@@ -154,6 +154,7 @@ int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, 
  * They are computed a tile at a time (tensor cores, fp32 sums) and never leave the chip.  The gradients go through the vocabulary piece by piece; of a piece
  * the rounded bf16 values
  *     G_tj = a_t (p_tj - 1[j = token])
+ * (a_t relative to a power of two near the largest |a_t|, so that the size of all of them together does not matter)
  * are held in the workspace, for the two products  dhidden = scale G head  and  dhead = scale G^T hidden  (sums in fp32, in a fixed order).  A piece is as wide as
  * 1 GiB of G allows (or as many bytes as the hidden states have, where that is more); ps_head_cross_entropy keeps the exponentials of the last piece from
  * its statistics (16 bits each, 10 of fraction), the other pieces' logits are computed again.

@@ -5,22 +5,26 @@
 
 namespace softsync {
 
-// Rows with a factor (weight or gradient) other than zero, in order: order[j] is the j-th of them, place[row] its number or -1, *live how many; and
-// their sum.  Rows without get zeros in up to two outputs.  One block; each thread takes a run of neighbouring rows a turn.
+// Rows with a factor (weight or gradient) other than zero, in order: order[j] is the j-th of them, place[row] its number or -1, *live how many; their
+// sum (fp64: beyond fp32's range too), and the power of two that they are taken relative to, that of the largest finite one (2^-126 to 2^100: its product with 1 / T stays finite), so that entries of G are rounded
+// alike whatever all factors are multiplied by.  Rows without get zeros in up to two outputs.  One block; each thread takes a run of neighbouring rows a turn.
 constexpr int kOrderThreads = 1024, kOrderRun = 8;
 struct OrderOut {
     int *order, *place, *live;
-    float *inverse, *sum;                  // 1 / sum of the factors (0 for 0), the sum; may be null
+    double *sum;
+    float *scales;                         // 1 / the power, the power, the power / the sum (0 for a sum of 0)
     float *zero_a, *zero_b;                // may be null
 };
 __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *factors, int rows, const __grid_constant__ OrderOut out)
 {
     __shared__ int counts[32];
     __shared__ double sums[32];
+    __shared__ unsigned tops[32];
     let_next_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int base = 0;
     double sum = 0;
+    unsigned top = 0;                                      // bits of the largest finite magnitude
     for (long long first = 0; first < rows; first += kOrderThreads * kOrderRun) {
         const long long at = first + threadIdx.x * kOrderRun;
         float f[kOrderRun];
@@ -30,6 +34,8 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
             f[k] = at + k < rows ? factors[at + k] : 0.f;
             mine += f[k] != 0.f;                           // NaN takes part
             sum += f[k];
+            const unsigned bits = __float_as_uint(f[k]) & 0x7fffffffu;
+            if (bits < 0x7f800000u) top = max(top, bits);
         }
         int before = mine;
         for (int o = 1; o < 32; o <<= 1) {
@@ -61,15 +67,21 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const float *facto
         __syncthreads();                                   // counts are written again
     }
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
-    if (lane == 0) sums[warp] = sum;
+    top = __reduce_max_sync(kAllLanes, top);
+    if (lane == 0) { sums[warp] = sum; tops[warp] = top; }
     __syncthreads();
     if (warp) return;
     sum = sums[lane];
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
+    top = __reduce_max_sync(kAllLanes, tops[lane]);
     if (lane) return;
     *out.live = base;
-    if (out.sum) *out.sum = static_cast<float>(sum);
-    if (out.inverse) *out.inverse = sum == 0 ? 0.f : static_cast<float>(1.0 / sum);
+    *out.sum = sum;
+    const unsigned exponent = min(max(top >> 23, 1u), 227u);
+    const float power = __uint_as_float(exponent << 23);
+    out.scales[0] = __uint_as_float((254u - exponent) << 23);
+    out.scales[1] = power;
+    out.scales[2] = sum == 0 ? 0.f : static_cast<float>(power / sum);
 }
 
 // Rows of a matrix one behind the other in 16-byte vectors, padded with zeros: all of them, or the listed ones, and zero rows up to a whole stage of
@@ -169,7 +181,7 @@ struct JoinIn {
     float2 *norms;
     double *sums;                          // sum w logp of each block
     unsigned *done;
-    const float *total;                    // sum of the weights, or null: rows
+    const double *total;                   // sum of the weights, or null: rows
     float *stats;                          // loss and sum of the weights, or null
 };
 __device__ __forceinline__ float2 join_parts(float2 a, float2 b, float scale)
@@ -242,9 +254,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     __syncthreads();
     if (tid) return;
     for (int w = 1; w < kJoinThreads / 32; ++w) sum += part[w];
-    const float all = in.total ? *in.total : static_cast<float>(in.rows);
-    in.stats[0] = all == 0.f ? 0.f : static_cast<float>(-sum / all);
-    in.stats[1] = all;
+    const double all = in.total ? *in.total : static_cast<double>(in.rows);
+    in.stats[0] = all == 0 ? 0.f : static_cast<float>(-sum / all);
+    in.stats[1] = static_cast<float>(all);
 }
 
 // G of the kept piece, from its exponentials and in their place: p = e 2^(scale (part's maximum - row's) - log2 sum).  A token that is its part's
@@ -258,7 +270,7 @@ struct KeptIn {
     long long part_stride;
     const long long *tokens;
     const int *order, *live;
-    const float *coef;
+    const float *coef, *coef_scale;        // factors of all rows, and what they are multiplied by; null: 1
     float sign, scale;
     int rows;
 };
@@ -285,7 +297,7 @@ __global__ void __launch_bounds__(kKeptThreads) kept_grad_kernel(const __grid_co
     }
     const int at = row < count ? in.order ? in.order[row] : row : 0;
     const long long token = row < count ? in.tokens[at] - in.first : -1;
-    const float a = row < count ? in.coef ? in.sign * in.coef[at] : 1.f : 0.f;
+    const float a = row < count ? in.coef ? in.sign * in.coef[at] * *in.coef_scale : 1.f : 0.f;
     const float2 norm = row < count ? in.norms[row] : make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < kKeptTurns; ++j) {
@@ -293,7 +305,7 @@ __global__ void __launch_bounds__(kKeptThreads) kept_grad_kernel(const __grid_co
         if (col >= in.width) break;
         uint4 out = make_uint4(0, 0, 0, 0);
         if (row < count) {
-            const float f = a * mma_ex2(fmaf(top[j] - norm.x, in.scale, -norm.y)) * 18446744073709551616.f;
+            const float f = a * (mma_ex2(fmaf(top[j] - norm.x, in.scale, -norm.y)) * 18446744073709551616.f);
             const unsigned w[4] = {e[j].x, e[j].y, e[j].z, e[j].w};
             Unit u;
 #pragma unroll

@@ -336,7 +336,7 @@ struct GradEpilogue {
     const int *order;
     const long long *tokens;
     const float2 *norms;                  // of the rows that take part, or null: from lse
-    const float *lse, *coef;              // of all rows; coef null: 1
+    const float *lse, *coef, *coef_scale; // of all rows; coef, and what it is multiplied by, null: 1
     float sign;                           // of coef
     int rows, vocab;
     const int *live;
@@ -345,20 +345,21 @@ struct GradEpilogue {
     __nv_bfloat16 *g;
     long long g_stride;
 
-    int row, tok, write;
+    int row, tok, valid, write;
     float a;
     float2 norm;
     __device__ __forceinline__ void begin(int r, int)
     {
         const int n = live ? *live : rows;
         row = r;
+        valid = r < n;
         write = r < (n + kStep - 1) / kStep * kStep;        // rows up to a whole stage of the next product: zeros
         a = 0.f; norm = make_float2(0.f, 0.f); tok = -1;
-        if (r < n) {
+        if (valid) {
             const int at = order ? order[r] : r;
             const long long t = tokens[at];
             tok = t >= first && t < first + width ? static_cast<int>(t - first) : -1;
-            a = coef ? sign * coef[at] : 1.f;
+            a = coef ? sign * coef[at] * *coef_scale : 1.f;
             norm = row_normaliser(norms, lse, r, at);
             if (t < 0 || t >= vocab) norm.y = CUDART_NAN_F;
         }
@@ -375,7 +376,7 @@ struct GradEpilogue {
             for (int k = 0; k < 32; ++k) x[k] -= at == static_cast<unsigned>(k) ? 1.f : 0.f;
         }
 #pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = a == 0.f ? 0.f : a * x[k];
+        for (int k = 0; k < 32; ++k) x[k] = valid ? a * x[k] : 0.f;
         const int lane = threadIdx.x & 31, row0 = row - lane, k = lane & 3;
         const unsigned there = __ballot_sync(kAllLanes, write);
 #pragma unroll

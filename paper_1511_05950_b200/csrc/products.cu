@@ -188,8 +188,8 @@ struct HeadPlan : Places {
     int64_t rows, width, vocab, rows_padded, width_padded, first, piece, g_stride, parts, part_count;
     bool copy_head, copy_hidden;
     float2 *stat = nullptr, *norms = nullptr;
-    float *picked = nullptr, *inverse = nullptr, *sum = nullptr;
-    double *sums = nullptr;
+    float *picked = nullptr, *scales = nullptr;
+    double *sum = nullptr, *sums = nullptr;
     unsigned *done = nullptr;
     int *order = nullptr, *place = nullptr, *live = nullptr;
     bf16 *hidden = nullptr, *head = nullptr;
@@ -208,7 +208,7 @@ struct HeadPlan : Places {
         first = vocab > most ? round_up(vocab - most, kTile) : 0;
         piece = first ? round_up(div_up(first, div_up(first, most)), kTile) : 0;
         g_stride = round_up(std::max(piece, vocab - first), kTile);
-        take(inverse, 1);
+        take(scales, 3);
         take(sum, 1);
         take(live, 1);
         take(done, 1);
@@ -269,7 +269,7 @@ struct HeadCall {
         int status = PS_OK;
         if (listed)
             status = start(softsync::order_kernel, 1, softsync::kOrderThreads, 0, dependent(), st, factors, static_cast<int>(h.rows),
-                            softsync::OrderOut{w.order, w.place, w.live, w.inverse, w.sum, zero_a, zero_b});
+                            softsync::OrderOut{w.order, w.place, w.live, w.sum, w.scales, zero_a, zero_b});
         softsync::GatherIn in{};
         in.width = static_cast<int>(h.width); in.out_stride = static_cast<int>(w.width_padded);
         if (status == PS_OK && w.copy_head) {
@@ -319,11 +319,11 @@ struct HeadCall {
                 softsync::KeptIn in{};
                 in.g = reinterpret_cast<uint4 *>(w.g); in.stride = w.g_stride / 8; in.first = static_cast<int>(first); in.width = n;
                 in.segments = static_cast<int>(div_up(n, softsync::kKeptColumns)); in.parts = w.stat; in.norms = w.norms; in.part_stride = h.rows; in.tokens = tokens;
-                in.order = order(); in.live = live(); in.coef = coef; in.sign = sign; in.scale = scale; in.rows = rows;
+                in.order = order(); in.live = live(); in.coef = coef; in.coef_scale = w.scales; in.sign = sign; in.scale = scale; in.rows = rows;
                 status = start(softsync::kept_grad_kernel, w.rows_padded * in.segments, softsync::kKeptThreads, 0, dependent(), st, in);
             } else {
                 softsync::GradEpilogue ge{};
-                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live(); ge.scale = scale;
+                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.coef_scale = w.scales; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live(); ge.scale = scale;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
                 const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(rows, width)};
                 softsync::MmaJob<softsync::GradEpilogue> job;
@@ -400,7 +400,7 @@ int ps_head_logprob_grad(const ps_head *head, const float *lse_dev, const float 
     HeadCall call(*head, true, true, workspace_dev, st);
     if (!workspace_dev || !aligned_to(workspace_dev, 256) || workspace_bytes < call.w.bytes) return PS_ERR_INVALID_ARG;
     const int status = call.begin(dlogp_dev, nullptr, nullptr, dhidden_dev);
-    return status == PS_OK ? call.gradients(lse_dev, dlogp_dev, -1.f, call.inv_temperature, nullptr, dhidden_dev, dhead_dev) : status;
+    return status == PS_OK ? call.gradients(lse_dev, dlogp_dev, -1.f, call.inv_temperature, call.w.scales + 1, dhidden_dev, dhead_dev) : status;
 }
 
 int ps_head_cross_entropy(const ps_head *head, const float *weights_dev, float *stats_dev, float *logp_dev, float *lse_dev, void *dhidden_dev, void *dhead_dev,
@@ -418,7 +418,7 @@ int ps_head_cross_entropy(const ps_head *head, const float *weights_dev, float *
     int status = call.begin(weights_dev, logp_dev, lse_dev, dhidden_dev);
     if (status == PS_OK) status = call.statistics(weights_dev, logp_dev, lse_dev, stats_dev, grad);
     if (status != PS_OK || !grad) return status;
-    return call.gradients(nullptr, weights_dev, 1.f, listed ? call.inv_temperature : call.inv_temperature / static_cast<float>(head->rows), listed ? call.w.inverse : nullptr, dhidden_dev,
+    return call.gradients(nullptr, weights_dev, 1.f, listed ? call.inv_temperature : call.inv_temperature / static_cast<float>(head->rows), listed ? call.w.scales + 2 : nullptr, dhidden_dev,
                           dhead_dev);
 }
 
