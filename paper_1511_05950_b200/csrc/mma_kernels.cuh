@@ -256,13 +256,15 @@ __device__ __forceinline__ float2 shares_below(unsigned w)       // times 2^-64
     return make_float2(__uint_as_float((w & 0xffffu) << 13), __uint_as_float(w >> 3 & 0x1fffe000u));
 }
 
+// The tensor cores cut the running sum to 24 bits at every step, towards zero: over a width of 4096 that took 2e-6 of a product (256 steps of 16) whose terms have either sign, and
+// 1e-5 where all have one.  So sums are taken out of tensor memory every kSumStages stages and added up in registers, rounded to nearest: 4e-7.
+constexpr int kSumStages = 16, kNoSums = 1 << 30;
+
 // Maximum and sum of exponentials of a row's 128 columns, and the token's product; of the piece of the vocabulary that is kept, the exponentials
 // themselves, relative to that maximum, in 16 bits.
-//
-// The tensor cores cut the running sum to 24 bits at every step, towards zero: over a width of 4096 that took 2e-6 of a product (256 steps of 16).  So its sums
-// are taken out of tensor memory every kChunk stages and added up here, rounded to nearest: 4e-7.
 struct StatsEpilogue {
-    static constexpr int kChunk = 16;
+    static constexpr int kChunk = kSumStages;
+    static constexpr bool kAllColumns = true;                  // take: 128 columns at once, or 32
     const int *order;                     // the rows that take part, or null: all
     const long long *tokens;
     int rows, vocab;
@@ -330,9 +332,11 @@ __device__ __forceinline__ float2 row_normaliser(const float2 *norms, const floa
     return norms ? norms[row] : make_float2(0.f, lse[at] * 1.4426950408889634f);
 }
 
-// G = a (p - 1[j = token]) of a piece of the vocabulary, rounded to bf16.
+// G = a (p - 1[j = token]) of a piece of the vocabulary, rounded to bf16.  Products are added up as for the statistics, so that they are the very values that lse is made of: taken out once,
+// they left p of a confident row (product 100, width 4096) at 0.999 where it is one.
 struct GradEpilogue {
-    static constexpr int kChunk = 1 << 30;
+    static constexpr int kChunk = kSumStages;
+    static constexpr bool kAllColumns = false;
     const int *order;
     const long long *tokens;
     const float2 *norms;                  // of the rows that take part, or null: from lse
@@ -447,7 +451,8 @@ struct StoreTarget {
     }
 };
 struct StoreEpilogue {
-    static constexpr int kChunk = 1 << 30;
+    static constexpr int kChunk = kNoSums;
+    static constexpr bool kAllColumns = false;
     StoreTarget target;
 
     // This lane stores eight columns of four rows (8 j + lane / 4) of every 32 x 32 sums: their places (null: none), found once a tile.  Where rows allow no vectors it
@@ -603,7 +608,7 @@ struct MmaState {
 template <typename Epilogue, typename L>
 __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &bars, unsigned ring, unsigned tmem, unsigned rank, int pairs, int &start, unsigned &turn, unsigned &sums, bool &late)
 {
-    constexpr bool WHOLE = Epilogue::kChunk < (1 << 30);      // the epilogue takes all 128 columns of a row at once
+    constexpr bool SUMS = Epilogue::kChunk < kNoSums;
     const int warp = __shfl_sync(kAllLanes, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const TileWalk walk(job.plan);
     if (warp == 0) {
@@ -657,11 +662,11 @@ __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &b
         Epilogue ep = job.epilogue;
         const int quarter = warp & 3, half = (warp - kEpilogueWarp) >> 2;
         const unsigned lanes = tmem + (static_cast<unsigned>(quarter * 32) << 16) + half * kHalf, desk = ring + kDesks + (warp - kEpilogueWarp) * kDeskBytes;
-        if constexpr (WHOLE) if (blockIdx.x == 0 && threadIdx.x == 32 * kEpilogueWarp && ep.done) *ep.done = 0;
+        if constexpr (Epilogue::kAllColumns) if (blockIdx.x == 0 && threadIdx.x == 32 * kEpilogueWarp && ep.done) *ep.done = 0;
         for (int t = start; t < walk.count; t += pairs) {
             const TileAt at = walk.at(t);
             const int col = at.n * kTile + half * kHalf, row = at.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
-            if constexpr (WHOLE) {
+            if constexpr (SUMS) {
                 float x[kHalf];
 #pragma unroll
                 for (int k = 0; k < kHalf; ++k) x[k] = 0.f;
@@ -683,7 +688,17 @@ __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &b
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     if (lane == 0) bar_arrive_leader(mma_smem(&bars.drained[buffer]));
                 }
-                ep.take(x, row, col, late, desk);
+                if constexpr (Epilogue::kAllColumns) {
+                    ep.take(x, row, col, late, desk);
+                } else {
+                    ep.begin(row, at.part);
+                    if (late) {
+#pragma unroll
+                        for (int k = 0; k < kHalf; ++k) x[k] = CUDART_NAN_F;
+                    }
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += 32) ep.take(reinterpret_cast<float(&)[32]>(x[c]), col + c, desk);
+                }
             } else {
                 const unsigned buffer = sums & 1;
                 if (at.steps) {

@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import paper_1511_05950_b200 as P
-from tests.test_head_losses import Reference, close, make
+from tests.test_head_losses import BF16, HALF, Reference, close, make
 
 gpu = pytest.mark.gpu
 
@@ -67,6 +67,43 @@ def test_a_dlogp_that_is_no_number_spoils_its_row_alone(bad):
     got = P.head_logprob_grad(hidden, head, tokens, lse, dlogp)
     others = torch.arange(200, device="cuda") != 77
     assert torch.equal(got.dhidden[others], want.dhidden[others]) and not bool(got.dhidden[77].isfinite().any()) and not bool(got.dhead.isfinite().all(1).any())
+
+
+# ---- logits that are computed again ---------------------------------------------------------------------------------------
+
+def confident(rows, width, z, seed):
+    """Rows whose token 0 has a product of about z, all terms of one sign, and all else products of order one."""
+    g = torch.Generator().manual_seed(seed)
+    hidden = (0.5 + torch.rand(rows, width, generator=g)).to(BF16).cuda()
+    head = (0.2 / math.sqrt(width) * torch.randn(300, width, generator=g))
+    head[0] = z / width * (0.5 + torch.rand(width, generator=g))
+    return hidden, head.to(BF16).cuda(), torch.zeros(rows, dtype=torch.int64, device="cuda")
+
+
+@gpu
+@pytest.mark.parametrize("width", [1024, 4096, 16384])
+def test_wide_confident_rows_from_lse(width):
+    """p of the token is 1 but for e^-90, so its G = p - 1 shows how well lse and the logit that is computed again agree: both are the same sum.  What is left is the rounding
+    of lse (below 128: 2^-18), and of two products of about 150 in the exponent (2^-17 each, times log 2)."""
+    hidden, head, tokens = confident(60, width, 100.0, width)
+    score = P.head_logprob(hidden, head, tokens)
+    z = hidden.double() @ head.double().T
+    assert float(z[:, 0].min()) > 90 and float(z[:, 0].max()) < 128 and float(z[:, 1:].max()) < 10
+    dhidden = P.head_logprob_grad(hidden, head, tokens, score.lse, torch.full((60,), -1.0, device="cuda"), grad="hidden").dhidden.double()
+    tol = (2.0 ** -18 + 2 * 2.0 ** -17 * math.log(2)) * (1 + 2 * HALF)
+    rest = torch.exp(z[:, 1:] - score.lse.double()[:, None]).abs() @ head[1:].double().abs()
+    assert bool((dhidden.abs() <= tol * head[0].double().abs() + 2 * rest + 1e-38).all())
+
+
+@gpu
+@pytest.mark.parametrize("width", [1100, 2048])
+def test_gradient_from_lse_at_usual_widths(width):
+    hidden, head, tokens, weights = make(333, width, 3001, seed=width)
+    ref = Reference(hidden, head, tokens, 0.9)
+    lse = P.head_logprob(hidden, head, tokens, temperature=0.9).lse
+    g = P.head_logprob_grad(hidden, head, tokens, lse, -weights, temperature=0.9)
+    dhidden, tol_h, dhead, tol_w = ref.gradients(weights)
+    assert close(g.dhidden, dhidden, tol_h) and close(g.dhead, dhead, tol_w)
 
 
 # ---- memory and refusals (no GPU) -----------------------------------------------------------------------------------------
