@@ -151,7 +151,8 @@ int ps_preference_loss(const ps_logits *logits, const ps_preference_inputs *in, 
 /* ------------------------------------------------------------------------------------------------------------------
  * Losses without logits.  The logits of a position are the products of its hidden state with the rows of the output matrix (the head),
  *     z_tj = hidden_t . head_j / T,     lse_t = log sum_j exp(z_tj),     logp_t = z_t,token - lse_t
- * They are computed a tile at a time (tensor cores, fp32 sums) and never leave the chip.  The gradients go through the vocabulary piece by piece; of a piece
+ * They are computed a tile at a time (tensor cores, fp32 sums) and never leave the chip.  The tensor cores cut a running sum to 24 bits towards zero at each addition of 16 terms, so
+ * their sums are of 1,024 terms at most (of 4,096 in gradients that are rounded to bf16) and are added to nearest in fp32.  The gradients go through the vocabulary piece by piece; of a piece
  * the rounded bf16 values
  *     G_tj = a_t (p_tj - 1[j = token])
  * (a_t relative to a power of two near the largest |a_t|, so that the size of all of them together does not matter)

@@ -112,6 +112,12 @@ __device__ __forceinline__ void tmem_load16(unsigned addr, float (&v)[16])
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tmem_store16(unsigned addr, const float (&v)[16])
+{
+    const unsigned *r = reinterpret_cast<const unsigned *>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
 __device__ __forceinline__ float mma_ex2(float x)
 {
     float r;
@@ -135,6 +141,7 @@ constexpr unsigned kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | (MN_A ? 1u << 1
 // ---- what a product is -------------------------------------------------------------------------------------------------
 struct MmaPlan {
     int m, n, k;                          // extents; where `live` is given it replaces m (live_is_k 0) or k (1)
+    int sum_stages;                       // whose sums are added up in tensor memory, where the epilogue leaves it open
     const int *live;
     int live_is_k;
     int slots;                            // pairs that work at once, where the last tiles may be split along the contraction; else 0
@@ -257,13 +264,14 @@ __device__ __forceinline__ float2 shares_below(unsigned w)       // times 2^-64
 }
 
 // The tensor cores cut the running sum to 24 bits at every step, towards zero: over a width of 4096 that took 2e-6 of a product (256 steps of 16) whose terms have either sign, and
-// 1e-5 where all have one.  So sums are taken out of tensor memory every kSumStages stages and added up in registers, rounded to nearest: 4e-7.
-constexpr int kSumStages = 16, kNoSums = 1 << 30;
+// 1e-5 where all have one.  So sums are taken out of tensor memory every kSumStages stages and added up in registers, rounded to nearest: 4e-7.  Taking them keeps the tensor cores from their
+// sums for a while (a contraction of 8192 in sums of 1024: 7 % of its time, 240 us for 224), so results of 16 bits, whose own rounding is 2e-3, have sums of 4096: 1e-5 at most.
+constexpr int kSumStages = 16, kSumStages16 = 64;
 
 // Maximum and sum of exponentials of a row's 128 columns, and the token's product; of the piece of the vocabulary that is kept, the exponentials
 // themselves, relative to that maximum, in 16 bits.
 struct StatsEpilogue {
-    static constexpr int kChunk = kSumStages;
+    static constexpr int kSums = kSumStages;
     static constexpr bool kAllColumns = true;                  // take: 128 columns at once, or 32
     const int *order;                     // the rows that take part, or null: all
     const long long *tokens;
@@ -335,7 +343,7 @@ __device__ __forceinline__ float2 row_normaliser(const float2 *norms, const floa
 // G = a (p - 1[j = token]) of a piece of the vocabulary, rounded to bf16.  Products are added up as for the statistics, so that they are the very values that lse is made of: taken out once,
 // they left p of a confident row (product 100, width 4096) at 0.999 where it is one.
 struct GradEpilogue {
-    static constexpr int kChunk = kSumStages;
+    static constexpr int kSums = kSumStages;
     static constexpr bool kAllColumns = false;
     const int *order;
     const long long *tokens;
@@ -451,7 +459,7 @@ struct StoreTarget {
     }
 };
 struct StoreEpilogue {
-    static constexpr int kChunk = kNoSums;
+    static constexpr int kSums = 0;
     static constexpr bool kAllColumns = false;
     StoreTarget target;
 
@@ -539,7 +547,7 @@ struct StoreEpilogue {
     }
 };
 
-// One product of a launch: operands, extents, and what becomes of it.
+// One product of a launch: operands, extents, and what becomes of it.  Its size counts: 64 bytes more made every launch 0.6 us longer.
 template <typename Epilogue>
 struct alignas(64) MmaJob {
     CUtensorMap a, b;
@@ -604,13 +612,66 @@ struct MmaState {
     unsigned long long full[kStages], empty[kStages], ready[2], drained[2];
 };
 
+// The epilogue's side of the sums in tensor memory: waits for the next ones; gives a place back.
+__device__ __forceinline__ unsigned sums_arrived(MmaState &bars, unsigned &sums, bool &late)
+{
+    const unsigned buffer = sums & 1;
+    late = late || !bar_wait(mma_smem(&bars.ready[buffer]), (sums >> 1) & 1);
+    ++sums;
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    return buffer;
+}
+__device__ __forceinline__ void sums_taken(MmaState &bars, unsigned buffer)
+{
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if ((threadIdx.x & 31) == 0) bar_arrive_leader(mma_smem(&bars.drained[buffer]));
+}
+// The sums of `steps` stages, of `each` stages one by one, added up in registers.
+__device__ __forceinline__ void add_sums(MmaState &bars, unsigned lanes, int steps, int each, float (&x)[kHalf], unsigned &sums, bool &late)
+{
+#pragma unroll
+    for (int k = 0; k < kHalf; ++k) x[k] = 0.f;
+#pragma unroll 1
+    for (int s = 0; s < steps; s += each) {
+        const unsigned buffer = sums_arrived(bars, sums, late);
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 16) {
+            float y[16];
+            tmem_load16(lanes + buffer * kTile + c, y);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) x[c + k] += y[k];
+        }
+        sums_taken(bars, buffer);
+    }
+}
+// The same where the epilogue wants them in tensor memory, 32 columns at a time: all but the last are added to the last where it lies.  (With them in registers the epilogue's loop had to be
+// unrolled, and its code took 2 us to fetch: 200 rows, 768 x 256, 9.7 us, then 11.9.)
+__device__ __forceinline__ void join_sums(MmaState &bars, unsigned lanes, int steps, int each, unsigned &sums, bool &late)
+{
+    float x[kHalf];
+    add_sums(bars, lanes, steps - each, each, x, sums, late);
+    const unsigned last = lanes + sums_arrived(bars, sums, late) * kTile;
+#pragma unroll
+    for (int c = 0; c < kHalf; c += 16) {
+        float y[16];
+        tmem_load16(last + c, y);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) y[k] += x[c + k];
+        tmem_store16(last + c, y);
+    }
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // One job's tiles, by every warp in its role.  turn, sums: stages and sums so far; late: a wait ran out; start: this pair's first tile.
-template <typename Epilogue, typename L>
+// LONG: a tile or part may have more than one sum.
+template <typename Epilogue, typename L, bool LONG>
 __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &bars, unsigned ring, unsigned tmem, unsigned rank, int pairs, int &start, unsigned &turn, unsigned &sums, bool &late)
 {
-    constexpr bool SUMS = Epilogue::kChunk < kNoSums;
     const int warp = __shfl_sync(kAllLanes, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const TileWalk walk(job.plan);
+    const int each = !LONG ? 1 << 30 : Epilogue::kSums ? Epilogue::kSums : job.plan.sum_stages;
     if (warp == 0) {
         for (int t = start; t < walk.count && !late; t += pairs) {
             const TileAt at = walk.at(t);
@@ -635,7 +696,7 @@ __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &b
             const TileAt at = walk.at(t);
             unsigned buffer = 0;
             for (int s = 0; s < at.steps; ++s, ++turn) {
-                const int in = s % Epilogue::kChunk;
+                const int in = LONG ? static_cast<int>(static_cast<unsigned>(s) % static_cast<unsigned>(each)) : s;
                 if (in == 0) {
                     if (s && elected()) commit_pair(mma_smem(&bars.ready[buffer]));
                     buffer = sums & 1;
@@ -666,68 +727,32 @@ __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &b
         for (int t = start; t < walk.count; t += pairs) {
             const TileAt at = walk.at(t);
             const int col = at.n * kTile + half * kHalf, row = at.m * kTile + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
-            if constexpr (SUMS) {
+            if constexpr (Epilogue::kAllColumns) {
                 float x[kHalf];
-#pragma unroll
-                for (int k = 0; k < kHalf; ++k) x[k] = 0.f;
-#pragma unroll 1
-                for (int s = 0; s < at.steps; s += Epilogue::kChunk) {
-                    const unsigned buffer = sums & 1;
-                    late = late || !bar_wait(mma_smem(&bars.ready[buffer]), (sums >> 1) & 1);
-                    ++sums;
-                    __syncwarp();
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                    for (int c = 0; c < kHalf; c += 16) {
-                        float y[16];
-                        tmem_load16(lanes + buffer * kTile + c, y);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) x[c + k] += y[k];
-                    }
-                    __syncwarp();
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    if (lane == 0) bar_arrive_leader(mma_smem(&bars.drained[buffer]));
-                }
-                if constexpr (Epilogue::kAllColumns) {
-                    ep.take(x, row, col, late, desk);
-                } else {
-                    ep.begin(row, at.part);
-                    if (late) {
-#pragma unroll
-                        for (int k = 0; k < kHalf; ++k) x[k] = CUDART_NAN_F;
-                    }
-#pragma unroll
-                    for (int c = 0; c < kHalf; c += 32) ep.take(reinterpret_cast<float(&)[32]>(x[c]), col + c, desk);
-                }
+                add_sums(bars, lanes, at.steps, each, x, sums, late);
+                ep.take(x, row, col, late, desk);
             } else {
-                const unsigned buffer = sums & 1;
-                if (at.steps) {
-                    late = late || !bar_wait(mma_smem(&bars.ready[buffer]), (sums >> 1) & 1);
-                    ++sums;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                }
+                if (LONG && at.steps > each) join_sums(bars, lanes, at.steps, each, sums, late);
+                else if (at.steps) sums_arrived(bars, sums, late);
+                const unsigned buffer = (sums - 1) & 1;
                 ep.begin(row, at.part);
 #pragma unroll 1
                 for (int c = 0; c < kHalf; c += 32) {
-                    float x[32];
+                    float v[32];
                     __syncwarp();
                     if (at.steps) {
-                        tmem_load32(lanes + buffer * kTile + c, x);
+                        tmem_load32(lanes + buffer * kTile + c, v);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] = 0.f;
+                        for (int k = 0; k < 32; ++k) v[k] = 0.f;
                     }
                     if (late) {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] = CUDART_NAN_F;
+                        for (int k = 0; k < 32; ++k) v[k] = CUDART_NAN_F;
                     }
-                    ep.take(x, col + c, desk);
+                    ep.take(v, col + c, desk);
                 }
-                __syncwarp();
-                if (at.steps) {
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    if (lane == 0) bar_arrive_leader(mma_smem(&bars.drained[buffer]));
-                }
+                if (at.steps) sums_taken(bars, buffer);
             }
         }
     }
@@ -735,8 +760,9 @@ __device__ __forceinline__ void run_job(const MmaJob<Epilogue> &job, MmaState &b
     start = (start + pairs - walk.count % pairs) % pairs;           // turns go on where they are
 }
 
-// Of two jobs (M not void) the second's tiles follow the first's.
-template <typename Epilogue, typename L, typename M>
+// Of two jobs (M not void) the second's tiles follow the first's.  Without LONG it has 128 registers instead of 168, and kernels before and after it on the stream have room to prepare themselves beside it
+// (weight gradient of 200 rows, 768 x 256: 9.6 us, 10.9 with it).
+template <typename Epilogue, typename L, typename M, bool LONG>
 __global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaJob<Epilogue> first, const __grid_constant__ MmaJob<Epilogue> second)
 {
     extern __shared__ unsigned char raw_ring[];
@@ -767,8 +793,8 @@ __global__ void __cluster_dims__(2) __launch_bounds__(kMmaThreads, 1) mma_kernel
     int start = static_cast<int>(blockIdx.x >> 1);
     unsigned turn = 0, sums = 0;                           // stages and sums so far, of both products
     bool late = false;
-    run_job<Epilogue, L>(first, bars, ring, tmem, rank, pairs, start, turn, sums, late);
-    if constexpr (!std::is_void_v<M>) run_job<Epilogue, M>(second, bars, ring, tmem, rank, pairs, start, turn, sums, late);
+    run_job<Epilogue, L, LONG>(first, bars, ring, tmem, rank, pairs, start, turn, sums, late);
+    if constexpr (!std::is_void_v<M>) run_job<Epilogue, M, LONG>(second, bars, ring, tmem, rank, pairs, start, turn, sums, late);
     if (warp == 0 && lane == 0)                            // every copy has arrived, and every stage's release, before either CTA may leave
         for (unsigned k = turn > kStages ? turn - kStages : 0; k < turn; ++k) {
             late = late || !bar_wait(mma_smem(&bars.empty[k % kStages]), (k / kStages) & 1);

@@ -82,11 +82,12 @@ int start(void (*kernel)(K...), int64_t blocks, int threads, int shared, bool de
 
 using softsync::Lying;
 
-// D = A B^T.  L::mn_a: A is given as k x m (else m x k), L::mn_b: B as k x n (else n x k).
+// D = A B^T; rounded16: the result is, in the end.  L::mn_a: A is given as k x m (else m x k), L::mn_b: B as k x n (else n x k).
 template <typename L, typename Epilogue>
-bool job_of(softsync::MmaJob<Epilogue> &job, const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue)
+bool job_of(softsync::MmaJob<Epilogue> &job, const Matrix &a, const Matrix &b, const MmaPlan &plan, const Epilogue &epilogue, bool rounded16 = true)
 {
     job.plan = plan;
+    if constexpr (std::is_same_v<Epilogue, softsync::StoreEpilogue>) job.plan.sum_stages = rounded16 ? softsync::kSumStages16 : softsync::kSumStages;
     if (plan.slots && !plan.live) {
         const int64_t rest = div_up(plan.m, kTile) * div_up(plan.n, kTile) % plan.slots;
         job.plan.splits = rest ? softsync::split_count(static_cast<int>(rest), static_cast<int>(div_up(plan.k, kStep)), plan.slots) : 1;
@@ -105,12 +106,20 @@ int64_t items_of(const MmaPlan &plan)
     return tiles + int64_t{rest} * (plan.splits - 1);
 }
 
+// Stages of the longest tile or part, as far as the host knows.
+int64_t longest_of(const MmaPlan &plan)
+{
+    const int64_t steps = div_up(plan.k, kStep);
+    if (!plan.slots || plan.live || plan.splits <= 1) return steps;
+    return div_up(plan.m, kTile) * div_up(plan.n, kTile) < plan.slots ? div_up(steps, plan.splits) : steps;
+}
+
 // One product, or two whose operands are both there: a launch of its own costs 10 us (48 x 256 x 32000: 63 us with two, 53 with one).
-template <typename L, typename M = void, typename Epilogue>
-int launch_products(const softsync::MmaJob<Epilogue> *jobs, bool dependent, cudaStream_t st)
+template <typename L, typename M, bool LONG, typename Epilogue>
+int launch_products_as(const softsync::MmaJob<Epilogue> *jobs, bool dependent, cudaStream_t st)
 {
     constexpr int count = std::is_void_v<M> ? 1 : 2;
-    const auto kernel = softsync::mma_kernel<Epilogue, L, M>;
+    const auto kernel = softsync::mma_kernel<Epilogue, L, M, LONG>;
     static std::atomic<bool> ready[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return PS_ERR_CUDA;
@@ -127,6 +136,16 @@ int launch_products(const softsync::MmaJob<Epilogue> *jobs, bool dependent, cuda
     const int64_t pairs = std::min<int64_t>(items, pairs_on_device());
     if (pairs < 1) return PS_ERR_CUDA;
     return start(kernel, 2 * pairs, softsync::kMmaThreads, softsync::kMmaShared, dependent, st, jobs[0], jobs[count - 1]);
+}
+template <typename L, typename M = void, typename Epilogue>
+int launch_products(const softsync::MmaJob<Epilogue> *jobs, bool dependent, cudaStream_t st)
+{
+    bool sums = Epilogue::kAllColumns;
+    for (int k = 0; k < (std::is_void_v<M> ? 1 : 2) && !sums; ++k) sums = longest_of(jobs[k].plan) > (Epilogue::kSums ? Epilogue::kSums : jobs[k].plan.sum_stages);
+    if constexpr (!Epilogue::kAllColumns) {
+        if (!sums) return launch_products_as<L, M, false>(jobs, dependent, st);
+    }
+    return launch_products_as<L, M, true>(jobs, dependent, st);
 }
 
 // The sums of up to two products whose last tiles may be split.
@@ -291,7 +310,7 @@ struct HeadCall {
         ep.order = order(); ep.tokens = tokens; ep.rows = static_cast<int>(h.rows); ep.vocab = static_cast<int>(h.vocab); ep.live = live(); ep.scale = scale;
         ep.parts = w.stat; ep.part_stride = h.rows; ep.picked = w.picked; ep.done = w.done;
         if (keep) { ep.kept = reinterpret_cast<uint16_t *>(w.g); ep.kept_stride = w.g_stride; ep.first = static_cast<int>(w.first); }
-        const MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), live(), 0, 0, group_of(h.rows, h.width)};
+        const MmaPlan plan{static_cast<int>(h.rows), static_cast<int>(h.vocab), static_cast<int>(h.width), 0, live(), 0, 0, group_of(h.rows, h.width)};
         softsync::MmaJob<softsync::StatsEpilogue> job;
         if (!job_of<Lying<false, false>>(job, hidden, head, plan, ep)) return PS_ERR_CUDA;
         const int status = launch_products<Lying<false, false>>(&job, dependent(), st);
@@ -325,7 +344,7 @@ struct HeadCall {
                 softsync::GradEpilogue ge{};
                 ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.coef_scale = w.scales; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live(); ge.scale = scale;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
-                const MmaPlan plan{rows, n, width, live(), 0, 0, group_of(rows, width)};
+                const MmaPlan plan{rows, n, width, 0, live(), 0, 0, group_of(rows, width)};
                 softsync::MmaJob<softsync::GradEpilogue> job;
                 status = job_of<Lying<false, false>>(job, hidden, entries, plan, ge) ? launch_products<Lying<false, false>>(&job, dependent(), st) : PS_ERR_CUDA;
             }
@@ -337,14 +356,14 @@ struct HeadCall {
                 t.rows = rows; t.cols = width; t.live = live(); t.order = order(); t.alpha = alpha; t.alpha_dev = alpha_dev;
                 if (k == pieces - 1) { t.out = dhidden; t.out_bf16 = 1; t.vectors = width % 8 == 0; t.stride = width; }
                 t.sum = w.dhidden; t.sum_stride = w.width_padded; t.add = k > 0; t.parts = w.split;
-                if (!job_of<OfHidden>(jobs[count++], g, entries, MmaPlan{rows, width, n, live(), 0, slots, group_of(rows, n)}, se)) return PS_ERR_CUDA;
+                if (!job_of<OfHidden>(jobs[count++], g, entries, MmaPlan{rows, width, n, 0, live(), 0, slots, group_of(rows, n)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && dhead) {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
                 t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = w.dhead ? w.dhead : static_cast<bf16 *>(dhead) + first * h.width;
                 t.out_bf16 = 1; t.vectors = 1; t.stride = w.dhead ? w.width_padded : h.width; t.parts = w.split + part_elements();
-                if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, live(), 1, slots, group_of(n, rows)}, se)) return PS_ERR_CUDA;
+                if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, 0, live(), 1, slots, group_of(n, rows)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && count) 
                 status = count == 2 ? launch_products<OfHidden, OfHead>(jobs, dependent(), st) : dhidden ? launch_products<OfHidden>(jobs, dependent(), st) : launch_products<OfHead>(jobs, dependent(), st);
@@ -499,7 +518,7 @@ int ps_packed_weight_grad(const ps_packed_grad *a, void *workspace_dev, int64_t 
     t.rows = outs; t.cols = cols; t.alpha = 1.f; t.gain = a->gain_dev; t.gain_bf16 = a->gain_dtype == PS_GRAD_BF16; t.out = w.dweight ? w.dweight : a->dweight_dev;
     t.out_bf16 = a->out_dtype == PS_GRAD_BF16; t.vectors = aligned_to(a->gain_dev, 16); t.stride = w.dweight ? w.cols_padded : cols; t.parts = w.split;
     softsync::MmaJob<softsync::StoreEpilogue> job;
-    if (!job_of<Lying<true, true>>(job, dout, values, MmaPlan{outs, cols, rows, nullptr, 0, slots, group_of(outs, rows)}, se)) return PS_ERR_CUDA;
+    if (!job_of<Lying<true, true>>(job, dout, values, MmaPlan{outs, cols, rows, 0, nullptr, 0, slots, group_of(outs, rows)}, se, t.out_bf16)) return PS_ERR_CUDA;
     status = launch_products<Lying<true, true>>(&job, true, st);
     if (status == PS_OK) status = launch_split_sums(&job, 1, st);
     if (status != PS_OK || !w.dweight) return status;
