@@ -182,6 +182,7 @@ int ps_head_logprob(const ps_head *head, const float *weights_dev, float *logp_d
                     void *stream);
 
 /* The gradients of any loss of the log probabilities, from dlogp_t = dloss/dlogp_t and lse (of ps_head_logprob): a_t = -dlogp_t, scale = 1 / T.
+ * p is exp(z - lse): off by lse's rounding to fp32 (2^-20 of p at an lse of 16, 2^-15 at 512), which is what is left of p - 1 where a row is that sure of its token.
  * dhidden_dev: rows x width, dhead_dev: vocab x width, dense, 16-byte aligned, bf16; either may be NULL. */
 int ps_head_logprob_grad(const ps_head *head, const float *lse_dev, const float *dlogp_dev, void *dhidden_dev, void *dhead_dev, void *workspace_dev,
                          int64_t workspace_bytes, void *stream);

@@ -333,15 +333,11 @@ struct StatsEpilogue {
     }
 };
 
-// A row's normaliser as the products' maximum and log2 of the sum relative to it: p = 2^(scale (x - maximum) - log2 sum), whose rounding is that of small
-// numbers where p is near one.
-__device__ __forceinline__ float2 row_normaliser(const float2 *norms, const float *lse, int row, int at)
-{
-    return norms ? norms[row] : make_float2(0.f, lse[at] * 1.4426950408889634f);
-}
-
 // G = a (p - 1[j = token]) of a piece of the vocabulary, rounded to bf16.  Products are added up as for the statistics, so that they are the very values that lse is made of: taken out once,
 // they left p of a confident row (product 100, width 4096) at 0.999 where it is one.
+//
+// p = 2^(scale (x - maximum) - log2 sum) from the statistics of the row, whose rounding is that of small numbers where p is near one.  From lse alone, p = 2^(log2(e) (x / T - lse)): the
+// difference first, for the same reason, so that what is left there is lse's own rounding.
 struct GradEpilogue {
     static constexpr int kSums = kSumStages;
     static constexpr bool kAllColumns = false;
@@ -352,7 +348,7 @@ struct GradEpilogue {
     float sign;                           // of coef
     int rows, vocab;
     const int *live;
-    float scale;
+    float scale, last;                    // p = 2^(last (scale (x - norm.x) - norm.y)): log2(e) / T and 1, or 1 / T and log2(e)
     int first, width;                     // the piece: columns [first, first + width)
     __nv_bfloat16 *g;
     long long g_stride;
@@ -372,7 +368,7 @@ struct GradEpilogue {
             const long long t = tokens[at];
             tok = t >= first && t < first + width ? static_cast<int>(t - first) : -1;
             a = coef ? sign * coef[at] * *coef_scale : 1.f;
-            norm = row_normaliser(norms, lse, r, at);
+            norm = norms ? norms[r] : make_float2(0.f, lse[at]);
             if (t < 0 || t >= vocab) norm.y = CUDART_NAN_F;
         }
     }
@@ -382,7 +378,7 @@ struct GradEpilogue {
         const unsigned at = static_cast<unsigned>(tok - col);
         const bool picked = __any_sync(kAllLanes, at < 32u);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = mma_ex2(fmaf(x[k] - norm.x, scale, -norm.y));
+        for (int k = 0; k < 32; ++k) x[k] = mma_ex2(fmaf(x[k] - norm.x, scale, -norm.y) * last);
         if (picked) {
 #pragma unroll
             for (int k = 0; k < 32; ++k) x[k] -= at == static_cast<unsigned>(k) ? 1.f : 0.f;

@@ -342,7 +342,8 @@ struct HeadCall {
                 status = start(softsync::kept_grad_kernel, w.rows_padded * in.segments, softsync::kKeptThreads, 0, dependent(), st, in);
             } else {
                 softsync::GradEpilogue ge{};
-                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.coef_scale = w.scales; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live(); ge.scale = scale;
+                ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.coef_scale = w.scales; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live();
+                ge.scale = lse ? inv_temperature : scale; ge.last = lse ? static_cast<float>(1.4426950408889634) : 1.f;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
                 const MmaPlan plan{rows, n, width, 0, live(), 0, 0, group_of(rows, width)};
                 softsync::MmaJob<softsync::GradEpilogue> job;

@@ -96,6 +96,19 @@ def test_wide_confident_rows_from_lse(width):
 
 
 @gpu
+@pytest.mark.parametrize("temperature", [0.7, 1.0, 0.3])
+def test_products_of_hundreds_from_lse(temperature):
+    """The difference to lse comes before the exponential's scale: with products over T of up to 512 only lse's own rounding is left (2^-16)."""
+    hidden, head, tokens = confident(200, 256, 330.0 * temperature, 61)
+    hidden *= torch.linspace(0.8, 1.25, 200, device="cuda")[:, None].to(BF16)
+    score = P.head_logprob(hidden, head, tokens, temperature=temperature)
+    z = hidden.double() @ head.double().T / temperature
+    assert 250 < float(z[:, 0].max()) < 512 and float((z[:, 1:] - z[:, :1]).max()) < -150
+    dhidden = P.head_logprob_grad(hidden, head, tokens, score.lse, torch.full((200,), -1.0, device="cuda"), temperature=temperature, grad="hidden").dhidden.double()
+    assert bool((dhidden.abs() <= 2.0 ** -16 * (1 + 2 * HALF) * head[0].double().abs() / temperature + 1e-38).all())
+
+
+@gpu
 @pytest.mark.parametrize("width", [1100, 2048])
 def test_gradient_from_lse_at_usual_widths(width):
     hidden, head, tokens, weights = make(333, width, 3001, seed=width)
@@ -107,3 +120,7 @@ def test_gradient_from_lse_at_usual_widths(width):
 
 
 # ---- memory and refusals (no GPU) -----------------------------------------------------------------------------------------
+
+
+def up(x, by):
+    return -(-x // by)
