@@ -206,6 +206,7 @@ int ps_unpack8(const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows,
 
 /* Root-mean-square norm of the residual stream, row by row:
  *     total = x + residual, rounded to dtype (x where residual_dev is NULL);     r = 1 / sqrt(mean(total^2) + eps);     n = total r
+ * (r to fp32's accuracy wherever it is a number of fp32, whether or not the squares are);
  *     out = n gain, rounded to dtype (n where gain_dev is NULL);     codes, scales = 8 bits of n (before the gain, which the backward pass and
  *     ps_packed_weight_grad apply)
  * total_dev (total_stride elements a row) may be NULL, or the memory of x or of residual (with the same stride); out_dev (dense) may be NULL, or x's memory where

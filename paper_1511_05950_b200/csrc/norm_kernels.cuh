@@ -34,6 +34,24 @@ __device__ __forceinline__ float row_sum(float x, float (*part)[32], int slot)
     return x;
 }
 
+// The same in fp64, for a row whose squares fp32 cannot hold.
+template <int WARPS>
+__device__ __forceinline__ double row_sum64(double x, float (*part)[32])
+{
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kAllLanes, x, o);
+    if constexpr (WARPS > 1) {
+        double *sums = reinterpret_cast<double *>(part);
+        __syncthreads();                                   // the row's sum in fp32 has been read
+        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = 0;
+        for (int w = 0; w < WARPS; ++w) x += sums[w];
+    }
+    return x;
+}
+// Whether a row's mean square plus eps, made in fp32, is what it should be: no square or sum overflowed, and what vanished below 2^-126 (at most 2^-150 of the mean) does not matter beside it.
+__device__ __forceinline__ bool mean_square_fits(float m) { return m >= 7.52316385e-37f && m <= 3.40282347e38f; }              // 2^-120, the largest
+
 // ---- forward -----------------------------------------------------------------------------------------------------------
 struct NormIn {
     const void *x, *residual, *gain;      // residual, gain: may be null
@@ -68,7 +86,8 @@ __device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, in
     }
 }
 
-// total = round(x + residual), r = 1 / sqrt(mean(total^2) + eps), n = total r; out = round(n gain), codes of n.
+// total = round(x + residual), r = 1 / sqrt(mean(total^2) + eps), n = total r; out = round(n gain), codes of n.  Rows whose squares overflow fp32 (values around 1e18 and more), or vanish in it beside an
+// eps that does too, are added up again in fp64: the row is there, and the test for it costs nothing (one comparison a row).
 // WARPS warps a row (one warp: a block has kNormRows rows), UNITS units a thread: the row stays in registers between its sum and its outputs, so
 // each byte crosses HBM once.  Bound by HBM: 16384 x 4096 bf16 with residual and both outputs moves 606 MB in 93 us (6.5 TB/s).
 constexpr int kNormRows = 4;
@@ -116,7 +135,16 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
         sum += s.x + s.y;
     }
     sum = row_sum<WARPS>(sum, part, 0);
-    const float r = __frsqrt_rn(sum / static_cast<float>(in.cols) + in.eps);
+    const float m = sum / static_cast<float>(in.cols) + in.eps;
+    float r = __frsqrt_rn(m);
+    if (!mean_square_fits(m)) {                            // the same for the whole row
+        double wide = 0;
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j)
+#pragma unroll
+            for (int k = 0; k < kUnit; ++k) wide = fma(static_cast<double>(u[j].v[k]), static_cast<double>(u[j].v[k]), wide);
+        r = static_cast<float>(1.0 / sqrt(row_sum64<WARPS>(wide, part) / in.cols + in.eps));
+    }
     if (tid == 0) in.rstd[row] = r;
 #pragma unroll
     for (int j = 0; j < UNITS; ++j) {
@@ -168,7 +196,21 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(const __gri
     __syncthreads();
     sum = 0;
     for (int k = 0; k < kLongThreads / 32; ++k) sum += part[k];
-    const float r = __frsqrt_rn(static_cast<float>(sum / in.cols) + in.eps);
+    float r = __frsqrt_rn(static_cast<float>(sum / in.cols) + in.eps);
+    if (!mean_square_fits(static_cast<float>(sum / in.cols) + in.eps)) {
+        sum = 0;
+        for (int col = threadIdx.x * kUnit; col < in.cols; col += kLongThreads * kUnit) {
+            const Unit u = values(col, in.cols - col);
+            for (int k = 0; k < kUnit; ++k) sum = fma(static_cast<double>(u.v[k]), static_cast<double>(u.v[k]), sum);
+        }
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
+        __syncthreads();                                   // the first sums have been read
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+        __syncthreads();
+        sum = 0;
+        for (int k = 0; k < kLongThreads / 32; ++k) sum += part[k];
+        r = static_cast<float>(1.0 / sqrt(sum / in.cols + in.eps));
+    }
     if (threadIdx.x == 0) in.rstd[row] = r;
     const int units = (in.cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kUnit);
     for (int first = 0; first < units; first += kLongThreads) {           // a unit is read and, where total replaces its source, written by one thread

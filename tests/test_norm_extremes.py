@@ -4,9 +4,50 @@ import pytest
 import torch
 
 import paper_1511_05950_b200 as P
-from tests.test_packed_activations import BF16, EPS, FP32
+from tests.test_packed_activations import BF16, EPS, FP32, HALF, SUM, norm_reference, rows_of, same_codes
 
 gpu = pytest.mark.gpu
+
+
+# ---- values far from one --------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 64), (5, 1000), (3, 1001), (400, 2048), (5, 4096), (700, 4096), (3, 16384), (3, 20000), (2, 40001)])
+def test_squares_beyond_fp32(dtype, rows, cols):
+    """Rows whose squares overflow or vanish in fp32 although their mean's root does not: total and 1 / root are representable, so out and codes are as exact as ever.  A row of
+    zeros is there too (NaN without an eps, by the formula), and a usual one."""
+    g = torch.Generator().manual_seed(cols)
+    x = rows_of(g, rows, cols, dtype)
+    x.clamp_(-3.5, 3.5)
+    for power in (125, 100, 63, -62, -80, -100, -120):
+        big = (x.double() * 2.0 ** power).to(dtype)
+        big[-1] = x[-1]
+        for eps in (0.0, 1e-6):
+            if eps and power < 0:
+                continue                                                # eps is all there is: below
+            total, rstd, n, out = norm_reference(big, None, None, eps, dtype)
+            r = P.rms_norm(big, eps=eps, pack=True)
+            assert bool(((r.rstd.double() - rstd).abs() <= SUM * EPS * rstd + 2.0 ** -150).all())
+            assert bool(((r.out.double() - out).abs() <= (SUM + 4) * EPS * out.abs() + HALF[dtype] * out.abs() * (1 + SUM * EPS) + 1e-40).all())
+            assert same_codes(r.packed, total.float() * r.rstd[:, None])
+    small = (x.double() * 2.0 ** -80).to(dtype)
+    r = P.rms_norm(small, eps=1e-6)
+    assert bool(((r.rstd.double() - 1e3).abs() <= 1e3 * SUM * EPS).all())
+    x[0] = 0.0
+    assert bool(P.rms_norm(x, eps=0.0).out[0].isnan().all()) and bool((P.rms_norm(x, eps=1e-6).out[0] == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("cols", [64, 1001, 4096, 20000])
+def test_a_large_total_of_residual_and_input(cols):
+    g = torch.Generator().manual_seed(cols)
+    x, residual = ((rows_of(g, 9, cols, BF16).clamp(-3, 3).double() * 2.0 ** k).to(BF16) for k in (90, 91))
+    gain = (torch.randn(cols, generator=g) + 1).cuda()
+    total, rstd, n, out = norm_reference(x, residual, gain, 1e-6, BF16)
+    r = P.rms_norm(x, gain, residual, inplace=True)
+    assert torch.equal(r.total, total) and bool(((r.rstd.double() - rstd).abs() <= SUM * EPS * rstd).all())
+    assert bool(((r.out.double() - out).abs() <= (SUM + 4) * EPS * out.abs() + 2.0 ** -8 * out.abs() * (1 + SUM * EPS) + 1e-40).all())
 
 
 # ---- long sums of one sign ------------------------------------------------------------------------------------------------
