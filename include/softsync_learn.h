@@ -174,7 +174,10 @@ typedef struct ps_head {
 
 /* Bytes of the device workspace (256-byte aligned) of the calls below; grad: of those with gradients.  It need not be initialised and holds nothing
  * between calls; calls that share one must not overlap in time.  Where the width is no multiple of 8, or a matrix is not aligned to 16 bytes
- * (address and stride), the workspace has room for an aligned copy of it. */
+ * (address and stride), the workspace has room for an aligned copy of it, and with gradients for a piece's rows of dhead.
+ * What it holds: 2 bytes for each row and entry of a piece (G: half of what the logits of the piece take in fp32, so a call whose logits are fewer than half a billion holds that much for
+ * them), the hidden states that take part, 8 bytes for each row and 128 entries, and the sums of split tiles (256 KB each; none where a contraction is below 1,024, at most 58 MB
+ * for each gradient). */
 int ps_head_workspace(const ps_head *head, int grad, int64_t *bytes);
 
 /* logp, lse (fp32, rows each) of the rows with a weight; zeros elsewhere.  weights_dev: rows fp32, or NULL (all). */
@@ -244,7 +247,7 @@ int ps_rms_norm_grad(const ps_norm_grad *grad, void *workspace_dev, int64_t work
  *     dweight_jk = gain_k sum_t dout_tj n_tk
  * dout_dev: bf16, rows of `outs` values; n: the 8 bits, which enter the tensor cores exactly; sums in fp32, in a fixed order.  gain_dev: cols values of
  * gain_dtype, or NULL.  dweight_dev: outs x cols, dense, 16-byte aligned, of out_dtype; no input's memory.  The workspace (256-byte aligned, as above) has room for the
- * values of the codes in bf16. */
+ * values of the codes in bf16, for the sums of split tiles (as above), and where cols is no multiple of 8 for aligned rows of the result. */
 typedef struct ps_packed_grad {
     const void *dout_dev, *gain_dev;
     const int8_t *codes_dev;

@@ -156,6 +156,7 @@ template <bool A, bool B> struct Lying { static constexpr bool mn_a = A, mn_b = 
 // written and read).  Measured: 8192 rows, 256 x 256 (one tile of 128 steps) 45 us whole, 23.6 in 4 parts, 19.4 in 12, 19.1 in 24, 19.9 in 37; 8192 x 2048 (34 tiles left over) 192 whole
 // and 193 in two parts, where the power limit gives the fewer SMs a higher clock.
 constexpr int kMostParts = 3;             // times slots: room in the workspace
+constexpr int kLeastSplit = 16, kLeastPart = 4;                  // stages of a tile that is split, and of a part
 constexpr int kSplitChoices = 11;
 __host__ __device__ inline int split_choice(int j)
 {
@@ -165,7 +166,7 @@ __host__ __device__ inline int split_choice(int j)
 __host__ __device__ inline int split_cost(int s, int rest, int steps, int slots)
 {
     if (s == 1) return 5 * (steps + 6);
-    if (steps < 16 || s * 4 > steps || rest * s > kMostParts * slots) return 0x7fffffff;
+    if (steps < kLeastSplit || s * kLeastPart > steps || rest * s > kMostParts * slots) return 0x7fffffff;
     return 5 * ((rest * s + slots - 1) / slots * ((steps + s - 1) / s + 6) + 8) + rest * s;
 }
 inline int split_count(int rest, int steps, int slots)

@@ -176,7 +176,14 @@ int launch_dense_rows(const T *from, int64_t rows, int64_t cols, int64_t stride,
     }
     return PS_OK;
 }
-int64_t part_elements() { return int64_t{softsync::kMostParts} * kPairs * kTile * kTile; }
+// Room for the parts of a product's split tiles, whatever the device leaves of its extents: at most kMostParts x kPairs, of fewer tiles than there are pairs, each in parts of four stages at least.
+int64_t part_elements(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t steps = div_up(k, kStep), tiles = div_up(m, kTile) * div_up(n, kTile);
+    if (steps < softsync::kLeastSplit) return 0;
+    const int64_t each = std::min<int64_t>(softsync::split_choice(softsync::kSplitChoices - 1), steps / softsync::kLeastPart);
+    return std::min(int64_t{softsync::kMostParts} * kPairs, std::min<int64_t>(tiles, kPairs - 1) * each) * kTile * kTile;
+}
 
 // Row tiles that take turns before the next column tile's: as many as leave their operand in the L2 (32 MB of it), so that the other one is read once for all of them
 // (7168 x 2048 x 131072: 10.02 ms with 8 MB, 9.93 with 32, 10.26 with 64).
@@ -213,7 +220,7 @@ struct HeadPlan : Places {
     int *order = nullptr, *place = nullptr, *live = nullptr;
     bf16 *hidden = nullptr, *head = nullptr;
     bf16 *g = nullptr, *dhead = nullptr;   // dhead: a piece's rows, where dense ones allow no vectors
-    float *dhidden = nullptr, *split = nullptr;
+    float *dhidden = nullptr, *split_hidden = nullptr, *split_head = nullptr;
     HeadPlan(const ps_head &h, bool grad, bool listed, void *p) : Places(p), rows(h.rows), width(h.width), vocab(h.vocab)
     {
         rows_padded = round_up(rows, kStep);
@@ -241,9 +248,11 @@ struct HeadPlan : Places {
         take(stat, part_count * rows);
         if (!grad) return;
         take(g, rows_padded * g_stride);
-        take(split, 2 * part_elements());
+        const int64_t widest = std::max(piece, vocab - first);
+        take(split_hidden, part_elements(rows, width, widest));
+        take(split_head, part_elements(widest, width, rows));
         if (first) take(dhidden, rows * width_padded);
-        if (width % 8) take(dhead, std::max(piece, vocab - first) * width_padded);
+        if (width % 8) take(dhead, widest * width_padded);
     }
 };
 
@@ -356,14 +365,14 @@ struct HeadCall {
                 softsync::StoreTarget &t = se.target;
                 t.rows = rows; t.cols = width; t.live = live(); t.order = order(); t.alpha = alpha; t.alpha_dev = alpha_dev;
                 if (k == pieces - 1) { t.out = dhidden; t.out_bf16 = 1; t.vectors = width % 8 == 0; t.stride = width; }
-                t.sum = w.dhidden; t.sum_stride = w.width_padded; t.add = k > 0; t.parts = w.split;
+                t.sum = w.dhidden; t.sum_stride = w.width_padded; t.add = k > 0; t.parts = w.split_hidden;
                 if (!job_of<OfHidden>(jobs[count++], g, entries, MmaPlan{rows, width, n, 0, live(), 0, slots, group_of(rows, n)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && dhead) {
                 softsync::StoreEpilogue se{};
                 softsync::StoreTarget &t = se.target;
                 t.rows = n; t.cols = width; t.alpha = alpha; t.alpha_dev = alpha_dev; t.out = w.dhead ? w.dhead : static_cast<bf16 *>(dhead) + first * h.width;
-                t.out_bf16 = 1; t.vectors = 1; t.stride = w.dhead ? w.width_padded : h.width; t.parts = w.split + part_elements();
+                t.out_bf16 = 1; t.vectors = 1; t.stride = w.dhead ? w.width_padded : h.width; t.parts = w.split_head;
                 if (!job_of<OfHead>(jobs[count++], g, hidden, MmaPlan{n, width, rows, 0, live(), 1, slots, group_of(n, rows)}, se)) return PS_ERR_CUDA;
             }
             if (status == PS_OK && count) 
@@ -458,7 +467,7 @@ struct PackedPlan : Places {
         copy_dout = !matrix_aligned(a.dout_dev, a.rows, a.dout_stride);
         if (copy_dout) take(dout, round_up(a.rows, kStep) * outs_padded);
         take(values, a.rows * cols_padded);
-        take(split, part_elements());
+        take(split, part_elements(a.outs, a.cols, a.rows));
         if (a.cols % 8) {
             char *place;
             take(place, a.outs * cols_padded * (a.out_dtype == PS_GRAD_BF16 ? 2 : 4));

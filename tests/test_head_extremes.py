@@ -4,13 +4,14 @@ sums are long, confident rows, and the memory that a call asks for.
 Tolerances are derived beside each test.  Sums of products in the tensor cores are cut towards zero to 24 bits at each of their additions (16 terms each), and are
 taken out and added up to nearest every 1,024 terms: 64 cuts of at most 2^-23 of the sum so far, which in a sum of one sign is half its end on average.
 """
+import ctypes as C
 import math
 
 import pytest
 import torch
 
 import paper_1511_05950_b200 as P
-from tests.test_head_losses import BF16, HALF, Reference, close, make
+from tests.test_head_losses import BF16, HALF, Reference, close, make, struct
 
 gpu = pytest.mark.gpu
 
@@ -121,6 +122,76 @@ def test_gradient_from_lse_at_usual_widths(width):
 
 # ---- memory and refusals (no GPU) -----------------------------------------------------------------------------------------
 
+SLOTS, TILE, STEP, MOST = 74, 256, 64, 3               # CTA pairs, tile, steps of a stage; parts of split tiles that there is room for, in slots
+CHOICES = (1, 2, 3, 4, 6, 8, 12, 16, 24, 37, 74)
+
 
 def up(x, by):
     return -(-x // by)
+
+
+def parts_of(m, n, k, slots):
+    """Parts of split tiles that a product of these extents has, by the rule that the kernels follow."""
+    steps, rest = up(k, STEP), up(m, TILE) * up(n, TILE) % slots
+
+    def cost(s):
+        if s == 1:
+            return 5 * (steps + 6)
+        if steps < 16 or s * 4 > steps or rest * s > MOST * slots:
+            return 1 << 40
+        return 5 * (up(rest * s, slots) * (up(steps, s) + 6) + 8) + rest * s
+
+    best = min(CHOICES, key=cost)
+    return rest * best if rest and best > 1 else 0
+
+
+def head_bytes(rows, width, vocab, grad=1):
+    n = C.c_int64()
+    h = struct(rows=rows, width=width, vocab=vocab, hidden_stride=width, head_stride=width)
+    assert P.ps_head_workspace(C.byref(h), grad, C.byref(n)) == P.PS_OK
+    return n.value
+
+
+def packed_bytes(rows, outs, cols):
+    n = C.c_int64()
+    a = P.binding.PackedGrad(dout_dev=4096, codes_dev=4096, scales_dev=4096, gain_dtype=P.PS_GRAD_FP32, out_dtype=P.PS_GRAD_BF16, rows=rows, outs=outs, cols=cols, dout_stride=outs,
+                             dweight_dev=8192)
+    assert P.ps_packed_grad_workspace(C.byref(a), C.byref(n)) == P.PS_OK
+    return n.value
+
+
+def pieces_of(rows, width, vocab):
+    """(first column of the kept piece, columns of the others) and the columns of G."""
+    most = max(TILE, max(1 << 30, rows * width * 2) // (2 * up(rows, STEP) * STEP) // TILE * TILE)
+    first = up(vocab - most, TILE) * TILE if vocab > most else 0
+    piece = up(up(first, up(first, most)), TILE) * TILE if first else 0
+    return first, piece, up(max(piece, vocab - first), TILE) * TILE
+
+
+@pytest.mark.parametrize("rows,width,vocab", [(1, 64, 500), (48, 256, 32000), (300, 512, 2000), (1000, 1000, 50257), (700, 4096, 4096), (8192, 2048, 131072), (5000, 64, 200), (2000, 520, 700),
+                                              (20001, 64, 60001)])
+def test_room_for_every_split(rows, width, vocab):
+    """Beside G and the sums over pieces there is room for the parts of both gradients, for any number of rows that take part and any number of pairs of CTAs, and not much more."""
+    first, piece, columns = pieces_of(rows, width, vocab)
+    others = up(rows, STEP) * STEP * columns * 2 + (rows * up(width, STEP) * STEP * 4 if first else 0)
+    room = head_bytes(rows, width, vocab) - head_bytes(rows, width, vocab, 0) - others
+    most_h = most_w = 0
+    for live in sorted({*range(1, min(rows, 70)), *range(1, rows, max(1, rows // 200)), rows}):
+        for slots in (SLOTS, SLOTS - 1, 60, 37, 2):
+            for n in {vocab - first, piece or vocab, (first % piece if piece else 0) or vocab - first}:
+                most_h, most_w = max(most_h, parts_of(live, width, n, slots)), max(most_w, parts_of(n, width, live, slots))
+    part = TILE * TILE * 4
+    assert room >= (most_h + most_w) * part
+    widest = max(piece, vocab - first)
+    ceiling = sum(min(MOST * SLOTS, min(up(m, TILE) * up(width, TILE), SLOTS - 1) * min(74, k // (4 * STEP) + 1)) * part for m, k in ((rows, widest), (widest, rows)) if k > 15 * STEP)
+    assert room <= ceiling + 2048
+
+
+def test_small_calls_ask_for_little():
+    assert head_bytes(1, 64, 500) < 1 << 18                                    # it was 116 MB
+    assert head_bytes(48, 256, 32000) < 64 * 32256 * 2 + 74 * TILE * TILE * 4 + (1 << 20)
+    assert packed_bytes(1, 8, 33) < 1 << 14
+    for rows, outs, cols in ((1, 8, 33), (200, 768, 256), (8192, 256, 256), (8192, 8192, 2048), (1023, 64, 64), (1024, 64, 64), (100000, 520, 72)):
+        parts = max(parts_of(outs, cols, rows, slots) for slots in (74, 73, 60, 37, 2))
+        values = rows * up(cols, 64) * 128
+        assert packed_bytes(rows, outs, cols) >= values + parts * TILE * TILE * 4
