@@ -378,13 +378,21 @@ def packed_weight_grad(dout: torch.Tensor, packed: Packed8, gain: Optional[torch
     return dweight
 
 
+def _product(a: torch.Tensor, b: torch.Tensor) -> torch.Tensor:
+    """a @ b in their own type, whatever autocast would make of it: the kernels around it take no other."""
+    if not torch.is_autocast_enabled("cuda"):
+        return a @ b
+    with torch.autocast("cuda", enabled=False):
+        return a @ b
+
+
 class _NormLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gain, weight, residual, eps):
         ctx.set_materialize_grads(False)
         r = rms_norm(x, gain, residual, eps, pack=True)
         ctx.save_for_backward(*r.packed[:2], r.rstd, gain, weight)
-        return r.out @ weight.T, r.total
+        return _product(r.out, weight.T), r.total
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -397,14 +405,14 @@ class _NormLinear(torch.autograd.Function):
         packed = Packed8(codes, scales, weight.shape[1])
         dx = dgain = None
         if needs_x or needs_gain or needs_residual:
-            dx, dgain = rms_norm_grad(dz @ weight, packed, rstd, gain, dtotal, needs_gain)
+            dx, dgain = rms_norm_grad(_product(dz, weight), packed, rstd, gain, dtotal, needs_gain)
         dweight = packed_weight_grad(dz, packed, gain) if needs_weight else None
         return (dx if needs_x else None), dgain, dweight, (dx if needs_residual else None), None
 
 
 def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
     """(z, total) with total = x + residual and z = (n * gain) @ weight.T (`rms_norm`, then a linear layer; all bf16, x and residual with
-    any leading dimensions), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
+    any leading dimensions; they stay bf16 under autocast), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
     input would take 4.  The gradients are those of the kept values; z and total are not touched by the 8 bits.  A backward pass is
     captured into a CUDA graph as any other of torch's: with no eager graph of the same leaves alive."""
     for t, what in ((x, "x"), (weight, "weight"), *(((residual, "residual"),) if residual is not None else ())):

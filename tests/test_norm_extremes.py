@@ -68,3 +68,37 @@ def test_long_sums_of_one_sign(rows, outs, cols):
         n = P.unpack8(P.Packed8(packed.codes[part:part + 65536], packed.scales[part:part + 65536], cols), FP32)
         want += dout[part:part + 65536, some].double().T @ n.double()
     assert bool(((got[some].double() / want - 1).abs() <= 32 * 2.0 ** -23 + (rows / 2048 + 2) * EPS).all())
+
+
+# ---- norm_linear ----------------------------------------------------------------------------------------------------------
+
+def layer(seed, rows=60, width=96, outs=40):
+    g = torch.Generator().manual_seed(seed)
+    rand = lambda *s: torch.randn(*s, generator=g).to(BF16).cuda()  # noqa: E731
+    return rand(rows, width), rand(width) + 1, rand(outs, width) / width ** 0.5, rand(rows, width), rand(rows, outs), rand(rows, width)
+
+
+@gpu
+@pytest.mark.parametrize("kind", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("inside", [True, False])
+def test_norm_linear_under_autocast(kind, inside):
+    """The layer is bf16 whatever type autocast gives to torch's products, and its backward pass runs with it and without."""
+    x, gain, weight, residual, dz, dtotal = layer(3)
+
+    def step():
+        leaves = [t.clone().requires_grad_(True) for t in (x, gain, weight, residual)]
+        out = P.norm_linear(*leaves[:3], residual=leaves[3])
+        if inside:
+            torch.autograd.backward(out, [dz, dtotal])
+        return leaves, out
+
+    def grads(leaves, out):
+        if not inside:
+            torch.autograd.backward(out, [dz, dtotal])
+        return [t.detach() for t in out] + [t.grad for t in leaves]
+
+    want = grads(*step())
+    with torch.autocast("cuda", dtype=kind):
+        leaves, out = step()
+    got = grads(leaves, out)
+    assert all(a.dtype == BF16 for a in got) and all(torch.equal(a, b) for a, b in zip(got, want))
