@@ -410,9 +410,16 @@ class _NormLinear(torch.autograd.Function):
         return (dx if needs_x else None), dgain, dweight, (dx if needs_residual else None), None
 
 
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """All leading dimensions as rows; copied where the columns are apart or rows share memory, which the kernels refuse."""
+    t = t if t.dim() == 2 else t.reshape(-1, t.shape[-1])
+    apart = t.shape[0] > 1 and t.stride(0) < t.shape[1]
+    return t.contiguous() if apart or t.stride(1) != 1 else t
+
+
 def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
     """(z, total) with total = x + residual and z = (n * gain) @ weight.T (`rms_norm`, then a linear layer; all bf16, x and residual with
-    any leading dimensions; they stay bf16 under autocast), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
+    any leading dimensions and strides; they stay bf16 under autocast), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
     input would take 4.  The gradients are those of the kept values; z and total are not touched by the 8 bits.  A backward pass is
     captured into a CUDA graph as any other of torch's: with no eager graph of the same leaves alive."""
     for t, what in ((x, "x"), (weight, "weight"), *(((residual, "residual"),) if residual is not None else ())):
@@ -422,10 +429,9 @@ def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, resid
         raise ValueError("x has width %d, weight shape %s" % (x.shape[-1], tuple(weight.shape)))
     if residual is not None and residual.shape != x.shape:
         raise ValueError("residual has shape %s, x %s" % (tuple(residual.shape), tuple(x.shape)))
+    z, total = _NormLinear.apply(_rows(x), gain, weight, None if residual is None else _rows(residual), eps)
     if x.dim() == 2:
-        return _NormLinear.apply(x, gain, weight, residual, eps)
-    rows = x.reshape(-1, x.shape[-1])
-    z, total = _NormLinear.apply(rows, gain, weight, None if residual is None else residual.reshape(rows.shape), eps)
+        return z, total
     return z.view(*x.shape[:-1], weight.shape[0]), total.view(x.shape)
 
 

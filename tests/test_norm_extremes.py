@@ -102,3 +102,26 @@ def test_norm_linear_under_autocast(kind, inside):
         leaves, out = step()
     got = grads(leaves, out)
     assert all(a.dtype == BF16 for a in got) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
+def test_norm_linear_takes_any_strides():
+    x, gain, weight, residual, dz, dtotal = layer(4)
+    forms = {
+        "columns apart": lambda t: t.T.contiguous().T,
+        "every other": lambda t: torch.stack([t, t], 2).view(len(t), -1)[:, ::2],
+        "rows apart": lambda t: torch.cat([t, t], 1)[:, :t.shape[1]],
+        "one row for all": lambda t: t[:1].expand(len(t), -1),
+        "three dimensions": lambda t: t.view(5, 12, -1).transpose(0, 1),
+    }
+    for name, form in forms.items():
+        results = []
+        for dense in (True, False):
+            a, b = (form(t.clone()) for t in (x, residual))
+            if dense:
+                a, b = (t.clone(memory_format=torch.contiguous_format) for t in (a, b))
+            leaves = [t.detach().requires_grad_(True) for t in (a, gain.clone(), weight.T.contiguous().T, b)]
+            z, total = P.norm_linear(*leaves[:3], residual=leaves[3])
+            torch.autograd.backward([z, total], [form(dz).reshape(z.shape), form(dtotal).reshape(total.shape)])
+            results.append([z.detach(), total.detach()] + [t.grad for t in leaves])
+        assert all(torch.equal(p, q) for p, q in zip(*results)), name
