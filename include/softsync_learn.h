@@ -169,7 +169,7 @@ typedef struct ps_head {
     const void *head_dev;                 /* bf16, vocab rows of `width` values, head_stride elements apart */
     int64_t rows, width, vocab, hidden_stride, head_stride;
     const int64_t *tokens_dev;            /* rows token ids */
-    float temperature;                    /* > 0 */
+    float temperature;                    /* > 0, log2(e) / temperature a number of fp32 */
 } ps_head;
 
 /* Bytes of the device workspace (256-byte aligned) of the calls below; grad: of those with gradients.  It need not be initialised and holds nothing

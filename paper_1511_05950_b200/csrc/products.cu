@@ -21,6 +21,7 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 int64_t div_up(int64_t x, int64_t by) { return (x + by - 1) / by; }
 
 constexpr int64_t kMaxRows = int64_t{1} << 26, kMaxWidth = int64_t{1} << 20, kMaxVocab = int64_t{1} << 28;
+constexpr double kLog2E = 1.4426950408889634;
 constexpr int kPairs = 74;                                 // CTA pairs that the GPU holds: sizes of workspaces go by it, launches by the device
 // Of G, or the hidden states' own size where that is more.  7168 x 2048 x 131072 takes 11.9 ms with 128 MiB, 11.2 with 256, 10.8 with 512, 10.3 with 1 GiB (half of the products are
 // computed once) and 9.5 with 2 GiB (all are): the memory is what the call is for, so it stops at a size that does not grow with the batch.
@@ -96,6 +97,10 @@ bool job_of(softsync::MmaJob<Epilogue> &job, const Matrix &a, const Matrix &b, c
     return encode(job.a, a, L::mn_a ? kStep : kHalf) && encode(job.b, b, L::mn_b ? kStep : kHalf);
 }
 
+// A launch counts its tiles, and the parts of split ones, in 31 bits.  Asked of a call's extents before its first kernel: a refusal leaves everything as it was.
+constexpr int64_t kMostItems = 0x70000000;
+bool too_many_tiles(int64_t m, int64_t n) { return div_up(m, kTile) * div_up(n, kTile) > kMostItems - softsync::kMostParts * kPairs; }
+
 // Items of a product (parts of split tiles one by one): exactly, or at most where only the device knows the extents.
 int64_t items_of(const MmaPlan &plan)
 {
@@ -130,7 +135,7 @@ int launch_products_as(const softsync::MmaJob<Epilogue> *jobs, bool dependent, c
     int64_t items = 0;
     for (int k = 0; k < count; ++k) {
         const int64_t n = items_of(jobs[k].plan);
-        if (n > 0x70000000) return PS_ERR_INVALID_ARG;
+        if (n > kMostItems) return PS_ERR_CUDA;
         items += n;
     }
     const int64_t pairs = std::min<int64_t>(items, pairs_on_device());
@@ -259,7 +264,9 @@ struct HeadPlan : Places {
 int check_head(const ps_head *h)
 {
     if (!h || h->rows < 0 || h->rows > kMaxRows || h->width < 1 || h->width > kMaxWidth || h->vocab < 1 || h->vocab > kMaxVocab) return PS_ERR_INVALID_ARG;
-    if (!(h->temperature > 0.f) || !std::isfinite(h->temperature) || !std::isfinite(1.f / h->temperature)) return PS_ERR_INVALID_ARG;
+    // 1 / T, and log2(e) / T: the exponentials' scale
+    if (!(h->temperature > 0.f) || !std::isfinite(h->temperature) || !std::isfinite(static_cast<float>(kLog2E / h->temperature))) return PS_ERR_INVALID_ARG;
+    if (too_many_tiles(h->rows, h->vocab) || too_many_tiles(h->rows, h->width) || too_many_tiles(h->vocab, h->width)) return PS_ERR_INVALID_ARG;
     if (h->rows == 0) return PS_OK;
     if (!h->hidden_dev || !h->head_dev || !h->tokens_dev || !aligned_to(h->hidden_dev, 2) || !aligned_to(h->head_dev, 2) || !aligned_to(h->tokens_dev, 8)) return PS_ERR_INVALID_ARG;
     const int64_t most = int64_t{1} << 38;                  // elements of a stride: the loads take 2^40 bytes
@@ -280,7 +287,7 @@ struct HeadCall {
 
     HeadCall(const ps_head &head_, bool grad, bool listed_, void *workspace, cudaStream_t stream)
         : h(head_), w(head_, grad, listed_, workspace), st(stream), listed(listed_), tokens(reinterpret_cast<const long long *>(head_.tokens_dev)),
-          scale(static_cast<float>(1.4426950408889634 / static_cast<double>(head_.temperature))), inv_temperature(1.f / head_.temperature)
+          scale(static_cast<float>(kLog2E / head_.temperature)), inv_temperature(1.f / head_.temperature)
     {
         const auto given = [](const void *p, int64_t rows, int64_t cols, int64_t stride) { return Matrix{static_cast<const bf16 *>(p), rows, cols, rows > 1 ? stride : round_up(cols, 8)}; };
         hidden = w.copy_hidden ? Matrix{w.hidden, w.rows_padded, w.width, w.width_padded} : given(h.hidden_dev, h.rows, h.width, h.hidden_stride);
@@ -352,7 +359,7 @@ struct HeadCall {
             } else {
                 softsync::GradEpilogue ge{};
                 ge.order = order(); ge.tokens = tokens; ge.norms = lse ? nullptr : w.norms; ge.lse = lse; ge.coef = coef; ge.coef_scale = w.scales; ge.sign = sign; ge.rows = rows; ge.vocab = static_cast<int>(h.vocab); ge.live = live();
-                ge.scale = lse ? inv_temperature : scale; ge.last = lse ? static_cast<float>(1.4426950408889634) : 1.f;
+                ge.scale = lse ? inv_temperature : scale; ge.last = lse ? static_cast<float>(kLog2E) : 1.f;
                 ge.first = static_cast<int>(first); ge.width = n; ge.g = w.g; ge.g_stride = w.g_stride;
                 const MmaPlan plan{rows, n, width, 0, live(), 0, 0, group_of(rows, width)};
                 softsync::MmaJob<softsync::GradEpilogue> job;
@@ -482,6 +489,7 @@ int check_packed(const ps_packed_grad *a)
     if (!a || a->rows < 0 || a->rows > kMaxRows || a->outs < 1 || a->outs > kMaxVocab || a->cols < 1 || a->cols > kMaxWidth || !is_dtype(a->out_dtype)) return PS_ERR_INVALID_ARG;
     if (a->gain_dev && (!is_dtype(a->gain_dtype) || !aligned_to(a->gain_dev, a->gain_dtype == PS_GRAD_BF16 ? 2 : 4))) return PS_ERR_INVALID_ARG;
     if (a->rows > 1 && (a->dout_stride < a->outs || a->dout_stride > (int64_t{1} << 38))) return PS_ERR_INVALID_ARG;
+    if (too_many_tiles(a->outs, a->cols)) return PS_ERR_INVALID_ARG;
     return PS_OK;
 }
 

@@ -195,3 +195,21 @@ def test_small_calls_ask_for_little():
         parts = max(parts_of(outs, cols, rows, slots) for slots in (74, 73, 60, 37, 2))
         values = rows * up(cols, 64) * 128
         assert packed_bytes(rows, outs, cols) >= values + parts * TILE * TILE * 4
+
+
+@pytest.mark.parametrize("bad", [dict(rows=1 << 26, vocab=1 << 28), dict(rows=1 << 26, vocab=1 << 26), dict(temperature=3e-39), dict(temperature=4e-39)], ids=str)
+def test_refused_before_anything_is_launched(bad):
+    """More tiles than a launch counts, and temperatures whose exponent's scale log2(e) / T is beyond fp32."""
+    n = C.c_int64()
+    h = struct(**bad)
+    assert P.ps_head_workspace(C.byref(h), 1, C.byref(n)) == P.PS_ERR_INVALID_ARG
+    assert P.ps_head_logprob(C.byref(h), 256, 256, 256, 256, 1 << 60, None) == P.PS_ERR_INVALID_ARG
+    assert P.ps_head_cross_entropy(C.byref(h), 256, 256, 256, 256, 256, 256, 256, 1 << 60, None) == P.PS_ERR_INVALID_ARG
+
+
+def test_weight_gradient_of_too_many_tiles_is_refused():
+    n = C.c_int64()
+    a = P.binding.PackedGrad(dout_dev=4096, codes_dev=4096, scales_dev=4096, gain_dtype=P.PS_GRAD_FP32, out_dtype=P.PS_GRAD_BF16, rows=4, outs=1 << 28, cols=1 << 20, dout_stride=1 << 28,
+                             dweight_dev=8192)
+    assert P.ps_packed_grad_workspace(C.byref(a), C.byref(n)) == P.PS_ERR_INVALID_ARG
+    assert P.ps_packed_weight_grad(C.byref(a), 256, 1 << 60, None) == P.PS_ERR_INVALID_ARG
