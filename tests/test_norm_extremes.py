@@ -50,6 +50,51 @@ def test_a_large_total_of_residual_and_input(cols):
     assert bool(((r.out.double() - out).abs() <= (SUM + 4) * EPS * out.abs() + 2.0 ** -8 * out.abs() * (1 + SUM * EPS) + 1e-40).all())
 
 
+# ---- gains off their alignment --------------------------------------------------------------------------------------------
+
+def gain_at(g, cols, dtype, shift):
+    return (torch.randn(cols + shift, generator=g) + 1).to(dtype).cuda()[shift:]
+
+
+@gpu
+@pytest.mark.parametrize("gain_dtype", [FP32, BF16])
+@pytest.mark.parametrize("shift", [1, 2, 3])
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 64), (40, 1024), (300, 2056), (3, 20000)])
+def test_norm_with_a_gain_off_its_alignment(dtype, rows, cols, shift, gain_dtype):
+    g = torch.Generator().manual_seed(rows + cols)
+    x, residual, dout, dtotal = (rows_of(g, rows, cols, dtype) for _ in range(4))
+    gain = gain_at(g, cols, gain_dtype, shift)
+    want = P.rms_norm(x, gain.clone(), residual, pack=True)
+    got = P.rms_norm(x, gain, residual, pack=True)
+    assert gain.data_ptr() % 16 and torch.equal(got.out, want.out) and torch.equal(got.packed.codes, want.packed.codes) and torch.equal(got.total, want.total)
+    n, rstd = P.unpack8(want.packed, FP32).double(), want.rstd.double()[:, None]
+    r = P.rms_norm_grad(dout, want.packed, want.rstd, gain, dtotal)
+    gd = dout.double() * gain.double()
+    dx = rstd * (gd - n * (gd * n).mean(1, keepdim=True)) + dtotal.double()
+    off = (SUM + 8) * EPS * (rstd * (gd.abs() + n.abs() * (gd * n).abs().mean(1, keepdim=True)) + dtotal.double().abs())
+    assert bool(((r.dx.double() - dx).abs() <= off + HALF[dtype] * dx.abs() + 1e-40).all())
+    terms = dout.double() * n
+    assert bool(((r.dgain.double() - terms.sum(0)).abs() <= (rows / 4 + SUM) * EPS * terms.abs().sum(0) + HALF[gain_dtype] * terms.sum(0).abs()).all())
+
+
+@gpu
+@pytest.mark.parametrize("gain_dtype", [FP32, BF16])
+@pytest.mark.parametrize("rows,outs,cols", [(200, 100, 304), (65, 257, 255), (4097, 300, 520), (3000, 64, 72), (3000, 257, 255), (70, 40, 1), (129, 2500, 1104)])
+def test_weight_gradient_with_a_gain_off_its_alignment(rows, outs, cols, gain_dtype):
+    g = torch.Generator().manual_seed(rows + cols)
+    dout, packed = rows_of(g, rows, outs, BF16), P.pack8(rows_of(g, rows, cols, FP32))
+    for shift in (1, 3):
+        gain = gain_at(g, cols, gain_dtype, shift)
+        assert gain.data_ptr() % 16
+        for dtype in (BF16, FP32):
+            assert torch.equal(P.packed_weight_grad(dout, packed, gain, dtype), P.packed_weight_grad(dout, packed, gain.clone(), dtype))
+        want = dout.double().T @ P.unpack8(packed, FP32).double() * gain.double()
+        off = (rows / 16 + 32) * 2.0 ** -23 * (dout.double().abs().T @ P.unpack8(packed, FP32).double().abs()) * gain.double().abs()
+        got = P.packed_weight_grad(dout, packed, gain, FP32)
+        assert bool(((got.double() - want).abs() <= off * (1 + EPS) + EPS * want.abs() + 1e-38).all())
+
+
 # ---- long sums of one sign ------------------------------------------------------------------------------------------------
 
 @gpu
