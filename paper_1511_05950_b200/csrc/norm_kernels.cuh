@@ -34,22 +34,9 @@ __device__ __forceinline__ float row_sum(float x, float (*part)[32], int slot)
     return x;
 }
 
-// The same in fp64, for a row whose squares fp32 cannot hold.
-template <int WARPS>
-__device__ __forceinline__ double row_sum64(double x, float (*part)[32])
-{
-    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kAllLanes, x, o);
-    if constexpr (WARPS > 1) {
-        double *sums = reinterpret_cast<double *>(part);
-        __syncthreads();                                   // the row's sum in fp32 has been read
-        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = x;
-        __syncthreads();
-        x = 0;
-        for (int w = 0; w < WARPS; ++w) x += sums[w];
-    }
-    return x;
-}
 // Whether a row's mean square plus eps, made in fp32, is what it should be: no square or sum overflowed, and what vanished below 2^-126 (at most 2^-150 of the mean) does not matter beside it.
+// Otherwise the squares are those of the values times a power of two: of large rows 2^-80 (of values up to 2^128, up to 2^28 of them; what vanishes is nothing beside one of 2^49 and more),
+// of small ones 2^100 (values below 2^-46, since their mean square is below 2^-120; the least subnormal's square is a normal number).
 __device__ __forceinline__ bool mean_square_fits(float m) { return m >= 7.52316385e-37f && m <= 3.40282347e38f; }              // 2^-120, the largest
 
 // ---- forward -----------------------------------------------------------------------------------------------------------
@@ -87,12 +74,15 @@ __device__ __forceinline__ void norm_outputs(const NormIn &in, long long row, in
 }
 
 // total = round(x + residual), r = 1 / sqrt(mean(total^2) + eps), n = total r; out = round(n gain), codes of n.  Rows whose squares overflow fp32 (values around 1e18 and more), or vanish in it beside an
-// eps that does too, are added up again in fp64: the row is there, and the test for it costs nothing (one comparison a row).
+// eps that does too, are added up again times a power of two: the row is there, and the test for it costs nothing (one comparison a row).
 // WARPS warps a row (one warp: a block has kNormRows rows), UNITS units a thread: the row stays in registers between its sum and its outputs, so
 // each byte crosses HBM once.  Bound by HBM: 16384 x 4096 bf16 with residual and both outputs moves 606 MB in 93 us (6.5 TB/s).
 constexpr int kNormRows = 4;
+// Blocks that an SM has registers for, where the compiler would take a few too many for them (bf16, 64 M elements: 16384 wide 130 us with one block and 96 with two, 512 wide 98 with eight and 95 with
+// nine); 0: as it likes.
+template <typename T, int WARPS, int UNITS> constexpr int kNormBlocks = sizeof(T) == 4 ? 0 : WARPS == 16 && UNITS == 4 ? 2 : WARPS == 1 && UNITS == 2 ? 9 : 0;
 template <typename T, int WARPS, int UNITS, bool ALIGNED>
-__global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_norm_kernel(const __grid_constant__ NormIn in)
+__global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS, kNormBlocks<T, WARPS, UNITS>) rms_norm_kernel(const __grid_constant__ NormIn in)
 {
     __shared__ __align__(16) float part[2][32];
     __shared__ WarpDesk<T> desk[ALIGNED ? 1 : WARPS == 1 ? kNormRows : WARPS];
@@ -138,12 +128,16 @@ __global__ void __launch_bounds__(WARPS == 1 ? 32 * kNormRows : 32 * WARPS) rms_
     const float m = sum / static_cast<float>(in.cols) + in.eps;
     float r = __frsqrt_rn(m);
     if (!mean_square_fits(m)) {                            // the same for the whole row
-        double wide = 0;
+        const float scale = m < 1.f ? 1.26765060e30f : 8.27180613e-25f;               // 2^100, 2^-80
+        sum = 0.f;
 #pragma unroll
         for (int j = 0; j < UNITS; ++j)
 #pragma unroll
-            for (int k = 0; k < kUnit; ++k) wide = fma(static_cast<double>(u[j].v[k]), static_cast<double>(u[j].v[k]), wide);
-        r = static_cast<float>(1.0 / sqrt(row_sum64<WARPS>(wide, part) / in.cols + in.eps));
+            for (int k = 0; k < kUnit; ++k) {
+                const float v = u[j].v[k] * scale;
+                sum = fmaf(v, v, sum);
+            }
+        r = __frsqrt_rn(row_sum<WARPS>(sum, part, 1) / static_cast<float>(in.cols) + in.eps * scale * scale) * scale;
     }
     if (tid == 0) in.rstd[row] = r;
 #pragma unroll
