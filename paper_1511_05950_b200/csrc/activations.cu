@@ -51,11 +51,12 @@ int over_rows(int64_t rows, int64_t cols, int64_t stride, bool aligned, F launch
     return PS_OK;
 }
 
-// Warps of a row and units (of eight elements) a thread.  As many units as a thread can hold where rows are many: a row costs each of its warps some hundred instructions. More warps where
-// rows are few and the row's latency counts.  us, bf16, residual, both outputs; 32 rows (in a graph) | 64 M elements:
-//     width 1024: 1 x 4 3.6 | 94.7, 4 x 1 1.9 | 100.9 (1 x 4 pulls ahead beyond 2368 rows)       2048: 4 x 2 2.5 | 92.5, 8 x 1 2.1 | 106.0 (592 rows: 3.1, 3.3)
-//     width 4096: 4 x 4 3.7 | 93.3, 8 x 2 2.7 | 94.9, 16 x 1 2.3 | 113.6 (296 rows: 4.1, 3.2, 3.4; 1184: 6.4, 6.9, 7.9)       8192: 8 x 4 4.1 | 94.7, 16 x 2 3.2 | 95.1 (296 rows: 4.9, 5.2)
-// fp32 at 8192: 16 x 2 at every number of rows (296: 6.7 against 10.1; 8192: 89.2, 91.3).  Rows of more than 16384 are read twice (16384: 201 us against 96).
+// Warps of a row and units (of eight elements) a thread.  As many units as a thread can hold where rows are many: a row costs each of its warps some hundred instructions.  More warps where
+// rows are few and the row's latency counts.  us, bf16, residual, both outputs; 32 rows in the L2 (in a graph; from HBM 0.2 to 0.4 more, in the same order) | 64 M elements:
+//     width 1024: 1 x 4 3.7 | 95.3, 4 x 1 2.0 | 101.7 (2368 rows: 5.5, 4.7)       2048: 4 x 2 2.5 | 92.4, 8 x 1 2.1 | 106.2 (296 rows: 2.8, 2.4; 592: 3.2, 3.4)
+//     width 4096: 4 x 4 3.8 | 93.3, 8 x 2 2.7 | 94.3, 16 x 1 2.4 | 114.3 (148 rows: 3.9, 2.8, 2.5; 296: 4.1, 3.2, 3.5; 592: 4.8, 4.6, 5.4; 1184: 6.5, 7.0, 8.2)
+//     width 8192: 8 x 4 4.0 | 93.9, 16 x 2 3.2 | 108.2 (148 rows: 4.2, 3.4; 296: 4.9, 4.2; 592: 6.4, 7.4)
+// fp32 at 8192: 16 x 2 at every number of rows (296: 6.8 against 10.5; 592: 12.9, 18.2; 8192, twice the bytes: 172, 173).  Rows of more than 16384 are read twice (32768: 197 us; 16384: 96).
 constexpr int64_t kSms = 148;
 template <typename T, bool ALIGNED>
 int launch_norm(const NormIn &in, cudaStream_t st)

@@ -257,6 +257,7 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: torch.T
 
 
 # ---- losses without logits ----------------------------------------------------------------------------------------------
+# Values only, here and below: autograd sees none of these calls but norm_linear; the others' gradients are calls of their own.
 
 class HeadLogprob(NamedTuple):
     logp: torch.Tensor
@@ -421,7 +422,8 @@ def norm_linear(x: torch.Tensor, gain: torch.Tensor, weight: torch.Tensor, resid
     """(z, total) with total = x + residual and z = (n * gain) @ weight.T (`rms_norm`, then a linear layer; all bf16, x and residual with
     any leading dimensions and strides; they stay bf16 under autocast), for autograd: between the passes it keeps n in 8 bits and a number a row, 1.03 bytes an element where the total and the product's
     input would take 4.  The gradients are those of the kept values; z and total are not touched by the 8 bits.  A backward pass is
-    captured into a CUDA graph as any other of torch's: with no eager graph of the same leaves alive."""
+    captured into a CUDA graph as any other of torch's: with no eager graph of the same leaves alive.  The two plain products (z, and the gradient of n * gain) are
+    torch's, under its settings for bf16 products."""
     for t, what in ((x, "x"), (weight, "weight"), *(((residual, "residual"),) if residual is not None else ())):
         if t.dtype != torch.bfloat16:
             raise TypeError("%s must be bf16, got %s" % (what, t.dtype))
