@@ -6,7 +6,7 @@
 namespace softsync {
 
 // Rows with a factor (weight or gradient) other than zero, in order: order[j] is the j-th of them, place[row] its number or -1, *live how many; their
-// sum (fp64: beyond fp32's range too), and the power of two that they are taken relative to, that of the largest finite one (2^-126 to 2^100: its product with 1 / T stays finite), so that entries of G are rounded
+// sum (fp64: beyond fp32's range too), and the power of two that they are taken relative to, that of the largest finite one (2^-126 to 2^100: its product with 1 / T stays finite for T of 2^-28 and more), so that entries of G are rounded
 // alike whatever all factors are multiplied by.  Rows without get zeros in up to two outputs.  One block; each thread takes a run of neighbouring rows a turn.
 constexpr int kOrderThreads = 1024, kOrderRun = 8;
 struct OrderOut {
